@@ -11,6 +11,9 @@
  *   3. ut_bsattn_fwd  -- block-sparse attention over the listed key blocks.
  *   4. ut_bsattn_bwd  -- its gradient (the paper trains stage 3 with it).
  *   5. ut_fg_scatter  -- put compacted rows back at their canvas positions.
+ * Next to it, the operators that condition such a model: cross attention to
+ * an encoder's states (ut_xattn_*) and group norm with an activation
+ * (ut_group_norm_*), forward and backward.
  *
  * Conventions shared by every entry point
  *   - Pointers are DEVICE pointers unless the parameter name starts with h_
@@ -331,6 +334,114 @@ ut_status ut_bsattn_bwd(const ut_attn_shape* shape, const void* q, const void* k
                         const int32_t* col_ptr_t, const int32_t* row_idx_t, float softmax_scale,
                         void* dq, void* dk, void* dv, void* ws, size_t ws_bytes,
                         int32_t* dev_status, void* stream);
+
+/* ------------------------------------------------------------------------
+ * Conditioning operators.  They work on packed rows: the rows of n_seg
+ * segments (samples or images) one after another, with the prefix of the
+ * segments' lengths cu[n_seg + 1] (int32, device; cu[0] = 0, ascending,
+ * cu[n_seg] = all rows; a segment may be empty).  cu = NULL with n_seg = 1 is
+ * one segment of all rows.  The lengths stay on the device: no entry point
+ * reads them on the host.  dev_status (may be NULL) receives
+ * UT_ERR_INVALID_ARG for a cu that is not such a prefix; its values are
+ * clamped, so the results are then wrong but nothing outside the tensors is
+ * read or written.
+ *
+ * Cross attention to an encoder's states of another length (a prompt's, a
+ * reference image's).  For every segment, query head h and its kv head
+ * h' = h / (n_heads / n_kv_heads), over the segment's keys j with
+ * key_mask[j] != 0:
+ *   O_i = softmax_j(softmax_scale * q_i . k_j) v_j
+ *   LSE_i = ln sum_j exp(softmax_scale * q_i . k_j)
+ * A query row without a key (an empty segment, or all keys masked) gets
+ * O = 0 and LSE = -inf.  Keys and values that are masked, and rows of other
+ * segments, never enter a product: whatever they hold (NaN, infinities) has
+ * no effect. */
+typedef struct {
+  int64_t n_q, n_k;       /* query rows, encoder rows (of all segments), >= 0 */
+  int32_t n_seg;          /* segments, >= 1 */
+  int32_t n_heads;        /* H: query heads */
+  int32_t n_kv_heads;     /* H_kv: divides n_heads; n_heads / n_kv_heads <= 64 */
+  int32_t head_dim;       /* d: 64 or 128 */
+  int32_t dtype;          /* ut_dtype of q, k, v, o and their gradients */
+  /* elements between consecutive rows: at least the row's heads * d (the
+   * heads of a row are contiguous), a multiple of 16 bytes.  K and V as slices of one
+   * projection's rows have a larger one.  The last four are read by the
+   * backward only. */
+  int64_t q_stride, k_stride, v_stride, o_stride;
+  int64_t do_stride, dq_stride, dk_stride, dv_stride;
+} ut_xattn_shape;
+
+/*   q, o         [n_q, H, d];  k, v  [n_k, H_kv, d]
+ *   cu_q, cu_k   [n_seg + 1], both or neither (NULL: n_seg = 1)
+ *   key_mask     [n_k] uint8, nonzero = attend; NULL = all
+ *   lse          [H, n_q] fp32
+ *   ws           ut_xattn_fwd_workspace_size(shape) bytes (may be 0: then
+ *                NULL is fine), 16-byte aligned: partial results where the
+ *                keys are split over CTAs because there are few query rows.
+ * bf16 accumulates in fp32 and rounds P to bf16 before P V and O to bf16;
+ * fp32 is fp32 throughout.  The result does not depend on the run. */
+size_t ut_xattn_fwd_workspace_size(const ut_xattn_shape* shape);
+ut_status ut_xattn_fwd(const ut_xattn_shape* shape, const void* q, const void* k, const void* v,
+                       const int32_t* cu_q, const int32_t* cu_k, const uint8_t* key_mask,
+                       float softmax_scale, void* o, float* lse, void* ws, size_t ws_bytes,
+                       int32_t* dev_status, void* stream);
+
+/* Gradient of ut_xattn_fwd given dO:
+ *   D_i = dO_i . O_i,  P = exp(S - LSE),  dS = P o (dO V^T - D),
+ *   dV = P^T dO,  dQ = softmax_scale dS K,  dK = softmax_scale dS^T Q,
+ * dK and dV summed over the query heads that share the kv head.  Rows of dK
+ * and dV of masked keys, and rows of dQ without a key, are zero.
+ *   o, lse      the forward's outputs;  dout  [n_q, H, d]
+ *   dq          [n_q, H, d];  dk, dv  [n_k, H_kv, d], fully overwritten
+ *   ws          ut_xattn_bwd_workspace_size(shape) bytes, 16-byte aligned. */
+size_t ut_xattn_bwd_workspace_size(const ut_xattn_shape* shape);
+ut_status ut_xattn_bwd(const ut_xattn_shape* shape, const void* q, const void* k, const void* v,
+                       const int32_t* cu_q, const int32_t* cu_k, const uint8_t* key_mask,
+                       float softmax_scale, const void* o, const float* lse, const void* dout,
+                       void* dq, void* dk, void* dv, void* ws, size_t ws_bytes,
+                       int32_t* dev_status, void* stream);
+
+/* Group norm with an activation, channels last.  For every segment s (rows of
+ * one image) and group g of channels / groups consecutive channels, over the
+ * group's M values of the segment:
+ *   mu = mean(x),  r = 1 / sqrt(mean((x - mu)^2) + eps)
+ *   u = gamma (x - mu) r + beta,  y = u (UT_ACT_NONE) or u / (1 + exp(-u))
+ * An empty segment has mu = 0, r = 1 / sqrt(eps). */
+enum { UT_ACT_NONE = 0, UT_ACT_SILU = 1 };
+typedef struct {
+  int64_t n_rows;         /* rows of all segments, >= 0 */
+  int32_t n_seg;          /* segments, >= 1 */
+  int32_t channels;       /* C <= 8192, C * element size a multiple of 16 bytes */
+  int32_t groups;         /* divides channels */
+  int32_t dtype;          /* ut_dtype of x, y, dy, dx */
+  int32_t act;            /* UT_ACT_NONE or UT_ACT_SILU */
+  float eps;              /* > 0 */
+  /* elements between consecutive rows, >= channels, a multiple of 16 bytes;
+   * the last two are read by the backward only */
+  int64_t x_stride, y_stride, dy_stride, dx_stride;
+} ut_gnorm_shape;
+
+/*   x, y          [n_rows, C]; may not overlap
+ *   cu            [n_seg + 1] or NULL (n_seg = 1)
+ *   gamma, beta   [C] fp32, or NULL (1 and 0)
+ *   mean, rstd    [n_seg, groups] fp32 outputs (mu and r, for the backward)
+ *   ws            ut_group_norm_fwd_workspace_size(shape) bytes, 16-byte aligned
+ * Statistics and the arithmetic are fp32; y is rounded once.  The result does
+ * not depend on the run. */
+size_t ut_group_norm_fwd_workspace_size(const ut_gnorm_shape* shape);
+ut_status ut_group_norm_fwd(const ut_gnorm_shape* shape, const void* x, const int32_t* cu,
+                            const float* gamma, const float* beta, void* y, float* mean, float* rstd,
+                            void* ws, size_t ws_bytes, int32_t* dev_status, void* stream);
+
+/* Gradient of ut_group_norm_fwd given dy; mean and rstd are the forward's.
+ *   dx             [n_rows, C]; may not overlap x or dy
+ *   dgamma, dbeta  [C] fp32 (summed over the segments), or NULL
+ *   ws             ut_group_norm_bwd_workspace_size(shape) bytes, 16-byte aligned */
+size_t ut_group_norm_bwd_workspace_size(const ut_gnorm_shape* shape);
+ut_status ut_group_norm_bwd(const ut_gnorm_shape* shape, const void* x, const void* dy, const int32_t* cu,
+                            const float* gamma, const float* beta, const float* mean, const float* rstd,
+                            void* dx, float* dgamma, float* dbeta, void* ws, size_t ws_bytes,
+                            int32_t* dev_status, void* stream);
 
 #ifdef __cplusplus
 }

@@ -12,7 +12,7 @@
 
 namespace ut {
 
-static int device_sms() {
+int device_sms() {
   int dev = 0, sms = 0;
   if (cudaGetDevice(&dev) != cudaSuccess) return 1;
   if (cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return 1;
@@ -58,7 +58,7 @@ static ut_status from_cuda(cudaError_t e) { return e == cudaSuccess ? UT_OK : UT
 // Limit of every bounded device wait: 2 s, or UT_WAIT_TIMEOUT_NS from the
 // environment (read at each call; 0 = give up at the first wait that is not
 // already satisfied, which the failure-detection tests use).
-static uint64_t wait_timeout_ns() {
+uint64_t wait_timeout_ns() {
   const char* e = getenv("UT_WAIT_TIMEOUT_NS");
   if (e && *e) {
     char* end = nullptr;

@@ -81,7 +81,9 @@ cudaError_t launch_attn_bwd_tc(const AttnProblem& p, const void* q, const void* 
                                const int32_t* col_ptr_t, const int32_t* row_idx_t, void* dq, void* dk, void* dv,
                                void* ws, int32_t* status, uint64_t timeout_ns, int sms, cudaStream_t stream);
 
-// tensor maps (api.cu)
+// api.cu
+int device_sms();            // SMs of the current device (1 without one)
+uint64_t wait_timeout_ns();  // limit of every bounded device wait
 bool encode_tmap_2d_bf16(CUtensorMap* map, const void* base, uint64_t inner_elems, uint64_t rows,
                          uint64_t row_stride_bytes, uint32_t box_inner, uint32_t box_rows);
 

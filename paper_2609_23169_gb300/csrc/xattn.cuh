@@ -1,0 +1,39 @@
+// Parameters of the cross-attention kernels and the launchers of their forms.
+#pragma once
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+namespace ut {
+
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.69314718055994531f;
+
+struct XattnParams {
+  const void* q; const void* k; const void* v;
+  void* o; float* lse;                   // outputs of the forward, inputs of the backward
+  const void* dout; void* dq; void* dk; void* dv;
+  const int32_t* cu_q; const int32_t* cu_k; const uint8_t* mask;
+  int32_t* status;
+  int64_t nq, nk;
+  int B, H, Hk, G, d;                    // segments, query heads, kv heads, H / Hk, head dimension
+  int64_t qs, ks, vs, os, dos, dqs, dks, dvs;  // elements between rows
+  float scale;
+  uint64_t timeout_ns;
+  int sms;
+  // Work split over the long axis: keys in the forward (part_o [nsplit, nq,
+  // H, d] unnormalised, part_ml [nsplit, nq, H] the running maximum in the
+  // base-2 domain and the sum), query rows in the backward (part_dk, part_dv
+  // [nsplit, nk, Hk, d]).
+  int nsplit;
+  float* part_o; float2* part_ml;
+  float* dsum;                           // [H, nq] D = dO . O
+  float* part_dk; float* part_dv;
+};
+
+// Work items of a pass without splits, and how many parts its long axis is
+// split into.
+int64_t xattn_items(const XattnParams& p, bool bf16, bool backward);
+int xattn_splits(const XattnParams& p, bool bf16, bool backward);
+cudaError_t launch_xattn_fwd_simt(const XattnParams& p, bool bf16, cudaStream_t s);
+cudaError_t launch_xattn_bwd_simt(const XattnParams& p, bool bf16, cudaStream_t s);
+
+}  // namespace ut

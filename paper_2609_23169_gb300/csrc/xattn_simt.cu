@@ -1,0 +1,559 @@
+// Cross attention to an encoder's states on the CUDA cores, in fp32 arithmetic.
+//
+// Per segment s, query head h and its kv head h' = h / G (G = H / H_kv):
+//   O_i = softmax_j(scale q_i . k_j) v_j,   LSE_i = ln sum_j exp(scale q_i . k_j)
+//   D_i = dO_i . O_i,  P = exp(S - LSE),  dS = P o (dO V^T - D)
+//   dQ = scale dS K,  dK = scale sum dS^T Q,  dV = sum P^T dO
+// over the segment's keys whose mask is set.
+//
+// A tile holds 64 rows: the G heads that share a kv head of 64 / G
+// consecutive tokens (row = token * G + head), so that K and V are read once
+// for the group and dK, dV sum over its heads inside the tile products.  256
+// threads as 16 x 16; a thread computes 4 x 4 of a 64 x 64 product (4 rows,
+// columns tx + 16 j) and 4 x D/16 of a 64 x D product; all operands are
+// row-major in shared memory with 4 floats of padding (16-byte reads without
+// bank conflicts).  Rows and keys that do not exist or are masked are staged
+// as zeros, so that whatever their memory holds never enters a product.
+#include <math.h>
+
+#include "common.cuh"
+#include "kernels.h"
+#include "segments.cuh"
+#include "xattn.cuh"
+
+namespace ut {
+
+constexpr int kXs = 64;        // rows and keys of a tile
+constexpr int kXsThreads = 256;
+constexpr int kXsLdP = kXs + 4;
+
+UT_DEV float4 ld4(const float* p) { return *reinterpret_cast<const float4*>(p); }
+UT_DEV float4 ld4(const __nv_bfloat16* p) {
+  const uint2 u = *reinterpret_cast<const uint2*>(p);
+  return make_float4(__uint_as_float(u.x << 16), __uint_as_float(u.x & 0xFFFF0000u), __uint_as_float(u.y << 16),
+                     __uint_as_float(u.y & 0xFFFF0000u));
+}
+UT_DEV void st4(float* p, float4 v) { *reinterpret_cast<float4*>(p) = v; }
+UT_DEV void st4(__nv_bfloat16* p, float4 v) {
+  *reinterpret_cast<uint2*>(p) = make_uint2(pack_bf16x2(v.x, v.y), pack_bf16x2(v.z, v.w));
+}
+
+struct XsTile {  // the query rows of a tile
+  int64_t tok0;  // first token
+  int rows;      // valid rows
+  int head0;     // first query head
+  int G;
+  UT_DEV int64_t off(int r, int64_t stride, int d) const {
+    return (tok0 + r / G) * stride + (int64_t)(head0 + r % G) * d;
+  }
+};
+
+// dst[64][D + 4] <- the tile's rows of x (zeros past the valid ones)
+template <typename T, int D>
+UT_DEV void stage_q(float* dst, const void* x, const XsTile& t, int64_t stride) {
+  for (int e = threadIdx.x; e < kXs * (D / 4); e += kXsThreads) {
+    const int r = e / (D / 4), c = (e % (D / 4)) * 4;
+    const float4 v = r < t.rows ? ld4(static_cast<const T*>(x) + t.off(r, stride, D) + c) : make_float4(0, 0, 0, 0);
+    st4(dst + r * (D + 4) + c, v);
+  }
+}
+// dst[64][D + 4] <- keys key0 .. of kv head hk (zeros where `on` is 0)
+template <typename T, int D>
+UT_DEV void stage_k(float* dst, const void* x, int64_t key0, const float* on, int hk, int64_t stride) {
+  for (int e = threadIdx.x; e < kXs * (D / 4); e += kXsThreads) {
+    const int r = e / (D / 4), c = (e % (D / 4)) * 4;
+    const float4 v = on[r] != 0.f ? ld4(static_cast<const T*>(x) + (key0 + r) * stride + (int64_t)hk * D + c)
+                                  : make_float4(0, 0, 0, 0);
+    st4(dst + r * (D + 4) + c, v);
+  }
+}
+// on[64] <- 1 where the key exists and is not masked
+UT_DEV void stage_mask(float* on, const uint8_t* mask, int64_t key0, int64_t left) {
+  if (threadIdx.x < kXs) {
+    const int r = threadIdx.x;
+    on[r] = r < left && (!mask || mask[key0 + r]) ? 1.f : 0.f;
+  }
+}
+
+// acc[i][j] = a[ty * 4 + i] . b[tx + 16 j]
+template <int D>
+UT_DEV void product_nt(const float* a, const float* b, float (&acc)[4][4]) {
+  const int ty = threadIdx.x >> 4, tx = threadIdx.x & 15;
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) acc[i][j] = 0.f;
+#pragma unroll 4
+  for (int e = 0; e < D; e += 4) {
+    float4 x[4], y[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = ld4(a + (ty * 4 + i) * (D + 4) + e);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) y[j] = ld4(b + (tx + 16 * j) * (D + 4) + e);
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        acc[i][j] = fmaf(x[i].x, y[j].x, acc[i][j]);
+        acc[i][j] = fmaf(x[i].y, y[j].y, acc[i][j]);
+        acc[i][j] = fmaf(x[i].z, y[j].z, acc[i][j]);
+        acc[i][j] = fmaf(x[i].w, y[j].w, acc[i][j]);
+      }
+  }
+}
+// acc[i][c] += sum_k p[ty * 4 + i][k] b[k][tx * 4 + ...]
+template <int D>
+UT_DEV void product_nn(const float* p, const float* b, float4 (&acc)[4][D / 64]) {
+  const int ty = threadIdx.x >> 4, tx = threadIdx.x & 15;
+#pragma unroll 4
+  for (int k = 0; k < kXs; k += 4) {
+    float w[4][4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) *reinterpret_cast<float4*>(w[i]) = ld4(p + (ty * 4 + i) * kXsLdP + k);
+#pragma unroll
+    for (int kk = 0; kk < 4; ++kk)
+#pragma unroll
+      for (int c = 0; c < D / 64; ++c) {
+        const float4 v = ld4(b + (k + kk) * (D + 4) + tx * 4 + 64 * c);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          acc[i][c].x = fmaf(w[i][kk], v.x, acc[i][c].x);
+          acc[i][c].y = fmaf(w[i][kk], v.y, acc[i][c].y);
+          acc[i][c].z = fmaf(w[i][kk], v.z, acc[i][c].z);
+          acc[i][c].w = fmaf(w[i][kk], v.w, acc[i][c].w);
+        }
+      }
+  }
+}
+// acc[i][c] += sum_r p[r][ty * 4 + i] b[r][tx * 4 + ...]
+template <int D>
+UT_DEV void product_tn(const float* p, const float* b, float4 (&acc)[4][D / 64]) {
+  const int ty = threadIdx.x >> 4, tx = threadIdx.x & 15;
+#pragma unroll 4
+  for (int r = 0; r < kXs; ++r) {
+    float w[4];
+    *reinterpret_cast<float4*>(w) = ld4(p + r * kXsLdP + ty * 4);
+#pragma unroll
+    for (int c = 0; c < D / 64; ++c) {
+      const float4 v = ld4(b + r * (D + 4) + tx * 4 + 64 * c);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        acc[i][c].x = fmaf(w[i], v.x, acc[i][c].x);
+        acc[i][c].y = fmaf(w[i], v.y, acc[i][c].y);
+        acc[i][c].z = fmaf(w[i], v.z, acc[i][c].z);
+        acc[i][c].w = fmaf(w[i], v.w, acc[i][c].w);
+      }
+    }
+  }
+}
+
+UT_DEV float half_warp_max(float x) {
+#pragma unroll
+  for (int o = 8; o; o >>= 1) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, o));
+  return x;
+}
+UT_DEV float half_warp_sum(float x) {
+#pragma unroll
+  for (int o = 8; o; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
+  return x;
+}
+
+// grid (q slots, kv heads, key splits)
+template <typename T, int D>
+__global__ void __launch_bounds__(kXsThreads) xattn_fwd_simt_kernel(const XattnParams p) {
+  extern __shared__ float sm[];
+  float* qs = sm;
+  float* ks = qs + kXs * (D + 4);
+  float* vs = ks + kXs * (D + 4);
+  float* ps = vs + kXs * (D + 4);
+  float* on = ps + kXs * kXsLdP;
+  if (blockIdx.x == 0 && blockIdx.y == 0 && blockIdx.z == 0) {
+    check_cu(p.cu_q, p.B, p.nq, p.status);
+    check_cu(p.cu_k, p.B, p.nk, p.status);
+  }
+  const int tpt = kXs / p.G;
+  const Segment g = segment_of_slot(p.cu_q, p.B, p.nq, tpt, blockIdx.x);
+  if (g.tile * tpt >= g.n) return;
+  const int hk = blockIdx.y, split = blockIdx.z;
+  XsTile t{g.row + g.tile * tpt, (int)min((int64_t)tpt, g.n - g.tile * tpt) * p.G, hk * p.G, p.G};
+  int64_t k0, kn;
+  segment_rows(p.cu_k, g.s, p.nk, k0, kn);
+  const int64_t nblk = (kn + kXs - 1) / kXs, per = (nblk + p.nsplit - 1) / p.nsplit;
+  const int64_t b0 = per * split, b1 = min(nblk, b0 + per);
+  const int ty = threadIdx.x >> 4, tx = threadIdx.x & 15;
+  stage_q<T, D>(qs, p.q, t, p.qs);
+  float m[4], l[4];
+  float4 o[4][D / 64];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    m[i] = -INFINITY;
+    l[i] = 0.f;
+#pragma unroll
+    for (int c = 0; c < D / 64; ++c) o[i][c] = make_float4(0, 0, 0, 0);
+  }
+  for (int64_t b = b0; b < b1; ++b) {
+    __syncthreads();
+    stage_mask(on, p.mask, k0 + b * kXs, kn - b * kXs);
+    __syncthreads();
+    stage_k<T, D>(ks, p.k, k0 + b * kXs, on, hk, p.ks);
+    stage_k<T, D>(vs, p.v, k0 + b * kXs, on, hk, p.vs);
+    __syncthreads();
+    float s[4][4];
+    product_nt<D>(qs, ks, s);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      float mx = -INFINITY;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        s[i][j] = on[tx + 16 * j] != 0.f ? s[i][j] * p.scale : -INFINITY;
+        mx = fmaxf(mx, s[i][j]);
+      }
+      mx = fmaxf(m[i], half_warp_max(mx));
+      const float ref = mx == -INFINITY ? 0.f : mx;  // a row that saw no key yet
+      const float alpha = expf(m[i] - ref);
+      float sum = 0.f;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const float e = expf(s[i][j] - ref);
+        sum += e;
+        ps[(ty * 4 + i) * kXsLdP + tx + 16 * j] = e;
+      }
+      l[i] = l[i] * alpha + half_warp_sum(sum);
+      m[i] = mx;
+#pragma unroll
+      for (int c = 0; c < D / 64; ++c) {
+        o[i][c].x *= alpha;
+        o[i][c].y *= alpha;
+        o[i][c].z *= alpha;
+        o[i][c].w *= alpha;
+      }
+    }
+    __syncthreads();
+    product_nn<D>(ps, vs, o);
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int r = ty * 4 + i;
+    if (r >= t.rows) continue;
+    const int64_t tok = t.tok0 + r / p.G;
+    const int h = t.head0 + r % p.G;
+    if (p.nsplit == 1) {
+      const float inv = l[i] > 0.f ? 1.f / l[i] : (l[i] == 0.f ? 0.f : l[i]);
+#pragma unroll
+      for (int c = 0; c < D / 64; ++c)
+        st4(static_cast<T*>(p.o) + t.off(r, p.os, D) + tx * 4 + 64 * c,
+            make_float4(o[i][c].x * inv, o[i][c].y * inv, o[i][c].z * inv, o[i][c].w * inv));
+      if (tx == 0) p.lse[(int64_t)h * p.nq + tok] = m[i] + logf(l[i]);
+    } else {
+      const int64_t row = ((int64_t)split * p.nq + tok) * p.H + h;
+#pragma unroll
+      for (int c = 0; c < D / 64; ++c) st4(p.part_o + row * D + tx * 4 + 64 * c, o[i][c]);
+      if (tx == 0) p.part_ml[row] = make_float2(m[i] * kLog2e, l[i]);
+    }
+  }
+}
+
+// P and dS of one 64 x 64 pair of tiles; s, dp are its products
+UT_DEV void probabilities(const XattnParams& p, const float* on, const float* lse, const float* dsum, float (&s)[4][4],
+                          float (&dp)[4][4]) {
+  const int ty = threadIdx.x >> 4, tx = threadIdx.x & 15;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const float le = lse[ty * 4 + i], ds = dsum[ty * 4 + i];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      s[i][j] = on[tx + 16 * j] != 0.f && le != -INFINITY ? expf(s[i][j] * p.scale - le) : 0.f;
+      dp[i][j] = s[i][j] * (dp[i][j] - ds);
+    }
+  }
+}
+
+// lse / D of the tile's rows (rows that do not exist: LSE = -inf, P = 0)
+UT_DEV void stage_rows(float* lse, float* dsum, const XattnParams& p, const XsTile& t) {
+  if (threadIdx.x < kXs) {
+    const int r = threadIdx.x;
+    const int64_t at = (int64_t)(t.head0 + r % p.G) * p.nq + t.tok0 + r / p.G;
+    lse[r] = r < t.rows ? p.lse[at] : -INFINITY;
+    dsum[r] = r < t.rows ? p.dsum[at] : 0.f;
+  }
+}
+
+// grid (q slots, kv heads): dQ of a tile over the segment's keys
+template <typename T, int D>
+__global__ void __launch_bounds__(kXsThreads) xattn_dq_simt_kernel(const XattnParams p) {
+  extern __shared__ float sm[];
+  float* qs = sm;
+  float* dos = qs + kXs * (D + 4);
+  float* ks = dos + kXs * (D + 4);
+  float* vs = ks + kXs * (D + 4);
+  float* dss = vs + kXs * (D + 4);
+  float* on = dss + kXs * kXsLdP;
+  float* lse = on + kXs;
+  float* dsum = lse + kXs;
+  const int tpt = kXs / p.G;
+  const Segment g = segment_of_slot(p.cu_q, p.B, p.nq, tpt, blockIdx.x);
+  if (g.tile * tpt >= g.n) return;
+  const int hk = blockIdx.y;
+  XsTile t{g.row + g.tile * tpt, (int)min((int64_t)tpt, g.n - g.tile * tpt) * p.G, hk * p.G, p.G};
+  int64_t k0, kn;
+  segment_rows(p.cu_k, g.s, p.nk, k0, kn);
+  const int ty = threadIdx.x >> 4, tx = threadIdx.x & 15;
+  stage_q<T, D>(qs, p.q, t, p.qs);
+  stage_q<T, D>(dos, p.dout, t, p.dos);
+  stage_rows(lse, dsum, p, t);
+  float4 acc[4][D / 64];
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+#pragma unroll
+    for (int c = 0; c < D / 64; ++c) acc[i][c] = make_float4(0, 0, 0, 0);
+  for (int64_t b = 0; b * kXs < kn; ++b) {
+    __syncthreads();
+    stage_mask(on, p.mask, k0 + b * kXs, kn - b * kXs);
+    __syncthreads();
+    stage_k<T, D>(ks, p.k, k0 + b * kXs, on, hk, p.ks);
+    stage_k<T, D>(vs, p.v, k0 + b * kXs, on, hk, p.vs);
+    __syncthreads();
+    float s[4][4], dp[4][4];
+    product_nt<D>(qs, ks, s);
+    product_nt<D>(dos, vs, dp);
+    probabilities(p, on, lse, dsum, s, dp);
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) dss[(ty * 4 + i) * kXsLdP + tx + 16 * j] = dp[i][j];
+    __syncthreads();
+    product_nn<D>(dss, ks, acc);
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int r = ty * 4 + i;
+    if (r >= t.rows) continue;
+#pragma unroll
+    for (int c = 0; c < D / 64; ++c)
+      st4(static_cast<T*>(p.dq) + t.off(r, p.dqs, D) + tx * 4 + 64 * c,
+          make_float4(acc[i][c].x * p.scale, acc[i][c].y * p.scale, acc[i][c].z * p.scale, acc[i][c].w * p.scale));
+  }
+}
+
+// grid (k slots, kv heads, query splits): partial dK, dV of a key tile over a
+// range of the segment's query tiles
+template <typename T, int D>
+__global__ void __launch_bounds__(kXsThreads) xattn_dkdv_simt_kernel(const XattnParams p) {
+  extern __shared__ float sm[];
+  float* qs = sm;
+  float* dos = qs + kXs * (D + 4);
+  float* ks = dos + kXs * (D + 4);
+  float* vs = ks + kXs * (D + 4);
+  float* ps = vs + kXs * (D + 4);
+  float* dss = ps + kXs * kXsLdP;
+  float* on = dss + kXs * kXsLdP;
+  float* lse = on + kXs;
+  float* dsum = lse + kXs;
+  const Segment g = segment_of_slot(p.cu_k, p.B, p.nk, kXs, blockIdx.x);
+  if (g.tile * kXs >= g.n) return;
+  const int hk = blockIdx.y, split = blockIdx.z;
+  const int64_t key0 = g.row + g.tile * kXs, left = g.n - g.tile * kXs;
+  int64_t q0, qn;
+  segment_rows(p.cu_q, g.s, p.nq, q0, qn);
+  const int tpt = kXs / p.G;
+  const int64_t nt = (qn + tpt - 1) / tpt, per = (nt + p.nsplit - 1) / p.nsplit;
+  const int64_t t0 = per * split, t1 = min(nt, t0 + per);
+  const int ty = threadIdx.x >> 4, tx = threadIdx.x & 15;
+  stage_mask(on, p.mask, key0, left);
+  __syncthreads();
+  stage_k<T, D>(ks, p.k, key0, on, hk, p.ks);
+  stage_k<T, D>(vs, p.v, key0, on, hk, p.vs);
+  float4 dk[4][D / 64], dv[4][D / 64];
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+#pragma unroll
+    for (int c = 0; c < D / 64; ++c) dk[i][c] = dv[i][c] = make_float4(0, 0, 0, 0);
+  for (int64_t tt = t0; tt < t1; ++tt) {
+    XsTile t{q0 + tt * tpt, (int)min((int64_t)tpt, qn - tt * tpt) * p.G, hk * p.G, p.G};
+    __syncthreads();
+    stage_q<T, D>(qs, p.q, t, p.qs);
+    stage_q<T, D>(dos, p.dout, t, p.dos);
+    stage_rows(lse, dsum, p, t);
+    __syncthreads();
+    float s[4][4], dp[4][4];
+    product_nt<D>(qs, ks, s);
+    product_nt<D>(dos, vs, dp);
+    probabilities(p, on, lse, dsum, s, dp);
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        ps[(ty * 4 + i) * kXsLdP + tx + 16 * j] = s[i][j];
+        dss[(ty * 4 + i) * kXsLdP + tx + 16 * j] = dp[i][j];
+      }
+    __syncthreads();
+    product_tn<D>(ps, dos, dv);
+    product_tn<D>(dss, qs, dk);
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int r = ty * 4 + i;
+    if (r >= left) continue;
+    const int64_t row = ((int64_t)split * p.nk + key0 + r) * p.Hk + hk;
+#pragma unroll
+    for (int c = 0; c < D / 64; ++c) {
+      st4(p.part_dk + row * D + tx * 4 + 64 * c, dk[i][c]);
+      st4(p.part_dv + row * D + tx * 4 + 64 * c, dv[i][c]);
+    }
+  }
+}
+
+// D_i = dO_i . O_i -> [H, nq]; half a warp a row and head
+template <typename T, int D>
+__global__ void __launch_bounds__(256) xattn_dsum_kernel(const XattnParams p) {
+  const int64_t x = ((int64_t)blockIdx.x * blockDim.x + threadIdx.x) >> 4;
+  const int lane = threadIdx.x & 15;
+  if (blockIdx.x == 0) {
+    check_cu(p.cu_q, p.B, p.nq, p.status);
+    check_cu(p.cu_k, p.B, p.nk, p.status);
+  }
+  float s = 0.f;
+  const int64_t tok = x / p.H;
+  const int h = (int)(x % p.H);
+  if (tok < p.nq) {
+    const T* o = static_cast<const T*>(p.o) + tok * p.os + (int64_t)h * D;
+    const T* d = static_cast<const T*>(p.dout) + tok * p.dos + (int64_t)h * D;
+#pragma unroll
+    for (int c = 0; c < D / 64; ++c) {
+      const float4 a = ld4(o + lane * 4 + 64 * c), b = ld4(d + lane * 4 + 64 * c);
+      s = fmaf(a.x, b.x, fmaf(a.y, b.y, fmaf(a.z, b.z, fmaf(a.w, b.w, s))));
+    }
+  }
+  s = half_warp_sum(s);
+  if (tok < p.nq && lane == 0) p.dsum[(int64_t)h * p.nq + tok] = s;
+}
+
+// dK, dV = the sum of the splits' partials, in split order; 4 values a thread
+template <typename T>
+__global__ void __launch_bounds__(256) xattn_dkdv_join_kernel(const XattnParams p) {
+  const int64_t x = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;
+  const int per_row = p.Hk * p.d / 4;
+  const int64_t n = p.nk * per_row;
+  if (x >= n) return;
+  const int64_t key = x / per_row;
+  const int e = (int)(x % per_row) * 4;
+#pragma unroll
+  for (int which = 0; which < 2; ++which) {
+    const float* src = (which ? p.part_dv : p.part_dk) + x * 4;
+    float4 a = make_float4(0, 0, 0, 0);
+    for (int s = 0; s < p.nsplit; ++s) {
+      const float4 b = ld4(src + (int64_t)s * n * 4);
+      a.x += b.x;
+      a.y += b.y;
+      a.z += b.z;
+      a.w += b.w;
+    }
+    const float f = which ? 1.f : p.scale;
+    st4(static_cast<T*>(which ? p.dv : p.dk) + key * (which ? p.dvs : p.dks) + e,
+        make_float4(a.x * f, a.y * f, a.z * f, a.w * f));
+  }
+}
+
+// O, LSE from the key splits' partials; half a warp a token and head
+template <typename T, int D>
+__global__ void __launch_bounds__(256) xattn_join_kernel(const XattnParams p) {
+  const int64_t x = ((int64_t)blockIdx.x * blockDim.x + threadIdx.x) >> 4;
+  const int lane = threadIdx.x & 15;
+  const int64_t rows = p.nq * p.H;
+  if (x >= rows) return;
+  float m = -INFINITY;
+  for (int s = 0; s < p.nsplit; ++s) m = fmaxf(m, p.part_ml[s * rows + x].x);
+  const float ref = m == -INFINITY ? 0.f : m;
+  float l = 0.f;
+  float4 o[D / 64];
+#pragma unroll
+  for (int c = 0; c < D / 64; ++c) o[c] = make_float4(0, 0, 0, 0);
+  for (int s = 0; s < p.nsplit; ++s) {
+    const float2 ml = p.part_ml[s * rows + x];
+    const float w = exp2f(ml.x - ref);
+    l = fmaf(ml.y, w, l);
+#pragma unroll
+    for (int c = 0; c < D / 64; ++c) {
+      const float4 v = ld4(p.part_o + (s * rows + x) * D + lane * 4 + 64 * c);
+      o[c].x = fmaf(v.x, w, o[c].x);
+      o[c].y = fmaf(v.y, w, o[c].y);
+      o[c].z = fmaf(v.z, w, o[c].z);
+      o[c].w = fmaf(v.w, w, o[c].w);
+    }
+  }
+  const int64_t tok = x / p.H;
+  const int h = (int)(x % p.H);
+  const float inv = l > 0.f ? 1.f / l : (l == 0.f ? 0.f : l);
+#pragma unroll
+  for (int c = 0; c < D / 64; ++c)
+    st4(static_cast<T*>(p.o) + tok * p.os + (int64_t)h * D + lane * 4 + 64 * c,
+        make_float4(o[c].x * inv, o[c].y * inv, o[c].z * inv, o[c].w * inv));
+  if (lane == 0) p.lse[(int64_t)h * p.nq + tok] = (m + log2f(l)) * kLn2;
+}
+
+// ----------------------------------------------------------------- launchers
+template <typename F>
+static cudaError_t launch(F kern, dim3 grid, size_t smem, const XattnParams& p, cudaStream_t s) {
+  cudaError_t e = cudaSuccess;
+  if (smem > 48 * 1024) e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+  if (e != cudaSuccess) return e;
+  kern<<<grid, kXsThreads, smem, s>>>(p);
+  return cudaGetLastError();
+}
+
+template <typename T, int D>
+static cudaError_t fwd(const XattnParams& p, cudaStream_t s) {
+  const size_t smem = sizeof(float) * (3 * kXs * (D + 4) + kXs * kXsLdP + kXs);
+  const dim3 grid((unsigned)segment_slots(p.nq, p.B, kXs / p.G), p.Hk, p.nsplit);
+  cudaError_t e = launch(xattn_fwd_simt_kernel<T, D>, grid, smem, p, s);
+  if (e != cudaSuccess || p.nsplit == 1) return e;
+  return launch(xattn_join_kernel<T, D>, dim3((unsigned)((p.nq * p.H + 15) / 16)), 0, p, s);
+}
+
+template <typename T, int D>
+static cudaError_t bwd(const XattnParams& p, cudaStream_t s) {
+  cudaError_t e = cudaSuccess;
+  const size_t tiles = sizeof(float) * 4 * kXs * (D + 4), pair = sizeof(float) * kXs * kXsLdP,
+               vecs = sizeof(float) * 3 * kXs;
+  e = launch(xattn_dsum_kernel<T, D>, dim3((unsigned)((p.nq * p.H + 16) / 16)), 0, p, s);
+  if (e != cudaSuccess) return e;
+  if (p.nq > 0) {
+    e = launch(xattn_dq_simt_kernel<T, D>, dim3((unsigned)segment_slots(p.nq, p.B, kXs / p.G), p.Hk),
+               tiles + pair + vecs, p, s);
+    if (e != cudaSuccess) return e;
+  }
+  if (p.nk > 0) {
+    e = launch(xattn_dkdv_simt_kernel<T, D>, dim3((unsigned)segment_slots(p.nk, p.B, kXs), p.Hk, p.nsplit),
+               tiles + 2 * pair + vecs, p, s);
+    if (e != cudaSuccess) return e;
+    e = launch(xattn_dkdv_join_kernel<T>, dim3((unsigned)((p.nk * p.Hk * D / 4 + 255) / 256)), 0, p, s);
+  }
+  return e;
+}
+
+int64_t xattn_items(const XattnParams& p, bool bf16, bool backward) {
+  (void)bf16;
+  return backward ? segment_slots(p.nk, p.B, kXs) * p.Hk : segment_slots(p.nq, p.B, kXs / p.G) * p.Hk;
+}
+
+// Enough parts for two blocks an SM, but none shorter than two tiles of an
+// average segment.
+int xattn_splits(const XattnParams& p, bool bf16, bool backward) {
+  const int64_t items = xattn_items(p, bf16, backward), want = (2 * (int64_t)p.sms + items - 1) / items;
+  const int64_t tile = backward ? kXs / p.G : kXs, tiles = ((backward ? p.nq : p.nk) / p.B + tile - 1) / tile;
+  const int64_t most = tiles / 2;
+  const int64_t n = want < most ? want : most;
+  return (int)(n < 1 ? 1 : n > 1024 ? 1024 : n);
+}
+
+cudaError_t launch_xattn_fwd_simt(const XattnParams& p, bool bf16, cudaStream_t s) {
+  if (bf16) return p.d == 64 ? fwd<__nv_bfloat16, 64>(p, s) : fwd<__nv_bfloat16, 128>(p, s);
+  return p.d == 64 ? fwd<float, 64>(p, s) : fwd<float, 128>(p, s);
+}
+
+cudaError_t launch_xattn_bwd_simt(const XattnParams& p, bool bf16, cudaStream_t s) {
+  if (bf16) return p.d == 64 ? bwd<__nv_bfloat16, 64>(p, s) : bwd<__nv_bfloat16, 128>(p, s);
+  return p.d == 64 ? bwd<float, 64>(p, s) : bwd<float, 128>(p, s);
+}
+
+}  // namespace ut

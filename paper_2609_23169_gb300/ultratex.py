@@ -20,12 +20,15 @@ UT_OK, UT_ERR_INVALID_ARG, UT_ERR_UNSUPPORTED, UT_ERR_CUDA, UT_ERR_TIMEOUT, UT_E
 UT_BF16, UT_F32 = 0, 1
 UT_BG_KEEP, UT_BG_ZERO, UT_BG_FILL = 0, 1, 2
 UT_MASK_TOPK, UT_MASK_BITMAP = 0, 1
+UT_ACT_NONE, UT_ACT_SILU = 0, 1
 
 EXPORTS = (
     "ut_strerror", "ut_topk_count", "ut_fg_compact_workspace_size", "ut_fg_compact", "ut_fg_scatter",
     "ut_block_mask_workspace_size", "ut_block_mask", "ut_bsattn_fwd", "ut_bsattn_bwd_workspace_size",
     "ut_bsattn_bwd", "ut_fg_compact_noalloc", "ut_fg_euler_update", "ut_fg_euler_update_gather", "ut_fg_composite",
     "ut_fg_gather_rope", "ut_fg_scatter_rope", "ut_fg_mask_from_alpha", "ut_device_accessible",
+    "ut_xattn_fwd_workspace_size", "ut_xattn_fwd", "ut_xattn_bwd_workspace_size", "ut_xattn_bwd",
+    "ut_group_norm_fwd_workspace_size", "ut_group_norm_fwd", "ut_group_norm_bwd_workspace_size", "ut_group_norm_bwd",
 )
 
 
@@ -39,6 +42,23 @@ class AttnShape(ctypes.Structure):
     _fields_ = [("n_tokens", ctypes.c_int64), ("n_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
                 ("block", ctypes.c_int32), ("dtype", ctypes.c_int32), ("row_stride", ctypes.c_int64),
                 ("block_k", ctypes.c_int32)]
+
+
+class XattnShape(ctypes.Structure):
+    """ut_xattn_shape: rows, segments, heads, head dimension, dtype, elements between rows."""
+    _fields_ = [("n_q", ctypes.c_int64), ("n_k", ctypes.c_int64), ("n_seg", ctypes.c_int32),
+                ("n_heads", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                ("dtype", ctypes.c_int32), ("q_stride", ctypes.c_int64), ("k_stride", ctypes.c_int64),
+                ("v_stride", ctypes.c_int64), ("o_stride", ctypes.c_int64), ("do_stride", ctypes.c_int64),
+                ("dq_stride", ctypes.c_int64), ("dk_stride", ctypes.c_int64), ("dv_stride", ctypes.c_int64)]
+
+
+class GnormShape(ctypes.Structure):
+    """ut_gnorm_shape: rows, segments, channels, groups, dtype, activation, eps, elements between rows."""
+    _fields_ = [("n_rows", ctypes.c_int64), ("n_seg", ctypes.c_int32), ("channels", ctypes.c_int32),
+                ("groups", ctypes.c_int32), ("dtype", ctypes.c_int32), ("act", ctypes.c_int32),
+                ("eps", ctypes.c_float), ("x_stride", ctypes.c_int64), ("y_stride", ctypes.c_int64),
+                ("dy_stride", ctypes.c_int64), ("dx_stride", ctypes.c_int64)]
 
 
 class Rope(ctypes.Structure):
@@ -102,6 +122,20 @@ def lib() -> ctypes.CDLL:
     L.ut_fg_mask_from_alpha.argtypes = [_vp, _i32, _i32, _i32, _i32, _i32, _i32, _vp, _vp]
     L.ut_device_accessible.restype = _i32
     L.ut_device_accessible.argtypes = [_vp]
+    xs, gs = ctypes.POINTER(XattnShape), ctypes.POINTER(GnormShape)
+    for name in ("ut_xattn_fwd_workspace_size", "ut_xattn_bwd_workspace_size"):
+        getattr(L, name).restype, getattr(L, name).argtypes = _sz, [xs]
+    for name in ("ut_group_norm_fwd_workspace_size", "ut_group_norm_bwd_workspace_size"):
+        getattr(L, name).restype, getattr(L, name).argtypes = _sz, [gs]
+    L.ut_xattn_fwd.restype = _i32
+    L.ut_xattn_fwd.argtypes = [xs, _vp, _vp, _vp, _vp, _vp, _vp, _flt, _vp, _vp, _vp, _sz, _vp, _vp]
+    L.ut_xattn_bwd.restype = _i32
+    L.ut_xattn_bwd.argtypes = [xs, _vp, _vp, _vp, _vp, _vp, _vp, _flt, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _sz, _vp,
+                               _vp]
+    L.ut_group_norm_fwd.restype = _i32
+    L.ut_group_norm_fwd.argtypes = [gs, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _sz, _vp, _vp]
+    L.ut_group_norm_bwd.restype = _i32
+    L.ut_group_norm_bwd.argtypes = [gs, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _sz, _vp, _vp]
     _lib = L
     return L
 
@@ -402,3 +436,171 @@ def ut_bsattn_bwd(q, k, v, o, lse, dout, row_ptr, col_idx, col_ptr_t, row_idx_t,
                          ws.numel(), _p(status), _stream())
     _check("ut_bsattn_bwd", st)
     return dq, dk, dv
+
+
+# ------------------------------------------------------- conditioning operators
+def _prefix(cu: Optional[torch.Tensor], what: str) -> int:
+    """Number of segments of a prefix of lengths (1 without one)."""
+    if cu is None:
+        return 1
+    if cu.dtype != torch.int32 or cu.dim() != 1 or cu.numel() < 2 or not cu.is_contiguous():
+        raise ValueError(f"{what} must be a contiguous int32 vector of segments + 1 entries")
+    return cu.numel() - 1
+
+
+def _same_device(first: torch.Tensor, *others: Optional[torch.Tensor]) -> None:
+    for t in others:
+        if t is not None and t.device != first.device:
+            raise ValueError(f"tensors on {first.device} and {t.device}; all must share one device")
+
+
+def _head_rows(t: torch.Tensor, like: torch.Tensor, shape, what: str) -> int:
+    """Elements between the rows of a [rows, heads, d] tensor whose heads are contiguous."""
+    if tuple(t.shape) != tuple(shape) or t.dtype != like.dtype:
+        raise ValueError(f"{what} must be {list(shape)} {like.dtype}, got {list(t.shape)} {t.dtype}")
+    rows, heads, d = t.shape
+    if (d > 1 and t.stride(2) != 1) or (heads > 1 and t.stride(1) != d):
+        raise ValueError(f"{what}: heads must be contiguous within a row")
+    return t.stride(0) if rows > 1 else heads * d
+
+
+def _xattn_shape(q, k, v, cu_q, cu_k, key_mask, o, lse) -> XattnShape:
+    if q.dim() != 3 or k.dim() != 3 or k.shape[2] != q.shape[2]:
+        raise ValueError("q is [rows, heads, d]; k and v are [encoder rows, kv heads, d]")
+    n_seg = _prefix(cu_q, "cu_q")
+    if (cu_q is None) != (cu_k is None) or _prefix(cu_k, "cu_k") != n_seg:
+        raise ValueError("cu_q and cu_k describe the same segments: both or neither")
+    (nq, H, d), (nk, Hk) = q.shape, k.shape[:2]
+    if key_mask is not None:
+        if key_mask.dtype not in (torch.uint8, torch.bool) or key_mask.shape != (nk,) or not key_mask.is_contiguous():
+            raise ValueError("key_mask must be a contiguous uint8 or bool vector of the encoder rows")
+    if lse.dtype != torch.float32 or tuple(lse.shape) != (H, nq) or not lse.is_contiguous():
+        raise ValueError("lse must be a contiguous [heads, rows] fp32 tensor")
+    _same_device(q, k, v, cu_q, cu_k, key_mask, o, lse)
+    return XattnShape(nq, nk, n_seg, H, Hk, d, _dtype_code(q), _head_rows(q, q, (nq, H, d), "q"),
+                      _head_rows(k, q, (nk, Hk, d), "k"), _head_rows(v, q, (nk, Hk, d), "v"),
+                      _head_rows(o, q, (nq, H, d), "o"))
+
+
+def _workspace(ws: Optional[torch.Tensor], size: int, device):
+    if ws is None:
+        ws = torch.empty(max(size, 16), dtype=torch.uint8, device=device)
+    return ws, ws.numel() * ws.element_size()
+
+
+def ut_xattn_fwd(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, softmax_scale: Optional[float] = None,
+                 cu_q: Optional[torch.Tensor] = None, cu_k: Optional[torch.Tensor] = None,
+                 key_mask: Optional[torch.Tensor] = None, o: Optional[torch.Tensor] = None,
+                 lse: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None,
+                 status: Optional[torch.Tensor] = None):
+    """Cross attention of packed query rows q [Nq, H, d] to encoder states k, v [Nk, Hkv, d] (rows may be strided:
+    slices of one projection), segment by segment (cu_q, cu_k: int32 prefixes of the lengths, on the device), over
+    the keys with key_mask != 0.  Returns (O [Nq, H, d], LSE [H, Nq] fp32)."""
+    if o is None:
+        o = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    if lse is None:
+        lse = torch.empty((q.shape[1], q.shape[0]), dtype=torch.float32, device=q.device)
+    shape = _xattn_shape(q, k, v, cu_q, cu_k, key_mask, o, lse)
+    scale = q.shape[2] ** -0.5 if softmax_scale is None else float(softmax_scale)
+    L = lib()
+    ws, wsb = _workspace(ws, L.ut_xattn_fwd_workspace_size(ctypes.byref(shape)), q.device)
+    st = L.ut_xattn_fwd(ctypes.byref(shape), _p(q), _p(k), _p(v), _p(cu_q), _p(cu_k), _p(key_mask), scale, _p(o),
+                        _p(lse), _p(ws), wsb, _p(status), _stream())
+    _check("ut_xattn_fwd", st)
+    return o, lse
+
+
+def ut_xattn_bwd(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, o: torch.Tensor, lse: torch.Tensor,
+                 dout: torch.Tensor, softmax_scale: Optional[float] = None, cu_q: Optional[torch.Tensor] = None,
+                 cu_k: Optional[torch.Tensor] = None, key_mask: Optional[torch.Tensor] = None,
+                 dq: Optional[torch.Tensor] = None, dk: Optional[torch.Tensor] = None,
+                 dv: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None,
+                 status: Optional[torch.Tensor] = None):
+    """Gradient of ut_xattn_fwd (o and lse are its outputs).  Returns (dQ, dK, dV)."""
+    shape = _xattn_shape(q, k, v, cu_q, cu_k, key_mask, o, lse)
+    dq = torch.empty(q.shape, dtype=q.dtype, device=q.device) if dq is None else dq
+    dk = torch.empty(k.shape, dtype=k.dtype, device=k.device) if dk is None else dk
+    dv = torch.empty(v.shape, dtype=v.dtype, device=v.device) if dv is None else dv
+    _same_device(q, dout, dq, dk, dv)
+    shape.do_stride = _head_rows(dout, q, q.shape, "dout")
+    shape.dq_stride = _head_rows(dq, q, q.shape, "dq")
+    shape.dk_stride = _head_rows(dk, q, k.shape, "dk")
+    shape.dv_stride = _head_rows(dv, q, k.shape, "dv")
+    scale = q.shape[2] ** -0.5 if softmax_scale is None else float(softmax_scale)
+    L = lib()
+    ws, wsb = _workspace(ws, L.ut_xattn_bwd_workspace_size(ctypes.byref(shape)), q.device)
+    st = L.ut_xattn_bwd(ctypes.byref(shape), _p(q), _p(k), _p(v), _p(cu_q), _p(cu_k), _p(key_mask), scale, _p(o),
+                        _p(lse), _p(dout), _p(dq), _p(dk), _p(dv), _p(ws), wsb, _p(status), _stream())
+    _check("ut_xattn_bwd", st)
+    return dq, dk, dv
+
+
+def _channel_rows(t: torch.Tensor, like: torch.Tensor, what: str) -> int:
+    if t.dim() != 2 or t.shape != like.shape or t.dtype != like.dtype:
+        raise ValueError(f"{what} must be [rows, channels] of x's shape and dtype")
+    if t.shape[1] > 1 and t.stride(1) != 1:
+        raise ValueError(f"{what}: channels must be contiguous within a row")
+    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+
+
+def _gnorm_shape(x, gamma, beta, groups, act, eps, cu, mean, rstd) -> GnormShape:
+    n_seg = _prefix(cu, "cu")
+    stride = _channel_rows(x, x, "x")
+    for t in (gamma, beta):
+        if t is not None and (t.dtype != torch.float32 or t.shape != (x.shape[1],) or not t.is_contiguous()):
+            raise ValueError("gamma and beta are contiguous fp32 vectors of the channels")
+    for t in (mean, rstd):
+        if t.dtype != torch.float32 or tuple(t.shape) != (n_seg, groups) or not t.is_contiguous():
+            raise ValueError("mean and rstd are contiguous [segments, groups] fp32 tensors")
+    _same_device(x, gamma, beta, cu, mean, rstd)
+    return GnormShape(x.shape[0], n_seg, x.shape[1], int(groups), _dtype_code(x), int(act), float(eps), stride)
+
+
+def ut_group_norm_fwd(x: torch.Tensor, gamma: Optional[torch.Tensor], beta: Optional[torch.Tensor], groups: int,
+                      eps: float = 1e-5, act: int = UT_ACT_SILU, cu: Optional[torch.Tensor] = None,
+                      y: Optional[torch.Tensor] = None, mean: Optional[torch.Tensor] = None,
+                      rstd: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None,
+                      status: Optional[torch.Tensor] = None):
+    """Group norm with an activation over channels-last rows x [N, C], segment by segment (cu: int32 prefix of the
+    lengths, on the device).  Returns (y [N, C], mean, rstd [segments, groups] fp32)."""
+    n_seg = _prefix(cu, "cu")
+    if mean is None:
+        mean = torch.empty((n_seg, groups), dtype=torch.float32, device=x.device)
+    if rstd is None:
+        rstd = torch.empty((n_seg, groups), dtype=torch.float32, device=x.device)
+    shape = _gnorm_shape(x, gamma, beta, groups, act, eps, cu, mean, rstd)
+    if y is None:
+        y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    _same_device(x, y)
+    shape.y_stride = _channel_rows(y, x, "y")
+    L = lib()
+    ws, wsb = _workspace(ws, L.ut_group_norm_fwd_workspace_size(ctypes.byref(shape)), x.device)
+    st = L.ut_group_norm_fwd(ctypes.byref(shape), _p(x), _p(cu), _p(gamma), _p(beta), _p(y), _p(mean), _p(rstd),
+                             _p(ws), wsb, _p(status), _stream())
+    _check("ut_group_norm_fwd", st)
+    return y, mean, rstd
+
+
+def ut_group_norm_bwd(x: torch.Tensor, dy: torch.Tensor, gamma: Optional[torch.Tensor], beta: Optional[torch.Tensor],
+                      mean: torch.Tensor, rstd: torch.Tensor, groups: int, act: int = UT_ACT_SILU,
+                      cu: Optional[torch.Tensor] = None, dx: Optional[torch.Tensor] = None,
+                      dgamma: Optional[torch.Tensor] = None, dbeta: Optional[torch.Tensor] = None,
+                      ws: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None):
+    """Gradient of ut_group_norm_fwd (mean and rstd are its outputs).  Returns (dx [N, C], dgamma, dbeta [C] fp32)."""
+    shape = _gnorm_shape(x, gamma, beta, groups, act, 1.0, cu, mean, rstd)
+    dx = torch.empty(x.shape, dtype=x.dtype, device=x.device) if dx is None else dx
+    if dgamma is None:
+        dgamma = torch.empty(x.shape[1], dtype=torch.float32, device=x.device)
+    if dbeta is None:
+        dbeta = torch.empty(x.shape[1], dtype=torch.float32, device=x.device)
+    for t in (dgamma, dbeta):
+        if t.dtype != torch.float32 or t.shape != (x.shape[1],) or not t.is_contiguous():
+            raise ValueError("dgamma and dbeta are contiguous fp32 vectors of the channels")
+    _same_device(x, dy, dx, dgamma, dbeta)
+    shape.dy_stride, shape.dx_stride = _channel_rows(dy, x, "dy"), _channel_rows(dx, x, "dx")
+    L = lib()
+    ws, wsb = _workspace(ws, L.ut_group_norm_bwd_workspace_size(ctypes.byref(shape)), x.device)
+    st = L.ut_group_norm_bwd(ctypes.byref(shape), _p(x), _p(dy), _p(cu), _p(gamma), _p(beta), _p(mean), _p(rstd),
+                             _p(dx), _p(dgamma), _p(dbeta), _p(ws), wsb, _p(status), _stream())
+    _check("ut_group_norm_bwd", st)
+    return dx, dgamma, dbeta
