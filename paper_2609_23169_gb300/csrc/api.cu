@@ -53,6 +53,23 @@ bool encode_tmap_2d_bf16(CUtensorMap* map, const void* base, uint64_t inner_elem
   return r == CUDA_SUCCESS;
 }
 
+// [rows, heads, d] bf16 with contiguous heads and a row pitch; 128B-swizzled
+// boxes of 64 elements x box_heads x box_rows (box_heads * box_rows rows of 128
+// bytes in shared memory); rows past `rows` read as zero.
+bool encode_tmap_heads_bf16(CUtensorMap* map, const void* base, uint64_t d, uint64_t heads, uint64_t rows,
+                            uint64_t row_stride_bytes, uint32_t box_heads, uint32_t box_rows) {
+  EncodeTiledFn fn = encode_fn();
+  if (!fn) return false;
+  cuuint64_t dims[3] = {d, heads, rows};
+  cuuint64_t strides[2] = {d * 2, row_stride_bytes};
+  cuuint32_t box[3] = {64, box_heads, box_rows};
+  cuuint32_t estr[3] = {1, 1, 1};
+  CUresult r = fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(base), dims, strides, box, estr,
+                  CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                  CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  return r == CUDA_SUCCESS;
+}
+
 static ut_status from_cuda(cudaError_t e) { return e == cudaSuccess ? UT_OK : UT_ERR_CUDA; }
 
 // Limit of every bounded device wait: 2 s, or UT_WAIT_TIMEOUT_NS from the

@@ -155,7 +155,11 @@ ut_status ut_xattn_fwd(const ut_xattn_shape* shape, const void* q, const void* k
     p.part_ml = reinterpret_cast<float2*>(static_cast<char*>(ws) +
                                           up256((size_t)p.nsplit * p.nq * p.H * p.d * sizeof(float)));
   }
-  return status_of(launch_xattn_fwd_simt(p, shape->dtype == UT_BF16, static_cast<cudaStream_t>(stream)));
+  const bool bf16 = shape->dtype == UT_BF16;
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  cudaError_t e = bf16 ? launch_xattn_fwd_tc(p, s) : launch_xattn_fwd_simt(p, s);
+  if (e == cudaSuccess && p.nsplit > 1) e = launch_xattn_join(p, bf16, s);
+  return status_of(e);
 }
 
 size_t ut_xattn_bwd_workspace_size(const ut_xattn_shape* shape) {

@@ -87,4 +87,7 @@ uint64_t wait_timeout_ns();  // limit of every bounded device wait
 bool encode_tmap_2d_bf16(CUtensorMap* map, const void* base, uint64_t inner_elems, uint64_t rows,
                          uint64_t row_stride_bytes, uint32_t box_inner, uint32_t box_rows);
 
+bool encode_tmap_heads_bf16(CUtensorMap* map, const void* base, uint64_t d, uint64_t heads, uint64_t rows,
+                            uint64_t row_stride_bytes, uint32_t box_heads, uint32_t box_rows);
+
 }  // namespace ut

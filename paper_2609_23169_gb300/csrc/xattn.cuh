@@ -33,7 +33,10 @@ struct XattnParams {
 // split into.
 int64_t xattn_items(const XattnParams& p, bool bf16, bool backward);
 int xattn_splits(const XattnParams& p, bool bf16, bool backward);
-cudaError_t launch_xattn_fwd_simt(const XattnParams& p, bool bf16, cudaStream_t s);
+int64_t xattn_fwd_tc_items(const XattnParams& p);
+cudaError_t launch_xattn_fwd_simt(const XattnParams& p, cudaStream_t s);  // fp32
+cudaError_t launch_xattn_fwd_tc(const XattnParams& p, cudaStream_t s);    // bf16
+cudaError_t launch_xattn_join(const XattnParams& p, bool bf16, cudaStream_t s);  // of the forward's key splits
 cudaError_t launch_xattn_bwd_simt(const XattnParams& p, bool bf16, cudaStream_t s);
 
 }  // namespace ut

@@ -505,9 +505,7 @@ template <typename T, int D>
 static cudaError_t fwd(const XattnParams& p, cudaStream_t s) {
   const size_t smem = sizeof(float) * (3 * kXs * (D + 4) + kXs * kXsLdP + kXs);
   const dim3 grid((unsigned)segment_slots(p.nq, p.B, kXs / p.G), p.Hk, p.nsplit);
-  cudaError_t e = launch(xattn_fwd_simt_kernel<T, D>, grid, smem, p, s);
-  if (e != cudaSuccess || p.nsplit == 1) return e;
-  return launch(xattn_join_kernel<T, D>, dim3((unsigned)((p.nq * p.H + 15) / 16)), 0, p, s);
+  return launch(xattn_fwd_simt_kernel<T, D>, grid, smem, p, s);
 }
 
 template <typename T, int D>
@@ -532,23 +530,31 @@ static cudaError_t bwd(const XattnParams& p, cudaStream_t s) {
 }
 
 int64_t xattn_items(const XattnParams& p, bool bf16, bool backward) {
-  (void)bf16;
-  return backward ? segment_slots(p.nk, p.B, kXs) * p.Hk : segment_slots(p.nq, p.B, kXs / p.G) * p.Hk;
+  if (backward) return segment_slots(p.nk, p.B, kXs) * p.Hk;
+  return bf16 ? xattn_fwd_tc_items(p) : segment_slots(p.nq, p.B, kXs / p.G) * p.Hk;
 }
 
 // Enough parts for two blocks an SM, but none shorter than two tiles of an
 // average segment.
 int xattn_splits(const XattnParams& p, bool bf16, bool backward) {
   const int64_t items = xattn_items(p, bf16, backward), want = (2 * (int64_t)p.sms + items - 1) / items;
-  const int64_t tile = backward ? kXs / p.G : kXs, tiles = ((backward ? p.nq : p.nk) / p.B + tile - 1) / tile;
-  const int64_t most = tiles / 2;
+  const int64_t tile = backward ? kXs / p.G : (bf16 ? 128 : kXs);
+  const int64_t tiles = ((backward ? p.nq : p.nk) / p.B + tile - 1) / tile, most = tiles / 2;
   const int64_t n = want < most ? want : most;
   return (int)(n < 1 ? 1 : n > 1024 ? 1024 : n);
 }
 
-cudaError_t launch_xattn_fwd_simt(const XattnParams& p, bool bf16, cudaStream_t s) {
-  if (bf16) return p.d == 64 ? fwd<__nv_bfloat16, 64>(p, s) : fwd<__nv_bfloat16, 128>(p, s);
+cudaError_t launch_xattn_fwd_simt(const XattnParams& p, cudaStream_t s) {
   return p.d == 64 ? fwd<float, 64>(p, s) : fwd<float, 128>(p, s);
+}
+
+cudaError_t launch_xattn_join(const XattnParams& p, bool bf16, cudaStream_t s) {
+  const dim3 grid((unsigned)((p.nq * p.H + 15) / 16));
+  if (bf16)
+    return p.d == 64 ? launch(xattn_join_kernel<__nv_bfloat16, 64>, grid, 0, p, s)
+                     : launch(xattn_join_kernel<__nv_bfloat16, 128>, grid, 0, p, s);
+  return p.d == 64 ? launch(xattn_join_kernel<float, 64>, grid, 0, p, s)
+                   : launch(xattn_join_kernel<float, 128>, grid, 0, p, s);
 }
 
 cudaError_t launch_xattn_bwd_simt(const XattnParams& p, bool bf16, cudaStream_t s) {
