@@ -14,10 +14,10 @@
 // flight read neighbouring 256-byte pieces of the same rows and share K and V
 // in L2.  Roles (384 threads, registers rebalanced with setmaxnreg):
 //   warp 0      TMA: the K and V tiles, one ring (K0 V0 K1 V1 ...)
-//   warp 1      TMEM owner and MMA issuer.  Over the blocks of all items in
-//               one stream, for each tile w: O_w += P_w V of the previous
-//               block, then S_w = Q_w K^T of this one (P_w overwrote S_w in
-//               TMEM, so this order needs no second buffer).
+//   warp 1      TMEM owner and MMA issuer.  Over the blocks of
+//               all items in one stream, for each tile w: O_w += P_w V of the
+//               previous block, then S_w = Q_w K^T of this one (P_w overwrote
+//               S_w in TMEM, so this order needs no second buffer).
 //   warp 2      TMA: the query tiles, a ring of their own
 //   warp 3      decodes the items (segment search, key range) into a ring
 //   warps 4-7   softmax of tile 0, warps 8-11 of tile 1: thread = row = TMEM
@@ -26,8 +26,7 @@
 //               exponentials stay bounded), write P as bf16 over S; after the
 //               last block O / l and LSE, or the split's partial result.
 // Masked keys and the rows of other segments: S there is replaced by -inf,
-// and the MMA warp zeroes those rows of the V tile before its products, so
-// that no value they hold (NaN, infinities) is multiplied.
+// and the softmax warps zero those rows of the V tile before its products, so that no value they hold (NaN, infinities) is multiplied.
 // TMEM columns: S_0 / P_0 [0,128), S_1 / P_1 [128,256), O_0 [256,256+d), O_1
 // [384,384+d).
 // Every wait is bounded; on expiry the kernel records UT_ERR_TIMEOUT, drains
@@ -35,7 +34,7 @@
 #include "common.cuh"
 #include "kernels.h"
 #include "segments.cuh"
-#include "xattn.cuh"
+#include "xattn_tc.cuh"
 
 namespace ut {
 
@@ -77,68 +76,13 @@ struct Smem {
 
 struct Params {
   XattnParams x;
+  uint32_t inv_g;    // ceil(2^16 / G): (r * inv_g) >> 16 = r / G for r < 128, G <= 64
   int tpt;           // tokens of a tile
   int slots;         // item slots along the query rows (two tiles each)
   int64_t n_items;   // slots * Hk * nsplit
   float scale_log2;
   bool keep_kv;      // K and V are read by several items: keep them in L2
 };
-
-UT_DEV void tma_load_3d(void* dst, const void* tmap, uint64_t* bar, int32_t x, int32_t y, int32_t z, uint64_t policy) {
-  asm volatile(
-      "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.L2::cache_hint"
-      " [%0], [%1, {%2, %3, %4}], [%5], %6;" ::"r"(smem_u32(dst)),
-      "l"(tmap), "r"(x), "r"(y), "r"(z), "r"(smem_u32(bar)), "l"(policy)
-      : "memory");
-}
-
-// This lane's four keys of a block (lane + 32 g): bit g set where the key
-// exists and is not masked.
-UT_DEV uint32_t lane_keys(const uint8_t* mask, int64_t key, int left, uint32_t lane) {
-  uint32_t b = 0;
-#pragma unroll
-  for (int g = 0; g < 4; ++g) {
-    const int x = (int)lane + 32 * g;
-    if (x < left && (!mask || mask[key + x])) b |= 1u << g;
-  }
-  return b;
-}
-
-// Pairs of fp32 values in one 64-bit register: one instruction for two.
-UT_DEV uint64_t pack_u32x2(uint32_t a, uint32_t b) {
-  uint64_t r;
-  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "r"(a), "r"(b));
-  return r;
-}
-UT_DEV uint64_t pack_f32x2(float a, float b) { return pack_u32x2(__float_as_uint(a), __float_as_uint(b)); }
-UT_DEV void unpack_f32x2(uint64_t v, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
-UT_DEV uint64_t fma_f32x2(uint64_t a, uint64_t b, uint64_t c) {
-  uint64_t r;
-  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
-  return r;
-}
-UT_DEV uint64_t add_f32x2(uint64_t a, uint64_t b) {
-  uint64_t r;
-  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-  return r;
-}
-
-// 32 lanes x 32 bit, 16 consecutive columns per thread
-UT_DEV void tmem_ld16(uint32_t taddr, uint32_t (&r)[16]) {
-  asm volatile(
-      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
-      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
-        "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
-      : "r"(taddr));
-}
-UT_DEV void tmem_st16(uint32_t taddr, const uint32_t (&r)[16]) {
-  asm volatile(
-      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};" ::"r"(
-          taddr),
-      "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
-      "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
-      : "memory");
-}
 
 template <int D>
 __global__ void __launch_bounds__(kThreads, 1)
@@ -157,11 +101,11 @@ __global__ void __launch_bounds__(kThreads, 1)
   if (threadIdx.x == 0) {
     for (int s = 0; s < S::kQ; ++s) {
       mbar_init(&sm.q_full[s], 1);
-      mbar_init(&sm.q_empty[s], 1);
+      mbar_init(&sm.q_empty[s], 5);  // its last product, and the four warps that sent its output
     }
     for (int s = 0; s < S::kKv; ++s) {
       mbar_init(&sm.kv_full[s], 1);
-      mbar_init(&sm.kv_empty[s], 1);
+      mbar_init(&sm.kv_empty[s], 2);  // both tiles' products
     }
     for (int w = 0; w < 2; ++w) {
       mbar_init(&sm.s_full[w], 1);
@@ -169,7 +113,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       mbar_init(&sm.o_full[w], 1);
       mbar_init(&sm.o_empty[w], 4);
     }
-    mbar_init(&sm.mma_done, 1);
+    mbar_init(&sm.mma_done, 2);
     for (int s = 0; s < kItemSlots; ++s) {
       mbar_init(&sm.item_full[s], 1);
       mbar_init(&sm.item_empty[s], kItemReaders);
@@ -188,7 +132,12 @@ __global__ void __launch_bounds__(kThreads, 1)
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  const uint32_t tmem = sm.tmem_base;
+  // all 512 columns are this CTA's, so they start at address 0, a constant in
+  // the instructions below
+  if (sm.tmem_base != 0 && threadIdx.x == 0) {
+    set_status(p.status, UT_ERR_CUDA);
+    sm.abort_flag = 1;
+  }
 
   auto wait = [&](uint64_t* bar, uint32_t parity) {  // whole warp, converged
     return warp_wait(bar, parity, abort_flag, p.status, p.timeout_ns);
@@ -238,45 +187,26 @@ __global__ void __launch_bounds__(kThreads, 1)
       }
       for (uint32_t x = at > S::kKv ? at - S::kKv : 0; x < at; ++x) drain(&sm.kv_full[x % S::kKv], (x / S::kKv) & 1);
     } else if (warp == 2 && lane == 0) {
-      // ---------------------------------------------------------- Q producer
+      // ------------------------------------------- item decoder, Q producer
       tma_prefetch_desc(&tm_q);
       const uint64_t pol = policy_evict_first();
       const uint32_t bytes = (uint32_t)prm.tpt * p.G * 128 * S::kChunks;
       uint32_t n = 0, at = 0;
       bool ok = true;
-      Item it;
-      while (ok && next_item(n, it, ok, true)) {
-        if (it.blocks == 0) continue;
-        for (int w = 0; w < 2 && ok; ++w) {
-          if (it.ntok[w] == 0) continue;
-          const uint32_t st = at % S::kQ, f = at / S::kQ;
-          if (!(ok = wait1(&sm.q_empty[st], (f & 1) ^ 1))) break;
-          mbar_expect_tx(&sm.q_full[st], bytes);
-          for (int c = 0; c < S::kChunks; ++c)
-            tma_load_3d(sm.q[st] + c * kChunkBytes, &tm_q, &sm.q_full[st], c * 64, it.hk * p.G, it.tok0 + w * prm.tpt,
-                        pol);
-          ++at;
-        }
-      }
-      for (uint32_t x = at > S::kQ ? at - S::kQ : 0; x < at; ++x) drain(&sm.q_full[x % S::kQ], (x / S::kQ) & 1);
-    } else if (warp == 3 && lane == 0) {
-      // -------------------------------------------------------- item decoder
-      uint32_t n = 0;
-      bool ok = true;
-      for (int64_t w = blockIdx.x; ok; w += gridDim.x) {
+      for (int64_t u = blockIdx.x; ok; u += gridDim.x) {
         Item it{};
         it.hk = -1;
-        if (w < prm.n_items) {
-          const int64_t u = w / p.Hk;
-          const Segment g = segment_of_slot(p.cu_q, p.B, p.nq, 2 * prm.tpt, u % prm.slots);
+        if (u < prm.n_items) {
+          const int64_t at_q = u / p.Hk;
+          const Segment g = segment_of_slot(p.cu_q, p.B, p.nq, 2 * prm.tpt, at_q % prm.slots);
           const int64_t t0 = g.tile * 2 * prm.tpt;
           if (t0 >= g.n) continue;  // an idle slot
           int64_t k0, kn;
           segment_rows(p.cu_k, g.s, p.nk, k0, kn);
           const int64_t nblk = (kn + kN - 1) / kN, per = (nblk + p.nsplit - 1) / p.nsplit;
-          it.split = (int)(u / prm.slots);
+          it.split = (int)(at_q / prm.slots);
           const int64_t b0 = min(nblk, per * it.split), b1 = min(nblk, b0 + per);
-          it.hk = (int)(w % p.Hk);
+          it.hk = (int)(u % p.Hk);
           it.blocks = (int)(b1 - b0);
           it.tok0 = (int)(g.row + t0);
           it.ntok[0] = (int)min((int64_t)prm.tpt, g.n - t0);
@@ -290,97 +220,83 @@ __global__ void __launch_bounds__(kThreads, 1)
         mbar_arrive(&sm.item_full[s]);
         ++n;
         if (it.hk < 0) break;
+        if (it.blocks == 0) continue;
+        for (int w = 0; w < 2 && ok; ++w) {
+          if (it.ntok[w] == 0) continue;
+          const uint32_t st = at % S::kQ, qf = at / S::kQ;
+          if (!(ok = wait1(&sm.q_empty[st], (qf & 1) ^ 1))) break;
+          mbar_expect_tx(&sm.q_full[st], bytes);
+          for (int c = 0; c < S::kChunks; ++c)
+            tma_load_3d(sm.q[st] + c * kChunkBytes, &tm_q, &sm.q_full[st], c * 64, it.hk * p.G, it.tok0 + w * prm.tpt,
+                        pol);
+          ++at;
+        }
       }
-    } else if (warp == 1) {
-      // ---------------------------------------------------------- MMA issuer
+      for (uint32_t x = at > S::kQ ? at - S::kQ : 0; x < at; ++x) drain(&sm.q_full[x % S::kQ], (x / S::kQ) & 1);
+    } else if (warp == 1 || warp == 3) {
+      // ---------------------------------------- MMA issuer of tile 0 / tile 1
+      // Converged, and uniform to the compiler: every branch depends on votes
+      // and on item fields made uniform.
       constexpr uint32_t idesc_s = idesc_bf16_f32(kM, kN, false, false);
       constexpr uint32_t idesc_o = idesc_bf16_f32(kM, D, false, true);
-      uint32_t n = 0, qat = 0, kvat = 0;
-      uint32_t nps[2] = {0, 0}, noe[2] = {0, 0};  // P tiles consumed, O accumulators begun
+      const uint32_t q_lo = desc_lo(smem_u32(sm.q[0]), 16), k_lo = desc_lo(smem_u32(sm.kv[0]), 16),
+                     v_lo = desc_lo(smem_u32(sm.kv[0]), kChunkBytes);
+      const uint32_t w = warp >> 1, ts = w * 128, to = 256 + w * 128;
+      uint64_t* p_full = &sm.p_full[w];
+      uint64_t* s_full = &sm.s_full[w];
+      uint32_t n = 0, qat = w, kvat = 0, np = 0, no = 0;
       bool ok = true;
-      // the previous block: its V stage, which tiles it has, and its place in its item
-      bool have = false, first = false, last = false, on[2] = {false, false};
-      uint32_t v_st = 0;
-      auto pv = [&](int w) -> bool {  // O_w (+)= P_w V of the previous block
-        if (!wait(&sm.p_full[w], nps[w] & 1)) return false;
-        ++nps[w];
-        if (first) {
-          if (!wait(&sm.o_empty[w], (noe[w] & 1) ^ 1)) return false;
-          ++noe[w];
-        }
-        tc_fence_after();
-        const uint32_t va = smem_u32(sm.kv[v_st]);
-#pragma unroll
-        for (int kk = 0; kk < kN / 16; ++kk)
-          mma_bf16_ts_w(tmem + 256 + w * 128, tmem + w * 128 + kk * 8, sdesc_sw128(va + kk * 2048, kChunkBytes, 1024),
-                        idesc_o, !first || kk > 0);
-        if (last) mma_commit_w(&sm.o_full[w]);
-        return true;
-      };
-      Item it;
-      while (ok && next_item(n, it, ok, false)) {
-        if (it.blocks == 0) continue;
-        const bool tile[2] = {true, it.ntok[1] > 0};
-        for (int j = 0; j < it.blocks && ok; ++j) {
-          const uint32_t k_st = kvat % S::kKv, kf = kvat / S::kKv;
-          const uint32_t vn = kvat + 1, vs = vn % S::kKv, vf = vn / S::kKv;
-          kvat += 2;
-          const int left = it.left - j * kN;
-          const bool full = !p.mask && left >= kN;
-          uint32_t keys = 15u;
-          if (!full) keys = lane_keys(p.mask, (int64_t)it.key0 + j * kN, left, lane);
-#pragma unroll
-          for (int w = 0; w < 2; ++w) {
-            if (!ok) break;
-            if (have && on[w] && !(ok = pv(w))) break;
-            if (have && w == 1) mma_commit_w(&sm.kv_empty[v_st]);
-            if (!tile[w]) continue;
-            if (w == 0 && !(ok = wait(&sm.kv_full[k_st], kf & 1))) break;
-            const uint32_t q_st = (qat + w) % S::kQ, qf = (qat + w) / S::kQ;
-            if (j == 0 && !(ok = wait(&sm.q_full[q_st], qf & 1))) break;
-            tc_fence_after();
-            const uint32_t qa = smem_u32(sm.q[q_st]), ka = smem_u32(sm.kv[k_st]);
-#pragma unroll
-            for (int kk = 0; kk < D / 16; ++kk) {
-              const uint32_t off = (kk >> 2) * kChunkBytes + (kk & 3) * 32;
-              mma_bf16_ss_w(tmem + w * 128, sdesc_sw128(qa + off, 16, 1024), sdesc_sw128(ka + off, 16, 1024), idesc_s,
-                            kk > 0);
-            }
-            mma_commit_w(&sm.s_full[w]);
-            if (j == it.blocks - 1) mma_commit_w(&sm.q_empty[q_st]);
+      for (;; ++n) {
+        const uint32_t slot = n % kItemSlots;
+        if (!(ok = wait(&sm.item_full[slot], (n / kItemSlots) & 1))) break;
+        const int hk = (int)warp_uniform((uint32_t)sm.item[slot].hk);
+        const int blocks = (int)warp_uniform((uint32_t)sm.item[slot].blocks);
+        const bool both = warp_uniform((uint32_t)sm.item[slot].ntok[1]) != 0;
+        if (hk < 0) break;
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&sm.item_empty[slot]);
+        if (blocks == 0) continue;
+        if (w == 1 && !both) {  // nothing for tile 1: pass the K and V tiles on
+#pragma unroll 1
+          for (int x = 0; x < 2 * blocks && ok; ++x, ++kvat) {
+            ok = wait(&sm.kv_full[kvat % S::kKv], (kvat / S::kKv) & 1);
+            if (ok && lane == 0) mbar_arrive(&sm.kv_empty[kvat % S::kKv]);
           }
           if (!ok) break;
-          mma_commit_w(&sm.kv_empty[k_st]);
-          // V of this block, needed by the next step's products: zero the rows
-          // that must not enter them while the softmax works
-          if (!(ok = wait(&sm.kv_full[vs], vf & 1))) break;
-          if (__any_sync(0xffffffffu, keys != 15u)) {
-#pragma unroll
-            for (int g = 0; g < 4; ++g)
-              if (!((keys >> g) & 1u)) {
-                const uint32_t row = smem_u32(sm.kv[vs]) + (lane + 32 * g) * 128;
-#pragma unroll
-                for (int c = 0; c < S::kChunks; ++c)
-#pragma unroll
-                  for (int x = 0; x < 8; ++x)
-                    st_shared_v4(row + c * kChunkBytes + (((x + lane) & 7) << 4), 0, 0, 0, 0);
-              }
-            fence_proxy_async_smem();
-            __syncwarp();
-          }
-          v_st = vs;
-          have = true;
-          first = j == 0;
-          last = j == it.blocks - 1;
-          on[0] = true;
-          on[1] = tile[1];
+          ++qat;
+          continue;
         }
-        qat += tile[1] ? 2 : 1;
-      }
-      if (ok && have) {
-#pragma unroll
-        for (int w = 0; w < 2; ++w)
-          if (ok && on[w]) ok = pv(w);
+        const uint32_t qs = qat % S::kQ, q_a = q_lo + qs * (S::kTile >> 4);
+        if (!(ok = wait(&sm.q_full[qs], (qat / S::kQ) & 1))) break;
+#pragma unroll 1
+        for (int j = 0;; ++j) {
+          const uint32_t ks = kvat % S::kKv;  // S = Q K^T
+          if (!(ok = wait(&sm.kv_full[ks], (kvat / S::kKv) & 1))) break;
+          tc_fence_after();
+          mma_nt<D>(ts, q_a, k_lo + ks * (S::kTile >> 4), idesc_s);
+          mma_commit_w(s_full);
+          mma_commit_w(&sm.kv_empty[ks]);
+          if (j == blocks - 1) mma_commit_w(&sm.q_empty[qs]);
+          // O += P V, V being needed (and zeroed in places) well before P is there
+          const uint32_t st = (kvat + 1) % S::kKv;
+          if (!(ok = wait(&sm.kv_full[st], ((kvat + 1) / S::kKv) & 1))) break;
+          if (j == 0) {
+            if (!(ok = wait(&sm.o_empty[w], (no & 1) ^ 1))) break;
+            ++no;
+          }
+          if (!(ok = wait(p_full, np & 1))) break;
+          ++np;
+          tc_fence_after();
+          mma_tn128(to, ts, v_lo + st * (S::kTile >> 4), idesc_o, j > 0);
+          mma_commit_w(&sm.kv_empty[st]);
+          kvat += 2;
+          if (j == blocks - 1) {
+            mma_commit_w(&sm.o_full[w]);
+            break;
+          }
+        }
+        if (!ok) break;
+        qat += both ? 2 : 1;
       }
       mma_commit_w(&sm.mma_done);  // every MMA has completed before TMEM is freed
       drain(&sm.mma_done, 0);
@@ -390,9 +306,10 @@ __global__ void __launch_bounds__(kThreads, 1)
     setmaxnreg_inc<kRegSoftmax>();
     const int w = warp < 8 ? 0 : 1;
     const uint32_t quarter = warp & 3, lane_base = (quarter * 32) << 16;
-    const uint32_t ts = tmem + lane_base + w * 128, to = tmem + lane_base + 256 + w * 128;
+    const uint32_t ts = lane_base + w * 128, to = lane_base + 256 + w * 128;
+    auto token_of = [&](uint32_t r) -> uint32_t { return (r * prm.inv_g) >> 16; };  // r / G
     const uint64_t c2 = pack_f32x2(prm.scale_log2, prm.scale_log2);
-    uint32_t n = 0, ns = 0, no = 0;
+    uint32_t n = 0, ns = 0, no = 0, qat = 0, kvat = 0;
     bool ok = true;
     for (;; ++n) {
       // the item stays in its slot until this tile is done with it
@@ -415,6 +332,19 @@ __global__ void __launch_bounds__(kThreads, 1)
         for (int g = 0; g < 4; ++g) tmem_ld32(ts + g * 32, *reinterpret_cast<uint32_t(*)[32]>(&r[g * 32]));
         tmem_wait_ld();
         if (!__all_sync(0xffffffffu, now == 15u)) {
+          {
+            // zero the rows of the V tile that must not enter the product
+            // (thread = row; the other tile's warps may write the same zeros)
+            const uint32_t vat = kvat + 2 * j + 1, st = vat % S::kKv;
+            if (!(ok = wait(&sm.kv_full[st], (vat / S::kKv) & 1))) break;
+            if (!((now >> quarter) & 1u)) {
+              const uint32_t v_row = smem_u32(sm.kv[st]) + (quarter * 32 + lane) * 128;
+#pragma unroll
+              for (int x = 0; x < 8 * S::kChunks; ++x)
+                st_shared_v4(v_row + (x >> 3) * kChunkBytes + (((x + lane) & 7) << 4), 0, 0, 0, 0);
+            }
+            fence_proxy_async_smem();
+          }
 #pragma unroll
           for (int g = 0; g < 4; ++g) {
             const uint32_t word = __ballot_sync(0xffffffffu, (now >> g) & 1u);
@@ -479,65 +409,96 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (lane == 0) mbar_arrive(&sm.p_full[w]);
       }
       if (!ok) break;
-      // O / l and LSE, or the split's partial result
       if (blocks > 0) {
         if (!(ok = wait(&sm.o_full[w], no & 1))) break;
         ++no;
         tc_fence_after();
       }
-      const int row = (int)(quarter * 32 + lane), rt = row / p.G;  // this row's token of the tile
-      const int h = it->hk * p.G + row % p.G, ntok = it->ntok[w], split = it->split;
-      const int64_t tok = (int64_t)it->tok0 + w * prm.tpt + rt;
-      const bool row_ok = rt < ntok;
+      const uint32_t row = quarter * 32 + lane, rt = token_of(row);  // this thread's row and its token
+      const int hk = it->hk, ntok = it->ntok[w], split = it->split;
+      const int64_t tok0 = (int64_t)it->tok0 + w * prm.tpt;
+      const bool two = it->ntok[1] > 0;
+      const uint32_t qst = (qat + w) % S::kQ;
+      if (it->blocks > 0) {
+        qat += two ? 2 : 1;
+        kvat += 2 * it->blocks;
+      }
       __syncwarp();
       if (lane == 0) mbar_arrive(&sm.item_empty[slot]);
-      const bool part = p.nsplit > 1;
-      const float f = part ? 1.f : (l > 0.f ? 1.f / l : (l == 0.f ? 0.f : l));
-      const int64_t prow = ((int64_t)split * p.nq + tok) * p.H + h;
-      __nv_bfloat16* orow = static_cast<__nv_bfloat16*>(p.o) + tok * p.os + (int64_t)h * D;
+      if (ntok == 0) continue;
+      const int h = hk * p.G + (int)(row - rt * p.G);
+      const bool row_ok = (int)rt < ntok;
+      if (p.nsplit > 1) {
+        const int64_t prow = ((int64_t)split * p.nq + tok0 + rt) * p.H + h;
 #pragma unroll
-      for (int g = 0; g < D / 32; ++g) {
-        uint32_t r[32];
-        if (blocks > 0) {
-          tmem_ld32(to + g * 32, r);
-          tmem_wait_ld();
-        } else {
+        for (int g = 0; g < D / 32; ++g) {
+          uint32_t r[32];
+          if (blocks > 0) {
+            tmem_ld32(to + g * 32, r);
+            tmem_wait_ld();
+          } else {
 #pragma unroll
-          for (int x = 0; x < 32; ++x) r[x] = 0;
-        }
-        if (!row_ok) continue;
-        if (part) {
+            for (int x = 0; x < 32; ++x) r[x] = 0;
+          }
+          if (!row_ok) continue;
 #pragma unroll
           for (int x = 0; x < 32; x += 4)
             *reinterpret_cast<uint4*>(p.part_o + prow * D + g * 32 + x) =
                 make_uint4(r[x], r[x + 1], r[x + 2], r[x + 3]);
-        } else {
+        }
+        if (row_ok) p.part_ml[prow] = make_float2(m, l);
+        tc_fence_before();
+        __syncwarp();
+        if (blocks > 0 && lane == 0) {
+          mbar_arrive(&sm.o_empty[w]);
+          mbar_arrive(&sm.q_empty[qst]);
+        }
+        continue;
+      }
+      if (row_ok) p.lse[(int64_t)h * p.nq + tok0 + rt] = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
+      // O / l in bf16 through the query tile's shared memory (its last product
+      // has read it): whole rows leave as 16-byte pieces of neighbouring lanes
+      const uint32_t stage = smem_u32(sm.q[qst]);
+      if (blocks > 0) {
+        const float f = l > 0.f ? 1.f / l : (l == 0.f ? 0.f : l);
 #pragma unroll
-          for (int x = 0; x < 32; x += 8) {
-            uint4 v;
-            v.x = pack_bf16x2(__uint_as_float(r[x + 0]) * f, __uint_as_float(r[x + 1]) * f);
-            v.y = pack_bf16x2(__uint_as_float(r[x + 2]) * f, __uint_as_float(r[x + 3]) * f);
-            v.z = pack_bf16x2(__uint_as_float(r[x + 4]) * f, __uint_as_float(r[x + 5]) * f);
-            v.w = pack_bf16x2(__uint_as_float(r[x + 6]) * f, __uint_as_float(r[x + 7]) * f);
-            *reinterpret_cast<uint4*>(orow + g * 32 + x) = v;
+        for (int g = 0; g < D / 32; ++g) {
+          uint32_t r[32];
+          tmem_ld32(to + g * 32, r);
+          tmem_wait_ld();
+          const uint32_t dst = stage + (g >> 1) * kChunkBytes + row * 128;
+#pragma unroll
+          for (int x = 0; x < 4; ++x) {
+            uint32_t v[4];
+#pragma unroll
+            for (int y = 0; y < 4; ++y)
+              v[y] = pack_bf16x2(__uint_as_float(r[x * 8 + 2 * y]) * f, __uint_as_float(r[x * 8 + 2 * y + 1]) * f);
+            st_shared_v4(dst + ((((g & 1) * 4 + x) ^ (row & 7)) << 4), v[0], v[1], v[2], v[3]);
           }
         }
-      }
-      if (blocks > 0) {
         tc_fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive(&sm.o_empty[w]);
       }
-      if (row_ok) {
-        if (part) p.part_ml[prow] = make_float2(m, l);
-        else p.lse[(int64_t)h * p.nq + tok] = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
+      constexpr int kUnits = D / 8, kRows = 32 / kUnits;  // 16-byte units of a row, rows of a warp's access
+      __nv_bfloat16* out = static_cast<__nv_bfloat16*>(p.o) + tok0 * p.os + (int64_t)hk * p.G * D;
+#pragma unroll 4
+      for (int i = 0; i < 32 / kRows; ++i) {
+        const uint32_t y = quarter * 32 + i * kRows + lane / kUnits, u = lane % kUnits, yt = token_of(y);
+        uint32_t v[4] = {0, 0, 0, 0};
+        if (blocks > 0) ld_shared_v4(stage + (u >> 3) * kChunkBytes + y * 128 + (((u & 7) ^ (y & 7)) << 4), v);
+        if ((int)yt < ntok)
+          *reinterpret_cast<uint4*>(out + yt * p.os + (int64_t)(y - yt * p.G) * D + u * 8) =
+              make_uint4(v[0], v[1], v[2], v[3]);
       }
+      __syncwarp();
+      if (blocks > 0 && lane == 0) mbar_arrive(&sm.q_empty[qst]);
     }
   }
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  if (warp == 1) tmem_dealloc(tmem, 512);
+  if (warp == 1) tmem_dealloc(sm.tmem_base, 512);
 }
 
 static_assert(sizeof(Smem<128>) <= 232448 && sizeof(Smem<64>) <= 232448, "shared layout exceeds the block limit");
@@ -565,6 +526,7 @@ int64_t xattn_fwd_tc_items(const XattnParams& p) { return segment_slots(p.nq, p.
 cudaError_t launch_xattn_fwd_tc(const XattnParams& p, cudaStream_t s) {
   Params prm{};
   prm.x = p;
+  prm.inv_g = (65536u + p.G - 1) / p.G;
   prm.tpt = kM / p.G;
   prm.slots = (int)segment_slots(p.nq, p.B, 2 * prm.tpt);
   prm.n_items = (int64_t)prm.slots * p.Hk * p.nsplit;

@@ -1,0 +1,122 @@
+// Device helpers of the cross-attention tensor-core kernels.
+#pragma once
+#include "common.cuh"
+#include "xattn.cuh"
+
+namespace ut {
+
+UT_DEV void tma_load_3d(void* dst, const void* tmap, uint64_t* bar, int32_t x, int32_t y, int32_t z, uint64_t policy) {
+  asm volatile(
+      "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.L2::cache_hint"
+      " [%0], [%1, {%2, %3, %4}], [%5], %6;" ::"r"(smem_u32(dst)),
+      "l"(tmap), "r"(x), "r"(y), "r"(z), "r"(smem_u32(bar)), "l"(policy)
+      : "memory");
+}
+
+// A whole product of tcgen05.mma instructions, executed by a converged warp
+// and issued by one elected lane, with the shared-memory descriptors split
+// into a constant high word and a low word that only needs additions.  The
+// operands have to be the same in every lane, and are kept in uniform
+// registers where the warp's control flow is provably uniform (votes,
+// warp_uniform below): a product then costs its issue and little else.  With
+// operands in ordinary registers (one thread in a divergent branch) an
+// instruction took 80-130 cycles to issue, more than it takes to run.
+//   kDescHi: 128-byte swizzle, 1024 bytes between groups of eight 128-byte
+//   rows; desc_lo: start address and leading byte offset, in units of 16 bytes
+constexpr uint32_t kDescHi = (1024u >> 4) | (1u << 14) | (2u << 29);
+UT_DEV uint32_t desc_lo(uint32_t addr, uint32_t lbo_bytes) { return ((addr & 0x3FFFFu) >> 4) | ((lbo_bytes >> 4) << 16); }
+UT_DEV uint32_t warp_uniform(uint32_t x) { return __reduce_or_sync(0xffffffffu, x); }
+
+#define UT_SS_STEP(off, acc)                                             \
+  "add.u32 x, %1, " off ";\n\tadd.u32 y, %2, " off ";\n\t"              \
+  "mov.b64 a, {x, %4};\n\tmov.b64 b, {y, %4};\n\t"                     \
+  "@e tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, " acc ";\n\t"
+#define UT_SS_HEAD                                                                     \
+  "{\n\t.reg .pred e, f, t;\n\t.reg .b64 a, b;\n\t.reg .b32 x, y;\n\t"              \
+  "setp.ne.b32 f, 0, 0;\n\tsetp.eq.b32 t, 0, 0;\n\telect.sync _|e, 0xffffffff;\n\t"
+// d = A B^T over D columns of two K-major tiles (128-row sub-tiles of 64 columns)
+template <int D>
+UT_DEV void mma_nt(uint32_t d, uint32_t a_lo, uint32_t b_lo, uint32_t idesc) {
+  if constexpr (D == 64)
+    asm volatile(UT_SS_HEAD UT_SS_STEP("0", "f") UT_SS_STEP("2", "t") UT_SS_STEP("4", "t") UT_SS_STEP("6", "t") "}" ::"r"(d),
+                 "r"(a_lo), "r"(b_lo), "r"(idesc), "r"(kDescHi)
+                 : "memory");
+  else
+    asm volatile(UT_SS_HEAD UT_SS_STEP("0", "f") UT_SS_STEP("2", "t") UT_SS_STEP("4", "t") UT_SS_STEP("6", "t")
+                     UT_SS_STEP("1024", "t") UT_SS_STEP("1026", "t") UT_SS_STEP("1028", "t") UT_SS_STEP("1030", "t") "}" ::"r"(d),
+                 "r"(a_lo), "r"(b_lo), "r"(idesc), "r"(kDescHi)
+                 : "memory");
+}
+#define UT_TS_STEP(acol, boff, acc)                                     \
+  "add.u32 x, %1, " acol ";\n\tadd.u32 y, %2, " boff ";\n\t"           \
+  "mov.b64 b, {y, %5};\n\t"                                            \
+  "@e tcgen05.mma.cta_group::1.kind::f16 [%0], [x], b, %3, " acc ";\n\t"
+// d (+)= A B over 128 rows of B: A in TMEM (bf16 pairs, 8 columns a step), B
+// row-major (MN-major operand, 16 rows of 128 bytes a step)
+UT_DEV void mma_tn128(uint32_t d, uint32_t a, uint32_t b_lo, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred e, p, t;\n\t.reg .b64 b;\n\t.reg .b32 x, y;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\tsetp.eq.b32 t, 0, 0;\n\telect.sync _|e, 0xffffffff;\n\t" UT_TS_STEP("0", "0", "p")
+          UT_TS_STEP("8", "128", "t") UT_TS_STEP("16", "256", "t") UT_TS_STEP("24", "384", "t")
+              UT_TS_STEP("32", "512", "t") UT_TS_STEP("40", "640", "t") UT_TS_STEP("48", "768", "t")
+                  UT_TS_STEP("56", "896", "t") "}" ::"r"(d),
+      "r"(a), "r"(b_lo), "r"(idesc), "r"(accumulate), "r"(kDescHi)
+      : "memory");
+}
+
+// This lane's four keys of a block (lane + 32 g): bit g set where the key
+// exists and is not masked.
+UT_DEV uint32_t lane_keys(const uint8_t* mask, int64_t key, int left, uint32_t lane) {
+  uint32_t b = 0;
+#pragma unroll
+  for (int g = 0; g < 4; ++g) {
+    const int x = (int)lane + 32 * g;
+    if (x < left && (!mask || mask[key + x])) b |= 1u << g;
+  }
+  return b;
+}
+
+// Pairs of fp32 values in one 64-bit register: one instruction for two.
+UT_DEV uint64_t pack_u32x2(uint32_t a, uint32_t b) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "r"(a), "r"(b));
+  return r;
+}
+UT_DEV uint64_t pack_f32x2(float a, float b) { return pack_u32x2(__float_as_uint(a), __float_as_uint(b)); }
+UT_DEV void unpack_f32x2(uint64_t v, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
+UT_DEV uint64_t fma_f32x2(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+UT_DEV uint64_t add_f32x2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+
+UT_DEV void ld_shared_v4(uint32_t addr, uint32_t (&v)[4]) {
+  asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
+               : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3])
+               : "r"(addr)
+               : "memory");
+}
+
+// 32 lanes x 32 bit, 16 consecutive columns per thread
+UT_DEV void tmem_ld16(uint32_t taddr, uint32_t (&r)[16]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+        "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+      : "r"(taddr));
+}
+UT_DEV void tmem_st16(uint32_t taddr, const uint32_t (&r)[16]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};" ::"r"(
+          taddr),
+      "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
+      "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
+      : "memory");
+}
+
+}  // namespace ut
