@@ -68,9 +68,10 @@ static size_t xattn_fwd_ws(const XattnParams& p) {
   return up256(rows * p.d * sizeof(float)) + up256(rows * sizeof(float2));
 }
 
-static size_t xattn_bwd_ws(const XattnParams& p) {
+// D, then partial dK and dV (and, in bf16, the CTAs' dQ buffers)
+static size_t xattn_bwd_ws(const XattnParams& p, bool bf16) {
   const size_t part = up256((size_t)p.nsplit * p.nk * p.Hk * p.d * sizeof(float));
-  return up256((size_t)p.H * p.nq * sizeof(float)) + 2 * part;
+  return up256((size_t)p.H * p.nq * sizeof(float)) + (bf16 ? xattn_bwd_tc_ws(p) : 2 * part);
 }
 
 static ut_status xattn_pointers(const ut_xattn_shape* s, const XattnParams& p) {
@@ -164,7 +165,7 @@ ut_status ut_xattn_fwd(const ut_xattn_shape* shape, const void* q, const void* k
 
 size_t ut_xattn_bwd_workspace_size(const ut_xattn_shape* shape) {
   XattnParams p;
-  return xattn_problem(shape, true, &p) == UT_OK ? xattn_bwd_ws(p) : 0;
+  return xattn_problem(shape, true, &p) == UT_OK ? xattn_bwd_ws(p, shape->dtype == UT_BF16) : 0;
 }
 
 ut_status ut_xattn_bwd(const ut_xattn_shape* shape, const void* q, const void* k, const void* v,
@@ -194,13 +195,18 @@ ut_status ut_xattn_bwd(const ut_xattn_shape* shape, const void* q, const void* k
   if ((p.nq > 0 && (!dout || !dq)) || (p.nk > 0 && (!dk || !dv))) return UT_ERR_INVALID_ARG;
   if (!at16(dout) || !at16(dq) || !at16(dk) || !at16(dv)) return UT_ERR_INVALID_ARG;
   if (p.nq == 0 && p.nk == 0) return UT_OK;
-  if (!ws || ws_bytes < xattn_bwd_ws(p) || !at16(ws)) return UT_ERR_INVALID_ARG;
+  const bool bf16 = shape->dtype == UT_BF16;
+  if (!ws || ws_bytes < xattn_bwd_ws(p, bf16) || !at16(ws)) return UT_ERR_INVALID_ARG;
   char* w = static_cast<char*>(ws);
-  const size_t part = up256((size_t)p.nsplit * p.nk * p.Hk * p.d * sizeof(float));
+  p.dsum = reinterpret_cast<float*>(w);
+  w += up256((size_t)p.H * p.nq * sizeof(float));
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  cudaError_t e = launch_xattn_dsum(p, bf16, s);
+  if (e != cudaSuccess) return UT_ERR_CUDA;
+  if (bf16) return status_of(launch_xattn_bwd_tc(p, w, s));
   p.part_dk = reinterpret_cast<float*>(w);
-  p.part_dv = reinterpret_cast<float*>(w + part);
-  p.dsum = reinterpret_cast<float*>(w + 2 * part);
-  return status_of(launch_xattn_bwd_simt(p, shape->dtype == UT_BF16, static_cast<cudaStream_t>(stream)));
+  p.part_dv = reinterpret_cast<float*>(w + up256((size_t)p.nsplit * p.nk * p.Hk * p.d * sizeof(float)));
+  return status_of(launch_xattn_bwd_simt(p, s));
 }
 
 size_t ut_group_norm_fwd_workspace_size(const ut_gnorm_shape* shape) {

@@ -21,8 +21,8 @@ struct XattnParams {
   int sms;
   // Work split over the long axis: keys in the forward (part_o [nsplit, nq,
   // H, d] unnormalised, part_ml [nsplit, nq, H] the running maximum in the
-  // base-2 domain and the sum), query rows in the backward (part_dk, part_dv
-  // [nsplit, nk, Hk, d]).
+  // base-2 domain and the sum), query rows in the fp32 backward (part_dk,
+  // part_dv [nsplit, nk, Hk, d]).
   int nsplit;
   float* part_o; float2* part_ml;
   float* dsum;                           // [H, nq] D = dO . O
@@ -37,6 +37,10 @@ int64_t xattn_fwd_tc_items(const XattnParams& p);
 cudaError_t launch_xattn_fwd_simt(const XattnParams& p, cudaStream_t s);  // fp32
 cudaError_t launch_xattn_fwd_tc(const XattnParams& p, cudaStream_t s);    // bf16
 cudaError_t launch_xattn_join(const XattnParams& p, bool bf16, cudaStream_t s);  // of the forward's key splits
-cudaError_t launch_xattn_bwd_simt(const XattnParams& p, bool bf16, cudaStream_t s);
+int64_t xattn_bwd_tc_items(const XattnParams& p);
+size_t xattn_bwd_tc_ws(const XattnParams& p);
+cudaError_t launch_xattn_dsum(const XattnParams& p, bool bf16, cudaStream_t s);  // D, and the check of the prefixes
+cudaError_t launch_xattn_bwd_simt(const XattnParams& p, cudaStream_t s);         // fp32, after D
+cudaError_t launch_xattn_bwd_tc(const XattnParams& p, void* ws, cudaStream_t s); // bf16, after D
 
 }  // namespace ut

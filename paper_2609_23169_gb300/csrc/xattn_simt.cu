@@ -429,7 +429,6 @@ __global__ void __launch_bounds__(256) xattn_dsum_kernel(const XattnParams p) {
 }
 
 // dK, dV = the sum of the splits' partials, in split order; 4 values a thread
-template <typename T>
 __global__ void __launch_bounds__(256) xattn_dkdv_join_kernel(const XattnParams p) {
   const int64_t x = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;
   const int per_row = p.Hk * p.d / 4;
@@ -449,7 +448,7 @@ __global__ void __launch_bounds__(256) xattn_dkdv_join_kernel(const XattnParams 
       a.w += b.w;
     }
     const float f = which ? 1.f : p.scale;
-    st4(static_cast<T*>(which ? p.dv : p.dk) + key * (which ? p.dvs : p.dks) + e,
+    st4(static_cast<float*>(which ? p.dv : p.dk) + key * (which ? p.dvs : p.dks) + e,
         make_float4(a.x * f, a.y * f, a.z * f, a.w * f));
   }
 }
@@ -513,8 +512,6 @@ static cudaError_t bwd(const XattnParams& p, cudaStream_t s) {
   cudaError_t e = cudaSuccess;
   const size_t tiles = sizeof(float) * 4 * kXs * (D + 4), pair = sizeof(float) * kXs * kXsLdP,
                vecs = sizeof(float) * 3 * kXs;
-  e = launch(xattn_dsum_kernel<T, D>, dim3((unsigned)((p.nq * p.H + 16) / 16)), 0, p, s);
-  if (e != cudaSuccess) return e;
   if (p.nq > 0) {
     e = launch(xattn_dq_simt_kernel<T, D>, dim3((unsigned)segment_slots(p.nq, p.B, kXs / p.G), p.Hk),
                tiles + pair + vecs, p, s);
@@ -524,19 +521,20 @@ static cudaError_t bwd(const XattnParams& p, cudaStream_t s) {
     e = launch(xattn_dkdv_simt_kernel<T, D>, dim3((unsigned)segment_slots(p.nk, p.B, kXs), p.Hk, p.nsplit),
                tiles + 2 * pair + vecs, p, s);
     if (e != cudaSuccess) return e;
-    e = launch(xattn_dkdv_join_kernel<T>, dim3((unsigned)((p.nk * p.Hk * D / 4 + 255) / 256)), 0, p, s);
+    e = launch(xattn_dkdv_join_kernel, dim3((unsigned)((p.nk * p.Hk * D / 4 + 255) / 256)), 0, p, s);
   }
   return e;
 }
 
 int64_t xattn_items(const XattnParams& p, bool bf16, bool backward) {
-  if (backward) return segment_slots(p.nk, p.B, kXs) * p.Hk;
-  return bf16 ? xattn_fwd_tc_items(p) : segment_slots(p.nq, p.B, kXs / p.G) * p.Hk;
+  if (bf16) return backward ? xattn_bwd_tc_items(p) : xattn_fwd_tc_items(p);
+  return (backward ? segment_slots(p.nk, p.B, kXs) : segment_slots(p.nq, p.B, kXs / p.G)) * p.Hk;
 }
 
 // Enough parts for two blocks an SM, but none shorter than two tiles of an
 // average segment.
 int xattn_splits(const XattnParams& p, bool bf16, bool backward) {
+  if (bf16 && backward) return 1;
   const int64_t items = xattn_items(p, bf16, backward), want = (2 * (int64_t)p.sms + items - 1) / items;
   const int64_t tile = backward ? kXs / p.G : (bf16 ? 128 : kXs);
   const int64_t tiles = ((backward ? p.nq : p.nk) / p.B + tile - 1) / tile, most = tiles / 2;
@@ -557,8 +555,16 @@ cudaError_t launch_xattn_join(const XattnParams& p, bool bf16, cudaStream_t s) {
                    : launch(xattn_join_kernel<float, 128>, grid, 0, p, s);
 }
 
-cudaError_t launch_xattn_bwd_simt(const XattnParams& p, bool bf16, cudaStream_t s) {
-  if (bf16) return p.d == 64 ? bwd<__nv_bfloat16, 64>(p, s) : bwd<__nv_bfloat16, 128>(p, s);
+cudaError_t launch_xattn_dsum(const XattnParams& p, bool bf16, cudaStream_t s) {
+  const dim3 grid((unsigned)((p.nq * p.H + 16) / 16));
+  if (bf16)
+    return p.d == 64 ? launch(xattn_dsum_kernel<__nv_bfloat16, 64>, grid, 0, p, s)
+                     : launch(xattn_dsum_kernel<__nv_bfloat16, 128>, grid, 0, p, s);
+  return p.d == 64 ? launch(xattn_dsum_kernel<float, 64>, grid, 0, p, s)
+                   : launch(xattn_dsum_kernel<float, 128>, grid, 0, p, s);
+}
+
+cudaError_t launch_xattn_bwd_simt(const XattnParams& p, cudaStream_t s) {
   return p.d == 64 ? bwd<float, 64>(p, s) : bwd<float, 128>(p, s);
 }
 

@@ -64,6 +64,31 @@ UT_DEV void mma_tn128(uint32_t d, uint32_t a, uint32_t b_lo, uint32_t idesc, uin
       : "memory");
 }
 
+#define UT_SS2_STEP(aoff, boff, acc)                                     \
+  "add.u32 x, %1, " aoff ";\n\tadd.u32 y, %2, " boff ";\n\t"            \
+  "mov.b64 a, {x, %5};\n\tmov.b64 b, {y, %5};\n\t"                     \
+  "@e tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, " acc ";\n\t"
+#define UT_SS2_HEAD                                                                \
+  "{\n\t.reg .pred e, p, t;\n\t.reg .b64 a, b;\n\t.reg .b32 x, y;\n\t"          \
+  "setp.ne.b32 p, %4, 0;\n\tsetp.eq.b32 t, 0, 0;\n\telect.sync _|e, 0xffffffff;\n\t"
+// d (+)= A B over 128 rows of B: A a K-major tile of 128 columns in two
+// sub-tiles, B row-major (MN-major operand)
+UT_DEV void mma_nn128(uint32_t d, uint32_t a_lo, uint32_t b_lo, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(UT_SS2_HEAD UT_SS2_STEP("0", "0", "p") UT_SS2_STEP("2", "128", "t") UT_SS2_STEP("4", "256", "t")
+                   UT_SS2_STEP("6", "384", "t") UT_SS2_STEP("1024", "512", "t") UT_SS2_STEP("1026", "640", "t")
+                       UT_SS2_STEP("1028", "768", "t") UT_SS2_STEP("1030", "896", "t") "}" ::"r"(d),
+               "r"(a_lo), "r"(b_lo), "r"(idesc), "r"(accumulate), "r"(kDescHi)
+               : "memory");
+}
+// d = A^T B over 128 rows of both, each row-major (MN-major operands)
+UT_DEV void mma_tt128(uint32_t d, uint32_t a_lo, uint32_t b_lo, uint32_t idesc) {
+  asm volatile(UT_SS2_HEAD UT_SS2_STEP("0", "0", "p") UT_SS2_STEP("128", "128", "t") UT_SS2_STEP("256", "256", "t")
+                   UT_SS2_STEP("384", "384", "t") UT_SS2_STEP("512", "512", "t") UT_SS2_STEP("640", "640", "t")
+                       UT_SS2_STEP("768", "768", "t") UT_SS2_STEP("896", "896", "t") "}" ::"r"(d),
+               "r"(a_lo), "r"(b_lo), "r"(idesc), "r"(0u), "r"(kDescHi)
+               : "memory");
+}
+
 // This lane's four keys of a block (lane + 32 g): bit g set where the key
 // exists and is not masked.
 UT_DEV uint32_t lane_keys(const uint8_t* mask, int64_t key, int left, uint32_t lane) {
