@@ -13,28 +13,29 @@
 //     S^T  = K_j Q_t^T        (TMEM lanes = keys)
 //     dP^T = V_j dO_t^T
 //     dV_j += P^T dO_t,  dK_j += dS^T Q_t     (TMEM, over the tiles of the group)
-//     dQ_t^T = K_j^T dS^T
+//     dQ_t = dS K_j           (TMEM lanes = query rows)
 // so S and dP are computed once per pair, and one CTA sees all key blocks of a
 // query tile: its dQ is added up in a buffer of the CTA's own (kSub tiles in
 // fp32, 512 KB at d = 128, 78 MB over the device: it stays in L2), first
 // block stored, middle ones added, the last one read, added and written as
 // bf16, always by the same thread.  No clear, no second pass, no atomic whose
 // order changes the result.  A segment of one key block needs no buffer.
-// dK_j, dV_j of an item go to partial sums of their own (part [P, nk, Hk, d],
-// the item's place in its segment first), which a last kernel adds in order.
+// dK_j, dV_j of an item go to partial sums of their own (by the item's place
+// in its segment), which a last kernel adds in order.  Both buffers hold
+// 16-byte pieces of neighbouring rows side by side, as the threads (a row
+// each) write and read them.
 //
 // Roles (512 threads, registers rebalanced with setmaxnreg):
-//   warp 0        TMA: lane 0 K, V and the Q ring, lane 1 dO
+//   warp 0        TMA: K, V and the Q ring
 //   warp 1        TMEM owner and MMA issuer
 //   warp 2        zeroes the rows of a Q tile that are not this item's (past
-//   warp 3        the segment's end, or between the rows of G heads and 128),
-//                 warp 3 those of dO and the masked keys of K: what they hold
-//                 (NaN, infinities) must not enter a sum over rows
+//                 the segment's end, or between the rows of G heads and 128):
+//                 what they hold (NaN, infinities) must not enter a sum over rows
+//   warp 3        TMA: dO; zeroes its rows likewise, and the masked keys of K
 //   warps 4-11    P^T and dS^T as bf16 into shared tiles; dK, dV out
-//   warps 12-15   dQ^T out of TMEM (lane = d)
-// TMEM columns: S^T / dP^T [0,128), dQ^T [128,256), dV [256,256+d), dK
-// [384,384+d).  For d = 64 the A operand K^T of dQ^T is padded to 128 rows by
-// a zero sub-tile after K.
+//   warps 12-15   dQ out of TMEM (thread = row)
+// TMEM columns: S^T / dP^T [0,128), dQ [128,128+d), dV [256,256+d), dK
+// [384,384+d).
 // Every wait is bounded; on expiry the kernel records UT_ERR_TIMEOUT, drains
 // its own copies and MMAs, frees TMEM and returns.
 #include "common.cuh"
@@ -49,7 +50,7 @@ namespace {
 constexpr int kT = 128;  // rows of a tile, keys of a block
 constexpr int kSub = 8;  // query tiles whose dQ a CTA adds up at a time
 constexpr int kThreads = 512;
-constexpr int kRegLaunch = 128, kRegCtl = 96, kRegEw = 168, kRegDrain = 80;
+constexpr int kRegLaunch = 128, kRegCtl = 80, kRegEw = 160, kRegDrain = 112;
 static_assert(kRegCtl + 2 * kRegEw + kRegDrain == 4 * kRegLaunch, "setmaxnreg split must match the launch");
 constexpr uint32_t kChunkB = 128 * 128;  // 128 rows x 64 bf16
 constexpr int kQStages = 2;
@@ -59,7 +60,7 @@ template <int D>
 struct BwdSmem {
   static constexpr int kC = D / 64;
   static constexpr uint32_t kTile = kT * D * 2;
-  alignas(1024) uint8_t k[2 * kChunkB];
+  alignas(1024) uint8_t k[kTile];
   alignas(1024) uint8_t v[kTile];
   alignas(1024) uint8_t pt[2 * kChunkB];
   alignas(1024) uint8_t dst[2 * kChunkB];
@@ -83,13 +84,16 @@ struct BwdParams {
   int64_t slots;    // items along the query rows
   int64_t n_items;
   float scale_log2;
-  float* dq_acc;    // [grid, kSub * 128, d]
+  int64_t kslots;   // key blocks of all segments (with idle ones): nk / 128 + n_seg
+  bool wide;        // dq takes 32-byte stores
+  float* dq_acc;    // [grid, kSub, d / 4, 128, 4]
 };
 
 struct Work {  // one item
   int hk, part, tiles, blocks;
   int64_t tok0, key0;
   int ntok, keys;  // tokens and keys of the item
+  int64_t kslot;   // first key block's place among all segments'
 };
 
 // Item u; false where its slot is idle.
@@ -106,22 +110,29 @@ UT_DEV bool decode(const BwdParams& b, int64_t u, Work& w) {
   w.ntok = (int)min((int64_t)b.R * b.tpt, g.n - t0);
   w.tiles = (w.ntok + b.tpt - 1) / b.tpt;
   w.key0 = k0;
+  w.kslot = k0 / kT + g.s;
   w.keys = (int)kn;
   w.blocks = (int)((kn + kT - 1) / kT);
   return true;
 }
 
-UT_DEV void red_add(float* p, float v) {
-  asm volatile("red.relaxed.gpu.global.add.f32 [%0], %1;" ::"l"(p), "f"(v) : "memory");
-}
 UT_DEV void red_add4(float* p, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
   asm volatile("red.relaxed.gpu.global.add.v4.f32 [%0], {%1, %2, %3, %4};" ::"l"(p), "f"(__uint_as_float(a)), "f"(__uint_as_float(b)),
                "f"(__uint_as_float(c)), "f"(__uint_as_float(d))
                : "memory");
 }
-UT_DEV float ld_l2(const float* p) {
-  float v;
-  asm volatile("ld.relaxed.gpu.global.f32 %0, [%1];" : "=f"(v) : "l"(p) : "memory");
+// a whole 32-byte sector (a pair of 16-byte stores would write it in halves)
+UT_DEV void st_v8(void* p, const uint32_t (&v)[8]) {
+  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(v[0]), "r"(v[1]), "r"(v[2]),
+               "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7])
+               : "memory");
+}
+UT_DEV float4 ld_l2(const float* p) {
+  float4 v;
+  asm volatile("ld.relaxed.gpu.global.v4.f32 {%0, %1, %2, %3}, [%4];"
+               : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w)
+               : "l"(p)
+               : "memory");
   return v;
 }
 UT_DEV void tmem_ld64(uint32_t taddr, uint32_t* r) {
@@ -149,11 +160,6 @@ __global__ void __launch_bounds__(kThreads, 1)
   if ((smem_u32(smem_raw) & 1023u) != 0) {
     if (threadIdx.x == 0) set_status(p.status, UT_ERR_INVALID_ARG);
     return;
-  }
-  if (D == 64) {
-    uint4* z = reinterpret_cast<uint4*>(sm.k + kChunkB);
-    for (uint32_t x = threadIdx.x; x < kChunkB / 16; x += kThreads) z[x] = make_uint4(0, 0, 0, 0);
-    fence_proxy_async_smem();
   }
   if (threadIdx.x == 0) {
     uint64_t* one[] = {&sm.kv_full, &sm.kv_ready, &sm.kv_empty, &sm.do_full, &sm.do_ready, &sm.do_empty, &sm.s_full,
@@ -200,8 +206,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   if (wg == 0) {
     setmaxnreg_dec<kRegCtl>();
     if (warp == 0) {
-      if (lane < 2) {
-        const bool is_q = lane == 0;
+      if (lane == 0) {
         const uint64_t first_pol = policy_evict_first(), keep = policy_evict_last();
         const uint32_t bytes = (uint32_t)prm.tpt * p.G * 128 * S::kC;
         uint32_t nkv = 0, nt = 0;
@@ -212,42 +217,33 @@ __global__ void __launch_bounds__(kThreads, 1)
           const int step = group_of(w);
           for (int s0 = 0; s0 < w.tiles && ok; s0 += step)
             for (int j = 0; j < w.blocks && ok; ++j) {
-              if (is_q) {
-                if (!(ok = wait1(&sm.kv_empty, (nkv & 1) ^ 1))) break;
-                mbar_expect_tx(&sm.kv_full, 2 * S::kTile);
-                for (int c = 0; c < S::kC; ++c) {
-                  tma_load_3d(sm.k + c * kChunkB, &tm_k, &sm.kv_full, c * 64, w.hk, (int)w.key0 + j * kT, keep);
-                  tma_load_3d(sm.v + c * kChunkB, &tm_v, &sm.kv_full, c * 64, w.hk, (int)w.key0 + j * kT, keep);
-                }
-                ++nkv;
+              if (!(ok = wait1(&sm.kv_empty, (nkv & 1) ^ 1))) break;
+              mbar_expect_tx(&sm.kv_full, 2 * S::kTile);
+              for (int c = 0; c < S::kC; ++c) {
+                tma_load_3d(sm.k + c * kChunkB, &tm_k, &sm.kv_full, c * 64, w.hk, (int)w.key0 + j * kT, keep);
+                tma_load_3d(sm.v + c * kChunkB, &tm_v, &sm.kv_full, c * 64, w.hk, (int)w.key0 + j * kT, keep);
               }
-              // the last pass over a tile is the last reader of its rows
+              ++nkv;
+              // the last block's pass over a tile is the last reader of its rows
               const uint64_t pol = j == w.blocks - 1 ? first_pol : keep;
-              for (int t = s0; t < min(s0 + step, w.tiles) && ok; ++t, ++nt) {
-                const uint32_t st = is_q ? nt % kQStages : 0, f = is_q ? nt / kQStages : nt;
-                uint64_t* empty = is_q ? &sm.q_empty[st] : &sm.do_empty;
-                uint64_t* full = is_q ? &sm.q_full[st] : &sm.do_full;
-                if (!(ok = wait1(empty, (f & 1) ^ 1))) break;
-                mbar_expect_tx(full, bytes);
-                uint8_t* dst = is_q ? sm.q[st] : sm.dout;
+              for (int t = s0; t < min(s0 + step, w.tiles); ++t, ++nt) {
+                const uint32_t st = nt % kQStages;
+                if (!(ok = wait1(&sm.q_empty[st], ((nt / kQStages) & 1) ^ 1))) break;
+                mbar_expect_tx(&sm.q_full[st], bytes);
                 for (int c = 0; c < S::kC; ++c)
-                  tma_load_3d(dst + c * kChunkB, is_q ? &tm_q : &tm_do, full, c * 64, w.hk * p.G,
+                  tma_load_3d(sm.q[st] + c * kChunkB, &tm_q, &sm.q_full[st], c * 64, w.hk * p.G,
                               (int)w.tok0 + t * prm.tpt, pol);
               }
             }
         }
-        if (is_q) {
-          if (nkv > 0) drain(&sm.kv_full, (nkv - 1) & 1);
-          for (uint32_t x = nt > kQStages ? nt - kQStages : 0; x < nt; ++x)
-            drain(&sm.q_full[x % kQStages], (x / kQStages) & 1);
-        } else if (nt > 0) {
-          drain(&sm.do_full, (nt - 1) & 1);
-        }
+        if (nkv > 0) drain(&sm.kv_full, (nkv - 1) & 1);
+        for (uint32_t x = nt > kQStages ? nt - kQStages : 0; x < nt; ++x)
+          drain(&sm.q_full[x % kQStages], (x / kQStages) & 1);
       }
     } else if (warp == 1) {
       constexpr uint32_t idesc_s = idesc_bf16_f32(kT, kT, false, false);
       constexpr uint32_t idesc_acc = idesc_bf16_f32(kT, D, false, true);
-      constexpr uint32_t idesc_dq = idesc_bf16_f32(kT, kT, true, true);
+      constexpr uint32_t idesc_dq = idesc_bf16_f32(kT, D, true, true);
       const uint32_t k_lo = desc_lo(smem_u32(sm.k), 16), v_lo = desc_lo(smem_u32(sm.v), 16),
                      q_lo = desc_lo(smem_u32(sm.q[0]), 16), do_lo = desc_lo(smem_u32(sm.dout), 16),
                      pt_lo = desc_lo(smem_u32(sm.pt), 16), dst_lo = desc_lo(smem_u32(sm.dst), 16);
@@ -298,10 +294,10 @@ __global__ void __launch_bounds__(kThreads, 1)
               tc_fence_after();
               mma_nn128(kColDk, dst_lo, q_mn + qst * (S::kTile >> 4), idesc_acc, t > 0);
               mma_commit_w(&sm.q_empty[qst]);
-              // dQ^T = K^T dS^T once the previous one has been read
+              // dQ = dS K once the previous one has been read
               if (!(ok = wait(&sm.dq_empty, par ^ 1))) break;
               tc_fence_after();
-              mma_tt128(kColDq, k_mn, dst_mn, idesc_dq);
+              mma_tt128(kColDq, dst_mn, k_mn, idesc_dq);
               mma_commit_w(&sm.ds_done);
             }
             if (!ok) break;
@@ -313,9 +309,10 @@ __global__ void __launch_bounds__(kThreads, 1)
       mma_commit_w(&sm.mma_done);
       drain(&sm.mma_done, 0);
     } else {
-      // ------------------------------------------- rows that must read as zero
+      // ------------- rows that must read as zero (warp 2: Q, warp 3: dO, K); dO loads
       const bool is_q = warp == 2;
-      const uint32_t kv_base = smem_u32(sm.k);
+      const uint32_t kv_base = smem_u32(sm.k), bytes = (uint32_t)prm.tpt * p.G * 128 * S::kC;
+      const uint64_t first_pol = policy_evict_first(), keep = policy_evict_last();
       uint32_t nkv = 0, nt = 0;
       bool ok = true;
       for (int64_t u = blockIdx.x; u < prm.n_items && ok; u += gridDim.x) {
@@ -324,22 +321,32 @@ __global__ void __launch_bounds__(kThreads, 1)
         const int step = group_of(w);
         for (int s0 = 0; s0 < w.tiles && ok; s0 += step)
           for (int j = 0; j < w.blocks && ok; ++j) {
-            if (!is_q) {
-              const uint32_t keys = lane_keys(p.mask, w.key0 + j * kT, w.keys - j * kT, lane);
-              if (!(ok = wait(&sm.kv_full, nkv & 1))) break;
-              if (__any_sync(0xffffffffu, keys != 15u)) {
-                for (int g = 0; g < 4; ++g)
-                  if (!((keys >> g) & 1u))
-                    for (int x = 0; x < 8 * S::kC; ++x)
-                      st_shared_v4(kv_base + (x >> 3) * kChunkB + (lane + 32 * g) * 128 + (((x + lane) & 7) << 4), 0,
-                                   0, 0, 0);
-                fence_proxy_async_smem();
+            for (int t = s0; t < min(s0 + step, w.tiles); ++t, ++nt) {
+              if (!is_q) {
+                if (!(ok = wait(&sm.do_empty, (nt & 1) ^ 1))) break;
+                if (lane == 0) {
+                  mbar_expect_tx(&sm.do_full, bytes);
+                  for (int c = 0; c < S::kC; ++c)
+                    tma_load_3d(sm.dout + c * kChunkB, &tm_do, &sm.do_full, c * 64, w.hk * p.G,
+                                (int)w.tok0 + t * prm.tpt, j == w.blocks - 1 ? first_pol : keep);
+                }
                 __syncwarp();
+                if (t == s0) {
+                  const uint32_t keys = lane_keys(p.mask, w.key0 + j * kT, w.keys - j * kT, lane);
+                  if (!(ok = wait(&sm.kv_full, nkv & 1))) break;
+                  if (__any_sync(0xffffffffu, keys != 15u)) {
+                    for (int g = 0; g < 4; ++g)
+                      if (!((keys >> g) & 1u))
+                        for (int x = 0; x < 8 * S::kC; ++x)
+                          st_shared_v4(kv_base + (x >> 3) * kChunkB + (lane + 32 * g) * 128 + (((x + lane) & 7) << 4),
+                                       0, 0, 0, 0);
+                    fence_proxy_async_smem();
+                    __syncwarp();
+                  }
+                  if (lane == 0) mbar_arrive(&sm.kv_ready);
+                  ++nkv;
+                }
               }
-              if (lane == 0) mbar_arrive(&sm.kv_ready);
-              ++nkv;
-            }
-            for (int t = s0; t < min(s0 + step, w.tiles) && ok; ++t, ++nt) {
               const int rows = min(prm.tpt, w.ntok - t * prm.tpt) * p.G;
               const uint32_t st = is_q ? nt % kQStages : 0, f = is_q ? nt / kQStages : nt;
               if (!(ok = wait(is_q ? &sm.q_full[st] : &sm.do_full, f & 1))) break;
@@ -351,6 +358,10 @@ __global__ void __launch_bounds__(kThreads, 1)
               if (lane == 0) mbar_arrive(is_q ? &sm.q_ready[st] : &sm.do_ready);
             }
           }
+      }
+      if (!is_q) {  // every copy it issued has landed (the last may not have been waited for on an abort)
+        const bool fine = __all_sync(0xffffffffu, ok);
+        if (!fine && lane == 0 && nt > 0) drain(&sm.do_full, (nt - 1) & 1);
       }
     }
   } else if (wg < 3) {
@@ -424,34 +435,23 @@ __global__ void __launch_bounds__(kThreads, 1)
             if (lane == 0) mbar_arrive(&sm.pt_full);
             if (!(ok = wait(&sm.dp_full, par))) break;
             tc_fence_after();
+            uint32_t r[HC];
+            tmem_ld64(lane_base + half * HC, r);
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&sm.dp_empty);  // S^T of the next tile may be computed
 #pragma unroll
-            for (int hh = 0; hh < 2; ++hh) {
-              uint32_t r[32];
-              tmem_ld32(lane_base + half * HC + hh * 32, r);
-              tmem_wait_ld();
-              if (hh == 1) {
-                tc_fence_before();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(&sm.dp_empty);
-              }
-              uint32_t ds[16];
-#pragma unroll
-              for (int x = 0; x < 32; x += 4) {
-                const float4 d4 = *reinterpret_cast<const float4*>(dv + hh * 32 + x);
-                const float* pp = pr + hh * 32 + x;
-                ds[x / 2] = pack_bf16x2(pp[0] * (__uint_as_float(r[x]) - d4.x),
-                                        pp[1] * (__uint_as_float(r[x + 1]) - d4.y)) & on;
-                ds[x / 2 + 1] = pack_bf16x2(pp[2] * (__uint_as_float(r[x + 2]) - d4.z),
-                                            pp[3] * (__uint_as_float(r[x + 3]) - d4.w)) & on;
-              }
-              // the previous dK and dQ^T have read the dS^T tile
-              if (hh == 0 && !(ok = wait(&sm.ds_done, par ^ 1))) break;
-#pragma unroll
-              for (int x = 0; x < 4; ++x)
-                st_shared_v4(dst_row + (((hh * 4 + x) ^ (krow & 7)) << 4), ds[4 * x], ds[4 * x + 1], ds[4 * x + 2],
-                             ds[4 * x + 3]);
+            for (int x = 0; x < HC; x += 4) {
+              const float4 d4 = *reinterpret_cast<const float4*>(dv + x);
+              r[x / 2] = pack_bf16x2(pr[x] * (__uint_as_float(r[x]) - d4.x),
+                                     pr[x + 1] * (__uint_as_float(r[x + 1]) - d4.y)) & on;
+              r[x / 2 + 1] = pack_bf16x2(pr[x + 2] * (__uint_as_float(r[x + 2]) - d4.z),
+                                         pr[x + 3] * (__uint_as_float(r[x + 3]) - d4.w)) & on;
             }
-            if (!ok) break;
+            if (!(ok = wait(&sm.ds_done, par ^ 1))) break;  // the previous dK and dQ have read the dS^T tile
+#pragma unroll
+            for (int x = 0; x < HC / 8; ++x)
+              st_shared_v4(dst_row + ((x ^ (krow & 7)) << 4), r[4 * x], r[4 * x + 1], r[4 * x + 2], r[4 * x + 3]);
             fence_proxy_async_smem();
             __syncwarp();
             if (lane == 0) mbar_arrive(&sm.dst_full);
@@ -460,24 +460,20 @@ __global__ void __launch_bounds__(kThreads, 1)
           // dV, dK of the group: stored by the item's first group, added by the others
           if (!(ok = wait(&sm.acc_full, ng & 1))) break;
           tc_fence_after();
-          const int64_t at = (((int64_t)w.part * p.nk + w.key0 + key) * p.Hk + w.hk) * D + half * HD;
+          const int64_t at = ((((int64_t)w.part * prm.kslots + w.kslot + j) * p.Hk + w.hk) * (D / 4) + half * (HD / 4)) * kT + krow;
 #pragma unroll
           for (int which = 0; which < 2; ++which) {
-            float* dst = (which ? p.part_dk : p.part_dv) + at;
+            float* dst = (which ? p.part_dk : p.part_dv) + at * 4;
 #pragma unroll
             for (int g = 0; g < HD / 32; ++g) {
               uint32_t r[32];
               tmem_ld32(lane_base + (which ? kColDk : kColDv) + half * HD + g * 32, r);
               tmem_wait_ld();
-              if (key < w.keys) {
-                if (s0 == 0) {
 #pragma unroll
-                  for (int x = 0; x < 32; x += 4)
-                    *reinterpret_cast<uint4*>(dst + g * 32 + x) = make_uint4(r[x], r[x + 1], r[x + 2], r[x + 3]);
-                } else {
-#pragma unroll
-                  for (int x = 0; x < 32; x += 4) red_add4(dst + g * 32 + x, r[x], r[x + 1], r[x + 2], r[x + 3]);
-                }
+              for (int x = 0; x < 8; ++x) {
+                float* at4 = dst + (g * 8 + x) * kT * 4;
+                if (s0 == 0) *reinterpret_cast<uint4*>(at4) = make_uint4(r[4 * x], r[4 * x + 1], r[4 * x + 2], r[4 * x + 3]);
+                else red_add4(at4, r[4 * x], r[4 * x + 1], r[4 * x + 2], r[4 * x + 3]);
               }
             }
           }
@@ -488,76 +484,89 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
   } else {
     setmaxnreg_dec<kRegDrain>();
-    // dQ^T: TMEM lane = d, column = query row
-    const uint32_t quarter = warp & 3, dcol = quarter * 32 + lane;
-    const uint32_t lane_base = (quarter * 32) << 16;
-    float* acc = prm.dq_acc + (int64_t)blockIdx.x * kSub * kT * D + dcol;
+    // dQ: TMEM lane = query row, column = d
+    const uint32_t quarter = warp & 3, row = quarter * 32 + lane, lane_base = (quarter * 32) << 16;
+    const int rt = (int)((row * prm.inv_g) >> 16);
+    const int64_t row_off = (int64_t)rt * p.dqs + (int)(row - rt * p.G) * D;
+    // the CTA's buffer: 16-byte pieces, [tile][d / 4][row]
+    float* acc = prm.dq_acc + ((int64_t)blockIdx.x * kSub * (D / 4) * kT + row) * 4;
     uint32_t nt = 0;
     bool ok = true;
-    // two rows' values of this lane's d -> bf16 pairs: even lanes take the first row, odd lanes the second
-    auto send = [&](float a, float b, int r, int rows, __nv_bfloat16* out) {
-      const bool odd = lane & 1;
-      const float got = __shfl_xor_sync(0xffffffffu, odd ? a : b, 1);
-      const uint32_t v = odd ? pack_bf16x2(got, b) : pack_bf16x2(a, got);
-      const int row = r + (odd ? 1 : 0), rt = (int)(((uint32_t)row * prm.inv_g) >> 16);
-      if (row < rows && dcol < (uint32_t)D)
-        *reinterpret_cast<uint32_t*>(out + (int64_t)rt * p.dqs + (row - rt * p.G) * D + (dcol & ~1u)) = v;
-    };
     for (int64_t u = blockIdx.x; u < prm.n_items && ok; u += gridDim.x) {
       Work w;
       if (!decode(prm, u, w)) continue;
       const int step = group_of(w);
-      for (int s0 = 0; s0 < w.tiles && ok; s0 += max(step, 1)) {
-        if (w.blocks == 0) {  // no keys: dQ = 0
-          for (int t = s0; t < w.tiles; ++t) {
-            const int rows = min(prm.tpt, w.ntok - t * prm.tpt) * p.G;
-            __nv_bfloat16* out = static_cast<__nv_bfloat16*>(p.dq) + (w.tok0 + (int64_t)t * prm.tpt) * p.dqs +
-                                 (int64_t)w.hk * p.G * D;
-            for (int x = 0; x < kT; x += 2) send(0.f, 0.f, x, rows, out);
-          }
-          break;
-        }
-        for (int j = 0; j < w.blocks && ok; ++j)
+      __nv_bfloat16* out0 = static_cast<__nv_bfloat16*>(p.dq) + w.tok0 * p.dqs + (int64_t)w.hk * p.G * D + row_off;
+      if (w.blocks == 0) {  // no keys: dQ = 0
+        for (int t = 0; t < w.tiles; ++t)
+          if (rt < min(prm.tpt, w.ntok - t * prm.tpt))
+            for (int x = 0; x < D; x += 8)
+              *reinterpret_cast<uint4*>(out0 + (int64_t)t * prm.tpt * p.dqs + x) = make_uint4(0, 0, 0, 0);
+        continue;
+      }
+      for (int s0 = 0; s0 < w.tiles && ok; s0 += step)
+        for (int j = 0; j < w.blocks && ok; ++j) {
+          const bool last = j == w.blocks - 1, add = j > 0;
           for (int t = s0; t < min(s0 + step, w.tiles); ++t, ++nt) {
+            float* a = acc + (int64_t)(t - s0) * (D / 4) * kT * 4;
+            const bool there = rt < min(prm.tpt, w.ntok - t * prm.tpt);
+            __nv_bfloat16* out = out0 + (int64_t)t * prm.tpt * p.dqs;
+            float4 pre[16];  // the sum so far, 64 columns at a time, the first before the wait
+            if (last && add) {
+#pragma unroll
+              for (int x = 0; x < 16; ++x) pre[x] = ld_l2(a + x * kT * 4);
+            }
             if (!(ok = wait(&sm.ds_done, nt & 1))) break;
             tc_fence_after();
-            const int rows = min(prm.tpt, w.ntok - t * prm.tpt) * p.G;
-            __nv_bfloat16* out = static_cast<__nv_bfloat16*>(p.dq) + (w.tok0 + (int64_t)t * prm.tpt) * p.dqs +
-                                 (int64_t)w.hk * p.G * D;
-            float* a = acc + (int64_t)(t - s0) * kT * D;
-#pragma unroll 1
-            for (int g = 0; g < 4; ++g) {
-              uint32_t r[32];
-              tmem_ld32(lane_base + kColDq + g * 32, r);
+#pragma unroll
+            for (int g = 0; g < D / 16; ++g) {
+              uint32_t r[16];
+              tmem_ld16(lane_base + kColDq + g * 16, r);
               tmem_wait_ld();
-              if (g == 3) {
+              if (g == D / 16 - 1) {
                 tc_fence_before();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&sm.dq_empty);
               }
-              float* ag = a + g * 32 * D;
-              if (j < w.blocks - 1) {
-                if (dcol < (uint32_t)D) {
-                  if (j == 0) {
+              float* ag = a + g * 4 * kT * 4;
+              if (!last) {
 #pragma unroll
-                    for (int x = 0; x < 32; ++x) ag[x * D] = __uint_as_float(r[x]);
-                  } else {
-#pragma unroll
-                    for (int x = 0; x < 32; ++x) red_add(ag + x * D, __uint_as_float(r[x]));
-                  }
+                for (int x = 0; x < 4; ++x) {
+                  if (add) red_add4(ag + x * kT * 4, r[4 * x], r[4 * x + 1], r[4 * x + 2], r[4 * x + 3]);
+                  else
+                    *reinterpret_cast<uint4*>(ag + x * kT * 4) =
+                        make_uint4(r[4 * x], r[4 * x + 1], r[4 * x + 2], r[4 * x + 3]);
                 }
                 continue;
               }
-              if (j > 0 && dcol < (uint32_t)D) {
+              float v[16];
 #pragma unroll
-                for (int x = 0; x < 32; ++x) r[x] = __float_as_uint(__uint_as_float(r[x]) + ld_l2(ag + x * D));
+              for (int x = 0; x < 16; ++x) v[x] = __uint_as_float(r[x]);
+              if (add) {
+#pragma unroll
+                for (int x = 0; x < 4; ++x) {
+                  const float4 f = pre[(g & 3) * 4 + x];
+                  v[4 * x] += f.x;
+                  v[4 * x + 1] += f.y;
+                  v[4 * x + 2] += f.z;
+                  v[4 * x + 3] += f.w;
+                  if (g + 4 < D / 16) pre[(g & 3) * 4 + x] = ld_l2(ag + (16 + x) * kT * 4);
+                }
               }
+              if (there) {
+                uint32_t o[8];
 #pragma unroll
-              for (int x = 0; x < 32; x += 2)
-                send(__uint_as_float(r[x]) * p.scale, __uint_as_float(r[x + 1]) * p.scale, g * 32 + x, rows, out);
+                for (int y = 0; y < 8; ++y) o[y] = pack_bf16x2(v[2 * y] * p.scale, v[2 * y + 1] * p.scale);
+                if (prm.wide) {
+                  st_v8(out + g * 16, o);
+                } else {
+                  *reinterpret_cast<uint4*>(out + g * 16) = make_uint4(o[0], o[1], o[2], o[3]);
+                  *reinterpret_cast<uint4*>(out + g * 16 + 8) = make_uint4(o[4], o[5], o[6], o[7]);
+                }
+              }
             }
           }
-      }
+        }
     }
   }
   tc_fence_before();
@@ -566,42 +575,45 @@ __global__ void __launch_bounds__(kThreads, 1)
   if (warp == 1) tmem_dealloc(sm.tmem_base, 512);
 }
 
-// dK, dV: the sum of the partials of the key's segment, in order; 4 values a thread
+// dK, dV: the sum of the partials of the key's segment, in order.  grid (key
+// slots, kv heads, dK / dV), a block one key block: read 16 bytes a thread
+// along the keys, written as rows through shared memory.
+template <int D>
 __global__ void __launch_bounds__(256) xattn_bwd_join_kernel(const BwdParams prm) {
+  __shared__ __align__(16) uint8_t rows[kT * (D * 2 + 16)];
   const XattnParams& p = prm.x;
-  const int64_t x = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;
-  const int per_row = p.Hk * p.d / 4;
-  const int64_t n = p.nk * per_row;
-  if (x >= n) return;
-  const int64_t key = x / per_row;
-  const int e = (int)(x % per_row) * 4;
-  int s = 0;
-  if (p.cu_k) {  // the last segment that starts at or before the key and is not empty there
-    int hi = p.B;
-    while (hi - s > 1) {
-      const int mid = (s + hi) >> 1;
-      if (p.cu_k[mid] <= key) s = mid;
-      else hi = mid;
-    }
-  }
+  const Segment g = segment_of_slot(p.cu_k, p.B, p.nk, kT, blockIdx.x);
+  const int keys = (int)min((int64_t)kT, g.n - g.tile * kT);
+  if (keys <= 0) return;
   int64_t row, nq;
-  segment_rows(p.cu_q, s, p.nq, row, nq);
+  segment_rows(p.cu_q, g.s, p.nq, row, nq);
   const int64_t tiles = (nq + prm.tpt - 1) / prm.tpt;
   const int parts = (int)((tiles + prm.R - 1) / prm.R);
-#pragma unroll
-  for (int which = 0; which < 2; ++which) {
-    const float* src = (which ? p.part_dv : p.part_dk) + x * 4;
+  const int64_t kslot = min(g.row / kT + g.s + g.tile, prm.kslots - 1);
+  const bool is_k = blockIdx.z == 0;
+  const float* src = (is_k ? p.part_dk : p.part_dv) + (kslot * p.Hk + blockIdx.y) * (D * kT);
+  const int64_t step = prm.kslots * p.Hk * (D * kT);
+  const float f = is_k ? p.scale : 1.f;
+  for (int x = threadIdx.x; x < D / 4 * kT; x += 256) {
     float4 a = make_float4(0, 0, 0, 0);
+#pragma unroll 4
     for (int i = 0; i < parts; ++i) {
-      const float4 b = *reinterpret_cast<const float4*>(src + (int64_t)i * n * 4);
+      const float4 b = *reinterpret_cast<const float4*>(src + i * step + x * 4);
       a.x += b.x;
       a.y += b.y;
       a.z += b.z;
       a.w += b.w;
     }
-    const float f = which ? 1.f : p.scale;
-    __nv_bfloat16* dst = static_cast<__nv_bfloat16*>(which ? p.dv : p.dk) + key * (which ? p.dvs : p.dks) + e;
-    *reinterpret_cast<uint2*>(dst) = make_uint2(pack_bf16x2(a.x * f, a.y * f), pack_bf16x2(a.z * f, a.w * f));
+    *reinterpret_cast<uint2*>(rows + (x % kT) * (D * 2 + 16) + (x / kT) * 8) =
+        make_uint2(pack_bf16x2(a.x * f, a.y * f), pack_bf16x2(a.z * f, a.w * f));
+  }
+  __syncthreads();
+  __nv_bfloat16* out = static_cast<__nv_bfloat16*>(is_k ? p.dk : p.dv) + (int64_t)blockIdx.y * D;
+  const int64_t stride = is_k ? p.dks : p.dvs;
+  for (int x = threadIdx.x; x < keys * (D / 8); x += 256) {
+    const int r = x / (D / 8), e = x % (D / 8);
+    *reinterpret_cast<uint4*>(out + (g.row + g.tile * kT + r) * stride + e * 8) =
+        *reinterpret_cast<const uint4*>(rows + r * (D * 2 + 16) + e * 16);
   }
 }
 
@@ -642,16 +654,17 @@ int tiles_per_item(const XattnParams& p) {
     }
   }
   if (best_use == 0.0) best = tiles;  // more kv heads than four waves
-  const int64_t part = 2 * p.nk * p.Hk * p.d * (int64_t)sizeof(float);
+  const int64_t part = 2 * segment_slots(p.nk, p.B, kT) * kT * p.Hk * p.d * (int64_t)sizeof(float);
   const int64_t most = ((int64_t)1 << 30) / (part > 0 ? part : 1);
   const int64_t least = most > 0 ? (tiles + most - 1) / most : tiles;
   if (best < least) best = least;
   return (int)(best < 1 ? 1 : best);
 }
 
-int64_t parts_of(const XattnParams& p, int R) {
+// one of the two partial sums: [parts of a segment, key slots, kv heads, d / 4, 128, 4]
+size_t part_bytes(const XattnParams& p, int R) {
   const int64_t tpt = kT / p.G, tiles = (p.nq + tpt - 1) / tpt;
-  return (tiles + R - 1) / R;
+  return (size_t)((tiles + R - 1) / R) * segment_slots(p.nk, p.B, kT) * p.Hk * p.d * kT * sizeof(float);
 }
 
 }  // namespace
@@ -662,8 +675,7 @@ int64_t xattn_bwd_tc_items(const XattnParams& p) {
 
 // partial dK, dV; the CTAs' dQ buffers
 size_t xattn_bwd_tc_ws(const XattnParams& p) {
-  const size_t part = (size_t)parts_of(p, tiles_per_item(p)) * p.nk * p.Hk * p.d * sizeof(float);
-  return 2 * ((part + 255) & ~(size_t)255) + (size_t)p.sms * kSub * kT * p.d * sizeof(float);
+  return 2 * part_bytes(p, tiles_per_item(p)) + (size_t)p.sms * kSub * kT * p.d * sizeof(float);
 }
 
 cudaError_t launch_xattn_bwd_tc(const XattnParams& p, void* ws, cudaStream_t s) {
@@ -672,7 +684,9 @@ cudaError_t launch_xattn_bwd_tc(const XattnParams& p, void* ws, cudaStream_t s) 
   prm.inv_g = (65536u + p.G - 1) / p.G;
   prm.tpt = kT / p.G;
   prm.R = tiles_per_item(p);
-  const size_t part = ((size_t)parts_of(p, prm.R) * p.nk * p.Hk * p.d * sizeof(float) + 255) & ~(size_t)255;
+  const size_t part = part_bytes(p, prm.R);
+  prm.kslots = segment_slots(p.nk, p.B, kT);
+  prm.wide = (reinterpret_cast<uintptr_t>(p.dq) & 31u) == 0 && (p.dqs * 2) % 32 == 0;
   prm.x.part_dk = static_cast<float*>(ws);
   prm.x.part_dv = reinterpret_cast<float*>(static_cast<char*>(ws) + part);
   prm.dq_acc = reinterpret_cast<float*>(static_cast<char*>(ws) + 2 * part);
@@ -695,8 +709,9 @@ cudaError_t launch_xattn_bwd_tc(const XattnParams& p, void* ws, cudaStream_t s) 
     if (e != cudaSuccess) return e;
   }
   if (p.nk > 0) {
-    const int64_t n = p.nk * p.Hk * p.d / 4;
-    xattn_bwd_join_kernel<<<(unsigned)((n + 255) / 256), 256, 0, s>>>(prm);
+    const dim3 grid((unsigned)prm.kslots, p.Hk, 2);
+    if (p.d == 64) xattn_bwd_join_kernel<64><<<grid, 256, 0, s>>>(prm);
+    else xattn_bwd_join_kernel<128><<<grid, 256, 0, s>>>(prm);
     e = cudaGetLastError();
   }
   return e;
