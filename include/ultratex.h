@@ -412,7 +412,7 @@ typedef struct {
   int64_t n_rows;         /* rows of all segments, >= 0 */
   int32_t n_seg;          /* segments, >= 1 */
   int32_t channels;       /* C <= 8192, C * element size a multiple of 16 bytes */
-  int32_t groups;         /* divides channels */
+  int32_t groups;         /* divides channels; channels + groups <= 12288 */
   int32_t dtype;          /* ut_dtype of x, y, dy, dx */
   int32_t act;            /* UT_ACT_NONE or UT_ACT_SILU */
   float eps;              /* > 0 */

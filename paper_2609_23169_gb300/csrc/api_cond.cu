@@ -100,7 +100,7 @@ static ut_status gnorm_problem(const ut_gnorm_shape* s, bool backward, GnormPara
     if (strides[i] < s->channels || (strides[i] * esz) % 16 != 0 || strides[i] > ((int64_t)1 << 38) / esz)
       return UT_ERR_INVALID_ARG;
   }
-  if (s->channels > kGnMaxChannels) return UT_ERR_UNSUPPORTED;
+  if (s->channels > kGnMaxChannels || s->channels + s->groups > kGnMaxBoth) return UT_ERR_UNSUPPORTED;
   if (s->n_rows > INT32_MAX / 2 || s->n_seg > INT32_MAX / 4) return UT_ERR_UNSUPPORTED;
   *p = GnormParams{};
   p->n = s->n_rows;
@@ -114,7 +114,7 @@ static ut_status gnorm_problem(const ut_gnorm_shape* s, bool backward, GnormPara
   p->act = s->act;
   p->eps = s->eps;
   p->sms = device_sms();
-  p->R = gnorm_rows_per_slot(p->n, p->C, (int)esz, p->sms);
+  p->timeout_ns = wait_timeout_ns();
   return UT_OK;
 }
 

@@ -16,15 +16,16 @@ struct GnormParams {
   int64_t xs, ys, dys, dxs;                // elements between rows
   int B, C, G, act;
   float eps;
-  int R;                                   // rows of a slot
+  int64_t batch_rows;                      // rows of a batch of segments
+  int slots, slot_bytes, ring_at;          // the ring in shared memory
+  uint64_t timeout_ns;
   void* ws;
   int sms;
 };
 
-constexpr int kGnMaxChannels = 8192;
+constexpr int kGnMaxChannels = 8192, kGnMaxBoth = 12288;  // channels; channels + groups (shared memory)
 
 size_t gnorm_ws(const GnormParams& p, bool backward);
-int gnorm_rows_per_slot(int64_t n, int C, int elem, int sms);
 cudaError_t launch_gnorm_fwd(const GnormParams& p, bool bf16, cudaStream_t s);
 cudaError_t launch_gnorm_bwd(const GnormParams& p, bool bf16, cudaStream_t s);
 
