@@ -28,7 +28,8 @@
 // differences from its first row, and the windows' means and squared distances
 // merged pairwise,
 //   M2 = M2a + M2b + (mean_b - mean_a)^2 na nb / (na + nb),
-// so a mean far from zero costs no digits.  All sums are in 32 bits, of a
+// so a mean far from zero costs no digits; means are averaged as differences
+// from one of them, so that equal values have themselves as their mean.  All sums are in 32 bits, of a
 // window first and of windows then, in an order that the sizes fix.
 #include <cooperative_groups.h>
 #include <math.h>
@@ -36,6 +37,7 @@
 #include "common.cuh"
 #include "gnorm.cuh"
 #include "kernels.h"
+#include "pairs.cuh"
 #include "segments.cuh"
 
 namespace ut {
@@ -48,35 +50,72 @@ constexpr int kFwdThreads = 480, kBwdThreads = 352;
 constexpr int kFwdPer = 4, kBwdPer = 2;              // rows of a chunk for each thread
 constexpr int kWindow = 16;                          // rows summed before they are merged (forward)
 constexpr int kMaxSlots = 16;
-constexpr int64_t kBatchBytes = 64ll << 20;          // of the tensors read, per batch
-constexpr size_t kSmem = 227 * 1024;
+constexpr int64_t kBatchBytes = 128ll << 20;          // of the tensors read, per batch
+constexpr size_t kSmem = 225 * 1024;                 // with 2 KB of static shared memory
 
 template <typename T>
-struct Vec;  // 16 bytes of channels
+struct Vec;  // 16 bytes of channels as pairs of fp32
 template <>
 struct Vec<float> {
   static constexpr int n = 4;
-  UT_DEV static void unpack(const uint4& u, float (&v)[4]) { *reinterpret_cast<uint4*>(v) = u; }
-  UT_DEV static uint4 pack(const float (&v)[4]) { return *reinterpret_cast<const uint4*>(v); }
+  UT_DEV static void unpack(const uint4& u, uint64_t (&v)[2]) {
+    v[0] = pack_u32x2(u.x, u.y);
+    v[1] = pack_u32x2(u.z, u.w);
+  }
+  UT_DEV static uint4 pack(const uint64_t (&v)[2]) {
+    float a, b, c, d;
+    unpack_f32x2(v[0], a, b);
+    unpack_f32x2(v[1], c, d);
+    return make_uint4(__float_as_uint(a), __float_as_uint(b), __float_as_uint(c), __float_as_uint(d));
+  }
 };
 template <>
 struct Vec<__nv_bfloat16> {
   static constexpr int n = 8;
-  UT_DEV static void unpack(const uint4& u, float (&v)[8]) {
+  UT_DEV static void unpack(const uint4& u, uint64_t (&v)[4]) {
     const uint32_t w[4] = {u.x, u.y, u.z, u.w};
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      v[2 * i] = __uint_as_float(w[i] << 16);
-      v[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
-    }
+    for (int i = 0; i < 4; ++i) v[i] = pack_u32x2(w[i] << 16, w[i] & 0xFFFF0000u);
   }
-  UT_DEV static uint4 pack(const float (&v)[8]) {
-    return make_uint4(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]),
-                      pack_bf16x2(v[6], v[7]));
+  UT_DEV static uint4 pack(const uint64_t (&v)[4]) {
+    uint32_t w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      float a, b;
+      unpack_f32x2(v[i], a, b);
+      w[i] = pack_bf16x2(a, b);
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
   }
 };
 
-UT_DEV float sigmoid(float u) { return __fdividef(1.f, 1.f + __expf(-u)); }
+UT_DEV uint64_t both(float x) { return pack_f32x2(x, x); }
+
+UT_DEV float rcp_approx(float x) {
+  float y;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+// 1 / (1 + exp(-u)) of a pair: two units of the special function pipe each,
+// relative error below 2^-21 (exp(-u) = infinity gives 0)
+UT_DEV uint64_t sigmoid2(uint64_t u) {
+  float a, b;
+  unpack_f32x2(mul_f32x2(u, both(-1.4426950408889634f)), a, b);
+  unpack_f32x2(add_f32x2(pack_f32x2(ex2_approx(a), ex2_approx(b)), both(1.f)), a, b);
+  return pack_f32x2(rcp_approx(a), rcp_approx(b));
+}
+
+// (n, mean, M2) of two sets of values
+struct Stat {
+  float n, mean, m2;
+  UT_DEV void add(float nb, float mb, float qb) {
+    if (nb <= 0.f) return;
+    const float tot = n + nb, w = nb * rcp_approx(tot), d = mb - mean;
+    m2 += fmaf(d * d, n * w, qb);
+    mean = fmaf(d, w, mean);
+    n = tot;
+  }
+};
 
 // A block's threads over a row: `cols` 16-byte columns from col0, `lanes` rows
 // at a time.
@@ -91,28 +130,35 @@ struct Layout {
     lane = threadIdx.x / cols;
     on = lane < lanes;
   }
-  UT_DEV int rows_of(int l, int64_t n) const { return l < n ? (int)((n - l + lanes - 1) / lanes) : 0; }
-};
+  };
 
-// Segments [s0, s1) with rows [row, row + n): as many whole segments as `most`
-// rows hold, at least one.
+// Row counts fit 32 bits (at most 2^30 rows): 64-bit divisions cost hundreds
+// of cycles each, on the path of every launch.
+UT_DEV void rows_of_segment(const GnormParams& p, int s, int& row, int& n) {
+  int64_t a, len;
+  segment_rows(p.cu, s, p.n, a, len);
+  row = (int)a;
+  n = (int)len;
+}
+
+// Segments [s0, s1) with rows [row, row + n): as many whole segments as
+// p.batch_rows hold, at least one.
 struct Batch {
-  int s0, s1;
-  int64_t row, n;
+  int s0, s1, row, n;
 };
 UT_DEV Batch batch_from(const GnormParams& p, int s0) {
   Batch b{s0, p.B, 0, 0};
-  int64_t row, n;
-  segment_rows(p.cu, s0, p.n, row, n);
+  int row, n;
+  rows_of_segment(p, s0, row, n);
   b.row = row;
-  if (p.n - row <= p.batch_rows || !p.cu) {
-    b.n = p.n - row;
+  if (!p.cu || p.n - row <= p.batch_rows) {
+    b.n = (int)p.n - row;
     return b;
   }
-  int64_t end = row + n;
+  int end = row + n;
   b.s1 = s0 + 1;
   while (b.s1 < p.B) {
-    segment_rows(p.cu, b.s1, p.n, row, n);
+    rows_of_segment(p, b.s1, row, n);
     if (row + n - b.row > p.batch_rows) break;
     end = max(end, row + n);
     ++b.s1;
@@ -123,22 +169,21 @@ UT_DEV Batch batch_from(const GnormParams& p, int s0) {
 
 // The blocks' shares of a batch: n / blocks rows each, the first n % blocks one more.
 struct Shares {
-  int64_t row, each;
-  int more, blocks;
+  int row, each, more, blocks;
   UT_DEV Shares(const Batch& b, int blocks_) : row(b.row), blocks(blocks_) {
     each = b.n / blocks;
-    more = (int)(b.n - each * blocks);
+    more = b.n - each * blocks;
   }
-  UT_DEV int64_t first(int block) const { return row + each * block + min(block, more); }
+  UT_DEV int first(int block) const { return row + each * block + min(block, more); }
   // the block that has row r (in range whatever cu holds)
-  UT_DEV int owner(int64_t r) const {
-    const int64_t at = r - row, big = (each + 1) * more;
-    const int64_t c = at < big ? at / (each + 1) : more + (at - big) / (each > 0 ? each : 1);
-    return (int)(c < 0 ? 0 : c < blocks ? c : blocks - 1);
+  UT_DEV int owner(int r) const {
+    const int at = r - row, big = (each + 1) * more;
+    const int c = at < big ? at / (each + 1) : more + (at - big) / max(each, 1);
+    return max(0, min(c, blocks - 1));
   }
 };
 // The last segment of the batch that starts at or before row r.
-UT_DEV int segment_at(const GnormParams& p, const Batch& b, int64_t r) {
+UT_DEV int segment_at(const GnormParams& p, const Batch& b, int r) {
   if (!p.cu) return 0;
   int lo = b.s0, hi = b.s1;
   while (hi - lo > 1) {
@@ -151,12 +196,12 @@ UT_DEV int segment_at(const GnormParams& p, const Batch& b, int64_t r) {
 
 // Calls f(segment, first row, end) for the pieces of rows [a, e).
 template <typename F>
-UT_DEV void for_pieces(const GnormParams& p, const Batch& b, int64_t a, int64_t e, F f) {
+UT_DEV void for_pieces(const GnormParams& p, const Batch& b, int a, int e, F f) {
   if (a >= e) return;
   for (int s = segment_at(p, b, a); s < b.s1; ++s) {
-    int64_t row, n;
-    segment_rows(p.cu, s, p.n, row, n);
-    const int64_t lo = max(a, row), hi = min(e, row + n);
+    int row, n;
+    rows_of_segment(p, s, row, n);
+    const int lo = max(a, row), hi = min(e, row + n);
     if (row >= e) break;
     if (lo < hi) f(s, lo, hi);
   }
@@ -175,8 +220,8 @@ struct Chunks {
     rows = kThreads / cols * kPer;
   }
   UT_DEV int slab_cols(int slab) const { return min(cols, cv - slab * kThreads); }
-  UT_DEV int64_t row_chunks(int64_t n) const { return (n + rows - 1) / rows; }
-  UT_DEV int64_t of_piece(int64_t n) const { return slabs * row_chunks(n); }
+  UT_DEV int row_chunks(int n) const { return (n + rows - 1) / rows; }
+  UT_DEV int of_piece(int n) const { return slabs * row_chunks(n); }
 };
 
 struct RingState {
@@ -218,7 +263,7 @@ UT_DEV void bulk_load(void* dst, const void* src, uint32_t bytes, uint64_t* bar)
 
 // Rows [r, r + n) of a slab of 16-byte columns -> shared memory, packed; the
 // whole producer warp.
-UT_DEV void load_rows(uint8_t* dst, const void* x, int64_t row_stride, int64_t r, int n, int col, int cols,
+UT_DEV void load_rows(uint8_t* dst, const void* x, int64_t row_stride, int r, int n, int col, int cols,
                       uint64_t* bar) {
   const uint8_t* src = static_cast<const uint8_t*>(x) + r * row_stride + (int64_t)col * 16;
   const uint32_t bytes = (uint32_t)cols * 16;
@@ -236,12 +281,12 @@ UT_DEV void sync_compute() {  // the computing warps
 
 // Pieces of rows [a, e), last first.
 template <typename F>
-UT_DEV void for_pieces_back(const GnormParams& p, const Batch& b, int64_t a, int64_t e, F f) {
+UT_DEV void for_pieces_back(const GnormParams& p, const Batch& b, int a, int e, F f) {
   if (a >= e) return;
   for (int s = segment_at(p, b, e - 1); s >= b.s0; --s) {
-    int64_t row, n;
-    segment_rows(p.cu, s, p.n, row, n);
-    const int64_t lo = max(a, row), hi = min(e, row + n);
+    int row, n;
+    rows_of_segment(p, s, row, n);
+    const int lo = max(a, row), hi = min(e, row + n);
     if (lo < hi) f(s, lo, hi);
     if (row <= a) break;
   }
@@ -249,9 +294,9 @@ UT_DEV void for_pieces_back(const GnormParams& p, const Batch& b, int64_t a, int
 
 // The producer's part of both passes over a batch: tensors x (and dy).
 template <int kThreads, int kPer, int kTensors>
-UT_DEV void produce(const GnormParams& p, const Batch& b, int64_t a, int64_t e, const Chunks<kThreads, kPer>& ck,
-                    Ring& ring, int64_t total, int elem) {
-  auto load = [&](int at, int slab, int64_t r, int n) {
+UT_DEV void produce(const GnormParams& p, const Batch& b, int a, int e, const Chunks<kThreads, kPer>& ck,
+                    Ring& ring, int total, int elem) {
+  auto load = [&](int at, int slab, int r, int n) {
     ring.wait_empty(at);
     uint64_t* bar = &ring.st->full[at];
     const int cols = ck.slab_cols(slab);
@@ -263,22 +308,21 @@ UT_DEV void produce(const GnormParams& p, const Batch& b, int64_t a, int64_t e, 
       load_rows(dst + ring.slot_bytes / 2, p.dy, p.dys * elem, r, n, slab * kThreads, cols, bar);
   };
   int slot = 0;
-  for_pieces(p, b, a, e, [&](int s, int64_t lo, int64_t hi) {
+  for_pieces(p, b, a, e, [&](int s, int lo, int hi) {
     for (int slab = 0; slab < ck.slabs; ++slab)
-      for (int64_t r = lo; r < hi; r += ck.rows, slot = ring.next(slot))
-        load(slot, slab, r, (int)min((int64_t)ck.rows, hi - r));
+      for (int r = lo; r < hi; r += ck.rows, slot = ring.next(slot)) load(slot, slab, r, min(ck.rows, hi - r));
   });
   cooperative_groups::this_grid().sync();
   // backwards; the last `slots` chunks are there
-  int64_t i = total - 1;
+  int i = total - 1;
   slot = ring.before(slot);
-  for_pieces_back(p, b, a, e, [&](int s, int64_t lo, int64_t hi) {
-    const int64_t n = ck.row_chunks(hi - lo);
+  for_pieces_back(p, b, a, e, [&](int s, int lo, int hi) {
+    const int n = ck.row_chunks(hi - lo);
     for (int slab = ck.slabs - 1; slab >= 0; --slab)
-      for (int64_t c = n - 1; c >= 0; --c, --i, slot = ring.before(slot))
+      for (int c = n - 1; c >= 0; --c, --i, slot = ring.before(slot))
         if (total - 1 - i >= ring.slots) {
-          const int64_t r = lo + c * ck.rows;
-          load(slot, slab, r, (int)min((int64_t)ck.rows, hi - r));
+          const int r = lo + c * ck.rows;
+          load(slot, slab, r, min(ck.rows, hi - r));
         }
   });
 }
@@ -304,19 +348,38 @@ UT_DEV float warp_sum(float x) {
   return x;
 }
 
-// mean, rstd and the affine of a thread's channels
+// gamma and beta are first read behind the first chunk or the grid barrier:
+// fetch them while that is awaited.
+UT_DEV void prefetch_affine(const GnormParams& p) {
+  for (int c = threadIdx.x * 32; c < p.C; c += blockDim.x * 32) {
+    if (p.gamma) asm volatile("prefetch.global.L1 [%0];" ::"l"(p.gamma + c));
+    if (p.beta) asm volatile("prefetch.global.L1 [%0];" ::"l"(p.beta + c));
+  }
+}
+
+// A thread's channels: their groups' values of a [G] table, their affine.
 template <int V>
 struct Channels {
-  float mean[V], rstd[V], gamma[V], beta[V];
+  uint64_t neg_mean[V / 2], rstd[V / 2], gamma[V / 2], beta[V / 2];
   UT_DEV void load(const GnormParams& p, const float2* stat, int c0) {
     const int cpg = p.C / p.G;
+    int g = c0 / cpg, left = cpg - (c0 - g * cpg);  // channels left in group g
 #pragma unroll
-    for (int c = 0; c < V; ++c) {
-      const float2 m = stat[(c0 + c) / cpg];
-      mean[c] = m.x;
-      rstd[c] = m.y;
-      gamma[c] = p.gamma ? p.gamma[c0 + c] : 1.f;
-      beta[c] = p.beta ? p.beta[c0 + c] : 0.f;
+    for (int c = 0; c < V; c += 2) {
+      float m[2], r[2];
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        m[x] = stat[g].x;
+        r[x] = stat[g].y;
+        if (--left == 0) {
+          ++g;
+          left = cpg;
+        }
+      }
+      neg_mean[c / 2] = pack_f32x2(-m[0], -m[1]);
+      rstd[c / 2] = pack_f32x2(r[0], r[1]);
+      gamma[c / 2] = p.gamma ? pack_f32x2(p.gamma[c0 + c], p.gamma[c0 + c + 1]) : both(1.f);
+      beta[c / 2] = p.beta ? pack_f32x2(p.beta[c0 + c], p.beta[c0 + c + 1]) : both(0.f);
     }
   }
 };
@@ -326,35 +389,44 @@ struct Channels {
 // present window as differences from its first.
 template <int V>
 struct Moments {
-  float mean[V], m2[V], first[V], sum[V], sq[V];
+  float mean[V], m2[V];
+  uint64_t neg_first[V / 2], sum[V / 2], sq[V / 2];
   float cnt, have;
   UT_DEV Moments() : cnt(0.f), have(0.f) {
 #pragma unroll
-    for (int c = 0; c < V; ++c) mean[c] = m2[c] = first[c] = sum[c] = sq[c] = 0.f;
+    for (int c = 0; c < V; ++c) mean[c] = m2[c] = 0.f;
+#pragma unroll
+    for (int c = 0; c < V / 2; ++c) neg_first[c] = sum[c] = sq[c] = 0;
   }
-  UT_DEV void add(const float (&v)[V]) {
-    if (have == 0.f) {
+  UT_DEV void begin(const uint64_t (&v)[V / 2]) {  // the window's first row
 #pragma unroll
-      for (int c = 0; c < V; ++c) first[c] = v[c];
-    }
+    for (int c = 0; c < V / 2; ++c) neg_first[c] = mul_f32x2(v[c], both(-1.f));
+  }
+  UT_DEV void add(const uint64_t (&v)[V / 2]) {
 #pragma unroll
-    for (int c = 0; c < V; ++c) {
-      const float d = v[c] - first[c];
-      sum[c] += d;
-      sq[c] = fmaf(d, d, sq[c]);
+    for (int c = 0; c < V / 2; ++c) {
+      const uint64_t d = add_f32x2(v[c], neg_first[c]);
+      sum[c] = add_f32x2(sum[c], d);
+      sq[c] = fma_f32x2(d, d, sq[c]);
     }
-    have += 1.f;
   }
   UT_DEV void merge() {  // the window into the mean and M2
     if (have == 0.f) return;
     const float tot = cnt + have, wb = have / tot, wm = cnt * wb, inv = 1.f / have;
 #pragma unroll
-    for (int c = 0; c < V; ++c) {
-      const float off = sum[c] * inv, q = fmaf(-off, sum[c], sq[c]);
-      const float d = first[c] + off - mean[c];
-      m2[c] += fmaf(d * d, wm, q > 0.f || q != q ? q : 0.f);
-      mean[c] = fmaf(d, wb, mean[c]);
-      sum[c] = sq[c] = 0.f;
+    for (int i = 0; i < V / 2; ++i) {
+      float f[2], s[2], q[2];
+      unpack_f32x2(neg_first[i], f[0], f[1]);
+      unpack_f32x2(sum[i], s[0], s[1]);
+      unpack_f32x2(sq[i], q[0], q[1]);
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        const int c = 2 * i + x;
+        const float off = s[x] * inv, m = fmaf(-off, s[x], q[x]), d = off - f[x] - mean[c];
+        m2[c] += fmaf(d * d, wm, m > 0.f || m != m ? m : 0.f);
+        mean[c] = fmaf(d, wb, mean[c]);
+      }
+      sum[i] = sq[i] = 0;
     }
     cnt = tot;
     have = 0.f;
@@ -369,9 +441,12 @@ __global__ void __launch_bounds__(kFwdThreads + 32, 1) gn_fwd_kernel(const Gnorm
   float2* lane_stat = reinterpret_cast<float2*>(smem + sizeof(RingState) + 8);  // [V][threads]
   float2* chan = lane_stat + V * kFwdThreads;                                            // [C]
   float2* stat = chan + p.C;                                                    // [G]: mean, rstd
+  __shared__ float warp_rows[kFwdThreads / 32];
   const int blocks = gridDim.x, me = blockIdx.x, cpg = p.C / p.G;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const float inv_cpg = 1.f / (float)cpg;
   const Chunks<kFwdThreads, kFwdPer> ck(p.C / V);
+  prefetch_affine(p);
   Ring ring{st, smem + p.ring_at, p.slots, p.slot_bytes, p.status, p.timeout_ns, 0, 0};
   float2* part0 = static_cast<float2*>(p.ws);
   ring_init<kFwdThreads>(st, p.slots);
@@ -391,126 +466,187 @@ __global__ void __launch_bounds__(kFwdThreads + 32, 1) gn_fwd_kernel(const Gnorm
     s0 = b.s1;
     float2* part = part0 + (int64_t)(nb & 1) * (blocks + p.B) * p.G;  // two batches may be under way
     const Shares sh(b, blocks);
-    const int64_t a = sh.first(me), e = sh.first(me + 1);
-    int64_t total = 0;  // chunks
-    for_pieces(p, b, a, e, [&](int, int64_t lo, int64_t hi) { total += ck.of_piece(hi - lo); });
+    const int a = sh.first(me), e = sh.first(me + 1);
+    int total = 0;  // chunks
+    for_pieces(p, b, a, e, [&](int, int lo, int hi) { total += ck.of_piece(hi - lo); });
     if (warp == kFwdThreads / 32) {
       produce<kFwdThreads, kFwdPer, 1>(p, b, a, e, ck, ring, total, sizeof(T));
       continue;
     }
-    int64_t i = 0;
-    int slot = 0;
-    for_pieces(p, b, a, e, [&](int s, int64_t lo, int64_t hi) {
-      const int64_t n = hi - lo;
+    int i = 0, slot = 0;
+    for_pieces(p, b, a, e, [&](int s, int lo, int hi) {
+      const int n = hi - lo;
       for (int slab = 0; slab < ck.slabs; ++slab) {
         const Layout<kFwdThreads> L(ck.cv, slab * kFwdThreads);
         Moments<V> mo;
-        for (int64_t r = 0; r < n; r += ck.rows, ++i, slot = ring.next(slot)) {
+        for (int r = 0; r < n; r += ck.rows, ++i, slot = ring.next(slot)) {
           ring.wait_full(slot);
           if (L.on) {
             const uint8_t* src = ring.mem + (int64_t)slot * ring.slot_bytes + (L.lane * L.cols + L.col - slab * kFwdThreads) * 16;
+            const int step = L.lanes * L.cols * 16;
+            uint64_t v[V / 2];
+            if (r + ck.rows <= n) {  // a full chunk
+              uint4 w[kFwdPer];
 #pragma unroll
-            for (int k = 0; k < kFwdPer; ++k)
-              if (r + L.lane + k * L.lanes < n) {
-                float v[V];
-                Vec<T>::unpack(*reinterpret_cast<const uint4*>(src + k * L.lanes * L.cols * 16), v);
+              for (int k = 0; k < kFwdPer; ++k) w[k] = *reinterpret_cast<const uint4*>(src + k * step);
+              if (mo.have == 0.f) {
+                Vec<T>::unpack(w[0], v);
+                mo.begin(v);
+              }
+#pragma unroll
+              for (int k = 0; k < kFwdPer; ++k) {
+                Vec<T>::unpack(w[k], v);
                 mo.add(v);
               }
+              mo.have += (float)kFwdPer;
+            } else {
+              for (int k = 0; k < kFwdPer && r + L.lane + k * L.lanes < n; ++k) {
+                Vec<T>::unpack(*reinterpret_cast<const uint4*>(src + k * step), v);
+                if (mo.have == 0.f) mo.begin(v);
+                mo.add(v);
+                mo.have += 1.f;
+              }
+            }
             if (mo.have >= (float)kWindow) mo.merge();
           }
           if (i + ring.slots < total) ring.release(slot);  // else it stays for the second pass
         }
         mo.merge();
         sync_compute<kFwdThreads>();
+        // over the lanes of a column, a thread a channel
 #pragma unroll
         for (int c = 0; c < V; ++c) lane_stat[c * kFwdThreads + threadIdx.x] = make_float2(mo.mean[c], mo.m2[c]);
         sync_compute<kFwdThreads>();
-        for (int ch = threadIdx.x; ch < L.cols * V; ch += kFwdThreads) {
-          const float2* ls = lane_stat + (ch % V) * kFwdThreads + ch / V;
+        const int each = n / L.lanes, more = n - each * L.lanes;  // rows of a lane
+        const float inv = 1.f / (float)n;
+        for (int x = threadIdx.x; x < L.cols * V; x += kFwdThreads) {
+          const int c = x / L.cols, col = x - c * L.cols;
+          const float2* ls = lane_stat + c * kFwdThreads + col;
           float m = 0.f, q = 0.f;
-          for (int l = 0; l < L.lanes; ++l) m = fmaf((float)L.rows_of(l, n), ls[l * L.cols].x, m);
-          m /= (float)n;
+#pragma unroll 8
+          for (int l = 0; l < L.lanes; ++l) m = fmaf((float)(each + (l < more)), ls[l * L.cols].x - ls[0].x, m);
+          m = fmaf(m, inv, ls[0].x);
+#pragma unroll 8
           for (int l = 0; l < L.lanes; ++l) {
             const float2 t = ls[l * L.cols];
-            q += fmaf((float)L.rows_of(l, n) * (t.x - m), t.x - m, t.y);
+            q += fmaf((float)(each + (l < more)) * (t.x - m), t.x - m, t.y);
           }
-          chan[slab * kFwdThreads * V + ch] = make_float2(m, q);
+          chan[(slab * kFwdThreads + col) * V + c] = make_float2(m, q);
         }
       }
       sync_compute<kFwdThreads>();
-      for (int g = warp; g < p.G; g += kFwdThreads / 32) {
+      // over the channels of a group, p.group_lanes threads a group
+      for (int g0 = 0; g0 < p.G; g0 += kFwdThreads / p.group_lanes) {
+        const int g = g0 + threadIdx.x / p.group_lanes, l = threadIdx.x % p.group_lanes;
+        const bool on = g < p.G && threadIdx.x < kFwdThreads / p.group_lanes * p.group_lanes;
+        const float2* cs = chan + g * cpg;
         float m = 0.f, q = 0.f;
-        for (int c = lane; c < cpg; c += 32) m += chan[g * cpg + c].x;
-        m = warp_sum(m) / (float)cpg;
-        for (int c = lane; c < cpg; c += 32) {
-          const float2 t = chan[g * cpg + c];
-          q += fmaf((float)n * (t.x - m), t.x - m, t.y);
-        }
-        q = warp_sum(q);
-        if (lane == 0) part[(int64_t)(me + s) * p.G + g] = make_float2(m, q);
+        if (on)
+          for (int c = l; c < cpg; c += p.group_lanes) m += cs[c].x - cs[0].x;
+        for (int o = p.group_lanes / 2; o; o >>= 1) m += __shfl_xor_sync(0xffffffffu, m, o);
+        if (on) m = fmaf(m, inv_cpg, cs[0].x);
+        if (on)
+          for (int c = l; c < cpg; c += p.group_lanes) {
+            const float2 t = cs[c];
+            q += fmaf((float)n * (t.x - m), t.x - m, t.y);
+          }
+        for (int o = p.group_lanes / 2; o; o >>= 1) q += __shfl_xor_sync(0xffffffffu, q, o);
+        if (on && l == 0) part[(int64_t)(me + s) * p.G + g] = make_float2(m, q);
       }
     });
     cooperative_groups::this_grid().sync();
     i = total - 1;
     slot = ring.before(slot);
-    for_pieces_back(p, b, a, e, [&](int s, int64_t lo, int64_t hi) {
-      int64_t row, n;
-      segment_rows(p.cu, s, p.n, row, n);
+    for_pieces_back(p, b, a, e, [&](int s, int lo, int hi) {
+      int row, n;
+      rows_of_segment(p, s, row, n);
       const int c0 = sh.owner(row), c1 = sh.owner(row + n - 1);
       sync_compute<kFwdThreads>();
-      for (int g = warp; g < p.G; g += kFwdThreads / 32) {  // the segment's statistics from its pieces'
-        auto rows = [&](int c) {
-          return (float)(min(sh.first(c + 1), row + n) - max(sh.first(c), row));
-        };
-        float m = 0.f, q = 0.f;
-        for (int c = c0 + lane; c <= c1; c += 32) {
-          const float k = rows(c);
-          if (k > 0.f) m = fmaf(k, part[(int64_t)(c + s) * p.G + g].x, m);
-        }
-        m = warp_sum(m) / (float)n;
-        for (int c = c0 + lane; c <= c1; c += 32) {
-          const float k = rows(c);
-          if (k > 0.f) {
-            const float2 t = part[(int64_t)(c + s) * p.G + g];
-            q += fmaf(k * (float)cpg * (t.x - m), t.x - m, t.y);
+      // the segment's statistics from its pieces': lanes over the groups, warps
+      // over the blocks (all of a warp's reads in flight), then one warp over the
+      // warps
+      for (int g0 = 0; g0 < p.G; g0 += 32) {
+        const int g = g0 + lane;
+        constexpr int kW = kFwdThreads / 32, kIn = 11;  // 11 x 15 blocks a round
+        Stat t{0.f, 0.f, 0.f};
+        for (int c = c0 + warp; c <= c1; c += kIn * kW) {
+          float2 o[kIn];
+#pragma unroll
+          for (int x = 0; x < kIn; ++x) {
+            const int at = c + x * kW;
+            o[x] = at <= c1 && g < p.G ? part[(int64_t)(at + s) * p.G + g] : make_float2(0.f, 0.f);
+          }
+#pragma unroll
+          for (int x = 0; x < kIn; ++x) {
+            const int at = c + x * kW;
+            if (at <= c1) t.add((float)(min(sh.first(at + 1), row + n) - max(sh.first(at), row)), o[x].x, o[x].y * inv_cpg);
           }
         }
-        q = warp_sum(q);
-        const float r = 1.f / sqrtf(q / ((float)n * (float)cpg) + p.eps);
-        if (lane == 0) {
+        lane_stat[threadIdx.x] = make_float2(t.mean, t.m2);
+        if (lane == 0) warp_rows[warp] = t.n;
+        sync_compute<kFwdThreads>();
+        if (warp == 0 && g < p.G) {
+          const float inv_n = 1.f / (float)n;
+          float m = 0.f, q = 0.f;
+#pragma unroll
+          for (int x = 1; x < kW; ++x) m = fmaf(warp_rows[x], lane_stat[x * 32 + lane].x - t.mean, m);
+          m = fmaf(m, inv_n, t.mean);
+#pragma unroll
+          for (int x = 0; x < kW; ++x) {
+            const float2 o = lane_stat[x * 32 + lane];
+            q += fmaf(warp_rows[x] * (o.x - m), o.x - m, o.y);
+          }
+          const float r = 1.f / sqrtf(q * inv_n + p.eps);
           stat[g] = make_float2(m, r);
           if (me == c0) {
             p.mean[(int64_t)s * p.G + g] = m;
             p.rstd[(int64_t)s * p.G + g] = r;
           }
         }
+        sync_compute<kFwdThreads>();
       }
-      sync_compute<kFwdThreads>();
-      const int64_t chunks = ck.row_chunks(hi - lo);
+      const int chunks = ck.row_chunks(hi - lo);
       for (int slab = ck.slabs - 1; slab >= 0; --slab) {
         const Layout<kFwdThreads> L(ck.cv, slab * kFwdThreads);
         Channels<V> ch;
         if (L.on) ch.load(p, stat, L.col * V);
+        // u = x a + b in bf16, whose inputs are coarser than what folding the mean
+        // into b costs; in fp32 (x - mu) a + beta
+        constexpr bool kFold = sizeof(T) == 2;
 #pragma unroll
-        for (int c = 0; c < V; ++c) ch.rstd[c] *= ch.gamma[c];
+        for (int c = 0; c < V / 2; ++c) {
+          ch.rstd[c] = mul_f32x2(ch.rstd[c], ch.gamma[c]);
+          if (kFold) ch.beta[c] = fma_f32x2(ch.neg_mean[c], ch.rstd[c], ch.beta[c]);
+        }
+        auto row_of = [&](const uint4& w) -> uint4 {
+          uint64_t v[V / 2];
+          Vec<T>::unpack(w, v);
+#pragma unroll
+          for (int x = 0; x < V / 2; ++x) {
+            const uint64_t u = fma_f32x2(sizeof(T) == 2 ? v[x] : add_f32x2(v[x], ch.neg_mean[x]), ch.rstd[x], ch.beta[x]);
+            v[x] = kAct ? mul_f32x2(u, sigmoid2(u)) : u;
+          }
+          return Vec<T>::pack(v);
+        };
         uint8_t* dst = static_cast<uint8_t*>(p.y) + (int64_t)L.col * 16;
-        for (int64_t c = chunks - 1; c >= 0; --c, --i, slot = ring.before(slot)) {
+        for (int c = chunks - 1; c >= 0; --c, --i, slot = ring.before(slot)) {
           if (total - 1 - i >= ring.slots) ring.wait_full(slot);
-          const int64_t r = lo + c * ck.rows + L.lane;
+          const int r = lo + c * ck.rows + L.lane;
           if (L.on) {
             const uint8_t* src = ring.mem + (int64_t)slot * ring.slot_bytes + (L.lane * L.cols + L.col - slab * kFwdThreads) * 16;
+            const int step = L.lanes * L.cols * 16;
+            uint8_t* to = dst + (int64_t)r * p.ys * (int64_t)sizeof(T);
+            const int64_t to_step = L.lanes * p.ys * (int64_t)sizeof(T);
+            if (lo + (c + 1) * ck.rows <= hi) {  // a full chunk
+              uint4 w[kFwdPer];
 #pragma unroll
-            for (int k = 0; k < kFwdPer; ++k)
-              if (r + k * L.lanes < hi) {
-                float v[V];
-                Vec<T>::unpack(*reinterpret_cast<const uint4*>(src + k * L.lanes * L.cols * 16), v);
+              for (int k = 0; k < kFwdPer; ++k) w[k] = *reinterpret_cast<const uint4*>(src + k * step);
 #pragma unroll
-                for (int x = 0; x < V; ++x) {
-                  const float u = fmaf(v[x] - ch.mean[x], ch.rstd[x], ch.beta[x]);
-                  v[x] = kAct ? u * sigmoid(u) : u;
-                }
-                store_stream(dst + (r + k * L.lanes) * p.ys * (int64_t)sizeof(T), Vec<T>::pack(v));
-              }
+              for (int k = 0; k < kFwdPer; ++k) store_stream(to + k * to_step, row_of(w[k]));
+            } else {
+              for (int k = 0; k < kFwdPer && r + k * L.lanes < hi; ++k)
+                store_stream(to + k * to_step, row_of(*reinterpret_cast<const uint4*>(src + k * step)));
+            }
           }
           ring.release(slot);
         }
@@ -520,13 +656,16 @@ __global__ void __launch_bounds__(kFwdThreads + 32, 1) gn_fwd_kernel(const Gnorm
 }
 
 // ------------------------------------------------------------------ backward
-// xh and du of one value
+// xh and du of a pair
 template <bool kAct>
-UT_DEV float du_of(float x, float dy, float mean, float rstd, float gamma, float beta, float& xh) {
-  xh = (x - mean) * rstd;
+UT_DEV uint64_t du_of(uint64_t x, uint64_t dy, uint64_t neg_mean, uint64_t rstd, uint64_t gamma, uint64_t beta,
+                      uint64_t& xh) {
+  xh = mul_f32x2(add_f32x2(x, neg_mean), rstd);
   if (!kAct) return dy;
-  const float u = fmaf(xh, gamma, beta), s = sigmoid(u);
-  return dy * (s * fmaf(u, 1.f - s, 1.f));
+  const uint64_t u = fma_f32x2(xh, gamma, beta), s = sigmoid2(u);
+  // s (1 + u (1 - s)) = s + u s (1 - s)
+  const uint64_t us = mul_f32x2(u, s), rest = fma_f32x2(s, both(-1.f), both(1.f));
+  return mul_f32x2(dy, fma_f32x2(us, rest, s));
 }
 
 template <typename T, bool kAct>
@@ -542,6 +681,7 @@ __global__ void __launch_bounds__(kBwdThreads + 32, 1) gn_bwd_kernel(const Gnorm
   const int blocks = gridDim.x, me = blockIdx.x, cpg = p.C / p.G;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const Chunks<kBwdThreads, kBwdPer> ck(p.C / V);
+  prefetch_affine(p);
   Ring ring{st, smem + p.ring_at, p.slots, p.slot_bytes, p.status, p.timeout_ns, 0, 0};
   float2* part0 = static_cast<float2*>(p.ws);                // [2][blocks + B][G]
   float2* sums = part0 + (int64_t)2 * (blocks + p.B) * p.G;  // [blocks][C]
@@ -559,84 +699,99 @@ __global__ void __launch_bounds__(kBwdThreads + 32, 1) gn_bwd_kernel(const Gnorm
     s0 = b.s1;
     float2* part = part0 + (int64_t)(nb & 1) * (blocks + p.B) * p.G;
     const Shares sh(b, blocks);
-    const int64_t a = sh.first(me), e = sh.first(me + 1);
-    int64_t total = 0;  // chunks
-    for_pieces(p, b, a, e, [&](int, int64_t lo, int64_t hi) { total += ck.of_piece(hi - lo); });
+    const int a = sh.first(me), e = sh.first(me + 1);
+    int total = 0;  // chunks
+    for_pieces(p, b, a, e, [&](int, int lo, int hi) { total += ck.of_piece(hi - lo); });
     if (warp == kBwdThreads / 32) {
       produce<kBwdThreads, kBwdPer, 2>(p, b, a, e, ck, ring, total, sizeof(T));
       continue;
     }
-    int64_t i = 0;
-    int slot = 0;
-    for_pieces(p, b, a, e, [&](int s, int64_t lo, int64_t hi) {
-      const int64_t n = hi - lo;
+    int i = 0, slot = 0;
+    for_pieces(p, b, a, e, [&](int s, int lo, int hi) {
+      const int n = hi - lo;
       sync_compute<kBwdThreads>();
       load_stat(s);
       sync_compute<kBwdThreads>();
       for (int slab = 0; slab < ck.slabs; ++slab) {
         const Layout<kBwdThreads> L(ck.cv, slab * kBwdThreads);
-        float s1[V], s2[V];
+        uint64_t t1[V / 2], t2[V / 2];
 #pragma unroll
-        for (int c = 0; c < V; ++c) s1[c] = s2[c] = 0.f;
+        for (int c = 0; c < V / 2; ++c) t1[c] = t2[c] = 0;
         Channels<V> ch;
         if (L.on) ch.load(p, stat, L.col * V);
-        for (int64_t r = 0; r < n; r += ck.rows, ++i, slot = ring.next(slot)) {
+        for (int r = 0; r < n; r += ck.rows, ++i, slot = ring.next(slot)) {
           ring.wait_full(slot);
           if (L.on) {
             const uint8_t* src = ring.mem + (int64_t)slot * ring.slot_bytes + (L.lane * L.cols + L.col - slab * kBwdThreads) * 16;
-            float b1[V], b2[V];
+            uint64_t b1[V / 2], b2[V / 2];
 #pragma unroll
-            for (int c = 0; c < V; ++c) b1[c] = b2[c] = 0.f;
+            for (int c = 0; c < V / 2; ++c) b1[c] = b2[c] = 0;
 #pragma unroll
             for (int k = 0; k < kBwdPer; ++k)
               if (r + L.lane + k * L.lanes < n) {
                 const uint8_t* at = src + k * L.lanes * L.cols * 16;
-                float v[V], g[V];
+                uint64_t v[V / 2], g[V / 2];
                 Vec<T>::unpack(*reinterpret_cast<const uint4*>(at), v);
                 Vec<T>::unpack(*reinterpret_cast<const uint4*>(at + ring.slot_bytes / 2), g);
 #pragma unroll
-                for (int c = 0; c < V; ++c) {
-                  float xh;
-                  const float du = du_of<kAct>(v[c], g[c], ch.mean[c], ch.rstd[c], ch.gamma[c], ch.beta[c], xh);
-                  b1[c] += du;
-                  b2[c] = fmaf(du, xh, b2[c]);
+                for (int c = 0; c < V / 2; ++c) {
+                  uint64_t xh;
+                  const uint64_t du = du_of<kAct>(v[c], g[c], ch.neg_mean[c], ch.rstd[c], ch.gamma[c], ch.beta[c], xh);
+                  b1[c] = add_f32x2(b1[c], du);
+                  b2[c] = fma_f32x2(du, xh, b2[c]);
                 }
               }
 #pragma unroll
-            for (int c = 0; c < V; ++c) {
-              s1[c] += b1[c];
-              s2[c] += b2[c];
+            for (int c = 0; c < V / 2; ++c) {
+              t1[c] = add_f32x2(t1[c], b1[c]);
+              t2[c] = add_f32x2(t2[c], b2[c]);
             }
           }
           if (i + ring.slots < total) ring.release(slot);  // else it stays for the second pass
         }
         sync_compute<kBwdThreads>();
+        float s1[V], s2[V];
+#pragma unroll
+        for (int c = 0; c < V / 2; ++c) {
+          unpack_f32x2(t1[c], s1[2 * c], s1[2 * c + 1]);
+          unpack_f32x2(t2[c], s2[2 * c], s2[2 * c + 1]);
+        }
+        // over the lanes of a column, a thread a channel
 #pragma unroll
         for (int c = 0; c < V; ++c) lane_sum[c * kBwdThreads + threadIdx.x] = make_float2(s1[c], s2[c]);
         sync_compute<kBwdThreads>();
         for (int x = threadIdx.x; x < L.cols * V; x += kBwdThreads) {
-          const float2* ls = lane_sum + (x % V) * kBwdThreads + x / V;
+          const int c = x / L.cols, col = x - c * L.cols;
+          const float2* ls = lane_sum + c * kBwdThreads + col;
           float2 t = make_float2(0.f, 0.f);
+#pragma unroll 8
           for (int l = 0; l < L.lanes; ++l) {
-            t.x += ls[l * L.cols].x;
-            t.y += ls[l * L.cols].y;
+            const float2 o = ls[l * L.cols];
+            t.x += o.x;
+            t.y += o.y;
           }
-          const int c = slab * kBwdThreads * V + x;
-          chan[c] = t;
-          all[c] = make_float2(all[c].x + t.x, all[c].y + t.y);
+          const int at = (slab * kBwdThreads + col) * V + c;
+          chan[at] = t;
+          all[at] = make_float2(all[at].x + t.x, all[at].y + t.y);
         }
       }
       sync_compute<kBwdThreads>();
-      for (int g = warp; g < p.G; g += kBwdThreads / 32) {
+      // over the channels of a group, p.group_lanes threads a group
+      for (int g0 = 0; g0 < p.G; g0 += kBwdThreads / p.group_lanes) {
+        const int g = g0 + threadIdx.x / p.group_lanes, l = threadIdx.x % p.group_lanes;
+        const bool on = g < p.G && threadIdx.x < kBwdThreads / p.group_lanes * p.group_lanes;
         float2 t = make_float2(0.f, 0.f);
-        for (int c = g * cpg + lane; c < (g + 1) * cpg; c += 32) {
-          const float w = p.gamma ? p.gamma[c] : 1.f;
-          t.x = fmaf(w, chan[c].x, t.x);
-          t.y = fmaf(w, chan[c].y, t.y);
+        if (on)
+          for (int c = g * cpg + l; c < (g + 1) * cpg; c += p.group_lanes) {
+            const float w = p.gamma ? p.gamma[c] : 1.f;
+            t.x = fmaf(w, chan[c].x, t.x);
+            t.y = fmaf(w, chan[c].y, t.y);
+          }
+        for (int o = p.group_lanes / 2; o; o >>= 1) {
+          t.x += __shfl_xor_sync(0xffffffffu, t.x, o);
+          t.y += __shfl_xor_sync(0xffffffffu, t.y, o);
         }
-        t.x = warp_sum(t.x);
-        t.y = warp_sum(t.y);
-        if (lane == 0) part[(int64_t)(me + s) * p.G + g] = t;
+        if (on && l == 0) part[(int64_t)(me + s) * p.G + g] = t;
       }
     });
     if (s0 >= p.B) {  // the last batch: this block's sums over all segments are complete
@@ -662,56 +817,76 @@ __global__ void __launch_bounds__(kBwdThreads + 32, 1) gn_bwd_kernel(const Gnorm
     }
     i = total - 1;
     slot = ring.before(slot);
-    for_pieces_back(p, b, a, e, [&](int s, int64_t lo, int64_t hi) {
-      int64_t row, n;
-      segment_rows(p.cu, s, p.n, row, n);
+    for_pieces_back(p, b, a, e, [&](int s, int lo, int hi) {
+      int row, n;
+      rows_of_segment(p, s, row, n);
       const int c0 = sh.owner(row), c1 = sh.owner(row + n - 1);
       const float inv = 1.f / ((float)n * (float)cpg);
       sync_compute<kBwdThreads>();
       load_stat(s);
-      for (int g = warp; g < p.G; g += kBwdThreads / 32) {
+      // the segment's sums from its pieces': lanes over the groups, warps over
+      // the blocks, then one warp over the warps
+      for (int g0 = 0; g0 < p.G; g0 += 32) {
+        const int g = g0 + lane;
         float2 t = make_float2(0.f, 0.f);
-        for (int c = c0 + lane; c <= c1; c += 32)
-          if (min(sh.first(c + 1), row + n) > max(sh.first(c), row)) {
-            const float2 u = part[(int64_t)(c + s) * p.G + g];
-            t.x += u.x;
-            t.y += u.y;
+        constexpr int kW = kBwdThreads / 32, kIn = 14;  // 14 x 11 blocks a round
+        for (int c = c0 + warp; c <= c1; c += kIn * kW) {
+          float2 o[kIn];
+#pragma unroll
+          for (int x = 0; x < kIn; ++x) {
+            const int at = c + x * kW;
+            const bool there = at <= c1 && g < p.G && min(sh.first(at + 1), row + n) > max(sh.first(at), row);
+            o[x] = there ? part[(int64_t)(at + s) * p.G + g] : make_float2(0.f, 0.f);
           }
-        t.x = warp_sum(t.x);
-        t.y = warp_sum(t.y);
-        if (lane == 0) coef[g] = make_float2(t.x * inv, t.y * inv);
+#pragma unroll
+          for (int x = 0; x < kIn; ++x) {
+            t.x += o[x].x;
+            t.y += o[x].y;
+          }
+        }
+        lane_sum[threadIdx.x] = t;
+        sync_compute<kBwdThreads>();
+        if (warp == 0 && g < p.G) {
+#pragma unroll
+          for (int x = 1; x < kW; ++x) {
+            const float2 o = lane_sum[x * 32 + lane];
+            t.x += o.x;
+            t.y += o.y;
+          }
+          coef[g] = make_float2(t.x * inv, t.y * inv);
+        }
+        sync_compute<kBwdThreads>();
       }
-      sync_compute<kBwdThreads>();
-      const int64_t chunks = ck.row_chunks(hi - lo);
+      const int chunks = ck.row_chunks(hi - lo);
       for (int slab = ck.slabs - 1; slab >= 0; --slab) {
         const Layout<kBwdThreads> L(ck.cv, slab * kBwdThreads);
         Channels<V> ch;
-        float2 ab[V];
+        Channels<V> ab;  // -a / M and b / M (the affine is not used)
         if (L.on) {
           ch.load(p, stat, L.col * V);
-#pragma unroll
-          for (int x = 0; x < V; ++x) ab[x] = coef[(L.col * V + x) / cpg];
+          ab.load(p, coef, L.col * V);
         }
         uint8_t* dst = static_cast<uint8_t*>(p.dx) + (int64_t)L.col * 16;
-        for (int64_t c = chunks - 1; c >= 0; --c, --i, slot = ring.before(slot)) {
+        for (int c = chunks - 1; c >= 0; --c, --i, slot = ring.before(slot)) {
           if (total - 1 - i >= ring.slots) ring.wait_full(slot);
-          const int64_t r = lo + c * ck.rows + L.lane;
+          const int r = lo + c * ck.rows + L.lane;
           if (L.on) {
             const uint8_t* src = ring.mem + (int64_t)slot * ring.slot_bytes + (L.lane * L.cols + L.col - slab * kBwdThreads) * 16;
 #pragma unroll
             for (int k = 0; k < kBwdPer; ++k)
               if (r + k * L.lanes < hi) {
                 const uint8_t* at = src + k * L.lanes * L.cols * 16;
-                float v[V], g[V];
+                uint64_t v[V / 2], g[V / 2];
                 Vec<T>::unpack(*reinterpret_cast<const uint4*>(at), v);
                 Vec<T>::unpack(*reinterpret_cast<const uint4*>(at + ring.slot_bytes / 2), g);
 #pragma unroll
-                for (int x = 0; x < V; ++x) {
-                  float xh;
-                  const float du = du_of<kAct>(v[x], g[x], ch.mean[x], ch.rstd[x], ch.gamma[x], ch.beta[x], xh);
-                  v[x] = ch.rstd[x] * (fmaf(ch.gamma[x], du, -ab[x].x) - xh * ab[x].y);
+                for (int x = 0; x < V / 2; ++x) {
+                  uint64_t xh;
+                  const uint64_t du = du_of<kAct>(v[x], g[x], ch.neg_mean[x], ch.rstd[x], ch.gamma[x], ch.beta[x], xh);
+                  const uint64_t t = fma_f32x2(ch.gamma[x], du, ab.neg_mean[x]);
+                  v[x] = mul_f32x2(ch.rstd[x], fma_f32x2(mul_f32x2(xh, both(-1.f)), ab.rstd[x], t));
                 }
-                store_stream(dst + (r + k * L.lanes) * p.dxs * (int64_t)sizeof(T), Vec<T>::pack(v));
+                store_stream(dst + (int64_t)(r + k * L.lanes) * p.dxs * (int64_t)sizeof(T), Vec<T>::pack(v));
               }
           }
           ring.release(slot);
@@ -737,7 +912,10 @@ cudaError_t launch(F kern, GnormParams p, size_t fixed, int tensors, int threads
   const int slots = (int)((kSmem - fixed) / p.slot_bytes);
   p.slots = slots < kMaxSlots ? slots : kMaxSlots;
   if (p.slots < 1) return cudaErrorInvalidValue;
-  p.batch_rows = kBatchBytes / ((int64_t)p.C * elem * tensors);
+  // threads a group of channels is summed by: all groups in one round if they fit
+  p.group_lanes = 32;
+  while (p.group_lanes > 1 && p.group_lanes * p.G > threads) p.group_lanes /= 2;
+  p.batch_rows = (int)(kBatchBytes / ((int64_t)p.C * elem * tensors));
   const size_t smem = fixed + (size_t)p.slots * p.slot_bytes;
   cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
   if (e != cudaSuccess) return e;

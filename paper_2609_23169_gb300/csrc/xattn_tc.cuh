@@ -1,6 +1,7 @@
 // Device helpers of the cross-attention tensor-core kernels.
 #pragma once
 #include "common.cuh"
+#include "pairs.cuh"
 #include "xattn.cuh"
 
 namespace ut {
@@ -99,25 +100,6 @@ UT_DEV uint32_t lane_keys(const uint8_t* mask, int64_t key, int left, uint32_t l
     if (x < left && (!mask || mask[key + x])) b |= 1u << g;
   }
   return b;
-}
-
-// Pairs of fp32 values in one 64-bit register: one instruction for two.
-UT_DEV uint64_t pack_u32x2(uint32_t a, uint32_t b) {
-  uint64_t r;
-  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "r"(a), "r"(b));
-  return r;
-}
-UT_DEV uint64_t pack_f32x2(float a, float b) { return pack_u32x2(__float_as_uint(a), __float_as_uint(b)); }
-UT_DEV void unpack_f32x2(uint64_t v, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
-UT_DEV uint64_t fma_f32x2(uint64_t a, uint64_t b, uint64_t c) {
-  uint64_t r;
-  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
-  return r;
-}
-UT_DEV uint64_t add_f32x2(uint64_t a, uint64_t b) {
-  uint64_t r;
-  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-  return r;
 }
 
 UT_DEV void ld_shared_v4(uint32_t addr, uint32_t (&v)[4]) {
