@@ -47,10 +47,10 @@ namespace {
 // threads that compute; with the producer warp after them a multiple of four warps
 // (128 and 168 registers a thread)
 constexpr int kFwdThreads = 480, kBwdThreads = 352;
-constexpr int kFwdPer = 4, kBwdPer = 2;              // rows of a chunk for each thread
+constexpr int kFwdPer = 4, kBwdPer = 4;              // rows of a chunk for each thread
 constexpr int kWindow = 16;                          // rows summed before they are merged (forward)
 constexpr int kMaxSlots = 16;
-constexpr int64_t kBatchBytes = 128ll << 20;          // of the tensors read, per batch
+constexpr int64_t kBatchBytes = 192ll << 20;          // of the tensors read, per batch
 constexpr size_t kSmem = 225 * 1024;                 // with 2 KB of static shared memory
 
 template <typename T>
@@ -96,8 +96,10 @@ UT_DEV float rcp_approx(float x) {
   asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
-// 1 / (1 + exp(-u)) of a pair: two units of the special function pipe each,
-// relative error below 2^-21 (exp(-u) = infinity gives 0)
+// 1 / (1 + exp(-u)) of a pair, relative error below 2^-21 (exp(-u) = infinity
+// gives 0).  Sharing one reciprocal between the two (1 / a = b / (a b)) takes a
+// third off the special function pipe and adds four instructions: no faster
+// forward, 8% slower backward.
 UT_DEV uint64_t sigmoid2(uint64_t u) {
   float a, b;
   unpack_f32x2(mul_f32x2(u, both(-1.4426950408889634f)), a, b);
@@ -363,23 +365,34 @@ struct Channels {
   uint64_t neg_mean[V / 2], rstd[V / 2], gamma[V / 2], beta[V / 2];
   UT_DEV void load(const GnormParams& p, const float2* stat, int c0) {
     const int cpg = p.C / p.G;
+    float w[V], b[V];
+    load_or(p.gamma, c0, 1.f, w);
+    load_or(p.beta, c0, 0.f, b);
     int g = c0 / cpg, left = cpg - (c0 - g * cpg);  // channels left in group g
 #pragma unroll
     for (int c = 0; c < V; c += 2) {
-      float m[2], r[2];
+      float2 t[2];
 #pragma unroll
       for (int x = 0; x < 2; ++x) {
-        m[x] = stat[g].x;
-        r[x] = stat[g].y;
+        t[x] = stat[g];
         if (--left == 0) {
           ++g;
           left = cpg;
         }
       }
-      neg_mean[c / 2] = pack_f32x2(-m[0], -m[1]);
-      rstd[c / 2] = pack_f32x2(r[0], r[1]);
-      gamma[c / 2] = p.gamma ? pack_f32x2(p.gamma[c0 + c], p.gamma[c0 + c + 1]) : both(1.f);
-      beta[c / 2] = p.beta ? pack_f32x2(p.beta[c0 + c], p.beta[c0 + c + 1]) : both(0.f);
+      neg_mean[c / 2] = pack_f32x2(-t[0].x, -t[1].x);
+      rstd[c / 2] = pack_f32x2(t[0].y, t[1].y);
+      gamma[c / 2] = pack_f32x2(w[c], w[c + 1]);
+      beta[c / 2] = pack_f32x2(b[c], b[c + 1]);
+    }
+  }
+  UT_DEV static void load_or(const float* src, int c0, float otherwise, float (&v)[V]) {
+    if (src) {  // all loads in flight
+#pragma unroll
+      for (int c = 0; c < V; ++c) v[c] = src[c0 + c];
+    } else {
+#pragma unroll
+      for (int c = 0; c < V; ++c) v[c] = otherwise;
     }
   }
 };
