@@ -14,19 +14,24 @@
 // flight read neighbouring 256-byte pieces of the same rows and share K and V
 // in L2.  Roles (384 threads, registers rebalanced with setmaxnreg):
 //   warp 0      TMA: the K and V tiles, one ring (K0 V0 K1 V1 ...)
-//   warp 1      TMEM owner and MMA issuer.  Over the blocks of
-//               all items in one stream, for each tile w: O_w += P_w V of the
-//               previous block, then S_w = Q_w K^T of this one (P_w overwrote
-//               S_w in TMEM, so this order needs no second buffer).
-//   warp 2      TMA: the query tiles, a ring of their own
-//   warp 3      decodes the items (segment search, key range) into a ring
+//   warp 2      decodes the items (segment search, key range) into a ring;
+//               TMA: the query tiles, a ring of their own
+//   warp 1      TMEM owner and MMA issuer of tile 0, warp 3 of tile 1: per
+//               block S = Q K^T, then, as P is written over S in TMEM, O += P V
+//               (of the first 96 keys while the last 32 are being written).
+//               Two issuers, so that one tile's warp waits for its operands
+//               while the other tile's products run; they issue in turn (P V
+//               and the next S of one tile together), else the tensor core
+//               mixes the two tiles' instructions, both finish late, and both
+//               softmaxes then run at once with the tensor core idle.
 //   warps 4-7   softmax of tile 0, warps 8-11 of tile 1: thread = row = TMEM
 //               lane.  Read S from TMEM, mask, keep a running maximum (O is
 //               rescaled in TMEM only where it grew by more than 2^8, so the
 //               exponentials stay bounded), write P as bf16 over S; after the
 //               last block O / l and LSE, or the split's partial result.
 // Masked keys and the rows of other segments: S there is replaced by -inf,
-// and the softmax warps zero those rows of the V tile before its products, so that no value they hold (NaN, infinities) is multiplied.
+// and the softmax warps zero those rows of the V tile before its products, so
+// that no value they hold (NaN, infinities) is multiplied.
 // TMEM columns: S_0 / P_0 [0,128), S_1 / P_1 [128,256), O_0 [256,256+d), O_1
 // [384,384+d).
 // Every wait is bounded; on expiry the kernel records UT_ERR_TIMEOUT, drains
@@ -67,7 +72,7 @@ struct Smem {
   alignas(1024) uint8_t q[kQ][kTile];
   alignas(1024) uint8_t kv[kKv][kTile];
   uint64_t q_full[kQ], q_empty[kQ], kv_full[kKv], kv_empty[kKv];
-  uint64_t s_full[2], p_full[2], o_full[2], o_empty[2], mma_done;
+  uint64_t s_full[2], p_most[2], p_full[2], o_full[2], o_empty[2], turn[2], mma_done;
   uint64_t item_full[kItemSlots], item_empty[kItemSlots];
   Item item[kItemSlots];
   uint32_t tmem_base;
@@ -101,7 +106,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   if (threadIdx.x == 0) {
     for (int s = 0; s < S::kQ; ++s) {
       mbar_init(&sm.q_full[s], 1);
-      mbar_init(&sm.q_empty[s], 5);  // its last product, and the four warps that sent its output
+      mbar_init(&sm.q_empty[s], 1);
     }
     for (int s = 0; s < S::kKv; ++s) {
       mbar_init(&sm.kv_full[s], 1);
@@ -109,6 +114,8 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
     for (int w = 0; w < 2; ++w) {
       mbar_init(&sm.s_full[w], 1);
+      mbar_init(&sm.turn[w], 1);
+      mbar_init(&sm.p_most[w], 4);
       mbar_init(&sm.p_full[w], 4);
       mbar_init(&sm.o_full[w], 1);
       mbar_init(&sm.o_empty[w], 4);
@@ -242,9 +249,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       const uint32_t q_lo = desc_lo(smem_u32(sm.q[0]), 16), k_lo = desc_lo(smem_u32(sm.kv[0]), 16),
                      v_lo = desc_lo(smem_u32(sm.kv[0]), kChunkBytes);
       const uint32_t w = warp >> 1, ts = w * 128, to = 256 + w * 128;
-      uint64_t* p_full = &sm.p_full[w];
-      uint64_t* s_full = &sm.s_full[w];
-      uint32_t n = 0, qat = w, kvat = 0, np = 0, no = 0;
+      uint32_t n = 0, qat = w, kvat = 0, np = 0, no = 0, turns = 0;
       bool ok = true;
       for (;; ++n) {
         const uint32_t slot = n % kItemSlots;
@@ -268,31 +273,47 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
         const uint32_t qs = qat % S::kQ, q_a = q_lo + qs * (S::kTile >> 4);
         if (!(ok = wait(&sm.q_full[qs], (qat / S::kQ) & 1))) break;
+        // step j: O += P V of block j - 1, S = Q K^T of block j
 #pragma unroll 1
-        for (int j = 0;; ++j) {
-          const uint32_t ks = kvat % S::kKv;  // S = Q K^T
-          if (!(ok = wait(&sm.kv_full[ks], (kvat / S::kKv) & 1))) break;
-          tc_fence_after();
-          mma_nt<D>(ts, q_a, k_lo + ks * (S::kTile >> 4), idesc_s);
-          mma_commit_w(s_full);
-          mma_commit_w(&sm.kv_empty[ks]);
-          if (j == blocks - 1) mma_commit_w(&sm.q_empty[qs]);
-          // O += P V, V being needed (and zeroed in places) well before P is there
-          const uint32_t st = (kvat + 1) % S::kKv;
-          if (!(ok = wait(&sm.kv_full[st], ((kvat + 1) / S::kKv) & 1))) break;
-          if (j == 0) {
-            if (!(ok = wait(&sm.o_empty[w], (no & 1) ^ 1))) break;
-            ++no;
+        for (int j = 0; j <= blocks; ++j) {
+          const uint32_t ks = kvat % S::kKv, vs = (kvat - 1) % S::kKv;
+          if (j < blocks && !(ok = wait(&sm.kv_full[ks], (kvat / S::kKv) & 1))) break;
+          if (j > 0) {
+            if (!(ok = wait(&sm.kv_full[vs], ((kvat - 1) / S::kKv) & 1))) break;
+            if (j == 1) {
+              if (!(ok = wait(&sm.o_empty[w], (no & 1) ^ 1))) break;
+              ++no;
+            }
+            if (!(ok = wait(&sm.p_most[w], np & 1))) break;
           }
-          if (!(ok = wait(p_full, np & 1))) break;
-          ++np;
+          // an item's first S and its last P V wait for no turn: the tiles need
+          // not start or end together
+          const bool turn = both && j > 0 && j < blocks;
+          if (turn) {
+            if (!(ok = wait(&sm.turn[w], (turns & 1) ^ (w ^ 1)))) break;
+            ++turns;
+          }
           tc_fence_after();
-          mma_tn128(to, ts, v_lo + st * (S::kTile >> 4), idesc_o, j > 0);
-          mma_commit_w(&sm.kv_empty[st]);
-          kvat += 2;
-          if (j == blocks - 1) {
-            mma_commit_w(&sm.o_full[w]);
-            break;
+          if (j > 0) {
+            const uint32_t v_b = v_lo + vs * (S::kTile >> 4);
+            mma_tn96(to, ts, v_b, idesc_o, j > 1);
+            if (!(ok = wait(&sm.p_full[w], np & 1))) break;
+            ++np;
+            tc_fence_after();
+            mma_tn32(to, ts + 48, v_b + 768, idesc_o);
+            mma_commit_w(&sm.kv_empty[vs]);
+            if (j == blocks) mma_commit_w(&sm.o_full[w]);
+          }
+          if (j < blocks) {
+            mma_nt<D>(ts, q_a, k_lo + ks * (S::kTile >> 4), idesc_s);
+            mma_commit_w(&sm.s_full[w]);
+            mma_commit_w(&sm.kv_empty[ks]);
+            if (j == blocks - 1) mma_commit_w(&sm.q_empty[qs]);
+            kvat += 2;
+          }
+          if (turn) {
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&sm.turn[w ^ 1]);
           }
         }
         if (!ok) break;
@@ -309,7 +330,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     const uint32_t ts = lane_base + w * 128, to = lane_base + 256 + w * 128;
     auto token_of = [&](uint32_t r) -> uint32_t { return (r * prm.inv_g) >> 16; };  // r / G
     const uint64_t c2 = pack_f32x2(prm.scale_log2, prm.scale_log2);
-    uint32_t n = 0, ns = 0, no = 0, qat = 0, kvat = 0;
+    uint32_t n = 0, ns = 0, no = 0, kvat = 0;
     bool ok = true;
     for (;; ++n) {
       // the item stays in its slot until this tile is done with it
@@ -355,16 +376,12 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
         float m8[8];
 #pragma unroll
-        for (int x = 0; x < 8; ++x) m8[x] = __uint_as_float(r[x]);
+        for (int x = 0; x < 8; ++x) m8[x] = fmaxf(__uint_as_float(r[x]), __uint_as_float(r[x + 8]));
 #pragma unroll
-        for (int x = 8; x < kN; x += 16) {
+        for (int x = 16; x < kN; x += 16)
 #pragma unroll
-          for (int y = 0; y < 8; ++y)
-            m8[y] = x + 8 + y < kN ? fmaxf(fmaxf(m8[y], __uint_as_float(r[x + y])), __uint_as_float(r[x + 8 + y < kN ? x + 8 + y : 0]))
-                                   : fmaxf(m8[y], __uint_as_float(r[x + y]));
-        }
-        float mx = fmaxf(fmaxf(fmaxf(m8[0], m8[1]), fmaxf(m8[2], m8[3])),
-                         fmaxf(fmaxf(m8[4], m8[5]), fmaxf(m8[6], m8[7])));
+          for (int y = 0; y < 8; ++y) m8[y] = max3(m8[y], __uint_as_float(r[x + y]), __uint_as_float(r[x + y + 8]));
+        float mx = max3(max3(m8[0], m8[1], m8[2]), max3(m8[3], m8[4], m8[5]), fmaxf(m8[6], m8[7]));
         mx = fmaxf(mx * prm.scale_log2, -1e30f);  // finite where a row sees no key of the block
         const bool need = j > 0 && mx > m + 8.0f;
         if (j == 0) m = mx;
@@ -399,6 +416,12 @@ __global__ void __launch_bounds__(kThreads, 1)
             pk[x / 2] = pack_bf16x2(p0, p1);
           }
           tmem_st16(ts + g * 16, pk);
+          if (g == 2) {  // three quarters of P: its product may begin
+            tmem_wait_st();
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&sm.p_most[w]);
+          }
         }
         float a0, a1;
         unpack_f32x2(add_f32x2(add_f32x2(sum[0], sum[1]), add_f32x2(sum[2], sum[3])), a0, a1);
@@ -417,12 +440,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       const uint32_t row = quarter * 32 + lane, rt = token_of(row);  // this thread's row and its token
       const int hk = it->hk, ntok = it->ntok[w], split = it->split;
       const int64_t tok0 = (int64_t)it->tok0 + w * prm.tpt;
-      const bool two = it->ntok[1] > 0;
-      const uint32_t qst = (qat + w) % S::kQ;
-      if (it->blocks > 0) {
-        qat += two ? 2 : 1;
-        kvat += 2 * it->blocks;
-      }
+      kvat += 2 * it->blocks;
       __syncwarp();
       if (lane == 0) mbar_arrive(&sm.item_empty[slot]);
       if (ntok == 0) continue;
@@ -449,50 +467,50 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (row_ok) p.part_ml[prow] = make_float2(m, l);
         tc_fence_before();
         __syncwarp();
-        if (blocks > 0 && lane == 0) {
-          mbar_arrive(&sm.o_empty[w]);
-          mbar_arrive(&sm.q_empty[qst]);
-        }
+        if (blocks > 0 && lane == 0) mbar_arrive(&sm.o_empty[w]);
         continue;
       }
       if (row_ok) p.lse[(int64_t)h * p.nq + tok0 + rt] = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
-      // O / l in bf16 through the query tile's shared memory (its last product
-      // has read it): whole rows leave as 16-byte pieces of neighbouring lanes
-      const uint32_t stage = smem_u32(sm.q[qst]);
-      if (blocks > 0) {
-        const float f = l > 0.f ? 1.f / l : (l == 0.f ? 0.f : l);
+      // O / l in bf16.  A thread holds a row; the four lanes of a quad exchange
+      // 16-byte units so that lane c holds unit c of each of the quad's rows, and
+      // a store covers 64 contiguous bytes of eight rows instead of 16 of 32.
+      const float f = l > 0.f ? 1.f / l : (l == 0.f ? 0.f : l);
+      const uint32_t c = lane & 3;
+      __nv_bfloat16* out[4];
 #pragma unroll
-        for (int g = 0; g < D / 32; ++g) {
+      for (int i = 0; i < 4; ++i) {
+        const uint32_t y = quarter * 32 + (lane & ~3u) + i, yt = token_of(y);
+        out[i] = (int)yt < ntok ? static_cast<__nv_bfloat16*>(p.o) + (tok0 + yt) * p.os +
+                                      ((int64_t)hk * p.G + (y - yt * p.G)) * D + c * 8
+                                : nullptr;
+      }
+#pragma unroll 1
+      for (int g = 0; g < D / 32; ++g) {
+        uint32_t u[4][4];
+        if (blocks > 0) {
           uint32_t r[32];
           tmem_ld32(to + g * 32, r);
           tmem_wait_ld();
-          const uint32_t dst = stage + (g >> 1) * kChunkBytes + row * 128;
 #pragma unroll
-          for (int x = 0; x < 4; ++x) {
-            uint32_t v[4];
+          for (int x = 0; x < 16; ++x)
+            u[x >> 2][x & 3] = pack_bf16x2(__uint_as_float(r[2 * x]) * f, __uint_as_float(r[2 * x + 1]) * f);
+        } else {
 #pragma unroll
-            for (int y = 0; y < 4; ++y)
-              v[y] = pack_bf16x2(__uint_as_float(r[x * 8 + 2 * y]) * f, __uint_as_float(r[x * 8 + 2 * y + 1]) * f);
-            st_shared_v4(dst + ((((g & 1) * 4 + x) ^ (row & 7)) << 4), v[0], v[1], v[2], v[3]);
-          }
+          for (int x = 0; x < 16; ++x) u[x >> 2][x & 3] = 0;
         }
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(&sm.o_empty[w]);
+        if (g == D / 32 - 1) {
+          tc_fence_before();
+          __syncwarp();
+          if (blocks > 0 && lane == 0) mbar_arrive(&sm.o_empty[w]);
+        }
+        exchange_units<1>(u, c & 1, 0, 1);
+        exchange_units<1>(u, c & 1, 2, 3);
+        exchange_units<2>(u, c >> 1, 0, 2);
+        exchange_units<2>(u, c >> 1, 1, 3);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (out[i]) *reinterpret_cast<uint4*>(out[i] + g * 32) = make_uint4(u[i][0], u[i][1], u[i][2], u[i][3]);
       }
-      constexpr int kUnits = D / 8, kRows = 32 / kUnits;  // 16-byte units of a row, rows of a warp's access
-      __nv_bfloat16* out = static_cast<__nv_bfloat16*>(p.o) + tok0 * p.os + (int64_t)hk * p.G * D;
-#pragma unroll 4
-      for (int i = 0; i < 32 / kRows; ++i) {
-        const uint32_t y = quarter * 32 + i * kRows + lane / kUnits, u = lane % kUnits, yt = token_of(y);
-        uint32_t v[4] = {0, 0, 0, 0};
-        if (blocks > 0) ld_shared_v4(stage + (u >> 3) * kChunkBytes + y * 128 + (((u & 7) ^ (y & 7)) << 4), v);
-        if ((int)yt < ntok)
-          *reinterpret_cast<uint4*>(out + yt * p.os + (int64_t)(y - yt * p.G) * D + u * 8) =
-              make_uint4(v[0], v[1], v[2], v[3]);
-      }
-      __syncwarp();
-      if (blocks > 0 && lane == 0) mbar_arrive(&sm.q_empty[qst]);
     }
   }
   tc_fence_before();

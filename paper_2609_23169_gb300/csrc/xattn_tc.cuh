@@ -52,17 +52,21 @@ UT_DEV void mma_nt(uint32_t d, uint32_t a_lo, uint32_t b_lo, uint32_t idesc) {
   "add.u32 x, %1, " acol ";\n\tadd.u32 y, %2, " boff ";\n\t"           \
   "mov.b64 b, {y, %5};\n\t"                                            \
   "@e tcgen05.mma.cta_group::1.kind::f16 [%0], [x], b, %3, " acc ";\n\t"
-// d (+)= A B over 128 rows of B: A in TMEM (bf16 pairs, 8 columns a step), B
+// d (+)= A B over 96 / 32 rows of B: A in TMEM (bf16 pairs, 8 columns a step), B
 // row-major (MN-major operand, 16 rows of 128 bytes a step)
-UT_DEV void mma_tn128(uint32_t d, uint32_t a, uint32_t b_lo, uint32_t idesc, uint32_t accumulate) {
-  asm volatile(
-      "{\n\t.reg .pred e, p, t;\n\t.reg .b64 b;\n\t.reg .b32 x, y;\n\t"
-      "setp.ne.b32 p, %4, 0;\n\tsetp.eq.b32 t, 0, 0;\n\telect.sync _|e, 0xffffffff;\n\t" UT_TS_STEP("0", "0", "p")
-          UT_TS_STEP("8", "128", "t") UT_TS_STEP("16", "256", "t") UT_TS_STEP("24", "384", "t")
-              UT_TS_STEP("32", "512", "t") UT_TS_STEP("40", "640", "t") UT_TS_STEP("48", "768", "t")
-                  UT_TS_STEP("56", "896", "t") "}" ::"r"(d),
-      "r"(a), "r"(b_lo), "r"(idesc), "r"(accumulate), "r"(kDescHi)
-      : "memory");
+#define UT_TS_HEAD                                                  \
+  "{\n\t.reg .pred e, p, t;\n\t.reg .b64 b;\n\t.reg .b32 x, y;\n\t" \
+  "setp.ne.b32 p, %4, 0;\n\tsetp.eq.b32 t, 0, 0;\n\telect.sync _|e, 0xffffffff;\n\t"
+UT_DEV void mma_tn96(uint32_t d, uint32_t a, uint32_t b_lo, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(UT_TS_HEAD UT_TS_STEP("0", "0", "p") UT_TS_STEP("8", "128", "t") UT_TS_STEP("16", "256", "t")
+                   UT_TS_STEP("24", "384", "t") UT_TS_STEP("32", "512", "t") UT_TS_STEP("40", "640", "t") "}" ::"r"(d),
+               "r"(a), "r"(b_lo), "r"(idesc), "r"(accumulate), "r"(kDescHi)
+               : "memory");
+}
+UT_DEV void mma_tn32(uint32_t d, uint32_t a, uint32_t b_lo, uint32_t idesc) {
+  asm volatile(UT_TS_HEAD UT_TS_STEP("0", "0", "p") UT_TS_STEP("8", "128", "t") "}" ::"r"(d), "r"(a), "r"(b_lo),
+               "r"(idesc), "r"(1u), "r"(kDescHi)
+               : "memory");
 }
 
 #define UT_SS2_STEP(aoff, boff, acc)                                     \
@@ -102,11 +106,21 @@ UT_DEV uint32_t lane_keys(const uint8_t* mask, int64_t key, int left, uint32_t l
   return b;
 }
 
-UT_DEV void ld_shared_v4(uint32_t addr, uint32_t (&v)[4]) {
-  asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
-               : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3])
-               : "r"(addr)
-               : "memory");
+UT_DEV float max3(float a, float b, float c) {
+  float r;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+  return r;
+}
+// Lanes whose number differs in bit kBit exchange unit b of the lower one (bit =
+// 0) for unit a of the upper one (bit = 1).
+template <int kBit>
+UT_DEV void exchange_units(uint32_t (&u)[4][4], uint32_t bit, int a, int b) {
+#pragma unroll
+  for (int x = 0; x < 4; ++x) {
+    const uint32_t got = __shfl_xor_sync(0xffffffffu, bit ? u[a][x] : u[b][x], kBit);
+    u[a][x] = bit ? got : u[a][x];
+    u[b][x] = bit ? u[b][x] : got;
+  }
 }
 
 // 32 lanes x 32 bit, 16 consecutive columns per thread
