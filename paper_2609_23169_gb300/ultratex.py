@@ -440,6 +440,11 @@ def ut_bsattn_bwd(q, k, v, o, lse, dout, row_ptr, col_idx, col_ptr_t, row_idx_t,
 
 
 # ------------------------------------------------------- conditioning operators
+# Small calls are bound by the host: tensors that these functions allocate
+# themselves are not checked, and each of the caller's attributes is read once.
+_DTYPES = {torch.bfloat16: UT_BF16, torch.float32: UT_F32}
+
+
 def _prefix(cu: Optional[torch.Tensor], what: str) -> int:
     """Number of segments of a prefix of lengths (1 without one)."""
     if cu is None:
@@ -449,44 +454,54 @@ def _prefix(cu: Optional[torch.Tensor], what: str) -> int:
     return cu.numel() - 1
 
 
-def _same_device(first: torch.Tensor, *others: Optional[torch.Tensor]) -> None:
+def _same_device(device: torch.device, *others: Optional[torch.Tensor]) -> None:
     for t in others:
-        if t is not None and t.device != first.device:
-            raise ValueError(f"tensors on {first.device} and {t.device}; all must share one device")
+        if t is not None and t.device != device:
+            raise ValueError(f"tensors on {device} and {t.device}; all must share one device")
 
 
-def _head_rows(t: torch.Tensor, like: torch.Tensor, shape, what: str) -> int:
+def _head_rows(t: torch.Tensor, dtype: torch.dtype, shape, what: str) -> int:
     """Elements between the rows of a [rows, heads, d] tensor whose heads are contiguous."""
-    if tuple(t.shape) != tuple(shape) or t.dtype != like.dtype:
-        raise ValueError(f"{what} must be {list(shape)} {like.dtype}, got {list(t.shape)} {t.dtype}")
-    rows, heads, d = t.shape
-    if (d > 1 and t.stride(2) != 1) or (heads > 1 and t.stride(1) != d):
+    if t.shape != shape or t.dtype != dtype:
+        raise ValueError(f"{what} must be {list(shape)} {dtype}, got {list(t.shape)} {t.dtype}")
+    rows, heads, d = shape
+    row, head, one = t.stride()
+    if (d > 1 and one != 1) or (heads > 1 and head != d):
         raise ValueError(f"{what}: heads must be contiguous within a row")
-    return t.stride(0) if rows > 1 else heads * d
+    return row if rows > 1 else heads * d
 
 
-def _xattn_shape(q, k, v, cu_q, cu_k, key_mask, o, lse) -> XattnShape:
-    if q.dim() != 3 or k.dim() != 3 or k.shape[2] != q.shape[2]:
+def _xattn_shape(q, k, v, cu_q, cu_k, key_mask) -> XattnShape:
+    qs, ks, dtype = q.shape, k.shape, q.dtype
+    if len(qs) != 3 or len(ks) != 3 or ks[2] != qs[2]:
         raise ValueError("q is [rows, heads, d]; k and v are [encoder rows, kv heads, d]")
+    if dtype not in _DTYPES:
+        raise TypeError(f"unsupported dtype {dtype}")
     n_seg = _prefix(cu_q, "cu_q")
     if (cu_q is None) != (cu_k is None) or _prefix(cu_k, "cu_k") != n_seg:
         raise ValueError("cu_q and cu_k describe the same segments: both or neither")
-    (nq, H, d), (nk, Hk) = q.shape, k.shape[:2]
+    nq, H, d = qs
+    nk, Hk, _ = ks
     if key_mask is not None:
         if key_mask.dtype not in (torch.uint8, torch.bool) or key_mask.shape != (nk,) or not key_mask.is_contiguous():
             raise ValueError("key_mask must be a contiguous uint8 or bool vector of the encoder rows")
-    if lse.dtype != torch.float32 or tuple(lse.shape) != (H, nq) or not lse.is_contiguous():
+    _same_device(q.device, k, v, cu_q, cu_k, key_mask)
+    return XattnShape(nq, nk, n_seg, H, Hk, d, _DTYPES[dtype], _head_rows(q, dtype, qs, "q"),
+                      _head_rows(k, dtype, ks, "k"), _head_rows(v, dtype, ks, "v"), H * d)
+
+
+def _check_lse(lse: torch.Tensor, q: torch.Tensor) -> None:
+    if lse.dtype != torch.float32 or lse.shape != (q.shape[1], q.shape[0]) or not lse.is_contiguous():
         raise ValueError("lse must be a contiguous [heads, rows] fp32 tensor")
-    _same_device(q, k, v, cu_q, cu_k, key_mask, o, lse)
-    return XattnShape(nq, nk, n_seg, H, Hk, d, _dtype_code(q), _head_rows(q, q, (nq, H, d), "q"),
-                      _head_rows(k, q, (nk, Hk, d), "k"), _head_rows(v, q, (nk, Hk, d), "v"),
-                      _head_rows(o, q, (nq, H, d), "o"))
 
 
 def _workspace(ws: Optional[torch.Tensor], size: int, device):
+    """A workspace (its pointer and size): the caller's, or a new one, or none where none is needed."""
     if ws is None:
-        ws = torch.empty(max(size, 16), dtype=torch.uint8, device=device)
-    return ws, ws.numel() * ws.element_size()
+        if size == 0:
+            return None, None, 0
+        ws = torch.empty(size, dtype=torch.uint8, device=device)
+    return ws, ws.data_ptr(), ws.numel() * ws.element_size()
 
 
 def ut_xattn_fwd(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, softmax_scale: Optional[float] = None,
@@ -497,17 +512,25 @@ def ut_xattn_fwd(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, softmax_scal
     """Cross attention of packed query rows q [Nq, H, d] to encoder states k, v [Nk, Hkv, d] (rows may be strided:
     slices of one projection), segment by segment (cu_q, cu_k: int32 prefixes of the lengths, on the device), over
     the keys with key_mask != 0.  Returns (O [Nq, H, d], LSE [H, Nq] fp32)."""
+    shape = _xattn_shape(q, k, v, cu_q, cu_k, key_mask)
+    device = q.device
     if o is None:
-        o = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        o = torch.empty(q.shape, dtype=q.dtype, device=device)
+    else:
+        shape.o_stride = _head_rows(o, q.dtype, q.shape, "o")
+        _same_device(device, o)
     if lse is None:
-        lse = torch.empty((q.shape[1], q.shape[0]), dtype=torch.float32, device=q.device)
-    shape = _xattn_shape(q, k, v, cu_q, cu_k, key_mask, o, lse)
-    scale = q.shape[2] ** -0.5 if softmax_scale is None else float(softmax_scale)
-    L = lib()
-    ws, wsb = _workspace(ws, L.ut_xattn_fwd_workspace_size(ctypes.byref(shape)), q.device)
-    st = L.ut_xattn_fwd(ctypes.byref(shape), _p(q), _p(k), _p(v), _p(cu_q), _p(cu_k), _p(key_mask), scale, _p(o),
-                        _p(lse), _p(ws), wsb, _p(status), _stream())
-    _check("ut_xattn_fwd", st)
+        lse = torch.empty((shape.n_heads, shape.n_q), dtype=torch.float32, device=device)
+    else:
+        _check_lse(lse, q)
+        _same_device(device, lse)
+    L, ref = lib(), ctypes.byref(shape)
+    ws, wsp, wsb = _workspace(ws, L.ut_xattn_fwd_workspace_size(ref), device)
+    st = L.ut_xattn_fwd(ref, q.data_ptr(), k.data_ptr(), v.data_ptr(), _p(cu_q), _p(cu_k), _p(key_mask),
+                        shape.head_dim ** -0.5 if softmax_scale is None else softmax_scale, o.data_ptr(),
+                        lse.data_ptr(), wsp, wsb, _p(status), _stream())
+    if st:
+        _check("ut_xattn_fwd", st)
     return o, lse
 
 
@@ -518,43 +541,52 @@ def ut_xattn_bwd(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, o: torch.Ten
                  dv: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None,
                  status: Optional[torch.Tensor] = None):
     """Gradient of ut_xattn_fwd (o and lse are its outputs).  Returns (dQ, dK, dV)."""
-    shape = _xattn_shape(q, k, v, cu_q, cu_k, key_mask, o, lse)
-    dq = torch.empty(q.shape, dtype=q.dtype, device=q.device) if dq is None else dq
-    dk = torch.empty(k.shape, dtype=k.dtype, device=k.device) if dk is None else dk
-    dv = torch.empty(v.shape, dtype=v.dtype, device=v.device) if dv is None else dv
-    _same_device(q, dout, dq, dk, dv)
-    shape.do_stride = _head_rows(dout, q, q.shape, "dout")
-    shape.dq_stride = _head_rows(dq, q, q.shape, "dq")
-    shape.dk_stride = _head_rows(dk, q, k.shape, "dk")
-    shape.dv_stride = _head_rows(dv, q, k.shape, "dv")
-    scale = q.shape[2] ** -0.5 if softmax_scale is None else float(softmax_scale)
-    L = lib()
-    ws, wsb = _workspace(ws, L.ut_xattn_bwd_workspace_size(ctypes.byref(shape)), q.device)
-    st = L.ut_xattn_bwd(ctypes.byref(shape), _p(q), _p(k), _p(v), _p(cu_q), _p(cu_k), _p(key_mask), scale, _p(o),
-                        _p(lse), _p(dout), _p(dq), _p(dk), _p(dv), _p(ws), wsb, _p(status), _stream())
-    _check("ut_xattn_bwd", st)
+    shape = _xattn_shape(q, k, v, cu_q, cu_k, key_mask)
+    device, dtype = q.device, q.dtype
+    _check_lse(lse, q)
+    _same_device(device, o, lse, dout, dq, dk, dv)
+    shape.o_stride = _head_rows(o, dtype, q.shape, "o")
+    shape.do_stride = _head_rows(dout, dtype, q.shape, "dout")
+    H_d, Hk_d = shape.n_heads * shape.head_dim, shape.n_kv_heads * shape.head_dim
+    shape.dq_stride = H_d if dq is None else _head_rows(dq, dtype, q.shape, "dq")
+    shape.dk_stride = Hk_d if dk is None else _head_rows(dk, dtype, k.shape, "dk")
+    shape.dv_stride = Hk_d if dv is None else _head_rows(dv, dtype, k.shape, "dv")
+    dq = torch.empty(q.shape, dtype=dtype, device=device) if dq is None else dq
+    dk = torch.empty(k.shape, dtype=dtype, device=device) if dk is None else dk
+    dv = torch.empty(v.shape, dtype=dtype, device=device) if dv is None else dv
+    L, ref = lib(), ctypes.byref(shape)
+    ws, wsp, wsb = _workspace(ws, L.ut_xattn_bwd_workspace_size(ref), device)
+    st = L.ut_xattn_bwd(ref, q.data_ptr(), k.data_ptr(), v.data_ptr(), _p(cu_q), _p(cu_k), _p(key_mask),
+                        shape.head_dim ** -0.5 if softmax_scale is None else softmax_scale, o.data_ptr(),
+                        lse.data_ptr(), dout.data_ptr(), dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), wsp, wsb,
+                        _p(status), _stream())
+    if st:
+        _check("ut_xattn_bwd", st)
     return dq, dk, dv
 
 
 def _channel_rows(t: torch.Tensor, like: torch.Tensor, what: str) -> int:
-    if t.dim() != 2 or t.shape != like.shape or t.dtype != like.dtype:
+    shape = t.shape
+    if len(shape) != 2 or shape != like.shape or t.dtype != like.dtype:
         raise ValueError(f"{what} must be [rows, channels] of x's shape and dtype")
-    if t.shape[1] > 1 and t.stride(1) != 1:
+    row, one = t.stride()
+    if shape[1] > 1 and one != 1:
         raise ValueError(f"{what}: channels must be contiguous within a row")
-    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+    return row if shape[0] > 1 else shape[1]
 
 
-def _gnorm_shape(x, gamma, beta, groups, act, eps, cu, mean, rstd) -> GnormShape:
-    n_seg = _prefix(cu, "cu")
-    stride = _channel_rows(x, x, "x")
-    for t in (gamma, beta):
-        if t is not None and (t.dtype != torch.float32 or t.shape != (x.shape[1],) or not t.is_contiguous()):
-            raise ValueError("gamma and beta are contiguous fp32 vectors of the channels")
+def _affine(t: Optional[torch.Tensor], channels: int, what: str) -> Optional[int]:
+    if t is None:
+        return None
+    if t.dtype != torch.float32 or t.shape != (channels,) or not t.is_contiguous():
+        raise ValueError(f"{what} must be a contiguous fp32 vector of the channels")
+    return t.data_ptr()
+
+
+def _stats(mean: torch.Tensor, rstd: torch.Tensor, n_seg: int, groups: int) -> None:
     for t in (mean, rstd):
-        if t.dtype != torch.float32 or tuple(t.shape) != (n_seg, groups) or not t.is_contiguous():
+        if t.dtype != torch.float32 or t.shape != (n_seg, groups) or not t.is_contiguous():
             raise ValueError("mean and rstd are contiguous [segments, groups] fp32 tensors")
-    _same_device(x, gamma, beta, cu, mean, rstd)
-    return GnormShape(x.shape[0], n_seg, x.shape[1], int(groups), _dtype_code(x), int(act), float(eps), stride)
 
 
 def ut_group_norm_fwd(x: torch.Tensor, gamma: Optional[torch.Tensor], beta: Optional[torch.Tensor], groups: int,
@@ -564,21 +596,30 @@ def ut_group_norm_fwd(x: torch.Tensor, gamma: Optional[torch.Tensor], beta: Opti
                       status: Optional[torch.Tensor] = None):
     """Group norm with an activation over channels-last rows x [N, C], segment by segment (cu: int32 prefix of the
     lengths, on the device).  Returns (y [N, C], mean, rstd [segments, groups] fp32)."""
-    n_seg = _prefix(cu, "cu")
-    if mean is None:
-        mean = torch.empty((n_seg, groups), dtype=torch.float32, device=x.device)
-    if rstd is None:
-        rstd = torch.empty((n_seg, groups), dtype=torch.float32, device=x.device)
-    shape = _gnorm_shape(x, gamma, beta, groups, act, eps, cu, mean, rstd)
+    n_seg, device, dtype = _prefix(cu, "cu"), x.device, x.dtype
+    stride = _channel_rows(x, x, "x")
+    N, C = x.shape
+    if dtype not in _DTYPES:
+        raise TypeError(f"unsupported dtype {dtype}")
+    gp, bp = _affine(gamma, C, "gamma"), _affine(beta, C, "beta")
+    _same_device(device, gamma, beta, cu, y, mean, rstd)
+    y_stride = C if y is None else _channel_rows(y, x, "y")
     if y is None:
-        y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-    _same_device(x, y)
-    shape.y_stride = _channel_rows(y, x, "y")
+        y = torch.empty((N, C), dtype=dtype, device=device)
+    new_stats = mean is None and rstd is None
+    if mean is None:
+        mean = torch.empty((n_seg, groups), dtype=torch.float32, device=device)
+    if rstd is None:
+        rstd = torch.empty((n_seg, groups), dtype=torch.float32, device=device)
+    if not new_stats:
+        _stats(mean, rstd, n_seg, groups)
     L = lib()
-    ws, wsb = _workspace(ws, L.ut_group_norm_fwd_workspace_size(ctypes.byref(shape)), x.device)
-    st = L.ut_group_norm_fwd(ctypes.byref(shape), _p(x), _p(cu), _p(gamma), _p(beta), _p(y), _p(mean), _p(rstd),
-                             _p(ws), wsb, _p(status), _stream())
-    _check("ut_group_norm_fwd", st)
+    ref = ctypes.byref(GnormShape(N, n_seg, C, groups, _DTYPES[dtype], act, eps, stride, y_stride))
+    ws, wsp, wsb = _workspace(ws, L.ut_group_norm_fwd_workspace_size(ref), device)
+    st = L.ut_group_norm_fwd(ref, x.data_ptr(), _p(cu), gp, bp, y.data_ptr(), mean.data_ptr(), rstd.data_ptr(), wsp,
+                             wsb, _p(status), _stream())
+    if st:
+        _check("ut_group_norm_fwd", st)
     return y, mean, rstd
 
 
@@ -588,20 +629,27 @@ def ut_group_norm_bwd(x: torch.Tensor, dy: torch.Tensor, gamma: Optional[torch.T
                       dgamma: Optional[torch.Tensor] = None, dbeta: Optional[torch.Tensor] = None,
                       ws: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None):
     """Gradient of ut_group_norm_fwd (mean and rstd are its outputs).  Returns (dx [N, C], dgamma, dbeta [C] fp32)."""
-    shape = _gnorm_shape(x, gamma, beta, groups, act, 1.0, cu, mean, rstd)
-    dx = torch.empty(x.shape, dtype=x.dtype, device=x.device) if dx is None else dx
+    n_seg, device, dtype = _prefix(cu, "cu"), x.device, x.dtype
+    stride, dy_stride = _channel_rows(x, x, "x"), _channel_rows(dy, x, "dy")
+    N, C = x.shape
+    if dtype not in _DTYPES:
+        raise TypeError(f"unsupported dtype {dtype}")
+    gp, bp = _affine(gamma, C, "gamma"), _affine(beta, C, "beta")
+    _stats(mean, rstd, n_seg, groups)
+    _same_device(device, dy, gamma, beta, cu, mean, rstd, dx, dgamma, dbeta)
+    dx_stride = C if dx is None else _channel_rows(dx, x, "dx")
+    if dx is None:
+        dx = torch.empty((N, C), dtype=dtype, device=device)
     if dgamma is None:
-        dgamma = torch.empty(x.shape[1], dtype=torch.float32, device=x.device)
+        dgamma = torch.empty(C, dtype=torch.float32, device=device)
     if dbeta is None:
-        dbeta = torch.empty(x.shape[1], dtype=torch.float32, device=x.device)
-    for t in (dgamma, dbeta):
-        if t.dtype != torch.float32 or t.shape != (x.shape[1],) or not t.is_contiguous():
-            raise ValueError("dgamma and dbeta are contiguous fp32 vectors of the channels")
-    _same_device(x, dy, dx, dgamma, dbeta)
-    shape.dy_stride, shape.dx_stride = _channel_rows(dy, x, "dy"), _channel_rows(dx, x, "dx")
+        dbeta = torch.empty(C, dtype=torch.float32, device=device)
+    dgp, dbp = _affine(dgamma, C, "dgamma"), _affine(dbeta, C, "dbeta")
     L = lib()
-    ws, wsb = _workspace(ws, L.ut_group_norm_bwd_workspace_size(ctypes.byref(shape)), x.device)
-    st = L.ut_group_norm_bwd(ctypes.byref(shape), _p(x), _p(dy), _p(cu), _p(gamma), _p(beta), _p(mean), _p(rstd),
-                             _p(dx), _p(dgamma), _p(dbeta), _p(ws), wsb, _p(status), _stream())
-    _check("ut_group_norm_bwd", st)
+    ref = ctypes.byref(GnormShape(N, n_seg, C, groups, _DTYPES[dtype], act, 1.0, stride, 0, dy_stride, dx_stride))
+    ws, wsp, wsb = _workspace(ws, L.ut_group_norm_bwd_workspace_size(ref), device)
+    st = L.ut_group_norm_bwd(ref, x.data_ptr(), dy.data_ptr(), _p(cu), gp, bp, mean.data_ptr(), rstd.data_ptr(),
+                             dx.data_ptr(), dgp, dbp, wsp, wsb, _p(status), _stream())
+    if st:
+        _check("ut_group_norm_bwd", st)
     return dx, dgamma, dbeta
