@@ -67,12 +67,12 @@ UT_DEV void stage_k(float* dst, const void* x, int64_t key0, const float* on, in
     st4(dst + r * (D + 4) + c, v);
   }
 }
-// on[64] <- 1 where the key exists and is not masked
-UT_DEV void stage_mask(float* on, const uint8_t* mask, int64_t key0, int64_t left) {
-  if (threadIdx.x < kXs) {
-    const int r = threadIdx.x;
-    on[r] = r < left && (!mask || mask[key0 + r]) ? 1.f : 0.f;
-  }
+// on[64] <- 1 where the key exists and is not masked; whether any is.  Synchronises the block.
+UT_DEV bool stage_mask(float* on, const uint8_t* mask, int64_t key0, int64_t left) {
+  const int r = threadIdx.x;
+  const bool is = r < kXs && r < left && (!mask || mask[key0 + r]);
+  if (r < kXs) on[r] = is ? 1.f : 0.f;
+  return __syncthreads_or(is);
 }
 
 // acc[i][j] = a[ty * 4 + i] . b[tx + 16 j]
@@ -193,8 +193,7 @@ __global__ void __launch_bounds__(kXsThreads) xattn_fwd_simt_kernel(const XattnP
   }
   for (int64_t b = b0; b < b1; ++b) {
     __syncthreads();
-    stage_mask(on, p.mask, k0 + b * kXs, kn - b * kXs);
-    __syncthreads();
+    if (!stage_mask(on, p.mask, k0 + b * kXs, kn - b * kXs)) continue;  // no key of the tile is left
     stage_k<T, D>(ks, p.k, k0 + b * kXs, on, hk, p.ks);
     stage_k<T, D>(vs, p.v, k0 + b * kXs, on, hk, p.vs);
     __syncthreads();
@@ -308,8 +307,7 @@ __global__ void __launch_bounds__(kXsThreads) xattn_dq_simt_kernel(const XattnPa
     for (int c = 0; c < D / 64; ++c) acc[i][c] = make_float4(0, 0, 0, 0);
   for (int64_t b = 0; b * kXs < kn; ++b) {
     __syncthreads();
-    stage_mask(on, p.mask, k0 + b * kXs, kn - b * kXs);
-    __syncthreads();
+    if (!stage_mask(on, p.mask, k0 + b * kXs, kn - b * kXs)) continue;  // no key of the tile is left
     stage_k<T, D>(ks, p.k, k0 + b * kXs, on, hk, p.ks);
     stage_k<T, D>(vs, p.v, k0 + b * kXs, on, hk, p.vs);
     __syncthreads();
@@ -359,8 +357,7 @@ __global__ void __launch_bounds__(kXsThreads) xattn_dkdv_simt_kernel(const Xattn
   const int64_t nt = (qn + tpt - 1) / tpt, per = (nt + p.nsplit - 1) / p.nsplit;
   const int64_t t0 = per * split, t1 = min(nt, t0 + per);
   const int ty = threadIdx.x >> 4, tx = threadIdx.x & 15;
-  stage_mask(on, p.mask, key0, left);
-  __syncthreads();
+  const bool any = stage_mask(on, p.mask, key0, left);
   stage_k<T, D>(ks, p.k, key0, on, hk, p.ks);
   stage_k<T, D>(vs, p.v, key0, on, hk, p.vs);
   float4 dk[4][D / 64], dv[4][D / 64];
@@ -368,7 +365,7 @@ __global__ void __launch_bounds__(kXsThreads) xattn_dkdv_simt_kernel(const Xattn
   for (int i = 0; i < 4; ++i)
 #pragma unroll
     for (int c = 0; c < D / 64; ++c) dk[i][c] = dv[i][c] = make_float4(0, 0, 0, 0);
-  for (int64_t tt = t0; tt < t1; ++tt) {
+  for (int64_t tt = t0; any && tt < t1; ++tt) {
     XsTile t{q0 + tt * tpt, (int)min((int64_t)tpt, qn - tt * tpt) * p.G, hk * p.G, p.G};
     __syncthreads();
     stage_q<T, D>(qs, p.q, t, p.qs);
@@ -531,11 +528,13 @@ int64_t xattn_items(const XattnParams& p, bool bf16, bool backward) {
   return (backward ? segment_slots(p.nk, p.B, kXs) : segment_slots(p.nq, p.B, kXs / p.G)) * p.Hk;
 }
 
-// Enough parts for two blocks an SM, but none shorter than two tiles of an
+// Enough parts for two blocks an SM (four of the fp32 backward's, two of which
+// share an SM and whose lengths differ), but none shorter than two tiles of an
 // average segment.
 int xattn_splits(const XattnParams& p, bool bf16, bool backward) {
   if (bf16 && backward) return 1;
-  const int64_t items = xattn_items(p, bf16, backward), want = (2 * (int64_t)p.sms + items - 1) / items;
+  const int64_t items = xattn_items(p, bf16, backward);
+  const int64_t want = ((backward ? 4 : 2) * (int64_t)p.sms + items - 1) / items;
   const int64_t tile = backward ? kXs / p.G : (bf16 ? 128 : kXs);
   const int64_t tiles = ((backward ? p.nq : p.nk) / p.B + tile - 1) / tile, most = tiles / 2;
   const int64_t n = want < most ? want : most;
