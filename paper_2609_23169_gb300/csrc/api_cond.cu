@@ -196,7 +196,8 @@ ut_status ut_xattn_bwd(const ut_xattn_shape* shape, const void* q, const void* k
   if (!at16(dout) || !at16(dq) || !at16(dk) || !at16(dv)) return UT_ERR_INVALID_ARG;
   if (p.nq == 0 && p.nk == 0) return UT_OK;
   const bool bf16 = shape->dtype == UT_BF16;
-  if (!ws || ws_bytes < xattn_bwd_ws(p, bf16) || !at16(ws)) return UT_ERR_INVALID_ARG;
+  const size_t need = xattn_bwd_ws(p, bf16);  // 0 without queries
+  if (need > 0 && (!ws || ws_bytes < need || !at16(ws))) return UT_ERR_INVALID_ARG;
   char* w = static_cast<char*>(ws);
   p.dsum = reinterpret_cast<float*>(w);
   w += up256((size_t)p.H * p.nq * sizeof(float));

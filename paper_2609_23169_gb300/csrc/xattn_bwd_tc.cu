@@ -6,38 +6,33 @@
 // query heads that share the kv head.
 //
 // A query tile holds 128 rows: the G heads of a kv head of 128 / G consecutive
-// tokens of one segment (row = token * G + head).  Keys are few and queries
-// many, so a work item is a run of R query tiles of one segment and kv head,
-// against ALL the segment's key blocks (128 keys each):
-//   for each group of kSub query tiles: for each key block j: for each tile t:
-//     S^T  = K_j Q_t^T        (TMEM lanes = keys)
-//     dP^T = V_j dO_t^T
-//     dV_j += P^T dO_t,  dK_j += dS^T Q_t     (TMEM, over the tiles of the group)
-//     dQ_t = dS K_j           (TMEM lanes = query rows)
-// so S and dP are computed once per pair, and one CTA sees all key blocks of a
-// query tile: its dQ is added up in a buffer of the CTA's own (kSub tiles in
-// fp32, 512 KB at d = 128, 78 MB over the device: it stays in L2), first
-// block stored, middle ones added, the last one read, added and written as
-// bf16, always by the same thread.  No clear, no second pass, no atomic whose
-// order changes the result.  A segment of one key block needs no buffer.
-// dK_j, dV_j of an item go to partial sums of their own (by the item's place
-// in its segment), which a last kernel adds in order.  Both buffers hold
-// 16-byte pieces of neighbouring rows side by side, as the threads (a row
-// each) write and read them.
+// tokens of one segment (row = token * G + head); a key block 128 keys.
 //
-// Roles (512 threads, registers rebalanced with setmaxnreg):
-//   warp 0        TMA: K, V and the Q ring
-//   warp 1        TMEM owner and MMA issuer
-//   warp 2        zeroes the rows of a Q tile that are not this item's (past
-//                 the segment's end, or between the rows of G heads and 128):
-//                 what they hold (NaN, infinities) must not enter a sum over rows
-//   warp 3        TMA: dO; zeroes its rows likewise, and the masked keys of K
-//   warps 4-11    P^T and dS^T as bf16 into shared tiles; dK, dV out
-//   warps 12-15   dQ out of TMEM (thread = row)
-// TMEM columns: S^T / dP^T [0,128), dQ [128,128+d), dV [256,256+d), dK
-// [384,384+d).
-// Every wait is bounded; on expiry the kernel records UT_ERR_TIMEOUT, drains
-// its own copies and MMAs, frees TMEM and returns.
+// Two kernels, S and dP computed in each:
+//   xattn_dq_kernel    a query tile over its segment's key blocks j:
+//       S = Q K_j^T,  dP = dO V_j^T  ->  dS over S in TMEM,  dQ += dS K_j
+//     dQ stays in TMEM until it is whole: no partial sums, no atomics.
+//   xattn_dkdv_kernel  a key block over a run of R query tiles t:
+//       S^T = K Q_t^T -> P^T over it,  dV += P^T dO_t
+//       dP^T = V dO_t^T -> dS^T over it,  dK += dS^T Q_t
+//     A run's dK, dV go to partial sums of their own, which a last kernel adds
+//     in order.
+// That is seven products of 128 x 128 x d a pair of tiles against five of a
+// fused kernel.  The fused form was built first: its dQ parts, 64 KB of fp32 a
+// pair, have to be added up through L2, and its P^T and dS^T pass through
+// shared memory; it took 9,100 cycles a pair at 23,959 x 512 x 24 x 128 where
+// the products need 2,560.  Here P and dS never leave TMEM (they are the A
+// operands of the second products, written over the first ones' results), and
+// the elementwise work of one tile runs beside the products of the next.
+//
+// Roles of both kernels (registers rebalanced with setmaxnreg): warp 1 owns
+// TMEM and issues the products, warps 0, 2, 3 load (TMA) and zero the rows
+// that must not enter a sum over rows (masked keys, rows of other segments:
+// what they hold, NaN or infinities, is never multiplied), warps 4-11 are the
+// elementwise stage: warps w and w + 4 share 32 TMEM lanes and take 64 columns
+// each, and write their bf16 pairs over the first half of their own columns.
+// Every wait is bounded; on expiry a kernel records UT_ERR_TIMEOUT, drains its
+// own copies and MMAs, frees TMEM and returns.
 #include "common.cuh"
 #include "kernels.h"
 #include "segments.cuh"
@@ -48,93 +43,18 @@ namespace ut {
 namespace {
 
 constexpr int kT = 128;  // rows of a tile, keys of a block
-constexpr int kSub = 8;  // query tiles whose dQ a CTA adds up at a time
-constexpr int kThreads = 512;
-constexpr int kRegLaunch = 128, kRegCtl = 80, kRegEw = 160, kRegDrain = 112;
-static_assert(kRegCtl + 2 * kRegEw + kRegDrain == 4 * kRegLaunch, "setmaxnreg split must match the launch");
 constexpr uint32_t kChunkB = 128 * 128;  // 128 rows x 64 bf16
-constexpr int kQStages = 2;
-constexpr uint32_t kColDq = 128, kColDv = 256, kColDk = 384;
-
-template <int D>
-struct BwdSmem {
-  static constexpr int kC = D / 64;
-  static constexpr uint32_t kTile = kT * D * 2;
-  alignas(1024) uint8_t k[kTile];
-  alignas(1024) uint8_t v[kTile];
-  alignas(1024) uint8_t pt[2 * kChunkB];
-  alignas(1024) uint8_t dst[2 * kChunkB];
-  alignas(1024) uint8_t q[kQStages][kTile];
-  alignas(1024) uint8_t dout[kTile];
-  alignas(16) float lse2[2][kT];
-  alignas(16) float dsum[2][kT];
-  uint64_t kv_full, kv_ready, kv_empty, do_full, do_ready, do_empty;
-  uint64_t q_full[kQStages], q_ready[kQStages], q_empty[kQStages], rows_full[2];
-  uint64_t s_full, s_empty, dp_full, dp_empty, pt_full, pt_done, dst_full, ds_done, dq_empty;
-  uint64_t acc_full, acc_empty, mma_done;
-  uint32_t tmem_base;
-  int abort_flag;
-};
 
 struct BwdParams {
   XattnParams x;
   uint32_t inv_g;   // ceil(2^16 / G)
   int tpt;          // tokens of a tile
-  int R;            // tiles of an item
-  int64_t slots;    // items along the query rows
-  int64_t n_items;
+  int R;            // tiles of a run
+  int64_t n_items;  // of the launch
   float scale_log2;
   int64_t kslots;   // key blocks of all segments (with idle ones): nk / 128 + n_seg
-  bool wide;        // dq takes 32-byte stores
-  float* dq_acc;    // [grid, kSub, d / 4, 128, 4]
 };
 
-struct Work {  // one item
-  int hk, part, tiles, blocks;
-  int64_t tok0, key0;
-  int ntok, keys;  // tokens and keys of the item
-  int64_t kslot;   // first key block's place among all segments'
-};
-
-// Item u; false where its slot is idle.
-UT_DEV bool decode(const BwdParams& b, int64_t u, Work& w) {
-  const XattnParams& p = b.x;
-  w.hk = (int)(u % p.Hk);
-  const Segment g = segment_of_slot(p.cu_q, p.B, p.nq, b.R * b.tpt, u / p.Hk);
-  const int64_t t0 = g.tile * b.R * b.tpt;
-  if (t0 >= g.n) return false;
-  int64_t k0, kn;
-  segment_rows(p.cu_k, g.s, p.nk, k0, kn);
-  w.part = (int)g.tile;
-  w.tok0 = g.row + t0;
-  w.ntok = (int)min((int64_t)b.R * b.tpt, g.n - t0);
-  w.tiles = (w.ntok + b.tpt - 1) / b.tpt;
-  w.key0 = k0;
-  w.kslot = k0 / kT + g.s;
-  w.keys = (int)kn;
-  w.blocks = (int)((kn + kT - 1) / kT);
-  return true;
-}
-
-UT_DEV void red_add4(float* p, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
-  asm volatile("red.relaxed.gpu.global.add.v4.f32 [%0], {%1, %2, %3, %4};" ::"l"(p), "f"(__uint_as_float(a)), "f"(__uint_as_float(b)),
-               "f"(__uint_as_float(c)), "f"(__uint_as_float(d))
-               : "memory");
-}
-// a whole 32-byte sector (a pair of 16-byte stores would write it in halves)
-UT_DEV void st_v8(void* p, const uint32_t (&v)[8]) {
-  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(v[0]), "r"(v[1]), "r"(v[2]),
-               "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7])
-               : "memory");
-}
-UT_DEV float4 ld_l2(const float* p) {
-  float4 v;
-  asm volatile("ld.relaxed.gpu.global.v4.f32 {%0, %1, %2, %3}, [%4];"
-               : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w)
-               : "l"(p)
-               : "memory");
-  return v;
-}
 UT_DEV void tmem_ld64(uint32_t taddr, uint32_t* r) {
   tmem_ld32(taddr, *reinterpret_cast<uint32_t(*)[32]>(r));
   tmem_ld32(taddr + 32, *reinterpret_cast<uint32_t(*)[32]>(r + 32));
@@ -146,13 +66,53 @@ UT_DEV void zero_tail(uint32_t base, int chunks, int first, uint32_t lane) {
     for (int c = 0; c < chunks; ++c) st_shared_v4(base + c * kChunkB + r * 128 + ((lane & 7) << 4), 0, 0, 0, 0);
 }
 
+// =========================================================================
+//                                   dQ
+// =========================================================================
+// TMEM columns: S_j / dS_j [0,128) and [256,384) in turn, dP [128,256), dQ
+// [384,384+d).  The tensor core is given S two blocks and dP one block ahead
+// of dQ, across items, so that it works while the elementwise warps do.
+//   warp 0      TMA: K and V rings
+//   warp 2      decodes the items into a ring; TMA: Q and dO
+//   warp 3      zeroes the masked keys of K
+//   warps 12-15 dQ out
+constexpr int kDqThreads = 512;
+constexpr int kDqLaunch = 128, kDqCtl = 80, kDqEw = 152, kDqOut = 128;
+static_assert(kDqCtl + 2 * kDqEw + kDqOut <= 4 * kDqLaunch, "setmaxnreg split must fit the launch");
+constexpr int kDqSlots = 8, kDqReaders = 15;
+
+struct DqItem {
+  int32_t hk;      // kv head; -1: no more items
+  int32_t blocks;  // key blocks, at least one
+  int32_t tok0, ntok;
+  int32_t key0, keys;
+};
+
 template <int D>
-__global__ void __launch_bounds__(kThreads, 1)
-    xattn_bwd_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k,
-                        const __grid_constant__ CUtensorMap tm_v, const __grid_constant__ CUtensorMap tm_do,
-                        const BwdParams prm) {
+struct DqSmem {
+  static constexpr int kC = D / 64;
+  static constexpr uint32_t kTile = kT * D * 2;
+  static constexpr int kK = D == 128 ? 3 : 5, kV = D == 128 ? 2 : 4;
+  alignas(1024) uint8_t q[kTile];
+  alignas(1024) uint8_t dout[kTile];
+  alignas(1024) uint8_t k[kK][kTile];
+  alignas(1024) uint8_t v[kV][kTile];
+  uint64_t q_full, q_empty, do_full, do_empty;
+  uint64_t k_full[kK], k_ready[kK], k_empty[kK], v_full[kV], v_empty[kV];
+  uint64_t s_full[2], dp_full, dp_empty, ds_full[2], dq_full, dq_empty, mma_done;
+  uint64_t item_full[kDqSlots], item_empty[kDqSlots];
+  DqItem item[kDqSlots];
+  uint32_t tmem_base;
+  int abort_flag;
+};
+
+template <int D>
+__global__ void __launch_bounds__(kDqThreads, 1)
+    xattn_dq_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k,
+                    const __grid_constant__ CUtensorMap tm_v, const __grid_constant__ CUtensorMap tm_do,
+                    const BwdParams prm) {
   extern __shared__ __align__(1024) uint8_t smem_raw[];
-  using S = BwdSmem<D>;
+  using S = DqSmem<D>;
   S& sm = *reinterpret_cast<S*>(smem_raw);
   const XattnParams& p = prm.x;
   const uint32_t warp = warp_id(), lane = lane_id();
@@ -162,19 +122,26 @@ __global__ void __launch_bounds__(kThreads, 1)
     return;
   }
   if (threadIdx.x == 0) {
-    uint64_t* one[] = {&sm.kv_full, &sm.kv_ready, &sm.kv_empty, &sm.do_full, &sm.do_ready, &sm.do_empty, &sm.s_full,
-                       &sm.dp_full, &sm.pt_done, &sm.ds_done, &sm.acc_full, &sm.mma_done};
-    for (uint64_t* b : one) mbar_init(b, 1);
-    for (int s = 0; s < kQStages; ++s) {
-      mbar_init(&sm.q_full[s], 1);
-      mbar_init(&sm.q_ready[s], 1);
-      mbar_init(&sm.q_empty[s], 1);
+    uint64_t* one[] = {&sm.q_full, &sm.q_empty, &sm.do_full, &sm.do_empty, &sm.s_full[0], &sm.s_full[1], &sm.dp_full,
+                       &sm.dq_full, &sm.mma_done};
+    for (uint64_t* x : one) mbar_init(x, 1);
+    for (int s = 0; s < S::kK; ++s) {
+      mbar_init(&sm.k_full[s], 1);
+      mbar_init(&sm.k_ready[s], 1);
+      mbar_init(&sm.k_empty[s], 1);
     }
-    uint64_t* eight[] = {&sm.s_empty, &sm.dp_empty, &sm.pt_full, &sm.dst_full, &sm.acc_empty};
-    for (uint64_t* b : eight) mbar_init(b, 8);
+    for (int s = 0; s < S::kV; ++s) {
+      mbar_init(&sm.v_full[s], 1);
+      mbar_init(&sm.v_empty[s], 1);
+    }
+    mbar_init(&sm.dp_empty, 8);
+    mbar_init(&sm.ds_full[0], 8);
+    mbar_init(&sm.ds_full[1], 8);
     mbar_init(&sm.dq_empty, 4);
-    mbar_init(&sm.rows_full[0], 256);
-    mbar_init(&sm.rows_full[1], 256);
+    for (int s = 0; s < kDqSlots; ++s) {
+      mbar_init(&sm.item_full[s], 1);
+      mbar_init(&sm.item_empty[s], kDqReaders);
+    }
     sm.abort_flag = 0;
     fence_barrier_init();
   }
@@ -199,374 +166,721 @@ __global__ void __launch_bounds__(kThreads, 1)
   auto drain = [&](uint64_t* bar, uint32_t parity) {
     if (!mbar_drain(bar, parity, kDrainTimeoutNs)) set_status(p.status, UT_ERR_TIMEOUT);
   };
-  // tiles that dQ is added up for at a time
-  auto group_of = [&](const Work& w) { return w.blocks > 1 ? kSub : w.tiles; };
+  // The next item; false at the end or on an abort (then ok = false).
+  auto next_item = [&](uint32_t& n, DqItem& it, bool& ok, bool one) -> bool {
+    const uint32_t s = n % kDqSlots, f = (n / kDqSlots) & 1;
+    ok = one ? wait1(&sm.item_full[s], f) : wait(&sm.item_full[s], f);
+    if (!ok) return false;
+    it = sm.item[s];
+    if (!one) __syncwarp();
+    if (one || lane == 0) mbar_arrive(&sm.item_empty[s]);
+    ++n;
+    return it.hk >= 0;
+  };
 
-  const uint32_t wg = warp >> 2;
-  if (wg == 0) {
-    setmaxnreg_dec<kRegCtl>();
+  if (warp < 4) {
+    setmaxnreg_dec<kDqCtl>();
+    if (warp == 0 && lane == 0) {
+      // ------------------------------------------------------------- K, V
+      tma_prefetch_desc(&tm_k);
+      tma_prefetch_desc(&tm_v);
+      const uint64_t keep = policy_evict_last();
+      uint32_t n = 0, at = 0;
+      bool ok = true;
+      DqItem it;
+      while (ok && next_item(n, it, ok, true))
+        for (int j = 0; j < it.blocks; ++j, ++at) {
+          const uint32_t ks = at % S::kK, vs = at % S::kV;
+          if (!(ok = wait1(&sm.k_empty[ks], ((at / S::kK) & 1) ^ 1))) break;
+          mbar_expect_tx(&sm.k_full[ks], S::kTile);
+          for (int c = 0; c < S::kC; ++c)
+            tma_load_3d(sm.k[ks] + c * kChunkB, &tm_k, &sm.k_full[ks], c * 64, it.hk, it.key0 + j * kT, keep);
+          if (!(ok = wait1(&sm.v_empty[vs], ((at / S::kV) & 1) ^ 1))) {
+            drain(&sm.k_full[ks], (at / S::kK) & 1);
+            break;
+          }
+          mbar_expect_tx(&sm.v_full[vs], S::kTile);
+          for (int c = 0; c < S::kC; ++c)
+            tma_load_3d(sm.v[vs] + c * kChunkB, &tm_v, &sm.v_full[vs], c * 64, it.hk, it.key0 + j * kT, keep);
+        }
+      for (uint32_t x = at > S::kK ? at - S::kK : 0; x < at; ++x) drain(&sm.k_full[x % S::kK], (x / S::kK) & 1);
+      for (uint32_t x = at > S::kV ? at - S::kV : 0; x < at; ++x) drain(&sm.v_full[x % S::kV], (x / S::kV) & 1);
+    } else if (warp == 2 && lane == 0) {
+      // ---------------------------------------------- items; Q and dO tiles
+      tma_prefetch_desc(&tm_q);
+      tma_prefetch_desc(&tm_do);
+      const uint64_t pol = policy_evict_first();
+      const uint32_t bytes = (uint32_t)prm.tpt * p.G * 128 * S::kC;
+      uint32_t n = 0, at = 0;
+      bool ok = true;
+      for (int64_t u = blockIdx.x; ok; u += gridDim.x) {
+        DqItem it{};
+        it.hk = -1;
+        if (u < prm.n_items) {
+          const Segment g = segment_of_slot(p.cu_q, p.B, p.nq, prm.tpt, u / p.Hk);
+          const int64_t t0 = g.tile * prm.tpt;
+          if (t0 >= g.n) continue;  // an idle slot
+          int64_t k0, kn;
+          segment_rows(p.cu_k, g.s, p.nk, k0, kn);
+          if (kn == 0) continue;  // no keys: the output warps have it
+          it.hk = (int)(u % p.Hk);
+          it.blocks = (int)((kn + kT - 1) / kT);
+          it.tok0 = (int)(g.row + t0);
+          it.ntok = (int)min((int64_t)prm.tpt, g.n - t0);
+          it.key0 = (int)k0;
+          it.keys = (int)kn;
+        }
+        const uint32_t s = n % kDqSlots, f = n / kDqSlots;
+        if (!(ok = wait1(&sm.item_empty[s], (f & 1) ^ 1))) break;
+        sm.item[s] = it;
+        mbar_arrive(&sm.item_full[s]);
+        ++n;
+        if (it.hk < 0) break;
+        if (!(ok = wait1(&sm.q_empty, (at & 1) ^ 1))) break;
+        mbar_expect_tx(&sm.q_full, bytes);
+        for (int c = 0; c < S::kC; ++c)
+          tma_load_3d(sm.q + c * kChunkB, &tm_q, &sm.q_full, c * 64, it.hk * p.G, it.tok0, pol);
+        if (!(ok = wait1(&sm.do_empty, (at & 1) ^ 1))) {
+          drain(&sm.q_full, at & 1);
+          break;
+        }
+        mbar_expect_tx(&sm.do_full, bytes);
+        for (int c = 0; c < S::kC; ++c)
+          tma_load_3d(sm.dout + c * kChunkB, &tm_do, &sm.do_full, c * 64, it.hk * p.G, it.tok0, pol);
+        ++at;
+      }
+      if (at > 0) {
+        drain(&sm.q_full, (at - 1) & 1);
+        drain(&sm.do_full, (at - 1) & 1);
+      }
+    } else if (warp == 3) {
+      // ------------------------------------------------ masked keys of K
+      uint32_t n = 0, at = 0;
+      bool ok = true;
+      DqItem it;
+      while (ok && next_item(n, it, ok, false))
+        for (int j = 0; j < it.blocks; ++j, ++at) {
+          const uint32_t st = at % S::kK;
+          const uint32_t keys = lane_keys(p.mask, (int64_t)it.key0 + j * kT, it.keys - j * kT, lane);
+          if (!(ok = wait(&sm.k_full[st], (at / S::kK) & 1))) break;
+          if (__any_sync(0xffffffffu, keys != 15u)) {
+            const uint32_t base = smem_u32(sm.k[st]);
+            for (int g = 0; g < 4; ++g)
+              if (!((keys >> g) & 1u))
+                for (int x = 0; x < 8 * S::kC; ++x)
+                  st_shared_v4(base + (x >> 3) * kChunkB + (lane + 32 * g) * 128 + (((x + lane) & 7) << 4), 0, 0, 0, 0);
+            fence_proxy_async_smem();
+            __syncwarp();
+          }
+          if (lane == 0) mbar_arrive(&sm.k_ready[st]);
+        }
+    } else if (warp == 1) {
+      // ---------------------------------------------------------- products
+      constexpr uint32_t idesc_s = idesc_bf16_f32(kT, kT, false, false);
+      constexpr uint32_t idesc_q = idesc_bf16_f32(kT, D, false, true);
+      const uint32_t q_lo = desc_lo(smem_u32(sm.q), 16), do_lo = desc_lo(smem_u32(sm.dout), 16),
+                     k_lo = desc_lo(smem_u32(sm.k[0]), 16), v_lo = desc_lo(smem_u32(sm.v[0]), 16),
+                     k_mn = desc_lo(smem_u32(sm.k[0]), kChunkB);
+      // Three cursors over the blocks of all items: S leads dP leads dQ, by two
+      // blocks at most, so by fewer items than the ring holds.
+      struct Cursor {
+        uint32_t n;     // items begun
+        int j, blocks;  // block of the item, its blocks
+        uint32_t at;    // blocks passed
+        bool end;
+      };
+      bool ok = true;
+      // makes the cursor stand on a block, or at the end
+      auto stand = [&](Cursor& c, bool release) {
+        if (c.end || c.j < c.blocks) return;
+        const uint32_t s = c.n % kDqSlots;
+        if (!(ok = wait(&sm.item_full[s], (c.n / kDqSlots) & 1))) return;
+        c.end = (int)warp_uniform((uint32_t)sm.item[s].hk) < 0;
+        c.blocks = (int)warp_uniform((uint32_t)sm.item[s].blocks);
+        c.j = 0;
+        ++c.n;
+        if (release) {  // the last cursor to read it
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&sm.item_empty[s]);
+        }
+      };
+      Cursor cs{0, 0, 0, 0, false}, cp = cs, cq = cs;
+      auto issue_s = [&]() {
+        stand(cs, false);
+        if (!ok || cs.end) return;
+        const uint32_t st = cs.at % S::kK;
+        if (cs.j == 0 && !(ok = wait(&sm.q_full, (cs.n - 1) & 1))) return;
+        if (!(ok = wait(&sm.k_ready[st], (cs.at / S::kK) & 1))) return;
+        tc_fence_after();
+        mma_nt<D>((cs.at & 1) * 256, q_lo, k_lo + st * (S::kTile >> 4), idesc_s);
+        mma_commit_w(&sm.s_full[cs.at & 1]);
+        if (cs.j == cs.blocks - 1) mma_commit_w(&sm.q_empty);
+        ++cs.j;
+        ++cs.at;
+      };
+      auto issue_dp = [&]() {
+        stand(cp, false);
+        if (!ok || cp.end) return;
+        const uint32_t st = cp.at % S::kV;
+        if (cp.j == 0 && !(ok = wait(&sm.do_full, (cp.n - 1) & 1))) return;
+        if (!(ok = wait(&sm.v_full[st], (cp.at / S::kV) & 1))) return;
+        if (!(ok = wait(&sm.dp_empty, (cp.at & 1) ^ 1))) return;
+        tc_fence_after();
+        mma_nt<D>(128, do_lo, v_lo + st * (S::kTile >> 4), idesc_s);
+        mma_commit_w(&sm.dp_full);
+        mma_commit_w(&sm.v_empty[st]);
+        if (cp.j == cp.blocks - 1) mma_commit_w(&sm.do_empty);
+        ++cp.j;
+        ++cp.at;
+      };
+      issue_s();
+      if (ok) issue_dp();
+      if (ok) issue_s();
+#pragma unroll 1
+      while (ok) {
+        stand(cq, true);
+        if (!ok || cq.end) break;
+        issue_dp();
+        if (!ok) break;
+        const uint32_t st = cq.at % S::kK;
+        if (cq.j == 0 && !(ok = wait(&sm.dq_empty, cq.n & 1))) break;  // of the item before
+        if (!(ok = wait(&sm.ds_full[cq.at & 1], (cq.at >> 1) & 1))) break;
+        tc_fence_after();
+        mma_tnh(384, (cq.at & 1) * 256, k_mn + st * (S::kTile >> 4), idesc_q, cq.j > 0);
+        mma_commit_w(&sm.k_empty[st]);
+        if (cq.j == cq.blocks - 1) mma_commit_w(&sm.dq_full);
+        ++cq.j;
+        ++cq.at;
+        issue_s();
+      }
+      mma_commit_w(&sm.mma_done);
+      drain(&sm.mma_done, 0);
+    }
+  } else if (warp < 12) {
+    setmaxnreg_inc<kDqEw>();
+    const uint32_t quarter = warp & 3, half = (warp - 4) >> 2, lane_base = (quarter * 32) << 16;
+    const int row = (int)(quarter * 32 + lane), rt = (int)(((uint32_t)row * prm.inv_g) >> 16), rg = row - rt * p.G;
+    const uint64_t c2 = pack_f32x2(prm.scale_log2, prm.scale_log2);
+    uint32_t n = 0, at = 0;
+    bool ok = true;
+    DqItem it;
+    while (ok && next_item(n, it, ok, false)) {
+      const bool there = rt < it.ntok;
+      const int64_t rv = (int64_t)(it.hk * p.G + rg) * p.nq + it.tok0 + rt;
+      const float l = there ? p.lse[rv] : INFINITY, dsum = there ? p.dsum[rv] : 0.f;
+      // a row without keys has all its columns masked; one that does not exist P = 0
+      const uint64_t l2 = pack_f32x2(-l * kLog2e, -l * kLog2e), d2 = pack_f32x2(-dsum, -dsum);
+      uint32_t keys = lane_keys(p.mask, it.key0, it.keys, lane);
+      for (int j = 0; j < it.blocks; ++j, ++at) {
+        const uint32_t now = keys;
+        if (j + 1 < it.blocks) keys = lane_keys(p.mask, (int64_t)it.key0 + (j + 1) * kT, it.keys - (j + 1) * kT, lane);
+        const uint32_t ts = lane_base + (at & 1) * 256 + half * 64;
+        if (!(ok = wait(&sm.s_full[at & 1], (at >> 1) & 1))) break;
+        tc_fence_after();
+        uint32_t r[64];
+        tmem_ld64(ts, r);
+#pragma unroll
+        for (int x = 0; x < 64; x += 2) {
+          float a, b;
+          unpack_f32x2(fma_f32x2(pack_u32x2(r[x], r[x + 1]), c2, l2), a, b);
+          r[x] = __float_as_uint(ex2_approx(a));
+          r[x + 1] = __float_as_uint(ex2_approx(b));
+        }
+        if (!(ok = wait(&sm.dp_full, at & 1))) break;
+        tc_fence_after();
+        uint32_t ds[32];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          uint32_t v[32];
+          tmem_ld32(lane_base + 128 + half * 64 + h * 32, v);
+          tmem_wait_ld();
+          if (h == 1) {
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&sm.dp_empty);
+          }
+#pragma unroll
+          for (int x = 0; x < 32; x += 2) {
+            float a, b;
+            unpack_f32x2(mul_f32x2(pack_u32x2(r[h * 32 + x], r[h * 32 + x + 1]),
+                                   add_f32x2(pack_u32x2(v[x], v[x + 1]), d2)),
+                         a, b);
+            ds[h * 16 + x / 2] = pack_bf16x2(a, b);
+          }
+        }
+        if (!__all_sync(0xffffffffu, now == 15u)) {  // dS of a masked key is zero, whatever S and dP are
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const uint32_t word = __ballot_sync(0xffffffffu, (now >> (half * 2 + h)) & 1u);
+#pragma unroll
+            for (int x = 0; x < 16; ++x)
+              ds[h * 16 + x] &= (((word >> (2 * x)) & 1u) ? 0xFFFFu : 0u) | (((word >> (2 * x + 1)) & 1u) ? 0xFFFF0000u : 0u);
+          }
+        }
+        tmem_st32(ts, ds);
+        tmem_wait_st();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&sm.ds_full[at & 1]);
+      }
+    }
+  } else {
+    static_assert(kDqOut == kDqLaunch, "the output warps keep their registers");
+    const uint32_t quarter = warp & 3, lane_base = (quarter * 32) << 16, c = lane & 3;
+    auto token_of = [&](uint32_t r) -> uint32_t { return (r * prm.inv_g) >> 16; };
+    // dQ of row y of a tile, nullptr where it has no such row
+    auto row_of = [&](int64_t tok0, int ntok, int hk, uint32_t y) -> __nv_bfloat16* {
+      const uint32_t yt = token_of(y);
+      return (int)yt < ntok ? static_cast<__nv_bfloat16*>(p.dq) + (tok0 + yt) * p.dqs +
+                                  ((int64_t)hk * p.G + (y - yt * p.G)) * D + c * 8
+                            : nullptr;
+    };
+    // Tiles of segments without keys: dQ = 0.  32 items are looked at together.
+    if (p.cu_k || p.nk == 0)
+      for (int64_t u0 = blockIdx.x; u0 < prm.n_items; u0 += (int64_t)32 * gridDim.x) {
+        const int64_t u = u0 + (int64_t)lane * gridDim.x;
+        int64_t tok0 = 0, k0, kn;
+        int ntok = 0;
+        if (u < prm.n_items) {
+          const Segment g = segment_of_slot(p.cu_q, p.B, p.nq, prm.tpt, u / p.Hk);
+          const int64_t t0 = g.tile * prm.tpt;
+          segment_rows(p.cu_k, g.s, p.nk, k0, kn);
+          tok0 = g.row + t0;
+          if (t0 < g.n && kn == 0) ntok = (int)min((int64_t)prm.tpt, g.n - t0);
+        }
+        for (uint32_t found = __ballot_sync(0xffffffffu, ntok > 0); found; found &= found - 1) {
+          const int who = __ffs(found) - 1;
+          const int64_t tk = __shfl_sync(0xffffffffu, tok0, who);
+          const int nt = __shfl_sync(0xffffffffu, ntok, who), hk = (int)((u0 + (int64_t)who * gridDim.x) % p.Hk);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            __nv_bfloat16* o = row_of(tk, nt, hk, quarter * 32 + (lane & ~3u) + i);
+            if (o)
+              for (int g = 0; g < D / 32; ++g) *reinterpret_cast<uint4*>(o + g * 32) = make_uint4(0, 0, 0, 0);
+          }
+        }
+      }
+    uint32_t n = 0;
+    bool ok = true;
+    DqItem it;
+    while (ok && next_item(n, it, ok, false)) {
+      __nv_bfloat16* out[4];  // the rows of this lane's quad, its 16-byte unit
+#pragma unroll
+      for (int i = 0; i < 4; ++i) out[i] = row_of(it.tok0, it.ntok, it.hk, quarter * 32 + (lane & ~3u) + i);
+      if (!(ok = wait(&sm.dq_full, (n - 1) & 1))) break;
+      tc_fence_after();
+#pragma unroll 2
+      for (int g = 0; g < D / 32; ++g) {
+        uint32_t r[32], u[4][4];
+        tmem_ld32(lane_base + 384 + g * 32, r);
+        tmem_wait_ld();
+        if (g == D / 32 - 1) {
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&sm.dq_empty);
+        }
+#pragma unroll
+        for (int x = 0; x < 16; ++x)
+          u[x >> 2][x & 3] =
+              pack_bf16x2(__uint_as_float(r[2 * x]) * p.scale, __uint_as_float(r[2 * x + 1]) * p.scale);
+        exchange_units<1>(u, c & 1, 0, 1);
+        exchange_units<1>(u, c & 1, 2, 3);
+        exchange_units<2>(u, c >> 1, 0, 2);
+        exchange_units<2>(u, c >> 1, 1, 3);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (out[i]) *reinterpret_cast<uint4*>(out[i] + g * 32) = make_uint4(u[i][0], u[i][1], u[i][2], u[i][3]);
+      }
+    }
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  if (warp == 1) tmem_dealloc(sm.tmem_base, 512);
+}
+
+// =========================================================================
+//                                 dK, dV
+// =========================================================================
+// TMEM columns: S^T / P^T [0,128), dP^T / dS^T [128,256), dV [256,256+d), dK
+// [384,384+d); lanes = keys.  Per tile t the tensor core runs dV_t, S^T_{t+1}
+// while the elementwise warps form dS^T_t, and dK_t, dP^T_{t+1} while they form
+// P^T_{t+1}.
+//   warp 0   TMA: K, V and the Q ring      warp 2   zeroes Q rows that are not
+//   warp 3   TMA: the dO ring, and its rows          the item's
+constexpr int kKvThreads = 384;
+constexpr int kKvLaunch = 168, kKvCtl = 88, kKvEw = 208;
+static_assert(kKvCtl + 2 * kKvEw <= 3 * kKvLaunch, "setmaxnreg split must fit the launch");
+
+template <int D>
+struct KvSmem {
+  static constexpr int kC = D / 64;
+  static constexpr uint32_t kTile = kT * D * 2;
+  static constexpr int kQ = D == 128 ? 3 : 4, kDo = D == 128 ? 2 : 4;
+  alignas(1024) uint8_t k[kTile];
+  alignas(1024) uint8_t v[kTile];
+  alignas(1024) uint8_t q[kQ][kTile];
+  alignas(1024) uint8_t dout[kDo][kTile];
+  alignas(16) float lse2[2][kT];
+  alignas(16) float dsum[2][kT];
+  uint64_t kv_full, kv_empty, q_full[kQ], q_ready[kQ], q_empty[kQ], do_full[kDo], do_ready[kDo], do_empty[kDo];
+  uint64_t rows_full[2], s_full, dp_full, p_full, ds_full, acc_full, acc_empty, mma_done;
+  uint32_t tmem_base;
+  int abort_flag;
+};
+
+struct Work {  // one item: a run of query tiles and a kv head
+  int hk, part, tiles, blocks;
+  int64_t tok0, key0;
+  int ntok, keys;  // tokens of the run, keys of the segment
+  int64_t kslot;   // first key block's place among all segments'
+};
+
+// Item u; false where its slot is idle.
+UT_DEV bool decode(const BwdParams& b, int64_t u, Work& w) {
+  const XattnParams& p = b.x;
+  w.hk = (int)(u % p.Hk);
+  const Segment g = segment_of_slot(p.cu_q, p.B, p.nq, b.R * b.tpt, u / p.Hk);
+  const int64_t t0 = g.tile * b.R * b.tpt;
+  if (t0 >= g.n) return false;
+  int64_t k0, kn;
+  segment_rows(p.cu_k, g.s, p.nk, k0, kn);
+  w.part = (int)g.tile;
+  w.tok0 = g.row + t0;
+  w.ntok = (int)min((int64_t)b.R * b.tpt, g.n - t0);
+  w.tiles = (w.ntok + b.tpt - 1) / b.tpt;
+  w.key0 = k0;
+  w.kslot = k0 / kT + g.s;
+  w.keys = (int)kn;
+  w.blocks = (int)((kn + kT - 1) / kT);
+  return true;
+}
+
+template <int D>
+__global__ void __launch_bounds__(kKvThreads, 1)
+    xattn_dkdv_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k,
+                      const __grid_constant__ CUtensorMap tm_v, const __grid_constant__ CUtensorMap tm_do,
+                      const BwdParams prm) {
+  extern __shared__ __align__(1024) uint8_t smem_raw[];
+  using S = KvSmem<D>;
+  S& sm = *reinterpret_cast<S*>(smem_raw);
+  const XattnParams& p = prm.x;
+  const uint32_t warp = warp_id(), lane = lane_id();
+  volatile int* abort_flag = &sm.abort_flag;
+  if ((smem_u32(smem_raw) & 1023u) != 0) {
+    if (threadIdx.x == 0) set_status(p.status, UT_ERR_INVALID_ARG);
+    return;
+  }
+  if (threadIdx.x == 0) {
+    uint64_t* one[] = {&sm.kv_full, &sm.kv_empty, &sm.s_full, &sm.dp_full, &sm.acc_full, &sm.mma_done};
+    for (uint64_t* x : one) mbar_init(x, 1);
+    for (int s = 0; s < S::kQ; ++s) {
+      mbar_init(&sm.q_full[s], 1);
+      mbar_init(&sm.q_ready[s], 1);
+      mbar_init(&sm.q_empty[s], 1);
+    }
+    for (int s = 0; s < S::kDo; ++s) {
+      mbar_init(&sm.do_full[s], 1);
+      mbar_init(&sm.do_ready[s], 1);
+      mbar_init(&sm.do_empty[s], 1);
+    }
+    uint64_t* eight[] = {&sm.p_full, &sm.ds_full, &sm.acc_empty};
+    for (uint64_t* x : eight) mbar_init(x, 8);
+    mbar_init(&sm.rows_full[0], 256);
+    mbar_init(&sm.rows_full[1], 256);
+    sm.abort_flag = 0;
+    fence_barrier_init();
+  }
+  if (warp == 1) {
+    tmem_alloc(&sm.tmem_base, 512);
+    tmem_relinquish();
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  if (sm.tmem_base != 0 && threadIdx.x == 0) {  // as in the dQ kernel
+    set_status(p.status, UT_ERR_CUDA);
+    sm.abort_flag = 1;
+  }
+  auto wait = [&](uint64_t* bar, uint32_t parity) {  // whole warp, converged
+    return warp_wait(bar, parity, abort_flag, p.status, p.timeout_ns);
+  };
+  auto wait1 = [&](uint64_t* bar, uint32_t parity) {  // one thread
+    return mbar_wait(bar, parity, abort_flag, p.status, p.timeout_ns);
+  };
+  auto drain = [&](uint64_t* bar, uint32_t parity) {
+    if (!mbar_drain(bar, parity, kDrainTimeoutNs)) set_status(p.status, UT_ERR_TIMEOUT);
+  };
+
+  if (warp < 4) {
+    setmaxnreg_dec<kKvCtl>();
     if (warp == 0) {
       if (lane == 0) {
-        const uint64_t first_pol = policy_evict_first(), keep = policy_evict_last();
+        const uint64_t keep = policy_evict_last();
         const uint32_t bytes = (uint32_t)prm.tpt * p.G * 128 * S::kC;
         uint32_t nkv = 0, nt = 0;
         bool ok = true;
         for (int64_t u = blockIdx.x; u < prm.n_items && ok; u += gridDim.x) {
           Work w;
           if (!decode(prm, u, w)) continue;
-          const int step = group_of(w);
-          for (int s0 = 0; s0 < w.tiles && ok; s0 += step)
-            for (int j = 0; j < w.blocks && ok; ++j) {
-              if (!(ok = wait1(&sm.kv_empty, (nkv & 1) ^ 1))) break;
-              mbar_expect_tx(&sm.kv_full, 2 * S::kTile);
-              for (int c = 0; c < S::kC; ++c) {
-                tma_load_3d(sm.k + c * kChunkB, &tm_k, &sm.kv_full, c * 64, w.hk, (int)w.key0 + j * kT, keep);
-                tma_load_3d(sm.v + c * kChunkB, &tm_v, &sm.kv_full, c * 64, w.hk, (int)w.key0 + j * kT, keep);
-              }
-              ++nkv;
-              // the last block's pass over a tile is the last reader of its rows
-              const uint64_t pol = j == w.blocks - 1 ? first_pol : keep;
-              for (int t = s0; t < min(s0 + step, w.tiles); ++t, ++nt) {
-                const uint32_t st = nt % kQStages;
-                if (!(ok = wait1(&sm.q_empty[st], ((nt / kQStages) & 1) ^ 1))) break;
-                mbar_expect_tx(&sm.q_full[st], bytes);
-                for (int c = 0; c < S::kC; ++c)
-                  tma_load_3d(sm.q[st] + c * kChunkB, &tm_q, &sm.q_full[st], c * 64, w.hk * p.G,
-                              (int)w.tok0 + t * prm.tpt, pol);
-              }
+          for (int j = 0; j < w.blocks && ok; ++j) {
+            if (!(ok = wait1(&sm.kv_empty, (nkv & 1) ^ 1))) break;
+            mbar_expect_tx(&sm.kv_full, 2 * S::kTile);
+            for (int c = 0; c < S::kC; ++c) {
+              tma_load_3d(sm.k + c * kChunkB, &tm_k, &sm.kv_full, c * 64, w.hk, (int)w.key0 + j * kT, keep);
+              tma_load_3d(sm.v + c * kChunkB, &tm_v, &sm.kv_full, c * 64, w.hk, (int)w.key0 + j * kT, keep);
             }
+            ++nkv;
+            for (int t = 0; t < w.tiles; ++t, ++nt) {
+              const uint32_t st = nt % S::kQ;
+              if (!(ok = wait1(&sm.q_empty[st], ((nt / S::kQ) & 1) ^ 1))) break;
+              mbar_expect_tx(&sm.q_full[st], bytes);
+              for (int c = 0; c < S::kC; ++c)
+                tma_load_3d(sm.q[st] + c * kChunkB, &tm_q, &sm.q_full[st], c * 64, w.hk * p.G,
+                            (int)w.tok0 + t * prm.tpt, keep);
+            }
+          }
         }
         if (nkv > 0) drain(&sm.kv_full, (nkv - 1) & 1);
-        for (uint32_t x = nt > kQStages ? nt - kQStages : 0; x < nt; ++x)
-          drain(&sm.q_full[x % kQStages], (x / kQStages) & 1);
+        for (uint32_t x = nt > S::kQ ? nt - S::kQ : 0; x < nt; ++x) drain(&sm.q_full[x % S::kQ], (x / S::kQ) & 1);
       }
     } else if (warp == 1) {
       constexpr uint32_t idesc_s = idesc_bf16_f32(kT, kT, false, false);
       constexpr uint32_t idesc_acc = idesc_bf16_f32(kT, D, false, true);
-      constexpr uint32_t idesc_dq = idesc_bf16_f32(kT, D, true, true);
       const uint32_t k_lo = desc_lo(smem_u32(sm.k), 16), v_lo = desc_lo(smem_u32(sm.v), 16),
-                     q_lo = desc_lo(smem_u32(sm.q[0]), 16), do_lo = desc_lo(smem_u32(sm.dout), 16),
-                     pt_lo = desc_lo(smem_u32(sm.pt), 16), dst_lo = desc_lo(smem_u32(sm.dst), 16);
-      // the same tiles read along their rows (MN-major operands)
-      const uint32_t k_mn = desc_lo(smem_u32(sm.k), kChunkB), q_mn = desc_lo(smem_u32(sm.q[0]), kChunkB),
-                     do_mn = desc_lo(smem_u32(sm.dout), kChunkB), dst_mn = desc_lo(smem_u32(sm.dst), kChunkB);
+                     q_lo = desc_lo(smem_u32(sm.q[0]), 16), do_lo = desc_lo(smem_u32(sm.dout[0]), 16),
+                     q_mn = desc_lo(smem_u32(sm.q[0]), kChunkB), do_mn = desc_lo(smem_u32(sm.dout[0]), kChunkB);
       uint32_t nkv = 0, nt = 0;
       bool ok = true;
+      auto issue_s = [&](uint32_t x) {  // S^T of tile number x
+        const uint32_t st = x % S::kQ;
+        if (!(ok = wait(&sm.q_ready[st], (x / S::kQ) & 1))) return;
+        tc_fence_after();
+        mma_nt<D>(0, k_lo, q_lo + st * (S::kTile >> 4), idesc_s);
+        mma_commit_w(&sm.s_full);
+      };
+      auto issue_dp = [&](uint32_t x) {  // dP^T of tile number x
+        const uint32_t st = x % S::kDo;
+        if (!(ok = wait(&sm.do_ready[st], (x / S::kDo) & 1))) return;
+        tc_fence_after();
+        mma_nt<D>(128, v_lo, do_lo + st * (S::kTile >> 4), idesc_s);
+        mma_commit_w(&sm.dp_full);
+      };
       for (int64_t u = blockIdx.x; u < prm.n_items && ok; u += gridDim.x) {
         Work w;
         if (!warp_uniform(decode(prm, u, w))) continue;
         const int tiles = (int)warp_uniform((uint32_t)w.tiles), blocks = (int)warp_uniform((uint32_t)w.blocks);
-        const int step = blocks > 1 ? kSub : tiles;
-        for (int s0 = 0; s0 < tiles && ok; s0 += step)
-          for (int j = 0; j < blocks && ok; ++j) {
-            const int L = min(step, tiles - s0);
-            if (!(ok = wait(&sm.kv_ready, nkv & 1))) break;
-            auto issue_st = [&](uint32_t x) -> bool {  // S^T of tile number x
-              const uint32_t st = x % kQStages;
-              if (!wait(&sm.q_ready[st], (x / kQStages) & 1)) return false;
-              if (!wait(&sm.dp_empty, (x & 1) ^ 1)) return false;
-              tc_fence_after();
-              mma_nt<D>(0, k_lo, q_lo + st * (S::kTile >> 4), idesc_s);
-              mma_commit_w(&sm.s_full);
-              return true;
-            };
-            if (!(ok = issue_st(nt))) break;
+        for (int j = 0; j < blocks && ok; ++j) {
+          if (!(ok = wait(&sm.kv_full, nkv & 1))) break;
+          issue_s(nt);
+          if (ok) issue_dp(nt);
+          if (!ok) break;
 #pragma unroll 1
-            for (int t = 0; t < L; ++t, ++nt) {
-              const uint32_t par = nt & 1, qst = nt % kQStages;
-              // dP^T once S^T has been read
-              if (!(ok = wait(&sm.do_ready, par))) break;
-              if (!(ok = wait(&sm.s_empty, par))) break;
-              tc_fence_after();
-              mma_nt<D>(0, v_lo, do_lo, idesc_s);
-              mma_commit_w(&sm.dp_full);
-              // dV += P^T dO
-              if (!(ok = wait(&sm.pt_full, par))) break;
-              if (t == 0 && !(ok = wait(&sm.acc_empty, (nkv & 1) ^ 1))) break;
-              tc_fence_after();
-              mma_nn128(kColDv, pt_lo, do_mn, idesc_acc, t > 0);
-              mma_commit_w(&sm.pt_done);
-              mma_commit_w(&sm.do_empty);
-              // S^T of the next tile once dP^T has been read
-              if (t + 1 < L && !(ok = issue_st(nt + 1))) break;
-              // dK += dS^T Q
-              if (!(ok = wait(&sm.dst_full, par))) break;
-              tc_fence_after();
-              mma_nn128(kColDk, dst_lo, q_mn + qst * (S::kTile >> 4), idesc_acc, t > 0);
-              mma_commit_w(&sm.q_empty[qst]);
-              // dQ = dS K once the previous one has been read
-              if (!(ok = wait(&sm.dq_empty, par ^ 1))) break;
-              tc_fence_after();
-              mma_tt128(kColDq, dst_mn, k_mn, idesc_dq);
-              mma_commit_w(&sm.ds_done);
+          for (int t = 0; t < tiles; ++t, ++nt) {
+            const uint32_t qs = nt % S::kQ, ds = nt % S::kDo;
+            if (t == 0 && !(ok = wait(&sm.acc_empty, (nkv & 1) ^ 1))) break;
+            if (!(ok = wait(&sm.p_full, nt & 1))) break;
+            tc_fence_after();
+            mma_tnh(256, 0, do_mn + ds * (S::kTile >> 4), idesc_acc, t > 0);
+            mma_commit_w(&sm.do_empty[ds]);
+            if (t + 1 < tiles) {
+              issue_s(nt + 1);
+              if (!ok) break;
             }
-            if (!ok) break;
-            mma_commit_w(&sm.kv_empty);
-            mma_commit_w(&sm.acc_full);
-            ++nkv;
+            if (!(ok = wait(&sm.ds_full, nt & 1))) break;
+            tc_fence_after();
+            mma_tnh(384, 128, q_mn + qs * (S::kTile >> 4), idesc_acc, t > 0);
+            mma_commit_w(&sm.q_empty[qs]);
+            if (t + 1 < tiles) {
+              issue_dp(nt + 1);
+              if (!ok) break;
+            }
           }
+          if (!ok) break;
+          mma_commit_w(&sm.kv_empty);
+          mma_commit_w(&sm.acc_full);
+          ++nkv;
+        }
       }
       mma_commit_w(&sm.mma_done);
       drain(&sm.mma_done, 0);
     } else {
-      // ------------- rows that must read as zero (warp 2: Q, warp 3: dO, K); dO loads
+      // ------- rows that must read as zero (warp 2: Q, warp 3: dO); dO loads
       const bool is_q = warp == 2;
-      const uint32_t kv_base = smem_u32(sm.k), bytes = (uint32_t)prm.tpt * p.G * 128 * S::kC;
-      const uint64_t first_pol = policy_evict_first(), keep = policy_evict_last();
-      uint32_t nkv = 0, nt = 0;
+      const uint32_t bytes = (uint32_t)prm.tpt * p.G * 128 * S::kC;
+      const uint64_t keep = policy_evict_last();
+      uint32_t nt = 0, sent = 0;  // tiles made ready, dO tiles asked for
       bool ok = true;
+      int64_t u2 = blockIdx.x;  // the load cursor runs ahead of the other
+      Work w2;
+      int j2 = 0, t2 = 0;
+      bool have2 = false;
+      auto load_ahead = [&]() {  // asks for the next dO tile if its stage is free; whole warp
+        while (!have2 && u2 < prm.n_items) {
+          have2 = decode(prm, u2, w2) && w2.blocks > 0;
+          if (!have2) u2 += gridDim.x;
+          j2 = t2 = 0;
+        }
+        if (!have2) return;
+        const uint32_t st = sent % S::kDo;
+        if (!(ok = wait(&sm.do_empty[st], ((sent / S::kDo) & 1) ^ 1))) return;
+        if (lane == 0) {
+          mbar_expect_tx(&sm.do_full[st], bytes);
+          for (int c = 0; c < S::kC; ++c)
+            tma_load_3d(sm.dout[st] + c * kChunkB, &tm_do, &sm.do_full[st], c * 64, w2.hk * p.G,
+                        (int)w2.tok0 + t2 * prm.tpt, keep);
+        }
+        __syncwarp();
+        ++sent;
+        if (++t2 == w2.tiles) {
+          t2 = 0;
+          if (++j2 == w2.blocks) {
+            have2 = false;
+            u2 += gridDim.x;
+          }
+        }
+      };
+      // A stage's next load is only waited for once the tile kDo - 1 before it
+      // has been made ready, so the wait always ends.
+      if (!is_q)
+        for (int x = 0; x < S::kDo - 1 && ok; ++x) load_ahead();
       for (int64_t u = blockIdx.x; u < prm.n_items && ok; u += gridDim.x) {
         Work w;
         if (!decode(prm, u, w)) continue;
-        const int step = group_of(w);
-        for (int s0 = 0; s0 < w.tiles && ok; s0 += step)
-          for (int j = 0; j < w.blocks && ok; ++j) {
-            for (int t = s0; t < min(s0 + step, w.tiles); ++t, ++nt) {
-              if (!is_q) {
-                if (!(ok = wait(&sm.do_empty, (nt & 1) ^ 1))) break;
-                if (lane == 0) {
-                  mbar_expect_tx(&sm.do_full, bytes);
-                  for (int c = 0; c < S::kC; ++c)
-                    tma_load_3d(sm.dout + c * kChunkB, &tm_do, &sm.do_full, c * 64, w.hk * p.G,
-                                (int)w.tok0 + t * prm.tpt, j == w.blocks - 1 ? first_pol : keep);
-                }
-                __syncwarp();
-                if (t == s0) {
-                  const uint32_t keys = lane_keys(p.mask, w.key0 + j * kT, w.keys - j * kT, lane);
-                  if (!(ok = wait(&sm.kv_full, nkv & 1))) break;
-                  if (__any_sync(0xffffffffu, keys != 15u)) {
-                    for (int g = 0; g < 4; ++g)
-                      if (!((keys >> g) & 1u))
-                        for (int x = 0; x < 8 * S::kC; ++x)
-                          st_shared_v4(kv_base + (x >> 3) * kChunkB + (lane + 32 * g) * 128 + (((x + lane) & 7) << 4),
-                                       0, 0, 0, 0);
-                    fence_proxy_async_smem();
-                    __syncwarp();
-                  }
-                  if (lane == 0) mbar_arrive(&sm.kv_ready);
-                  ++nkv;
-                }
-              }
-              const int rows = min(prm.tpt, w.ntok - t * prm.tpt) * p.G;
-              const uint32_t st = is_q ? nt % kQStages : 0, f = is_q ? nt / kQStages : nt;
-              if (!(ok = wait(is_q ? &sm.q_full[st] : &sm.do_full, f & 1))) break;
-              if (rows < kT) {
-                zero_tail(smem_u32(is_q ? sm.q[st] : sm.dout), S::kC, rows, lane);
-                fence_proxy_async_smem();
-                __syncwarp();
-              }
-              if (lane == 0) mbar_arrive(is_q ? &sm.q_ready[st] : &sm.do_ready);
+        for (int j = 0; j < w.blocks && ok; ++j)
+          for (int t = 0; t < w.tiles; ++t, ++nt) {
+            const int rows = min(prm.tpt, w.ntok - t * prm.tpt) * p.G;
+            const uint32_t nst = is_q ? S::kQ : S::kDo, st = nt % nst, f = nt / nst;
+            if (!(ok = wait(is_q ? &sm.q_full[st] : &sm.do_full[st], f & 1))) break;
+            if (rows < kT) {
+              zero_tail(smem_u32(is_q ? sm.q[st] : sm.dout[st]), S::kC, rows, lane);
+              fence_proxy_async_smem();
+              __syncwarp();
+            }
+            if (lane == 0) mbar_arrive(is_q ? &sm.q_ready[st] : &sm.do_ready[st]);
+            if (!is_q) {
+              load_ahead();
+              if (!ok) break;
             }
           }
       }
-      if (!is_q) {  // every copy it issued has landed (the last may not have been waited for on an abort)
-        const bool fine = __all_sync(0xffffffffu, ok);
-        if (!fine && lane == 0 && nt > 0) drain(&sm.do_full, (nt - 1) & 1);
-      }
+      if (!is_q && lane == 0)  // every copy it asked for has landed
+        for (uint32_t x = sent > S::kDo ? sent - S::kDo : 0; x < sent; ++x)
+          drain(&sm.do_full[x % S::kDo], (x / S::kDo) & 1);
     }
-  } else if (wg < 3) {
-    setmaxnreg_inc<kRegEw>();
-    // warps w and w + 4 share the 32 keys of a TMEM lane quarter and split the
-    // 128 query columns (and the d output columns) into halves
+  } else {
+    setmaxnreg_inc<kKvEw>();
     const uint32_t quarter = warp & 3, half = (warp - 4) >> 2;
     const uint32_t krow = quarter * 32 + lane, tid = threadIdx.x - 128;
-    const uint32_t lane_base = (quarter * 32) << 16;
+    const uint32_t lane_base = (quarter * 32) << 16, ts = lane_base + half * 64;
     constexpr int HC = kT / 2, HD = D / 2;
-    const float c = prm.scale_log2;
-    const uint32_t pt_row = smem_u32(sm.pt) + half * kChunkB + krow * 128;
-    const uint32_t dst_row = smem_u32(sm.dst) + half * kChunkB + krow * 128;
+    const uint64_t c2 = pack_f32x2(prm.scale_log2, prm.scale_log2);
     const int col = (int)(tid & (kT - 1)), rt = (int)(((uint32_t)col * prm.inv_g) >> 16), rg = col - rt * p.G;
     uint32_t nt = 0, ng = 0;
     bool ok = true;
     for (int64_t u = blockIdx.x; u < prm.n_items && ok; u += gridDim.x) {
       Work w;
       if (!decode(prm, u, w)) continue;
-      const int step = group_of(w);
-      // this thread's query column: LSE (threads 0-127) or D (128-255), a tile ahead
+      // this thread's query column: -LSE (threads 0-127) or -D (128-255), a tile ahead
       const float* vec = (tid < kT ? p.lse : p.dsum) + (int64_t)(w.hk * p.G + rg) * p.nq + w.tok0 + rt;
       auto row_value = [&](int t) -> float {
         const bool there = rt < min(prm.tpt, w.ntok - t * prm.tpt);
-        if (tid >= kT) return there ? vec[t * prm.tpt] : 0.f;
+        if (tid >= kT) return there ? -vec[t * prm.tpt] : 0.f;
         const float l = there ? vec[t * prm.tpt] : -INFINITY;
-        return l == -INFINITY ? INFINITY : l * kLog2e;  // no such row, or a row without keys: P = 0
+        return l == -INFINITY ? -INFINITY : -l * kLog2e;  // no such row, or a row without keys: P = 0
       };
-      for (int s0 = 0; s0 < w.tiles && ok; s0 += step)
-        for (int j = 0; j < w.blocks && ok; ++j, ++ng) {
-          const int key = j * kT + (int)krow, L = min(step, w.tiles - s0);
-          // P and dS of a masked key are zero: as a mask of the packed pairs
-          const uint32_t on = key < w.keys && (!p.mask || p.mask[w.key0 + key]) ? 0xffffffffu : 0u;
-          float rv = row_value(s0);
-          for (int t = 0; t < L; ++t, ++nt) {
-            const uint32_t par = nt & 1;
-            if (tid < kT) sm.lse2[par][col] = rv;
-            else sm.dsum[par][col] = rv;
-            mbar_arrive(&sm.rows_full[par]);
-            if (t + 1 < L) rv = row_value(s0 + t + 1);
-            if (!(ok = wait(&sm.rows_full[par], (nt >> 1) & 1))) break;
-            const float* ls = sm.lse2[par] + half * HC;
-            const float* dv = sm.dsum[par] + half * HC;
-            if (!(ok = wait(&sm.s_full, par))) break;
-            tc_fence_after();
-            float pr[HC];
-            {
-              uint32_t r[HC];
-              tmem_ld64(lane_base + half * HC, r);
-              tc_fence_before();
-              __syncwarp();
-              if (lane == 0) mbar_arrive(&sm.s_empty);
-#pragma unroll
-              for (int x = 0; x < HC; x += 4) {
-                const float4 l4 = *reinterpret_cast<const float4*>(ls + x);
-                pr[x + 0] = ex2_approx(fmaf(__uint_as_float(r[x + 0]), c, -l4.x));
-                pr[x + 1] = ex2_approx(fmaf(__uint_as_float(r[x + 1]), c, -l4.y));
-                pr[x + 2] = ex2_approx(fmaf(__uint_as_float(r[x + 2]), c, -l4.z));
-                pr[x + 3] = ex2_approx(fmaf(__uint_as_float(r[x + 3]), c, -l4.w));
-              }
-            }
-            if (!(ok = wait(&sm.pt_done, par ^ 1))) break;  // the previous dV has read the P^T tile
-#pragma unroll
-            for (int x = 0; x < HC / 8; ++x)
-              st_shared_v4(pt_row + ((x ^ (krow & 7)) << 4), pack_bf16x2(pr[8 * x], pr[8 * x + 1]) & on,
-                           pack_bf16x2(pr[8 * x + 2], pr[8 * x + 3]) & on,
-                           pack_bf16x2(pr[8 * x + 4], pr[8 * x + 5]) & on,
-                           pack_bf16x2(pr[8 * x + 6], pr[8 * x + 7]) & on);
-            fence_proxy_async_smem();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(&sm.pt_full);
-            if (!(ok = wait(&sm.dp_full, par))) break;
-            tc_fence_after();
-            uint32_t r[HC];
-            tmem_ld64(lane_base + half * HC, r);
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(&sm.dp_empty);  // S^T of the next tile may be computed
-#pragma unroll
-            for (int x = 0; x < HC; x += 4) {
-              const float4 d4 = *reinterpret_cast<const float4*>(dv + x);
-              r[x / 2] = pack_bf16x2(pr[x] * (__uint_as_float(r[x]) - d4.x),
-                                     pr[x + 1] * (__uint_as_float(r[x + 1]) - d4.y)) & on;
-              r[x / 2 + 1] = pack_bf16x2(pr[x + 2] * (__uint_as_float(r[x + 2]) - d4.z),
-                                         pr[x + 3] * (__uint_as_float(r[x + 3]) - d4.w)) & on;
-            }
-            if (!(ok = wait(&sm.ds_done, par ^ 1))) break;  // the previous dK and dQ have read the dS^T tile
-#pragma unroll
-            for (int x = 0; x < HC / 8; ++x)
-              st_shared_v4(dst_row + ((x ^ (krow & 7)) << 4), r[4 * x], r[4 * x + 1], r[4 * x + 2], r[4 * x + 3]);
-            fence_proxy_async_smem();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(&sm.dst_full);
-          }
-          if (!ok) break;
-          // dV, dK of the group: stored by the item's first group, added by the others
-          if (!(ok = wait(&sm.acc_full, ng & 1))) break;
+      for (int j = 0; j < w.blocks && ok; ++j, ++ng) {
+        const int key = j * kT + (int)krow;
+        // P and dS of a masked key are zero: as a mask of the packed pairs
+        const uint32_t on = key < w.keys && (!p.mask || p.mask[w.key0 + key]) ? 0xffffffffu : 0u;
+        float rv = row_value(0);
+        for (int t = 0; t < w.tiles; ++t, ++nt) {
+          const uint32_t par = nt & 1;
+          if (tid < kT) sm.lse2[par][col] = rv;
+          else sm.dsum[par][col] = rv;
+          mbar_arrive(&sm.rows_full[par]);
+          if (t + 1 < w.tiles) rv = row_value(t + 1);
+          if (!(ok = wait(&sm.rows_full[par], (nt >> 1) & 1))) break;
+          const float* ls = sm.lse2[par] + half * HC;
+          const float* dv = sm.dsum[par] + half * HC;
+          if (!(ok = wait(&sm.s_full, par))) break;
           tc_fence_after();
-          const int64_t at = ((((int64_t)w.part * prm.kslots + w.kslot + j) * p.Hk + w.hk) * (D / 4) + half * (HD / 4)) * kT + krow;
+          uint32_t r[HC];
+          tmem_ld64(ts, r);
+          uint32_t pk[32];
 #pragma unroll
-          for (int which = 0; which < 2; ++which) {
-            float* dst = (which ? p.part_dk : p.part_dv) + at * 4;
-#pragma unroll
-            for (int g = 0; g < HD / 32; ++g) {
-              uint32_t r[32];
-              tmem_ld32(lane_base + (which ? kColDk : kColDv) + half * HD + g * 32, r);
-              tmem_wait_ld();
-#pragma unroll
-              for (int x = 0; x < 8; ++x) {
-                float* at4 = dst + (g * 8 + x) * kT * 4;
-                if (s0 == 0) *reinterpret_cast<uint4*>(at4) = make_uint4(r[4 * x], r[4 * x + 1], r[4 * x + 2], r[4 * x + 3]);
-                else red_add4(at4, r[4 * x], r[4 * x + 1], r[4 * x + 2], r[4 * x + 3]);
-              }
-            }
+          for (int x = 0; x < HC; x += 4) {
+            const ulonglong2 l4 = *reinterpret_cast<const ulonglong2*>(ls + x);
+            float a, b, c, d;
+            unpack_f32x2(fma_f32x2(pack_u32x2(r[x], r[x + 1]), c2, l4.x), a, b);
+            unpack_f32x2(fma_f32x2(pack_u32x2(r[x + 2], r[x + 3]), c2, l4.y), c, d);
+            a = ex2_approx(a);
+            b = ex2_approx(b);
+            c = ex2_approx(c);
+            d = ex2_approx(d);
+            r[x] = __float_as_uint(a);
+            r[x + 1] = __float_as_uint(b);
+            r[x + 2] = __float_as_uint(c);
+            r[x + 3] = __float_as_uint(d);
+            pk[x / 2] = pack_bf16x2(a, b) & on;
+            pk[x / 2 + 1] = pack_bf16x2(c, d) & on;
           }
+          tmem_st32(ts, pk);
+          tmem_wait_st();
           tc_fence_before();
           __syncwarp();
-          if (lane == 0) mbar_arrive(&sm.acc_empty);
-        }
-    }
-  } else {
-    setmaxnreg_dec<kRegDrain>();
-    // dQ: TMEM lane = query row, column = d
-    const uint32_t quarter = warp & 3, row = quarter * 32 + lane, lane_base = (quarter * 32) << 16;
-    const int rt = (int)((row * prm.inv_g) >> 16);
-    const int64_t row_off = (int64_t)rt * p.dqs + (int)(row - rt * p.G) * D;
-    // the CTA's buffer: 16-byte pieces, [tile][d / 4][row]
-    float* acc = prm.dq_acc + ((int64_t)blockIdx.x * kSub * (D / 4) * kT + row) * 4;
-    uint32_t nt = 0;
-    bool ok = true;
-    for (int64_t u = blockIdx.x; u < prm.n_items && ok; u += gridDim.x) {
-      Work w;
-      if (!decode(prm, u, w)) continue;
-      const int step = group_of(w);
-      __nv_bfloat16* out0 = static_cast<__nv_bfloat16*>(p.dq) + w.tok0 * p.dqs + (int64_t)w.hk * p.G * D + row_off;
-      if (w.blocks == 0) {  // no keys: dQ = 0
-        for (int t = 0; t < w.tiles; ++t)
-          if (rt < min(prm.tpt, w.ntok - t * prm.tpt))
-            for (int x = 0; x < D; x += 8)
-              *reinterpret_cast<uint4*>(out0 + (int64_t)t * prm.tpt * p.dqs + x) = make_uint4(0, 0, 0, 0);
-        continue;
-      }
-      for (int s0 = 0; s0 < w.tiles && ok; s0 += step)
-        for (int j = 0; j < w.blocks && ok; ++j) {
-          const bool last = j == w.blocks - 1, add = j > 0;
-          for (int t = s0; t < min(s0 + step, w.tiles); ++t, ++nt) {
-            float* a = acc + (int64_t)(t - s0) * (D / 4) * kT * 4;
-            const bool there = rt < min(prm.tpt, w.ntok - t * prm.tpt);
-            __nv_bfloat16* out = out0 + (int64_t)t * prm.tpt * p.dqs;
-            float4 pre[16];  // the sum so far, 64 columns at a time, the first before the wait
-            if (last && add) {
+          if (lane == 0) mbar_arrive(&sm.p_full);
+          if (!(ok = wait(&sm.dp_full, par))) break;
+          tc_fence_after();
 #pragma unroll
-              for (int x = 0; x < 16; ++x) pre[x] = ld_l2(a + x * kT * 4);
-            }
-            if (!(ok = wait(&sm.ds_done, nt & 1))) break;
-            tc_fence_after();
+          for (int h = 0; h < 2; ++h) {
+            uint32_t v[32];
+            tmem_ld32(ts + 128 + h * 32, v);
+            tmem_wait_ld();
 #pragma unroll
-            for (int g = 0; g < D / 16; ++g) {
-              uint32_t r[16];
-              tmem_ld16(lane_base + kColDq + g * 16, r);
-              tmem_wait_ld();
-              if (g == D / 16 - 1) {
-                tc_fence_before();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(&sm.dq_empty);
-              }
-              float* ag = a + g * 4 * kT * 4;
-              if (!last) {
-#pragma unroll
-                for (int x = 0; x < 4; ++x) {
-                  if (add) red_add4(ag + x * kT * 4, r[4 * x], r[4 * x + 1], r[4 * x + 2], r[4 * x + 3]);
-                  else
-                    *reinterpret_cast<uint4*>(ag + x * kT * 4) =
-                        make_uint4(r[4 * x], r[4 * x + 1], r[4 * x + 2], r[4 * x + 3]);
-                }
-                continue;
-              }
-              float v[16];
-#pragma unroll
-              for (int x = 0; x < 16; ++x) v[x] = __uint_as_float(r[x]);
-              if (add) {
-#pragma unroll
-                for (int x = 0; x < 4; ++x) {
-                  const float4 f = pre[(g & 3) * 4 + x];
-                  v[4 * x] += f.x;
-                  v[4 * x + 1] += f.y;
-                  v[4 * x + 2] += f.z;
-                  v[4 * x + 3] += f.w;
-                  if (g + 4 < D / 16) pre[(g & 3) * 4 + x] = ld_l2(ag + (16 + x) * kT * 4);
-                }
-              }
-              if (there) {
-                uint32_t o[8];
-#pragma unroll
-                for (int y = 0; y < 8; ++y) o[y] = pack_bf16x2(v[2 * y] * p.scale, v[2 * y + 1] * p.scale);
-                if (prm.wide) {
-                  st_v8(out + g * 16, o);
-                } else {
-                  *reinterpret_cast<uint4*>(out + g * 16) = make_uint4(o[0], o[1], o[2], o[3]);
-                  *reinterpret_cast<uint4*>(out + g * 16 + 8) = make_uint4(o[4], o[5], o[6], o[7]);
-                }
-              }
+            for (int x = 0; x < 32; x += 4) {
+              const ulonglong2 d4 = *reinterpret_cast<const ulonglong2*>(dv + h * 32 + x);
+              float a, b, c, d;
+              unpack_f32x2(mul_f32x2(pack_u32x2(r[h * 32 + x], r[h * 32 + x + 1]),
+                                     add_f32x2(pack_u32x2(v[x], v[x + 1]), d4.x)),
+                           a, b);
+              unpack_f32x2(mul_f32x2(pack_u32x2(r[h * 32 + x + 2], r[h * 32 + x + 3]),
+                                     add_f32x2(pack_u32x2(v[x + 2], v[x + 3]), d4.y)),
+                           c, d);
+              pk[h * 16 + x / 2] = pack_bf16x2(a, b) & on;
+              pk[h * 16 + x / 2 + 1] = pack_bf16x2(c, d) & on;
             }
           }
+          tmem_st32(ts + 128, pk);
+          tmem_wait_st();
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&sm.ds_full);
         }
+        if (!ok) break;
+        // this run's dV, dK of the key block
+        if (!(ok = wait(&sm.acc_full, ng & 1))) break;
+        tc_fence_after();
+        const int64_t at =
+            ((((int64_t)w.part * prm.kslots + w.kslot + j) * p.Hk + w.hk) * (D / 4) + half * (HD / 4)) * kT + krow;
+#pragma unroll
+        for (int which = 0; which < 2; ++which) {
+          float* dst = (which ? p.part_dk : p.part_dv) + at * 4;
+#pragma unroll
+          for (int g = 0; g < HD / 32; ++g) {
+            uint32_t r[32];
+            tmem_ld32(lane_base + (which ? 384 : 256) + half * HD + g * 32, r);
+            tmem_wait_ld();
+#pragma unroll
+            for (int x = 0; x < 8; ++x)
+              *reinterpret_cast<uint4*>(dst + (g * 8 + x) * kT * 4) =
+                  make_uint4(r[4 * x], r[4 * x + 1], r[4 * x + 2], r[4 * x + 3]);
+          }
+        }
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&sm.acc_empty);
+      }
     }
   }
   tc_fence_before();
@@ -617,25 +931,26 @@ __global__ void __launch_bounds__(256) xattn_bwd_join_kernel(const BwdParams prm
   }
 }
 
-static_assert(sizeof(BwdSmem<128>) <= 232448, "shared layout exceeds the block limit");
+static_assert(sizeof(DqSmem<128>) <= 232448 && sizeof(KvSmem<128>) <= 232448 && sizeof(DqSmem<64>) <= 232448,
+              "shared layout exceeds the block limit");
 
-template <int D>
-cudaError_t launch_d(const BwdParams& prm, const CUtensorMap* tm, cudaStream_t s) {
-  const size_t smem = sizeof(BwdSmem<D>);
-  cudaError_t e = cudaFuncSetAttribute(xattn_bwd_tc_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+// The setmaxnreg split assumes exactly `regs` registers per thread at launch:
+// with fewer, the increases would wait for registers that never come.
+template <typename F>
+cudaError_t launch(F kern, int threads, size_t smem, int regs, const BwdParams& prm, const CUtensorMap* tm,
+                   cudaStream_t s) {
+  cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
   if (e != cudaSuccess) return e;
-  // the setmaxnreg split assumes exactly kRegLaunch registers per thread at
-  // launch: with fewer, the increases would wait for registers that never come
   cudaFuncAttributes fa;
-  e = cudaFuncGetAttributes(&fa, xattn_bwd_tc_kernel<D>);
+  e = cudaFuncGetAttributes(&fa, kern);
   if (e != cudaSuccess) return e;
-  if (fa.numRegs != kRegLaunch) return cudaErrorInvalidConfiguration;
+  if (fa.numRegs != regs) return cudaErrorInvalidConfiguration;
   const int grid = (int)(prm.n_items < prm.x.sms ? prm.n_items : prm.x.sms);
-  xattn_bwd_tc_kernel<D><<<grid, kThreads, smem, s>>>(tm[0], tm[1], tm[2], tm[3], prm);
+  kern<<<grid, threads, smem, s>>>(tm[0], tm[1], tm[2], tm[3], prm);
   return cudaGetLastError();
 }
 
-// Tiles of an item: the smallest number of whole waves of CTAs (up to four)
+// Tiles of a run: the smallest number of whole waves of CTAs (up to four)
 // that keeps them busy to within 8% of the best, so that the partial sums stay
 // few; more tiles where the partial sums would pass 1 GB.
 int tiles_per_item(const XattnParams& p) {
@@ -669,14 +984,9 @@ size_t part_bytes(const XattnParams& p, int R) {
 
 }  // namespace
 
-int64_t xattn_bwd_tc_items(const XattnParams& p) {
-  return segment_slots(p.nq, p.B, tiles_per_item(p) * (kT / p.G)) * p.Hk;
-}
+int64_t xattn_bwd_tc_items(const XattnParams& p) { return segment_slots(p.nq, p.B, kT / p.G) * p.Hk; }
 
-// partial dK, dV; the CTAs' dQ buffers
-size_t xattn_bwd_tc_ws(const XattnParams& p) {
-  return 2 * part_bytes(p, tiles_per_item(p)) + (size_t)p.sms * kSub * kT * p.d * sizeof(float);
-}
+size_t xattn_bwd_tc_ws(const XattnParams& p) { return 2 * part_bytes(p, tiles_per_item(p)); }
 
 cudaError_t launch_xattn_bwd_tc(const XattnParams& p, void* ws, cudaStream_t s) {
   BwdParams prm{};
@@ -684,14 +994,9 @@ cudaError_t launch_xattn_bwd_tc(const XattnParams& p, void* ws, cudaStream_t s) 
   prm.inv_g = (65536u + p.G - 1) / p.G;
   prm.tpt = kT / p.G;
   prm.R = tiles_per_item(p);
-  const size_t part = part_bytes(p, prm.R);
   prm.kslots = segment_slots(p.nk, p.B, kT);
-  prm.wide = (reinterpret_cast<uintptr_t>(p.dq) & 31u) == 0 && (p.dqs * 2) % 32 == 0;
   prm.x.part_dk = static_cast<float*>(ws);
-  prm.x.part_dv = reinterpret_cast<float*>(static_cast<char*>(ws) + part);
-  prm.dq_acc = reinterpret_cast<float*>(static_cast<char*>(ws) + 2 * part);
-  prm.slots = segment_slots(p.nq, p.B, prm.R * prm.tpt);
-  prm.n_items = prm.slots * p.Hk;
+  prm.x.part_dv = reinterpret_cast<float*>(static_cast<char*>(ws) + part_bytes(p, prm.R));
   prm.scale_log2 = p.scale * kLog2e;
   cudaError_t e = cudaSuccess;
   if (p.nq > 0) {
@@ -705,8 +1010,16 @@ cudaError_t launch_xattn_bwd_tc(const XattnParams& p, void* ws, cudaStream_t s) 
         !encode_tmap_heads_bf16(&tm[2], v, p.d, p.Hk, nk, vs * 2, 1, kT) ||
         !encode_tmap_heads_bf16(&tm[3], p.dout, p.d, p.H, p.nq, p.dos * 2, p.G, prm.tpt))
       return cudaErrorInvalidValue;
-    e = p.d == 64 ? launch_d<64>(prm, tm, s) : launch_d<128>(prm, tm, s);
+    prm.n_items = segment_slots(p.nq, p.B, prm.tpt) * p.Hk;
+    e = p.d == 64 ? launch(xattn_dq_kernel<64>, kDqThreads, sizeof(DqSmem<64>), kDqLaunch, prm, tm, s)
+                  : launch(xattn_dq_kernel<128>, kDqThreads, sizeof(DqSmem<128>), kDqLaunch, prm, tm, s);
     if (e != cudaSuccess) return e;
+    if (p.nk > 0) {
+      prm.n_items = segment_slots(p.nq, p.B, prm.R * prm.tpt) * p.Hk;
+      e = p.d == 64 ? launch(xattn_dkdv_kernel<64>, kKvThreads, sizeof(KvSmem<64>), kKvLaunch, prm, tm, s)
+                    : launch(xattn_dkdv_kernel<128>, kKvThreads, sizeof(KvSmem<128>), kKvLaunch, prm, tm, s);
+      if (e != cudaSuccess) return e;
+    }
   }
   if (p.nk > 0) {
     const dim3 grid((unsigned)prm.kslots, p.Hk, 2);

@@ -69,28 +69,13 @@ UT_DEV void mma_tn32(uint32_t d, uint32_t a, uint32_t b_lo, uint32_t idesc) {
                : "memory");
 }
 
-#define UT_SS2_STEP(aoff, boff, acc)                                     \
-  "add.u32 x, %1, " aoff ";\n\tadd.u32 y, %2, " boff ";\n\t"            \
-  "mov.b64 a, {x, %5};\n\tmov.b64 b, {y, %5};\n\t"                     \
-  "@e tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, " acc ";\n\t"
-#define UT_SS2_HEAD                                                                \
-  "{\n\t.reg .pred e, p, t;\n\t.reg .b64 a, b;\n\t.reg .b32 x, y;\n\t"          \
-  "setp.ne.b32 p, %4, 0;\n\tsetp.eq.b32 t, 0, 0;\n\telect.sync _|e, 0xffffffff;\n\t"
-// d (+)= A B over 128 rows of B: A a K-major tile of 128 columns in two
-// sub-tiles, B row-major (MN-major operand)
-UT_DEV void mma_nn128(uint32_t d, uint32_t a_lo, uint32_t b_lo, uint32_t idesc, uint32_t accumulate) {
-  asm volatile(UT_SS2_HEAD UT_SS2_STEP("0", "0", "p") UT_SS2_STEP("2", "128", "t") UT_SS2_STEP("4", "256", "t")
-                   UT_SS2_STEP("6", "384", "t") UT_SS2_STEP("1024", "512", "t") UT_SS2_STEP("1026", "640", "t")
-                       UT_SS2_STEP("1028", "768", "t") UT_SS2_STEP("1030", "896", "t") "}" ::"r"(d),
-               "r"(a_lo), "r"(b_lo), "r"(idesc), "r"(accumulate), "r"(kDescHi)
-               : "memory");
-}
-// d = A^T B over 128 rows of both, each row-major (MN-major operands)
-UT_DEV void mma_tt128(uint32_t d, uint32_t a_lo, uint32_t b_lo, uint32_t idesc) {
-  asm volatile(UT_SS2_HEAD UT_SS2_STEP("0", "0", "p") UT_SS2_STEP("128", "128", "t") UT_SS2_STEP("256", "256", "t")
-                   UT_SS2_STEP("384", "384", "t") UT_SS2_STEP("512", "512", "t") UT_SS2_STEP("640", "640", "t")
-                       UT_SS2_STEP("768", "768", "t") UT_SS2_STEP("896", "896", "t") "}" ::"r"(d),
-               "r"(a_lo), "r"(b_lo), "r"(idesc), "r"(0u), "r"(kDescHi)
+// d (+)= A B over 128 rows of B, A in TMEM as two halves of 64 columns, each in
+// the first 32 of the 64 columns that it replaced
+UT_DEV void mma_tnh(uint32_t d, uint32_t a, uint32_t b_lo, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(UT_TS_HEAD UT_TS_STEP("0", "0", "p") UT_TS_STEP("8", "128", "t") UT_TS_STEP("16", "256", "t")
+                   UT_TS_STEP("24", "384", "t") UT_TS_STEP("64", "512", "t") UT_TS_STEP("72", "640", "t")
+                       UT_TS_STEP("80", "768", "t") UT_TS_STEP("88", "896", "t") "}" ::"r"(d),
+               "r"(a), "r"(b_lo), "r"(idesc), "r"(accumulate), "r"(kDescHi)
                : "memory");
 }
 
