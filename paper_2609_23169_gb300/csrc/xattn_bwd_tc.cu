@@ -70,20 +70,27 @@ UT_DEV void zero_tail(uint32_t base, int chunks, int first, uint32_t lane) {
 //                                   dQ
 // =========================================================================
 // TMEM columns: S_j / dS_j [0,128) and [256,384) in turn, dP [128,256), dQ
-// [384,384+d).  The tensor core is given S two blocks and dP one block ahead
-// of dQ, across items, so that it works while the elementwise warps do.
-//   warp 0      TMA: K and V rings
-//   warp 2      decodes the items into a ring; TMA: Q and dO
-//   warp 3      zeroes the masked keys of K
+// [384,384+d).  With dS_i formed, the tensor core is given dP_{i+1}, dQ_i and
+// S_{i+2}, across items: the elementwise warps find their next S there and
+// take its exponentials while dP runs.
+//   warp 0      decodes the items into a ring; TMA, in the order of their use:
+//               Q, K_0, V_0, dO, K_1, V_1, ...
+//   warp 1      the products
+//   warp 3      zeroes the masked keys of K, says when a block has all it needs
 //   warps 12-15 dQ out
+// The issuing warp's instructions are fetched anew every block (the
+// elementwise code lies between), and it bounded the first form: 700 of them a
+// block, 3,900 cycles.  So it counts stages instead of dividing, follows one
+// cursor, whose flags the later products take over, waits for two barriers a
+// block, and calls the part of a wait that spins.
 constexpr int kDqThreads = 512;
 constexpr int kDqLaunch = 128, kDqCtl = 80, kDqEw = 152, kDqOut = 128;
 static_assert(kDqCtl + 2 * kDqEw + kDqOut <= 4 * kDqLaunch, "setmaxnreg split must fit the launch");
-constexpr int kDqSlots = 8, kDqReaders = 15;
+constexpr int kDqSlots = 8, kDqReaders = 14;
 
 struct DqItem {
-  int32_t hk;      // kv head; -1: no more items
-  int32_t blocks;  // key blocks, at least one
+  int32_t blocks;  // key blocks; 0: no more items
+  int32_t hk;      // kv head
   int32_t tok0, ntok;
   int32_t key0, keys;
 };
@@ -92,14 +99,14 @@ template <int D>
 struct DqSmem {
   static constexpr int kC = D / 64;
   static constexpr uint32_t kTile = kT * D * 2;
-  static constexpr int kK = D == 128 ? 3 : 5, kV = D == 128 ? 2 : 4;
-  alignas(1024) uint8_t q[kTile];
-  alignas(1024) uint8_t dout[kTile];
+  static constexpr int kQ = D == 128 ? 1 : 2, kK = D == 128 ? 3 : 4, kV = D == 128 ? 2 : 4;
+  alignas(1024) uint8_t q[kQ][kTile];
+  alignas(1024) uint8_t dout[kQ][kTile];
   alignas(1024) uint8_t k[kK][kTile];
   alignas(1024) uint8_t v[kV][kTile];
-  uint64_t q_full, q_empty, do_full, do_empty;
-  uint64_t k_full[kK], k_ready[kK], k_empty[kK], v_full[kV], v_empty[kV];
-  uint64_t s_full[2], dp_full, dp_empty, ds_full[2], dq_full, dq_empty, mma_done;
+  uint64_t q_full[kQ], q_empty[kQ], do_full[kQ], do_empty[kQ];
+  uint64_t k_full[kK], ready[kK], k_empty[kK], v_full[kV], dp_full[kV];  // dP done: V is free
+  uint64_t s_full[2], ds_full[2], dq_full, dq_empty, mma_done;
   uint64_t item_full[kDqSlots], item_empty[kDqSlots];
   DqItem item[kDqSlots];
   uint32_t tmem_base;
@@ -122,19 +129,23 @@ __global__ void __launch_bounds__(kDqThreads, 1)
     return;
   }
   if (threadIdx.x == 0) {
-    uint64_t* one[] = {&sm.q_full, &sm.q_empty, &sm.do_full, &sm.do_empty, &sm.s_full[0], &sm.s_full[1], &sm.dp_full,
-                       &sm.dq_full, &sm.mma_done};
+    uint64_t* one[] = {&sm.s_full[0], &sm.s_full[1], &sm.dq_full, &sm.mma_done};
     for (uint64_t* x : one) mbar_init(x, 1);
+    for (int s = 0; s < S::kQ; ++s) {
+      mbar_init(&sm.q_full[s], 1);
+      mbar_init(&sm.q_empty[s], 1);
+      mbar_init(&sm.do_full[s], 1);
+      mbar_init(&sm.do_empty[s], 1);
+    }
     for (int s = 0; s < S::kK; ++s) {
       mbar_init(&sm.k_full[s], 1);
-      mbar_init(&sm.k_ready[s], 1);
+      mbar_init(&sm.ready[s], 1);
       mbar_init(&sm.k_empty[s], 1);
     }
     for (int s = 0; s < S::kV; ++s) {
       mbar_init(&sm.v_full[s], 1);
-      mbar_init(&sm.v_empty[s], 1);
+      mbar_init(&sm.dp_full[s], 1);
     }
-    mbar_init(&sm.dp_empty, 8);
     mbar_init(&sm.ds_full[0], 8);
     mbar_init(&sm.ds_full[1], 8);
     mbar_init(&sm.dq_empty, 4);
@@ -167,55 +178,31 @@ __global__ void __launch_bounds__(kDqThreads, 1)
     if (!mbar_drain(bar, parity, kDrainTimeoutNs)) set_status(p.status, UT_ERR_TIMEOUT);
   };
   // The next item; false at the end or on an abort (then ok = false).
-  auto next_item = [&](uint32_t& n, DqItem& it, bool& ok, bool one) -> bool {
-    const uint32_t s = n % kDqSlots, f = (n / kDqSlots) & 1;
-    ok = one ? wait1(&sm.item_full[s], f) : wait(&sm.item_full[s], f);
+  auto next_item = [&](uint32_t& n, DqItem& it, bool& ok) -> bool {
+    const uint32_t s = n % kDqSlots;
+    ok = wait(&sm.item_full[s], (n / kDqSlots) & 1);
     if (!ok) return false;
     it = sm.item[s];
-    if (!one) __syncwarp();
-    if (one || lane == 0) mbar_arrive(&sm.item_empty[s]);
+    __syncwarp();
+    if (lane == 0) mbar_arrive(&sm.item_empty[s]);
     ++n;
-    return it.hk >= 0;
+    return it.blocks > 0;
   };
 
   if (warp < 4) {
     setmaxnreg_dec<kDqCtl>();
     if (warp == 0 && lane == 0) {
-      // ------------------------------------------------------------- K, V
+      // --------------------------------------------------- items and loads
+      tma_prefetch_desc(&tm_q);
       tma_prefetch_desc(&tm_k);
       tma_prefetch_desc(&tm_v);
-      const uint64_t keep = policy_evict_last();
-      uint32_t n = 0, at = 0;
-      bool ok = true;
-      DqItem it;
-      while (ok && next_item(n, it, ok, true))
-        for (int j = 0; j < it.blocks; ++j, ++at) {
-          const uint32_t ks = at % S::kK, vs = at % S::kV;
-          if (!(ok = wait1(&sm.k_empty[ks], ((at / S::kK) & 1) ^ 1))) break;
-          mbar_expect_tx(&sm.k_full[ks], S::kTile);
-          for (int c = 0; c < S::kC; ++c)
-            tma_load_3d(sm.k[ks] + c * kChunkB, &tm_k, &sm.k_full[ks], c * 64, it.hk, it.key0 + j * kT, keep);
-          if (!(ok = wait1(&sm.v_empty[vs], ((at / S::kV) & 1) ^ 1))) {
-            drain(&sm.k_full[ks], (at / S::kK) & 1);
-            break;
-          }
-          mbar_expect_tx(&sm.v_full[vs], S::kTile);
-          for (int c = 0; c < S::kC; ++c)
-            tma_load_3d(sm.v[vs] + c * kChunkB, &tm_v, &sm.v_full[vs], c * 64, it.hk, it.key0 + j * kT, keep);
-        }
-      for (uint32_t x = at > S::kK ? at - S::kK : 0; x < at; ++x) drain(&sm.k_full[x % S::kK], (x / S::kK) & 1);
-      for (uint32_t x = at > S::kV ? at - S::kV : 0; x < at; ++x) drain(&sm.v_full[x % S::kV], (x / S::kV) & 1);
-    } else if (warp == 2 && lane == 0) {
-      // ---------------------------------------------- items; Q and dO tiles
-      tma_prefetch_desc(&tm_q);
       tma_prefetch_desc(&tm_do);
-      const uint64_t pol = policy_evict_first();
+      const uint64_t keep = policy_evict_last();
       const uint32_t bytes = (uint32_t)prm.tpt * p.G * 128 * S::kC;
-      uint32_t n = 0, at = 0;
+      uint32_t n = 0, at = 0, nv = 0, ndo = 0;  // items, K, V and dO tiles asked for
       bool ok = true;
       for (int64_t u = blockIdx.x; ok; u += gridDim.x) {
         DqItem it{};
-        it.hk = -1;
         if (u < prm.n_items) {
           const Segment g = segment_of_slot(p.cu_q, p.B, p.nq, prm.tpt, u / p.Hk);
           const int64_t t0 = g.tile * prm.tpt;
@@ -230,35 +217,50 @@ __global__ void __launch_bounds__(kDqThreads, 1)
           it.key0 = (int)k0;
           it.keys = (int)kn;
         }
-        const uint32_t s = n % kDqSlots, f = n / kDqSlots;
-        if (!(ok = wait1(&sm.item_empty[s], (f & 1) ^ 1))) break;
+        const uint32_t s = n % kDqSlots;
+        if (!(ok = wait1(&sm.item_empty[s], ((n / kDqSlots) & 1) ^ 1))) break;
         sm.item[s] = it;
         mbar_arrive(&sm.item_full[s]);
+        if (it.blocks == 0) break;
+        const uint32_t qs = n % S::kQ, qf = (n / S::kQ) & 1;
+        if (!(ok = wait1(&sm.q_empty[qs], qf ^ 1))) break;
+        mbar_expect_tx(&sm.q_full[qs], bytes);
+        for (int c = 0; c < S::kC; ++c)
+          tma_load_3d(sm.q[qs] + c * kChunkB, &tm_q, &sm.q_full[qs], c * 64, it.hk * p.G, it.tok0, keep);
         ++n;
-        if (it.hk < 0) break;
-        if (!(ok = wait1(&sm.q_empty, (at & 1) ^ 1))) break;
-        mbar_expect_tx(&sm.q_full, bytes);
-        for (int c = 0; c < S::kC; ++c)
-          tma_load_3d(sm.q + c * kChunkB, &tm_q, &sm.q_full, c * 64, it.hk * p.G, it.tok0, pol);
-        if (!(ok = wait1(&sm.do_empty, (at & 1) ^ 1))) {
-          drain(&sm.q_full, at & 1);
-          break;
+        for (int j = 0; j < it.blocks; ++j) {
+          const uint32_t ks = at % S::kK, vs = nv % S::kV;
+          if (!(ok = wait1(&sm.k_empty[ks], ((at / S::kK) & 1) ^ 1))) break;
+          mbar_expect_tx(&sm.k_full[ks], S::kTile);
+          for (int c = 0; c < S::kC; ++c)
+            tma_load_3d(sm.k[ks] + c * kChunkB, &tm_k, &sm.k_full[ks], c * 64, it.hk, it.key0 + j * kT, keep);
+          ++at;
+          if (!(ok = wait1(&sm.dp_full[vs], ((nv / S::kV) & 1) ^ 1))) break;
+          mbar_expect_tx(&sm.v_full[vs], S::kTile);
+          for (int c = 0; c < S::kC; ++c)
+            tma_load_3d(sm.v[vs] + c * kChunkB, &tm_v, &sm.v_full[vs], c * 64, it.hk, it.key0 + j * kT, keep);
+          ++nv;
+          if (j > 0) continue;
+          if (!(ok = wait1(&sm.do_empty[qs], qf ^ 1))) break;
+          mbar_expect_tx(&sm.do_full[qs], bytes);
+          for (int c = 0; c < S::kC; ++c)
+            tma_load_3d(sm.dout[qs] + c * kChunkB, &tm_do, &sm.do_full[qs], c * 64, it.hk * p.G, it.tok0, keep);
+          ++ndo;
         }
-        mbar_expect_tx(&sm.do_full, bytes);
-        for (int c = 0; c < S::kC; ++c)
-          tma_load_3d(sm.dout + c * kChunkB, &tm_do, &sm.do_full, c * 64, it.hk * p.G, it.tok0, pol);
-        ++at;
       }
-      if (at > 0) {
-        drain(&sm.q_full, (at - 1) & 1);
-        drain(&sm.do_full, (at - 1) & 1);
-      }
+      auto landed = [&](uint64_t* bar, uint32_t stages, uint32_t sent) {
+        for (uint32_t x = sent > stages ? sent - stages : 0; x < sent; ++x) drain(bar + x % stages, (x / stages) & 1);
+      };
+      landed(sm.q_full, S::kQ, n);
+      landed(sm.k_full, S::kK, at);
+      landed(sm.v_full, S::kV, nv);
+      landed(sm.do_full, S::kQ, ndo);
     } else if (warp == 3) {
-      // ------------------------------------------------ masked keys of K
+      // ------------------------ masked keys of K; Q (of a first block), K, V
       uint32_t n = 0, at = 0;
       bool ok = true;
       DqItem it;
-      while (ok && next_item(n, it, ok, false))
+      while (ok && next_item(n, it, ok))
         for (int j = 0; j < it.blocks; ++j, ++at) {
           const uint32_t st = at % S::kK;
           const uint32_t keys = lane_keys(p.mask, (int64_t)it.key0 + j * kT, it.keys - j * kT, lane);
@@ -272,87 +274,92 @@ __global__ void __launch_bounds__(kDqThreads, 1)
             fence_proxy_async_smem();
             __syncwarp();
           }
-          if (lane == 0) mbar_arrive(&sm.k_ready[st]);
+          if (j == 0 && !(ok = wait(&sm.q_full[(n - 1) % S::kQ], ((n - 1) / S::kQ) & 1))) break;
+          if (!(ok = wait(&sm.v_full[at % S::kV], (at / S::kV) & 1))) break;
+          if (lane == 0) mbar_arrive(&sm.ready[st]);
         }
     } else if (warp == 1) {
       // ---------------------------------------------------------- products
       constexpr uint32_t idesc_s = idesc_bf16_f32(kT, kT, false, false);
       constexpr uint32_t idesc_q = idesc_bf16_f32(kT, D, false, true);
-      const uint32_t q_lo = desc_lo(smem_u32(sm.q), 16), do_lo = desc_lo(smem_u32(sm.dout), 16),
+      constexpr uint32_t kStep = S::kTile >> 4, kFirst = 2, kLast = 4;
+      const uint32_t q_lo = desc_lo(smem_u32(sm.q[0]), 16), do_lo = desc_lo(smem_u32(sm.dout[0]), 16),
                      k_lo = desc_lo(smem_u32(sm.k[0]), 16), v_lo = desc_lo(smem_u32(sm.v[0]), 16),
                      k_mn = desc_lo(smem_u32(sm.k[0]), kChunkB);
-      // Three cursors over the blocks of all items: S leads dP leads dQ, by two
-      // blocks at most, so by fewer items than the ring holds.
-      struct Cursor {
-        uint32_t n;     // items begun
-        int j, blocks;  // block of the item, its blocks
-        uint32_t at;    // blocks passed
-        bool end;
+      auto waitq = [&](uint64_t* bar, uint32_t parity) -> bool {
+        return quick_wait(bar, parity, abort_flag, p.status, p.timeout_ns);
       };
-      bool ok = true;
-      // makes the cursor stand on a block, or at the end
-      auto stand = [&](Cursor& c, bool release) {
-        if (c.end || c.j < c.blocks) return;
-        const uint32_t s = c.n % kDqSlots;
-        if (!(ok = wait(&sm.item_full[s], (c.n / kDqSlots) & 1))) return;
-        c.end = (int)warp_uniform((uint32_t)sm.item[s].hk) < 0;
-        c.blocks = (int)warp_uniform((uint32_t)sm.item[s].blocks);
-        c.j = 0;
-        ++c.n;
-        if (release) {  // the last cursor to read it
+      uint32_t n = 0, left = 0;             // items begun; blocks left of the one of S
+      uint32_t sk = 0, sf = 0;              // K stage and phase of S
+      uint32_t pv = 0, qk = 0;              // V stage of dP, K stage of dQ
+      uint32_t buf = 0, dsf = 0;            // S buffer of S (and of dQ), phases of ds_full
+      uint32_t sq = S::kQ - 1, pq = sq;     // Q stage of S, dO stage of dP
+      uint32_t pf = 1, dqf = 0;             // phases of do_full and dq_empty
+      uint32_t f0 = 0, f1 = 0, f2;          // flags of the blocks of dQ, dP and S; 0: none
+      bool ok = true, end = false;
+#pragma unroll 1
+      do {
+        f2 = 0;
+        if (left > 0) {
+          f2 = left == 1 ? 1u | kLast : 1u;
+          --left;
+        } else if (!end) {
+          const uint32_t s = n % kDqSlots;
+          if (!(ok = waitq(&sm.item_full[s], (n / kDqSlots) & 1))) break;
+          left = warp_uniform((uint32_t)sm.item[s].blocks);
           __syncwarp();
           if (lane == 0) mbar_arrive(&sm.item_empty[s]);
+          ++n;
+          end = left == 0;
+          if (!end) {
+            sq = sq + 1 == S::kQ ? 0 : sq + 1;
+            f2 = left == 1 ? 1u | kFirst | kLast : 1u | kFirst;
+            --left;
+          }
         }
-      };
-      Cursor cs{0, 0, 0, 0, false}, cp = cs, cq = cs;
-      auto issue_s = [&]() {
-        stand(cs, false);
-        if (!ok || cs.end) return;
-        const uint32_t st = cs.at % S::kK;
-        if (cs.j == 0 && !(ok = wait(&sm.q_full, (cs.n - 1) & 1))) return;
-        if (!(ok = wait(&sm.k_ready[st], (cs.at / S::kK) & 1))) return;
-        tc_fence_after();
-        mma_nt<D>((cs.at & 1) * 256, q_lo, k_lo + st * (S::kTile >> 4), idesc_s);
-        mma_commit_w(&sm.s_full[cs.at & 1]);
-        if (cs.j == cs.blocks - 1) mma_commit_w(&sm.q_empty);
-        ++cs.j;
-        ++cs.at;
-      };
-      auto issue_dp = [&]() {
-        stand(cp, false);
-        if (!ok || cp.end) return;
-        const uint32_t st = cp.at % S::kV;
-        if (cp.j == 0 && !(ok = wait(&sm.do_full, (cp.n - 1) & 1))) return;
-        if (!(ok = wait(&sm.v_full[st], (cp.at / S::kV) & 1))) return;
-        if (!(ok = wait(&sm.dp_empty, (cp.at & 1) ^ 1))) return;
-        tc_fence_after();
-        mma_nt<D>(128, do_lo, v_lo + st * (S::kTile >> 4), idesc_s);
-        mma_commit_w(&sm.dp_full);
-        mma_commit_w(&sm.v_empty[st]);
-        if (cp.j == cp.blocks - 1) mma_commit_w(&sm.do_empty);
-        ++cp.j;
-        ++cp.at;
-      };
-      issue_s();
-      if (ok) issue_dp();
-      if (ok) issue_s();
-#pragma unroll 1
-      while (ok) {
-        stand(cq, true);
-        if (!ok || cq.end) break;
-        issue_dp();
-        if (!ok) break;
-        const uint32_t st = cq.at % S::kK;
-        if (cq.j == 0 && !(ok = wait(&sm.dq_empty, cq.n & 1))) break;  // of the item before
-        if (!(ok = wait(&sm.ds_full[cq.at & 1], (cq.at >> 1) & 1))) break;
-        tc_fence_after();
-        mma_tnh(384, (cq.at & 1) * 256, k_mn + st * (S::kTile >> 4), idesc_q, cq.j > 0);
-        mma_commit_w(&sm.k_empty[st]);
-        if (cq.j == cq.blocks - 1) mma_commit_w(&sm.dq_full);
-        ++cq.j;
-        ++cq.at;
-        issue_s();
-      }
+        if (f0) {
+          if (!(ok = waitq(&sm.ds_full[buf], (dsf >> buf) & 1))) break;
+          dsf ^= 1u << buf;
+          tc_fence_after();
+        }
+        if (f1) {
+          if (f1 & kFirst) {
+            pq = pq + 1 == S::kQ ? 0 : pq + 1;
+            if (pq == 0) pf ^= 1;
+            if (!(ok = waitq(&sm.do_full[pq], pf))) break;
+            tc_fence_after();
+          }
+          mma_nt<D>(128, do_lo + pq * kStep, v_lo + pv * kStep, idesc_s);
+          mma_commit_w(&sm.dp_full[pv]);
+          if (f1 & kLast) mma_commit_w(&sm.do_empty[pq]);
+          pv = (pv + 1) % S::kV;
+        }
+        if (f0) {
+          if (f0 & kFirst) {  // dQ of the item before has been read
+            dqf ^= 1;
+            if (!(ok = waitq(&sm.dq_empty, dqf))) break;
+            tc_fence_after();
+          }
+          mma_tnh(384, buf * 256, k_mn + qk * kStep, idesc_q, (f0 & kFirst) ^ kFirst);
+          mma_commit_w(&sm.k_empty[qk]);
+          if (f0 & kLast) mma_commit_w(&sm.dq_full);
+          qk = qk + 1 == S::kK ? 0 : qk + 1;
+        }
+        if (f2) {
+          if (!(ok = waitq(&sm.ready[sk], sf))) break;
+          tc_fence_after();
+          mma_nt<D>(buf * 256, q_lo + sq * kStep, k_lo + sk * kStep, idesc_s);
+          mma_commit_w(&sm.s_full[buf]);
+          if (f2 & kLast) mma_commit_w(&sm.q_empty[sq]);
+          if (++sk == S::kK) {
+            sk = 0;
+            sf ^= 1;
+          }
+        }
+        buf ^= 1;
+        f0 = f1;
+        f1 = f2;
+      } while (f0 | f1);
       mma_commit_w(&sm.mma_done);
       drain(&sm.mma_done, 0);
     }
@@ -364,7 +371,7 @@ __global__ void __launch_bounds__(kDqThreads, 1)
     uint32_t n = 0, at = 0;
     bool ok = true;
     DqItem it;
-    while (ok && next_item(n, it, ok, false)) {
+    while (ok && next_item(n, it, ok)) {
       const bool there = rt < it.ntok;
       const int64_t rv = (int64_t)(it.hk * p.G + rg) * p.nq + it.tok0 + rt;
       const float l = there ? p.lse[rv] : INFINITY, dsum = there ? p.dsum[rv] : 0.f;
@@ -386,7 +393,7 @@ __global__ void __launch_bounds__(kDqThreads, 1)
           r[x] = __float_as_uint(ex2_approx(a));
           r[x + 1] = __float_as_uint(ex2_approx(b));
         }
-        if (!(ok = wait(&sm.dp_full, at & 1))) break;
+        if (!(ok = wait(&sm.dp_full[at % S::kV], (at / S::kV) & 1))) break;
         tc_fence_after();
         uint32_t ds[32];
 #pragma unroll
@@ -394,11 +401,6 @@ __global__ void __launch_bounds__(kDqThreads, 1)
           uint32_t v[32];
           tmem_ld32(lane_base + 128 + half * 64 + h * 32, v);
           tmem_wait_ld();
-          if (h == 1) {
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(&sm.dp_empty);
-          }
 #pragma unroll
           for (int x = 0; x < 32; x += 2) {
             float a, b;
@@ -463,7 +465,7 @@ __global__ void __launch_bounds__(kDqThreads, 1)
     uint32_t n = 0;
     bool ok = true;
     DqItem it;
-    while (ok && next_item(n, it, ok, false)) {
+    while (ok && next_item(n, it, ok)) {
       __nv_bfloat16* out[4];  // the rows of this lane's quad, its 16-byte unit
 #pragma unroll
       for (int i = 0; i < 4; ++i) out[i] = row_of(it.tok0, it.ntok, it.hk, quarter * 32 + (lane & ~3u) + i);
@@ -523,7 +525,7 @@ struct KvSmem {
   alignas(1024) uint8_t dout[kDo][kTile];
   alignas(16) float lse2[2][kT];
   alignas(16) float dsum[2][kT];
-  uint64_t kv_full, kv_empty, q_full[kQ], q_ready[kQ], q_empty[kQ], do_full[kDo], do_ready[kDo], do_empty[kDo];
+  uint64_t kv_full, kv_empty, q_full[kQ], q_empty[kQ], do_full[kDo], do_empty[kDo], ready[4];
   uint64_t rows_full[2], s_full, dp_full, p_full, ds_full, acc_full, acc_empty, mma_done;
   uint32_t tmem_base;
   int abort_flag;
@@ -576,18 +578,17 @@ __global__ void __launch_bounds__(kKvThreads, 1)
     for (uint64_t* x : one) mbar_init(x, 1);
     for (int s = 0; s < S::kQ; ++s) {
       mbar_init(&sm.q_full[s], 1);
-      mbar_init(&sm.q_ready[s], 1);
       mbar_init(&sm.q_empty[s], 1);
     }
     for (int s = 0; s < S::kDo; ++s) {
       mbar_init(&sm.do_full[s], 1);
-      mbar_init(&sm.do_ready[s], 1);
       mbar_init(&sm.do_empty[s], 1);
     }
     uint64_t* eight[] = {&sm.p_full, &sm.ds_full, &sm.acc_empty};
     for (uint64_t* x : eight) mbar_init(x, 8);
-    mbar_init(&sm.rows_full[0], 256);
-    mbar_init(&sm.rows_full[1], 256);
+    mbar_init(&sm.rows_full[0], 8);
+    mbar_init(&sm.rows_full[1], 8);
+    for (int s = 0; s < 4; ++s) mbar_init(&sm.ready[s], 2);  // of the warps of Q and dO
     sm.abort_flag = 0;
     fence_barrier_init();
   }
@@ -650,51 +651,51 @@ __global__ void __launch_bounds__(kKvThreads, 1)
       const uint32_t k_lo = desc_lo(smem_u32(sm.k), 16), v_lo = desc_lo(smem_u32(sm.v), 16),
                      q_lo = desc_lo(smem_u32(sm.q[0]), 16), do_lo = desc_lo(smem_u32(sm.dout[0]), 16),
                      q_mn = desc_lo(smem_u32(sm.q[0]), kChunkB), do_mn = desc_lo(smem_u32(sm.dout[0]), kChunkB);
-      uint32_t nkv = 0, nt = 0;
-      bool ok = true;
-      auto issue_s = [&](uint32_t x) {  // S^T of tile number x
-        const uint32_t st = x % S::kQ;
-        if (!(ok = wait(&sm.q_ready[st], (x / S::kQ) & 1))) return;
-        tc_fence_after();
-        mma_nt<D>(0, k_lo, q_lo + st * (S::kTile >> 4), idesc_s);
-        mma_commit_w(&sm.s_full);
+      constexpr uint32_t kStep = S::kTile >> 4;
+      auto waitq = [&](uint64_t* bar, uint32_t parity) -> bool {
+        return quick_wait(bar, parity, abort_flag, p.status, p.timeout_ns);
       };
-      auto issue_dp = [&](uint32_t x) {  // dP^T of tile number x
-        const uint32_t st = x % S::kDo;
-        if (!(ok = wait(&sm.do_ready[st], (x / S::kDo) & 1))) return;
-        tc_fence_after();
-        mma_nt<D>(128, v_lo, do_lo + st * (S::kTile >> 4), idesc_s);
+      uint32_t nkv = 0, nt = 0;                   // key blocks, tiles
+      uint32_t qs = 0, ds = 0, qn = 0, dn = 0;    // stages: of dK, dV; of S, dP
+      bool ok = true;
+      auto issue_s = [&]() {
+        mma_nt<D>(0, k_lo, q_lo + qn * kStep, idesc_s);
+        mma_commit_w(&sm.s_full);
+        qn = qn + 1 == S::kQ ? 0 : qn + 1;
+      };
+      auto issue_dp = [&]() {
+        mma_nt<D>(128, v_lo, do_lo + dn * kStep, idesc_s);
         mma_commit_w(&sm.dp_full);
+        dn = dn + 1 == S::kDo ? 0 : dn + 1;
       };
       for (int64_t u = blockIdx.x; u < prm.n_items && ok; u += gridDim.x) {
         Work w;
         if (!warp_uniform(decode(prm, u, w))) continue;
-        const int tiles = (int)warp_uniform((uint32_t)w.tiles), blocks = (int)warp_uniform((uint32_t)w.blocks);
-        for (int j = 0; j < blocks && ok; ++j) {
-          if (!(ok = wait(&sm.kv_full, nkv & 1))) break;
-          issue_s(nt);
-          if (ok) issue_dp(nt);
-          if (!ok) break;
+        const uint32_t tiles = warp_uniform((uint32_t)w.tiles);
+        uint32_t blocks = warp_uniform((uint32_t)w.blocks);
+        for (; blocks > 0; --blocks) {
+          if (!(ok = waitq(&sm.kv_full, nkv & 1))) break;
+          if (!(ok = waitq(&sm.ready[nt & 3], (nt >> 2) & 1))) break;
+          tc_fence_after();
+          issue_s();
+          issue_dp();
+          if (!(ok = waitq(&sm.acc_empty, (nkv & 1) ^ 1))) break;
 #pragma unroll 1
-          for (int t = 0; t < tiles; ++t, ++nt) {
-            const uint32_t qs = nt % S::kQ, ds = nt % S::kDo;
-            if (t == 0 && !(ok = wait(&sm.acc_empty, (nkv & 1) ^ 1))) break;
-            if (!(ok = wait(&sm.p_full, nt & 1))) break;
+          for (uint32_t t = 0; t < tiles; ++t, ++nt) {
+            const bool more = t + 1 < tiles;
+            if (more && !(ok = waitq(&sm.ready[(nt + 1) & 3], ((nt + 1) >> 2) & 1))) break;
+            if (!(ok = waitq(&sm.p_full, nt & 1))) break;
             tc_fence_after();
-            mma_tnh(256, 0, do_mn + ds * (S::kTile >> 4), idesc_acc, t > 0);
+            mma_tnh(256, 0, do_mn + ds * kStep, idesc_acc, t);
             mma_commit_w(&sm.do_empty[ds]);
-            if (t + 1 < tiles) {
-              issue_s(nt + 1);
-              if (!ok) break;
-            }
-            if (!(ok = wait(&sm.ds_full, nt & 1))) break;
+            ds = ds + 1 == S::kDo ? 0 : ds + 1;
+            if (more) issue_s();
+            if (!(ok = waitq(&sm.ds_full, nt & 1))) break;
             tc_fence_after();
-            mma_tnh(384, 128, q_mn + qs * (S::kTile >> 4), idesc_acc, t > 0);
+            mma_tnh(384, 128, q_mn + qs * kStep, idesc_acc, t);
             mma_commit_w(&sm.q_empty[qs]);
-            if (t + 1 < tiles) {
-              issue_dp(nt + 1);
-              if (!ok) break;
-            }
+            qs = qs + 1 == S::kQ ? 0 : qs + 1;
+            if (more) issue_dp();
           }
           if (!ok) break;
           mma_commit_w(&sm.kv_empty);
@@ -757,7 +758,7 @@ __global__ void __launch_bounds__(kKvThreads, 1)
               fence_proxy_async_smem();
               __syncwarp();
             }
-            if (lane == 0) mbar_arrive(is_q ? &sm.q_ready[st] : &sm.do_ready[st]);
+            if (lane == 0) mbar_arrive(&sm.ready[nt & 3]);
             if (!is_q) {
               load_ahead();
               if (!ok) break;
@@ -798,7 +799,8 @@ __global__ void __launch_bounds__(kKvThreads, 1)
           const uint32_t par = nt & 1;
           if (tid < kT) sm.lse2[par][col] = rv;
           else sm.dsum[par][col] = rv;
-          mbar_arrive(&sm.rows_full[par]);
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&sm.rows_full[par]);
           if (t + 1 < w.tiles) rv = row_value(t + 1);
           if (!(ok = wait(&sm.rows_full[par], (nt >> 1) & 1))) break;
           const float* ls = sm.lse2[par] + half * HC;

@@ -79,6 +79,24 @@ UT_DEV void mma_tnh(uint32_t d, uint32_t a, uint32_t b_lo, uint32_t idesc, uint3
                : "memory");
 }
 
+// warp_wait for warps whose code has to stay short: one try, and the loop that
+// spins (bounded as always) out of line.
+static __device__ __noinline__ bool spin_wait(uint64_t* bar, uint32_t parity, volatile int* abort_flag, int32_t* status,
+                                       uint64_t timeout_ns) {
+  return warp_wait(bar, parity, abort_flag, status, timeout_ns);
+}
+UT_DEV bool quick_wait(uint64_t* bar, uint32_t parity, volatile int* abort_flag, int32_t* status, uint64_t timeout_ns) {
+  uint32_t r;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.acquire.cta.shared::cta.b64 p, [%1], %2;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(r)
+      : "r"(smem_u32(bar)), "r"(parity)
+      : "memory");
+  if (__builtin_expect(__all_sync(0xffffffffu, r), 1)) return true;
+  return warp_uniform(spin_wait(bar, parity, abort_flag, status, timeout_ns));
+}
+
 // This lane's four keys of a block (lane + 32 g): bit g set where the key
 // exists and is not masked.
 UT_DEV uint32_t lane_keys(const uint8_t* mask, int64_t key, int left, uint32_t lane) {
