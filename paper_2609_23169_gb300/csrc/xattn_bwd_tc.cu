@@ -201,27 +201,33 @@ __global__ void __launch_bounds__(kDqThreads, 1)
       const uint32_t bytes = (uint32_t)prm.tpt * p.G * 128 * S::kC;
       uint32_t n = 0, at = 0, nv = 0, ndo = 0;  // items, K, V and dO tiles asked for
       bool ok = true;
-      for (int64_t u = blockIdx.x; ok; u += gridDim.x) {
+      int64_t u = blockIdx.x;
+      auto publish = [&](uint32_t n) -> DqItem {  // decodes the next item
         DqItem it{};
-        if (u < prm.n_items) {
+        for (; u < prm.n_items && it.blocks == 0; u += gridDim.x) {
           const Segment g = segment_of_slot(p.cu_q, p.B, p.nq, prm.tpt, u / p.Hk);
           const int64_t t0 = g.tile * prm.tpt;
           if (t0 >= g.n) continue;  // an idle slot
           int64_t k0, kn;
           segment_rows(p.cu_k, g.s, p.nk, k0, kn);
-          if (kn == 0) continue;  // no keys: the output warps have it
+          it.blocks = (int)((kn + kT - 1) / kT);  // 0: no keys, the output warps have it
           it.hk = (int)(u % p.Hk);
-          it.blocks = (int)((kn + kT - 1) / kT);
           it.tok0 = (int)(g.row + t0);
           it.ntok = (int)min((int64_t)prm.tpt, g.n - t0);
           it.key0 = (int)k0;
           it.keys = (int)kn;
         }
         const uint32_t s = n % kDqSlots;
-        if (!(ok = wait1(&sm.item_empty[s], ((n / kDqSlots) & 1) ^ 1))) break;
+        if (!(ok = wait1(&sm.item_empty[s], ((n / kDqSlots) & 1) ^ 1))) return it;
         sm.item[s] = it;
         mbar_arrive(&sm.item_full[s]);
-        if (it.blocks == 0) break;
+        return it;
+      };
+      DqItem next = publish(0);
+      while (ok && next.blocks > 0) {
+        const DqItem it = next;
+        next = publish(n + 1);
+        if (!ok) break;
         const uint32_t qs = n % S::kQ, qf = (n / S::kQ) & 1;
         if (!(ok = wait1(&sm.q_empty[qs], qf ^ 1))) break;
         mbar_expect_tx(&sm.q_full[qs], bytes);
@@ -370,13 +376,27 @@ __global__ void __launch_bounds__(kDqThreads, 1)
     const uint64_t c2 = pack_f32x2(prm.scale_log2, prm.scale_log2);
     uint32_t n = 0, at = 0;
     bool ok = true;
-    DqItem it;
-    while (ok && next_item(n, it, ok)) {
-      const bool there = rt < it.ntok;
-      const int64_t rv = (int64_t)(it.hk * p.G + rg) * p.nq + it.tok0 + rt;
-      const float l = there ? p.lse[rv] : INFINITY, dsum = there ? p.dsum[rv] : 0.f;
+    DqItem it, nx;
+    // LSE and D of this row, loaded an item ahead; +inf and 0 where there is none
+    auto row_load = [&](const DqItem& x, float& l, float& d) {
+      l = INFINITY;
+      d = 0.f;
+      if (x.blocks > 0 && rt < x.ntok) {
+        const int64_t rv = (int64_t)(x.hk * p.G + rg) * p.nq + x.tok0 + rt;
+        l = p.lse[rv];
+        d = p.dsum[rv];
+      }
+    };
+    float nl, nd;
+    bool more = next_item(n, nx, ok);
+    if (more) row_load(nx, nl, nd);
+    while (ok && more) {
+      it = nx;
       // a row without keys has all its columns masked; one that does not exist P = 0
-      const uint64_t l2 = pack_f32x2(-l * kLog2e, -l * kLog2e), d2 = pack_f32x2(-dsum, -dsum);
+      const uint64_t l2 = pack_f32x2(-nl * kLog2e, -nl * kLog2e), d2 = pack_f32x2(-nd, -nd);
+      more = next_item(n, nx, ok);
+      if (!ok) break;
+      row_load(nx, nl, nd);
       uint32_t keys = lane_keys(p.mask, it.key0, it.keys, lane);
       for (int j = 0; j < it.blocks; ++j, ++at) {
         const uint32_t now = keys;
@@ -782,26 +802,28 @@ __global__ void __launch_bounds__(kKvThreads, 1)
     for (int64_t u = blockIdx.x; u < prm.n_items && ok; u += gridDim.x) {
       Work w;
       if (!decode(prm, u, w)) continue;
-      // this thread's query column: -LSE (threads 0-127) or -D (128-255), a tile ahead
+      // this thread's query column: LSE (threads 0-127) or D (128-255), loaded a
+      // tile ahead and left as it is until then: arithmetic on it here would
+      // wait for the load (1,600 of 3,000 cycles a tile)
       const float* vec = (tid < kT ? p.lse : p.dsum) + (int64_t)(w.hk * p.G + rg) * p.nq + w.tok0 + rt;
-      auto row_value = [&](int t) -> float {
-        const bool there = rt < min(prm.tpt, w.ntok - t * prm.tpt);
-        if (tid >= kT) return there ? -vec[t * prm.tpt] : 0.f;
-        const float l = there ? vec[t * prm.tpt] : -INFINITY;
-        return l == -INFINITY ? -INFINITY : -l * kLog2e;  // no such row, or a row without keys: P = 0
+      auto row_load = [&](int t) -> float {
+        float l = -INFINITY;
+        if (rt < min(prm.tpt, w.ntok - t * prm.tpt)) l = vec[t * prm.tpt];
+        return l;
       };
       for (int j = 0; j < w.blocks && ok; ++j, ++ng) {
         const int key = j * kT + (int)krow;
         // P and dS of a masked key are zero: as a mask of the packed pairs
         const uint32_t on = key < w.keys && (!p.mask || p.mask[w.key0 + key]) ? 0xffffffffu : 0u;
-        float rv = row_value(0);
+        float rv = row_load(0);
         for (int t = 0; t < w.tiles; ++t, ++nt) {
           const uint32_t par = nt & 1;
-          if (tid < kT) sm.lse2[par][col] = rv;
-          else sm.dsum[par][col] = rv;
+          // -inf: no such row, or a row without keys (P = 0)
+          if (tid < kT) sm.lse2[par][col] = rv == -INFINITY ? rv : -rv * kLog2e;
+          else sm.dsum[par][col] = rv == -INFINITY ? 0.f : -rv;
           __syncwarp();
           if (lane == 0) mbar_arrive(&sm.rows_full[par]);
-          if (t + 1 < w.tiles) rv = row_value(t + 1);
+          if (t + 1 < w.tiles) rv = row_load(t + 1);
           if (!(ok = wait(&sm.rows_full[par], (nt >> 1) & 1))) break;
           const float* ls = sm.lse2[par] + half * HC;
           const float* dv = sm.dsum[par] + half * HC;
