@@ -50,6 +50,7 @@ struct BwdParams {
   uint32_t inv_g;   // ceil(2^16 / G)
   int tpt;          // tokens of a tile
   int R;            // tiles of a run
+  int ks;           // items of a run: item c has its key blocks c, c + ks, ...
   int64_t n_items;  // of the launch
   float scale_log2;
   int64_t kslots;   // key blocks of all segments (with idle ones): nk / 128 + n_seg
@@ -551,8 +552,8 @@ struct KvSmem {
   int abort_flag;
 };
 
-struct Work {  // one item: a run of query tiles and a kv head
-  int hk, part, tiles, blocks;
+struct Work {  // one item: a run of query tiles, a kv head, every ks-th key block
+  int hk, part, tiles, block0, blocks;
   int64_t tok0, key0;
   int ntok, keys;  // tokens of the run, keys of the segment
   int64_t kslot;   // first key block's place among all segments'
@@ -561,8 +562,10 @@ struct Work {  // one item: a run of query tiles and a kv head
 // Item u; false where its slot is idle.
 UT_DEV bool decode(const BwdParams& b, int64_t u, Work& w) {
   const XattnParams& p = b.x;
-  w.hk = (int)(u % p.Hk);
-  const Segment g = segment_of_slot(p.cu_q, p.B, p.nq, b.R * b.tpt, u / p.Hk);
+  const int64_t v = u / b.ks;
+  w.block0 = (int)(u - v * b.ks);
+  w.hk = (int)(v % p.Hk);
+  const Segment g = segment_of_slot(p.cu_q, p.B, p.nq, b.R * b.tpt, v / p.Hk);
   const int64_t t0 = g.tile * b.R * b.tpt;
   if (t0 >= g.n) return false;
   int64_t k0, kn;
@@ -574,8 +577,8 @@ UT_DEV bool decode(const BwdParams& b, int64_t u, Work& w) {
   w.key0 = k0;
   w.kslot = k0 / kT + g.s;
   w.keys = (int)kn;
-  w.blocks = (int)((kn + kT - 1) / kT);
-  return true;
+  w.blocks = ((int)((kn + kT - 1) / kT) - w.block0 + b.ks - 1) / b.ks;
+  return w.blocks > 0;
 }
 
 template <int D>
@@ -644,7 +647,8 @@ __global__ void __launch_bounds__(kKvThreads, 1)
         for (int64_t u = blockIdx.x; u < prm.n_items && ok; u += gridDim.x) {
           Work w;
           if (!decode(prm, u, w)) continue;
-          for (int j = 0; j < w.blocks && ok; ++j) {
+          for (int b = 0; b < w.blocks && ok; ++b) {
+            const int j = w.block0 + b * prm.ks;
             if (!(ok = wait1(&sm.kv_empty, (nkv & 1) ^ 1))) break;
             mbar_expect_tx(&sm.kv_full, 2 * S::kTile);
             for (int c = 0; c < S::kC; ++c) {
@@ -738,7 +742,7 @@ __global__ void __launch_bounds__(kKvThreads, 1)
       bool have2 = false;
       auto load_ahead = [&]() {  // asks for the next dO tile if its stage is free; whole warp
         while (!have2 && u2 < prm.n_items) {
-          have2 = decode(prm, u2, w2) && w2.blocks > 0;
+          have2 = decode(prm, u2, w2);
           if (!have2) u2 += gridDim.x;
           j2 = t2 = 0;
         }
@@ -811,7 +815,8 @@ __global__ void __launch_bounds__(kKvThreads, 1)
         if (rt < min(prm.tpt, w.ntok - t * prm.tpt)) l = vec[t * prm.tpt];
         return l;
       };
-      for (int j = 0; j < w.blocks && ok; ++j, ++ng) {
+      for (int b = 0; b < w.blocks && ok; ++b, ++ng) {
+        const int j = w.block0 + b * prm.ks;
         const int key = j * kT + (int)krow;
         // P and dS of a masked key are zero: as a mask of the packed pairs
         const uint32_t on = key < w.keys && (!p.mask || p.mask[w.key0 + key]) ? 0xffffffffu : 0u;
@@ -974,29 +979,32 @@ cudaError_t launch(F kern, int threads, size_t smem, int regs, const BwdParams& 
   return cudaGetLastError();
 }
 
-// Tiles of a run: the smallest number of whole waves of CTAs (up to four)
-// that keeps them busy to within 8% of the best, so that the partial sums stay
-// few; more tiles where the partial sums would pass 1 GB.
+// Items of a run along the keys: the blocks of a segment of mean length, so
+// that CTAs side by side go over the same Q and dO tiles together and read
+// them from L2.  (One CTA over all four blocks of 23,959 x 512 x 24 x 128: the
+// runs of all CTAs pass L2, Q and dO came from DRAM four times, 237 us.)
+int key_split(const XattnParams& p) {
+  const int64_t mean = (p.nk / p.B + kT - 1) / kT;
+  return (int)(mean < 1 ? 1 : (mean > 256 ? 256 : mean));
+}
+
+// Tiles of a run: the number of runs with the least modelled time, in cycles:
+// whole waves of items of R tiles (2,200 each, 5,000 an item), and each run's
+// partial sums written and read (3,400 bytes a cycle).  At most 1 GB of them.
 int tiles_per_item(const XattnParams& p) {
-  const int64_t tpt = kT / p.G, tiles = (p.nq + tpt - 1) / tpt;
-  int64_t best = 1;
-  double best_use = 0.0;
-  for (int waves = 1; waves <= 4; ++waves) {
-    const int64_t runs = (int64_t)waves * p.sms / p.Hk;  // items along the rows
-    if (runs < 1) continue;
-    const int64_t R = (tiles + runs - 1) / runs, items = (tiles + R - 1) / R * p.Hk;
-    const int64_t w = (items + p.sms - 1) / p.sms;
-    const double use = (double)(tiles * p.Hk) / ((double)(w * p.sms) * R);
-    if (use > best_use + 0.08) {
-      best_use = use;
+  const int64_t tpt = kT / p.G, tiles = (p.nq + tpt - 1) / tpt, across = (int64_t)p.Hk * key_split(p);
+  const int64_t part = 2 * segment_slots(p.nk, p.B, kT) * kT * p.Hk * p.d * (int64_t)sizeof(float);
+  int64_t best = tiles;
+  double least = 0;
+  for (int64_t runs = 1; runs <= tiles && runs <= 128; ++runs) {
+    const int64_t R = (tiles + runs - 1) / runs, waves = (runs * across + p.sms - 1) / p.sms;
+    if (runs > 1 && runs * part > ((int64_t)1 << 30)) break;
+    const double t = (double)waves * (R * 2200.0 + 5000.0) + (double)runs * (2 * part) / 3400.0;
+    if (runs == 1 || t < least) {
+      least = t;
       best = R;
     }
   }
-  if (best_use == 0.0) best = tiles;  // more kv heads than four waves
-  const int64_t part = 2 * segment_slots(p.nk, p.B, kT) * kT * p.Hk * p.d * (int64_t)sizeof(float);
-  const int64_t most = ((int64_t)1 << 30) / (part > 0 ? part : 1);
-  const int64_t least = most > 0 ? (tiles + most - 1) / most : tiles;
-  if (best < least) best = least;
   return (int)(best < 1 ? 1 : best);
 }
 
@@ -1018,6 +1026,7 @@ cudaError_t launch_xattn_bwd_tc(const XattnParams& p, void* ws, cudaStream_t s) 
   prm.inv_g = (65536u + p.G - 1) / p.G;
   prm.tpt = kT / p.G;
   prm.R = tiles_per_item(p);
+  prm.ks = key_split(p);
   prm.kslots = segment_slots(p.nk, p.B, kT);
   prm.x.part_dk = static_cast<float*>(ws);
   prm.x.part_dv = reinterpret_cast<float*>(static_cast<char*>(ws) + part_bytes(p, prm.R));
@@ -1039,7 +1048,7 @@ cudaError_t launch_xattn_bwd_tc(const XattnParams& p, void* ws, cudaStream_t s) 
                   : launch(xattn_dq_kernel<128>, kDqThreads, sizeof(DqSmem<128>), kDqLaunch, prm, tm, s);
     if (e != cudaSuccess) return e;
     if (p.nk > 0) {
-      prm.n_items = segment_slots(p.nq, p.B, prm.R * prm.tpt) * p.Hk;
+      prm.n_items = segment_slots(p.nq, p.B, prm.R * prm.tpt) * p.Hk * prm.ks;
       e = p.d == 64 ? launch(xattn_dkdv_kernel<64>, kKvThreads, sizeof(KvSmem<64>), kKvLaunch, prm, tm, s)
                     : launch(xattn_dkdv_kernel<128>, kKvThreads, sizeof(KvSmem<128>), kKvLaunch, prm, tm, s);
       if (e != cudaSuccess) return e;
