@@ -532,7 +532,7 @@ __global__ void __launch_bounds__(kDqThreads, 1)
 //   warp 0   TMA: K, V and the Q ring      warp 2   zeroes Q rows that are not
 //   warp 3   TMA: the dO ring, and its rows          the item's
 constexpr int kKvThreads = 384;
-constexpr int kKvLaunch = 168, kKvCtl = 88, kKvEw = 208;
+constexpr int kKvLaunch = 168, kKvCtl = 104, kKvEw = 200;
 static_assert(kKvCtl + 2 * kKvEw <= 3 * kKvLaunch, "setmaxnreg split must fit the launch");
 
 template <int D>
@@ -544,10 +544,10 @@ struct KvSmem {
   alignas(1024) uint8_t v[kTile];
   alignas(1024) uint8_t q[kQ][kTile];
   alignas(1024) uint8_t dout[kDo][kTile];
-  alignas(16) float lse2[2][kT];
+  alignas(16) float lse2[2][kT];  // -LSE log2(e) and -D of the rows of a tile
   alignas(16) float dsum[2][kT];
-  uint64_t kv_full, kv_empty, q_full[kQ], q_empty[kQ], do_full[kDo], do_empty[kDo], ready[4];
-  uint64_t rows_full[2], s_full, dp_full, p_full, ds_full, acc_full, acc_empty, mma_done;
+  uint64_t kv_full, kv_empty, q_full[kQ], q_empty[kQ], do_full[kDo], do_empty[kDo], q_ready[4], do_ready[4];
+  uint64_t s_full, dp_full, p_full, ds_full, acc_full, acc_empty, mma_done;
   uint32_t tmem_base;
   int abort_flag;
 };
@@ -609,9 +609,10 @@ __global__ void __launch_bounds__(kKvThreads, 1)
     }
     uint64_t* eight[] = {&sm.p_full, &sm.ds_full, &sm.acc_empty};
     for (uint64_t* x : eight) mbar_init(x, 8);
-    mbar_init(&sm.rows_full[0], 8);
-    mbar_init(&sm.rows_full[1], 8);
-    for (int s = 0; s < 4; ++s) mbar_init(&sm.ready[s], 2);  // of the warps of Q and dO
+    for (int s = 0; s < 4; ++s) {
+      mbar_init(&sm.q_ready[s], 1);
+      mbar_init(&sm.do_ready[s], 1);
+    }
     sm.abort_flag = 0;
     fence_barrier_init();
   }
@@ -699,15 +700,16 @@ __global__ void __launch_bounds__(kKvThreads, 1)
         uint32_t blocks = warp_uniform((uint32_t)w.blocks);
         for (; blocks > 0; --blocks) {
           if (!(ok = waitq(&sm.kv_full, nkv & 1))) break;
-          if (!(ok = waitq(&sm.ready[nt & 3], (nt >> 2) & 1))) break;
+          if (!(ok = waitq(&sm.q_ready[nt & 3], (nt >> 2) & 1))) break;
           tc_fence_after();
           issue_s();
+          if (!(ok = waitq(&sm.do_ready[nt & 3], (nt >> 2) & 1))) break;
           issue_dp();
           if (!(ok = waitq(&sm.acc_empty, (nkv & 1) ^ 1))) break;
 #pragma unroll 1
           for (uint32_t t = 0; t < tiles; ++t, ++nt) {
             const bool more = t + 1 < tiles;
-            if (more && !(ok = waitq(&sm.ready[(nt + 1) & 3], ((nt + 1) >> 2) & 1))) break;
+            if (more && !(ok = waitq(&sm.q_ready[(nt + 1) & 3], ((nt + 1) >> 2) & 1))) break;
             if (!(ok = waitq(&sm.p_full, nt & 1))) break;
             tc_fence_after();
             mma_tnh(256, 0, do_mn + ds * kStep, idesc_acc, t);
@@ -719,7 +721,10 @@ __global__ void __launch_bounds__(kKvThreads, 1)
             mma_tnh(384, 128, q_mn + qs * kStep, idesc_acc, t);
             mma_commit_w(&sm.q_empty[qs]);
             qs = qs + 1 == S::kQ ? 0 : qs + 1;
-            if (more) issue_dp();
+            if (more) {
+              if (!(ok = waitq(&sm.do_ready[(nt + 1) & 3], ((nt + 1) >> 2) & 1))) break;
+              issue_dp();
+            }
           }
           if (!ok) break;
           mma_commit_w(&sm.kv_empty);
@@ -730,7 +735,8 @@ __global__ void __launch_bounds__(kKvThreads, 1)
       mma_commit_w(&sm.mma_done);
       drain(&sm.mma_done, 0);
     } else {
-      // ------- rows that must read as zero (warp 2: Q, warp 3: dO); dO loads
+      // ------- rows that must read as zero (warp 2: Q, warp 3: dO); dO loads;
+      // warp 2 also brings LSE and D of the rows, four a lane, a tile ahead
       const bool is_q = warp == 2;
       const uint32_t bytes = (uint32_t)prm.tpt * p.G * 128 * S::kC;
       const uint64_t keep = policy_evict_last();
@@ -772,6 +778,21 @@ __global__ void __launch_bounds__(kKvThreads, 1)
       for (int64_t u = blockIdx.x; u < prm.n_items && ok; u += gridDim.x) {
         Work w;
         if (!decode(prm, u, w)) continue;
+        float rl[4], rd[4];  // as loaded: arithmetic on them here would wait for the loads
+        auto rows_load = [&](int t) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const int col = (int)lane + 32 * i, rt = (int)(((uint32_t)col * prm.inv_g) >> 16), rg = col - rt * p.G;
+            rl[i] = -INFINITY;
+            rd[i] = 0.f;
+            if (rt < min(prm.tpt, w.ntok - t * prm.tpt)) {
+              const int64_t rv = (int64_t)(w.hk * p.G + rg) * p.nq + w.tok0 + t * prm.tpt + rt;
+              rl[i] = p.lse[rv];
+              rd[i] = p.dsum[rv];
+            }
+          }
+        };
+        if (is_q) rows_load(0);
         for (int j = 0; j < w.blocks && ok; ++j)
           for (int t = 0; t < w.tiles; ++t, ++nt) {
             const int rows = min(prm.tpt, w.ntok - t * prm.tpt) * p.G;
@@ -782,8 +803,22 @@ __global__ void __launch_bounds__(kKvThreads, 1)
               fence_proxy_async_smem();
               __syncwarp();
             }
-            if (lane == 0) mbar_arrive(&sm.ready[nt & 3]);
-            if (!is_q) {
+            if (is_q) {
+              // once the rows of two tiles back have been read; -inf: no such row,
+              // or a row without keys (P = 0)
+              if (nt >= 2 && !(ok = wait(&sm.q_empty[(nt - 2) % S::kQ], ((nt - 2) / S::kQ) & 1))) break;
+#pragma unroll
+              for (int i = 0; i < 4; ++i) {
+                sm.lse2[nt & 1][lane + 32 * i] = rl[i] == -INFINITY ? rl[i] : -rl[i] * kLog2e;
+                sm.dsum[nt & 1][lane + 32 * i] = -rd[i];
+              }
+              __syncwarp();
+            }
+            if (lane == 0) mbar_arrive(is_q ? &sm.q_ready[nt & 3] : &sm.do_ready[nt & 3]);
+            if (is_q) {
+              if (t + 1 < w.tiles) rows_load(t + 1);
+              else if (j + 1 < w.blocks) rows_load(0);
+            } else {
               load_ahead();
               if (!ok) break;
             }
@@ -796,46 +831,32 @@ __global__ void __launch_bounds__(kKvThreads, 1)
   } else {
     setmaxnreg_inc<kKvEw>();
     const uint32_t quarter = warp & 3, half = (warp - 4) >> 2;
-    const uint32_t krow = quarter * 32 + lane, tid = threadIdx.x - 128;
+    const uint32_t krow = quarter * 32 + lane;
     const uint32_t lane_base = (quarter * 32) << 16, ts = lane_base + half * 64;
     constexpr int HC = kT / 2, HD = D / 2;
     const uint64_t c2 = pack_f32x2(prm.scale_log2, prm.scale_log2);
-    const int col = (int)(tid & (kT - 1)), rt = (int)(((uint32_t)col * prm.inv_g) >> 16), rg = col - rt * p.G;
     uint32_t nt = 0, ng = 0;
     bool ok = true;
     for (int64_t u = blockIdx.x; u < prm.n_items && ok; u += gridDim.x) {
       Work w;
       if (!decode(prm, u, w)) continue;
-      // this thread's query column: LSE (threads 0-127) or D (128-255), loaded a
-      // tile ahead and left as it is until then: arithmetic on it here would
-      // wait for the load (1,600 of 3,000 cycles a tile)
-      const float* vec = (tid < kT ? p.lse : p.dsum) + (int64_t)(w.hk * p.G + rg) * p.nq + w.tok0 + rt;
-      auto row_load = [&](int t) -> float {
-        float l = -INFINITY;
-        if (rt < min(prm.tpt, w.ntok - t * prm.tpt)) l = vec[t * prm.tpt];
-        return l;
-      };
       for (int b = 0; b < w.blocks && ok; ++b, ++ng) {
         const int j = w.block0 + b * prm.ks;
         const int key = j * kT + (int)krow;
         // P and dS of a masked key are zero: as a mask of the packed pairs
         const uint32_t on = key < w.keys && (!p.mask || p.mask[w.key0 + key]) ? 0xffffffffu : 0u;
-        float rv = row_load(0);
         for (int t = 0; t < w.tiles; ++t, ++nt) {
           const uint32_t par = nt & 1;
-          // -inf: no such row, or a row without keys (P = 0)
-          if (tid < kT) sm.lse2[par][col] = rv == -INFINITY ? rv : -rv * kLog2e;
-          else sm.dsum[par][col] = rv == -INFINITY ? 0.f : -rv;
-          __syncwarp();
-          if (lane == 0) mbar_arrive(&sm.rows_full[par]);
-          if (t + 1 < w.tiles) rv = row_load(t + 1);
-          if (!(ok = wait(&sm.rows_full[par], (nt >> 1) & 1))) break;
           const float* ls = sm.lse2[par] + half * HC;
           const float* dv = sm.dsum[par] + half * HC;
           if (!(ok = wait(&sm.s_full, par))) break;
           tc_fence_after();
           uint32_t r[HC];
-          tmem_ld64(ts, r);
+          tmem_ld32(ts, *reinterpret_cast<uint32_t(*)[32]>(r));
+          tmem_ld32(ts + 32, *reinterpret_cast<uint32_t(*)[32]>(r + 32));
+          ok = wait(&sm.q_ready[nt & 3], (nt >> 2) & 1);  // the rows' values
+          tmem_wait_ld();
+          if (!ok) break;
           uint32_t pk[32];
 #pragma unroll
           for (int x = 0; x < HC; x += 4) {
