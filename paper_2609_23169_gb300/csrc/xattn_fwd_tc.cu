@@ -248,12 +248,15 @@ __global__ void __launch_bounds__(kThreads, 1)
       constexpr uint32_t idesc_o = idesc_bf16_f32(kM, D, false, true);
       const uint32_t q_lo = desc_lo(smem_u32(sm.q[0]), 16), k_lo = desc_lo(smem_u32(sm.kv[0]), 16),
                      v_lo = desc_lo(smem_u32(sm.kv[0]), kChunkBytes);
+      auto waitq = [&](uint64_t* bar, uint32_t parity) -> bool {
+        return quick_wait(bar, parity, abort_flag, p.status, p.timeout_ns);
+      };
       const uint32_t w = warp >> 1, ts = w * 128, to = 256 + w * 128;
       uint32_t n = 0, qat = w, kvat = 0, np = 0, no = 0, turns = 0;
       bool ok = true;
       for (;; ++n) {
         const uint32_t slot = n % kItemSlots;
-        if (!(ok = wait(&sm.item_full[slot], (n / kItemSlots) & 1))) break;
+        if (!(ok = waitq(&sm.item_full[slot], (n / kItemSlots) & 1))) break;
         const int hk = (int)warp_uniform((uint32_t)sm.item[slot].hk);
         const int blocks = (int)warp_uniform((uint32_t)sm.item[slot].blocks);
         const bool both = warp_uniform((uint32_t)sm.item[slot].ntok[1]) != 0;
@@ -264,7 +267,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (w == 1 && !both) {  // nothing for tile 1: pass the K and V tiles on
 #pragma unroll 1
           for (int x = 0; x < 2 * blocks && ok; ++x, ++kvat) {
-            ok = wait(&sm.kv_full[kvat % S::kKv], (kvat / S::kKv) & 1);
+            ok = waitq(&sm.kv_full[kvat % S::kKv], (kvat / S::kKv) & 1);
             if (ok && lane == 0) mbar_arrive(&sm.kv_empty[kvat % S::kKv]);
           }
           if (!ok) break;
@@ -272,32 +275,32 @@ __global__ void __launch_bounds__(kThreads, 1)
           continue;
         }
         const uint32_t qs = qat % S::kQ, q_a = q_lo + qs * (S::kTile >> 4);
-        if (!(ok = wait(&sm.q_full[qs], (qat / S::kQ) & 1))) break;
+        if (!(ok = waitq(&sm.q_full[qs], (qat / S::kQ) & 1))) break;
         // step j: O += P V of block j - 1, S = Q K^T of block j
 #pragma unroll 1
         for (int j = 0; j <= blocks; ++j) {
           const uint32_t ks = kvat % S::kKv, vs = (kvat - 1) % S::kKv;
-          if (j < blocks && !(ok = wait(&sm.kv_full[ks], (kvat / S::kKv) & 1))) break;
+          if (j < blocks && !(ok = waitq(&sm.kv_full[ks], (kvat / S::kKv) & 1))) break;
           if (j > 0) {
-            if (!(ok = wait(&sm.kv_full[vs], ((kvat - 1) / S::kKv) & 1))) break;
+            if (!(ok = waitq(&sm.kv_full[vs], ((kvat - 1) / S::kKv) & 1))) break;
             if (j == 1) {
-              if (!(ok = wait(&sm.o_empty[w], (no & 1) ^ 1))) break;
+              if (!(ok = waitq(&sm.o_empty[w], (no & 1) ^ 1))) break;
               ++no;
             }
-            if (!(ok = wait(&sm.p_most[w], np & 1))) break;
+            if (!(ok = waitq(&sm.p_most[w], np & 1))) break;
           }
           // an item's first S and its last P V wait for no turn: the tiles need
           // not start or end together
           const bool turn = both && j > 0 && j < blocks;
           if (turn) {
-            if (!(ok = wait(&sm.turn[w], (turns & 1) ^ (w ^ 1)))) break;
+            if (!(ok = waitq(&sm.turn[w], (turns & 1) ^ (w ^ 1)))) break;
             ++turns;
           }
           tc_fence_after();
           if (j > 0) {
             const uint32_t v_b = v_lo + vs * (S::kTile >> 4);
             mma_tn96(to, ts, v_b, idesc_o, j > 1);
-            if (!(ok = wait(&sm.p_full[w], np & 1))) break;
+            if (!(ok = waitq(&sm.p_full[w], np & 1))) break;
             ++np;
             tc_fence_after();
             mma_tn32(to, ts + 48, v_b + 768, idesc_o);
