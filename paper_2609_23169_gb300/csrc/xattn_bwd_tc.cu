@@ -74,9 +74,10 @@ UT_DEV void zero_tail(uint32_t base, int chunks, int first, uint32_t lane) {
 // [384,384+d).  With dS_i formed, the tensor core is given dP_{i+1}, dQ_i and
 // S_{i+2}, across items: the elementwise warps find their next S there and
 // take its exponentials while dP runs.
-//   warp 0      decodes the items into a ring; TMA, in the order of their use:
-//               Q, K_0, V_0, dO, K_1, V_1, ...
+//   warp 0      TMA, in the order of their use: Q, K_0, V_0, dO, K_1, V_1, ...
 //   warp 1      the products
+//   warp 2      decodes the items into a ring, 32 at once, one a lane (one after
+//               another each took 2,500 cycles, more than a block)
 //   warp 3      zeroes the masked keys of K, says when a block has all it needs
 //   warps 12-15 dQ out
 // The issuing warp's instructions are fetched anew every block (the
@@ -87,7 +88,7 @@ UT_DEV void zero_tail(uint32_t base, int chunks, int first, uint32_t lane) {
 constexpr int kDqThreads = 512;
 constexpr int kDqLaunch = 128, kDqCtl = 80, kDqEw = 152, kDqOut = 128;
 static_assert(kDqCtl + 2 * kDqEw + kDqOut <= 4 * kDqLaunch, "setmaxnreg split must fit the launch");
-constexpr int kDqSlots = 8, kDqReaders = 14;
+constexpr int kDqSlots = 8, kDqReaders = 15;
 
 struct DqItem {
   int32_t blocks;  // key blocks; 0: no more items
@@ -202,33 +203,12 @@ __global__ void __launch_bounds__(kDqThreads, 1)
       const uint32_t bytes = (uint32_t)prm.tpt * p.G * 128 * S::kC;
       uint32_t n = 0, at = 0, nv = 0, ndo = 0;  // items, K, V and dO tiles asked for
       bool ok = true;
-      int64_t u = blockIdx.x;
-      auto publish = [&](uint32_t n) -> DqItem {  // decodes the next item
-        DqItem it{};
-        for (; u < prm.n_items && it.blocks == 0; u += gridDim.x) {
-          const Segment g = segment_of_slot(p.cu_q, p.B, p.nq, prm.tpt, u / p.Hk);
-          const int64_t t0 = g.tile * prm.tpt;
-          if (t0 >= g.n) continue;  // an idle slot
-          int64_t k0, kn;
-          segment_rows(p.cu_k, g.s, p.nk, k0, kn);
-          it.blocks = (int)((kn + kT - 1) / kT);  // 0: no keys, the output warps have it
-          it.hk = (int)(u % p.Hk);
-          it.tok0 = (int)(g.row + t0);
-          it.ntok = (int)min((int64_t)prm.tpt, g.n - t0);
-          it.key0 = (int)k0;
-          it.keys = (int)kn;
-        }
-        const uint32_t s = n % kDqSlots;
-        if (!(ok = wait1(&sm.item_empty[s], ((n / kDqSlots) & 1) ^ 1))) return it;
-        sm.item[s] = it;
-        mbar_arrive(&sm.item_full[s]);
-        return it;
-      };
-      DqItem next = publish(0);
-      while (ok && next.blocks > 0) {
-        const DqItem it = next;
-        next = publish(n + 1);
-        if (!ok) break;
+      for (;;) {
+        const uint32_t slot = n % kDqSlots;
+        if (!(ok = wait1(&sm.item_full[slot], (n / kDqSlots) & 1))) break;
+        const DqItem it = sm.item[slot];
+        mbar_arrive(&sm.item_empty[slot]);
+        if (it.blocks == 0) break;
         const uint32_t qs = n % S::kQ, qf = (n / S::kQ) & 1;
         if (!(ok = wait1(&sm.q_empty[qs], qf ^ 1))) break;
         mbar_expect_tx(&sm.q_full[qs], bytes);
@@ -254,6 +234,7 @@ __global__ void __launch_bounds__(kDqThreads, 1)
             tma_load_3d(sm.dout[qs] + c * kChunkB, &tm_do, &sm.do_full[qs], c * 64, it.hk * p.G, it.tok0, keep);
           ++ndo;
         }
+        if (!ok) break;
       }
       auto landed = [&](uint64_t* bar, uint32_t stages, uint32_t sent) {
         for (uint32_t x = sent > stages ? sent - stages : 0; x < sent; ++x) drain(bar + x % stages, (x / stages) & 1);
@@ -262,6 +243,45 @@ __global__ void __launch_bounds__(kDqThreads, 1)
       landed(sm.k_full, S::kK, at);
       landed(sm.v_full, S::kV, nv);
       landed(sm.do_full, S::kQ, ndo);
+    } else if (warp == 2) {
+      // ------------------------------------------------------------- items
+      uint32_t n = 0;
+      bool ok = true, end = false;
+      for (int64_t u0 = blockIdx.x; ok && !end; u0 += (int64_t)32 * gridDim.x) {
+        const int64_t u = u0 + (int64_t)lane * gridDim.x;
+        DqItem it{};
+        if (u < prm.n_items) {
+          const Segment g = segment_of_slot(p.cu_q, p.B, p.nq, prm.tpt, u / p.Hk);
+          const int64_t t0 = g.tile * prm.tpt;
+          int64_t k0, kn;
+          segment_rows(p.cu_k, g.s, p.nk, k0, kn);
+          if (t0 < g.n)  // else an idle slot
+            it.blocks = (int)((kn + kT - 1) / kT);  // 0: no keys, the output warps have it
+          it.hk = (int)(u % p.Hk);
+          it.tok0 = (int)(g.row + t0);
+          it.ntok = (int)min((int64_t)prm.tpt, g.n - t0);
+          it.key0 = (int)k0;
+          it.keys = (int)kn;
+        }
+        end = u0 + (int64_t)32 * gridDim.x >= prm.n_items;
+        uint32_t have = __ballot_sync(0xffffffffu, it.blocks > 0);
+        for (; have | (uint32_t)end; have &= have - 1, ++n) {
+          const uint32_t s = n % kDqSlots;
+          if (!(ok = wait(&sm.item_empty[s], ((n / kDqSlots) & 1) ^ 1))) break;
+          if (have == 0) {  // no more items
+            if (lane == 0) {
+              sm.item[s].blocks = 0;
+              mbar_arrive(&sm.item_full[s]);
+            }
+            break;
+          }
+          if ((int)lane == __ffs(have) - 1) {
+            sm.item[s] = it;
+            mbar_arrive(&sm.item_full[s]);
+          }
+          __syncwarp();
+        }
+      }
     } else if (warp == 3) {
       // ------------------------ masked keys of K; Q (of a first block), K, V
       uint32_t n = 0, at = 0;

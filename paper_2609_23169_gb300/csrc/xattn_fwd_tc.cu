@@ -14,8 +14,8 @@
 // flight read neighbouring 256-byte pieces of the same rows and share K and V
 // in L2.  Roles (384 threads, registers rebalanced with setmaxnreg):
 //   warp 0      TMA: the K and V tiles, one ring (K0 V0 K1 V1 ...)
-//   warp 2      decodes the items (segment search, key range) into a ring;
-//               TMA: the query tiles, a ring of their own
+//   warp 2      decodes the items (segment search, key range) into a ring, 32
+//               at once, one a lane; TMA: the query tiles, a ring of their own
 //   warp 1      TMEM owner and MMA issuer of tile 0, warp 3 of tile 1: per
 //               block S = Q K^T, then, as P is written over S in TMEM, O += P V
 //               (of the first 96 keys while the last 32 are being written).
@@ -193,27 +193,27 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
       }
       for (uint32_t x = at > S::kKv ? at - S::kKv : 0; x < at; ++x) drain(&sm.kv_full[x % S::kKv], (x / S::kKv) & 1);
-    } else if (warp == 2 && lane == 0) {
+    } else if (warp == 2) {
       // ------------------------------------------- item decoder, Q producer
-      tma_prefetch_desc(&tm_q);
+      if (lane == 0) tma_prefetch_desc(&tm_q);
       const uint64_t pol = policy_evict_first();
       const uint32_t bytes = (uint32_t)prm.tpt * p.G * 128 * S::kChunks;
       uint32_t n = 0, at = 0;
-      bool ok = true;
-      for (int64_t u = blockIdx.x; ok; u += gridDim.x) {
+      bool ok = true, end = false;
+      for (int64_t u0 = blockIdx.x; ok && !end; u0 += (int64_t)32 * gridDim.x) {
+        const int64_t u = u0 + (int64_t)lane * gridDim.x;
         Item it{};
         it.hk = -1;
         if (u < prm.n_items) {
           const int64_t at_q = u / p.Hk;
           const Segment g = segment_of_slot(p.cu_q, p.B, p.nq, 2 * prm.tpt, at_q % prm.slots);
           const int64_t t0 = g.tile * 2 * prm.tpt;
-          if (t0 >= g.n) continue;  // an idle slot
           int64_t k0, kn;
           segment_rows(p.cu_k, g.s, p.nk, k0, kn);
           const int64_t nblk = (kn + kN - 1) / kN, per = (nblk + p.nsplit - 1) / p.nsplit;
           it.split = (int)(at_q / prm.slots);
           const int64_t b0 = min(nblk, per * it.split), b1 = min(nblk, b0 + per);
-          it.hk = (int)(u % p.Hk);
+          if (t0 < g.n) it.hk = (int)(u % p.Hk);  // else an idle slot
           it.blocks = (int)(b1 - b0);
           it.tok0 = (int)(g.row + t0);
           it.ntok[0] = (int)min((int64_t)prm.tpt, g.n - t0);
@@ -221,25 +221,41 @@ __global__ void __launch_bounds__(kThreads, 1)
           it.key0 = (int)(k0 + b0 * kN);
           it.left = (int)(kn - b0 * kN);
         }
-        const uint32_t s = n % kItemSlots, f = n / kItemSlots;
-        if (!(ok = wait1(&sm.item_empty[s], (f & 1) ^ 1))) break;
-        sm.item[s] = it;
-        mbar_arrive(&sm.item_full[s]);
-        ++n;
-        if (it.hk < 0) break;
-        if (it.blocks == 0) continue;
-        for (int w = 0; w < 2 && ok; ++w) {
-          if (it.ntok[w] == 0) continue;
-          const uint32_t st = at % S::kQ, qf = at / S::kQ;
-          if (!(ok = wait1(&sm.q_empty[st], (qf & 1) ^ 1))) break;
-          mbar_expect_tx(&sm.q_full[st], bytes);
-          for (int c = 0; c < S::kChunks; ++c)
-            tma_load_3d(sm.q[st] + c * kChunkBytes, &tm_q, &sm.q_full[st], c * 64, it.hk * p.G, it.tok0 + w * prm.tpt,
-                        pol);
-          ++at;
+        end = u0 + (int64_t)32 * gridDim.x >= prm.n_items;
+        uint32_t have = __ballot_sync(0xffffffffu, it.hk >= 0);
+        for (; have | (uint32_t)end; have &= have - 1, ++n) {
+          const uint32_t s = n % kItemSlots;
+          if (!(ok = wait(&sm.item_empty[s], ((n / kItemSlots) & 1) ^ 1))) break;
+          if (have == 0) {  // no more items
+            if (lane == 0) {
+              sm.item[s].hk = -1;
+              mbar_arrive(&sm.item_full[s]);
+            }
+            break;
+          }
+          const int who = __ffs(have) - 1;
+          if ((int)lane == who) {
+            sm.item[s] = it;
+            mbar_arrive(&sm.item_full[s]);
+          }
+          const int hk = __shfl_sync(0xffffffffu, it.hk, who), tok0 = __shfl_sync(0xffffffffu, it.tok0, who);
+          const int tiles = __shfl_sync(0xffffffffu, it.blocks == 0 ? 0 : it.ntok[1] > 0 ? 2 : 1, who);
+          for (int w = 0; w < tiles; ++w, ++at) {
+            const uint32_t st = at % S::kQ;
+            if (!(ok = wait(&sm.q_empty[st], ((at / S::kQ) & 1) ^ 1))) break;
+            if (lane == 0) {
+              mbar_expect_tx(&sm.q_full[st], bytes);
+              for (int c = 0; c < S::kChunks; ++c)
+                tma_load_3d(sm.q[st] + c * kChunkBytes, &tm_q, &sm.q_full[st], c * 64, hk * p.G, tok0 + w * prm.tpt,
+                            pol);
+            }
+            __syncwarp();
+          }
+          if (!ok) break;
         }
       }
-      for (uint32_t x = at > S::kQ ? at - S::kQ : 0; x < at; ++x) drain(&sm.q_full[x % S::kQ], (x / S::kQ) & 1);
+      if (lane == 0)
+        for (uint32_t x = at > S::kQ ? at - S::kQ : 0; x < at; ++x) drain(&sm.q_full[x % S::kQ], (x / S::kQ) & 1);
     } else if (warp == 1 || warp == 3) {
       // ---------------------------------------- MMA issuer of tile 0 / tile 1
       // Converged, and uniform to the compiler: every branch depends on votes
