@@ -961,9 +961,11 @@ __global__ void __launch_bounds__(kKvThreads, 1)
 
 // dK, dV: the sum of the partials of the key's segment, in order.  grid (key
 // slots, kv heads, dK / dV), a block one key block: read 16 bytes a thread
-// along the keys, written as rows through shared memory.
+// along the keys, all of a part in flight, written as rows through shared
+// memory.
 template <int D>
 __global__ void __launch_bounds__(256) xattn_bwd_join_kernel(const BwdParams prm) {
+  constexpr int kPer = D / 4 * kT / 256;
   __shared__ __align__(16) uint8_t rows[kT * (D * 2 + 16)];
   const XattnParams& p = prm.x;
   const Segment g = segment_of_slot(p.cu_k, p.B, p.nk, kT, blockIdx.x);
@@ -975,21 +977,30 @@ __global__ void __launch_bounds__(256) xattn_bwd_join_kernel(const BwdParams prm
   const int parts = (int)((tiles + prm.R - 1) / prm.R);
   const int64_t kslot = min(g.row / kT + g.s + g.tile, prm.kslots - 1);
   const bool is_k = blockIdx.z == 0;
-  const float* src = (is_k ? p.part_dk : p.part_dv) + (kslot * p.Hk + blockIdx.y) * (D * kT);
+  const float* src = (is_k ? p.part_dk : p.part_dv) + (kslot * p.Hk + blockIdx.y) * (D * kT) + threadIdx.x * 4;
   const int64_t step = prm.kslots * p.Hk * (D * kT);
   const float f = is_k ? p.scale : 1.f;
-  for (int x = threadIdx.x; x < D / 4 * kT; x += 256) {
-    float4 a = make_float4(0, 0, 0, 0);
-#pragma unroll 4
-    for (int i = 0; i < parts; ++i) {
-      const float4 b = *reinterpret_cast<const float4*>(src + i * step + x * 4);
-      a.x += b.x;
-      a.y += b.y;
-      a.z += b.z;
-      a.w += b.w;
+  float4 a[kPer];
+#pragma unroll
+  for (int x = 0; x < kPer; ++x) a[x] = make_float4(0, 0, 0, 0);
+#pragma unroll 1
+  for (int i = 0; i < parts; ++i, src += step) {
+    float4 b[kPer];
+#pragma unroll
+    for (int x = 0; x < kPer; ++x) b[x] = *reinterpret_cast<const float4*>(src + x * 1024);
+#pragma unroll
+    for (int x = 0; x < kPer; ++x) {
+      a[x].x += b[x].x;
+      a[x].y += b[x].y;
+      a[x].z += b[x].z;
+      a[x].w += b[x].w;
     }
-    *reinterpret_cast<uint2*>(rows + (x % kT) * (D * 2 + 16) + (x / kT) * 8) =
-        make_uint2(pack_bf16x2(a.x * f, a.y * f), pack_bf16x2(a.z * f, a.w * f));
+  }
+#pragma unroll
+  for (int x = 0; x < kPer; ++x) {
+    const int at = x * 256 + threadIdx.x;
+    *reinterpret_cast<uint2*>(rows + (at % kT) * (D * 2 + 16) + (at / kT) * 8) =
+        make_uint2(pack_bf16x2(a[x].x * f, a[x].y * f), pack_bf16x2(a[x].z * f, a[x].w * f));
   }
   __syncthreads();
   __nv_bfloat16* out = static_cast<__nv_bfloat16*>(is_k ? p.dk : p.dv) + (int64_t)blockIdx.y * D;
