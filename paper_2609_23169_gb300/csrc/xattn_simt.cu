@@ -400,29 +400,49 @@ __global__ void __launch_bounds__(kXsThreads) xattn_dkdv_simt_kernel(const Xattn
   }
 }
 
-// D_i = dO_i . O_i -> [H, nq]; half a warp a row and head
+// D_i = dO_i . O_i -> [H, nq]: 16 bytes of O and dO a thread and step, the
+// threads of a row side by side, four steps in flight.  Also checks the
+// prefixes.  Bound by memory: 46 us for 23,959 x 24 x 128 in bf16 (295 MB).
+constexpr int kDsumSteps = 4;
 template <typename T, int D>
 __global__ void __launch_bounds__(256) xattn_dsum_kernel(const XattnParams p) {
-  const int64_t x = ((int64_t)blockIdx.x * blockDim.x + threadIdx.x) >> 4;
-  const int lane = threadIdx.x & 15;
+  constexpr int kVals = 16 / sizeof(T), kLanes = D / kVals;  // values of a thread, threads of a row
   if (blockIdx.x == 0) {
     check_cu(p.cu_q, p.B, p.nq, p.status);
     check_cu(p.cu_k, p.B, p.nk, p.status);
   }
-  float s = 0.f;
-  const int64_t tok = x / p.H;
-  const int h = (int)(x % p.H);
-  if (tok < p.nq) {
-    const T* o = static_cast<const T*>(p.o) + tok * p.os + (int64_t)h * D;
-    const T* d = static_cast<const T*>(p.dout) + tok * p.dos + (int64_t)h * D;
+  const uint32_t first = blockIdx.x * (256 / kLanes * kDsumSteps) + threadIdx.x / kLanes;  // row and head: 2^32 would be 512 GB
+  const int e = (int)(threadIdx.x % kLanes) * kVals;
+  uint4 a[kDsumSteps], b[kDsumSteps];
+  uint32_t tok[kDsumSteps], h[kDsumSteps];
 #pragma unroll
-    for (int c = 0; c < D / 64; ++c) {
-      const float4 a = ld4(o + lane * 4 + 64 * c), b = ld4(d + lane * 4 + 64 * c);
-      s = fmaf(a.x, b.x, fmaf(a.y, b.y, fmaf(a.z, b.z, fmaf(a.w, b.w, s))));
+  for (int i = 0; i < kDsumSteps; ++i) {
+    const uint32_t x = first + i * (256 / kLanes);
+    tok[i] = x / (uint32_t)p.H;
+    h[i] = x - tok[i] * (uint32_t)p.H;
+    a[i] = b[i] = make_uint4(0, 0, 0, 0);
+    if (tok[i] < p.nq) {
+      a[i] = *reinterpret_cast<const uint4*>(static_cast<const T*>(p.o) + (int64_t)tok[i] * p.os + h[i] * D + e);
+      b[i] = *reinterpret_cast<const uint4*>(static_cast<const T*>(p.dout) + (int64_t)tok[i] * p.dos + h[i] * D + e);
     }
   }
-  s = half_warp_sum(s);
-  if (tok < p.nq && lane == 0) p.dsum[(int64_t)h * p.nq + tok] = s;
+#pragma unroll
+  for (int i = 0; i < kDsumSteps; ++i) {
+    const uint32_t x[4] = {a[i].x, a[i].y, a[i].z, a[i].w}, y[4] = {b[i].x, b[i].y, b[i].z, b[i].w};
+    float s = 0.f;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      if constexpr (sizeof(T) == 4) {
+        s = fmaf(__uint_as_float(x[q]), __uint_as_float(y[q]), s);
+      } else {
+        s = fmaf(__uint_as_float(x[q] << 16), __uint_as_float(y[q] << 16), s);
+        s = fmaf(__uint_as_float(x[q] & 0xffff0000u), __uint_as_float(y[q] & 0xffff0000u), s);
+      }
+    }
+#pragma unroll
+    for (int q = kLanes / 2; q > 0; q >>= 1) s += __shfl_xor_sync(0xffffffffu, s, q);
+    if (e == 0 && tok[i] < p.nq) p.dsum[(int64_t)h[i] * p.nq + tok[i]] = s;
+  }
 }
 
 // dK, dV = the sum of the splits' partials, in split order; 4 values a thread
@@ -569,13 +589,14 @@ cudaError_t launch_xattn_join(const XattnParams& p, bool bf16, cudaStream_t s) {
                    : launch(xattn_join_kernel<float, 128>, grid, 0, p, s);
 }
 
+template <typename T, int D>
+static cudaError_t dsum(const XattnParams& p, cudaStream_t s) {
+  constexpr int64_t rows = 256 * 16 / sizeof(T) / D * kDsumSteps;  // of a block
+  return launch(xattn_dsum_kernel<T, D>, dim3((unsigned)((p.nq * p.H + rows) / rows)), 0, p, s);
+}
 cudaError_t launch_xattn_dsum(const XattnParams& p, bool bf16, cudaStream_t s) {
-  const dim3 grid((unsigned)((p.nq * p.H + 16) / 16));
-  if (bf16)
-    return p.d == 64 ? launch(xattn_dsum_kernel<__nv_bfloat16, 64>, grid, 0, p, s)
-                     : launch(xattn_dsum_kernel<__nv_bfloat16, 128>, grid, 0, p, s);
-  return p.d == 64 ? launch(xattn_dsum_kernel<float, 64>, grid, 0, p, s)
-                   : launch(xattn_dsum_kernel<float, 128>, grid, 0, p, s);
+  if (bf16) return p.d == 64 ? dsum<__nv_bfloat16, 64>(p, s) : dsum<__nv_bfloat16, 128>(p, s);
+  return p.d == 64 ? dsum<float, 64>(p, s) : dsum<float, 128>(p, s);
 }
 
 cudaError_t launch_xattn_bwd_simt(const XattnParams& p, cudaStream_t s) {
