@@ -202,8 +202,6 @@ ut_status ut_xattn_bwd(const ut_xattn_shape* shape, const void* q, const void* k
   p.dsum = reinterpret_cast<float*>(w);
   w += up256((size_t)p.H * p.nq * sizeof(float));
   cudaStream_t s = static_cast<cudaStream_t>(stream);
-  cudaError_t e = launch_xattn_dsum(p, bf16, s);
-  if (e != cudaSuccess) return UT_ERR_CUDA;
   if (bf16) return status_of(launch_xattn_bwd_tc(p, w, s));
   p.part_dk = reinterpret_cast<float*>(w);
   p.part_dv = reinterpret_cast<float*>(w + up256((size_t)p.nsplit * p.nk * p.Hk * p.d * sizeof(float)));

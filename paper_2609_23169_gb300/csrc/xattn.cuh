@@ -40,7 +40,28 @@ cudaError_t launch_xattn_join(const XattnParams& p, bool bf16, cudaStream_t s); 
 int64_t xattn_bwd_tc_items(const XattnParams& p);
 size_t xattn_bwd_tc_ws(const XattnParams& p);
 cudaError_t launch_xattn_dsum(const XattnParams& p, bool bf16, cudaStream_t s);  // D, and the check of the prefixes
-cudaError_t launch_xattn_bwd_simt(const XattnParams& p, cudaStream_t s);         // fp32, after D
-cudaError_t launch_xattn_bwd_tc(const XattnParams& p, void* ws, cudaStream_t s); // bf16, after D
+cudaError_t launch_xattn_bwd_simt(const XattnParams& p, cudaStream_t s);         // fp32
+cudaError_t launch_xattn_bwd_tc(const XattnParams& p, void* ws, cudaStream_t s); // bf16
+
+// The kernels of a backward pass follow one another without a gap: each says
+// at once that the next may be launched, and the next does what needs no
+// result (barriers, TMEM, its own decoding) and then waits for the whole grid
+// before it.
+__device__ __forceinline__ void grid_next() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+__device__ __forceinline__ void grid_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+template <typename F, typename... A>
+cudaError_t launch_next(F kern, dim3 grid, dim3 block, size_t smem, cudaStream_t s, const A&... args) {
+  cudaLaunchAttribute attr{};
+  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr.val.programmaticStreamSerializationAllowed = 1;
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = grid;
+  cfg.blockDim = block;
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = s;
+  cfg.attrs = &attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, kern, args...);
+}
 
 }  // namespace ut

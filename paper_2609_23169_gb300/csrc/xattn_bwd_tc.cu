@@ -162,9 +162,11 @@ __global__ void __launch_bounds__(kDqThreads, 1)
     tmem_alloc(&sm.tmem_base, 512);
     tmem_relinquish();
   }
+  grid_next();
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
+  grid_wait();
   // all 512 columns are this CTA's, so they start at address 0
   if (sm.tmem_base != 0 && threadIdx.x == 0) {
     set_status(p.status, UT_ERR_CUDA);
@@ -640,9 +642,11 @@ __global__ void __launch_bounds__(kKvThreads, 1)
     tmem_alloc(&sm.tmem_base, 512);
     tmem_relinquish();
   }
+  grid_next();
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
+  grid_wait();
   if (sm.tmem_base != 0 && threadIdx.x == 0) {  // as in the dQ kernel
     set_status(p.status, UT_ERR_CUDA);
     sm.abort_flag = 1;
@@ -968,6 +972,7 @@ __global__ void __launch_bounds__(256) xattn_bwd_join_kernel(const BwdParams prm
   constexpr int kPer = D / 4 * kT / 256;
   __shared__ __align__(16) uint8_t rows[kT * (D * 2 + 16)];
   const XattnParams& p = prm.x;
+  grid_wait();
   const Segment g = segment_of_slot(p.cu_k, p.B, p.nk, kT, blockIdx.x);
   const int keys = (int)min((int64_t)kT, g.n - g.tile * kT);
   if (keys <= 0) return;
@@ -1027,8 +1032,7 @@ cudaError_t launch(F kern, int threads, size_t smem, int regs, const BwdParams& 
   if (e != cudaSuccess) return e;
   if (fa.numRegs != regs) return cudaErrorInvalidConfiguration;
   const int grid = (int)(prm.n_items < prm.x.sms ? prm.n_items : prm.x.sms);
-  kern<<<grid, threads, smem, s>>>(tm[0], tm[1], tm[2], tm[3], prm);
-  return cudaGetLastError();
+  return launch_next(kern, dim3(grid), dim3(threads), smem, s, tm[0], tm[1], tm[2], tm[3], prm);
 }
 
 // Items of a run along the keys: the blocks of a segment of mean length, so
@@ -1083,7 +1087,8 @@ cudaError_t launch_xattn_bwd_tc(const XattnParams& p, void* ws, cudaStream_t s) 
   prm.x.part_dk = static_cast<float*>(ws);
   prm.x.part_dv = reinterpret_cast<float*>(static_cast<char*>(ws) + part_bytes(p, prm.R));
   prm.scale_log2 = p.scale * kLog2e;
-  cudaError_t e = cudaSuccess;
+  cudaError_t e = launch_xattn_dsum(p, true, s);
+  if (e != cudaSuccess) return e;
   if (p.nq > 0) {
     // without keys the K and V maps are never used
     const void* k = p.nk > 0 ? p.k : p.q;
@@ -1108,9 +1113,8 @@ cudaError_t launch_xattn_bwd_tc(const XattnParams& p, void* ws, cudaStream_t s) 
   }
   if (p.nk > 0) {
     const dim3 grid((unsigned)prm.kslots, p.Hk, 2);
-    if (p.d == 64) xattn_bwd_join_kernel<64><<<grid, 256, 0, s>>>(prm);
-    else xattn_bwd_join_kernel<128><<<grid, 256, 0, s>>>(prm);
-    e = cudaGetLastError();
+    e = p.d == 64 ? launch_next(xattn_bwd_join_kernel<64>, grid, dim3(256), 0, s, prm)
+                  : launch_next(xattn_bwd_join_kernel<128>, grid, dim3(256), 0, s, prm);
   }
   return e;
 }

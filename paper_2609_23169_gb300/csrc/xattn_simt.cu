@@ -277,10 +277,9 @@ UT_DEV void stage_rows(float* lse, float* dsum, const XattnParams& p, const XsTi
   }
 }
 
-// grid (q slots, kv heads): dQ of a tile over the segment's keys
+// dQ of a query tile over the segment's keys
 template <typename T, int D>
-__global__ void __launch_bounds__(kXsThreads) xattn_dq_simt_kernel(const XattnParams p) {
-  extern __shared__ float sm[];
+UT_DEV void dq_tile(const XattnParams& p, float* sm, int64_t slot, int hk) {
   float* qs = sm;
   float* dos = qs + kXs * (D + 4);
   float* ks = dos + kXs * (D + 4);
@@ -290,9 +289,8 @@ __global__ void __launch_bounds__(kXsThreads) xattn_dq_simt_kernel(const XattnPa
   float* lse = on + kXs;
   float* dsum = lse + kXs;
   const int tpt = kXs / p.G;
-  const Segment g = segment_of_slot(p.cu_q, p.B, p.nq, tpt, blockIdx.x);
+  const Segment g = segment_of_slot(p.cu_q, p.B, p.nq, tpt, slot);
   if (g.tile * tpt >= g.n) return;
-  const int hk = blockIdx.y;
   XsTile t{g.row + g.tile * tpt, (int)min((int64_t)tpt, g.n - g.tile * tpt) * p.G, hk * p.G, p.G};
   int64_t k0, kn;
   segment_rows(p.cu_k, g.s, p.nk, k0, kn);
@@ -333,11 +331,9 @@ __global__ void __launch_bounds__(kXsThreads) xattn_dq_simt_kernel(const XattnPa
   }
 }
 
-// grid (k slots, kv heads, query splits): partial dK, dV of a key tile over a
-// range of the segment's query tiles
+// Partial dK, dV of a key tile over a range of the segment's query tiles
 template <typename T, int D>
-__global__ void __launch_bounds__(kXsThreads) xattn_dkdv_simt_kernel(const XattnParams p) {
-  extern __shared__ float sm[];
+UT_DEV void dkdv_tile(const XattnParams& p, float* sm, int64_t slot, int hk, int split) {
   float* qs = sm;
   float* dos = qs + kXs * (D + 4);
   float* ks = dos + kXs * (D + 4);
@@ -347,9 +343,8 @@ __global__ void __launch_bounds__(kXsThreads) xattn_dkdv_simt_kernel(const Xattn
   float* on = dss + kXs * kXsLdP;
   float* lse = on + kXs;
   float* dsum = lse + kXs;
-  const Segment g = segment_of_slot(p.cu_k, p.B, p.nk, kXs, blockIdx.x);
+  const Segment g = segment_of_slot(p.cu_k, p.B, p.nk, kXs, slot);
   if (g.tile * kXs >= g.n) return;
-  const int hk = blockIdx.y, split = blockIdx.z;
   const int64_t key0 = g.row + g.tile * kXs, left = g.n - g.tile * kXs;
   int64_t q0, qn;
   segment_rows(p.cu_q, g.s, p.nq, q0, qn);
@@ -400,6 +395,24 @@ __global__ void __launch_bounds__(kXsThreads) xattn_dkdv_simt_kernel(const Xattn
   }
 }
 
+// One launch for both, the longer blocks first: n_kv blocks of dK, dV (k slots
+// fastest, then kv heads, query splits), then dQ (q slots, kv heads).  Apart,
+// each ended in a wave of a few blocks (2,501 x 301, 8 heads: 38 + 66 us).
+template <typename T, int D>
+__global__ void __launch_bounds__(kXsThreads) xattn_bwd_simt_kernel(const XattnParams p, uint32_t n_kv,
+                                                                     uint32_t kslots, uint32_t qslots) {
+  extern __shared__ float sm[];
+  grid_wait();
+  const uint32_t x = blockIdx.x;
+  if (x < n_kv) {
+    const uint32_t y = x / kslots;
+    dkdv_tile<T, D>(p, sm, x - y * kslots, (int)(y % p.Hk), (int)(y / p.Hk));
+  } else {
+    const uint32_t y = (x - n_kv) / qslots;
+    dq_tile<T, D>(p, sm, x - n_kv - y * qslots, (int)y);
+  }
+}
+
 // D_i = dO_i . O_i -> [H, nq]: 16 bytes of O and dO a thread and step, the
 // threads of a row side by side, four steps in flight.  Also checks the
 // prefixes.  Bound by memory: 46 us for 23,959 x 24 x 128 in bf16 (295 MB).
@@ -407,6 +420,7 @@ constexpr int kDsumSteps = 4;
 template <typename T, int D>
 __global__ void __launch_bounds__(256) xattn_dsum_kernel(const XattnParams p) {
   constexpr int kVals = 16 / sizeof(T), kLanes = D / kVals;  // values of a thread, threads of a row
+  grid_next();
   if (blockIdx.x == 0) {
     check_cu(p.cu_q, p.B, p.nq, p.status);
     check_cu(p.cu_k, p.B, p.nk, p.status);
@@ -450,6 +464,7 @@ __global__ void __launch_bounds__(256) xattn_dkdv_join_kernel(const XattnParams 
   const int64_t x = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;
   const int per_row = p.Hk * p.d / 4;
   const int64_t n = p.nk * per_row;
+  grid_wait();
   if (x >= n) return;
   const int64_t key = x / per_row;
   const int e = (int)(x % per_row) * 4;
@@ -457,6 +472,7 @@ __global__ void __launch_bounds__(256) xattn_dkdv_join_kernel(const XattnParams 
   for (int which = 0; which < 2; ++which) {
     const float* src = (which ? p.part_dv : p.part_dk) + x * 4;
     float4 a = make_float4(0, 0, 0, 0);
+#pragma unroll 8
     for (int s = 0; s < p.nsplit; ++s) {
       const float4 b = ld4(src + (int64_t)s * n * 4);
       a.x += b.x;
@@ -526,20 +542,20 @@ static cudaError_t fwd(const XattnParams& p, cudaStream_t s) {
 
 template <typename T, int D>
 static cudaError_t bwd(const XattnParams& p, cudaStream_t s) {
-  cudaError_t e = cudaSuccess;
+  cudaError_t e = launch_xattn_dsum(p, sizeof(T) == 2, s);
+  if (e != cudaSuccess) return e;
   const size_t tiles = sizeof(float) * 4 * kXs * (D + 4), pair = sizeof(float) * kXs * kXsLdP,
                vecs = sizeof(float) * 3 * kXs;
-  if (p.nq > 0) {
-    e = launch(xattn_dq_simt_kernel<T, D>, dim3((unsigned)segment_slots(p.nq, p.B, kXs / p.G), p.Hk),
-               tiles + pair + vecs, p, s);
-    if (e != cudaSuccess) return e;
-  }
-  if (p.nk > 0) {
-    e = launch(xattn_dkdv_simt_kernel<T, D>, dim3((unsigned)segment_slots(p.nk, p.B, kXs), p.Hk, p.nsplit),
-               tiles + 2 * pair + vecs, p, s);
-    if (e != cudaSuccess) return e;
-    e = launch(xattn_dkdv_join_kernel, dim3((unsigned)((p.nk * p.Hk * D / 4 + 255) / 256)), 0, p, s);
-  }
+  const uint32_t kslots = (uint32_t)segment_slots(p.nk, p.B, kXs), qslots = (uint32_t)segment_slots(p.nq, p.B, kXs / p.G);
+  const int64_t n_kv = p.nk > 0 ? (int64_t)kslots * p.Hk * p.nsplit : 0, n_q = p.nq > 0 ? (int64_t)qslots * p.Hk : 0;
+  if (n_kv + n_q > INT32_MAX) return cudaErrorInvalidValue;
+  const size_t smem = tiles + 2 * pair + vecs;
+  e = cudaFuncSetAttribute(xattn_bwd_simt_kernel<T, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+  if (e == cudaSuccess)
+    e = launch_next(xattn_bwd_simt_kernel<T, D>, dim3((unsigned)(n_kv + n_q)), dim3(kXsThreads), smem, s, p,
+                    (uint32_t)n_kv, kslots, qslots);
+  if (e == cudaSuccess && p.nk > 0)
+    e = launch_next(xattn_dkdv_join_kernel, dim3((unsigned)((p.nk * p.Hk * D / 4 + 255) / 256)), dim3(256), 0, s, p);
   return e;
 }
 
