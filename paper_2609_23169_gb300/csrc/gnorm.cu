@@ -231,14 +231,19 @@ struct RingState {
   int abort_flag;
 };
 
-// One side's view of the ring: which phase of each slot's barrier is next.
+// One side's view of the ring: which phase of each slot's barrier is next.  A
+// wait that runs out leaves UT_ERR_TIMEOUT in the status word and ends the
+// block's waits; the block still meets the others at the grid barriers and
+// writes its rows (wrong ones, inside the tensors), the producer loads nothing
+// more and sees that what it asked for has landed.
 struct Ring {
   RingState* st;
   uint8_t* mem;
   int slots, slot_bytes;
   int32_t* status;
   uint64_t timeout_ns;
-  uint32_t full_par, empty_par;  // bit per slot
+  uint32_t full_par, empty_par;  // bit per slot; the producer's full_par: loads asked for
+  bool dead;
   UT_DEV int next(int s) const { return s + 1 < slots ? s + 1 : 0; }
   UT_DEV int before(int s) const { return s > 0 ? s - 1 : slots - 1; }
   UT_DEV void wait_full(int s) {
@@ -250,9 +255,17 @@ struct Ring {
     if (lane_id() == 0) mbar_arrive(&st->empty[s]);
   }
   // producer: waits until the slot's last use is over (a first use waits for nothing)
-  UT_DEV void wait_empty(int s) {
-    mbar_wait(&st->empty[s], ((empty_par >> s) & 1) ^ 1, &st->abort_flag, status, timeout_ns);
+  UT_DEV bool wait_empty(int s) {
+    if (!dead) dead = !warp_wait(&st->empty[s], ((empty_par >> s) & 1) ^ 1, &st->abort_flag, status, timeout_ns);
     empty_par ^= 1u << s;
+    return !dead;
+  }
+  // producer, at the end: its loads into the used slots have landed
+  UT_DEV void finish(uint32_t used) {
+    if (lane_id() == 0)
+      for (int s = 0; s < slots; ++s)
+        if ((used >> s) & 1)
+          if (!mbar_drain(&st->full[s], ((full_par >> s) & 1) ^ 1, kDrainTimeoutNs)) set_status(status, UT_ERR_TIMEOUT);
   }
 };
 
@@ -297,9 +310,11 @@ UT_DEV void for_pieces_back(const GnormParams& p, const Batch& b, int a, int e, 
 // The producer's part of both passes over a batch: tensors x (and dy).
 template <int kThreads, int kPer, int kTensors>
 UT_DEV void produce(const GnormParams& p, const Batch& b, int a, int e, const Chunks<kThreads, kPer>& ck,
-                    Ring& ring, int total, int elem) {
+                    Ring& ring, uint32_t& used, int total, int elem) {
   auto load = [&](int at, int slab, int r, int n) {
-    ring.wait_empty(at);
+    if (!ring.wait_empty(at)) return;
+    ring.full_par ^= 1u << at;
+    used |= 1u << at;
     uint64_t* bar = &ring.st->full[at];
     const int cols = ck.slab_cols(slab);
     if (lane_id() == 0) mbar_expect_tx(bar, (uint32_t)n * cols * 16 * kTensors);
@@ -460,7 +475,8 @@ __global__ void __launch_bounds__(kFwdThreads + 32, 1) gn_fwd_kernel(const Gnorm
   const float inv_cpg = 1.f / (float)cpg;
   const Chunks<kFwdThreads, kFwdPer> ck(p.C / V);
   prefetch_affine(p);
-  Ring ring{st, smem + p.ring_at, p.slots, p.slot_bytes, p.status, p.timeout_ns, 0, 0};
+  Ring ring{st, smem + p.ring_at, p.slots, p.slot_bytes, p.status, p.timeout_ns, 0, 0, false};
+  uint32_t used = 0;  // slots that the producer has loaded
   float2* part0 = static_cast<float2*>(p.ws);
   ring_init<kFwdThreads>(st, p.slots);
   if (me == 0 && warp < kFwdThreads / 32) {
@@ -483,7 +499,7 @@ __global__ void __launch_bounds__(kFwdThreads + 32, 1) gn_fwd_kernel(const Gnorm
     int total = 0;  // chunks
     for_pieces(p, b, a, e, [&](int, int lo, int hi) { total += ck.of_piece(hi - lo); });
     if (warp == kFwdThreads / 32) {
-      produce<kFwdThreads, kFwdPer, 1>(p, b, a, e, ck, ring, total, sizeof(T));
+      produce<kFwdThreads, kFwdPer, 1>(p, b, a, e, ck, ring, used, total, sizeof(T));
       continue;
     }
     int i = 0, slot = 0;
@@ -666,6 +682,7 @@ __global__ void __launch_bounds__(kFwdThreads + 32, 1) gn_fwd_kernel(const Gnorm
       }
     });
   }
+  if (warp == kFwdThreads / 32) ring.finish(used);
 }
 
 // ------------------------------------------------------------------ backward
@@ -695,7 +712,8 @@ __global__ void __launch_bounds__(kBwdThreads + 32, 1) gn_bwd_kernel(const Gnorm
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const Chunks<kBwdThreads, kBwdPer> ck(p.C / V);
   prefetch_affine(p);
-  Ring ring{st, smem + p.ring_at, p.slots, p.slot_bytes, p.status, p.timeout_ns, 0, 0};
+  Ring ring{st, smem + p.ring_at, p.slots, p.slot_bytes, p.status, p.timeout_ns, 0, 0, false};
+  uint32_t used = 0;  // slots that the producer has loaded
   float2* part0 = static_cast<float2*>(p.ws);                // [2][blocks + B][G]
   float2* sums = part0 + (int64_t)2 * (blocks + p.B) * p.G;  // [blocks][C]
   ring_init<kBwdThreads>(st, p.slots);
@@ -716,7 +734,7 @@ __global__ void __launch_bounds__(kBwdThreads + 32, 1) gn_bwd_kernel(const Gnorm
     int total = 0;  // chunks
     for_pieces(p, b, a, e, [&](int, int lo, int hi) { total += ck.of_piece(hi - lo); });
     if (warp == kBwdThreads / 32) {
-      produce<kBwdThreads, kBwdPer, 2>(p, b, a, e, ck, ring, total, sizeof(T));
+      produce<kBwdThreads, kBwdPer, 2>(p, b, a, e, ck, ring, used, total, sizeof(T));
       continue;
     }
     int i = 0, slot = 0;
@@ -907,6 +925,7 @@ __global__ void __launch_bounds__(kBwdThreads + 32, 1) gn_bwd_kernel(const Gnorm
       }
     });
   }
+  if (warp == kBwdThreads / 32) ring.finish(used);
 }
 
 // ----------------------------------------------------------------- launchers
