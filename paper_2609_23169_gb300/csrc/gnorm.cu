@@ -757,21 +757,34 @@ __global__ void __launch_bounds__(kBwdThreads + 32, 1) gn_bwd_kernel(const Gnorm
             uint64_t b1[V / 2], b2[V / 2];
 #pragma unroll
             for (int c = 0; c < V / 2; ++c) b1[c] = b2[c] = 0;
+            const int step = L.lanes * L.cols * 16;
+            auto row = [&](const uint4& wx, const uint4& wg) {
+              uint64_t v[V / 2], g[V / 2];
+              Vec<T>::unpack(wx, v);
+              Vec<T>::unpack(wg, g);
 #pragma unroll
-            for (int k = 0; k < kBwdPer; ++k)
-              if (r + L.lane + k * L.lanes < n) {
-                const uint8_t* at = src + k * L.lanes * L.cols * 16;
-                uint64_t v[V / 2], g[V / 2];
-                Vec<T>::unpack(*reinterpret_cast<const uint4*>(at), v);
-                Vec<T>::unpack(*reinterpret_cast<const uint4*>(at + ring.slot_bytes / 2), g);
-#pragma unroll
-                for (int c = 0; c < V / 2; ++c) {
-                  uint64_t xh;
-                  const uint64_t du = du_of<kAct>(v[c], g[c], ch.neg_mean[c], ch.rstd[c], ch.gamma[c], ch.beta[c], xh);
-                  b1[c] = add_f32x2(b1[c], du);
-                  b2[c] = fma_f32x2(du, xh, b2[c]);
-                }
+              for (int c = 0; c < V / 2; ++c) {
+                uint64_t xh;
+                const uint64_t du = du_of<kAct>(v[c], g[c], ch.neg_mean[c], ch.rstd[c], ch.gamma[c], ch.beta[c], xh);
+                b1[c] = add_f32x2(b1[c], du);
+                b2[c] = fma_f32x2(du, xh, b2[c]);
               }
+            };
+            if (r + ck.rows <= n) {  // a full chunk
+              uint4 wx[kBwdPer], wg[kBwdPer];
+#pragma unroll
+              for (int k = 0; k < kBwdPer; ++k) {
+                wx[k] = *reinterpret_cast<const uint4*>(src + k * step);
+                wg[k] = *reinterpret_cast<const uint4*>(src + k * step + ring.slot_bytes / 2);
+              }
+#pragma unroll
+              for (int k = 0; k < kBwdPer; ++k) row(wx[k], wg[k]);
+            } else {
+#pragma unroll 1
+              for (int k = 0; k < kBwdPer && r + L.lane + k * L.lanes < n; ++k)
+                row(*reinterpret_cast<const uint4*>(src + k * step),
+                    *reinterpret_cast<const uint4*>(src + k * step + ring.slot_bytes / 2));
+            }
 #pragma unroll
             for (int c = 0; c < V / 2; ++c) {
               t1[c] = add_f32x2(t1[c], b1[c]);
@@ -903,22 +916,37 @@ __global__ void __launch_bounds__(kBwdThreads + 32, 1) gn_bwd_kernel(const Gnorm
           const int r = lo + c * ck.rows + L.lane;
           if (L.on) {
             const uint8_t* src = ring.mem + (int64_t)slot * ring.slot_bytes + (L.lane * L.cols + L.col - slab * kBwdThreads) * 16;
+            const int step = L.lanes * L.cols * 16;
+            uint8_t* to = dst + (int64_t)r * p.dxs * (int64_t)sizeof(T);
+            const int64_t to_step = L.lanes * p.dxs * (int64_t)sizeof(T);
+            auto row = [&](const uint4& wx, const uint4& wg) -> uint4 {
+              uint64_t v[V / 2], g[V / 2];
+              Vec<T>::unpack(wx, v);
+              Vec<T>::unpack(wg, g);
 #pragma unroll
-            for (int k = 0; k < kBwdPer; ++k)
-              if (r + k * L.lanes < hi) {
-                const uint8_t* at = src + k * L.lanes * L.cols * 16;
-                uint64_t v[V / 2], g[V / 2];
-                Vec<T>::unpack(*reinterpret_cast<const uint4*>(at), v);
-                Vec<T>::unpack(*reinterpret_cast<const uint4*>(at + ring.slot_bytes / 2), g);
-#pragma unroll
-                for (int x = 0; x < V / 2; ++x) {
-                  uint64_t xh;
-                  const uint64_t du = du_of<kAct>(v[x], g[x], ch.neg_mean[x], ch.rstd[x], ch.gamma[x], ch.beta[x], xh);
-                  const uint64_t t = fma_f32x2(ch.gamma[x], du, ab.neg_mean[x]);
-                  v[x] = mul_f32x2(ch.rstd[x], fma_f32x2(mul_f32x2(xh, both(-1.f)), ab.rstd[x], t));
-                }
-                store_stream(dst + (int64_t)(r + k * L.lanes) * p.dxs * (int64_t)sizeof(T), Vec<T>::pack(v));
+              for (int x = 0; x < V / 2; ++x) {
+                uint64_t xh;
+                const uint64_t du = du_of<kAct>(v[x], g[x], ch.neg_mean[x], ch.rstd[x], ch.gamma[x], ch.beta[x], xh);
+                const uint64_t t = fma_f32x2(ch.gamma[x], du, ab.neg_mean[x]);
+                v[x] = mul_f32x2(ch.rstd[x], fma_f32x2(mul_f32x2(xh, both(-1.f)), ab.rstd[x], t));
               }
+              return Vec<T>::pack(v);
+            };
+            if (lo + (c + 1) * ck.rows <= hi) {  // a full chunk
+              uint4 wx[kBwdPer], wg[kBwdPer];
+#pragma unroll
+              for (int k = 0; k < kBwdPer; ++k) {
+                wx[k] = *reinterpret_cast<const uint4*>(src + k * step);
+                wg[k] = *reinterpret_cast<const uint4*>(src + k * step + ring.slot_bytes / 2);
+              }
+#pragma unroll
+              for (int k = 0; k < kBwdPer; ++k) store_stream(to + k * to_step, row(wx[k], wg[k]));
+            } else {
+#pragma unroll 1
+              for (int k = 0; k < kBwdPer && r + k * L.lanes < hi; ++k)
+                store_stream(to + k * to_step, row(*reinterpret_cast<const uint4*>(src + k * step),
+                                                   *reinterpret_cast<const uint4*>(src + k * step + ring.slot_bytes / 2)));
+            }
           }
           ring.release(slot);
         }
