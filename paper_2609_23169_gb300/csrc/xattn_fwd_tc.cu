@@ -13,7 +13,8 @@
 // Persistent CTAs, one per SM; items with the head fastest, so that CTAs in
 // flight read neighbouring 256-byte pieces of the same rows and share K and V
 // in L2.  Roles (384 threads, registers rebalanced with setmaxnreg):
-//   warp 0      TMA: the K and V tiles, one ring (K0 V0 K1 V1 ...)
+//   warp 0      TMA: the K and V tiles, one ring (K0 V0 K1 V1 ...); with a V
+//               tile, which of its keys count
 //   warp 2      decodes the items (segment search, key range) into a ring, 32
 //               at once, one a lane; TMA: the query tiles, a ring of their own
 //   warp 1      TMEM owner and MMA issuer of tile 0, warp 3 of tile 1: per
@@ -29,9 +30,12 @@
 //               rescaled in TMEM only where it grew by more than 2^8, so the
 //               exponentials stay bounded), write P as bf16 over S; after the
 //               last block O / l and LSE, or the split's partial result.
-// Masked keys and the rows of other segments: S there is replaced by -inf,
-// and the softmax warps zero those rows of the V tile before its products, so
-// that no value they hold (NaN, infinities) is multiplied.
+// Masked keys and the rows of other segments: S there becomes -inf, the
+// smaller of S and a bias of +-inf that warp 0 leaves in shared memory (the
+// min of NaN and -inf is -inf; selecting by bits of the mask took 900 to 1,300
+// cycles a block, this takes 400), and the softmax warps zero those rows of the
+// V tile before its products, so that no value they hold (NaN, infinities) is
+// multiplied.
 // TMEM columns: S_0 / P_0 [0,128), S_1 / P_1 [128,256), O_0 [256,256+d), O_1
 // [384,384+d).
 // Every wait is bounded; on expiry the kernel records UT_ERR_TIMEOUT, drains
@@ -71,6 +75,8 @@ struct Smem {
   static constexpr int kKv = D == 128 ? 4 : 8;  // K and V tiles in flight
   alignas(1024) uint8_t q[kQ][kTile];
   alignas(1024) uint8_t kv[kKv][kTile];
+  float bias[kKv / 2][kN];        // of the keys of a V tile: 0 < bias = attend
+  alignas(16) uint32_t keys[kKv / 2][4];  // and as bits
   uint64_t q_full[kQ], q_empty[kQ], kv_full[kKv], kv_empty[kKv];
   uint64_t s_full[2], p_most[2], p_full[2], o_full[2], o_empty[2], turn[2], mma_done;
   uint64_t item_full[kItemSlots], item_empty[kItemSlots];
@@ -78,6 +84,9 @@ struct Smem {
   uint32_t tmem_base;
   int abort_flag;
 };
+
+// whether a block with `left` keys to the end of its segment needs no masking
+UT_DEV bool all_keys(const uint8_t* mask, int left) { return !mask && left >= kN; }
 
 struct Params {
   XattnParams x;
@@ -149,50 +158,62 @@ __global__ void __launch_bounds__(kThreads, 1)
   auto wait = [&](uint64_t* bar, uint32_t parity) {  // whole warp, converged
     return warp_wait(bar, parity, abort_flag, p.status, p.timeout_ns);
   };
-  auto wait1 = [&](uint64_t* bar, uint32_t parity) {  // one thread
-    return mbar_wait(bar, parity, abort_flag, p.status, p.timeout_ns);
-  };
   auto drain = [&](uint64_t* bar, uint32_t parity) {
     if (!mbar_drain(bar, parity, kDrainTimeoutNs)) set_status(p.status, UT_ERR_TIMEOUT);
   };
-  // The next item; false at the end or on an abort (then ok = false).  Whole
-  // warp, or a single thread with one = true.
-  auto next_item = [&](uint32_t& n, Item& it, bool& ok, bool one) -> bool {
-    const uint32_t s = n % kItemSlots, f = (n / kItemSlots) & 1;
-    ok = one ? wait1(&sm.item_full[s], f) : wait(&sm.item_full[s], f);
-    if (!ok) return false;
+  // The next item; false at the end or on an abort (then ok = false).
+  auto next_item = [&](uint32_t& n, Item& it, bool& ok) -> bool {
+    const uint32_t s = n % kItemSlots;
+    if (!(ok = wait(&sm.item_full[s], (n / kItemSlots) & 1))) return false;
     it = sm.item[s];
-    if (!one) __syncwarp();
-    if (one || lane == 0) mbar_arrive(&sm.item_empty[s]);
+    __syncwarp();
+    if (lane == 0) mbar_arrive(&sm.item_empty[s]);
     ++n;
     return it.hk >= 0;
   };
 
   if (warp < 4) {
     setmaxnreg_dec<kRegCtl>();
-    if (warp == 0 && lane == 0) {
+    if (warp == 0) {
       // ------------------------------------------------------- K, V producer
-      tma_prefetch_desc(&tm_k);
-      tma_prefetch_desc(&tm_v);
+      if (lane == 0) {
+        tma_prefetch_desc(&tm_k);
+        tma_prefetch_desc(&tm_v);
+      }
       const uint64_t pol = prm.keep_kv ? policy_evict_last() : policy_evict_first();
       uint32_t n = 0, at = 0;
       bool ok = true;
       Item it;
-      while (ok && next_item(n, it, ok, true)) {
+      while (ok && next_item(n, it, ok)) {
         for (int j = 0; j < it.blocks && ok; ++j) {
+          const bool plain = all_keys(p.mask, it.left - j * kN);
+          const uint32_t keys = plain ? 15u : lane_keys(p.mask, (int64_t)it.key0 + j * kN, it.left - j * kN, lane);
 #pragma unroll 1
-          for (int which = 0; which < 2; ++which) {
-            const uint32_t st = at % S::kKv, f = at / S::kKv;
-            if (!(ok = wait1(&sm.kv_empty[st], (f & 1) ^ 1))) break;
-            mbar_expect_tx(&sm.kv_full[st], S::kTile);
-            const void* tm = which ? static_cast<const void*>(&tm_v) : static_cast<const void*>(&tm_k);
-            for (int c = 0; c < S::kChunks; ++c)
-              tma_load_3d(sm.kv[st] + c * kChunkBytes, tm, &sm.kv_full[st], c * 64, it.hk, it.key0 + j * kN, pol);
-            ++at;
+          for (int which = 0; which < 2; ++which, ++at) {
+            const uint32_t st = at % S::kKv;
+            if (!(ok = wait(&sm.kv_empty[st], ((at / S::kKv) & 1) ^ 1))) break;
+            if (which && !plain) {
+#pragma unroll
+              for (int g = 0; g < 4; ++g) {
+                const bool on = (keys >> g) & 1u;
+                const uint32_t word = __ballot_sync(0xffffffffu, on);
+                sm.bias[st / 2][g * 32 + lane] = on ? INFINITY : -INFINITY;
+                if (lane == 0) sm.keys[st / 2][g] = word;
+              }
+              __syncwarp();
+            }
+            if (lane == 0) {
+              mbar_expect_tx(&sm.kv_full[st], S::kTile);
+              const void* tm = which ? static_cast<const void*>(&tm_v) : static_cast<const void*>(&tm_k);
+              for (int c = 0; c < S::kChunks; ++c)
+                tma_load_3d(sm.kv[st] + c * kChunkBytes, tm, &sm.kv_full[st], c * 64, it.hk, it.key0 + j * kN, pol);
+            }
+            __syncwarp();
           }
         }
       }
-      for (uint32_t x = at > S::kKv ? at - S::kKv : 0; x < at; ++x) drain(&sm.kv_full[x % S::kKv], (x / S::kKv) & 1);
+      if (lane == 0)
+        for (uint32_t x = at > S::kKv ? at - S::kKv : 0; x < at; ++x) drain(&sm.kv_full[x % S::kKv], (x / S::kKv) & 1);
     } else if (warp == 2) {
       // ------------------------------------------- item decoder, Q producer
       if (lane == 0) tma_prefetch_desc(&tm_q);
@@ -359,38 +380,40 @@ __global__ void __launch_bounds__(kThreads, 1)
       if (it->hk < 0) break;
       const int blocks = it->ntok[w] > 0 ? it->blocks : 0;
       float m = -1e30f, l = 0.f;
-      uint32_t keys = blocks > 0 ? lane_keys(p.mask, it->key0, it->left, lane) : 0;
       for (int j = 0; j < blocks; ++j) {
-        const uint32_t now = keys;
-        if (j + 1 < blocks)  // the next block's, fetched a block ahead
-          keys = lane_keys(p.mask, (int64_t)it->key0 + (j + 1) * kN, it->left - (j + 1) * kN, lane);
+        const bool plain = all_keys(p.mask, it->left - j * kN);
+        const uint32_t vat = kvat + 2 * j + 1, vst = vat % S::kKv;
         if (!(ok = wait(&sm.s_full[w], ns & 1))) break;
         ++ns;
         tc_fence_after();
         uint32_t r[kN];
 #pragma unroll
         for (int g = 0; g < 4; ++g) tmem_ld32(ts + g * 32, *reinterpret_cast<uint32_t(*)[32]>(&r[g * 32]));
-        tmem_wait_ld();
-        if (!__all_sync(0xffffffffu, now == 15u)) {
-          {
-            // zero the rows of the V tile that must not enter the product
-            // (thread = row; the other tile's warps may write the same zeros)
-            const uint32_t vat = kvat + 2 * j + 1, st = vat % S::kKv;
-            if (!(ok = wait(&sm.kv_full[st], (vat / S::kKv) & 1))) break;
-            if (!((now >> quarter) & 1u)) {
-              const uint32_t v_row = smem_u32(sm.kv[st]) + (quarter * 32 + lane) * 128;
+        if (!plain) {
+          // the V tile and its keys; its rows that must not enter the product
+          // become zero (thread = row; the other tile's warps may write the same)
+          ok = wait(&sm.kv_full[vst], (vat / S::kKv) & 1);
+          if (ok && !((sm.keys[vst / 2][quarter] >> lane) & 1u)) {
+            const uint32_t v_row = smem_u32(sm.kv[vst]) + (quarter * 32 + lane) * 128;
 #pragma unroll
-              for (int x = 0; x < 8 * S::kChunks; ++x)
-                st_shared_v4(v_row + (x >> 3) * kChunkBytes + (((x + lane) & 7) << 4), 0, 0, 0, 0);
-            }
-            fence_proxy_async_smem();
+            for (int x = 0; x < 8 * S::kChunks; ++x)
+              st_shared_v4(v_row + (x >> 3) * kChunkBytes + (((x + lane) & 7) << 4), 0, 0, 0, 0);
           }
+          fence_proxy_async_smem();
+        }
+        tmem_wait_ld();
+        if (!ok) break;
+        if (!plain) {
+          const uint4 word = *reinterpret_cast<const uint4*>(sm.keys[vst / 2]);
+          if ((word.x & word.y & word.z & word.w) != 0xffffffffu) {
 #pragma unroll
-          for (int g = 0; g < 4; ++g) {
-            const uint32_t word = __ballot_sync(0xffffffffu, (now >> g) & 1u);
-#pragma unroll
-            for (int x = 0; x < 32; ++x)
-              if (!((word >> x) & 1u)) r[g * 32 + x] = 0xff800000u;  // -inf
+            for (int x = 0; x < kN; x += 4) {
+              const float4 b = *reinterpret_cast<const float4*>(sm.bias[vst / 2] + x);
+              r[x] = __float_as_uint(fminf(__uint_as_float(r[x]), b.x));
+              r[x + 1] = __float_as_uint(fminf(__uint_as_float(r[x + 1]), b.y));
+              r[x + 2] = __float_as_uint(fminf(__uint_as_float(r[x + 2]), b.z));
+              r[x + 3] = __float_as_uint(fminf(__uint_as_float(r[x + 3]), b.w));
+            }
           }
         }
         float m8[8];
