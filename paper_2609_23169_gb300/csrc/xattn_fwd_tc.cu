@@ -13,8 +13,8 @@
 // Persistent CTAs, one per SM; items with the head fastest, so that CTAs in
 // flight read neighbouring 256-byte pieces of the same rows and share K and V
 // in L2.  Roles (384 threads, registers rebalanced with setmaxnreg):
-//   warp 0      TMA: the K and V tiles, one ring (K0 V0 K1 V1 ...); with a V
-//               tile, which of its keys count
+//   warp 0      TMA: the K and V tiles, one ring (K0 V0 K1 V1 ...); leaves
+//               beside a V tile which of its keys count
 //   warp 2      decodes the items (segment search, key range) into a ring, 32
 //               at once, one a lane; TMA: the query tiles, a ring of their own
 //   warp 1      TMEM owner and MMA issuer of tile 0, warp 3 of tile 1: per
@@ -33,9 +33,9 @@
 // Masked keys and the rows of other segments: S there becomes -inf, the
 // smaller of S and a bias of +-inf that warp 0 leaves in shared memory (the
 // min of NaN and -inf is -inf; selecting by bits of the mask took 900 to 1,300
-// cycles a block, this takes 400), and the softmax warps zero those rows of the
-// V tile before its products, so that no value they hold (NaN, infinities) is
-// multiplied.
+// cycles a block, this takes 400), and those rows of the V tile become zero
+// before its products (by warp 0 or the softmax warps), so that no value they
+// hold (NaN, infinities) is multiplied.
 // TMEM columns: S_0 / P_0 [0,128), S_1 / P_1 [128,256), O_0 [256,256+d), O_1
 // [384,384+d).
 // Every wait is bounded; on expiry the kernel records UT_ERR_TIMEOUT, drains
@@ -50,18 +50,26 @@ namespace ut {
 namespace {
 
 constexpr int kM = 128;  // rows of a query tile
-constexpr int kN = 128;  // keys of a block
-constexpr int kThreads = 384;
+// Registers of the two-tile form (384 threads)
 constexpr int kRegLaunch = 168, kRegCtl = 120, kRegSoftmax = 192;  // per thread; setmaxnreg split
 static_assert(kRegCtl + 2 * kRegSoftmax <= 3 * kRegLaunch, "the split must fit the launch's registers");
-constexpr uint32_t kChunkBytes = 128 * 128;  // 128 rows x 64 bf16
-constexpr int kItemSlots = 4, kItemReaders = 11;
+constexpr uint32_t kChunkBytes = kM * 128;  // 128 rows x 64 bf16
+constexpr int kItemSlots = 4;
+
+// Two tiles and blocks of 128 keys at d = 128, four and 64 at d = 64: the
+// tiles' S and O fill tensor memory either way.
+template <int D>
+struct Form {
+  static constexpr int kTiles = D == 128 ? 2 : 4;
+  static constexpr int kN = D == 128 ? 128 : 64;       // keys of a block
+  static constexpr int kThreads = 128 + 128 * kTiles;
+};
 
 struct Item {
   int32_t hk;      // kv head; -1: no more items
   int32_t blocks;  // key blocks of this item (0: write the empty result)
   int32_t tok0;    // first token of tile 0
-  int32_t ntok[2]; // tokens of the tiles (tile 1 may be empty)
+  int32_t ntok;    // tokens of all tiles (the last ones may be empty)
   int32_t key0;    // first key
   int32_t left;    // keys from key0 to the end of the segment
   int32_t split;
@@ -69,42 +77,45 @@ struct Item {
 
 template <int D>
 struct Smem {
-  static constexpr int kChunks = D / 64;
-  static constexpr uint32_t kTile = 128 * D * 2;
-  static constexpr int kQ = D == 128 ? 3 : 4;   // query tiles in flight
+  static constexpr int kChunks = D / 64, T = Form<D>::kTiles, kN = Form<D>::kN;
+  static constexpr uint32_t kTile = kM * D * 2, kKvTile = kN * D * 2, kKvChunk = kN * 128;
+  static constexpr int kQ = D == 128 ? 3 : 8;   // query tiles in flight
   static constexpr int kKv = D == 128 ? 4 : 8;  // K and V tiles in flight
   alignas(1024) uint8_t q[kQ][kTile];
-  alignas(1024) uint8_t kv[kKv][kTile];
-  float bias[kKv / 2][kN];        // of the keys of a V tile: 0 < bias = attend
+  alignas(1024) uint8_t kv[kKv][kKvTile];
+  float bias[kKv / 2][kN];                // of the keys of a V tile: 0 < bias = attend
   alignas(16) uint32_t keys[kKv / 2][4];  // and as bits
-  uint64_t q_full[kQ], q_empty[kQ], kv_full[kKv], kv_empty[kKv];
-  uint64_t s_full[2], p_most[2], p_full[2], o_full[2], o_empty[2], turn[2], mma_done;
+  uint64_t q_full[kQ], q_empty[kQ], kv_full[kKv], kv_empty[kKv], keys_full[kKv / 2], v_ready[kKv / 2];
+  uint64_t s_full[T], p_most[T], p_full[T], o_full[T], o_empty[T], turn[2], mma_done;
   uint64_t item_full[kItemSlots], item_empty[kItemSlots];
   Item item[kItemSlots];
   uint32_t tmem_base;
   int abort_flag;
 };
 
-// whether a block with `left` keys to the end of its segment needs no masking
-UT_DEV bool all_keys(const uint8_t* mask, int left) { return !mask && left >= kN; }
-
 struct Params {
   XattnParams x;
   uint32_t inv_g;    // ceil(2^16 / G): (r * inv_g) >> 16 = r / G for r < 128, G <= 64
   int tpt;           // tokens of a tile
-  int slots;         // item slots along the query rows (two tiles each)
+  int slots;         // item slots along the query rows
   int64_t n_items;   // slots * Hk * nsplit
   float scale_log2;
   bool keep_kv;      // K and V are read by several items: keep them in L2
 };
 
 template <int D>
-__global__ void __launch_bounds__(kThreads, 1)
+__global__ void __launch_bounds__(Form<D>::kThreads, 1)
     xattn_fwd_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k,
                         const __grid_constant__ CUtensorMap tm_v, const Params prm) {
   extern __shared__ __align__(1024) uint8_t smem_raw[];
   Smem<D>& sm = *reinterpret_cast<Smem<D>*>(smem_raw);
   using S = Smem<D>;
+  constexpr int T = S::T, kN = S::kN, kGroups = kN / 32;
+  // who zeroes rows of V: warp 0, two blocks behind its loads, where four blocks
+  // are in flight (four tiles); else the softmax warps
+  constexpr bool kZeroes = T == 4;
+  // TMEM columns of tile t: S and P at t kN, O at 256 + t D
+  static_assert(T * kN <= 256 && 256 + T * D <= 512, "tensor memory");
   const XattnParams& p = prm.x;
   const uint32_t warp = warp_id(), lane = lane_id();
   volatile int* abort_flag = &sm.abort_flag;
@@ -119,11 +130,15 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
     for (int s = 0; s < S::kKv; ++s) {
       mbar_init(&sm.kv_full[s], 1);
-      mbar_init(&sm.kv_empty[s], 2);  // both tiles' products
+      mbar_init(&sm.kv_empty[s], 2);  // both issuers' products
+      if (s % 2 == 0) {
+        mbar_init(&sm.keys_full[s / 2], 1);
+        mbar_init(&sm.v_ready[s / 2], 1);
+      }
     }
-    for (int w = 0; w < 2; ++w) {
+    for (int w = 0; w < 2; ++w) mbar_init(&sm.turn[w], 1);
+    for (int w = 0; w < T; ++w) {
       mbar_init(&sm.s_full[w], 1);
-      mbar_init(&sm.turn[w], 1);
       mbar_init(&sm.p_most[w], 4);
       mbar_init(&sm.p_full[w], 4);
       mbar_init(&sm.o_full[w], 1);
@@ -132,7 +147,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     mbar_init(&sm.mma_done, 2);
     for (int s = 0; s < kItemSlots; ++s) {
       mbar_init(&sm.item_full[s], 1);
-      mbar_init(&sm.item_empty[s], kItemReaders);
+      mbar_init(&sm.item_empty[s], 3 + 4 * T);  // warps 0, 1, 3 and the softmax warps
     }
     sm.abort_flag = 0;
     fence_barrier_init();
@@ -172,8 +187,11 @@ __global__ void __launch_bounds__(kThreads, 1)
     return it.hk >= 0;
   };
 
+  // whether a block with `left` keys to the end of its segment needs no masking
+  auto all_keys = [&](int left) { return !p.mask && left >= kN; };
+
   if (warp < 4) {
-    setmaxnreg_dec<kRegCtl>();
+    if constexpr (T == 2) setmaxnreg_dec<kRegCtl>();
     if (warp == 0) {
       // ------------------------------------------------------- K, V producer
       if (lane == 0) {
@@ -181,20 +199,46 @@ __global__ void __launch_bounds__(kThreads, 1)
         tma_prefetch_desc(&tm_v);
       }
       const uint64_t pol = prm.keep_kv ? policy_evict_last() : policy_evict_first();
-      uint32_t n = 0, at = 0;
+      uint32_t n = 0, at = 0, ready = 0;         // tiles asked for, V tiles made ready
+      uint32_t waiting = 0, older = 0, newer = 0;  // V tiles to be made ready (two at most), their keys
       bool ok = true;
       Item it;
+      auto make_ready = [&]() {  // the next V tile, once it is there
+        const uint32_t st = (2 * ready + 1) % S::kKv;
+        if (!(ok = wait(&sm.kv_full[st], (2 * ready / S::kKv) & 1))) return;
+        const uint32_t keys = waiting == 2 ? older : newer;
+        if (!__all_sync(0xffffffffu, keys == 15u)) {
+          const uint32_t base = smem_u32(sm.kv[st]);
+#pragma unroll
+          for (int g = 0; g < kGroups; ++g)
+            if (!((keys >> g) & 1u))
+              for (int x = 0; x < 8 * S::kChunks; ++x)
+                st_shared_v4(base + (x >> 3) * S::kKvChunk + (g * 32 + lane) * 128 + (((x + lane) & 7) << 4), 0, 0, 0, 0);
+          fence_proxy_async_smem();
+          __syncwarp();
+        }
+        if (lane == 0) mbar_arrive(&sm.v_ready[st / 2]);
+        ++ready;
+        --waiting;
+      };
       while (ok && next_item(n, it, ok)) {
+        auto keys_of = [&](int j) -> uint32_t {
+          if (all_keys(it.left - j * kN)) return 15u;
+          return lane_keys(p.mask, (int64_t)it.key0 + j * kN, it.left - j * kN, lane);
+        };
+        uint32_t next = it.blocks > 0 ? keys_of(0) : 0;
         for (int j = 0; j < it.blocks && ok; ++j) {
-          const bool plain = all_keys(p.mask, it.left - j * kN);
-          const uint32_t keys = plain ? 15u : lane_keys(p.mask, (int64_t)it.key0 + j * kN, it.left - j * kN, lane);
+          const bool plain = all_keys(it.left - j * kN);
+          const uint32_t keys = next;
+          if (j + 1 < it.blocks) next = keys_of(j + 1);  // a block ahead
 #pragma unroll 1
           for (int which = 0; which < 2; ++which, ++at) {
             const uint32_t st = at % S::kKv;
-            if (!(ok = wait(&sm.kv_empty[st], ((at / S::kKv) & 1) ^ 1))) break;
+            if (which && waiting == 2) make_ready();
+            if (!ok || !(ok = wait(&sm.kv_empty[st], ((at / S::kKv) & 1) ^ 1))) break;
             if (which && !plain) {
 #pragma unroll
-              for (int g = 0; g < 4; ++g) {
+              for (int g = 0; g < kGroups; ++g) {
                 const bool on = (keys >> g) & 1u;
                 const uint32_t word = __ballot_sync(0xffffffffu, on);
                 sm.bias[st / 2][g * 32 + lane] = on ? INFINITY : -INFINITY;
@@ -203,14 +247,19 @@ __global__ void __launch_bounds__(kThreads, 1)
               __syncwarp();
             }
             if (lane == 0) {
-              mbar_expect_tx(&sm.kv_full[st], S::kTile);
+              if (which) mbar_arrive(&sm.keys_full[st / 2]);
+              mbar_expect_tx(&sm.kv_full[st], S::kKvTile);
               const void* tm = which ? static_cast<const void*>(&tm_v) : static_cast<const void*>(&tm_k);
               for (int c = 0; c < S::kChunks; ++c)
-                tma_load_3d(sm.kv[st] + c * kChunkBytes, tm, &sm.kv_full[st], c * 64, it.hk, it.key0 + j * kN, pol);
+                tma_load_3d(sm.kv[st] + c * S::kKvChunk, tm, &sm.kv_full[st], c * 64, it.hk, it.key0 + j * kN, pol);
             }
             __syncwarp();
           }
+          older = newer;
+          newer = keys;
+          if constexpr (kZeroes) ++waiting;
         }
+        while (ok && waiting > 0) make_ready();  // nothing may be left waiting for the next item
       }
       if (lane == 0)
         for (uint32_t x = at > S::kKv ? at - S::kKv : 0; x < at; ++x) drain(&sm.kv_full[x % S::kKv], (x / S::kKv) & 1);
@@ -227,8 +276,8 @@ __global__ void __launch_bounds__(kThreads, 1)
         it.hk = -1;
         if (u < prm.n_items) {
           const int64_t at_q = u / p.Hk;
-          const Segment g = segment_of_slot(p.cu_q, p.B, p.nq, 2 * prm.tpt, at_q % prm.slots);
-          const int64_t t0 = g.tile * 2 * prm.tpt;
+          const Segment g = segment_of_slot(p.cu_q, p.B, p.nq, T * prm.tpt, at_q % prm.slots);
+          const int64_t t0 = g.tile * T * prm.tpt;
           int64_t k0, kn;
           segment_rows(p.cu_k, g.s, p.nk, k0, kn);
           const int64_t nblk = (kn + kN - 1) / kN, per = (nblk + p.nsplit - 1) / p.nsplit;
@@ -237,8 +286,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           if (t0 < g.n) it.hk = (int)(u % p.Hk);  // else an idle slot
           it.blocks = (int)(b1 - b0);
           it.tok0 = (int)(g.row + t0);
-          it.ntok[0] = (int)min((int64_t)prm.tpt, g.n - t0);
-          it.ntok[1] = (int)max((int64_t)0, min((int64_t)prm.tpt, g.n - t0 - prm.tpt));
+          it.ntok = (int)min((int64_t)T * prm.tpt, g.n - t0);
           it.key0 = (int)(k0 + b0 * kN);
           it.left = (int)(kn - b0 * kN);
         }
@@ -260,7 +308,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             mbar_arrive(&sm.item_full[s]);
           }
           const int hk = __shfl_sync(0xffffffffu, it.hk, who), tok0 = __shfl_sync(0xffffffffu, it.tok0, who);
-          const int tiles = __shfl_sync(0xffffffffu, it.blocks == 0 ? 0 : it.ntok[1] > 0 ? 2 : 1, who);
+          const int tiles = __shfl_sync(0xffffffffu, it.blocks == 0 ? 0 : (it.ntok + prm.tpt - 1) / prm.tpt, who);
           for (int w = 0; w < tiles; ++w, ++at) {
             const uint32_t st = at % S::kQ;
             if (!(ok = wait(&sm.q_empty[st], ((at / S::kQ) & 1) ^ 1))) break;
@@ -278,98 +326,110 @@ __global__ void __launch_bounds__(kThreads, 1)
       if (lane == 0)
         for (uint32_t x = at > S::kQ ? at - S::kQ : 0; x < at; ++x) drain(&sm.q_full[x % S::kQ], (x / S::kQ) & 1);
     } else if (warp == 1 || warp == 3) {
-      // ---------------------------------------- MMA issuer of tile 0 / tile 1
+      // ------------------- MMA issuer of the even tiles (warp 1) / the odd ones
       // Converged, and uniform to the compiler: every branch depends on votes
       // and on item fields made uniform.
       constexpr uint32_t idesc_s = idesc_bf16_f32(kM, kN, false, false);
       constexpr uint32_t idesc_o = idesc_bf16_f32(kM, D, false, true);
+      constexpr uint32_t kQStep = S::kTile >> 4, kKvStep = S::kKvTile >> 4;
       const uint32_t q_lo = desc_lo(smem_u32(sm.q[0]), 16), k_lo = desc_lo(smem_u32(sm.kv[0]), 16),
-                     v_lo = desc_lo(smem_u32(sm.kv[0]), kChunkBytes);
+                     v_lo = desc_lo(smem_u32(sm.kv[0]), S::kKvChunk);
       auto waitq = [&](uint64_t* bar, uint32_t parity) -> bool {
         return quick_wait(bar, parity, abort_flag, p.status, p.timeout_ns);
       };
-      const uint32_t w = warp >> 1, ts = w * 128, to = 256 + w * 128;
-      uint32_t n = 0, qat = w, kvat = 0, np = 0, no = 0, turns = 0;
+      const uint32_t w = warp >> 1;
+      uint32_t n = 0, qat = 0, kvat = 0, np = 0, no = 0, turns = 0;  // np, no: phases, a bit per tile
       bool ok = true;
       for (;; ++n) {
         const uint32_t slot = n % kItemSlots;
         if (!(ok = waitq(&sm.item_full[slot], (n / kItemSlots) & 1))) break;
         const int hk = (int)warp_uniform((uint32_t)sm.item[slot].hk);
         const int blocks = (int)warp_uniform((uint32_t)sm.item[slot].blocks);
-        const bool both = warp_uniform((uint32_t)sm.item[slot].ntok[1]) != 0;
+        const uint32_t tiles = warp_uniform((uint32_t)((sm.item[slot].ntok + prm.tpt - 1) / prm.tpt));
         if (hk < 0) break;
         __syncwarp();
         if (lane == 0) mbar_arrive(&sm.item_empty[slot]);
         if (blocks == 0) continue;
-        if (w == 1 && !both) {  // nothing for tile 1: pass the K and V tiles on
+        if (w >= tiles) {  // nothing for this warp's tiles: pass the K and V tiles on
 #pragma unroll 1
           for (int x = 0; x < 2 * blocks && ok; ++x, ++kvat) {
-            ok = waitq(&sm.kv_full[kvat % S::kKv], (kvat / S::kKv) & 1);
+            ok = waitq((x & 1) && kZeroes ? &sm.v_ready[kvat % S::kKv / 2] : &sm.kv_full[kvat % S::kKv],
+                       (kvat / S::kKv) & 1);
             if (ok && lane == 0) mbar_arrive(&sm.kv_empty[kvat % S::kKv]);
           }
           if (!ok) break;
-          ++qat;
+          qat += tiles;
           continue;
         }
-        const uint32_t qs = qat % S::kQ, q_a = q_lo + qs * (S::kTile >> 4);
-        if (!(ok = waitq(&sm.q_full[qs], (qat / S::kQ) & 1))) break;
+        const uint32_t q0 = (qat + w) % S::kQ, q0_phase = (qat + w) / S::kQ & 1;  // of the first of its tiles
         // step j: O += P V of block j - 1, S = Q K^T of block j
 #pragma unroll 1
         for (int j = 0; j <= blocks; ++j) {
           const uint32_t ks = kvat % S::kKv, vs = (kvat - 1) % S::kKv;
           if (j < blocks && !(ok = waitq(&sm.kv_full[ks], (kvat / S::kKv) & 1))) break;
-          if (j > 0) {
-            if (!(ok = waitq(&sm.kv_full[vs], ((kvat - 1) / S::kKv) & 1))) break;
+          if (j > 0 && !(ok = waitq(kZeroes ? &sm.v_ready[vs / 2] : &sm.kv_full[vs], ((kvat - 1) / S::kKv) & 1))) break;
+#pragma unroll 1
+          for (uint32_t t = w; t < tiles; t += 2) {
+            const uint32_t ts = t * kN, to = 256 + t * D, qs = T == 2 ? q0 : (qat + t) % S::kQ;
+            const bool last = T == 2 || t + 2 >= tiles;  // of this warp's tiles
+            if (j == 0 && !(ok = waitq(&sm.q_full[qs], T == 2 ? q0_phase : ((qat + t) / S::kQ) & 1))) break;
             if (j == 1) {
-              if (!(ok = waitq(&sm.o_empty[w], (no & 1) ^ 1))) break;
-              ++no;
+              if (!(ok = waitq(&sm.o_empty[t], ((no >> t) & 1) ^ 1))) break;
+              no ^= 1u << t;
             }
-            if (!(ok = waitq(&sm.p_most[w], np & 1))) break;
-          }
-          // an item's first S and its last P V wait for no turn: the tiles need
-          // not start or end together
-          const bool turn = both && j > 0 && j < blocks;
-          if (turn) {
-            if (!(ok = waitq(&sm.turn[w], (turns & 1) ^ (w ^ 1)))) break;
-            ++turns;
-          }
-          tc_fence_after();
-          if (j > 0) {
-            const uint32_t v_b = v_lo + vs * (S::kTile >> 4);
-            mma_tn96(to, ts, v_b, idesc_o, j > 1);
-            if (!(ok = waitq(&sm.p_full[w], np & 1))) break;
-            ++np;
+            if (j > 0 && !(ok = waitq(T == 2 ? &sm.p_most[t] : &sm.p_full[t], (np >> t) & 1))) break;
+            // an item's first S and its last P V wait for no turn: the tiles need
+            // not start or end together
+            const bool turn = T == 2 && tiles == 2 && j > 0 && j < blocks;
+            if (turn) {
+              if (!(ok = waitq(&sm.turn[w], (turns & 1) ^ (w ^ 1)))) break;
+              ++turns;
+            }
             tc_fence_after();
-            mma_tn32(to, ts + 48, v_b + 768, idesc_o);
-            mma_commit_w(&sm.kv_empty[vs]);
-            if (j == blocks) mma_commit_w(&sm.o_full[w]);
+            if (j > 0) {
+              const uint32_t v_b = v_lo + vs * kKvStep;
+              if constexpr (T == 2) {
+                mma_tn<96>(to, ts, v_b, idesc_o, j > 1);
+                if (!(ok = waitq(&sm.p_full[t], (np >> t) & 1))) break;
+                tc_fence_after();
+                mma_tn<32>(to, ts + 48, v_b + 768, idesc_o, 1);
+              } else {
+                mma_tn<64>(to, ts, v_b, idesc_o, j > 1);
+              }
+              np ^= 1u << t;
+              if (last) mma_commit_w(&sm.kv_empty[vs]);
+              if (j == blocks) mma_commit_w(&sm.o_full[t]);
+            }
+            if (j < blocks) {
+              mma_nt<D>(ts, q_lo + qs * kQStep, k_lo + ks * kKvStep, idesc_s);
+              mma_commit_w(&sm.s_full[t]);
+              if (last) mma_commit_w(&sm.kv_empty[ks]);
+              if (j == blocks - 1) mma_commit_w(&sm.q_empty[qs]);
+            }
+            if (turn) {
+              __syncwarp();
+              if (lane == 0) mbar_arrive(&sm.turn[w ^ 1]);
+            }
+            if constexpr (T == 2) break;
           }
-          if (j < blocks) {
-            mma_nt<D>(ts, q_a, k_lo + ks * (S::kTile >> 4), idesc_s);
-            mma_commit_w(&sm.s_full[w]);
-            mma_commit_w(&sm.kv_empty[ks]);
-            if (j == blocks - 1) mma_commit_w(&sm.q_empty[qs]);
-            kvat += 2;
-          }
-          if (turn) {
-            __syncwarp();
-            if (lane == 0) mbar_arrive(&sm.turn[w ^ 1]);
-          }
+          if (!ok) break;
+          if (j < blocks) kvat += 2;
         }
         if (!ok) break;
-        qat += both ? 2 : 1;
+        qat += tiles;
       }
       mma_commit_w(&sm.mma_done);  // every MMA has completed before TMEM is freed
       drain(&sm.mma_done, 0);
     }
   } else {
     // ----------------------------------------------------------------- softmax
-    setmaxnreg_inc<kRegSoftmax>();
-    const int w = warp < 8 ? 0 : 1;
+    if constexpr (T == 2) setmaxnreg_inc<kRegSoftmax>();
+    const int w = (int)(warp >> 2) - 1;  // its tile
     const uint32_t quarter = warp & 3, lane_base = (quarter * 32) << 16;
-    const uint32_t ts = lane_base + w * 128, to = lane_base + 256 + w * 128;
+    const uint32_t ts = lane_base + w * kN, to = lane_base + 256 + w * D;
     auto token_of = [&](uint32_t r) -> uint32_t { return (r * prm.inv_g) >> 16; };  // r / G
     const uint64_t c2 = pack_f32x2(prm.scale_log2, prm.scale_log2);
+    const uint32_t row = quarter * 32 + lane, rt = token_of(row);  // this thread's row and its token
     uint32_t n = 0, ns = 0, no = 0, kvat = 0;
     bool ok = true;
     for (;; ++n) {
@@ -378,34 +438,35 @@ __global__ void __launch_bounds__(kThreads, 1)
       if (!(ok = wait(&sm.item_full[slot], (n / kItemSlots) & 1))) break;
       const volatile Item* it = &sm.item[slot];
       if (it->hk < 0) break;
-      const int blocks = it->ntok[w] > 0 ? it->blocks : 0;
+      const int ntok = min(prm.tpt, it->ntok - w * prm.tpt);  // of this tile
+      const int blocks = ntok > 0 ? it->blocks : 0;
       float m = -1e30f, l = 0.f;
       for (int j = 0; j < blocks; ++j) {
-        const bool plain = all_keys(p.mask, it->left - j * kN);
+        const bool plain = all_keys(it->left - j * kN);
         const uint32_t vat = kvat + 2 * j + 1, vst = vat % S::kKv;
         if (!(ok = wait(&sm.s_full[w], ns & 1))) break;
         ++ns;
         tc_fence_after();
         uint32_t r[kN];
 #pragma unroll
-        for (int g = 0; g < 4; ++g) tmem_ld32(ts + g * 32, *reinterpret_cast<uint32_t(*)[32]>(&r[g * 32]));
+        for (int g = 0; g < kGroups; ++g) tmem_ld32(ts + g * 32, *reinterpret_cast<uint32_t(*)[32]>(&r[g * 32]));
         if (!plain) {
-          // the V tile and its keys; its rows that must not enter the product
-          // become zero (thread = row; the other tile's warps may write the same)
-          ok = wait(&sm.kv_full[vst], (vat / S::kKv) & 1);
-          if (ok && !((sm.keys[vst / 2][quarter] >> lane) & 1u)) {
-            const uint32_t v_row = smem_u32(sm.kv[vst]) + (quarter * 32 + lane) * 128;
+          ok = wait(kZeroes ? &sm.keys_full[vst / 2] : &sm.kv_full[vst], (vat / S::kKv) & 1);
+          if constexpr (!kZeroes) {  // thread = row; the other tile's warps may write the same zeros
+            if (ok && !((sm.keys[vst / 2][quarter] >> lane) & 1u)) {
+              const uint32_t v_row = smem_u32(sm.kv[vst]) + (quarter * 32 + lane) * 128;
 #pragma unroll
-            for (int x = 0; x < 8 * S::kChunks; ++x)
-              st_shared_v4(v_row + (x >> 3) * kChunkBytes + (((x + lane) & 7) << 4), 0, 0, 0, 0);
+              for (int x = 0; x < 8 * S::kChunks; ++x)
+                st_shared_v4(v_row + (x >> 3) * S::kKvChunk + (((x + lane) & 7) << 4), 0, 0, 0, 0);
+            }
+            fence_proxy_async_smem();
           }
-          fence_proxy_async_smem();
         }
         tmem_wait_ld();
         if (!ok) break;
         if (!plain) {
           const uint4 word = *reinterpret_cast<const uint4*>(sm.keys[vst / 2]);
-          if ((word.x & word.y & word.z & word.w) != 0xffffffffu) {
+          if ((word.x & word.y & (kGroups == 4 ? word.z & word.w : ~0u)) != 0xffffffffu) {
 #pragma unroll
             for (int x = 0; x < kN; x += 4) {
               const float4 b = *reinterpret_cast<const float4*>(sm.bias[vst / 2] + x);
@@ -446,7 +507,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         const uint64_t m2 = pack_f32x2(-m, -m);
         uint64_t sum[4] = {0, 0, 0, 0};
 #pragma unroll
-        for (int g = 0; g < 4; ++g) {
+        for (int g = 0; g < kGroups; ++g) {
           uint32_t pk[16];
 #pragma unroll
           for (int x = 0; x < 32; x += 2) {
@@ -458,7 +519,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             pk[x / 2] = pack_bf16x2(p0, p1);
           }
           tmem_st16(ts + g * 16, pk);
-          if (g == 2) {  // three quarters of P: its product may begin
+          if (T == 2 && g == 2) {  // three quarters of P: its product may begin
             tmem_wait_st();
             tc_fence_before();
             __syncwarp();
@@ -479,13 +540,12 @@ __global__ void __launch_bounds__(kThreads, 1)
         ++no;
         tc_fence_after();
       }
-      const uint32_t row = quarter * 32 + lane, rt = token_of(row);  // this thread's row and its token
-      const int hk = it->hk, ntok = it->ntok[w], split = it->split;
+      const int hk = it->hk, split = it->split;
       const int64_t tok0 = (int64_t)it->tok0 + w * prm.tpt;
       kvat += 2 * it->blocks;
       __syncwarp();
       if (lane == 0) mbar_arrive(&sm.item_empty[slot]);
-      if (ntok == 0) continue;
+      if (ntok <= 0) continue;
       const int h = hk * p.G + (int)(row - rt * p.G);
       const bool row_ok = (int)rt < ntok;
       if (p.nsplit > 1) {
@@ -519,12 +579,11 @@ __global__ void __launch_bounds__(kThreads, 1)
       const float f = l > 0.f ? 1.f / l : (l == 0.f ? 0.f : l);
       const uint32_t c = lane & 3;
       __nv_bfloat16* out[4];
+      __nv_bfloat16* const base = static_cast<__nv_bfloat16*>(p.o) + tok0 * p.os + (int64_t)hk * p.G * D + c * 8;
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const uint32_t y = quarter * 32 + (lane & ~3u) + i, yt = token_of(y);
-        out[i] = (int)yt < ntok ? static_cast<__nv_bfloat16*>(p.o) + (tok0 + yt) * p.os +
-                                      ((int64_t)hk * p.G + (y - yt * p.G)) * D + c * 8
-                                : nullptr;
+        out[i] = (int)yt < ntok ? base + (int64_t)yt * p.os + (y - yt * p.G) * D : nullptr;
       }
 #pragma unroll 1
       for (int g = 0; g < D / 32; ++g) {
@@ -570,25 +629,31 @@ cudaError_t launch_d(const Params& prm, const CUtensorMap* tm, cudaStream_t s) {
   if (e != cudaSuccess) return e;
   // the setmaxnreg split assumes exactly kRegLaunch registers per thread at
   // launch: with fewer, the increases would wait for registers that never come
-  cudaFuncAttributes fa;
-  e = cudaFuncGetAttributes(&fa, xattn_fwd_tc_kernel<D>);
-  if (e != cudaSuccess) return e;
-  if (fa.numRegs != kRegLaunch) return cudaErrorInvalidConfiguration;
+  if (Form<D>::kTiles == 2) {
+    cudaFuncAttributes fa;
+    e = cudaFuncGetAttributes(&fa, xattn_fwd_tc_kernel<D>);
+    if (e != cudaSuccess) return e;
+    if (fa.numRegs != kRegLaunch) return cudaErrorInvalidConfiguration;
+  }
   const int grid = (int)(prm.n_items < prm.x.sms ? prm.n_items : prm.x.sms);
-  xattn_fwd_tc_kernel<D><<<grid, kThreads, smem, s>>>(tm[0], tm[1], tm[2], prm);
+  xattn_fwd_tc_kernel<D><<<grid, Form<D>::kThreads, smem, s>>>(tm[0], tm[1], tm[2], prm);
   return cudaGetLastError();
 }
 
 }  // namespace
 
-int64_t xattn_fwd_tc_items(const XattnParams& p) { return segment_slots(p.nq, p.B, 2 * (kM / p.G)) * p.Hk; }
+static int tiles_of_item(int d) { return d == 64 ? Form<64>::kTiles : Form<128>::kTiles; }
+
+int64_t xattn_fwd_tc_items(const XattnParams& p) {
+  return segment_slots(p.nq, p.B, tiles_of_item(p.d) * (kM / p.G)) * p.Hk;
+}
 
 cudaError_t launch_xattn_fwd_tc(const XattnParams& p, cudaStream_t s) {
   Params prm{};
   prm.x = p;
   prm.inv_g = (65536u + p.G - 1) / p.G;
   prm.tpt = kM / p.G;
-  prm.slots = (int)segment_slots(p.nq, p.B, 2 * prm.tpt);
+  prm.slots = (int)segment_slots(p.nq, p.B, tiles_of_item(p.d) * prm.tpt);
   prm.n_items = (int64_t)prm.slots * p.Hk * p.nsplit;
   prm.scale_log2 = p.scale * kLog2e;
   prm.keep_kv = prm.slots > p.B;
@@ -597,6 +662,7 @@ cudaError_t launch_xattn_fwd_tc(const XattnParams& p, cudaStream_t s) {
   const void* k = p.nk > 0 ? p.k : p.q;
   const void* v = p.nk > 0 ? p.v : p.q;
   const int64_t ks = p.nk > 0 ? p.ks : p.qs, vs = p.nk > 0 ? p.vs : p.qs, nk = p.nk > 0 ? p.nk : 1;
+  const int kN = p.d == 64 ? Form<64>::kN : Form<128>::kN;
   if (!encode_tmap_heads_bf16(&tm[0], p.q, p.d, p.H, p.nq, p.qs * 2, p.G, prm.tpt) ||
       !encode_tmap_heads_bf16(&tm[1], k, p.d, p.Hk, nk, ks * 2, 1, kN) ||
       !encode_tmap_heads_bf16(&tm[2], v, p.d, p.Hk, nk, vs * 2, 1, kN))

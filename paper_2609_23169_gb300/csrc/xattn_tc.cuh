@@ -52,21 +52,27 @@ UT_DEV void mma_nt(uint32_t d, uint32_t a_lo, uint32_t b_lo, uint32_t idesc) {
   "add.u32 x, %1, " acol ";\n\tadd.u32 y, %2, " boff ";\n\t"           \
   "mov.b64 b, {y, %5};\n\t"                                            \
   "@e tcgen05.mma.cta_group::1.kind::f16 [%0], [x], b, %3, " acc ";\n\t"
-// d (+)= A B over 96 / 32 rows of B: A in TMEM (bf16 pairs, 8 columns a step), B
+// d (+)= A B over N rows of B: A in TMEM (bf16 pairs, 8 columns a step), B
 // row-major (MN-major operand, 16 rows of 128 bytes a step)
 #define UT_TS_HEAD                                                  \
   "{\n\t.reg .pred e, p, t;\n\t.reg .b64 b;\n\t.reg .b32 x, y;\n\t" \
   "setp.ne.b32 p, %4, 0;\n\tsetp.eq.b32 t, 0, 0;\n\telect.sync _|e, 0xffffffff;\n\t"
-UT_DEV void mma_tn96(uint32_t d, uint32_t a, uint32_t b_lo, uint32_t idesc, uint32_t accumulate) {
-  asm volatile(UT_TS_HEAD UT_TS_STEP("0", "0", "p") UT_TS_STEP("8", "128", "t") UT_TS_STEP("16", "256", "t")
-                   UT_TS_STEP("24", "384", "t") UT_TS_STEP("32", "512", "t") UT_TS_STEP("40", "640", "t") "}" ::"r"(d),
-               "r"(a), "r"(b_lo), "r"(idesc), "r"(accumulate), "r"(kDescHi)
-               : "memory");
-}
-UT_DEV void mma_tn32(uint32_t d, uint32_t a, uint32_t b_lo, uint32_t idesc) {
-  asm volatile(UT_TS_HEAD UT_TS_STEP("0", "0", "p") UT_TS_STEP("8", "128", "t") "}" ::"r"(d), "r"(a), "r"(b_lo),
-               "r"(idesc), "r"(1u), "r"(kDescHi)
-               : "memory");
+template <int N>
+UT_DEV void mma_tn(uint32_t d, uint32_t a, uint32_t b_lo, uint32_t idesc, uint32_t accumulate) {
+  if constexpr (N == 96)
+    asm volatile(UT_TS_HEAD UT_TS_STEP("0", "0", "p") UT_TS_STEP("8", "128", "t") UT_TS_STEP("16", "256", "t")
+                     UT_TS_STEP("24", "384", "t") UT_TS_STEP("32", "512", "t") UT_TS_STEP("40", "640", "t") "}" ::"r"(d),
+                 "r"(a), "r"(b_lo), "r"(idesc), "r"(accumulate), "r"(kDescHi)
+                 : "memory");
+  else if constexpr (N == 64)
+    asm volatile(UT_TS_HEAD UT_TS_STEP("0", "0", "p") UT_TS_STEP("8", "128", "t") UT_TS_STEP("16", "256", "t")
+                     UT_TS_STEP("24", "384", "t") "}" ::"r"(d),
+                 "r"(a), "r"(b_lo), "r"(idesc), "r"(accumulate), "r"(kDescHi)
+                 : "memory");
+  else
+    asm volatile(UT_TS_HEAD UT_TS_STEP("0", "0", "p") UT_TS_STEP("8", "128", "t") "}" ::"r"(d), "r"(a), "r"(b_lo),
+                 "r"(idesc), "r"(accumulate), "r"(kDescHi)
+                 : "memory");
 }
 
 // d (+)= A B over 128 rows of B, A in TMEM as two halves of 64 columns, each in

@@ -103,10 +103,11 @@ def test_image_prefix(u):
 
 def test_expired_waits_report_timeout_and_context_survives(u, monkeypatch):
     """With the limit at 0 the waits run out: the kernels say so in the status word, end, and the next calls work.
-    (The norm's need 400,000 rows for that: a load of a few rows lands within the wait's first try.)"""
+    (The sizes are such that some warps wait for 100 us and more, or many times: the first try of a wait may itself take
+    microseconds, so that a short one is met within it.)"""
     g = torch.Generator().manual_seed(6)
-    q, do = (torch.randn(700, 4, 128, generator=g).bfloat16().cuda() for _ in range(2))
-    k, v = (torch.randn(300, 2, 128, generator=g).bfloat16().cuda() for _ in range(2))
+    q, do = (torch.randn(20480, 4, 128, generator=g).bfloat16().cuda() for _ in range(2))
+    k, v = (torch.randn(16384, 2, 128, generator=g).bfloat16().cuda() for _ in range(2))
     x, dy = (torch.randn(400000, 320, generator=g).bfloat16().cuda() for _ in range(2))
     want = u.ut_xattn_fwd(q, k, v)
     want_g = u.ut_xattn_bwd(q, k, v, *want, do)
