@@ -10,13 +10,13 @@
 // turns on the tensor cores, so that one tile's products run while the other
 // tile's softmax does, and share every K and V tile in shared memory.
 //
-// Persistent CTAs, one per SM; items with the head fastest, so that CTAs in
-// flight read neighbouring 256-byte pieces of the same rows and share K and V
-// in L2.  Roles (384 threads, registers rebalanced with setmaxnreg):
+// One CTA per SM, which takes item after item (NextItem); items with the head
+// fastest, so that CTAs in flight read neighbouring 256-byte pieces of the same
+// rows and share K and V in L2.  Roles (384 threads, registers rebalanced with setmaxnreg):
 //   warp 0      TMA: the K and V tiles, one ring (K0 V0 K1 V1 ...); leaves
 //               beside a V tile which of its keys count
-//   warp 2      decodes the items (segment search, key range) into a ring, 32
-//               at once, one a lane; TMA: the query tiles, a ring of their own
+//   warp 2      asks for the items and decodes them (segment search, key
+//               range) into a ring; TMA: the query tiles, a ring of their own
 //   warp 1      TMEM owner and MMA issuer of tile 0, warp 3 of tile 1: per
 //               block S = Q K^T, then, as P is written over S in TMEM, O += P V
 //               (of the first 96 keys while the last 32 are being written).
@@ -54,7 +54,7 @@ constexpr int kM = 128;  // rows of a query tile
 constexpr int kRegLaunch = 168, kRegCtl = 120, kRegSoftmax = 192;  // per thread; setmaxnreg split
 static_assert(kRegCtl + 2 * kRegSoftmax <= 3 * kRegLaunch, "the split must fit the launch's registers");
 constexpr uint32_t kChunkBytes = kM * 128;  // 128 rows x 64 bf16
-constexpr int kItemSlots = 4;
+constexpr int kItemSlots = 3;  // no more are taken ahead: other CTAs may be idle
 
 // Two tiles and blocks of 128 keys at d = 128, four and 64 at d = 64: the
 // tiles' S and O fill tensor memory either way.
@@ -89,6 +89,7 @@ struct Smem {
   uint64_t s_full[T], p_most[T], p_full[T], o_full[T], o_empty[T], turn[2], mma_done;
   uint64_t item_full[kItemSlots], item_empty[kItemSlots];
   Item item[kItemSlots];
+  NextItem next;
   uint32_t tmem_base;
   int abort_flag;
 };
@@ -149,6 +150,7 @@ __global__ void __launch_bounds__(Form<D>::kThreads, 1)
       mbar_init(&sm.item_full[s], 1);
       mbar_init(&sm.item_empty[s], 3 + 4 * T);  // warps 0, 1, 3 and the softmax warps
     }
+    next_item_init(sm.next);
     sm.abort_flag = 0;
     fence_barrier_init();
   }
@@ -268,61 +270,62 @@ __global__ void __launch_bounds__(Form<D>::kThreads, 1)
       if (lane == 0) tma_prefetch_desc(&tm_q);
       const uint64_t pol = policy_evict_first();
       const uint32_t bytes = (uint32_t)prm.tpt * p.G * 128 * S::kChunks;
-      uint32_t n = 0, at = 0;
-      bool ok = true, end = false;
-      for (int64_t u0 = blockIdx.x; ok && !end; u0 += (int64_t)32 * gridDim.x) {
-        const int64_t u = u0 + (int64_t)lane * gridDim.x;
+      uint32_t n = 0, at = 0, asked = 0;
+      bool ok = true;
+      for (int u = (int)blockIdx.x; ok;) {
+        if (u >= 0) {
+          if (lane == 0) next_item_ask(sm.next, asked);
+          __syncwarp();
+          ++asked;
+        }
         Item it{};
         it.hk = -1;
-        if (u < prm.n_items) {
-          const int64_t at_q = u / p.Hk;
-          const Segment g = segment_of_slot(p.cu_q, p.B, p.nq, T * prm.tpt, at_q % prm.slots);
+        if (u >= 0) {
+          const int at_q = u / p.Hk, split = at_q / prm.slots;
+          const Segment g = warp_segment_of_slot(p.cu_q, p.B, p.nq, T * prm.tpt, at_q - split * prm.slots);
           const int64_t t0 = g.tile * T * prm.tpt;
           int64_t k0, kn;
           segment_rows(p.cu_k, g.s, p.nk, k0, kn);
-          const int64_t nblk = (kn + kN - 1) / kN, per = (nblk + p.nsplit - 1) / p.nsplit;
-          it.split = (int)(at_q / prm.slots);
-          const int64_t b0 = min(nblk, per * it.split), b1 = min(nblk, b0 + per);
-          if (t0 < g.n) it.hk = (int)(u % p.Hk);  // else an idle slot
-          it.blocks = (int)(b1 - b0);
+          const int nblk = (int)((kn + kN - 1) / kN), per = (nblk + p.nsplit - 1) / p.nsplit;
+          const int b0 = min(nblk, per * split), b1 = min(nblk, b0 + per);
+          it.split = split;
+          if (t0 < g.n) it.hk = u - at_q * p.Hk;  // else an idle slot
+          it.blocks = b1 - b0;
           it.tok0 = (int)(g.row + t0);
           it.ntok = (int)min((int64_t)T * prm.tpt, g.n - t0);
-          it.key0 = (int)(k0 + b0 * kN);
-          it.left = (int)(kn - b0 * kN);
+          it.key0 = (int)(k0 + (int64_t)b0 * kN);
+          it.left = (int)(kn - (int64_t)b0 * kN);
         }
-        end = u0 + (int64_t)32 * gridDim.x >= prm.n_items;
-        uint32_t have = __ballot_sync(0xffffffffu, it.hk >= 0);
-        for (; have | (uint32_t)end; have &= have - 1, ++n) {
+        if (u < 0 || it.hk >= 0) {
           const uint32_t s = n % kItemSlots;
           if (!(ok = wait(&sm.item_empty[s], ((n / kItemSlots) & 1) ^ 1))) break;
-          if (have == 0) {  // no more items
-            if (lane == 0) {
-              sm.item[s].hk = -1;
-              mbar_arrive(&sm.item_full[s]);
-            }
-            break;
-          }
-          const int who = __ffs(have) - 1;
-          if ((int)lane == who) {
+          if (lane == 0) {
             sm.item[s] = it;
             mbar_arrive(&sm.item_full[s]);
           }
-          const int hk = __shfl_sync(0xffffffffu, it.hk, who), tok0 = __shfl_sync(0xffffffffu, it.tok0, who);
-          const int tiles = __shfl_sync(0xffffffffu, it.blocks == 0 ? 0 : (it.ntok + prm.tpt - 1) / prm.tpt, who);
+          __syncwarp();
+          ++n;
+          if (u < 0) break;  // no more items
+          const int tiles = it.blocks == 0 ? 0 : (it.ntok + prm.tpt - 1) / prm.tpt;
           for (int w = 0; w < tiles; ++w, ++at) {
             const uint32_t st = at % S::kQ;
             if (!(ok = wait(&sm.q_empty[st], ((at / S::kQ) & 1) ^ 1))) break;
             if (lane == 0) {
               mbar_expect_tx(&sm.q_full[st], bytes);
               for (int c = 0; c < S::kChunks; ++c)
-                tma_load_3d(sm.q[st] + c * kChunkBytes, &tm_q, &sm.q_full[st], c * 64, hk * p.G, tok0 + w * prm.tpt,
-                            pol);
+                tma_load_3d(sm.q[st] + c * kChunkBytes, &tm_q, &sm.q_full[st], c * 64, it.hk * p.G,
+                            it.tok0 + w * prm.tpt, pol);
             }
             __syncwarp();
           }
           if (!ok) break;
         }
+        if (!(ok = wait(&sm.next.full[(asked - 1) & 1], ((asked - 1) >> 1) & 1))) break;
+        u = (int)warp_uniform((uint32_t)next_item_answer(sm.next, asked - 1));
+        fence_proxy_async_smem();  // the answer is read before its place is used again
+        __syncwarp();
       }
+      if (lane == 0 && asked > 0) drain(&sm.next.full[(asked - 1) & 1], ((asked - 1) >> 1) & 1);
       if (lane == 0)
         for (uint32_t x = at > S::kQ ? at - S::kQ : 0; x < at; ++x) drain(&sm.q_full[x % S::kQ], (x / S::kQ) & 1);
     } else if (warp == 1 || warp == 3) {
@@ -635,8 +638,7 @@ cudaError_t launch_d(const Params& prm, const CUtensorMap* tm, cudaStream_t s) {
     if (e != cudaSuccess) return e;
     if (fa.numRegs != kRegLaunch) return cudaErrorInvalidConfiguration;
   }
-  const int grid = (int)(prm.n_items < prm.x.sms ? prm.n_items : prm.x.sms);
-  xattn_fwd_tc_kernel<D><<<grid, Form<D>::kThreads, smem, s>>>(tm[0], tm[1], tm[2], prm);
+  xattn_fwd_tc_kernel<D><<<(unsigned)prm.n_items, Form<D>::kThreads, smem, s>>>(tm[0], tm[1], tm[2], prm);
   return cudaGetLastError();
 }
 

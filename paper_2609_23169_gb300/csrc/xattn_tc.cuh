@@ -103,6 +103,43 @@ UT_DEV bool quick_wait(uint64_t* bar, uint32_t parity, volatile int* abort_flag,
   return warp_uniform(spin_wait(bar, parity, abort_flag, status, timeout_ns));
 }
 
+// ------------------------------------------------------------- next item
+// The grid has a block for each item; the blocks that run take the items of
+// those that have not started, one after another, until none is left (a block
+// is asked for an item ahead).  So segments of unequal lengths fill the SMs
+// evenly: with a fixed share of the items each, the longest of 152 shares was
+// 1.42 times the mean for 13 ragged images.
+struct NextItem {
+  alignas(16) uint8_t answer[2][16];
+  uint64_t full[2];
+};
+UT_DEV void next_item_init(NextItem& x) {
+  mbar_init(&x.full[0], 1);
+  mbar_init(&x.full[1], 1);
+}
+UT_DEV void next_item_ask(NextItem& x, uint32_t i) {  // request i, by one thread
+  mbar_expect_tx(&x.full[i & 1], 16);
+  asm volatile("clusterlaunchcontrol.try_cancel.async.shared::cta.mbarrier::complete_tx::bytes.b128 [%0], [%1];" ::"r"(
+                   smem_u32(x.answer[i & 1])),
+               "r"(smem_u32(&x.full[i & 1]))
+               : "memory");
+}
+// the answer to request i (its barrier waited for): an item, or -1
+UT_DEV int next_item_answer(NextItem& x, uint32_t i) {
+  int item;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t.reg .b128 h;\n\t.reg .b32 c, y, z, w;\n\t"
+      "ld.shared.b128 h, [%1];\n\t"
+      "clusterlaunchcontrol.query_cancel.is_canceled.pred.b128 p, h;\n\t"
+      "mov.b32 %0, -1;\n\t"
+      "@p clusterlaunchcontrol.query_cancel.get_first_ctaid.v4.b32.b128 {c, y, z, w}, h;\n\t"
+      "@p mov.b32 %0, c;\n\t}"
+      : "=r"(item)
+      : "r"(smem_u32(x.answer[i & 1]))
+      : "memory");
+  return item;
+}
+
 // This lane's four keys of a block (lane + 32 g): bit g set where the key
 // exists and is not masked.
 UT_DEV uint32_t lane_keys(const uint8_t* mask, int64_t key, int left, uint32_t lane) {
