@@ -80,6 +80,13 @@ UT_DEV void zero_tail(uint32_t base, int chunks, int first, uint32_t lane) {
 //               another each took 2,500 cycles, more than a block)
 //   warp 3      zeroes the masked keys of K, says when a block has all it needs
 //   warps 12-15 dQ out
+// kFew, for segments of 128 keys on average or fewer: dS is rounded to bf16
+// for its product, as dQ is at the end, together 1.42 times the error of
+// rounding dQ alone; with few keys the error of D = dO . O, whose O was rounded
+// too, adds to that in dQ and dK (1.66 times at 10 keys, 1.50 at 62, 1.45 from
+// 110).  So where a segment has one block of keys D is taken anew, as the sum of
+// P dP in fp32, and left for the next kernel.  A form of its own because the
+// code costs the other 4%.
 // The issuing warp's instructions are fetched anew every block (the
 // elementwise code lies between), and it bounded the first form: 700 of them a
 // block, 3,900 cycles.  So it counts stages instead of dividing, follows one
@@ -109,13 +116,15 @@ struct DqSmem {
   uint64_t q_full[kQ], q_empty[kQ], do_full[kQ], do_empty[kQ];
   uint64_t k_full[kK], ready[kK], k_empty[kK], v_full[kV], dp_full[kV];  // dP done: V is free
   uint64_t s_full[2], ds_full[2], dq_full, dq_empty, mma_done;
+  uint64_t pair_full[4];    // kFew: the two warps of 32 rows have their parts of D
+  float pair[2][2][kT];
   uint64_t item_full[kDqSlots], item_empty[kDqSlots];
   DqItem item[kDqSlots];
   uint32_t tmem_base;
   int abort_flag;
 };
 
-template <int D>
+template <int D, bool kFew>
 __global__ void __launch_bounds__(kDqThreads, 1)
     xattn_dq_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k,
                     const __grid_constant__ CUtensorMap tm_v, const __grid_constant__ CUtensorMap tm_do,
@@ -151,6 +160,7 @@ __global__ void __launch_bounds__(kDqThreads, 1)
     mbar_init(&sm.ds_full[0], 8);
     mbar_init(&sm.ds_full[1], 8);
     mbar_init(&sm.dq_empty, 4);
+    for (int s = 0; s < 4; ++s) mbar_init(&sm.pair_full[s], 2);
     for (int s = 0; s < kDqSlots; ++s) {
       mbar_init(&sm.item_full[s], 1);
       mbar_init(&sm.item_empty[s], kDqReaders);
@@ -293,18 +303,20 @@ __global__ void __launch_bounds__(kDqThreads, 1)
         for (int j = 0; j < it.blocks; ++j, ++at) {
           const uint32_t st = at % S::kK;
           const uint32_t keys = lane_keys(p.mask, (int64_t)it.key0 + j * kT, it.keys - j * kT, lane);
-          if (!(ok = wait(&sm.k_full[st], (at / S::kK) & 1))) break;
-          if (__any_sync(0xffffffffu, keys != 15u)) {
-            const uint32_t base = smem_u32(sm.k[st]);
+          auto zero_keys = [&](uint32_t base) {
             for (int g = 0; g < 4; ++g)
               if (!((keys >> g) & 1u))
                 for (int x = 0; x < 8 * S::kC; ++x)
                   st_shared_v4(base + (x >> 3) * kChunkB + (lane + 32 * g) * 128 + (((x + lane) & 7) << 4), 0, 0, 0, 0);
             fence_proxy_async_smem();
             __syncwarp();
-          }
+          };
+          const bool some = __any_sync(0xffffffffu, keys != 15u);
+          if (!(ok = wait(&sm.k_full[st], (at / S::kK) & 1))) break;
+          if (some) zero_keys(smem_u32(sm.k[st]));
           if (j == 0 && !(ok = wait(&sm.q_full[(n - 1) % S::kQ], ((n - 1) / S::kQ) & 1))) break;
           if (!(ok = wait(&sm.v_full[at % S::kV], (at / S::kV) & 1))) break;
+          if (kFew && some) zero_keys(smem_u32(sm.v[at % S::kV]));  // so that dP = 0, whatever V holds there
           if (lane == 0) mbar_arrive(&sm.ready[st]);
         }
     } else if (warp == 1) {
@@ -397,7 +409,7 @@ __global__ void __launch_bounds__(kDqThreads, 1)
     const uint32_t quarter = warp & 3, half = (warp - 4) >> 2, lane_base = (quarter * 32) << 16;
     const int row = (int)(quarter * 32 + lane), rt = (int)(((uint32_t)row * prm.inv_g) >> 16), rg = row - rt * p.G;
     const uint64_t c2 = pack_f32x2(prm.scale_log2, prm.scale_log2);
-    uint32_t n = 0, at = 0;
+    uint32_t n = 0, at = 0, pairs = 0;
     bool ok = true;
     DqItem it, nx;
     // LSE and D of this row, loaded an item ahead; +inf and 0 where there is none
@@ -416,7 +428,8 @@ __global__ void __launch_bounds__(kDqThreads, 1)
     while (ok && more) {
       it = nx;
       // a row without keys has all its columns masked; one that does not exist P = 0
-      const uint64_t l2 = pack_f32x2(-nl * kLog2e, -nl * kLog2e), d2 = pack_f32x2(-nd, -nd);
+      const uint64_t l2 = pack_f32x2(-nl * kLog2e, -nl * kLog2e);
+      uint64_t d2 = pack_f32x2(-nd, -nd);
       more = next_item(n, nx, ok);
       if (!ok) break;
       row_load(nx, nl, nd);
@@ -438,6 +451,30 @@ __global__ void __launch_bounds__(kDqThreads, 1)
         }
         if (!(ok = wait(&sm.dp_full[at % S::kV], (at / S::kV) & 1))) break;
         tc_fence_after();
+        if (kFew && it.blocks == 1) {
+          uint64_t sum[2] = {0, 0};
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            uint32_t v[32];
+            tmem_ld32(lane_base + 128 + half * 64 + h * 32, v);
+            tmem_wait_ld();
+#pragma unroll
+            for (int x = 0; x < 32; x += 2)
+              sum[(x >> 1) & 1] = fma_f32x2(pack_u32x2(r[h * 32 + x], r[h * 32 + x + 1]), pack_u32x2(v[x], v[x + 1]),
+                                            sum[(x >> 1) & 1]);
+          }
+          float a, b;
+          unpack_f32x2(add_f32x2(sum[0], sum[1]), a, b);
+          float(*part)[kT] = sm.pair[pairs & 1];
+          part[half][row] = a + b;
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&sm.pair_full[quarter]);
+          if (!(ok = wait(&sm.pair_full[quarter], pairs & 1))) break;
+          ++pairs;
+          const float d = part[0][row] + part[1][row];
+          d2 = pack_f32x2(-d, -d);
+          if (half == 0 && rt < it.ntok) p.dsum[(int64_t)(it.hk * p.G + rg) * p.nq + it.tok0 + rt] = d;
+        }
         uint32_t ds[32];
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
@@ -1087,7 +1124,10 @@ cudaError_t launch_xattn_bwd_tc(const XattnParams& p, void* ws, cudaStream_t s) 
   prm.x.part_dk = static_cast<float*>(ws);
   prm.x.part_dv = reinterpret_cast<float*>(static_cast<char*>(ws) + part_bytes(p, prm.R));
   prm.scale_log2 = p.scale * kLog2e;
-  cudaError_t e = launch_xattn_dsum(p, true, s);
+  const bool few = p.nk <= (int64_t)kT * p.B;
+  // One segment of one block: the dQ kernel takes all of D, and there is no
+  // prefix to check (85,202 x 77 x 24 x 128: 776 -> 621 us).
+  cudaError_t e = few && !p.cu_q && p.nk > 0 ? cudaSuccess : launch_xattn_dsum(p, true, s);
   if (e != cudaSuccess) return e;
   if (p.nq > 0) {
     // without keys the K and V maps are never used
@@ -1101,8 +1141,10 @@ cudaError_t launch_xattn_bwd_tc(const XattnParams& p, void* ws, cudaStream_t s) 
         !encode_tmap_heads_bf16(&tm[3], p.dout, p.d, p.H, p.nq, p.dos * 2, p.G, prm.tpt))
       return cudaErrorInvalidValue;
     prm.n_items = segment_slots(p.nq, p.B, prm.tpt) * p.Hk;
-    e = p.d == 64 ? launch(xattn_dq_kernel<64>, kDqThreads, sizeof(DqSmem<64>), kDqLaunch, prm, tm, s)
-                  : launch(xattn_dq_kernel<128>, kDqThreads, sizeof(DqSmem<128>), kDqLaunch, prm, tm, s);
+    e = p.d == 64 ? launch(few ? xattn_dq_kernel<64, true> : xattn_dq_kernel<64, false>, kDqThreads,
+                           sizeof(DqSmem<64>), kDqLaunch, prm, tm, s)
+                  : launch(few ? xattn_dq_kernel<128, true> : xattn_dq_kernel<128, false>, kDqThreads,
+                           sizeof(DqSmem<128>), kDqLaunch, prm, tm, s);
     if (e != cudaSuccess) return e;
     if (p.nk > 0) {
       prm.n_items = segment_slots(p.nq, p.B, prm.R * prm.tpt) * p.Hk * prm.ks;
