@@ -393,7 +393,10 @@ ut_status ut_xattn_fwd(const ut_xattn_shape* shape, const void* q, const void* k
  * and dV of masked keys, and rows of dQ without a key, are zero.
  *   o, lse      the forward's outputs;  dout  [n_q, H, d]
  *   dq          [n_q, H, d];  dk, dv  [n_k, H_kv, d], fully overwritten
- *   ws          ut_xattn_bwd_workspace_size(shape) bytes, 16-byte aligned. */
+ *   ws          ut_xattn_bwd_workspace_size(shape) bytes (may be 0: then NULL
+ *               is fine), 16-byte aligned
+ * In bf16 P and dS are rounded to bf16 for their products and each gradient
+ * once at the end; the rest is fp32.  The result does not depend on the run. */
 size_t ut_xattn_bwd_workspace_size(const ut_xattn_shape* shape);
 ut_status ut_xattn_bwd(const ut_xattn_shape* shape, const void* q, const void* k, const void* v,
                        const int32_t* cu_q, const int32_t* cu_k, const uint8_t* key_mask,

@@ -5,39 +5,49 @@
 //
 // A query tile holds 128 rows: the G heads that share a kv head of 128 / G
 // consecutive tokens of one segment (row = token * G + head; one TMA box), so
-// that K and V are read once for the group.  A work item is two such tiles,
-// one kv head and one range of key blocks (128 keys each); its tiles take
-// turns on the tensor cores, so that one tile's products run while the other
-// tile's softmax does, and share every K and V tile in shared memory.
+// that K and V are read once for the group.  A work item is T such tiles, one
+// kv head and one range of key blocks; the tiles share every K and V tile in
+// shared memory, and while one tile's softmax runs the others' products do.
+// T = 2 and blocks of 128 keys at d = 128, T = 4 and 64 keys at d = 64: either
+// fills tensor memory with S and O.  (Two tiles at d = 64 too: 89 us instead of
+// 71 for 23,959 x 257 x 24, the softmax warps wait for products 1,000 of 2,700
+// cycles a block.)
 //
 // One CTA per SM, which takes item after item (NextItem); items with the head
 // fastest, so that CTAs in flight read neighbouring 256-byte pieces of the same
-// rows and share K and V in L2.  Roles (384 threads, registers rebalanced with setmaxnreg):
+// rows and share K and V in L2.  Roles (128 + 128 T threads; with T = 2
+// registers rebalanced with setmaxnreg):
 //   warp 0      TMA: the K and V tiles, one ring (K0 V0 K1 V1 ...); leaves
 //               beside a V tile which of its keys count
 //   warp 2      asks for the items and decodes them (segment search, key
 //               range) into a ring; TMA: the query tiles, a ring of their own
-//   warp 1      TMEM owner and MMA issuer of tile 0, warp 3 of tile 1: per
-//               block S = Q K^T, then, as P is written over S in TMEM, O += P V
-//               (of the first 96 keys while the last 32 are being written).
-//               Two issuers, so that one tile's warp waits for its operands
-//               while the other tile's products run; they issue in turn (P V
-//               and the next S of one tile together), else the tensor core
-//               mixes the two tiles' instructions, both finish late, and both
-//               softmaxes then run at once with the tensor core idle.
-//   warps 4-7   softmax of tile 0, warps 8-11 of tile 1: thread = row = TMEM
-//               lane.  Read S from TMEM, mask, keep a running maximum (O is
-//               rescaled in TMEM only where it grew by more than 2^8, so the
-//               exponentials stay bounded), write P as bf16 over S; after the
-//               last block O / l and LSE, or the split's partial result.
+//   warp 1      TMEM owner and MMA issuer of the even tiles, warp 3 of the odd
+//               ones: per block S = Q K^T, then, as P is written over S in TMEM,
+//               O += P V.  With T = 2 that product begins with the first 96
+//               keys while P of the last 32 is being written, and the issuers
+//               take turns (P V and the next S of one tile together), else the
+//               tensor core mixes the two tiles' instructions, both finish late,
+//               and both softmaxes then run at once with the tensor core idle.
+//               Their code is fetched anew each time and kept short for that:
+//               the part of a wait that spins is called (431 -> 400 us for
+//               85,202 x 512 x 24 x 128).
+//   warps 4...  softmax, four warps a tile: thread = row = TMEM lane.  Read S
+//               from TMEM, mask, keep a running maximum (O is rescaled in TMEM
+//               only where it grew by more than 2^8, so the exponentials stay
+//               bounded), write P as bf16 over S; after the last block O / l and
+//               LSE, or the split's partial result.
 // Masked keys and the rows of other segments: S there becomes -inf, the
 // smaller of S and a bias of +-inf that warp 0 leaves in shared memory (the
 // min of NaN and -inf is -inf; selecting by bits of the mask took 900 to 1,300
 // cycles a block, this takes 400), and those rows of the V tile become zero
 // before its products (by warp 0 or the softmax warps), so that no value they
 // hold (NaN, infinities) is multiplied.
-// TMEM columns: S_0 / P_0 [0,128), S_1 / P_1 [128,256), O_0 [256,256+d), O_1
-// [384,384+d).
+// Rounding: P to bf16 for its product (the sum l is of the unrounded values),
+// O once at the end.
+// Measured: 85,202 x 512 x 24 x 128 385 us, 1,390 TFLOP/s, 0.74 of the card's
+// bf16 rate, bound by the softmax between the products (tensor pipe active 58%);
+// 23,959 x 257 x 24 x 64 67 us; one query over 85,202 keys, 24 heads of 128, 154
+// us, 6.8 TB/s.
 // Every wait is bounded; on expiry the kernel records UT_ERR_TIMEOUT, drains
 // its own copies and MMAs, frees TMEM and returns.
 #include "common.cuh"
