@@ -83,7 +83,8 @@ UT_DEV void zero_tail(uint32_t base, int chunks, int first, uint32_t lane) {
 //   warp 1      the products
 //   warp 2      decodes the items into a ring, 32 at once, one a lane (one after
 //               another each took 2,500 cycles, more than a block)
-//   warp 3      zeroes the masked keys of K, says when a block has all it needs
+//   warp 3      zeroes the masked keys of K and V, says when a block has all it
+//               needs
 //   warps 12-15 dQ out
 // kFew, for segments of 128 keys on average or fewer: dS is rounded to bf16
 // for its product, as dQ is at the end, together 1.42 times the error of
@@ -300,7 +301,8 @@ __global__ void __launch_bounds__(kDqThreads, 1)
         }
       }
     } else if (warp == 3) {
-      // ------------------------ masked keys of K; Q (of a first block), K, V
+      // Masked keys of K and V: S, dP and dQ's terms of theirs are then zero.
+      // And when Q (of a first block), K and V are there.
       uint32_t n = 0, at = 0;
       bool ok = true;
       DqItem it;
@@ -321,7 +323,7 @@ __global__ void __launch_bounds__(kDqThreads, 1)
           if (some) zero_keys(smem_u32(sm.k[st]));
           if (j == 0 && !(ok = wait(&sm.q_full[(n - 1) % S::kQ], ((n - 1) / S::kQ) & 1))) break;
           if (!(ok = wait(&sm.v_full[at % S::kV], (at / S::kV) & 1))) break;
-          if (kFew && some) zero_keys(smem_u32(sm.v[at % S::kV]));  // so that dP = 0, whatever V holds there
+          if (some) zero_keys(smem_u32(sm.v[at % S::kV]));
           if (lane == 0) mbar_arrive(&sm.ready[st]);
         }
     } else if (warp == 1) {
@@ -432,8 +434,10 @@ __global__ void __launch_bounds__(kDqThreads, 1)
     if (more) row_load(nx, nl, nd);
     while (ok && more) {
       it = nx;
-      // a row without keys has all its columns masked; one that does not exist P = 0
-      const uint64_t l2 = pack_f32x2(-nl * kLog2e, -nl * kLog2e);
+      // P = 0 in a row that does not exist or has no keys, and dS too in the latter
+      const uint32_t row_on = nl == -INFINITY ? 0u : ~0u;
+      const float le = row_on ? -nl * kLog2e : -INFINITY;
+      const uint64_t l2 = pack_f32x2(le, le);
       uint64_t d2 = pack_f32x2(-nd, -nd);
       more = next_item(n, nx, ok);
       if (!ok) break;
@@ -453,6 +457,11 @@ __global__ void __launch_bounds__(kDqThreads, 1)
           unpack_f32x2(fma_f32x2(pack_u32x2(r[x], r[x + 1]), c2, l2), a, b);
           r[x] = __float_as_uint(ex2_approx(a));
           r[x + 1] = __float_as_uint(ex2_approx(b));
+        }
+        const bool whole = __all_sync(0xffffffffu, now == 15u);
+        if (!whole) {  // P of a masked key (S = 0) may be infinite; the others' is at most 1
+#pragma unroll
+          for (int x = 0; x < 64; ++x) r[x] = __float_as_uint(fminf(__uint_as_float(r[x]), 2.f));
         }
         if (!(ok = wait(&sm.dp_full[at % S::kV], (at / S::kV) & 1))) break;
         tc_fence_after();
@@ -495,14 +504,9 @@ __global__ void __launch_bounds__(kDqThreads, 1)
             ds[h * 16 + x / 2] = pack_bf16x2(a, b);
           }
         }
-        if (!__all_sync(0xffffffffu, now == 15u)) {  // dS of a masked key is zero, whatever S and dP are
+        if (!whole) {
 #pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            const uint32_t word = __ballot_sync(0xffffffffu, (now >> (half * 2 + h)) & 1u);
-#pragma unroll
-            for (int x = 0; x < 16; ++x)
-              ds[h * 16 + x] &= (((word >> (2 * x)) & 1u) ? 0xFFFFu : 0u) | (((word >> (2 * x + 1)) & 1u) ? 0xFFFF0000u : 0u);
-          }
+          for (int x = 0; x < 32; ++x) ds[x] &= row_on;
         }
         tmem_st32(ts, ds);
         tmem_wait_st();
