@@ -1091,15 +1091,17 @@ int key_split(const XattnParams& p) {
 }
 
 // Tiles of a run: the number of runs with the least modelled time, in cycles:
-// whole waves of items of R tiles (2,200 each, 5,000 an item), and each run's
-// partial sums written and read (3,400 bytes a cycle).  At most 1 GB of them.
+// whole waves of items of R tiles (2,200 each, 5,000 an item; a segment's last
+// run is half full on average), and each run's partial sums written and read
+// (3,400 bytes a cycle).  At most 1 GB of them.
 int tiles_per_item(const XattnParams& p) {
   const int64_t tpt = kT / p.G, tiles = (p.nq + tpt - 1) / tpt, across = (int64_t)p.Hk * key_split(p);
   const int64_t part = 2 * segment_slots(p.nk, p.B, kT) * kT * p.Hk * p.d * (int64_t)sizeof(float);
   int64_t best = tiles;
   double least = 0;
   for (int64_t runs = 1; runs <= tiles && runs <= 128; ++runs) {
-    const int64_t R = (tiles + runs - 1) / runs, waves = (runs * across + p.sms - 1) / p.sms;
+    const int64_t R = (tiles + runs - 1) / runs, items = (runs + (p.B > 1 ? p.B / 2 : 0)) * across;
+    const int64_t waves = (items + p.sms - 1) / p.sms;
     if (runs > 1 && runs * part > ((int64_t)1 << 30)) break;
     const double t = (double)waves * (R * 2200.0 + 5000.0) + (double)runs * (2 * part) / 3400.0;
     if (runs == 1 || t < least) {
