@@ -597,11 +597,46 @@ __global__ void __launch_bounds__(kDqThreads, 1)
 // [384,384+d); lanes = keys.  Per tile t the tensor core runs dV_t, S^T_{t+1}
 // while the elementwise warps form dS^T_t, and dK_t, dP^T_{t+1} while they form
 // P^T_{t+1}.
-//   warp 0   TMA: K, V and the Q ring      warp 2   zeroes Q rows that are not
-//   warp 3   TMA: the dO ring, and its rows          the item's
+//   warp 0   asks for the items (NextItem) and decodes them into a ring; TMA:
+//            K, V and the Q ring
+//   warp 2   zeroes Q rows that are not the item's; LSE and D of the rows
+//   warp 3   TMA: the dO ring; zeroes its rows
+// An item is published once all loads of the one before have been asked for, and
+// nothing is loaded across items: no wait depends on the warp that waits.
 constexpr int kKvThreads = 384;
 constexpr int kKvLaunch = 168, kKvCtl = 104, kKvEw = 200;
 static_assert(kKvCtl + 2 * kKvEw <= 3 * kKvLaunch, "setmaxnreg split must fit the launch");
+
+constexpr int kKvSlots = 2, kKvReaders = 11;
+
+struct Work {  // one item: a run of query tiles, a kv head, every ks-th key block
+  int32_t hk, part, tiles, block0, blocks;  // blocks 0: no more items
+  int32_t tok0, key0, ntok, keys;           // tokens of the run, keys of the segment
+  int32_t kslot;                            // first key block's place among all segments'
+};
+
+// Item u, by a whole warp; blocks 0 where its slot is idle.
+UT_DEV Work decode(const BwdParams& b, int u) {
+  const XattnParams& p = b.x;
+  Work w{};
+  const int v = u / b.ks, slot = v / p.Hk;
+  w.block0 = u - v * b.ks;
+  w.hk = v - slot * p.Hk;
+  const Segment g = warp_segment_of_slot(p.cu_q, p.B, p.nq, b.R * b.tpt, slot);
+  const int64_t t0 = g.tile * b.R * b.tpt;
+  if (t0 >= g.n) return w;
+  int64_t k0, kn;
+  segment_rows(p.cu_k, g.s, p.nk, k0, kn);
+  w.part = (int)g.tile;
+  w.tok0 = (int)(g.row + t0);
+  w.ntok = (int)min((int64_t)b.R * b.tpt, g.n - t0);
+  w.tiles = (w.ntok + b.tpt - 1) / b.tpt;
+  w.key0 = (int)k0;
+  w.kslot = (int)(k0 / kT) + g.s;
+  w.keys = (int)kn;
+  w.blocks = max(0, ((int)((kn + kT - 1) / kT) - w.block0 + b.ks - 1) / b.ks);
+  return w;
+}
 
 template <int D>
 struct KvSmem {
@@ -612,42 +647,16 @@ struct KvSmem {
   alignas(1024) uint8_t v[kTile];
   alignas(1024) uint8_t q[kQ][kTile];
   alignas(1024) uint8_t dout[kDo][kTile];
+  Work item[kKvSlots];
+  NextItem next;
   alignas(16) float lse2[2][kT];  // -LSE log2(e) and -D of the rows of a tile
   alignas(16) float dsum[2][kT];
   uint64_t kv_full, kv_empty, q_full[kQ], q_empty[kQ], do_full[kDo], do_empty[kDo], q_ready[4], do_ready[4];
+  uint64_t item_full[kKvSlots], item_empty[kKvSlots];
   uint64_t s_full, dp_full, p_full, ds_full, acc_full, acc_empty, mma_done;
   uint32_t tmem_base;
   int abort_flag;
 };
-
-struct Work {  // one item: a run of query tiles, a kv head, every ks-th key block
-  int hk, part, tiles, block0, blocks;
-  int64_t tok0, key0;
-  int ntok, keys;  // tokens of the run, keys of the segment
-  int64_t kslot;   // first key block's place among all segments'
-};
-
-// Item u; false where its slot is idle.
-UT_DEV bool decode(const BwdParams& b, int64_t u, Work& w) {
-  const XattnParams& p = b.x;
-  const int64_t v = u / b.ks;
-  w.block0 = (int)(u - v * b.ks);
-  w.hk = (int)(v % p.Hk);
-  const Segment g = segment_of_slot(p.cu_q, p.B, p.nq, b.R * b.tpt, v / p.Hk);
-  const int64_t t0 = g.tile * b.R * b.tpt;
-  if (t0 >= g.n) return false;
-  int64_t k0, kn;
-  segment_rows(p.cu_k, g.s, p.nk, k0, kn);
-  w.part = (int)g.tile;
-  w.tok0 = g.row + t0;
-  w.ntok = (int)min((int64_t)b.R * b.tpt, g.n - t0);
-  w.tiles = (w.ntok + b.tpt - 1) / b.tpt;
-  w.key0 = k0;
-  w.kslot = k0 / kT + g.s;
-  w.keys = (int)kn;
-  w.blocks = ((int)((kn + kT - 1) / kT) - w.block0 + b.ks - 1) / b.ks;
-  return w.blocks > 0;
-}
 
 template <int D>
 __global__ void __launch_bounds__(kKvThreads, 1)
@@ -677,6 +686,11 @@ __global__ void __launch_bounds__(kKvThreads, 1)
     }
     uint64_t* eight[] = {&sm.p_full, &sm.ds_full, &sm.acc_empty};
     for (uint64_t* x : eight) mbar_init(x, 8);
+    for (int s = 0; s < kKvSlots; ++s) {
+      mbar_init(&sm.item_full[s], 1);
+      mbar_init(&sm.item_empty[s], kKvReaders);
+    }
+    next_item_init(sm.next);
     for (int s = 0; s < 4; ++s) {
       mbar_init(&sm.q_ready[s], 1);
       mbar_init(&sm.do_ready[s], 1);
@@ -700,43 +714,79 @@ __global__ void __launch_bounds__(kKvThreads, 1)
   auto wait = [&](uint64_t* bar, uint32_t parity) {  // whole warp, converged
     return warp_wait(bar, parity, abort_flag, p.status, p.timeout_ns);
   };
-  auto wait1 = [&](uint64_t* bar, uint32_t parity) {  // one thread
-    return mbar_wait(bar, parity, abort_flag, p.status, p.timeout_ns);
-  };
   auto drain = [&](uint64_t* bar, uint32_t parity) {
     if (!mbar_drain(bar, parity, kDrainTimeoutNs)) set_status(p.status, UT_ERR_TIMEOUT);
+  };
+
+  // The next item; false at the end or on an abort (then ok = false).  Whole warp.
+  auto next_item = [&](uint32_t& n, Work& w, bool& ok) -> bool {
+    const uint32_t s = n % kKvSlots;
+    if (!(ok = wait(&sm.item_full[s], (n / kKvSlots) & 1))) return false;
+    w = sm.item[s];
+    __syncwarp();
+    if (lane == 0) mbar_arrive(&sm.item_empty[s]);
+    ++n;
+    return w.blocks > 0;
   };
 
   if (warp < 4) {
     setmaxnreg_dec<kKvCtl>();
     if (warp == 0) {
-      if (lane == 0) {
-        const uint64_t keep = policy_evict_last();
-        const uint32_t bytes = (uint32_t)prm.tpt * p.G * 128 * S::kC;
-        uint32_t nkv = 0, nt = 0;
-        bool ok = true;
-        for (int64_t u = blockIdx.x; u < prm.n_items && ok; u += gridDim.x) {
-          Work w;
-          if (!decode(prm, u, w)) continue;
+      const uint64_t keep = policy_evict_last();
+      const uint32_t bytes = (uint32_t)prm.tpt * p.G * 128 * S::kC;
+      uint32_t nkv = 0, nt = 0, n = 0, asked = 0;
+      bool ok = true;
+      for (int u = (int)blockIdx.x; ok;) {
+        Work w{};
+        if (u >= 0) w = decode(prm, u);
+        if (u < 0 || w.blocks > 0) {
+          const uint32_t s = n % kKvSlots;
+          if (!(ok = wait(&sm.item_empty[s], ((n / kKvSlots) & 1) ^ 1))) break;
+          if (lane == 0) {
+            sm.item[s] = w;
+            mbar_arrive(&sm.item_full[s]);
+          }
+          __syncwarp();
+          ++n;
+          if (u < 0) break;  // no more items
           for (int b = 0; b < w.blocks && ok; ++b) {
             const int j = w.block0 + b * prm.ks;
-            if (!(ok = wait1(&sm.kv_empty, (nkv & 1) ^ 1))) break;
-            mbar_expect_tx(&sm.kv_full, 2 * S::kTile);
-            for (int c = 0; c < S::kC; ++c) {
-              tma_load_3d(sm.k + c * kChunkB, &tm_k, &sm.kv_full, c * 64, w.hk, (int)w.key0 + j * kT, keep);
-              tma_load_3d(sm.v + c * kChunkB, &tm_v, &sm.kv_full, c * 64, w.hk, (int)w.key0 + j * kT, keep);
+            if (!(ok = wait(&sm.kv_empty, (nkv & 1) ^ 1))) break;
+            if (lane == 0) {
+              mbar_expect_tx(&sm.kv_full, 2 * S::kTile);
+              for (int c = 0; c < S::kC; ++c) {
+                tma_load_3d(sm.k + c * kChunkB, &tm_k, &sm.kv_full, c * 64, w.hk, w.key0 + j * kT, keep);
+                tma_load_3d(sm.v + c * kChunkB, &tm_v, &sm.kv_full, c * 64, w.hk, w.key0 + j * kT, keep);
+              }
             }
+            __syncwarp();
             ++nkv;
             for (int t = 0; t < w.tiles; ++t, ++nt) {
               const uint32_t st = nt % S::kQ;
-              if (!(ok = wait1(&sm.q_empty[st], ((nt / S::kQ) & 1) ^ 1))) break;
-              mbar_expect_tx(&sm.q_full[st], bytes);
-              for (int c = 0; c < S::kC; ++c)
-                tma_load_3d(sm.q[st] + c * kChunkB, &tm_q, &sm.q_full[st], c * 64, w.hk * p.G,
-                            (int)w.tok0 + t * prm.tpt, keep);
+              if (!(ok = wait(&sm.q_empty[st], ((nt / S::kQ) & 1) ^ 1))) break;
+              if (lane == 0) {
+                mbar_expect_tx(&sm.q_full[st], bytes);
+                for (int c = 0; c < S::kC; ++c)
+                  tma_load_3d(sm.q[st] + c * kChunkB, &tm_q, &sm.q_full[st], c * 64, w.hk * p.G,
+                              w.tok0 + t * prm.tpt, keep);
+              }
+              __syncwarp();
             }
           }
+          if (!ok) break;
         }
+        // asked for now, two or three tiles before this item's end, not at its
+        // begin: who asks first should be who is done first
+        if (lane == 0) next_item_ask(sm.next, asked);
+        __syncwarp();
+        ++asked;
+        if (!(ok = wait(&sm.next.full[(asked - 1) & 1], ((asked - 1) >> 1) & 1))) break;
+        u = (int)warp_uniform((uint32_t)next_item_answer(sm.next, asked - 1));
+        fence_proxy_async_smem();  // the answer is read before its place is used again
+        __syncwarp();
+      }
+      if (lane == 0) {
+        if (asked > 0) drain(&sm.next.full[(asked - 1) & 1], ((asked - 1) >> 1) & 1);
         if (nkv > 0) drain(&sm.kv_full, (nkv - 1) & 1);
         for (uint32_t x = nt > S::kQ ? nt - S::kQ : 0; x < nt; ++x) drain(&sm.q_full[x % S::kQ], (x / S::kQ) & 1);
       }
@@ -763,11 +813,14 @@ __global__ void __launch_bounds__(kKvThreads, 1)
         mma_commit_w(&sm.dp_full);
         dn = dn + 1 == S::kDo ? 0 : dn + 1;
       };
-      for (int64_t u = blockIdx.x; u < prm.n_items && ok; u += gridDim.x) {
-        Work w;
-        if (!warp_uniform(decode(prm, u, w))) continue;
-        const uint32_t tiles = warp_uniform((uint32_t)w.tiles);
-        uint32_t blocks = warp_uniform((uint32_t)w.blocks);
+      for (uint32_t n = 0;; ++n) {
+        const uint32_t s = n % kKvSlots;
+        if (!(ok = waitq(&sm.item_full[s], (n / kKvSlots) & 1))) break;
+        const uint32_t tiles = warp_uniform((uint32_t)sm.item[s].tiles);
+        uint32_t blocks = warp_uniform((uint32_t)sm.item[s].blocks);
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&sm.item_empty[s]);
+        if (blocks == 0) break;
         for (; blocks > 0; --blocks) {
           if (!(ok = waitq(&sm.kv_full, nkv & 1))) break;
           if (!(ok = waitq(&sm.q_ready[nt & 3], (nt >> 2) & 1))) break;
@@ -801,6 +854,7 @@ __global__ void __launch_bounds__(kKvThreads, 1)
           mma_commit_w(&sm.acc_full);
           ++nkv;
         }
+        if (!ok) break;
       }
       mma_commit_w(&sm.mma_done);
       drain(&sm.mma_done, 0);
@@ -810,44 +864,31 @@ __global__ void __launch_bounds__(kKvThreads, 1)
       const bool is_q = warp == 2;
       const uint32_t bytes = (uint32_t)prm.tpt * p.G * 128 * S::kC;
       const uint64_t keep = policy_evict_last();
-      uint32_t nt = 0, sent = 0;  // tiles made ready, dO tiles asked for
+      uint32_t n = 0, nt = 0, sent = 0;  // items, tiles made ready, dO tiles asked for
       bool ok = true;
-      int64_t u2 = blockIdx.x;  // the load cursor runs ahead of the other
-      Work w2;
-      int j2 = 0, t2 = 0;
-      bool have2 = false;
-      auto load_ahead = [&]() {  // asks for the next dO tile if its stage is free; whole warp
-        while (!have2 && u2 < prm.n_items) {
-          have2 = decode(prm, u2, w2);
-          if (!have2) u2 += gridDim.x;
-          j2 = t2 = 0;
-        }
-        if (!have2) return;
-        const uint32_t st = sent % S::kDo;
-        if (!(ok = wait(&sm.do_empty[st], ((sent / S::kDo) & 1) ^ 1))) return;
-        if (lane == 0) {
-          mbar_expect_tx(&sm.do_full[st], bytes);
-          for (int c = 0; c < S::kC; ++c)
-            tma_load_3d(sm.dout[st] + c * kChunkB, &tm_do, &sm.do_full[st], c * 64, w2.hk * p.G,
-                        (int)w2.tok0 + t2 * prm.tpt, keep);
-        }
-        __syncwarp();
-        ++sent;
-        if (++t2 == w2.tiles) {
-          t2 = 0;
-          if (++j2 == w2.blocks) {
-            have2 = false;
-            u2 += gridDim.x;
+      Work w;
+      while (ok && next_item(n, w, ok)) {
+        int left = w.blocks * w.tiles, tok = w.tok0;  // dO tiles to ask for, the next one's token
+        const int end = w.tok0 + w.tiles * prm.tpt;
+        auto load_next = [&]() {
+          if (left == 0) return;
+          const uint32_t st = sent % S::kDo;
+          if (!(ok = wait(&sm.do_empty[st], ((sent / S::kDo) & 1) ^ 1))) return;
+          if (lane == 0) {
+            mbar_expect_tx(&sm.do_full[st], bytes);
+            for (int c = 0; c < S::kC; ++c)
+              tma_load_3d(sm.dout[st] + c * kChunkB, &tm_do, &sm.do_full[st], c * 64, w.hk * p.G, tok, keep);
           }
-        }
-      };
-      // A stage's next load is only waited for once the tile kDo - 1 before it
-      // has been made ready, so the wait always ends.
-      if (!is_q)
-        for (int x = 0; x < S::kDo - 1 && ok; ++x) load_ahead();
-      for (int64_t u = blockIdx.x; u < prm.n_items && ok; u += gridDim.x) {
-        Work w;
-        if (!decode(prm, u, w)) continue;
+          __syncwarp();
+          ++sent;
+          --left;
+          tok += prm.tpt;
+          if (tok == end) tok = w.tok0;  // again, for the next key block
+        };
+        // A stage's next load is only waited for once the tile kDo - 1 before it
+        // has been made ready, so the wait always ends.
+        if (!is_q)
+          for (int x = 0; x < S::kDo - 1 && ok; ++x) load_next();
         float rl[4], rd[4];  // as loaded: arithmetic on them here would wait for the loads
         auto rows_load = [&](int t) {
 #pragma unroll
@@ -889,7 +930,7 @@ __global__ void __launch_bounds__(kKvThreads, 1)
               if (t + 1 < w.tiles) rows_load(t + 1);
               else if (j + 1 < w.blocks) rows_load(0);
             } else {
-              load_ahead();
+              load_next();
               if (!ok) break;
             }
           }
@@ -905,11 +946,10 @@ __global__ void __launch_bounds__(kKvThreads, 1)
     const uint32_t lane_base = (quarter * 32) << 16, ts = lane_base + half * 64;
     constexpr int HC = kT / 2, HD = D / 2;
     const uint64_t c2 = pack_f32x2(prm.scale_log2, prm.scale_log2);
-    uint32_t nt = 0, ng = 0;
+    uint32_t n = 0, nt = 0, ng = 0;
     bool ok = true;
-    for (int64_t u = blockIdx.x; u < prm.n_items && ok; u += gridDim.x) {
-      Work w;
-      if (!decode(prm, u, w)) continue;
+    Work w;
+    while (ok && next_item(n, w, ok)) {
       for (int b = 0; b < w.blocks && ok; ++b, ++ng) {
         const int j = w.block0 + b * prm.ks;
         const int key = j * kT + (int)krow;
@@ -1069,16 +1109,15 @@ static_assert(sizeof(DqSmem<128>) <= 232448 && sizeof(KvSmem<128>) <= 232448 && 
 // The setmaxnreg split assumes exactly `regs` registers per thread at launch:
 // with fewer, the increases would wait for registers that never come.
 template <typename F>
-cudaError_t launch(F kern, int threads, size_t smem, int regs, const BwdParams& prm, const CUtensorMap* tm,
-                   cudaStream_t s) {
+cudaError_t launch(F kern, int64_t grid, int threads, size_t smem, int regs, const BwdParams& prm,
+                   const CUtensorMap* tm, cudaStream_t s) {
   cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
   if (e != cudaSuccess) return e;
   cudaFuncAttributes fa;
   e = cudaFuncGetAttributes(&fa, kern);
   if (e != cudaSuccess) return e;
   if (fa.numRegs != regs) return cudaErrorInvalidConfiguration;
-  const int grid = (int)(prm.n_items < prm.x.sms ? prm.n_items : prm.x.sms);
-  return launch_next(kern, dim3(grid), dim3(threads), smem, s, tm[0], tm[1], tm[2], tm[3], prm);
+  return launch_next(kern, dim3((unsigned)grid), dim3(threads), smem, s, tm[0], tm[1], tm[2], tm[3], prm);
 }
 
 // Items of a run along the keys: the blocks of a segment of mean length, so
@@ -1090,20 +1129,27 @@ int key_split(const XattnParams& p) {
   return (int)(mean < 1 ? 1 : (mean > 256 ? 256 : mean));
 }
 
-// Tiles of a run: the number of runs with the least modelled time, in cycles:
-// whole waves of items of R tiles (2,200 each, 5,000 an item; a segment's last
-// run is half full on average), and each run's partial sums written and read
+// Tiles of a run: the number of runs with the least modelled time, in cycles.
+// An item of R tiles takes 2,200 each and 5,000; equal items run in whole waves,
+// those of ragged segments (whose last runs are half full on average) end half
+// an item apart.  And the partial sums of a segment's runs are written and read
 // (3,400 bytes a cycle).  At most 1 GB of them.
 int tiles_per_item(const XattnParams& p) {
   const int64_t tpt = kT / p.G, tiles = (p.nq + tpt - 1) / tpt, across = (int64_t)p.Hk * key_split(p);
   const int64_t part = 2 * segment_slots(p.nk, p.B, kT) * kT * p.Hk * p.d * (int64_t)sizeof(float);
   int64_t best = tiles;
   double least = 0;
-  for (int64_t runs = 1; runs <= tiles && runs <= 128; ++runs) {
-    const int64_t R = (tiles + runs - 1) / runs, items = (runs + (p.B > 1 ? p.B / 2 : 0)) * across;
-    const int64_t waves = (items + p.sms - 1) / p.sms;
+  for (int64_t runs = 1; runs <= tiles && runs <= 256; ++runs) {
     if (runs > 1 && runs * part > ((int64_t)1 << 30)) break;
-    const double t = (double)waves * (R * 2200.0 + 5000.0) + (double)runs * (2 * part) / 3400.0;
+    const int64_t R = (tiles + runs - 1) / runs;
+    const double item = R * 2200.0 + 5000.0;
+    double t;
+    if (p.B == 1) {
+      t = (double)((runs * across + p.sms - 1) / p.sms) * item + (double)runs * (2 * part) / 3400.0;
+    } else {
+      const double waves = (runs + 0.5 * p.B) * (double)across / p.sms, each = (double)runs / p.B + 0.5;
+      t = (waves < 1.0 ? 1.0 : waves + 0.5) * item + each * (2 * part) / 3400.0;
+    }
     if (runs == 1 || t < least) {
       least = t;
       best = R;
@@ -1152,15 +1198,16 @@ cudaError_t launch_xattn_bwd_tc(const XattnParams& p, void* ws, cudaStream_t s) 
         !encode_tmap_heads_bf16(&tm[3], p.dout, p.d, p.H, p.nq, p.dos * 2, p.G, prm.tpt))
       return cudaErrorInvalidValue;
     prm.n_items = segment_slots(p.nq, p.B, prm.tpt) * p.Hk;
-    e = p.d == 64 ? launch(few ? xattn_dq_kernel<64, true> : xattn_dq_kernel<64, false>, kDqThreads,
+    const int64_t grid = prm.n_items < p.sms ? prm.n_items : p.sms;
+    e = p.d == 64 ? launch(few ? xattn_dq_kernel<64, true> : xattn_dq_kernel<64, false>, grid, kDqThreads,
                            sizeof(DqSmem<64>), kDqLaunch, prm, tm, s)
-                  : launch(few ? xattn_dq_kernel<128, true> : xattn_dq_kernel<128, false>, kDqThreads,
+                  : launch(few ? xattn_dq_kernel<128, true> : xattn_dq_kernel<128, false>, grid, kDqThreads,
                            sizeof(DqSmem<128>), kDqLaunch, prm, tm, s);
     if (e != cudaSuccess) return e;
     if (p.nk > 0) {
       prm.n_items = segment_slots(p.nq, p.B, prm.R * prm.tpt) * p.Hk * prm.ks;
-      e = p.d == 64 ? launch(xattn_dkdv_kernel<64>, kKvThreads, sizeof(KvSmem<64>), kKvLaunch, prm, tm, s)
-                    : launch(xattn_dkdv_kernel<128>, kKvThreads, sizeof(KvSmem<128>), kKvLaunch, prm, tm, s);
+      e = p.d == 64 ? launch(xattn_dkdv_kernel<64>, prm.n_items, kKvThreads, sizeof(KvSmem<64>), kKvLaunch, prm, tm, s)
+                    : launch(xattn_dkdv_kernel<128>, prm.n_items, kKvThreads, sizeof(KvSmem<128>), kKvLaunch, prm, tm, s);
       if (e != cudaSuccess) return e;
     }
   }
