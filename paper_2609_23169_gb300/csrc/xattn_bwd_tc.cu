@@ -24,9 +24,9 @@
 // the products need 2,560.  Here P and dS never leave TMEM (they are the A
 // operands of the second products, written over the first ones' results), and
 // the elementwise work of one tile runs beside the products of the next:
-// 2,700 and 2,600 cycles a pair where the products need 1,536 and 2,048.
-// Measured at that size: D 44 us (6.6 TB/s), dQ 168, dK and dV 175, their sum
-// 13: 404 us a pass, 933 TFLOP/s of the five products.  dQ is bound by the
+// 2,700 and 2,700 cycles a pair where the products need 1,536 and 2,048.
+// Measured at that size: D 44 us (6.6 TB/s), dQ 168, dK and dV 185, their sum
+// 13: 420 us a pass, 896 TFLOP/s of the five products.  dQ is bound by the
 // elementwise warps and by shared memory (S and dP read both operands there,
 // tensor pipe active 60%), dK and dV by shared memory (80%).
 //
