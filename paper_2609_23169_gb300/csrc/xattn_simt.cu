@@ -18,7 +18,7 @@
 //
 // Two blocks share an SM; bound by latency, of the staged rows and of the reads
 // from shared memory (an instruction in 55% of the cycles, a multiply-add in
-// half of them): 2,501 x 301, 8 / 4 heads of 64, forward 28 us, gradient 84.
+// half of them): 2,501 x 301, 8 / 4 heads of 64, forward 28 us, gradient 80.
 #include <math.h>
 
 #include "common.cuh"
@@ -465,31 +465,31 @@ __global__ void __launch_bounds__(256) xattn_dsum_kernel(const XattnParams p) {
   }
 }
 
-// dK, dV = the sum of the splits' partials, in split order; 4 values a thread
-__global__ void __launch_bounds__(256) xattn_dkdv_join_kernel(const XattnParams p) {
-  const int64_t x = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;
+// dK (blockIdx.y = 0), dV = the sum of the splits' partials, in split order; 4
+// values a thread, small blocks, 16 loads in flight
+constexpr int kJoinThreads = 64;
+__global__ void __launch_bounds__(kJoinThreads) xattn_dkdv_join_kernel(const XattnParams p) {
+  const int64_t x = (int64_t)blockIdx.x * kJoinThreads + threadIdx.x;
   const int per_row = p.Hk * p.d / 4;
   const int64_t n = p.nk * per_row;
   grid_wait();
   if (x >= n) return;
   const int64_t key = x / per_row;
   const int e = (int)(x % per_row) * 4;
-#pragma unroll
-  for (int which = 0; which < 2; ++which) {
-    const float* src = (which ? p.part_dv : p.part_dk) + x * 4;
-    float4 a = make_float4(0, 0, 0, 0);
-#pragma unroll 8
-    for (int s = 0; s < p.nsplit; ++s) {
-      const float4 b = ld4(src + (int64_t)s * n * 4);
-      a.x += b.x;
-      a.y += b.y;
-      a.z += b.z;
-      a.w += b.w;
-    }
-    const float f = which ? 1.f : p.scale;
-    st4(static_cast<float*>(which ? p.dv : p.dk) + key * (which ? p.dvs : p.dks) + e,
-        make_float4(a.x * f, a.y * f, a.z * f, a.w * f));
+  const bool is_v = blockIdx.y;
+  const float* src = (is_v ? p.part_dv : p.part_dk) + x * 4;
+  float4 a = make_float4(0, 0, 0, 0);
+#pragma unroll 16
+  for (int s = 0; s < p.nsplit; ++s) {
+    const float4 b = ld4(src + (int64_t)s * n * 4);
+    a.x += b.x;
+    a.y += b.y;
+    a.z += b.z;
+    a.w += b.w;
   }
+  const float f = is_v ? 1.f : p.scale;
+  st4(static_cast<float*>(is_v ? p.dv : p.dk) + key * (is_v ? p.dvs : p.dks) + e,
+      make_float4(a.x * f, a.y * f, a.z * f, a.w * f));
 }
 
 // O, LSE from the key splits' partials; half a warp a token and head
@@ -561,7 +561,8 @@ static cudaError_t bwd(const XattnParams& p, cudaStream_t s) {
     e = launch_next(xattn_bwd_simt_kernel<T, D>, dim3((unsigned)(n_kv + n_q)), dim3(kXsThreads), smem, s, p,
                     (uint32_t)n_kv, kslots, qslots);
   if (e == cudaSuccess && p.nk > 0)
-    e = launch_next(xattn_dkdv_join_kernel, dim3((unsigned)((p.nk * p.Hk * D / 4 + 255) / 256)), dim3(256), 0, s, p);
+    e = launch_next(xattn_dkdv_join_kernel, dim3((unsigned)((p.nk * p.Hk * D / 4 + kJoinThreads - 1) / kJoinThreads), 2),
+                    dim3(kJoinThreads), 0, s, p);
   return e;
 }
 
