@@ -7,19 +7,18 @@
 //   a = sum_g gamma du,  b = sum_g gamma du xh,
 //   dx = r (gamma du - (a + xh b) / M)
 //
-// One cooperative launch each way, at most one block per SM.  The segments are
-// taken in batches of up to kBatchBytes (a longer segment is a batch of its
-// own); every block has a contiguous share of the batch's rows.  It reads its
-// rows once for the statistics (forward) or the sums (backward) of each
-// segment's piece in its share; after a grid barrier it merges the pieces of its
-// segments and writes its rows, last read first: the last ones are still in its
-// shared memory, others in L2.  The bound is DRAM bandwidth, with x (and dy) read
-// once and in part twice; a batch costs a barrier and a merge, 4 us, so batches
-// larger than L2 are better than ones that fit it (6 x 65,536 x 512: 192 MB).
-// Measured: 2048 x 2048 x 128 forward 510 us (two reads and a write at the copy
-// rate: 475), backward 882 us (790); 85,202 x 640 in 13 segments 66 and 131 us,
-// of which pass 1 has 27 and 56, the rest of the way 36 and 75: there a thread's
-// chain of arithmetic bounds it, 12 and 11 warps an SM.
+// One cooperative launch each way, at most one block per SM; every block has a
+// contiguous share of the rows.  It reads its rows once for the statistics
+// (forward) or the sums (backward) of each segment's piece in its share; after a
+// grid barrier it merges the pieces of its segments and writes its rows, last
+// read first: the last ones are still in its shared memory, others in L2.  The
+// bound is DRAM bandwidth, with x (and dy) read once and in part twice.  (Batches
+// of segments that stay in L2 between the passes were tried: 4 us of barrier and
+// merge each and a loop around both passes cost more than the second reads, 225
+// us instead of 204 for 6 x 65,536 x 512.)
+// Measured: 2048 x 2048 x 128 forward 514 us (two reads and a write at the copy
+// rate: 475), backward 822 us (790); 6 x 65,536 x 512 forward 204 us (178),
+// backward 325 (297); 85,202 x 640 in 13 segments 62 and 108 us.
 //
 // Rows move in chunks of kPer rows a thread: a producer warp copies them to a
 // ring in shared memory with bulk copies (several chunks in flight whatever
@@ -54,7 +53,6 @@ constexpr int kFwdThreads = 480, kBwdThreads = 352;
 constexpr int kFwdPer = 4, kBwdPer = 4;              // rows of a chunk for each thread
 constexpr int kWindow = 16;                          // rows summed before they are merged (forward)
 constexpr int kMaxSlots = 16;
-constexpr int64_t kBatchBytes = 192ll << 20;          // of the tensors read, per batch
 constexpr size_t kSmem = 225 * 1024;                 // with 2 KB of static shared memory
 
 template <typename T>
@@ -147,38 +145,14 @@ UT_DEV void rows_of_segment(const GnormParams& p, int s, int& row, int& n) {
   n = (int)len;
 }
 
-// Segments [s0, s1) with rows [row, row + n): as many whole segments as
-// p.batch_rows hold, at least one.
-struct Batch {
-  int s0, s1, row, n;
-};
-UT_DEV Batch batch_from(const GnormParams& p, int s0) {
-  Batch b{s0, p.B, 0, 0};
-  int row, n;
-  rows_of_segment(p, s0, row, n);
-  b.row = row;
-  if (!p.cu || p.n - row <= p.batch_rows) {
-    b.n = (int)p.n - row;
-    return b;
-  }
-  int end = row + n;
-  b.s1 = s0 + 1;
-  while (b.s1 < p.B) {
-    rows_of_segment(p, b.s1, row, n);
-    if (row + n - b.row > p.batch_rows) break;
-    end = max(end, row + n);
-    ++b.s1;
-  }
-  b.n = end - b.row;
-  return b;
-}
-
-// The blocks' shares of a batch: n / blocks rows each, the first n % blocks one more.
+// The blocks' shares of the rows: n / blocks each, the first n % blocks one more.
 struct Shares {
   int row, each, more, blocks;
-  UT_DEV Shares(const Batch& b, int blocks_) : row(b.row), blocks(blocks_) {
-    each = b.n / blocks;
-    more = b.n - each * blocks;
+  UT_DEV Shares(const GnormParams& p, int blocks_) : blocks(blocks_) {
+    int n;
+    rows_of_segment(p, 0, row, n);
+    each = ((int)p.n - row) / blocks;
+    more = (int)p.n - row - each * blocks;
   }
   UT_DEV int first(int block) const { return row + each * block + min(block, more); }
   // the block that has row r (in range whatever cu holds)
@@ -188,10 +162,10 @@ struct Shares {
     return max(0, min(c, blocks - 1));
   }
 };
-// The last segment of the batch that starts at or before row r.
-UT_DEV int segment_at(const GnormParams& p, const Batch& b, int r) {
+// The last segment that starts at or before row r.
+UT_DEV int segment_at(const GnormParams& p, int r) {
   if (!p.cu) return 0;
-  int lo = b.s0, hi = b.s1;
+  int lo = 0, hi = p.B;
   while (hi - lo > 1) {
     const int mid = (lo + hi) >> 1;
     if (p.cu[mid] <= r) lo = mid;
@@ -202,9 +176,9 @@ UT_DEV int segment_at(const GnormParams& p, const Batch& b, int r) {
 
 // Calls f(segment, first row, end) for the pieces of rows [a, e).
 template <typename F>
-UT_DEV void for_pieces(const GnormParams& p, const Batch& b, int a, int e, F f) {
+UT_DEV void for_pieces(const GnormParams& p, int a, int e, F f) {
   if (a >= e) return;
-  for (int s = segment_at(p, b, a); s < b.s1; ++s) {
+  for (int s = segment_at(p, a); s < p.B; ++s) {
     int row, n;
     rows_of_segment(p, s, row, n);
     const int lo = max(a, row), hi = min(e, row + n);
@@ -213,7 +187,7 @@ UT_DEV void for_pieces(const GnormParams& p, const Batch& b, int a, int e, F f) 
   }
 }
 
-// The chunks of a block's share of a batch, in the order of the first pass:
+// The chunks of a block's share, in the order of the first pass:
 // pieces ascending, slabs of columns, rows.
 template <int kThreads, int kPer>
 struct Chunks {
@@ -300,9 +274,9 @@ UT_DEV void sync_compute() {  // the computing warps
 
 // Pieces of rows [a, e), last first.
 template <typename F>
-UT_DEV void for_pieces_back(const GnormParams& p, const Batch& b, int a, int e, F f) {
+UT_DEV void for_pieces_back(const GnormParams& p, int a, int e, F f) {
   if (a >= e) return;
-  for (int s = segment_at(p, b, e - 1); s >= b.s0; --s) {
+  for (int s = segment_at(p, e - 1); s >= 0; --s) {
     int row, n;
     rows_of_segment(p, s, row, n);
     const int lo = max(a, row), hi = min(e, row + n);
@@ -311,9 +285,9 @@ UT_DEV void for_pieces_back(const GnormParams& p, const Batch& b, int a, int e, 
   }
 }
 
-// The producer's part of both passes over a batch: tensors x (and dy).
+// The producer's part of both passes: tensors x (and dy).
 template <int kThreads, int kPer, int kTensors>
-UT_DEV void produce(const GnormParams& p, const Batch& b, int a, int e, const Chunks<kThreads, kPer>& ck,
+UT_DEV void produce(const GnormParams& p, int a, int e, const Chunks<kThreads, kPer>& ck,
                     Ring& ring, uint32_t& used, int total, int elem) {
   auto load = [&](int at, int slab, int r, int n) {
     if (!ring.wait_empty(at)) return;
@@ -329,7 +303,7 @@ UT_DEV void produce(const GnormParams& p, const Batch& b, int a, int e, const Ch
       load_rows(dst + ring.slot_bytes / 2, p.dy, p.dys * elem, r, n, slab * kThreads, cols, bar);
   };
   int slot = 0;
-  for_pieces(p, b, a, e, [&](int s, int lo, int hi) {
+  for_pieces(p, a, e, [&](int s, int lo, int hi) {
     for (int slab = 0; slab < ck.slabs; ++slab)
       for (int r = lo; r < hi; r += ck.rows, slot = ring.next(slot)) load(slot, slab, r, min(ck.rows, hi - r));
   });
@@ -337,7 +311,7 @@ UT_DEV void produce(const GnormParams& p, const Batch& b, int a, int e, const Ch
   // backwards; the last `slots` chunks are there
   int i = total - 1;
   slot = ring.before(slot);
-  for_pieces_back(p, b, a, e, [&](int s, int lo, int hi) {
+  for_pieces_back(p, a, e, [&](int s, int lo, int hi) {
     const int n = ck.row_chunks(hi - lo);
     for (int slab = ck.slabs - 1; slab >= 0; --slab)
       for (int c = n - 1; c >= 0; --c, --i, slot = ring.before(slot))
@@ -480,8 +454,7 @@ __global__ void __launch_bounds__(kFwdThreads + 32, 1) gn_fwd_kernel(const Gnorm
   const Chunks<kFwdThreads, kFwdPer> ck(p.C / V);
   prefetch_affine(p);
   Ring ring{st, smem + p.ring_at, p.slots, p.slot_bytes, p.status, p.timeout_ns, 0, 0, false};
-  uint32_t used = 0;  // slots that the producer has loaded
-  float2* part0 = static_cast<float2*>(p.ws);
+  float2* part = static_cast<float2*>(p.ws);  // [blocks + B][G]
   ring_init<kFwdThreads>(st, p.slots);
   if (me == 0 && warp < kFwdThreads / 32) {
     check_cu(p.cu, p.B, p.n, p.status);
@@ -494,199 +467,195 @@ __global__ void __launch_bounds__(kFwdThreads + 32, 1) gn_fwd_kernel(const Gnorm
       }
     }
   }
-  for (int s0 = 0, nb = 0; s0 < p.B; ++nb) {
-    const Batch b = batch_from(p, s0);
-    s0 = b.s1;
-    float2* part = part0 + (int64_t)(nb & 1) * (blocks + p.B) * p.G;  // two batches may be under way
-    const Shares sh(b, blocks);
-    const int a = sh.first(me), e = sh.first(me + 1);
-    int total = 0;  // chunks
-    for_pieces(p, b, a, e, [&](int, int lo, int hi) { total += ck.of_piece(hi - lo); });
-    if (warp == kFwdThreads / 32) {
-      produce<kFwdThreads, kFwdPer, 1>(p, b, a, e, ck, ring, used, total, sizeof(T));
-      continue;
-    }
-    int i = 0, slot = 0;
-    for_pieces(p, b, a, e, [&](int s, int lo, int hi) {
-      const int n = hi - lo;
-      for (int slab = 0; slab < ck.slabs; ++slab) {
-        const Layout<kFwdThreads> L(ck.cv, slab * kFwdThreads);
-        Moments<V> mo;
-        for (int r = 0; r < n; r += ck.rows, ++i, slot = ring.next(slot)) {
-          ring.wait_full(slot);
-          if (L.on) {
-            const uint8_t* src = ring.mem + (int64_t)slot * ring.slot_bytes + (L.lane * L.cols + L.col - slab * kFwdThreads) * 16;
-            const int step = L.lanes * L.cols * 16;
-            uint64_t v[V / 2];
-            if (r + ck.rows <= n) {  // a full chunk
-              uint4 w[kFwdPer];
-#pragma unroll
-              for (int k = 0; k < kFwdPer; ++k) w[k] = *reinterpret_cast<const uint4*>(src + k * step);
-              if (mo.have == 0.f) {
-                Vec<T>::unpack(w[0], v);
-                mo.begin(v);
-              }
-#pragma unroll
-              for (int k = 0; k < kFwdPer; ++k) {
-                Vec<T>::unpack(w[k], v);
-                mo.add(v);
-              }
-              mo.have += (float)kFwdPer;
-            } else {
-              for (int k = 0; k < kFwdPer && r + L.lane + k * L.lanes < n; ++k) {
-                Vec<T>::unpack(*reinterpret_cast<const uint4*>(src + k * step), v);
-                if (mo.have == 0.f) mo.begin(v);
-                mo.add(v);
-                mo.have += 1.f;
-              }
-            }
-            if (mo.have >= (float)kWindow) mo.merge();
-          }
-          if (i + ring.slots < total) ring.release(slot);  // else it stays for the second pass
-        }
-        mo.merge();
-        sync_compute<kFwdThreads>();
-        // over the lanes of a column, a thread a channel
-#pragma unroll
-        for (int c = 0; c < V; ++c) lane_stat[c * kFwdThreads + threadIdx.x] = make_float2(mo.mean[c], mo.m2[c]);
-        sync_compute<kFwdThreads>();
-        const int each = n / L.lanes, more = n - each * L.lanes;  // rows of a lane
-        const float inv = 1.f / (float)n;
-        for (int x = threadIdx.x; x < L.cols * V; x += kFwdThreads) {
-          const int c = x / L.cols, col = x - c * L.cols;
-          const float2* ls = lane_stat + c * kFwdThreads + col;
-          float m = 0.f, q = 0.f;
-#pragma unroll 8
-          for (int l = 0; l < L.lanes; ++l) m = fmaf((float)(each + (l < more)), ls[l * L.cols].x - ls[0].x, m);
-          m = fmaf(m, inv, ls[0].x);
-#pragma unroll 8
-          for (int l = 0; l < L.lanes; ++l) {
-            const float2 t = ls[l * L.cols];
-            q += fmaf((float)(each + (l < more)) * (t.x - m), t.x - m, t.y);
-          }
-          chan[(slab * kFwdThreads + col) * V + c] = make_float2(m, q);
-        }
-      }
-      sync_compute<kFwdThreads>();
-      // over the channels of a group, p.group_lanes threads a group
-      for (int g0 = 0; g0 < p.G; g0 += kFwdThreads / p.group_lanes) {
-        const int g = g0 + threadIdx.x / p.group_lanes, l = threadIdx.x % p.group_lanes;
-        const bool on = g < p.G && threadIdx.x < kFwdThreads / p.group_lanes * p.group_lanes;
-        const float2* cs = chan + g * cpg;
-        float m = 0.f, q = 0.f;
-        if (on)
-          for (int c = l; c < cpg; c += p.group_lanes) m += cs[c].x - cs[0].x;
-        for (int o = p.group_lanes / 2; o; o >>= 1) m += __shfl_xor_sync(0xffffffffu, m, o);
-        if (on) m = fmaf(m, inv_cpg, cs[0].x);
-        if (on)
-          for (int c = l; c < cpg; c += p.group_lanes) {
-            const float2 t = cs[c];
-            q += fmaf((float)n * (t.x - m), t.x - m, t.y);
-          }
-        for (int o = p.group_lanes / 2; o; o >>= 1) q += __shfl_xor_sync(0xffffffffu, q, o);
-        if (on && l == 0) part[(int64_t)(me + s) * p.G + g] = make_float2(m, q);
-      }
-    });
-    cooperative_groups::this_grid().sync();
-    i = total - 1;
-    slot = ring.before(slot);
-    for_pieces_back(p, b, a, e, [&](int s, int lo, int hi) {
-      int row, n;
-      rows_of_segment(p, s, row, n);
-      const int c0 = sh.owner(row), c1 = sh.owner(row + n - 1);
-      sync_compute<kFwdThreads>();
-      // the segment's statistics from its pieces': lanes over the groups, warps
-      // over the blocks (all of a warp's reads in flight), then one warp over the
-      // warps
-      for (int g0 = 0; g0 < p.G; g0 += 32) {
-        const int g = g0 + lane;
-        constexpr int kW = kFwdThreads / 32, kIn = 11;  // 11 x 15 blocks a round
-        Stat t{0.f, 0.f, 0.f};
-        for (int c = c0 + warp; c <= c1; c += kIn * kW) {
-          float2 o[kIn];
-#pragma unroll
-          for (int x = 0; x < kIn; ++x) {
-            const int at = c + x * kW;
-            o[x] = at <= c1 && g < p.G ? part[(int64_t)(at + s) * p.G + g] : make_float2(0.f, 0.f);
-          }
-#pragma unroll
-          for (int x = 0; x < kIn; ++x) {
-            const int at = c + x * kW;
-            if (at <= c1) t.add((float)(min(sh.first(at + 1), row + n) - max(sh.first(at), row)), o[x].x, o[x].y * inv_cpg);
-          }
-        }
-        lane_stat[threadIdx.x] = make_float2(t.mean, t.m2);
-        if (lane == 0) warp_rows[warp] = t.n;
-        sync_compute<kFwdThreads>();
-        if (warp == 0 && g < p.G) {
-          const float inv_n = 1.f / (float)n;
-          float m = 0.f, q = 0.f;
-#pragma unroll
-          for (int x = 1; x < kW; ++x) m = fmaf(warp_rows[x], lane_stat[x * 32 + lane].x - t.mean, m);
-          m = fmaf(m, inv_n, t.mean);
-#pragma unroll
-          for (int x = 0; x < kW; ++x) {
-            const float2 o = lane_stat[x * 32 + lane];
-            q += fmaf(warp_rows[x] * (o.x - m), o.x - m, o.y);
-          }
-          const float r = 1.f / sqrtf(q * inv_n + p.eps);
-          stat[g] = make_float2(m, r);
-          if (me == c0) {
-            p.mean[(int64_t)s * p.G + g] = m;
-            p.rstd[(int64_t)s * p.G + g] = r;
-          }
-        }
-        sync_compute<kFwdThreads>();
-      }
-      const int chunks = ck.row_chunks(hi - lo);
-      for (int slab = ck.slabs - 1; slab >= 0; --slab) {
-        const Layout<kFwdThreads> L(ck.cv, slab * kFwdThreads);
-        Channels<V> ch;
-        if (L.on) ch.load(p, stat, L.col * V);
-        // u = x a + b in bf16, whose inputs are coarser than what folding the mean
-        // into b costs; in fp32 (x - mu) a + beta
-        constexpr bool kFold = sizeof(T) == 2;
-#pragma unroll
-        for (int c = 0; c < V / 2; ++c) {
-          ch.rstd[c] = mul_f32x2(ch.rstd[c], ch.gamma[c]);
-          if (kFold) ch.beta[c] = fma_f32x2(ch.neg_mean[c], ch.rstd[c], ch.beta[c]);
-        }
-        auto row_of = [&](const uint4& w) -> uint4 {
-          uint64_t v[V / 2];
-          Vec<T>::unpack(w, v);
-#pragma unroll
-          for (int x = 0; x < V / 2; ++x) {
-            const uint64_t u = fma_f32x2(sizeof(T) == 2 ? v[x] : add_f32x2(v[x], ch.neg_mean[x]), ch.rstd[x], ch.beta[x]);
-            v[x] = kAct ? mul_f32x2(u, sigmoid2(u)) : u;
-          }
-          return Vec<T>::pack(v);
-        };
-        uint8_t* dst = static_cast<uint8_t*>(p.y) + (int64_t)L.col * 16;
-        for (int c = chunks - 1; c >= 0; --c, --i, slot = ring.before(slot)) {
-          if (total - 1 - i >= ring.slots) ring.wait_full(slot);
-          const int r = lo + c * ck.rows + L.lane;
-          if (L.on) {
-            const uint8_t* src = ring.mem + (int64_t)slot * ring.slot_bytes + (L.lane * L.cols + L.col - slab * kFwdThreads) * 16;
-            const int step = L.lanes * L.cols * 16;
-            uint8_t* to = dst + (int64_t)r * p.ys * (int64_t)sizeof(T);
-            const int64_t to_step = L.lanes * p.ys * (int64_t)sizeof(T);
-            if (lo + (c + 1) * ck.rows <= hi) {  // a full chunk
-              uint4 w[kFwdPer];
-#pragma unroll
-              for (int k = 0; k < kFwdPer; ++k) w[k] = *reinterpret_cast<const uint4*>(src + k * step);
-#pragma unroll
-              for (int k = 0; k < kFwdPer; ++k) store_stream(to + k * to_step, row_of(w[k]));
-            } else {
-              for (int k = 0; k < kFwdPer && r + k * L.lanes < hi; ++k)
-                store_stream(to + k * to_step, row_of(*reinterpret_cast<const uint4*>(src + k * step)));
-            }
-          }
-          ring.release(slot);
-        }
-      }
-    });
+  const Shares sh(p, blocks);
+  const int a = sh.first(me), e = sh.first(me + 1);
+  int total = 0;  // chunks
+  for_pieces(p, a, e, [&](int, int lo, int hi) { total += ck.of_piece(hi - lo); });
+  if (warp == kFwdThreads / 32) {
+    uint32_t used = 0;  // slots loaded
+    produce<kFwdThreads, kFwdPer, 1>(p, a, e, ck, ring, used, total, sizeof(T));
+    ring.finish(used);
+    return;
   }
-  if (warp == kFwdThreads / 32) ring.finish(used);
+  int i = 0, slot = 0;
+  for_pieces(p, a, e, [&](int s, int lo, int hi) {
+    const int n = hi - lo;
+    for (int slab = 0; slab < ck.slabs; ++slab) {
+      const Layout<kFwdThreads> L(ck.cv, slab * kFwdThreads);
+      Moments<V> mo;
+      for (int r = 0; r < n; r += ck.rows, ++i, slot = ring.next(slot)) {
+        ring.wait_full(slot);
+        if (L.on) {
+          const uint8_t* src = ring.mem + (int64_t)slot * ring.slot_bytes + (L.lane * L.cols + L.col - slab * kFwdThreads) * 16;
+          const int step = L.lanes * L.cols * 16;
+          uint64_t v[V / 2];
+          if (r + ck.rows <= n) {  // a full chunk
+            uint4 w[kFwdPer];
+#pragma unroll
+            for (int k = 0; k < kFwdPer; ++k) w[k] = *reinterpret_cast<const uint4*>(src + k * step);
+            if (mo.have == 0.f) {
+              Vec<T>::unpack(w[0], v);
+              mo.begin(v);
+            }
+#pragma unroll
+            for (int k = 0; k < kFwdPer; ++k) {
+              Vec<T>::unpack(w[k], v);
+              mo.add(v);
+            }
+            mo.have += (float)kFwdPer;
+          } else {
+            for (int k = 0; k < kFwdPer && r + L.lane + k * L.lanes < n; ++k) {
+              Vec<T>::unpack(*reinterpret_cast<const uint4*>(src + k * step), v);
+              if (mo.have == 0.f) mo.begin(v);
+              mo.add(v);
+              mo.have += 1.f;
+            }
+          }
+          if (mo.have >= (float)kWindow) mo.merge();
+        }
+        if (i + ring.slots < total) ring.release(slot);  // else it stays for the second pass
+      }
+      mo.merge();
+      sync_compute<kFwdThreads>();
+      // over the lanes of a column, a thread a channel
+#pragma unroll
+      for (int c = 0; c < V; ++c) lane_stat[c * kFwdThreads + threadIdx.x] = make_float2(mo.mean[c], mo.m2[c]);
+      sync_compute<kFwdThreads>();
+      const int each = n / L.lanes, more = n - each * L.lanes;  // rows of a lane
+      const float inv = 1.f / (float)n;
+      for (int x = threadIdx.x; x < L.cols * V; x += kFwdThreads) {
+        const int c = x / L.cols, col = x - c * L.cols;
+        const float2* ls = lane_stat + c * kFwdThreads + col;
+        float m = 0.f, q = 0.f;
+#pragma unroll 8
+        for (int l = 0; l < L.lanes; ++l) m = fmaf((float)(each + (l < more)), ls[l * L.cols].x - ls[0].x, m);
+        m = fmaf(m, inv, ls[0].x);
+#pragma unroll 8
+        for (int l = 0; l < L.lanes; ++l) {
+          const float2 t = ls[l * L.cols];
+          q += fmaf((float)(each + (l < more)) * (t.x - m), t.x - m, t.y);
+        }
+        chan[(slab * kFwdThreads + col) * V + c] = make_float2(m, q);
+      }
+    }
+    sync_compute<kFwdThreads>();
+    // over the channels of a group, p.group_lanes threads a group
+    for (int g0 = 0; g0 < p.G; g0 += kFwdThreads / p.group_lanes) {
+      const int g = g0 + threadIdx.x / p.group_lanes, l = threadIdx.x % p.group_lanes;
+      const bool on = g < p.G && threadIdx.x < kFwdThreads / p.group_lanes * p.group_lanes;
+      const float2* cs = chan + g * cpg;
+      float m = 0.f, q = 0.f;
+      if (on)
+        for (int c = l; c < cpg; c += p.group_lanes) m += cs[c].x - cs[0].x;
+      for (int o = p.group_lanes / 2; o; o >>= 1) m += __shfl_xor_sync(0xffffffffu, m, o);
+      if (on) m = fmaf(m, inv_cpg, cs[0].x);
+      if (on)
+        for (int c = l; c < cpg; c += p.group_lanes) {
+          const float2 t = cs[c];
+          q += fmaf((float)n * (t.x - m), t.x - m, t.y);
+        }
+      for (int o = p.group_lanes / 2; o; o >>= 1) q += __shfl_xor_sync(0xffffffffu, q, o);
+      if (on && l == 0) part[(int64_t)(me + s) * p.G + g] = make_float2(m, q);
+    }
+  });
+  cooperative_groups::this_grid().sync();
+  i = total - 1;
+  slot = ring.before(slot);
+  for_pieces_back(p, a, e, [&](int s, int lo, int hi) {
+    int row, n;
+    rows_of_segment(p, s, row, n);
+    const int c0 = sh.owner(row), c1 = sh.owner(row + n - 1);
+    sync_compute<kFwdThreads>();
+    // the segment's statistics from its pieces': lanes over the groups, warps
+    // over the blocks (all of a warp's reads in flight), then one warp over the
+    // warps
+    for (int g0 = 0; g0 < p.G; g0 += 32) {
+      const int g = g0 + lane;
+      constexpr int kW = kFwdThreads / 32, kIn = 11;  // 11 x 15 blocks a round
+      Stat t{0.f, 0.f, 0.f};
+      for (int c = c0 + warp; c <= c1; c += kIn * kW) {
+        float2 o[kIn];
+#pragma unroll
+        for (int x = 0; x < kIn; ++x) {
+          const int at = c + x * kW;
+          o[x] = at <= c1 && g < p.G ? part[(int64_t)(at + s) * p.G + g] : make_float2(0.f, 0.f);
+        }
+#pragma unroll
+        for (int x = 0; x < kIn; ++x) {
+          const int at = c + x * kW;
+          if (at <= c1) t.add((float)(min(sh.first(at + 1), row + n) - max(sh.first(at), row)), o[x].x, o[x].y * inv_cpg);
+        }
+      }
+      lane_stat[threadIdx.x] = make_float2(t.mean, t.m2);
+      if (lane == 0) warp_rows[warp] = t.n;
+      sync_compute<kFwdThreads>();
+      if (warp == 0 && g < p.G) {
+        const float inv_n = 1.f / (float)n;
+        float m = 0.f, q = 0.f;
+#pragma unroll
+        for (int x = 1; x < kW; ++x) m = fmaf(warp_rows[x], lane_stat[x * 32 + lane].x - t.mean, m);
+        m = fmaf(m, inv_n, t.mean);
+#pragma unroll
+        for (int x = 0; x < kW; ++x) {
+          const float2 o = lane_stat[x * 32 + lane];
+          q += fmaf(warp_rows[x] * (o.x - m), o.x - m, o.y);
+        }
+        const float r = 1.f / sqrtf(q * inv_n + p.eps);
+        stat[g] = make_float2(m, r);
+        if (me == c0) {
+          p.mean[(int64_t)s * p.G + g] = m;
+          p.rstd[(int64_t)s * p.G + g] = r;
+        }
+      }
+      sync_compute<kFwdThreads>();
+    }
+    const int chunks = ck.row_chunks(hi - lo);
+    for (int slab = ck.slabs - 1; slab >= 0; --slab) {
+      const Layout<kFwdThreads> L(ck.cv, slab * kFwdThreads);
+      Channels<V> ch;
+      if (L.on) ch.load(p, stat, L.col * V);
+      // u = x a + b in bf16, whose inputs are coarser than what folding the mean
+      // into b costs; in fp32 (x - mu) a + beta
+      constexpr bool kFold = sizeof(T) == 2;
+#pragma unroll
+      for (int c = 0; c < V / 2; ++c) {
+        ch.rstd[c] = mul_f32x2(ch.rstd[c], ch.gamma[c]);
+        if (kFold) ch.beta[c] = fma_f32x2(ch.neg_mean[c], ch.rstd[c], ch.beta[c]);
+      }
+      auto row_of = [&](const uint4& w) -> uint4 {
+        uint64_t v[V / 2];
+        Vec<T>::unpack(w, v);
+#pragma unroll
+        for (int x = 0; x < V / 2; ++x) {
+          const uint64_t u = fma_f32x2(sizeof(T) == 2 ? v[x] : add_f32x2(v[x], ch.neg_mean[x]), ch.rstd[x], ch.beta[x]);
+          v[x] = kAct ? mul_f32x2(u, sigmoid2(u)) : u;
+        }
+        return Vec<T>::pack(v);
+      };
+      uint8_t* dst = static_cast<uint8_t*>(p.y) + (int64_t)L.col * 16;
+      for (int c = chunks - 1; c >= 0; --c, --i, slot = ring.before(slot)) {
+        if (total - 1 - i >= ring.slots) ring.wait_full(slot);
+        const int r = lo + c * ck.rows + L.lane;
+        if (L.on) {
+          const uint8_t* src = ring.mem + (int64_t)slot * ring.slot_bytes + (L.lane * L.cols + L.col - slab * kFwdThreads) * 16;
+          const int step = L.lanes * L.cols * 16;
+          uint8_t* to = dst + (int64_t)r * p.ys * (int64_t)sizeof(T);
+          const int64_t to_step = L.lanes * p.ys * (int64_t)sizeof(T);
+          if (lo + (c + 1) * ck.rows <= hi) {  // a full chunk
+            uint4 w[kFwdPer];
+#pragma unroll
+            for (int k = 0; k < kFwdPer; ++k) w[k] = *reinterpret_cast<const uint4*>(src + k * step);
+#pragma unroll
+            for (int k = 0; k < kFwdPer; ++k) store_stream(to + k * to_step, row_of(w[k]));
+          } else {
+            for (int k = 0; k < kFwdPer && r + k * L.lanes < hi; ++k)
+              store_stream(to + k * to_step, row_of(*reinterpret_cast<const uint4*>(src + k * step)));
+          }
+        }
+        ring.release(slot);
+      }
+    }
+  });
 }
 
 // ------------------------------------------------------------------ backward
@@ -717,9 +686,8 @@ __global__ void __launch_bounds__(kBwdThreads + 32, 1) gn_bwd_kernel(const Gnorm
   const Chunks<kBwdThreads, kBwdPer> ck(p.C / V);
   prefetch_affine(p);
   Ring ring{st, smem + p.ring_at, p.slots, p.slot_bytes, p.status, p.timeout_ns, 0, 0, false};
-  uint32_t used = 0;  // slots that the producer has loaded
-  float2* part0 = static_cast<float2*>(p.ws);                // [2][blocks + B][G]
-  float2* sums = part0 + (int64_t)2 * (blocks + p.B) * p.G;  // [blocks][C]
+  float2* part = static_cast<float2*>(p.ws);            // [blocks + B][G]
+  float2* sums = part + (int64_t)(blocks + p.B) * p.G;  // [blocks][C]
   ring_init<kBwdThreads>(st, p.slots);
   if (warp < kBwdThreads / 32) {
     if (me == 0) check_cu(p.cu, p.B, p.n, p.status);
@@ -729,235 +697,229 @@ __global__ void __launch_bounds__(kBwdThreads + 32, 1) gn_bwd_kernel(const Gnorm
     for (int g = threadIdx.x; g < p.G; g += kBwdThreads)
       stat[g] = make_float2(p.mean[(int64_t)s * p.G + g], p.rstd[(int64_t)s * p.G + g]);
   };
-  for (int s0 = 0, nb = 0; s0 < p.B; ++nb) {
-    const Batch b = batch_from(p, s0);
-    s0 = b.s1;
-    float2* part = part0 + (int64_t)(nb & 1) * (blocks + p.B) * p.G;
-    const Shares sh(b, blocks);
-    const int a = sh.first(me), e = sh.first(me + 1);
-    int total = 0;  // chunks
-    for_pieces(p, b, a, e, [&](int, int lo, int hi) { total += ck.of_piece(hi - lo); });
-    if (warp == kBwdThreads / 32) {
-      produce<kBwdThreads, kBwdPer, 2>(p, b, a, e, ck, ring, used, total, sizeof(T));
-      continue;
-    }
-    int i = 0, slot = 0;
-    for_pieces(p, b, a, e, [&](int s, int lo, int hi) {
-      const int n = hi - lo;
-      sync_compute<kBwdThreads>();
-      load_stat(s);
-      sync_compute<kBwdThreads>();
-      for (int slab = 0; slab < ck.slabs; ++slab) {
-        const Layout<kBwdThreads> L(ck.cv, slab * kBwdThreads);
-        uint64_t t1[V / 2], t2[V / 2];
+  const Shares sh(p, blocks);
+  const int a = sh.first(me), e = sh.first(me + 1);
+  int total = 0;  // chunks
+  for_pieces(p, a, e, [&](int, int lo, int hi) { total += ck.of_piece(hi - lo); });
+  if (warp == kBwdThreads / 32) {
+    uint32_t used = 0;  // slots loaded
+    produce<kBwdThreads, kBwdPer, 2>(p, a, e, ck, ring, used, total, sizeof(T));
+    ring.finish(used);
+    return;
+  }
+  int i = 0, slot = 0;
+  for_pieces(p, a, e, [&](int s, int lo, int hi) {
+    const int n = hi - lo;
+    sync_compute<kBwdThreads>();
+    load_stat(s);
+    sync_compute<kBwdThreads>();
+    for (int slab = 0; slab < ck.slabs; ++slab) {
+      const Layout<kBwdThreads> L(ck.cv, slab * kBwdThreads);
+      uint64_t t1[V / 2], t2[V / 2];
 #pragma unroll
-        for (int c = 0; c < V / 2; ++c) t1[c] = t2[c] = 0;
-        Channels<V> ch;
-        if (L.on) ch.load(p, stat, L.col * V);
-        for (int r = 0; r < n; r += ck.rows, ++i, slot = ring.next(slot)) {
-          ring.wait_full(slot);
-          if (L.on) {
-            const uint8_t* src = ring.mem + (int64_t)slot * ring.slot_bytes + (L.lane * L.cols + L.col - slab * kBwdThreads) * 16;
-            uint64_t b1[V / 2], b2[V / 2];
+      for (int c = 0; c < V / 2; ++c) t1[c] = t2[c] = 0;
+      Channels<V> ch;
+      if (L.on) ch.load(p, stat, L.col * V);
+      for (int r = 0; r < n; r += ck.rows, ++i, slot = ring.next(slot)) {
+        ring.wait_full(slot);
+        if (L.on) {
+          const uint8_t* src = ring.mem + (int64_t)slot * ring.slot_bytes + (L.lane * L.cols + L.col - slab * kBwdThreads) * 16;
+          uint64_t b1[V / 2], b2[V / 2];
 #pragma unroll
-            for (int c = 0; c < V / 2; ++c) b1[c] = b2[c] = 0;
-            const int step = L.lanes * L.cols * 16;
-            auto row = [&](const uint4& wx, const uint4& wg) {
-              uint64_t v[V / 2], g[V / 2];
-              Vec<T>::unpack(wx, v);
-              Vec<T>::unpack(wg, g);
-#pragma unroll
-              for (int c = 0; c < V / 2; ++c) {
-                uint64_t xh;
-                const uint64_t du = du_of<kAct>(v[c], g[c], ch.neg_mean[c], ch.rstd[c], ch.gamma[c], ch.beta[c], xh);
-                b1[c] = add_f32x2(b1[c], du);
-                b2[c] = fma_f32x2(du, xh, b2[c]);
-              }
-            };
-            if (r + ck.rows <= n) {  // a full chunk
-              uint4 wx[kBwdPer], wg[kBwdPer];
-#pragma unroll
-              for (int k = 0; k < kBwdPer; ++k) {
-                wx[k] = *reinterpret_cast<const uint4*>(src + k * step);
-                wg[k] = *reinterpret_cast<const uint4*>(src + k * step + ring.slot_bytes / 2);
-              }
-#pragma unroll
-              for (int k = 0; k < kBwdPer; ++k) row(wx[k], wg[k]);
-            } else {
-#pragma unroll 1
-              for (int k = 0; k < kBwdPer && r + L.lane + k * L.lanes < n; ++k)
-                row(*reinterpret_cast<const uint4*>(src + k * step),
-                    *reinterpret_cast<const uint4*>(src + k * step + ring.slot_bytes / 2));
-            }
+          for (int c = 0; c < V / 2; ++c) b1[c] = b2[c] = 0;
+          const int step = L.lanes * L.cols * 16;
+          auto row = [&](const uint4& wx, const uint4& wg) {
+            uint64_t v[V / 2], g[V / 2];
+            Vec<T>::unpack(wx, v);
+            Vec<T>::unpack(wg, g);
 #pragma unroll
             for (int c = 0; c < V / 2; ++c) {
-              t1[c] = add_f32x2(t1[c], b1[c]);
-              t2[c] = add_f32x2(t2[c], b2[c]);
+              uint64_t xh;
+              const uint64_t du = du_of<kAct>(v[c], g[c], ch.neg_mean[c], ch.rstd[c], ch.gamma[c], ch.beta[c], xh);
+              b1[c] = add_f32x2(b1[c], du);
+              b2[c] = fma_f32x2(du, xh, b2[c]);
             }
-          }
-          if (i + ring.slots < total) ring.release(slot);  // else it stays for the second pass
-        }
-        sync_compute<kBwdThreads>();
-        float s1[V], s2[V];
+          };
+          if (r + ck.rows <= n) {  // a full chunk
+            uint4 wx[kBwdPer], wg[kBwdPer];
 #pragma unroll
-        for (int c = 0; c < V / 2; ++c) {
-          unpack_f32x2(t1[c], s1[2 * c], s1[2 * c + 1]);
-          unpack_f32x2(t2[c], s2[2 * c], s2[2 * c + 1]);
-        }
-        // over the lanes of a column, a thread a channel
+            for (int k = 0; k < kBwdPer; ++k) {
+              wx[k] = *reinterpret_cast<const uint4*>(src + k * step);
+              wg[k] = *reinterpret_cast<const uint4*>(src + k * step + ring.slot_bytes / 2);
+            }
 #pragma unroll
-        for (int c = 0; c < V; ++c) lane_sum[c * kBwdThreads + threadIdx.x] = make_float2(s1[c], s2[c]);
-        sync_compute<kBwdThreads>();
-        for (int x = threadIdx.x; x < L.cols * V; x += kBwdThreads) {
-          const int c = x / L.cols, col = x - c * L.cols;
-          const float2* ls = lane_sum + c * kBwdThreads + col;
-          float2 t = make_float2(0.f, 0.f);
-#pragma unroll 8
-          for (int l = 0; l < L.lanes; ++l) {
-            const float2 o = ls[l * L.cols];
-            t.x += o.x;
-            t.y += o.y;
-          }
-          const int at = (slab * kBwdThreads + col) * V + c;
-          chan[at] = t;
-          all[at] = make_float2(all[at].x + t.x, all[at].y + t.y);
-        }
-      }
-      sync_compute<kBwdThreads>();
-      // over the channels of a group, p.group_lanes threads a group
-      for (int g0 = 0; g0 < p.G; g0 += kBwdThreads / p.group_lanes) {
-        const int g = g0 + threadIdx.x / p.group_lanes, l = threadIdx.x % p.group_lanes;
-        const bool on = g < p.G && threadIdx.x < kBwdThreads / p.group_lanes * p.group_lanes;
-        float2 t = make_float2(0.f, 0.f);
-        if (on)
-          for (int c = g * cpg + l; c < (g + 1) * cpg; c += p.group_lanes) {
-            const float w = p.gamma ? p.gamma[c] : 1.f;
-            t.x = fmaf(w, chan[c].x, t.x);
-            t.y = fmaf(w, chan[c].y, t.y);
-          }
-        for (int o = p.group_lanes / 2; o; o >>= 1) {
-          t.x += __shfl_xor_sync(0xffffffffu, t.x, o);
-          t.y += __shfl_xor_sync(0xffffffffu, t.y, o);
-        }
-        if (on && l == 0) part[(int64_t)(me + s) * p.G + g] = t;
-      }
-    });
-    if (s0 >= p.B) {  // the last batch: this block's sums over all segments are complete
-      sync_compute<kBwdThreads>();
-      for (int c = threadIdx.x; c < p.C; c += kBwdThreads) sums[(int64_t)me * p.C + c] = all[c];
-    }
-    cooperative_groups::this_grid().sync();
-    if (s0 >= p.B && (p.dgamma || p.dbeta)) {  // a warp a channel, lanes over the blocks
-      for (int c = me + warp * blocks; c < p.C; c += blocks * (kBwdThreads / 32)) {
-        float2 t = make_float2(0.f, 0.f);
-        for (int x = lane; x < blocks; x += 32) {
-          const float2 u = sums[(int64_t)x * p.C + c];
-          t.x += u.x;
-          t.y += u.y;
-        }
-        t.x = warp_sum(t.x);
-        t.y = warp_sum(t.y);
-        if (lane == 0) {
-          if (p.dbeta) p.dbeta[c] = t.x;
-          if (p.dgamma) p.dgamma[c] = t.y;
-        }
-      }
-    }
-    i = total - 1;
-    slot = ring.before(slot);
-    for_pieces_back(p, b, a, e, [&](int s, int lo, int hi) {
-      int row, n;
-      rows_of_segment(p, s, row, n);
-      const int c0 = sh.owner(row), c1 = sh.owner(row + n - 1);
-      const float inv = 1.f / ((float)n * (float)cpg);
-      sync_compute<kBwdThreads>();
-      load_stat(s);
-      // the segment's sums from its pieces': lanes over the groups, warps over
-      // the blocks, then one warp over the warps
-      for (int g0 = 0; g0 < p.G; g0 += 32) {
-        const int g = g0 + lane;
-        float2 t = make_float2(0.f, 0.f);
-        constexpr int kW = kBwdThreads / 32, kIn = 14;  // 14 x 11 blocks a round
-        for (int c = c0 + warp; c <= c1; c += kIn * kW) {
-          float2 o[kIn];
-#pragma unroll
-          for (int x = 0; x < kIn; ++x) {
-            const int at = c + x * kW;
-            const bool there = at <= c1 && g < p.G && min(sh.first(at + 1), row + n) > max(sh.first(at), row);
-            o[x] = there ? part[(int64_t)(at + s) * p.G + g] : make_float2(0.f, 0.f);
-          }
-#pragma unroll
-          for (int x = 0; x < kIn; ++x) {
-            t.x += o[x].x;
-            t.y += o[x].y;
-          }
-        }
-        lane_sum[threadIdx.x] = t;
-        sync_compute<kBwdThreads>();
-        if (warp == 0 && g < p.G) {
-#pragma unroll
-          for (int x = 1; x < kW; ++x) {
-            const float2 o = lane_sum[x * 32 + lane];
-            t.x += o.x;
-            t.y += o.y;
-          }
-          coef[g] = make_float2(t.x * inv, t.y * inv);
-        }
-        sync_compute<kBwdThreads>();
-      }
-      const int chunks = ck.row_chunks(hi - lo);
-      for (int slab = ck.slabs - 1; slab >= 0; --slab) {
-        const Layout<kBwdThreads> L(ck.cv, slab * kBwdThreads);
-        Channels<V> ch;
-        Channels<V> ab;  // -a / M and b / M (the affine is not used)
-        if (L.on) {
-          ch.load(p, stat, L.col * V);
-          ab.load(p, coef, L.col * V);
-        }
-        uint8_t* dst = static_cast<uint8_t*>(p.dx) + (int64_t)L.col * 16;
-        for (int c = chunks - 1; c >= 0; --c, --i, slot = ring.before(slot)) {
-          if (total - 1 - i >= ring.slots) ring.wait_full(slot);
-          const int r = lo + c * ck.rows + L.lane;
-          if (L.on) {
-            const uint8_t* src = ring.mem + (int64_t)slot * ring.slot_bytes + (L.lane * L.cols + L.col - slab * kBwdThreads) * 16;
-            const int step = L.lanes * L.cols * 16;
-            uint8_t* to = dst + (int64_t)r * p.dxs * (int64_t)sizeof(T);
-            const int64_t to_step = L.lanes * p.dxs * (int64_t)sizeof(T);
-            auto row = [&](const uint4& wx, const uint4& wg) -> uint4 {
-              uint64_t v[V / 2], g[V / 2];
-              Vec<T>::unpack(wx, v);
-              Vec<T>::unpack(wg, g);
-#pragma unroll
-              for (int x = 0; x < V / 2; ++x) {
-                uint64_t xh;
-                const uint64_t du = du_of<kAct>(v[x], g[x], ch.neg_mean[x], ch.rstd[x], ch.gamma[x], ch.beta[x], xh);
-                const uint64_t t = fma_f32x2(ch.gamma[x], du, ab.neg_mean[x]);
-                v[x] = mul_f32x2(ch.rstd[x], fma_f32x2(mul_f32x2(xh, both(-1.f)), ab.rstd[x], t));
-              }
-              return Vec<T>::pack(v);
-            };
-            if (lo + (c + 1) * ck.rows <= hi) {  // a full chunk
-              uint4 wx[kBwdPer], wg[kBwdPer];
-#pragma unroll
-              for (int k = 0; k < kBwdPer; ++k) {
-                wx[k] = *reinterpret_cast<const uint4*>(src + k * step);
-                wg[k] = *reinterpret_cast<const uint4*>(src + k * step + ring.slot_bytes / 2);
-              }
-#pragma unroll
-              for (int k = 0; k < kBwdPer; ++k) store_stream(to + k * to_step, row(wx[k], wg[k]));
-            } else {
+            for (int k = 0; k < kBwdPer; ++k) row(wx[k], wg[k]);
+          } else {
 #pragma unroll 1
-              for (int k = 0; k < kBwdPer && r + k * L.lanes < hi; ++k)
-                store_stream(to + k * to_step, row(*reinterpret_cast<const uint4*>(src + k * step),
-                                                   *reinterpret_cast<const uint4*>(src + k * step + ring.slot_bytes / 2)));
-            }
+            for (int k = 0; k < kBwdPer && r + L.lane + k * L.lanes < n; ++k)
+              row(*reinterpret_cast<const uint4*>(src + k * step),
+                  *reinterpret_cast<const uint4*>(src + k * step + ring.slot_bytes / 2));
           }
-          ring.release(slot);
+#pragma unroll
+          for (int c = 0; c < V / 2; ++c) {
+            t1[c] = add_f32x2(t1[c], b1[c]);
+            t2[c] = add_f32x2(t2[c], b2[c]);
+          }
+        }
+        if (i + ring.slots < total) ring.release(slot);  // else it stays for the second pass
+      }
+      sync_compute<kBwdThreads>();
+      float s1[V], s2[V];
+#pragma unroll
+      for (int c = 0; c < V / 2; ++c) {
+        unpack_f32x2(t1[c], s1[2 * c], s1[2 * c + 1]);
+        unpack_f32x2(t2[c], s2[2 * c], s2[2 * c + 1]);
+      }
+      // over the lanes of a column, a thread a channel
+#pragma unroll
+      for (int c = 0; c < V; ++c) lane_sum[c * kBwdThreads + threadIdx.x] = make_float2(s1[c], s2[c]);
+      sync_compute<kBwdThreads>();
+      for (int x = threadIdx.x; x < L.cols * V; x += kBwdThreads) {
+        const int c = x / L.cols, col = x - c * L.cols;
+        const float2* ls = lane_sum + c * kBwdThreads + col;
+        float2 t = make_float2(0.f, 0.f);
+#pragma unroll 8
+        for (int l = 0; l < L.lanes; ++l) {
+          const float2 o = ls[l * L.cols];
+          t.x += o.x;
+          t.y += o.y;
+        }
+        const int at = (slab * kBwdThreads + col) * V + c;
+        chan[at] = t;
+        all[at] = make_float2(all[at].x + t.x, all[at].y + t.y);
+      }
+    }
+    sync_compute<kBwdThreads>();
+    // over the channels of a group, p.group_lanes threads a group
+    for (int g0 = 0; g0 < p.G; g0 += kBwdThreads / p.group_lanes) {
+      const int g = g0 + threadIdx.x / p.group_lanes, l = threadIdx.x % p.group_lanes;
+      const bool on = g < p.G && threadIdx.x < kBwdThreads / p.group_lanes * p.group_lanes;
+      float2 t = make_float2(0.f, 0.f);
+      if (on)
+        for (int c = g * cpg + l; c < (g + 1) * cpg; c += p.group_lanes) {
+          const float w = p.gamma ? p.gamma[c] : 1.f;
+          t.x = fmaf(w, chan[c].x, t.x);
+          t.y = fmaf(w, chan[c].y, t.y);
+        }
+      for (int o = p.group_lanes / 2; o; o >>= 1) {
+        t.x += __shfl_xor_sync(0xffffffffu, t.x, o);
+        t.y += __shfl_xor_sync(0xffffffffu, t.y, o);
+      }
+      if (on && l == 0) part[(int64_t)(me + s) * p.G + g] = t;
+    }
+  });
+  sync_compute<kBwdThreads>();
+  for (int c = threadIdx.x; c < p.C; c += kBwdThreads) sums[(int64_t)me * p.C + c] = all[c];
+  cooperative_groups::this_grid().sync();
+  if (p.dgamma || p.dbeta) {  // a warp a channel, lanes over the blocks
+    for (int c = me + warp * blocks; c < p.C; c += blocks * (kBwdThreads / 32)) {
+      float2 t = make_float2(0.f, 0.f);
+      for (int x = lane; x < blocks; x += 32) {
+        const float2 u = sums[(int64_t)x * p.C + c];
+        t.x += u.x;
+        t.y += u.y;
+      }
+      t.x = warp_sum(t.x);
+      t.y = warp_sum(t.y);
+      if (lane == 0) {
+        if (p.dbeta) p.dbeta[c] = t.x;
+        if (p.dgamma) p.dgamma[c] = t.y;
+      }
+    }
+  }
+  i = total - 1;
+  slot = ring.before(slot);
+  for_pieces_back(p, a, e, [&](int s, int lo, int hi) {
+    int row, n;
+    rows_of_segment(p, s, row, n);
+    const int c0 = sh.owner(row), c1 = sh.owner(row + n - 1);
+    const float inv = 1.f / ((float)n * (float)cpg);
+    sync_compute<kBwdThreads>();
+    load_stat(s);
+    // the segment's sums from its pieces': lanes over the groups, warps over
+    // the blocks, then one warp over the warps
+    for (int g0 = 0; g0 < p.G; g0 += 32) {
+      const int g = g0 + lane;
+      float2 t = make_float2(0.f, 0.f);
+      constexpr int kW = kBwdThreads / 32, kIn = 14;  // 14 x 11 blocks a round
+      for (int c = c0 + warp; c <= c1; c += kIn * kW) {
+        float2 o[kIn];
+#pragma unroll
+        for (int x = 0; x < kIn; ++x) {
+          const int at = c + x * kW;
+          const bool there = at <= c1 && g < p.G && min(sh.first(at + 1), row + n) > max(sh.first(at), row);
+          o[x] = there ? part[(int64_t)(at + s) * p.G + g] : make_float2(0.f, 0.f);
+        }
+#pragma unroll
+        for (int x = 0; x < kIn; ++x) {
+          t.x += o[x].x;
+          t.y += o[x].y;
         }
       }
-    });
-  }
-  if (warp == kBwdThreads / 32) ring.finish(used);
+      lane_sum[threadIdx.x] = t;
+      sync_compute<kBwdThreads>();
+      if (warp == 0 && g < p.G) {
+#pragma unroll
+        for (int x = 1; x < kW; ++x) {
+          const float2 o = lane_sum[x * 32 + lane];
+          t.x += o.x;
+          t.y += o.y;
+        }
+        coef[g] = make_float2(t.x * inv, t.y * inv);
+      }
+      sync_compute<kBwdThreads>();
+    }
+    const int chunks = ck.row_chunks(hi - lo);
+    for (int slab = ck.slabs - 1; slab >= 0; --slab) {
+      const Layout<kBwdThreads> L(ck.cv, slab * kBwdThreads);
+      Channels<V> ch;
+      Channels<V> ab;  // -a / M and b / M (the affine is not used)
+      if (L.on) {
+        ch.load(p, stat, L.col * V);
+        ab.load(p, coef, L.col * V);
+      }
+      uint8_t* dst = static_cast<uint8_t*>(p.dx) + (int64_t)L.col * 16;
+      for (int c = chunks - 1; c >= 0; --c, --i, slot = ring.before(slot)) {
+        if (total - 1 - i >= ring.slots) ring.wait_full(slot);
+        const int r = lo + c * ck.rows + L.lane;
+        if (L.on) {
+          const uint8_t* src = ring.mem + (int64_t)slot * ring.slot_bytes + (L.lane * L.cols + L.col - slab * kBwdThreads) * 16;
+          const int step = L.lanes * L.cols * 16;
+          uint8_t* to = dst + (int64_t)r * p.dxs * (int64_t)sizeof(T);
+          const int64_t to_step = L.lanes * p.dxs * (int64_t)sizeof(T);
+          auto row = [&](const uint4& wx, const uint4& wg) -> uint4 {
+            uint64_t v[V / 2], g[V / 2];
+            Vec<T>::unpack(wx, v);
+            Vec<T>::unpack(wg, g);
+#pragma unroll
+            for (int x = 0; x < V / 2; ++x) {
+              uint64_t xh;
+              const uint64_t du = du_of<kAct>(v[x], g[x], ch.neg_mean[x], ch.rstd[x], ch.gamma[x], ch.beta[x], xh);
+              const uint64_t t = fma_f32x2(ch.gamma[x], du, ab.neg_mean[x]);
+              v[x] = mul_f32x2(ch.rstd[x], fma_f32x2(mul_f32x2(xh, both(-1.f)), ab.rstd[x], t));
+            }
+            return Vec<T>::pack(v);
+          };
+          if (lo + (c + 1) * ck.rows <= hi) {  // a full chunk
+            uint4 wx[kBwdPer], wg[kBwdPer];
+#pragma unroll
+            for (int k = 0; k < kBwdPer; ++k) {
+              wx[k] = *reinterpret_cast<const uint4*>(src + k * step);
+              wg[k] = *reinterpret_cast<const uint4*>(src + k * step + ring.slot_bytes / 2);
+            }
+#pragma unroll
+            for (int k = 0; k < kBwdPer; ++k) store_stream(to + k * to_step, row(wx[k], wg[k]));
+          } else {
+#pragma unroll 1
+            for (int k = 0; k < kBwdPer && r + k * L.lanes < hi; ++k)
+              store_stream(to + k * to_step, row(*reinterpret_cast<const uint4*>(src + k * step),
+                                                 *reinterpret_cast<const uint4*>(src + k * step + ring.slot_bytes / 2)));
+          }
+        }
+        ring.release(slot);
+      }
+    }
+  });
 }
 
 // ----------------------------------------------------------------- launchers
@@ -979,7 +941,6 @@ cudaError_t launch(F kern, GnormParams p, size_t fixed, int tensors, int threads
   // threads a group of channels is summed by: all groups in one round if they fit
   p.group_lanes = 32;
   while (p.group_lanes > 1 && p.group_lanes * p.G > threads) p.group_lanes /= 2;
-  p.batch_rows = (int)(kBatchBytes / ((int64_t)p.C * elem * tensors));
   const size_t smem = fixed + (size_t)p.slots * p.slot_bytes;
   cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
   if (e != cudaSuccess) return e;
@@ -1012,7 +973,7 @@ cudaError_t bwd(const GnormParams& p, cudaStream_t s) {
 }  // namespace
 
 size_t gnorm_ws(const GnormParams& p, bool backward) {
-  const size_t part = (size_t)2 * (p.sms + p.B) * p.G * sizeof(float2);
+  const size_t part = (size_t)(p.sms + p.B) * p.G * sizeof(float2);
   return part + (backward ? (size_t)p.sms * p.C * sizeof(float2) : 0);
 }
 

@@ -16,7 +16,7 @@ struct GnormParams {
   int64_t xs, ys, dys, dxs;                // elements between rows
   int B, C, G, act;
   float eps;
-  int batch_rows, group_lanes;             // rows of a batch of segments; threads that sum a group
+  int group_lanes;                         // threads that sum a group
   int slots, slot_bytes, ring_at;          // the ring in shared memory
   uint64_t timeout_ns;
   void* ws;
