@@ -39,6 +39,7 @@
 
 #include "common.cuh"
 #include "gnorm.cuh"
+#include "gnorm_rows.cuh"
 #include "kernels.h"
 #include "pairs.cuh"
 #include "segments.cuh"
@@ -47,10 +48,6 @@ namespace ut {
 
 namespace {
 
-// threads that compute; with the producer warp after them a multiple of four warps
-// (128 and 168 registers a thread)
-constexpr int kFwdThreads = 480, kBwdThreads = 352;
-constexpr int kFwdPer = 4, kBwdPer = 4;              // rows of a chunk for each thread
 constexpr int kWindow = 16;                          // rows summed before they are merged (forward)
 constexpr int kMaxSlots = 16;
 constexpr size_t kSmem = 225 * 1024;                 // with 2 KB of static shared memory
@@ -121,21 +118,6 @@ struct Stat {
   }
 };
 
-// A block's threads over a row: `cols` 16-byte columns from col0, `lanes` rows
-// at a time.
-template <int kThreads>
-struct Layout {
-  int cols, lanes, col, lane;
-  bool on;
-  UT_DEV Layout(int cv, int col0) {
-    cols = min(cv - col0, kThreads);
-    lanes = kThreads / cols;
-    col = col0 + threadIdx.x % cols;
-    lane = threadIdx.x / cols;
-    on = lane < lanes;
-  }
-  };
-
 // Row counts fit 32 bits (at most 2^30 rows): 64-bit divisions cost hundreds
 // of cycles each, on the path of every launch.
 UT_DEV void rows_of_segment(const GnormParams& p, int s, int& row, int& n) {
@@ -186,23 +168,6 @@ UT_DEV void for_pieces(const GnormParams& p, int a, int e, F f) {
     if (lo < hi) f(s, lo, hi);
   }
 }
-
-// The chunks of a block's share, in the order of the first pass:
-// pieces ascending, slabs of columns, rows.
-template <int kThreads, int kPer>
-struct Chunks {
-  int cv, slabs, cols;  // 16-byte columns of a row, slabs, columns of a (full) slab
-  int rows;             // of a full chunk
-  UT_DEV explicit Chunks(int cv_) {
-    cv = cv_;
-    cols = min(cv, kThreads);
-    slabs = (cv + kThreads - 1) / kThreads;
-    rows = kThreads / cols * kPer;
-  }
-  UT_DEV int slab_cols(int slab) const { return min(cols, cv - slab * kThreads); }
-  UT_DEV int row_chunks(int n) const { return (n + rows - 1) / rows; }
-  UT_DEV int of_piece(int n) const { return slabs * row_chunks(n); }
-};
 
 struct RingState {
   uint64_t full[kMaxSlots], empty[kMaxSlots];
@@ -481,7 +446,7 @@ __global__ void __launch_bounds__(kFwdThreads + 32, 1) gn_fwd_kernel(const Gnorm
   for_pieces(p, a, e, [&](int s, int lo, int hi) {
     const int n = hi - lo;
     for (int slab = 0; slab < ck.slabs; ++slab) {
-      const Layout<kFwdThreads> L(ck.cv, slab * kFwdThreads);
+      const Layout<kFwdThreads, kFwdPer> L(ck, slab, threadIdx.x);
       Moments<V> mo;
       for (int r = 0; r < n; r += ck.rows, ++i, slot = ring.next(slot)) {
         ring.wait_full(slot);
@@ -611,7 +576,7 @@ __global__ void __launch_bounds__(kFwdThreads + 32, 1) gn_fwd_kernel(const Gnorm
     }
     const int chunks = ck.row_chunks(hi - lo);
     for (int slab = ck.slabs - 1; slab >= 0; --slab) {
-      const Layout<kFwdThreads> L(ck.cv, slab * kFwdThreads);
+      const Layout<kFwdThreads, kFwdPer> L(ck, slab, threadIdx.x);
       Channels<V> ch;
       if (L.on) ch.load(p, stat, L.col * V);
       // u = x a + b in bf16, whose inputs are coarser than what folding the mean
@@ -714,7 +679,7 @@ __global__ void __launch_bounds__(kBwdThreads + 32, 1) gn_bwd_kernel(const Gnorm
     load_stat(s);
     sync_compute<kBwdThreads>();
     for (int slab = 0; slab < ck.slabs; ++slab) {
-      const Layout<kBwdThreads> L(ck.cv, slab * kBwdThreads);
+      const Layout<kBwdThreads, kBwdPer> L(ck, slab, threadIdx.x);
       uint64_t t1[V / 2], t2[V / 2];
 #pragma unroll
       for (int c = 0; c < V / 2; ++c) t1[c] = t2[c] = 0;
@@ -871,7 +836,7 @@ __global__ void __launch_bounds__(kBwdThreads + 32, 1) gn_bwd_kernel(const Gnorm
     }
     const int chunks = ck.row_chunks(hi - lo);
     for (int slab = ck.slabs - 1; slab >= 0; --slab) {
-      const Layout<kBwdThreads> L(ck.cv, slab * kBwdThreads);
+      const Layout<kBwdThreads, kBwdPer> L(ck, slab, threadIdx.x);
       Channels<V> ch;
       Channels<V> ab;  // -a / M and b / M (the affine is not used)
       if (L.on) {

@@ -1,0 +1,29 @@
+"""Group norm on rows of several slabs of columns, with enough rows that every block has many chunks of each: against
+the float64 oracle with the tolerances of test_gpu_gnorm (no thread sums more rows there than in its longest case), and
+inside frames that have to stay untouched."""
+import pytest
+import torch
+
+from test_gpu_gnorm import check, cu_tensor, inputs, u  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("channels,groups", [(1536, 32), (2048, 32), (2560, 5), (3848, 1), (4096, 32), (8192, 64)])
+def test_many_rows_of_several_slabs(u, channels, groups, dtype):  # noqa: F811
+    lengths = [1201, 0, 1, 1806]
+    n = sum(lengths)
+    x, dy, gamma, beta = inputs(n, channels, dtype, seed=channels)
+    want = check(u, x, dy, gamma, beta, groups, lengths, 1)
+    e = 16 // x.element_size()
+    frames = [torch.full((n + 128, channels + 2 * e), 7.0, dtype=dtype, device="cuda") for _ in range(2)]
+    y, dx = (f[64:-64, e:-e] for f in frames)
+    cu = cu_tensor(lengths)
+    got = u.ut_group_norm_fwd(x, gamma, beta, groups, cu=cu, y=y)
+    got += u.ut_group_norm_bwd(x, dy, gamma, beta, *got[1:], groups, cu=cu, dx=dx)
+    for a, b in zip(got, want):
+        assert torch.equal(a, b)
+    for f in frames:
+        f[64:-64, e:-e] = 7.0
+        assert torch.equal(f, torch.full_like(f, 7.0))
