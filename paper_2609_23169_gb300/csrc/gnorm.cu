@@ -50,7 +50,8 @@ namespace {
 
 constexpr int kWindow = 16;                          // rows summed before they are merged (forward)
 constexpr int kMaxSlots = 16;
-constexpr size_t kSmem = 225 * 1024;                 // with 2 KB of static shared memory
+constexpr size_t kFwdSmem = 225 * 1024;              // 128 bytes of static shared memory beside it
+constexpr size_t kBwdSmem = 227 * 1024;              // none beside it
 
 template <typename T>
 struct Vec;  // 16 bytes of channels as pairs of fp32
@@ -645,7 +646,7 @@ __global__ void __launch_bounds__(kBwdThreads + 32, 1) gn_bwd_kernel(const Gnorm
   float2* chan = lane_sum + V * kBwdThreads;                                            // [C]: this piece's sums
   float2* all = chan + p.C;                                                    // [C]: this block's, over all segments
   float2* stat = all + p.C;                                                    // [G]: mean, rstd
-  float2* coef = stat + p.G;                                                   // [G]: a / M, b / M
+  float2* coef = chan;                                                         // [G], after pass 1: a / M, b / M
   const int blocks = gridDim.x, me = blockIdx.x, cpg = p.C / p.G;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const Chunks<kBwdThreads, kBwdPer> ck(p.C / V);
@@ -894,19 +895,31 @@ int blocks_of(const GnormParams& p, int elem) {
   return (int)(want < 1 ? 1 : want > p.sms ? p.sms : want);
 }
 
+constexpr size_t ring_at(size_t tables) { return (tables + sizeof(RingState) + 8 + 127) & ~(size_t)127; }
+
+// Tables in shared memory in front of the ring, in bytes.  The backward's go
+// twice over the channels and once over the groups.
+constexpr size_t tables(int vec, int C, int G, bool backward) {
+  return sizeof(float2) * ((size_t)vec * (backward ? kBwdThreads : kFwdThreads) + (backward ? 2 : 1) * (size_t)C + G);
+}
+// Every accepted size leaves at least one slot, the largest tables being those
+// of the most channels with the most groups beside them.
+constexpr int kMostGroups = kGnMaxBoth - kGnMaxChannels;
+static_assert(ring_at(tables(8, kGnMaxChannels, kMostGroups, false)) + kFwdThreads * kFwdPer * 16 <= kFwdSmem, "forward");
+static_assert(ring_at(tables(8, kGnMaxChannels, kMostGroups, true)) + kBwdThreads * kBwdPer * 32 <= kBwdSmem, "backward");
+
 template <typename F>
-cudaError_t launch(F kern, GnormParams p, size_t fixed, int tensors, int threads, int per, int elem, cudaStream_t s) {
+cudaError_t launch(F kern, GnormParams p, bool backward, int elem, cudaStream_t s) {
+  const int threads = backward ? kBwdThreads : kFwdThreads, per = backward ? kBwdPer : kFwdPer;
   const int cv = p.C * elem / 16, cols = cv < threads ? cv : threads;
-  fixed = (fixed + sizeof(RingState) + 8 + 127) & ~(size_t)127;
-  p.ring_at = (int)fixed;
-  p.slot_bytes = threads / cols * per * cols * 16 * tensors;
-  const int slots = (int)((kSmem - fixed) / p.slot_bytes);
+  p.ring_at = (int)ring_at(tables(16 / elem, p.C, p.G, backward));
+  p.slot_bytes = threads / cols * per * cols * 16 * (backward ? 2 : 1);
+  const int slots = (int)(((backward ? kBwdSmem : kFwdSmem) - p.ring_at) / p.slot_bytes);
   p.slots = slots < kMaxSlots ? slots : kMaxSlots;
-  if (p.slots < 1) return cudaErrorInvalidValue;
   // threads a group of channels is summed by: all groups in one round if they fit
   p.group_lanes = 32;
   while (p.group_lanes > 1 && p.group_lanes * p.G > threads) p.group_lanes /= 2;
-  const size_t smem = fixed + (size_t)p.slots * p.slot_bytes;
+  const size_t smem = p.ring_at + (size_t)p.slots * p.slot_bytes;
   cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
   if (e != cudaSuccess) return e;
   void* args[] = {&p};
@@ -915,24 +928,13 @@ cudaError_t launch(F kern, GnormParams p, size_t fixed, int tensors, int threads
 }
 
 template <typename T>
-size_t fixed_smem(const GnormParams& p, bool backward) {
-  const size_t n = (size_t)Vec<T>::n * (backward ? kBwdThreads : kFwdThreads) +
-                   (backward ? 2 * ((size_t)p.C + p.G) : (size_t)p.C + p.G);
-  return n * sizeof(float2);
-}
-
-template <typename T>
 cudaError_t fwd(const GnormParams& p, cudaStream_t s) {
-  const size_t fixed = fixed_smem<T>(p, false);
-  return p.act ? launch(gn_fwd_kernel<T, true>, p, fixed, 1, kFwdThreads, kFwdPer, sizeof(T), s)
-               : launch(gn_fwd_kernel<T, false>, p, fixed, 1, kFwdThreads, kFwdPer, sizeof(T), s);
+  return launch(p.act ? gn_fwd_kernel<T, true> : gn_fwd_kernel<T, false>, p, false, sizeof(T), s);
 }
 
 template <typename T>
 cudaError_t bwd(const GnormParams& p, cudaStream_t s) {
-  const size_t fixed = fixed_smem<T>(p, true);
-  return p.act ? launch(gn_bwd_kernel<T, true>, p, fixed, 2, kBwdThreads, kBwdPer, sizeof(T), s)
-               : launch(gn_bwd_kernel<T, false>, p, fixed, 2, kBwdThreads, kBwdPer, sizeof(T), s);
+  return launch(p.act ? gn_bwd_kernel<T, true> : gn_bwd_kernel<T, false>, p, true, sizeof(T), s);
 }
 
 }  // namespace

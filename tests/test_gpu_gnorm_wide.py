@@ -27,3 +27,11 @@ def test_many_rows_of_several_slabs(u, channels, groups, dtype):  # noqa: F811
     for f in frames:
         f[64:-64, e:-e] = 7.0
         assert torch.equal(f, torch.full_like(f, 7.0))
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("channels,groups", [(8192, 4096), (8192, 2048), (6144, 6144), (7680, 3840)])
+def test_limits_of_channels_and_groups(u, channels, groups, dtype):  # noqa: F811
+    """The most channels and groups that are accepted, forward and backward; several chunks a block."""
+    lengths = [900, 700]
+    check(u, *inputs(sum(lengths), channels, dtype, seed=groups), groups, lengths, 1)
