@@ -459,9 +459,9 @@ __global__ void __launch_bounds__(kDqThreads, 1)
           r[x + 1] = __float_as_uint(ex2_approx(b));
         }
         const bool whole = __all_sync(0xffffffffu, now == 15u);
-        if (!whole) {  // P of a masked key (S = 0) may be infinite; the others' is at most 1
+        if (!whole) {  // P of a masked key (S = 0) may be infinite; the others' is at most 1, or NaN, which stays
 #pragma unroll
-          for (int x = 0; x < 64; ++x) r[x] = __float_as_uint(fminf(__uint_as_float(r[x]), 2.f));
+          for (int x = 0; x < 64; ++x) r[x] = __float_as_uint(min_nan(__uint_as_float(r[x]), 2.f));
         }
         if (!(ok = wait(&sm.dp_full[at % S::kV], (at / S::kV) & 1))) break;
         tc_fence_after();

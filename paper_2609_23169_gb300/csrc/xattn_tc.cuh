@@ -157,6 +157,12 @@ UT_DEV float max3(float a, float b, float c) {
   asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
   return r;
 }
+// the smaller of two, NaN where either is
+UT_DEV float min_nan(float a, float b) {
+  float r;
+  asm("min.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+  return r;
+}
 // Lanes whose number differs in bit kBit exchange unit b of the lower one (bit =
 // 0) for unit a of the upper one (bit = 1).
 template <int kBit>

@@ -1,0 +1,35 @@
+"""Cross attention with values that are not finite: what they spoil shows, what they must not reach keeps its bits."""
+import pytest
+import torch
+
+from test_gpu_xattn import cu_tensor, inputs, u  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("lk", [[77, 20], [128, 40], [300, 77]])
+@pytest.mark.parametrize("value", [float("nan"), float("inf")])
+def test_spoilt_query_row_shows_in_its_gradient_alone(u, value, lk, d, dtype):  # noqa: F811
+    """One head of one query row: its O, LSE and dQ are NaN (an infinity gives scores of both signs); other heads and
+    rows keep their bits.  Segments of one key block and of several, whole and not, with masked keys and without."""
+    lq, heads = [40, 150], 4
+    q, k, v, dout = inputs(lq, lk, heads, 2, d, dtype, seed=d)
+    mask = (torch.rand(sum(lk), generator=torch.Generator().manual_seed(3)) < 0.7).to(torch.uint8).cuda()
+    rows = [7, 170]
+    for m in (None, mask):
+        how = dict(cu_q=cu_tensor(lq), cu_k=cu_tensor(lk), key_mask=m)
+        clean = u.ut_xattn_fwd(q, k, v, **how)
+        dq = u.ut_xattn_bwd(q, k, v, *clean, dout, **how)[0]
+        q2 = q.clone()
+        for r in rows:
+            q2[r, 1, 5] = value
+        out = u.ut_xattn_fwd(q2, k, v, **how)
+        dq2 = u.ut_xattn_bwd(q2, k, v, *out, dout, **how)[0]
+        for r in rows:
+            assert torch.isnan(out[0][r, 1]).all() and torch.isnan(out[1][1, r]) and torch.isnan(dq2[r, 1]).all()
+            for t, c in ((out[0], clean[0]), (dq2, dq)):
+                t[r, 1] = c[r, 1]
+            out[1][1, r] = clean[1][1, r]
+        assert torch.equal(out[0], clean[0]) and torch.equal(out[1], clean[1]) and torch.equal(dq2, dq)
