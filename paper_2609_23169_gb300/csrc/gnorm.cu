@@ -580,20 +580,17 @@ __global__ void __launch_bounds__(kFwdThreads + 32, 1) gn_fwd_kernel(const Gnorm
       const Layout<kFwdThreads, kFwdPer> L(ck, slab, threadIdx.x);
       Channels<V> ch;
       if (L.on) ch.load(p, stat, L.col * V);
-      // u = x a + b in bf16, whose inputs are coarser than what folding the mean
-      // into b costs; in fp32 (x - mu) a + beta
-      constexpr bool kFold = sizeof(T) == 2;
+      // u = (x - mu) a + beta: with mu folded into beta, a row at its mean would be
+      // the difference of two numbers of size |mu| a, which is far from beta where
+      // the variance is at or below eps
 #pragma unroll
-      for (int c = 0; c < V / 2; ++c) {
-        ch.rstd[c] = mul_f32x2(ch.rstd[c], ch.gamma[c]);
-        if (kFold) ch.beta[c] = fma_f32x2(ch.neg_mean[c], ch.rstd[c], ch.beta[c]);
-      }
+      for (int c = 0; c < V / 2; ++c) ch.rstd[c] = mul_f32x2(ch.rstd[c], ch.gamma[c]);
       auto row_of = [&](const uint4& w) -> uint4 {
         uint64_t v[V / 2];
         Vec<T>::unpack(w, v);
 #pragma unroll
         for (int x = 0; x < V / 2; ++x) {
-          const uint64_t u = fma_f32x2(sizeof(T) == 2 ? v[x] : add_f32x2(v[x], ch.neg_mean[x]), ch.rstd[x], ch.beta[x]);
+          const uint64_t u = fma_f32x2(add_f32x2(v[x], ch.neg_mean[x]), ch.rstd[x], ch.beta[x]);
           v[x] = kAct ? mul_f32x2(u, sigmoid2(u)) : u;
         }
         return Vec<T>::pack(v);
