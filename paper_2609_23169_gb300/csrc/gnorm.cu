@@ -112,8 +112,10 @@ struct Stat {
   float n, mean, m2;
   UT_DEV void add(float nb, float mb, float qb) {
     if (nb <= 0.f) return;
-    const float tot = n + nb, w = nb * rcp_approx(tot), d = mb - mean;
-    m2 += fmaf(d * d, n * w, qb);
+    // the first set as it is: nb / nb by an approximate reciprocal need not be 1
+    const bool first = n == 0.f;
+    const float tot = n + nb, w = first ? 1.f : nb * rcp_approx(tot), d = mb - mean, e = first ? 0.f : d;
+    m2 += fmaf(e * e, n * w, qb);
     mean = fmaf(d, w, mean);
     n = tot;
   }

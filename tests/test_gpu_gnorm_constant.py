@@ -35,3 +35,12 @@ def test_constant_groups_give_beta(u, value, eps, act, dtype):  # noqa: F811
     constant(u, value, 64, 64, 8, eps, act, dtype)  # one block
     sms = torch.cuda.get_device_properties(0).multi_processor_count
     constant(u, value, 32 * sms, 320, 32, eps, act, dtype)  # 32 rows a block
+
+
+@pytest.mark.parametrize("value", [1000.0, -0.1, 3.0e5])
+@pytest.mark.parametrize("rows", [3, 7, 23, 41, 47, 55, 61, 83, 97])
+def test_constant_groups_over_many_blocks(u, rows, value):  # noqa: F811
+    """Pieces of odd numbers of rows, some of one row more, merged over all blocks: the mean keeps every bit."""
+    sms = torch.cuda.get_device_properties(0).multi_processor_count
+    for more in (0, sms // 2):
+        constant(u, value, rows * sms + more, 1024, 32, 1e-5, 0, torch.float32)
