@@ -121,57 +121,6 @@ struct Stat {
   }
 };
 
-// Row counts fit 32 bits (at most 2^30 rows): 64-bit divisions cost hundreds
-// of cycles each, on the path of every launch.
-UT_DEV void rows_of_segment(const GnormParams& p, int s, int& row, int& n) {
-  int64_t a, len;
-  segment_rows(p.cu, s, p.n, a, len);
-  row = (int)a;
-  n = (int)len;
-}
-
-// The blocks' shares of the rows: n / blocks each, the first n % blocks one more.
-struct Shares {
-  int row, each, more, blocks;
-  UT_DEV Shares(const GnormParams& p, int blocks_) : blocks(blocks_) {
-    int n;
-    rows_of_segment(p, 0, row, n);
-    each = ((int)p.n - row) / blocks;
-    more = (int)p.n - row - each * blocks;
-  }
-  UT_DEV int first(int block) const { return row + each * block + min(block, more); }
-  // the block that has row r (in range whatever cu holds)
-  UT_DEV int owner(int r) const {
-    const int at = r - row, big = (each + 1) * more;
-    const int c = at < big ? at / (each + 1) : more + (at - big) / max(each, 1);
-    return max(0, min(c, blocks - 1));
-  }
-};
-// The last segment that starts at or before row r.
-UT_DEV int segment_at(const GnormParams& p, int r) {
-  if (!p.cu) return 0;
-  int lo = 0, hi = p.B;
-  while (hi - lo > 1) {
-    const int mid = (lo + hi) >> 1;
-    if (p.cu[mid] <= r) lo = mid;
-    else hi = mid;
-  }
-  return lo;
-}
-
-// Calls f(segment, first row, end) for the pieces of rows [a, e).
-template <typename F>
-UT_DEV void for_pieces(const GnormParams& p, int a, int e, F f) {
-  if (a >= e) return;
-  for (int s = segment_at(p, a); s < p.B; ++s) {
-    int row, n;
-    rows_of_segment(p, s, row, n);
-    const int lo = max(a, row), hi = min(e, row + n);
-    if (row >= e) break;
-    if (lo < hi) f(s, lo, hi);
-  }
-}
-
 struct RingState {
   uint64_t full[kMaxSlots], empty[kMaxSlots];
   int abort_flag;
@@ -240,23 +189,10 @@ UT_DEV void sync_compute() {  // the computing warps
   asm volatile("bar.sync 1, %0;" ::"n"(kThreads) : "memory");
 }
 
-// Pieces of rows [a, e), last first.
-template <typename F>
-UT_DEV void for_pieces_back(const GnormParams& p, int a, int e, F f) {
-  if (a >= e) return;
-  for (int s = segment_at(p, e - 1); s >= 0; --s) {
-    int row, n;
-    rows_of_segment(p, s, row, n);
-    const int lo = max(a, row), hi = min(e, row + n);
-    if (lo < hi) f(s, lo, hi);
-    if (row <= a) break;
-  }
-}
-
 // The producer's part of both passes: tensors x (and dy).
 template <int kThreads, int kPer, int kTensors>
-UT_DEV void produce(const GnormParams& p, int a, int e, const Chunks<kThreads, kPer>& ck,
-                    Ring& ring, uint32_t& used, int total, int elem) {
+UT_DEV void produce(const GnormParams& p, const Pieces& pieces, const Chunks<kThreads, kPer>& ck, Ring& ring,
+                    uint32_t& used, int total, int elem) {
   auto load = [&](int at, int slab, int r, int n) {
     if (!ring.wait_empty(at)) return;
     ring.full_par ^= 1u << at;
@@ -271,7 +207,7 @@ UT_DEV void produce(const GnormParams& p, int a, int e, const Chunks<kThreads, k
       load_rows(dst + ring.slot_bytes / 2, p.dy, p.dys * elem, r, n, slab * kThreads, cols, bar);
   };
   int slot = 0;
-  for_pieces(p, a, e, [&](int s, int lo, int hi) {
+  pieces.forward(p, [&](int s, int lo, int hi) {
     for (int slab = 0; slab < ck.slabs; ++slab)
       for (int r = lo; r < hi; r += ck.rows, slot = ring.next(slot)) load(slot, slab, r, min(ck.rows, hi - r));
   });
@@ -279,7 +215,7 @@ UT_DEV void produce(const GnormParams& p, int a, int e, const Chunks<kThreads, k
   // backwards; the last `slots` chunks are there
   int i = total - 1;
   slot = ring.before(slot);
-  for_pieces_back(p, a, e, [&](int s, int lo, int hi) {
+  pieces.backward(p, [&](int s, int lo, int hi) {
     const int n = ck.row_chunks(hi - lo);
     for (int slab = ck.slabs - 1; slab >= 0; --slab)
       for (int c = n - 1; c >= 0; --c, --i, slot = ring.before(slot))
@@ -436,17 +372,17 @@ __global__ void __launch_bounds__(kFwdThreads + 32, 1) gn_fwd_kernel(const Gnorm
     }
   }
   const Shares sh(p, blocks);
-  const int a = sh.first(me), e = sh.first(me + 1);
+  const Pieces pieces(p, sh.first(me), sh.first(me + 1));
   int total = 0;  // chunks
-  for_pieces(p, a, e, [&](int, int lo, int hi) { total += ck.of_piece(hi - lo); });
+  pieces.forward(p, [&](int, int lo, int hi) { total += ck.of_piece(hi - lo); });
   if (warp == kFwdThreads / 32) {
     uint32_t used = 0;  // slots loaded
-    produce<kFwdThreads, kFwdPer, 1>(p, a, e, ck, ring, used, total, sizeof(T));
+    produce<kFwdThreads, kFwdPer, 1>(p, pieces, ck, ring, used, total, sizeof(T));
     ring.finish(used);
     return;
   }
   int i = 0, slot = 0;
-  for_pieces(p, a, e, [&](int s, int lo, int hi) {
+  pieces.forward(p, [&](int s, int lo, int hi) {
     const int n = hi - lo;
     for (int slab = 0; slab < ck.slabs; ++slab) {
       const Layout<kFwdThreads, kFwdPer> L(ck, slab, threadIdx.x);
@@ -529,7 +465,7 @@ __global__ void __launch_bounds__(kFwdThreads + 32, 1) gn_fwd_kernel(const Gnorm
   cooperative_groups::this_grid().sync();
   i = total - 1;
   slot = ring.before(slot);
-  for_pieces_back(p, a, e, [&](int s, int lo, int hi) {
+  pieces.backward(p, [&](int s, int lo, int hi) {
     int row, n;
     rows_of_segment(p, s, row, n);
     const int c0 = sh.owner(row), c1 = sh.owner(row + n - 1);
@@ -663,17 +599,17 @@ __global__ void __launch_bounds__(kBwdThreads + 32, 1) gn_bwd_kernel(const Gnorm
       stat[g] = make_float2(p.mean[(int64_t)s * p.G + g], p.rstd[(int64_t)s * p.G + g]);
   };
   const Shares sh(p, blocks);
-  const int a = sh.first(me), e = sh.first(me + 1);
+  const Pieces pieces(p, sh.first(me), sh.first(me + 1));
   int total = 0;  // chunks
-  for_pieces(p, a, e, [&](int, int lo, int hi) { total += ck.of_piece(hi - lo); });
+  pieces.forward(p, [&](int, int lo, int hi) { total += ck.of_piece(hi - lo); });
   if (warp == kBwdThreads / 32) {
     uint32_t used = 0;  // slots loaded
-    produce<kBwdThreads, kBwdPer, 2>(p, a, e, ck, ring, used, total, sizeof(T));
+    produce<kBwdThreads, kBwdPer, 2>(p, pieces, ck, ring, used, total, sizeof(T));
     ring.finish(used);
     return;
   }
   int i = 0, slot = 0;
-  for_pieces(p, a, e, [&](int s, int lo, int hi) {
+  pieces.forward(p, [&](int s, int lo, int hi) {
     const int n = hi - lo;
     sync_compute<kBwdThreads>();
     load_stat(s);
@@ -794,7 +730,7 @@ __global__ void __launch_bounds__(kBwdThreads + 32, 1) gn_bwd_kernel(const Gnorm
   }
   i = total - 1;
   slot = ring.before(slot);
-  for_pieces_back(p, a, e, [&](int s, int lo, int hi) {
+  pieces.backward(p, [&](int s, int lo, int hi) {
     int row, n;
     rows_of_segment(p, s, row, n);
     const int c0 = sh.owner(row), c1 = sh.owner(row + n - 1);

@@ -23,7 +23,7 @@ struct Segment {
 
 // Values of cu outside [0, n] or out of order are clamped: a wrong cu gives
 // wrong results but no access outside the tensors (and see check_cu).
-__device__ __forceinline__ void segment_rows(const int32_t* cu, int s, int64_t n, int64_t& row, int64_t& len) {
+__host__ __device__ __forceinline__ void segment_rows(const int32_t* cu, int s, int64_t n, int64_t& row, int64_t& len) {
   if (!cu) {
     row = 0;
     len = n;

@@ -35,3 +35,22 @@ def test_limits_of_channels_and_groups(u, channels, groups, dtype):  # noqa: F81
     """The most channels and groups that are accepted, forward and backward; several chunks a block."""
     lengths = [900, 700]
     check(u, *inputs(sum(lengths), channels, dtype, seed=groups), groups, lengths, 1)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_wrong_prefixes_cost_no_waits(u, dtype):  # noqa: F811
+    """Prefixes out of order over rows of many chunks: reported as what they are, and no wait runs out on their account."""
+    n, channels = 60000, 320
+    x, dy, gamma, beta = inputs(n, channels, dtype, seed=2)
+    for cu in ([0, 50000, 20000, 60000], [30000, 10, 60000, 0, 60000], [0, 59000, 300, 20, 60000], [60000, 0]):
+        bad = torch.tensor(cu, dtype=torch.int32, device="cuda")
+        status = u.status_word()
+        start, end = (torch.cuda.Event(enable_timing=True) for _ in range(2))
+        start.record()
+        _, mean, rstd = u.ut_group_norm_fwd(x, gamma, beta, 32, cu=bad, status=status)
+        u.ut_group_norm_bwd(x, dy, gamma, beta, mean, rstd, 32, cu=bad, status=status)
+        end.record()
+        end.synchronize()
+        assert int(status.item()) == u.UT_ERR_INVALID_ARG
+        assert start.elapsed_time(end) < 500.0  # ms; the limit of one wait is 2,000
+    check(u, x, dy, gamma, beta, 32, [n], 1, one_segment=True)
