@@ -360,14 +360,19 @@ __global__ void __launch_bounds__(kFwdThreads + 32, 1) gn_fwd_kernel(const Gnorm
   Ring ring{st, smem + p.ring_at, p.slots, p.slot_bytes, p.status, p.timeout_ns, 0, 0, false};
   float2* part = static_cast<float2*>(p.ws);  // [blocks + B][G]
   ring_init<kFwdThreads>(st, p.slots);
-  if (me == 0 && warp < kFwdThreads / 32) {
-    check_cu(p.cu, p.B, p.n, p.status);
-    for (int x = threadIdx.x; x < p.B * p.G; x += kFwdThreads) {  // empty segments have no piece
-      int64_t row, n;
-      segment_rows(p.cu, x / p.G, p.n, row, n);
-      if (n == 0) {
-        p.mean[x] = 0.f;
-        p.rstd[x] = 1.f / sqrtf(p.eps);
+  if (warp < kFwdThreads / 32) {
+    if (me == 0) check_cu(p.cu, p.B, p.n, p.status);
+    // empty segments have no piece: 32 segments a warp at a time, a lane each
+    constexpr int kStep = kFwdThreads;  // segments of a block
+    for (int64_t s0 = (int64_t)me * kStep + warp * 32; s0 < p.B; s0 += (int64_t)blocks * kStep) {
+      int64_t row, n = 1;
+      if (s0 + lane < p.B) segment_rows(p.cu, (int)s0 + lane, p.n, row, n);
+      for (uint32_t none = __ballot_sync(0xffffffffu, n == 0); none; none &= none - 1) {
+        const int64_t at = (s0 + __ffs(none) - 1) * p.G;
+        for (int g = lane; g < p.G; g += 32) {
+          p.mean[at + g] = 0.f;
+          p.rstd[at + g] = 1.f / sqrtf(p.eps);
+        }
       }
     }
   }
@@ -824,9 +829,10 @@ __global__ void __launch_bounds__(kBwdThreads + 32, 1) gn_bwd_kernel(const Gnorm
 }
 
 // ----------------------------------------------------------------- launchers
-// Blocks: one per SM, fewer where a block would have under 8 KB of x.
+// Blocks: one per SM, fewer where a block would have under 8 KB of x and of the
+// segments' statistics.
 int blocks_of(const GnormParams& p, int elem) {
-  const int64_t want = (p.n * p.C * elem + 8191) / 8192;
+  const int64_t x = p.n * p.C * elem, stat = (int64_t)p.B * p.G * 8, want = ((x > stat ? x : stat) + 8191) / 8192;
   return (int)(want < 1 ? 1 : want > p.sms ? p.sms : want);
 }
 

@@ -54,3 +54,20 @@ def test_wrong_prefixes_cost_no_waits(u, dtype):  # noqa: F811
         assert int(status.item()) == u.UT_ERR_INVALID_ARG
         assert start.elapsed_time(end) < 500.0  # ms; the limit of one wait is 2,000
     check(u, x, dy, gamma, beta, 32, [n], 1, one_segment=True)
+
+
+def test_more_statistics_than_32_bits_count(u):  # noqa: F811
+    """2^31 and more pairs of segment and group, all but the last segment empty."""
+    B, groups, n, eps = (1 << 25) + 3, 64, 10, 1e-5
+    x, _, gamma, beta = inputs(n, groups, torch.bfloat16, seed=1)
+    cu = torch.zeros(B + 1, dtype=torch.int32, device="cuda")
+    cu[-1] = n
+    mean, rstd = (torch.full((B, groups), float("nan"), device="cuda") for _ in range(2))
+    status = u.status_word()
+    y, _, _ = u.ut_group_norm_fwd(x, gamma, beta, groups, eps=eps, cu=cu, mean=mean, rstd=rstd, status=status)
+    u.check_status(status)
+    want = u.ut_group_norm_fwd(x, gamma, beta, groups, eps=eps)
+    assert torch.equal(y, want[0]) and torch.equal(mean[-1:], want[1]) and torch.equal(rstd[-1:], want[2])
+    assert int(torch.count_nonzero(mean[:-1])) == 0
+    lo, hi = torch.aminmax(rstd[:-1])
+    assert lo == hi and abs(lo.item() - eps ** -0.5) <= 2.0 ** -22 * eps ** -0.5
