@@ -454,6 +454,14 @@ def _prefix(cu: Optional[torch.Tensor], what: str) -> int:
     return cu.numel() - 1
 
 
+def _current_device(device: torch.device, status: Optional[torch.Tensor]) -> None:
+    """The kernels run on the current device's stream and take device memory (the status word may be pinned)."""
+    if device.type != "cuda" or device.index != torch._C._cuda_getDevice():
+        raise ValueError(f"tensors on {device}; they must be on the current CUDA device")
+    if status is not None and status.device != device and not device_accessible(status):
+        raise ValueError("status must be device memory or host memory the device can address (pinned)")
+
+
 def _same_device(device: torch.device, *others: Optional[torch.Tensor]) -> None:
     for t in others:
         if t is not None and t.device != device:
@@ -471,7 +479,7 @@ def _head_rows(t: torch.Tensor, dtype: torch.dtype, shape, what: str) -> int:
     return row if rows > 1 else heads * d
 
 
-def _xattn_shape(q, k, v, cu_q, cu_k, key_mask) -> XattnShape:
+def _xattn_shape(q, k, v, cu_q, cu_k, key_mask, status) -> XattnShape:
     qs, ks, dtype = q.shape, k.shape, q.dtype
     if len(qs) != 3 or len(ks) != 3 or ks[2] != qs[2]:
         raise ValueError("q is [rows, heads, d]; k and v are [encoder rows, kv heads, d]")
@@ -485,6 +493,7 @@ def _xattn_shape(q, k, v, cu_q, cu_k, key_mask) -> XattnShape:
     if key_mask is not None:
         if key_mask.dtype not in (torch.uint8, torch.bool) or key_mask.shape != (nk,) or not key_mask.is_contiguous():
             raise ValueError("key_mask must be a contiguous uint8 or bool vector of the encoder rows")
+    _current_device(q.device, status)
     _same_device(q.device, k, v, cu_q, cu_k, key_mask)
     return XattnShape(nq, nk, n_seg, H, Hk, d, _DTYPES[dtype], _head_rows(q, dtype, qs, "q"),
                       _head_rows(k, dtype, ks, "k"), _head_rows(v, dtype, ks, "v"), H * d)
@@ -501,6 +510,8 @@ def _workspace(ws: Optional[torch.Tensor], size: int, device):
         if size == 0:
             return None, None, 0
         ws = torch.empty(size, dtype=torch.uint8, device=device)
+    elif ws.device != device or not ws.is_contiguous():
+        raise ValueError(f"ws must be contiguous on {device}")
     return ws, ws.data_ptr(), ws.numel() * ws.element_size()
 
 
@@ -512,7 +523,7 @@ def ut_xattn_fwd(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, softmax_scal
     """Cross attention of packed query rows q [Nq, H, d] to encoder states k, v [Nk, Hkv, d] (rows may be strided:
     slices of one projection), segment by segment (cu_q, cu_k: int32 prefixes of the lengths, on the device), over
     the keys with key_mask != 0.  Returns (O [Nq, H, d], LSE [H, Nq] fp32)."""
-    shape = _xattn_shape(q, k, v, cu_q, cu_k, key_mask)
+    shape = _xattn_shape(q, k, v, cu_q, cu_k, key_mask, status)
     device = q.device
     if o is None:
         o = torch.empty(q.shape, dtype=q.dtype, device=device)
@@ -541,7 +552,7 @@ def ut_xattn_bwd(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, o: torch.Ten
                  dv: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None,
                  status: Optional[torch.Tensor] = None):
     """Gradient of ut_xattn_fwd (o and lse are its outputs).  Returns (dQ, dK, dV)."""
-    shape = _xattn_shape(q, k, v, cu_q, cu_k, key_mask)
+    shape = _xattn_shape(q, k, v, cu_q, cu_k, key_mask, status)
     device, dtype = q.device, q.dtype
     _check_lse(lse, q)
     _same_device(device, o, lse, dout, dq, dk, dv)
@@ -602,6 +613,7 @@ def ut_group_norm_fwd(x: torch.Tensor, gamma: Optional[torch.Tensor], beta: Opti
     if dtype not in _DTYPES:
         raise TypeError(f"unsupported dtype {dtype}")
     gp, bp = _affine(gamma, C, "gamma"), _affine(beta, C, "beta")
+    _current_device(device, status)
     _same_device(device, gamma, beta, cu, y, mean, rstd)
     y_stride = C if y is None else _channel_rows(y, x, "y")
     if y is None:
@@ -636,6 +648,7 @@ def ut_group_norm_bwd(x: torch.Tensor, dy: torch.Tensor, gamma: Optional[torch.T
         raise TypeError(f"unsupported dtype {dtype}")
     gp, bp = _affine(gamma, C, "gamma"), _affine(beta, C, "beta")
     _stats(mean, rstd, n_seg, groups)
+    _current_device(device, status)
     _same_device(device, dy, gamma, beta, cu, mean, rstd, dx, dgamma, dbeta)
     dx_stride = C if dx is None else _channel_rows(dx, x, "dx")
     if dx is None:
