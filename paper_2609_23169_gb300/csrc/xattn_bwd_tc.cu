@@ -1098,8 +1098,11 @@ __global__ void __launch_bounds__(256) xattn_bwd_join_kernel(const BwdParams prm
   const int64_t stride = is_k ? p.dks : p.dvs;
   for (int x = threadIdx.x; x < keys * (D / 8); x += 256) {
     const int r = x / (D / 8), e = x % (D / 8);
-    *reinterpret_cast<uint4*>(out + (g.row + g.tile * kT + r) * stride + e * 8) =
-        *reinterpret_cast<const uint4*>(rows + r * (D * 2 + 16) + e * 16);
+    const int64_t key = g.row + g.tile * kT + r;
+    // a masked key's row is zero, also where a NaN or an infinity of Q or dO met its P and dS of 0
+    const uint4 v = p.mask && !p.mask[key] ? make_uint4(0, 0, 0, 0)
+                                           : *reinterpret_cast<const uint4*>(rows + r * (D * 2 + 16) + e * 16);
+    *reinterpret_cast<uint4*>(out + key * stride + e * 8) = v;
   }
 }
 

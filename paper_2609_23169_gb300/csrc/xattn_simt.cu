@@ -488,6 +488,8 @@ __global__ void __launch_bounds__(kJoinThreads) xattn_dkdv_join_kernel(const Xat
     a.w += b.w;
   }
   const float f = is_v ? 1.f : p.scale;
+  // a masked key's row is zero, also where a NaN or an infinity of Q or dO met its P and dS of 0
+  if (p.mask && !p.mask[key]) a = make_float4(0, 0, 0, 0);
   st4(static_cast<float*>(is_v ? p.dv : p.dk) + key * (is_v ? p.dvs : p.dks) + e,
       make_float4(a.x * f, a.y * f, a.z * f, a.w * f));
 }

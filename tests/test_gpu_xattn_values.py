@@ -33,3 +33,23 @@ def test_spoilt_query_row_shows_in_its_gradient_alone(u, value, lk, d, dtype):  
                 t[r, 1] = c[r, 1]
             out[1][1, r] = clean[1][1, r]
         assert torch.equal(out[0], clean[0]) and torch.equal(out[1], clean[1]) and torch.equal(dq2, dq)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("lq,lk", [([40, 150], [77, 20]), ([300, 9], [300, 129])])
+@pytest.mark.parametrize("value", [float("nan"), float("inf")])
+def test_masked_keys_have_zero_gradients_beside_spoilt_rows(u, value, lq, lk, dtype):  # noqa: F811
+    """Rows of Q and dO that are not finite make the gradients of their segment's keys so, not of masked ones; and a
+    segment whose keys are all masked has no gradient at all."""
+    q, k, v, dout = inputs(lq + [6], lk + [5], 4, 2, 64, dtype, seed=len(lk) + lk[0])
+    mask = (torch.rand(sum(lk) + 5, generator=torch.Generator().manual_seed(4)) < 0.5).to(torch.uint8).cuda()
+    mask[-5:] = 0
+    q[3], dout[5], dout[-2], q[-1] = value, value, value, value
+    how = dict(cu_q=cu_tensor(lq + [6]), cu_k=cu_tensor(lk + [5]), key_mask=mask)
+    out, lse = u.ut_xattn_fwd(q, k, v, **how)
+    dq, dk, dv = u.ut_xattn_bwd(q, k, v, out, lse, dout, **how)
+    off = mask == 0
+    assert not dk[off].any() and not dv[off].any() and not dq[-6:].any() and not out[-6:].any()
+    assert torch.isneginf(lse[:, -6:]).all()
+    mine = (mask[:lk[0]] != 0).nonzero()[:, 0]
+    assert not torch.isfinite(dv[mine]).any() and torch.isfinite(dv[lk[0]:]).all() and torch.isfinite(dk[lk[0]:]).all()
