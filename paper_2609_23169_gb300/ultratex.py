@@ -227,7 +227,7 @@ def ut_fg_compact(mask: torch.Tensor, srcs: Sequence[torch.Tensor], capacity: Op
     dev = mask.device
     if outs is None:
         outs = [torch.empty((cap,) + tuple(s.shape[1:]), dtype=s.dtype, device=dev) for s in srcs]
-    if len(outs) != len(srcs) or _row_bytes(outs, cap, "outs") != row_bytes:
+    if len(outs) != len(srcs) or (cap > 0 and _row_bytes(outs, cap, "outs") != row_bytes):
         raise ValueError("outs must match srcs row for row")
     if idx is not None and idx.numel() < cap:
         raise ValueError("idx holds fewer than capacity entries")
@@ -252,7 +252,7 @@ def ut_fg_scatter(idx: torch.Tensor, n: int, srcs: Sequence[torch.Tensor], dsts:
     """dst[idx[i]] = src[i] for i < n; background rows per bg_mode."""
     T = dsts[0].shape[0]
     row_bytes = _row_bytes(dsts, T, "dsts")
-    if len(srcs) != len(dsts) or _row_bytes(srcs, int(n), "srcs") != row_bytes:
+    if len(srcs) != len(dsts) or (int(n) > 0 and _row_bytes(srcs, int(n), "srcs") != row_bytes):
         raise ValueError("srcs must match dsts row for row")
     if fill_row is not None and fill_row.numel() * fill_row.element_size() != row_bytes:
         raise ValueError("fill_row must hold exactly one row")
