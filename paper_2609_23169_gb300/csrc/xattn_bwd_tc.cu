@@ -86,13 +86,14 @@ UT_DEV void zero_tail(uint32_t base, int chunks, int first, uint32_t lane) {
 //   warp 3      zeroes the masked keys of K and V, says when a block has all it
 //               needs
 //   warps 12-15 dQ out
-// kFew, for segments of 128 keys on average or fewer: dS is rounded to bf16
-// for its product, as dQ is at the end, together 1.42 times the error of
-// rounding dQ alone; with few keys the error of D = dO . O, whose O was rounded
-// too, adds to that in dQ and dK (1.66 times at 10 keys, 1.50 at 62, 1.45 from
-// 110).  So where a segment has one block of keys D is taken anew, as the sum of
-// P dP in fp32, and left for the next kernel.  A form of its own because the
-// code costs the other 4%.
+// kFew, where a segment may have one block of keys (several segments, or 128 keys
+// in all): dS is rounded to bf16 for its product, as dQ is at the end, together
+// 1.42 times the error of rounding dQ alone; with few keys the error of D = dO .
+// O, whose O was rounded too, adds to that in dQ and dK (1.66 times at 10 keys,
+// 1.50 at 62, 1.45 from 110).  So in such a segment D is taken anew, as the sum
+// of P dP in fp32, and left for the next kernel; which form a segment gets does
+// not depend on the others.  A form of its own because its code costs long segments
+// a pass 6% at d = 64 (23,959 x 257 keys each of 13: 290 -> 309 us), 0.4% at 128.
 // The issuing warp's instructions are fetched anew every block (the
 // elementwise code lies between), and it bounded the first form: 700 of them a
 // block, 3,900 cycles.  So it counts stages instead of dividing, follows one
@@ -1184,7 +1185,7 @@ cudaError_t launch_xattn_bwd_tc(const XattnParams& p, void* ws, cudaStream_t s) 
   prm.x.part_dk = static_cast<float*>(ws);
   prm.x.part_dv = reinterpret_cast<float*>(static_cast<char*>(ws) + part_bytes(p, prm.R));
   prm.scale_log2 = p.scale * kLog2e;
-  const bool few = p.nk <= (int64_t)kT * p.B;
+  const bool few = p.nk <= kT || p.B > 1;  // a segment may have one block of keys
   // One segment of one block: the dQ kernel takes all of D, and there is no
   // prefix to check (85,202 x 77 x 24 x 128: 776 -> 621 us).
   cudaError_t e = few && !p.cu_q && p.nk > 0 ? cudaSuccess : launch_xattn_dsum(p, true, s);
