@@ -96,10 +96,13 @@ UT_DEV float rcp_approx(float x) {
   asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
-// 1 / (1 + exp(-u)) of a pair, relative error below 2^-21 (exp(-u) = infinity
-// gives 0).  Sharing one reciprocal between the two (1 / a = b / (a b)) takes a
-// third off the special function pipe and adds four instructions: no faster
-// forward, 8% slower backward.
+// 1 / (1 + exp(-u)) of a pair.  Relative error below 2^-21 + |u| 2^-23 for
+// negative u (the product u log2(e) is rounded, and the exponential turns its
+// absolute error into a relative one; exponential and reciprocal add 2^-22 and
+// 2^-23), below 2^-21 for positive u; 0 where the value is below 2^-126.
+// Sharing one reciprocal between the two (1 / a = b / (a b)) takes a third off
+// the special function pipe and adds four instructions: no faster forward, 8%
+// slower backward.
 UT_DEV uint64_t sigmoid2(uint64_t u) {
   float a, b;
   unpack_f32x2(mul_f32x2(u, both(-1.4426950408889634f)), a, b);
