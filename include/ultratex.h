@@ -353,9 +353,12 @@ ut_status ut_bsattn_bwd(const ut_attn_shape* shape, const void* q, const void* k
  *   O_i = softmax_j(softmax_scale * q_i . k_j) v_j
  *   LSE_i = ln sum_j exp(softmax_scale * q_i . k_j)
  * A query row without a key (an empty segment, or all keys masked) gets
- * O = 0 and LSE = -inf.  Keys and values that are masked, and rows of other
- * segments, never enter a product: whatever they hold (NaN, infinities) has
- * no effect. */
+ * O = 0 and LSE = -inf, and so does one whose scores are all -inf (an infinity
+ * in q).  Keys and values that are masked, and rows of other segments, never
+ * enter a product: whatever they hold (NaN, infinities) has no effect.  Scores
+ * softmax_scale q . k may have magnitudes up to 2^29; exponents are fp32
+ * differences of numbers of that size.  With n_q = 0 the forward launches
+ * nothing and looks at no prefix. */
 typedef struct {
   int64_t n_q, n_k;       /* query rows, encoder rows (of all segments), >= 0 */
   int32_t n_seg;          /* segments, >= 1 */
@@ -390,13 +393,16 @@ ut_status ut_xattn_fwd(const ut_xattn_shape* shape, const void* q, const void* k
  *   D_i = dO_i . O_i,  P = exp(S - LSE),  dS = P o (dO V^T - D),
  *   dV = P^T dO,  dQ = softmax_scale dS K,  dK = softmax_scale dS^T Q,
  * dK and dV summed over the query heads that share the kv head.  Rows of dK
- * and dV of masked keys, and rows of dQ without a key, are zero.
+ * and dV of masked keys, and rows of dQ without a key, are zero, whatever q
+ * and dout hold; elsewhere what is not finite shows in the gradients.
  *   o, lse      the forward's outputs;  dout  [n_q, H, d]
  *   dq          [n_q, H, d];  dk, dv  [n_k, H_kv, d], fully overwritten
  *   ws          ut_xattn_bwd_workspace_size(shape) bytes (may be 0: then NULL
  *               is fine), 16-byte aligned
  * In bf16 P and dS are rounded to bf16 for their products and each gradient
- * once at the end; the rest is fp32.  The result does not depend on the run. */
+ * once at the end; the rest is fp32.  In a segment of at most 128 keys D is the
+ * sum of P dP in fp32, without O's rounding.  The result does not depend on the
+ * run. */
 size_t ut_xattn_bwd_workspace_size(const ut_xattn_shape* shape);
 ut_status ut_xattn_bwd(const ut_xattn_shape* shape, const void* q, const void* k, const void* v,
                        const int32_t* cu_q, const int32_t* cu_k, const uint8_t* key_mask,
@@ -429,8 +435,8 @@ typedef struct {
  *   gamma, beta   [C] fp32, or NULL (1 and 0)
  *   mean, rstd    [n_seg, groups] fp32 outputs (mu and r, for the backward)
  *   ws            ut_group_norm_fwd_workspace_size(shape) bytes, 16-byte aligned
- * Statistics and the arithmetic are fp32; y is rounded once.  The result does
- * not depend on the run. */
+ * Statistics and the arithmetic are fp32; y is rounded once.  A group of equal
+ * values has x - mu = 0.  The result does not depend on the run. */
 size_t ut_group_norm_fwd_workspace_size(const ut_gnorm_shape* shape);
 ut_status ut_group_norm_fwd(const ut_gnorm_shape* shape, const void* x, const int32_t* cu,
                             const float* gamma, const float* beta, void* y, float* mean, float* rstd,

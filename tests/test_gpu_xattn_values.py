@@ -53,3 +53,31 @@ def test_masked_keys_have_zero_gradients_beside_spoilt_rows(u, value, lq, lk, dt
     assert torch.isneginf(lse[:, -6:]).all()
     mine = (mask[:lk[0]] != 0).nonzero()[:, 0]
     assert not torch.isfinite(dv[mine]).any() and torch.isfinite(dv[lk[0]:]).all() and torch.isfinite(dk[lk[0]:]).all()
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("lq,lk", [([200], [300]), ([1], [9000])])
+@pytest.mark.parametrize("size", [-2.0 ** 10, 2.0 ** 10, -2.0 ** 14, 2.0 ** 14])
+def test_large_scores(u, size, lq, lk, dtype):  # noqa: F811
+    """Scores up to 2^28 of either sign.  Each is exact in fp32 and the largest is more than 4,000 above the next, so that
+    it has all the weight; blocks before its own hold lower ones, or masked keys only.
+
+    Tolerance, derived: in bf16 the exponent of the largest is its own rounding in base 2 (up to 2^4), so P = 2^x is
+    rounded for its product and the sum is not, 2^-8 each for P and O; in fp32 it is 0, and P = 1.  LSE: three roundings
+    of 2^-24."""
+    n, d, best = lk[0], 64, lk[0] - 40
+    q = torch.zeros(lq[0], 2, d, dtype=dtype, device="cuda")
+    k = torch.zeros(n, 2, d, dtype=dtype, device="cuda")
+    v = inputs(lq, lk, 2, 2, d, dtype, seed=1)[2]
+    rank = torch.randperm(n, generator=torch.Generator().manual_seed(2)) % 127  # of sizes that bf16 holds
+    rank[best] = 127
+    at = (128 + rank if size > 0 else 256 - rank) / 128
+    q[..., 0], k[..., 0] = size, (at * abs(size)).to(dtype).cuda()[:, None]
+    mask = torch.ones(n, dtype=torch.uint8, device="cuda")
+    mask[:140] = 0
+    want = float(at[best]) * size * abs(size) * 0.5
+    for m in (None, mask):
+        out, lse = u.ut_xattn_fwd(q, k, v, key_mask=m, softmax_scale=0.5)
+        e = 2.0 ** -7 if dtype == torch.bfloat16 else 0.0
+        assert torch.all((out - v[best]).abs().float() <= e * v[best].abs().float())
+        assert torch.all((lse - want).abs() <= 2.0 ** -22 * abs(want))
