@@ -68,7 +68,7 @@ static size_t xattn_fwd_ws(const XattnParams& p) {
   return up256(rows * p.d * sizeof(float)) + up256(rows * sizeof(float2));
 }
 
-// D, then partial dK and dV (and, in bf16, the CTAs' dQ buffers)
+// D, then partial dK and dV
 static size_t xattn_bwd_ws(const XattnParams& p, bool bf16) {
   const size_t part = up256((size_t)p.nsplit * p.nk * p.Hk * p.d * sizeof(float));
   return up256((size_t)p.H * p.nq * sizeof(float)) + (bf16 ? xattn_bwd_tc_ws(p) : 2 * part);
@@ -196,7 +196,7 @@ ut_status ut_xattn_bwd(const ut_xattn_shape* shape, const void* q, const void* k
   if (!at16(dout) || !at16(dq) || !at16(dk) || !at16(dv)) return UT_ERR_INVALID_ARG;
   if (p.nq == 0 && p.nk == 0) return UT_OK;
   const bool bf16 = shape->dtype == UT_BF16;
-  const size_t need = xattn_bwd_ws(p, bf16);  // 0 without queries
+  const size_t need = xattn_bwd_ws(p, bf16);  // 0 for bf16 without queries
   if (need > 0 && (!ws || ws_bytes < need || !at16(ws))) return UT_ERR_INVALID_ARG;
   char* w = static_cast<char*>(ws);
   p.dsum = reinterpret_cast<float*>(w);

@@ -16,24 +16,25 @@
 // of segments that stay in L2 between the passes were tried: 4 us of barrier and
 // merge each and a loop around both passes cost more than the second reads, 225
 // us instead of 204 for 6 x 65,536 x 512.)
-// Measured: 2048 x 2048 x 128 forward 514 us (two reads and a write at the copy
-// rate: 475), backward 822 us (790); 6 x 65,536 x 512 forward 204 us (178),
-// backward 325 (297); 85,202 x 640 in 13 segments 62 and 108 us.
+// Measured: 2048 x 2048 x 128 forward 510 us (two reads and a write at the copy
+// rate: 475), backward 815 us (790); 6 x 65,536 x 512 forward 204 us (178),
+// backward 324 (297); 85,202 x 640 in 13 segments 61 and 107 us.
 //
 // Rows move in chunks of kPer rows a thread: a producer warp copies them to a
 // ring in shared memory with bulk copies (several chunks in flight whatever
 // the other warps do), which in the second pass runs backwards from where the
 // first one stopped.  A thread owns one 16-byte column of channels, so any
 // number of channels per group works; rows of more than a column a thread are
-// taken in slabs.
+// taken in slabs (gnorm_rows.cuh).
 //
 // Statistics are never sums of squares: a window of rows is summed as
 // differences from its first row, and the windows' means and squared distances
 // merged pairwise,
 //   M2 = M2a + M2b + (mean_b - mean_a)^2 na nb / (na + nb),
 // so a mean far from zero costs no digits; means are averaged as differences
-// from one of them, so that equal values have themselves as their mean.  All sums are in 32 bits, of a
-// window first and of windows then, in an order that the sizes fix.
+// from one of them, so that equal values have themselves as their mean.  All
+// sums are in 32 bits, of a window first and of windows then, in an order that
+// the sizes fix.
 #include <cooperative_groups.h>
 #include <math.h>
 

@@ -25,10 +25,10 @@
 // operands of the second products, written over the first ones' results), and
 // the elementwise work of one tile runs beside the products of the next:
 // 2,700 and 2,700 cycles a pair where the products need 1,536 and 2,048.
-// Measured at that size: D 44 us (6.6 TB/s), dQ 168, dK and dV 185, their sum
-// 13: 420 us a pass, 896 TFLOP/s of the five products.  dQ is bound by the
+// Measured at that size: D 44 us (6.6 TB/s), dQ 172, dK and dV 191, their sum
+// 14: 417 us a pass, 904 TFLOP/s of the five products.  dQ is bound by the
 // elementwise warps and by shared memory (S and dP read both operands there,
-// tensor pipe active 60%), dK and dV by shared memory (80%).
+// tensor pipe active 59%), dK and dV by shared memory (tensor pipe 72%).
 //
 // Roles of both kernels (registers rebalanced with setmaxnreg): warp 1 owns
 // TMEM and issues the products, warps 0, 2, 3 load (TMA) and zero the rows
@@ -92,8 +92,9 @@ UT_DEV void zero_tail(uint32_t base, int chunks, int first, uint32_t lane) {
 // O, whose O was rounded too, adds to that in dQ and dK (1.66 times at 10 keys,
 // 1.50 at 62, 1.45 from 110).  So in such a segment D is taken anew, as the sum
 // of P dP in fp32, and left for the next kernel; which form a segment gets does
-// not depend on the others.  A form of its own because its code costs long segments
-// a pass 6% at d = 64 (23,959 x 257 keys each of 13: 290 -> 309 us), 0.4% at 128.
+// not depend on the others.  A form of its own because its code costs long
+// segments up to 6% of a backward pass (23,959 rows and 13 segments of 257 keys at d =
+// 64: 290 -> 309 us; 85,202 and 13 of 512 at d = 128: 1,836 -> 1,840 us).
 // The issuing warp's instructions are fetched anew every block (the
 // elementwise code lies between), and it bounded the first form: 700 of them a
 // block, 3,900 cycles.  So it counts stages instead of dividing, follows one
@@ -1187,7 +1188,8 @@ cudaError_t launch_xattn_bwd_tc(const XattnParams& p, void* ws, cudaStream_t s) 
   prm.scale_log2 = p.scale * kLog2e;
   const bool few = p.nk <= kT || p.B > 1;  // a segment may have one block of keys
   // One segment of one block: the dQ kernel takes all of D, and there is no
-  // prefix to check (85,202 x 77 x 24 x 128: 776 -> 621 us).
+  // prefix to check (85,202 x 77 x 24 x 128 takes 572 us; reading O and dO for D
+  // would be another 155).
   cudaError_t e = few && !p.cu_q && p.nk > 0 ? cudaSuccess : launch_xattn_dsum(p, true, s);
   if (e != cudaSuccess) return e;
   if (p.nq > 0) {

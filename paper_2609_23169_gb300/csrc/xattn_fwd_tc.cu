@@ -44,11 +44,11 @@
 // hold (NaN, infinities) is multiplied.
 // Rounding: P to bf16 for its product (the sum l is of the unrounded values),
 // O once at the end.
-// Measured: 85,202 x 512 x 24 x 128 385 us, 1,390 TFLOP/s, 0.74 of the card's
-// bf16 rate, bound by the softmax between the products (tensor pipe active 58%;
-// under sustained load the power cap makes it 410 to 440 us);
-// 23,959 x 257 x 24 x 64 67 us; one query over 85,202 keys, 24 heads of 128, 154
-// us, 6.8 TB/s.
+// Measured: 85,202 x 512 x 24 x 128 430 us a pass among others, 1,250 TFLOP/s,
+// 0.66 of the card's bf16 rate (390 us for the first twenty, before the power
+// cap holds), bound by the softmax between the products (tensor pipe active
+// 58%); 23,959 x 257 x 24 x 64 66 us; one query over 85,202 keys, 24 heads of
+// 128, 155 us, 6.7 TB/s.
 // Every wait is bounded; on expiry the kernel records UT_ERR_TIMEOUT, drains
 // its own copies and MMAs, frees TMEM and returns.
 #include "common.cuh"

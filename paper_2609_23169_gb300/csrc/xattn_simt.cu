@@ -421,7 +421,7 @@ __global__ void __launch_bounds__(kXsThreads) xattn_bwd_simt_kernel(const XattnP
 
 // D_i = dO_i . O_i -> [H, nq]: 16 bytes of O and dO a thread and step, the
 // threads of a row side by side, four steps in flight.  Also checks the
-// prefixes.  Bound by memory: 46 us for 23,959 x 24 x 128 in bf16 (295 MB).
+// prefixes.  Bound by memory: 44 us for 23,959 x 24 x 128 in bf16 (295 MB).
 constexpr int kDsumSteps = 4;
 template <typename T, int D>
 __global__ void __launch_bounds__(256) xattn_dsum_kernel(const XattnParams p) {
