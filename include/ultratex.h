@@ -452,6 +452,112 @@ ut_status ut_group_norm_bwd(const ut_gnorm_shape* shape, const void* x, const vo
                             void* dx, float* dgamma, float* dbeta, void* ws, size_t ws_bytes,
                             int32_t* dev_status, void* stream);
 
+/* ------------------------------------------------------------------------
+ * Windowed-attention operators: the norms of queries and keys with the position
+ * rotation, and attention with a sliding window and first keys that stay
+ * visible (a prompt's or the text tokens').  They work on packed rows and
+ * device prefixes as the conditioning operators do.
+ *
+ * Norms of queries and keys.  For every row (token) and head x of q or k:
+ *   y = R(pos) (x r w),   r = 1 / sqrt(mean(x^2) + eps)
+ * with the rotation of ut_rope at canvas position pos (positions below
+ * rope->prefix, negative ones too, are not rotated; side = 1 and axes
+ * {head_dim, 0, 0} give the plain rotation by the position itself).  Angles are
+ * exact to 2^-32 turns for positions up to 2^17, and to 2^-20 turns for any. */
+typedef struct {
+  int64_t n_rows;         /* tokens, >= 0 */
+  int32_t n_heads;        /* heads of q */
+  int32_t n_kv_heads;     /* heads of k and v (any number) */
+  int32_t head_dim;       /* d: 64 or 128 */
+  int32_t dtype;          /* ut_dtype of q, k, v, the outputs and their gradients */
+  float eps;              /* > 0 */
+  /* elements between consecutive rows, at least the row's heads * d, a multiple
+   * of 16 bytes.  v_stride and vo_stride are read where there is a v.  In the
+   * backward qo_stride and ko_stride are those of dq and dk, dqo_stride and
+   * dko_stride those of the given gradients (read by the backward only). */
+  int64_t q_stride, k_stride, v_stride, qo_stride, ko_stride, vo_stride;
+  int64_t dqo_stride, dko_stride;
+  int64_t cache_rows;     /* rows of k_out and v_out, read where there are `rows` */
+} ut_qknorm_shape;
+
+/*   pos          [n_rows] int32, or NULL: 0, 1, ...
+ *   q, q_out     [n_rows, H, d];  k  [n_rows, H_kv, d]
+ *   wq, wk       [d] fp32 weights, the same for all heads, or NULL (1)
+ *   rows         NULL: k_out is [n_rows, H_kv, d]; else [n_rows] int32, the rows
+ *                of k_out (a cache of cache_rows rows) that the tokens' keys are
+ *                written to.  A negative entry writes none (a padding token), one
+ *                of cache_rows or more neither, and reports UT_ERR_INVALID_ARG in
+ *                dev_status.  Of two tokens with the same row either may remain,
+ *                in parts.  Other rows of the cache stay as they are.
+ *   v, v_out     both or neither: V is copied as K is written, without a change
+ * An output may be its own input (same pointer and stride; K and V without
+ * `rows`), and overlap no other.  fp32 arithmetic, each value rounded once. */
+ut_status ut_qk_norm_rope_fwd(const ut_qknorm_shape* shape, const ut_rope* rope, const int32_t* pos,
+                              const void* q, const void* k, const void* v, const float* wq, const float* wk,
+                              const int32_t* rows, void* q_out, void* k_out, void* v_out,
+                              int32_t* dev_status, void* stream);
+
+/* Gradient of ut_qk_norm_rope_fwd (without rows and v) given dqo and dko.  With
+ * g = R(pos)^T dy and xh = x r:
+ *   dx = r (g w - xh mean(g w xh)),   dw = sum over rows and heads of g xh
+ *   dq, dk     [n_rows, heads, d]; may be dqo and dko themselves (same pointer
+ *              and stride), and overlap nothing else
+ *   dwq, dwk   [d] fp32, or NULL
+ *   ws         ut_qk_norm_rope_bwd_workspace_size(shape, rope) bytes (0 without
+ *              rows), 16-byte aligned: partial sums of dwq and dwk
+ * The result does not depend on the run. */
+size_t ut_qk_norm_rope_bwd_workspace_size(const ut_qknorm_shape* shape, const ut_rope* rope);
+ut_status ut_qk_norm_rope_bwd(const ut_qknorm_shape* shape, const ut_rope* rope, const int32_t* pos,
+                              const void* q, const void* k, const float* wq, const float* wk,
+                              const void* dqo, const void* dko, void* dq, void* dk, float* dwq, float* dwk,
+                              void* ws, size_t ws_bytes, void* stream);
+
+/* Windowed attention.  Segment s has the query rows of cu_q and, of the rows of
+ * cu_k, the first k_len[s] as keys (all of them without k_len): a cache of that
+ * capacity, filled that far.  Its queries are the last of its keys' tokens:
+ * query i of n_q stands at p = n_k - n_q + i (negative where there are more
+ * queries than keys) and sees the keys
+ *   j <= p + right  and  (j >= p - left  or  j < sinks),   0 <= j < n_k,
+ * with key_mask[j] != 0.  right = 0 is causal; left of the length or more has no
+ * window.  O, LSE, rows without a key, shared kv heads and scores are those of
+ * ut_xattn_fwd.  Masked keys, rows of other segments and behind k_len, and keys
+ * that none of a tile of consecutive queries sees (128 / (H / H_kv) tokens in
+ * bf16, half of that in fp32) never enter a product: whatever they hold has no
+ * effect.  A value that is not finite in a key or value that some queries of
+ * such a tile see may show in the tile's other rows too, and in the gradients
+ * of the 128 keys beside it. */
+typedef struct {
+  int32_t left;           /* keys before p that are seen, >= 0 */
+  int32_t right;          /* keys behind p that are seen, >= 0 */
+  int32_t sinks;          /* first keys of a segment that stay visible, >= 0 */
+} ut_window;
+
+/*   shape, q, k, v, cu_q, cu_k, key_mask, softmax_scale, o, lse   as ut_xattn_fwd
+ *   k_len        [n_seg] int32 (n_seg = 1 without prefixes too), or NULL; values
+ *                outside 0 .. rows of the segment are clamped and reported in
+ *                dev_status
+ *   ws           ut_window_attn_fwd_workspace_size(shape, window) bytes (may be
+ *                0: then NULL is fine), 16-byte aligned
+ * The result does not depend on the run. */
+size_t ut_window_attn_fwd_workspace_size(const ut_xattn_shape* shape, const ut_window* window);
+ut_status ut_window_attn_fwd(const ut_xattn_shape* shape, const ut_window* window, const void* q, const void* k,
+                             const void* v, const int32_t* cu_q, const int32_t* cu_k, const int32_t* k_len,
+                             const uint8_t* key_mask, float softmax_scale, void* o, float* lse,
+                             void* ws, size_t ws_bytes, int32_t* dev_status, void* stream);
+
+/* Gradient of ut_window_attn_fwd given dO, with the formulas of ut_xattn_bwd
+ * over the keys that each query sees.  dk and dv are fully overwritten: rows
+ * behind k_len, masked keys and keys that no query sees get zeros.
+ *   ws           ut_window_attn_bwd_workspace_size(shape, window) bytes, 16-byte
+ *                aligned
+ * The result does not depend on the run. */
+size_t ut_window_attn_bwd_workspace_size(const ut_xattn_shape* shape, const ut_window* window);
+ut_status ut_window_attn_bwd(const ut_xattn_shape* shape, const ut_window* window, const void* q, const void* k,
+                             const void* v, const int32_t* cu_q, const int32_t* cu_k, const int32_t* k_len,
+                             const uint8_t* key_mask, float softmax_scale, const void* o, const float* lse,
+                             const void* dout, void* dq, void* dk, void* dv, void* ws, size_t ws_bytes,
+                             int32_t* dev_status, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -6,6 +6,7 @@
 #include <stdint.h>
 
 #include "../../include/ultratex.h"
+#include "checks.h"
 #include "gnorm.cuh"
 #include "kernels.h"
 #include "segments.cuh"
@@ -13,14 +14,9 @@
 
 namespace ut {
 
-static bool at16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
-static bool at4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
-static size_t up256(size_t x) { return (x + 255) & ~(size_t)255; }
-
-static ut_status status_of(cudaError_t e) { return e == cudaSuccess ? UT_OK : UT_ERR_CUDA; }
 
 // ------------------------------------------------------------ cross attention
-static ut_status xattn_problem(const ut_xattn_shape* s, bool backward, XattnParams* p) {
+ut_status xattn_shape(const ut_xattn_shape* s, bool backward, XattnParams* p) {
   if (!s) return UT_ERR_INVALID_ARG;
   if (s->n_q < 0 || s->n_k < 0 || s->n_seg < 1 || s->n_heads < 1 || s->n_kv_heads < 1 || s->head_dim < 1)
     return UT_ERR_INVALID_ARG;
@@ -56,6 +52,12 @@ static ut_status xattn_problem(const ut_xattn_shape* s, bool backward, XattnPara
   p->dks = s->dk_stride;
   p->dvs = s->dv_stride;
   p->sms = device_sms();
+  return UT_OK;
+}
+
+static ut_status xattn_problem(const ut_xattn_shape* s, bool backward, XattnParams* p) {
+  const ut_status st = xattn_shape(s, backward, p);
+  if (st != UT_OK) return st;
   const bool bf16 = s->dtype == UT_BF16;
   if (xattn_items(*p, bf16, backward) > INT32_MAX / 2) return UT_ERR_UNSUPPORTED;
   p->nsplit = xattn_splits(*p, bf16, backward);
@@ -74,7 +76,7 @@ static size_t xattn_bwd_ws(const XattnParams& p, bool bf16) {
   return up256((size_t)p.H * p.nq * sizeof(float)) + (bf16 ? xattn_bwd_tc_ws(p) : 2 * part);
 }
 
-static ut_status xattn_pointers(const ut_xattn_shape* s, const XattnParams& p) {
+ut_status xattn_pointers(const ut_xattn_shape* s, const XattnParams& p) {
   if ((p.cu_q == nullptr) != (p.cu_k == nullptr) || (!p.cu_q && s->n_seg != 1)) return UT_ERR_INVALID_ARG;
   if (!at4(p.cu_q) || !at4(p.cu_k) || !at4(p.status)) return UT_ERR_INVALID_ARG;
   if (!(p.scale > 0.f) || !isfinite(p.scale)) return UT_ERR_INVALID_ARG;

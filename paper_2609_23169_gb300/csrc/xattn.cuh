@@ -3,6 +3,8 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include "../../include/ultratex.h"
+
 namespace ut {
 
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.69314718055994531f;
@@ -29,6 +31,11 @@ struct XattnParams {
   float* part_dk; float* part_dv;
 };
 
+// Checks of a shape and of the pointers (api_cond.cu); the rest of p is filled
+// in between.
+ut_status xattn_shape(const ut_xattn_shape* s, bool backward, XattnParams* p);
+ut_status xattn_pointers(const ut_xattn_shape* s, const XattnParams& p);
+
 // Work items of a pass without splits, and how many parts its long axis is
 // split into.
 int64_t xattn_items(const XattnParams& p, bool bf16, bool backward);
@@ -37,6 +44,7 @@ int64_t xattn_fwd_tc_items(const XattnParams& p);
 cudaError_t launch_xattn_fwd_simt(const XattnParams& p, cudaStream_t s);  // fp32
 cudaError_t launch_xattn_fwd_tc(const XattnParams& p, cudaStream_t s);    // bf16
 cudaError_t launch_xattn_join(const XattnParams& p, bool bf16, cudaStream_t s);  // of the forward's key splits
+cudaError_t launch_xattn_dkdv_join(const XattnParams& p, bool bf16, cudaStream_t s);  // of the backward's splits
 int64_t xattn_bwd_tc_items(const XattnParams& p);
 size_t xattn_bwd_tc_ws(const XattnParams& p);
 cudaError_t launch_xattn_dsum(const XattnParams& p, bool bf16, cudaStream_t s);  // D, and the check of the prefixes

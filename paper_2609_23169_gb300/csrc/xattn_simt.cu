@@ -26,143 +26,9 @@
 #include "pairs.cuh"
 #include "segments.cuh"
 #include "xattn.cuh"
+#include "xattn_simt.cuh"
 
 namespace ut {
-
-constexpr int kXs = 64;        // rows and keys of a tile
-constexpr int kXsThreads = 256;
-constexpr int kXsLdP = kXs + 4;
-
-UT_DEV float4 ld4(const float* p) { return *reinterpret_cast<const float4*>(p); }
-UT_DEV float4 ld4(const __nv_bfloat16* p) {
-  const uint2 u = *reinterpret_cast<const uint2*>(p);
-  return make_float4(__uint_as_float(u.x << 16), __uint_as_float(u.x & 0xFFFF0000u), __uint_as_float(u.y << 16),
-                     __uint_as_float(u.y & 0xFFFF0000u));
-}
-UT_DEV void st4(float* p, float4 v) { *reinterpret_cast<float4*>(p) = v; }
-UT_DEV void st4(__nv_bfloat16* p, float4 v) {
-  *reinterpret_cast<uint2*>(p) = make_uint2(pack_bf16x2(v.x, v.y), pack_bf16x2(v.z, v.w));
-}
-
-struct XsTile {  // the query rows of a tile
-  int64_t tok0;  // first token
-  int rows;      // valid rows
-  int head0;     // first query head
-  int G;
-  UT_DEV int64_t off(int r, int64_t stride, int d) const {
-    return (tok0 + r / G) * stride + (int64_t)(head0 + r % G) * d;
-  }
-};
-
-// dst[64][D + 4] <- the tile's rows of x (zeros past the valid ones)
-template <typename T, int D>
-UT_DEV void stage_q(float* dst, const void* x, const XsTile& t, int64_t stride) {
-  for (int e = threadIdx.x; e < kXs * (D / 4); e += kXsThreads) {
-    const int r = e / (D / 4), c = (e % (D / 4)) * 4;
-    const float4 v = r < t.rows ? ld4(static_cast<const T*>(x) + t.off(r, stride, D) + c) : make_float4(0, 0, 0, 0);
-    st4(dst + r * (D + 4) + c, v);
-  }
-}
-// dst[64][D + 4] <- keys key0 .. of kv head hk (zeros where `on` is 0)
-template <typename T, int D>
-UT_DEV void stage_k(float* dst, const void* x, int64_t key0, const float* on, int hk, int64_t stride) {
-  for (int e = threadIdx.x; e < kXs * (D / 4); e += kXsThreads) {
-    const int r = e / (D / 4), c = (e % (D / 4)) * 4;
-    const float4 v = on[r] != 0.f ? ld4(static_cast<const T*>(x) + (key0 + r) * stride + (int64_t)hk * D + c)
-                                  : make_float4(0, 0, 0, 0);
-    st4(dst + r * (D + 4) + c, v);
-  }
-}
-// on[64] <- 1 where the key exists and is not masked; whether any is.  Synchronises the block.
-UT_DEV bool stage_mask(float* on, const uint8_t* mask, int64_t key0, int64_t left) {
-  const int r = threadIdx.x;
-  const bool is = r < kXs && r < left && (!mask || mask[key0 + r]);
-  if (r < kXs) on[r] = is ? 1.f : 0.f;
-  return __syncthreads_or(is);
-}
-
-// acc[i][j] = a[ty * 4 + i] . b[tx + 16 j]
-template <int D>
-UT_DEV void product_nt(const float* a, const float* b, float (&acc)[4][4]) {
-  const int ty = threadIdx.x >> 4, tx = threadIdx.x & 15;
-  uint64_t sum[4][4];  // of the even and of the odd columns
-#pragma unroll
-  for (int i = 0; i < 4; ++i)
-#pragma unroll
-    for (int j = 0; j < 4; ++j) sum[i][j] = 0;
-#pragma unroll 4
-  for (int e = 0; e < D; e += 4) {
-    ulonglong2 x[4], y[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) x[i] = *reinterpret_cast<const ulonglong2*>(a + (ty * 4 + i) * (D + 4) + e);
-#pragma unroll
-    for (int j = 0; j < 4; ++j) y[j] = *reinterpret_cast<const ulonglong2*>(b + (tx + 16 * j) * (D + 4) + e);
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-#pragma unroll
-      for (int j = 0; j < 4; ++j) sum[i][j] = fma_f32x2(x[i].y, y[j].y, fma_f32x2(x[i].x, y[j].x, sum[i][j]));
-  }
-#pragma unroll
-  for (int i = 0; i < 4; ++i)
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      float u, v;
-      unpack_f32x2(sum[i][j], u, v);
-      acc[i][j] = u + v;
-    }
-}
-// acc[i][c] += sum_k p[ty * 4 + i][k] b[k][tx * 4 + ...]
-UT_DEV void axpy4(float w, const ulonglong2& v, float4& acc) {
-  const uint64_t ww = pack_f32x2(w, w);
-  ulonglong2& a = reinterpret_cast<ulonglong2&>(acc);
-  a.x = fma_f32x2(ww, v.x, a.x);
-  a.y = fma_f32x2(ww, v.y, a.y);
-}
-template <int D>
-UT_DEV void product_nn(const float* p, const float* b, float4 (&acc)[4][D / 64]) {
-  const int ty = threadIdx.x >> 4, tx = threadIdx.x & 15;
-#pragma unroll 4
-  for (int k = 0; k < kXs; k += 4) {
-    float w[4][4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) *reinterpret_cast<float4*>(w[i]) = ld4(p + (ty * 4 + i) * kXsLdP + k);
-#pragma unroll
-    for (int kk = 0; kk < 4; ++kk)
-#pragma unroll
-      for (int c = 0; c < D / 64; ++c) {
-        const ulonglong2 v = *reinterpret_cast<const ulonglong2*>(b + (k + kk) * (D + 4) + tx * 4 + 64 * c);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) axpy4(w[i][kk], v, acc[i][c]);
-      }
-  }
-}
-// acc[i][c] += sum_r p[r][ty * 4 + i] b[r][tx * 4 + ...]
-template <int D>
-UT_DEV void product_tn(const float* p, const float* b, float4 (&acc)[4][D / 64]) {
-  const int ty = threadIdx.x >> 4, tx = threadIdx.x & 15;
-#pragma unroll 4
-  for (int r = 0; r < kXs; ++r) {
-    float w[4];
-    *reinterpret_cast<float4*>(w) = ld4(p + r * kXsLdP + ty * 4);
-#pragma unroll
-    for (int c = 0; c < D / 64; ++c) {
-      const ulonglong2 v = *reinterpret_cast<const ulonglong2*>(b + r * (D + 4) + tx * 4 + 64 * c);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) axpy4(w[i], v, acc[i][c]);
-    }
-  }
-}
-
-UT_DEV float half_warp_max(float x) {
-#pragma unroll
-  for (int o = 8; o; o >>= 1) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, o));
-  return x;
-}
-UT_DEV float half_warp_sum(float x) {
-#pragma unroll
-  for (int o = 8; o; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
-  return x;
-}
 
 // grid (q slots, kv heads, key splits)
 template <typename T, int D>
@@ -270,16 +136,6 @@ UT_DEV void probabilities(const XattnParams& p, const float* on, const float* ls
       s[i][j] = on[tx + 16 * j] != 0.f && le != -INFINITY ? expf(s[i][j] * p.scale - le) : 0.f;
       dp[i][j] = s[i][j] * (dp[i][j] - ds);
     }
-  }
-}
-
-// lse / D of the tile's rows (rows that do not exist: LSE = -inf, P = 0)
-UT_DEV void stage_rows(float* lse, float* dsum, const XattnParams& p, const XsTile& t) {
-  if (threadIdx.x < kXs) {
-    const int r = threadIdx.x;
-    const int64_t at = (int64_t)(t.head0 + r % p.G) * p.nq + t.tok0 + r / p.G;
-    lse[r] = r < t.rows ? p.lse[at] : -INFINITY;
-    dsum[r] = r < t.rows ? p.dsum[at] : 0.f;
   }
 }
 
@@ -468,6 +324,7 @@ __global__ void __launch_bounds__(256) xattn_dsum_kernel(const XattnParams p) {
 // dK (blockIdx.y = 0), dV = the sum of the splits' partials, in split order; 4
 // values a thread, small blocks, 16 loads in flight
 constexpr int kJoinThreads = 64;
+template <typename T>
 __global__ void __launch_bounds__(kJoinThreads) xattn_dkdv_join_kernel(const XattnParams p) {
   const int64_t x = (int64_t)blockIdx.x * kJoinThreads + threadIdx.x;
   const int per_row = p.Hk * p.d / 4;
@@ -490,7 +347,7 @@ __global__ void __launch_bounds__(kJoinThreads) xattn_dkdv_join_kernel(const Xat
   const float f = is_v ? 1.f : p.scale;
   // a masked key's row is zero, also where a NaN or an infinity of Q or dO met its P and dS of 0
   if (p.mask && !p.mask[key]) a = make_float4(0, 0, 0, 0);
-  st4(static_cast<float*>(is_v ? p.dv : p.dk) + key * (is_v ? p.dvs : p.dks) + e,
+  st4(static_cast<T*>(is_v ? p.dv : p.dk) + key * (is_v ? p.dvs : p.dks) + e,
       make_float4(a.x * f, a.y * f, a.z * f, a.w * f));
 }
 
@@ -541,6 +398,12 @@ static cudaError_t launch(F kern, dim3 grid, size_t smem, const XattnParams& p, 
   return cudaGetLastError();
 }
 
+cudaError_t launch_xattn_dkdv_join(const XattnParams& p, bool bf16, cudaStream_t s) {
+  const dim3 grid((unsigned)((p.nk * p.Hk * p.d / 4 + kJoinThreads - 1) / kJoinThreads), 2);
+  return bf16 ? launch_next(xattn_dkdv_join_kernel<__nv_bfloat16>, grid, dim3(kJoinThreads), 0, s, p)
+              : launch_next(xattn_dkdv_join_kernel<float>, grid, dim3(kJoinThreads), 0, s, p);
+}
+
 template <typename T, int D>
 static cudaError_t fwd(const XattnParams& p, cudaStream_t s) {
   const size_t smem = sizeof(float) * (3 * kXs * (D + 4) + kXs * kXsLdP + kXs);
@@ -562,9 +425,7 @@ static cudaError_t bwd(const XattnParams& p, cudaStream_t s) {
   if (e == cudaSuccess)
     e = launch_next(xattn_bwd_simt_kernel<T, D>, dim3((unsigned)(n_kv + n_q)), dim3(kXsThreads), smem, s, p,
                     (uint32_t)n_kv, kslots, qslots);
-  if (e == cudaSuccess && p.nk > 0)
-    e = launch_next(xattn_dkdv_join_kernel, dim3((unsigned)((p.nk * p.Hk * D / 4 + kJoinThreads - 1) / kJoinThreads), 2),
-                    dim3(kJoinThreads), 0, s, p);
+  if (e == cudaSuccess && p.nk > 0) e = launch_xattn_dkdv_join(p, sizeof(T) == 2, s);
   return e;
 }
 

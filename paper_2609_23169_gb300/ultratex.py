@@ -29,6 +29,8 @@ EXPORTS = (
     "ut_fg_gather_rope", "ut_fg_scatter_rope", "ut_fg_mask_from_alpha", "ut_device_accessible",
     "ut_xattn_fwd_workspace_size", "ut_xattn_fwd", "ut_xattn_bwd_workspace_size", "ut_xattn_bwd",
     "ut_group_norm_fwd_workspace_size", "ut_group_norm_fwd", "ut_group_norm_bwd_workspace_size", "ut_group_norm_bwd",
+    "ut_qk_norm_rope_fwd", "ut_qk_norm_rope_bwd_workspace_size", "ut_qk_norm_rope_bwd",
+    "ut_window_attn_fwd_workspace_size", "ut_window_attn_fwd", "ut_window_attn_bwd_workspace_size", "ut_window_attn_bwd",
 )
 
 
@@ -59,6 +61,20 @@ class GnormShape(ctypes.Structure):
                 ("groups", ctypes.c_int32), ("dtype", ctypes.c_int32), ("act", ctypes.c_int32),
                 ("eps", ctypes.c_float), ("x_stride", ctypes.c_int64), ("y_stride", ctypes.c_int64),
                 ("dy_stride", ctypes.c_int64), ("dx_stride", ctypes.c_int64)]
+
+
+class QkNormShape(ctypes.Structure):
+    """ut_qknorm_shape: rows, heads, head dimension, dtype, eps, elements between rows, rows of a cache."""
+    _fields_ = [("n_rows", ctypes.c_int64), ("n_heads", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32), ("dtype", ctypes.c_int32), ("eps", ctypes.c_float),
+                ("q_stride", ctypes.c_int64), ("k_stride", ctypes.c_int64), ("v_stride", ctypes.c_int64),
+                ("qo_stride", ctypes.c_int64), ("ko_stride", ctypes.c_int64), ("vo_stride", ctypes.c_int64),
+                ("dqo_stride", ctypes.c_int64), ("dko_stride", ctypes.c_int64), ("cache_rows", ctypes.c_int64)]
+
+
+class Window(ctypes.Structure):
+    """ut_window: keys seen before and behind a query's position, first keys that stay visible."""
+    _fields_ = [("left", ctypes.c_int32), ("right", ctypes.c_int32), ("sinks", ctypes.c_int32)]
 
 
 class Rope(ctypes.Structure):
@@ -136,6 +152,19 @@ def lib() -> ctypes.CDLL:
     L.ut_group_norm_fwd.argtypes = [gs, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _sz, _vp, _vp]
     L.ut_group_norm_bwd.restype = _i32
     L.ut_group_norm_bwd.argtypes = [gs, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _sz, _vp, _vp]
+    rp, qs, wp = ctypes.POINTER(Rope), ctypes.POINTER(QkNormShape), ctypes.POINTER(Window)
+    L.ut_qk_norm_rope_fwd.restype = _i32
+    L.ut_qk_norm_rope_fwd.argtypes = [qs, rp] + [_vp] * 12
+    L.ut_qk_norm_rope_bwd_workspace_size.restype = _sz
+    L.ut_qk_norm_rope_bwd_workspace_size.argtypes = [qs, rp]
+    L.ut_qk_norm_rope_bwd.restype = _i32
+    L.ut_qk_norm_rope_bwd.argtypes = [qs, rp] + [_vp] * 12 + [_sz, _vp]
+    for name in ("ut_window_attn_fwd_workspace_size", "ut_window_attn_bwd_workspace_size"):
+        getattr(L, name).restype, getattr(L, name).argtypes = _sz, [xs, wp]
+    L.ut_window_attn_fwd.restype = _i32
+    L.ut_window_attn_fwd.argtypes = [xs, wp] + [_vp] * 7 + [_flt, _vp, _vp, _vp, _sz, _vp, _vp]
+    L.ut_window_attn_bwd.restype = _i32
+    L.ut_window_attn_bwd.argtypes = [xs, wp] + [_vp] * 7 + [_flt] + [_vp] * 7 + [_sz, _vp, _vp]
     _lib = L
     return L
 
@@ -666,3 +695,178 @@ def ut_group_norm_bwd(x: torch.Tensor, dy: torch.Tensor, gamma: Optional[torch.T
     if st:
         _check("ut_group_norm_bwd", st)
     return dx, dgamma, dbeta
+
+
+# ------------------------------------------------- windowed-attention operators
+def _qknorm_shape(q, k, eps, wq, wk, pos) -> QkNormShape:
+    qs, ks, dtype = q.shape, k.shape, q.dtype
+    if len(qs) != 3 or len(ks) != 3 or ks[0] != qs[0] or ks[2] != qs[2]:
+        raise ValueError("q is [rows, heads, d]; k is [rows, kv heads, d]")
+    if dtype not in _DTYPES:
+        raise TypeError(f"unsupported dtype {dtype}")
+    if pos is not None and (pos.dtype != torch.int32 or pos.shape != (qs[0],) or not pos.is_contiguous()):
+        raise ValueError("pos must be a contiguous int32 vector of the rows")
+    return QkNormShape(qs[0], qs[1], ks[1], qs[2], _DTYPES[dtype], eps, _head_rows(q, dtype, qs, "q"),
+                       _head_rows(k, dtype, ks, "k"), 0, qs[1] * qs[2], ks[1] * qs[2])
+
+
+def ut_qk_norm_rope_fwd(q: torch.Tensor, k: torch.Tensor, rope: Rope, v: Optional[torch.Tensor] = None,
+                        wq: Optional[torch.Tensor] = None, wk: Optional[torch.Tensor] = None, eps: float = 1e-6,
+                        pos: Optional[torch.Tensor] = None, rows: Optional[torch.Tensor] = None,
+                        q_out: Optional[torch.Tensor] = None, k_out: Optional[torch.Tensor] = None,
+                        v_out: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None):
+    """RMS norm of each head of q [N, H, d] and k [N, Hkv, d] (rows may be strided: slices of one projection) with fp32
+    weights wq, wk [d], and the position rotation at canvas positions pos [N] (int32; default 0, 1, ...).  With `rows`
+    [N] (int32) k, and v unchanged, go to those rows of the caches k_out, v_out [rows, Hkv, d]; negative entries write
+    none.  Returns (q_out, k_out), and v_out where there is a v."""
+    shape = _qknorm_shape(q, k, eps, wq, wk, pos)
+    device, dtype, d = q.device, q.dtype, shape.head_dim
+    wqp, wkp = _affine(wq, d, "wq"), _affine(wk, d, "wk")
+    _current_device(device, status)
+    _same_device(device, k, v, wq, wk, pos, rows, q_out, k_out, v_out)
+    if v is not None:
+        shape.v_stride = _head_rows(v, dtype, k.shape, "v")
+        shape.vo_stride = shape.n_kv_heads * d
+    elif v_out is not None:
+        raise ValueError("v_out without v")
+    kv = k.shape
+    if rows is not None:
+        if rows.dtype != torch.int32 or rows.shape != (shape.n_rows,) or not rows.is_contiguous():
+            raise ValueError("rows must be a contiguous int32 vector of the rows")
+        if k_out is None or (v is not None and v_out is None):
+            raise ValueError("rows are those of the caches: k_out (and v_out)")
+        kv = (k_out.shape[0],) + tuple(k.shape[1:])
+        shape.cache_rows = kv[0]
+    if q_out is None:
+        q_out = torch.empty(q.shape, dtype=dtype, device=device)
+    else:
+        shape.qo_stride = _head_rows(q_out, dtype, q.shape, "q_out")
+    if k_out is None:
+        k_out = torch.empty(kv, dtype=dtype, device=device)
+    else:
+        shape.ko_stride = _head_rows(k_out, dtype, kv, "k_out")
+    if v is not None:
+        if v_out is None:
+            v_out = torch.empty(kv, dtype=dtype, device=device)
+        else:
+            shape.vo_stride = _head_rows(v_out, dtype, kv, "v_out")
+    st = lib().ut_qk_norm_rope_fwd(ctypes.byref(shape), ctypes.byref(rope), _p(pos), q.data_ptr(), k.data_ptr(), _p(v),
+                                   wqp, wkp, _p(rows), q_out.data_ptr(), k_out.data_ptr(), _p(v_out), _p(status),
+                                   _stream())
+    if st:
+        _check("ut_qk_norm_rope_fwd", st)
+    return (q_out, k_out) if v is None else (q_out, k_out, v_out)
+
+
+def ut_qk_norm_rope_bwd(q: torch.Tensor, k: torch.Tensor, rope: Rope, dqo: torch.Tensor, dko: torch.Tensor,
+                        wq: Optional[torch.Tensor] = None, wk: Optional[torch.Tensor] = None, eps: float = 1e-6,
+                        pos: Optional[torch.Tensor] = None, dq: Optional[torch.Tensor] = None,
+                        dk: Optional[torch.Tensor] = None, dwq: Optional[torch.Tensor] = None,
+                        dwk: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None):
+    """Gradient of ut_qk_norm_rope_fwd (q and k are its inputs).  Returns (dq, dk, dwq [d], dwk [d] fp32)."""
+    shape = _qknorm_shape(q, k, eps, wq, wk, pos)
+    device, dtype, d = q.device, q.dtype, shape.head_dim
+    wqp, wkp = _affine(wq, d, "wq"), _affine(wk, d, "wk")
+    _current_device(device, None)
+    _same_device(device, k, wq, wk, pos, dqo, dko, dq, dk, dwq, dwk)
+    shape.dqo_stride = _head_rows(dqo, dtype, q.shape, "dqo")
+    shape.dko_stride = _head_rows(dko, dtype, k.shape, "dko")
+    if dq is None:
+        dq = torch.empty(q.shape, dtype=dtype, device=device)
+    else:
+        shape.qo_stride = _head_rows(dq, dtype, q.shape, "dq")
+    if dk is None:
+        dk = torch.empty(k.shape, dtype=dtype, device=device)
+    else:
+        shape.ko_stride = _head_rows(dk, dtype, k.shape, "dk")
+    if dwq is None:
+        dwq = torch.empty(d, dtype=torch.float32, device=device)
+    if dwk is None:
+        dwk = torch.empty(d, dtype=torch.float32, device=device)
+    dwqp, dwkp = _affine(dwq, d, "dwq"), _affine(dwk, d, "dwk")
+    L, ref, rr = lib(), ctypes.byref(shape), ctypes.byref(rope)
+    ws, wsp, wsb = _workspace(ws, L.ut_qk_norm_rope_bwd_workspace_size(ref, rr), device)
+    st = L.ut_qk_norm_rope_bwd(ref, rr, _p(pos), q.data_ptr(), k.data_ptr(), wqp, wkp, dqo.data_ptr(), dko.data_ptr(),
+                               dq.data_ptr(), dk.data_ptr(), dwqp, dwkp, wsp, wsb, _stream())
+    if st:
+        _check("ut_qk_norm_rope_bwd", st)
+    return dq, dk, dwq, dwk
+
+
+_MOST = 2 ** 31 - 1
+
+
+def _window(left: int, right: int, sinks: int, k_len: Optional[torch.Tensor], shape: XattnShape, device) -> Window:
+    if k_len is not None:
+        if k_len.dtype != torch.int32 or k_len.shape != (shape.n_seg,) or not k_len.is_contiguous():
+            raise ValueError("k_len must be a contiguous int32 vector of the segments")
+        _same_device(device, k_len)
+    if min(left, right, sinks) < 0:
+        raise ValueError("left, right and sinks are numbers of keys: not negative")
+    return Window(min(left, _MOST), min(right, _MOST), min(sinks, _MOST))
+
+
+def ut_window_attn_fwd(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, left: int, right: int = 0, sinks: int = 0,
+                       softmax_scale: Optional[float] = None, cu_q: Optional[torch.Tensor] = None,
+                       cu_k: Optional[torch.Tensor] = None, k_len: Optional[torch.Tensor] = None,
+                       key_mask: Optional[torch.Tensor] = None, o: Optional[torch.Tensor] = None,
+                       lse: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None,
+                       status: Optional[torch.Tensor] = None):
+    """Attention of packed query rows q [Nq, H, d] to k, v [Nk, Hkv, d], segment by segment (cu_q, cu_k: int32 prefixes
+    of the lengths, on the device; k_len [segments]: filled rows of each segment's keys, a cache).  Query i of a
+    segment's n_q stands at p = n_k - n_q + i and sees the keys j <= p + right that are j >= p - left or j < sinks and
+    have key_mask != 0.  Returns (O [Nq, H, d], LSE [H, Nq] fp32)."""
+    shape = _xattn_shape(q, k, v, cu_q, cu_k, key_mask, status)
+    device = q.device
+    window = _window(left, right, sinks, k_len, shape, device)
+    if o is None:
+        o = torch.empty(q.shape, dtype=q.dtype, device=device)
+    else:
+        shape.o_stride = _head_rows(o, q.dtype, q.shape, "o")
+        _same_device(device, o)
+    if lse is None:
+        lse = torch.empty((shape.n_heads, shape.n_q), dtype=torch.float32, device=device)
+    else:
+        _check_lse(lse, q)
+        _same_device(device, lse)
+    L, ref, wr = lib(), ctypes.byref(shape), ctypes.byref(window)
+    ws, wsp, wsb = _workspace(ws, L.ut_window_attn_fwd_workspace_size(ref, wr), device)
+    st = L.ut_window_attn_fwd(ref, wr, q.data_ptr(), k.data_ptr(), v.data_ptr(), _p(cu_q), _p(cu_k), _p(k_len),
+                              _p(key_mask), shape.head_dim ** -0.5 if softmax_scale is None else softmax_scale,
+                              o.data_ptr(), lse.data_ptr(), wsp, wsb, _p(status), _stream())
+    if st:
+        _check("ut_window_attn_fwd", st)
+    return o, lse
+
+
+def ut_window_attn_bwd(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, o: torch.Tensor, lse: torch.Tensor,
+                       dout: torch.Tensor, left: int, right: int = 0, sinks: int = 0,
+                       softmax_scale: Optional[float] = None, cu_q: Optional[torch.Tensor] = None,
+                       cu_k: Optional[torch.Tensor] = None, k_len: Optional[torch.Tensor] = None,
+                       key_mask: Optional[torch.Tensor] = None, dq: Optional[torch.Tensor] = None,
+                       dk: Optional[torch.Tensor] = None, dv: Optional[torch.Tensor] = None,
+                       ws: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None):
+    """Gradient of ut_window_attn_fwd (o and lse are its outputs).  Returns (dQ, dK, dV)."""
+    shape = _xattn_shape(q, k, v, cu_q, cu_k, key_mask, status)
+    device, dtype = q.device, q.dtype
+    window = _window(left, right, sinks, k_len, shape, device)
+    _check_lse(lse, q)
+    _same_device(device, o, lse, dout, dq, dk, dv)
+    shape.o_stride = _head_rows(o, dtype, q.shape, "o")
+    shape.do_stride = _head_rows(dout, dtype, q.shape, "dout")
+    H_d, Hk_d = shape.n_heads * shape.head_dim, shape.n_kv_heads * shape.head_dim
+    shape.dq_stride = H_d if dq is None else _head_rows(dq, dtype, q.shape, "dq")
+    shape.dk_stride = Hk_d if dk is None else _head_rows(dk, dtype, k.shape, "dk")
+    shape.dv_stride = Hk_d if dv is None else _head_rows(dv, dtype, k.shape, "dv")
+    dq = torch.empty(q.shape, dtype=dtype, device=device) if dq is None else dq
+    dk = torch.empty(k.shape, dtype=dtype, device=device) if dk is None else dk
+    dv = torch.empty(v.shape, dtype=dtype, device=device) if dv is None else dv
+    L, ref, wr = lib(), ctypes.byref(shape), ctypes.byref(window)
+    ws, wsp, wsb = _workspace(ws, L.ut_window_attn_bwd_workspace_size(ref, wr), device)
+    st = L.ut_window_attn_bwd(ref, wr, q.data_ptr(), k.data_ptr(), v.data_ptr(), _p(cu_q), _p(cu_k), _p(k_len),
+                              _p(key_mask), shape.head_dim ** -0.5 if softmax_scale is None else softmax_scale,
+                              o.data_ptr(), lse.data_ptr(), dout.data_ptr(), dq.data_ptr(), dk.data_ptr(),
+                              dv.data_ptr(), wsp, wsb, _p(status), _stream())
+    if st:
+        _check("ut_window_attn_bwd", st)
+    return dq, dk, dv
