@@ -81,8 +81,10 @@ static ut_status window_problem(const ut_xattn_shape* s, const ut_window* win, b
   w->left = win->left < kWinMost ? win->left : kWinMost;
   w->right = win->right < kWinMost ? win->right : kWinMost;
   w->sinks = win->sinks < kWinMost ? win->sinks : kWinMost;
-  if (wattn_simt_items(*w, backward) > INT32_MAX / 2) return UT_ERR_UNSUPPORTED;
-  w->x.nsplit = wattn_simt_splits(*w, backward);
+  if (s->n_q > kWinMost || s->n_k > kWinMost) return UT_ERR_UNSUPPORTED;
+  const bool tc = s->dtype == UT_BF16 && !backward;
+  if ((tc ? wattn_fwd_tc_items(*w) : wattn_simt_items(*w, backward)) > INT32_MAX / 2) return UT_ERR_UNSUPPORTED;
+  w->x.nsplit = tc ? wattn_fwd_tc_splits(*w) : wattn_simt_splits(*w, backward);
   return UT_OK;
 }
 
@@ -199,7 +201,7 @@ ut_status ut_window_attn_fwd(const ut_xattn_shape* shape, const ut_window* windo
   }
   const bool bf16 = shape->dtype == UT_BF16;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
-  cudaError_t e = launch_wattn_fwd_simt(w, bf16, s);
+  cudaError_t e = bf16 ? launch_wattn_fwd_tc(w, s) : launch_wattn_fwd_simt(w, s);
   if (e == cudaSuccess && p.nsplit > 1) e = launch_xattn_join(p, bf16, s);
   return status_of(e);
 }

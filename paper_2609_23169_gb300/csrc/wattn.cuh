@@ -19,7 +19,9 @@ struct WinParams {
   const int32_t* k_len;    // [B] or NULL
   int left, right, sinks;  // at most kWinMost
 };
-constexpr int kWinMost = (1 << 30) - 2;  // p + right + 1 and p - left fit 32 bits (rows are below 2^30)
+// Most rows, and the most that left, right and sinks need to be: positions of a
+// tile's rows (a few behind the last too) plus right or less left fit 32 bits.
+constexpr int kWinMost = (1 << 30) - 512;
 
 // Keys of segment s: their first row and number
 __host__ __device__ __forceinline__ void win_keys(const WinParams& w, int s, int64_t& row, int64_t& n) {
@@ -80,7 +82,11 @@ __device__ __forceinline__ void check_lens_of(const WinParams& w) {
 // wattn_simt.cu
 int64_t wattn_simt_items(const WinParams& w, bool backward);
 int wattn_simt_splits(const WinParams& w, bool backward);
-cudaError_t launch_wattn_fwd_simt(const WinParams& w, bool bf16, cudaStream_t s);
+cudaError_t launch_wattn_fwd_simt(const WinParams& w, cudaStream_t s);  // fp32
 cudaError_t launch_wattn_bwd_simt(const WinParams& w, bool bf16, cudaStream_t s);
+// wattn_fwd_tc.cu (bf16)
+int64_t wattn_fwd_tc_items(const WinParams& w);
+int wattn_fwd_tc_splits(const WinParams& w);
+cudaError_t launch_wattn_fwd_tc(const WinParams& w, cudaStream_t s);
 
 }  // namespace ut

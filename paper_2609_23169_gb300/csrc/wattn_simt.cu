@@ -354,8 +354,7 @@ int wattn_simt_splits(const WinParams& w, bool backward) {
   return (int)(n < 1 ? 1 : n > 1024 ? 1024 : n);
 }
 
-cudaError_t launch_wattn_fwd_simt(const WinParams& w, bool bf16, cudaStream_t s) {
-  if (bf16) return w.x.d == 64 ? fwd<__nv_bfloat16, 64>(w, s) : fwd<__nv_bfloat16, 128>(w, s);
+cudaError_t launch_wattn_fwd_simt(const WinParams& w, cudaStream_t s) {
   return w.x.d == 64 ? fwd<float, 64>(w, s) : fwd<float, 128>(w, s);
 }
 cudaError_t launch_wattn_bwd_simt(const WinParams& w, bool bf16, cudaStream_t s) {

@@ -69,10 +69,26 @@ UT_DEV void mma_tn(uint32_t d, uint32_t a, uint32_t b_lo, uint32_t idesc, uint32
                      UT_TS_STEP("24", "384", "t") "}" ::"r"(d),
                  "r"(a), "r"(b_lo), "r"(idesc), "r"(accumulate), "r"(kDescHi)
                  : "memory");
+  else if constexpr (N == 128)
+    asm volatile(UT_TS_HEAD UT_TS_STEP("0", "0", "p") UT_TS_STEP("8", "128", "t") UT_TS_STEP("16", "256", "t")
+                     UT_TS_STEP("24", "384", "t") UT_TS_STEP("32", "512", "t") UT_TS_STEP("40", "640", "t")
+                         UT_TS_STEP("48", "768", "t") UT_TS_STEP("56", "896", "t") "}" ::"r"(d),
+                 "r"(a), "r"(b_lo), "r"(idesc), "r"(accumulate), "r"(kDescHi)
+                 : "memory");
   else
     asm volatile(UT_TS_HEAD UT_TS_STEP("0", "0", "p") UT_TS_STEP("8", "128", "t") "}" ::"r"(d), "r"(a), "r"(b_lo),
                  "r"(idesc), "r"(accumulate), "r"(kDescHi)
                  : "memory");
+}
+
+// d = A B^T over 128 columns: A in TMEM (bf16 pairs), B a K-major tile
+UT_DEV void mma_tk128(uint32_t d, uint32_t a, uint32_t b_lo, uint32_t idesc) {
+  const uint32_t accumulate = 0;
+  asm volatile(UT_TS_HEAD UT_TS_STEP("0", "0", "p") UT_TS_STEP("8", "2", "t") UT_TS_STEP("16", "4", "t")
+                   UT_TS_STEP("24", "6", "t") UT_TS_STEP("32", "1024", "t") UT_TS_STEP("40", "1026", "t")
+                       UT_TS_STEP("48", "1028", "t") UT_TS_STEP("56", "1030", "t") "}" ::"r"(d),
+               "r"(a), "r"(b_lo), "r"(idesc), "r"(accumulate), "r"(kDescHi)
+               : "memory");
 }
 
 // d (+)= A B over 128 rows of B, A in TMEM as two halves of 64 columns, each in

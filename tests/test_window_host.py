@@ -318,7 +318,7 @@ int main() {
           for (int sinks : {0, 1, 4, 7, 8, 15, far})
             for (int tile : {1, 3, 8}) wrong += check<8>(n_q, n_k, left, right, sinks, tile) + check<4>(n_q, n_k, left, right, sinks, tile);
   // the largest numbers: no overflow
-  const int most = (1 << 30) - 1;
+  const int most = kWinMost;
   const WinRange r = win_range(most - 1, most - 1, most, far, far, far), s = win_range(-most, -most + 5, 7, far, far, 3);
   wrong += r.hi != most || r.lo != 0 || s.lo != 0 || s.hi < 0 || s.hi > 7;
   int a, b;
