@@ -64,7 +64,7 @@ static_assert(Form<64>::kRegCtl + Form<64>::kRegSoftmax <= 2 * Form<64>::kRegLau
 
 struct Item {
   int32_t hk;          // kv head; -1: no more items
-  int32_t blocks;      // key blocks of this item (0: write the empty result)
+  int32_t blocks;      // its key blocks, at least one
   int32_t tok0, ntok;  // its tokens
   int32_t p0;          // position of the first
   int32_t key0;        // first key of the segment
@@ -100,6 +100,24 @@ struct Params {
   float scale_log2;
   bool keep_kv;     // K and V are read by several items: keep them in L2
 };
+
+// The result of a tile without keys, or of a part without blocks: O = 0, LSE =
+// -inf, or their partial results.  Whole warp.
+template <int D>
+UT_DEV void empty_rows(const XattnParams& p, int hk, int tok0, int ntok, int split, uint32_t lane) {
+  for (int r = (int)lane / 8; r < ntok * p.G; r += 4) {
+    const int tok = tok0 + r / p.G, h = hk * p.G + r % p.G;
+    if (p.nsplit > 1) {
+      const int64_t row = ((int64_t)split * p.nq + tok) * p.H + h;
+      for (int c = (int)(lane & 7) * 4; c < D; c += 32) *reinterpret_cast<uint4*>(p.part_o + row * D + c) = make_uint4(0, 0, 0, 0);
+      if ((lane & 7) == 0) p.part_ml[row] = make_float2(-1e30f, 0.f);
+    } else {
+      __nv_bfloat16* out = static_cast<__nv_bfloat16*>(p.o) + (int64_t)tok * p.os + (int64_t)h * D;
+      for (int c = (int)(lane & 7) * 8; c < D; c += 64) *reinterpret_cast<uint4*>(out + c) = make_uint4(0, 0, 0, 0);
+      if ((lane & 7) == 0) p.lse[(int64_t)h * p.nq + tok] = -INFINITY;
+    }
+  }
+}
 
 template <int D>
 __global__ void __launch_bounds__(kThreads, Form<D>::kCtas)
@@ -197,7 +215,6 @@ __global__ void __launch_bounds__(kThreads, Form<D>::kCtas)
       bool ok = true;
       Item it;
       while (ok && next_item(n, it, ok)) {
-        if (it.blocks == 0) continue;
         const uint32_t qs = nq % F::kQ;
         if (!(ok = wait(&sm.q_empty[qs], ((nq / F::kQ) & 1) ^ 1))) break;
         if (lane == 0) {
@@ -263,6 +280,10 @@ __global__ void __launch_bounds__(kThreads, Form<D>::kCtas)
             const int all = win_blocks<kN>(it.rg), per = (all + p.nsplit - 1) / p.nsplit;
             it.j0 = min(all, per * split);
             it.blocks = min(all, it.j0 + per) - it.j0;
+            if (it.blocks == 0) {  // nothing to see: the result at once
+              empty_rows<D>(p, it.hk, it.tok0, it.ntok, split, lane);
+              it.hk = -1;
+            }
           }
         }
         if (u < 0 || it.hk >= 0) {
@@ -293,7 +314,7 @@ __global__ void __launch_bounds__(kThreads, Form<D>::kCtas)
           block_of(it, t, x, e);
           return all_keys(x, e) ? 15u : lane_keys(p.mask, (int64_t)it.key0 + x, e - x, lane);
         };
-        uint32_t next = it.blocks > 0 ? keys_of(0) : 0;
+        uint32_t next = keys_of(0);
         for (int t = 0; t < it.blocks; ++t, ++at) {
           const uint32_t st = at % F::kV, keys = next;
           int x, e;
@@ -355,7 +376,7 @@ __global__ void __launch_bounds__(kThreads, Form<D>::kCtas)
 #pragma unroll 1
       do {
         uint32_t fn = 0;
-        while (left == 0 && !end) {
+        if (left == 0 && !end) {
           const uint32_t s = n % kItemSlots;
           if (!(ok = waitq(&sm.item_full[s], (n / kItemSlots) & 1))) break;
           end = (int)warp_uniform((uint32_t)sm.item[s].hk) < 0;
@@ -363,9 +384,8 @@ __global__ void __launch_bounds__(kThreads, Form<D>::kCtas)
           __syncwarp();
           if (lane == 0) mbar_arrive(&sm.item_empty[s]);
           ++n;
-          if (left > 0) fn = kFirst;
+          if (!end) fn = kFirst;
         }
-        if (!ok) break;
         const bool early = F::kQt && (fn & kFirst);  // P V first
         if (early && f0 && !(ok = pv(f0))) break;
         if (left > 0) {
@@ -417,8 +437,8 @@ __global__ void __launch_bounds__(kThreads, Form<D>::kCtas)
     int e_hk = 0, e_tok0 = 0, e_ntok = 0, e_split = 0;
     float e_m = 0.f, e_l = 0.f;
 
-    // O / l in bf16 and LSE, or the partial result; `some`: O is in TMEM (else 0)
-    auto write_rows = [&](bool some, int hk, int tok0, int ntok, int split, float em, float el) {
+    // O / l in bf16 and LSE, or the partial result
+    auto write_rows = [&](int hk, int tok0, int ntok, int split, float em, float el) {
       const int h = hk * p.G + (int)(row - rt * p.G);
       const bool row_ok = rt < ntok;
       if (p.nsplit > 1) {
@@ -426,13 +446,8 @@ __global__ void __launch_bounds__(kThreads, Form<D>::kCtas)
 #pragma unroll 1
         for (int g = 0; g < D / 32; ++g) {
           uint32_t r[32];
-          if (some) {
-            tmem_ld32(lane_base + F::kO + g * 32, r);
-            tmem_wait_ld();
-          } else {
-#pragma unroll
-            for (int x = 0; x < 32; ++x) r[x] = 0;
-          }
+          tmem_ld32(lane_base + F::kO + g * 32, r);
+          tmem_wait_ld();
           if (!row_ok) continue;
 #pragma unroll
           for (int x = 0; x < 32; x += 4)
@@ -441,7 +456,7 @@ __global__ void __launch_bounds__(kThreads, Form<D>::kCtas)
         if (row_ok) p.part_ml[prow] = make_float2(em, el);
         tc_fence_before();
         __syncwarp();
-        if (some && lane == 0) mbar_arrive(&sm.o_empty);
+        if (lane == 0) mbar_arrive(&sm.o_empty);
         return;
       }
       if (row_ok) p.lse[(int64_t)h * p.nq + tok0 + rt] = el == 0.f ? -INFINITY : (em + log2f(el)) * kLn2;
@@ -460,23 +475,17 @@ __global__ void __launch_bounds__(kThreads, Form<D>::kCtas)
       }
 #pragma unroll 1
       for (int g = 0; g < D / 32; ++g) {
-        uint32_t u[4][4];
-        if (some) {
-          uint32_t r[32];
-          tmem_ld32(lane_base + F::kO + g * 32, r);
-          tmem_wait_ld();
-#pragma unroll
-          for (int x = 0; x < 16; ++x)
-            u[x >> 2][x & 3] = pack_bf16x2(__uint_as_float(r[2 * x]) * f, __uint_as_float(r[2 * x + 1]) * f);
-        } else {
-#pragma unroll
-          for (int x = 0; x < 16; ++x) u[x >> 2][x & 3] = 0;
-        }
+        uint32_t r[32], u[4][4];
+        tmem_ld32(lane_base + F::kO + g * 32, r);
+        tmem_wait_ld();
         if (g == D / 32 - 1) {
           tc_fence_before();
           __syncwarp();
-          if (some && lane == 0) mbar_arrive(&sm.o_empty);
+          if (lane == 0) mbar_arrive(&sm.o_empty);
         }
+#pragma unroll
+        for (int x = 0; x < 16; ++x)
+          u[x >> 2][x & 3] = pack_bf16x2(__uint_as_float(r[2 * x]) * f, __uint_as_float(r[2 * x + 1]) * f);
         exchange_units<1>(u, c & 1, 0, 1);
         exchange_units<1>(u, c & 1, 2, 3);
         exchange_units<2>(u, c >> 1, 0, 2);
@@ -485,11 +494,6 @@ __global__ void __launch_bounds__(kThreads, Form<D>::kCtas)
         for (int i = 0; i < 4; ++i)
           if (out[i]) *reinterpret_cast<uint4*>(out[i] + g * 32) = make_uint4(u[i][0], u[i][1], u[i][2], u[i][3]);
       }
-    };
-    // The next item with key blocks into nx (hk < 0: none); empty ones are written here.
-    auto advance = [&]() {
-      while (next_item(n, nx, ok) && nx.blocks == 0)
-        write_rows(false, nx.hk, nx.tok0, nx.ntok, nx.split, -1e30f, 0.f);
     };
     // nx's Q tile: shared memory (128B-swizzled, as TMA wrote it) -> TMEM, this
     // thread's row, bf16 pairs: the A operand of S = Q K^T
@@ -519,17 +523,50 @@ __global__ void __launch_bounds__(kThreads, Form<D>::kCtas)
       return true;
     };
 
-    advance();
-    if (F::kQt && ok && nx.hk >= 0) ok = load_q();
-    while (ok && nx.hk >= 0) {
-      it = nx;
-      const int pos = it.p0 + rt;  // of this row's token
-      for (int t = 0; t < it.blocks; ++t, ++b) {
+    bool more = next_item(n, nx, ok), first = true;
+    if (F::kQt && more) ok = load_q();
+    int t = 0, pos = 0;
+    // A block a round; the last round only writes the last item's rows.
+#pragma unroll 1
+    while (ok && (more || pend)) {
+      bool last = false;
+      if (more) {
+        if (first) {
+          it = nx;
+          pos = it.p0 + rt;  // of this row's token
+          t = 0;
+        }
         int x, e;
         block_of(it, t, x, e);
         const uint32_t sb = b % F::kS, ts = lane_base + sb * kN;
+        const bool whole = all_keys(x, e);
+        last = t == it.blocks - 1;
         if (!(ok = wait(&sm.s_full[sb], (b / F::kS) & 1))) break;
+        if (!whole && !(ok = wait(&sm.v_ready[vst], vf))) break;
         tc_fence_after();
+        // The rows' own limits, where some row of the warp has one in this block:
+        // S there becomes -inf in TMEM, 32 columns at a time.  (In the code below,
+        // unrolled over 128 columns, they cost every block 1,500 cycles: the code
+        // no longer fits the instruction cache.)
+        const bool lim_r = it.p0 + rt_first + prm.w.right - x < kN - 1,
+                   lim_l = it.p0 + rt_last - prm.w.left > x && x + kN > prm.w.sinks;
+        if (lim_r || lim_l) {
+          const int hi = pos + prm.w.right - x, lo = pos - prm.w.left - x, sink = prm.w.sinks - x;
+#pragma unroll 1
+          for (int g = 0; g < kN; g += 32) {
+            const bool cut = (g + 31 > it.p0 + rt_first + prm.w.right - x) ||
+                             (g < it.p0 + rt_last - prm.w.left - x && g + 31 >= sink);
+            if (!cut) continue;
+            uint32_t r[32];
+            tmem_ld32(ts + g, r);
+            tmem_wait_ld();
+#pragma unroll
+            for (int y = 0; y < 32; ++y)
+              if (y > hi - g || (y < lo - g && y >= sink - g)) r[y] = 0xff800000u;
+            tmem_st32(ts + g, r);
+          }
+          tmem_wait_st();
+        }
         uint32_t r[kN];
 #pragma unroll
         for (int g = 0; g < 4; ++g) tmem_ld32(ts + g * 32, *reinterpret_cast<uint32_t(*)[32]>(&r[g * 32]));
@@ -537,13 +574,13 @@ __global__ void __launch_bounds__(kThreads, Form<D>::kCtas)
         tc_fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive(&sm.s_empty[sb]);
-        if (t == it.blocks - 1) {
-          advance();
-          if (F::kQt && ok && nx.hk >= 0) ok = load_q();
+        if (last) {  // the next item's Q: its first S is computed while this block is in the softmax
+          more = next_item(n, nx, ok);
+          if (F::kQt && more) ok = load_q();
           if (!ok) break;
         }
-        if (!all_keys(x, e)) {
-          if (!(ok = wait(&sm.v_ready[vst], vf))) break;
+        if (!whole) {
+          asm volatile("" ::: "memory");  // a branch, not a choice between 128 values
 #pragma unroll
           for (int y = 0; y < kN; y += 4) {
             const float4 v = *reinterpret_cast<const float4*>(sm.bias[vst] + y);
@@ -557,19 +594,6 @@ __global__ void __launch_bounds__(kThreads, Form<D>::kCtas)
           vst = 0;
           vf ^= 1;
         }
-        // the rows' own limits, where some row of the warp has one in this block
-        if (it.p0 + rt_first + prm.w.right - x < kN - 1) {
-          const int last = pos + prm.w.right - x;
-#pragma unroll
-          for (int y = 0; y < kN; ++y)
-            if (y > last) r[y] = __float_as_uint(-INFINITY);
-        }
-        if (it.p0 + rt_last - prm.w.left > x && x + kN > prm.w.sinks) {
-          const int first = pos - prm.w.left - x, sink = prm.w.sinks - x;
-#pragma unroll
-          for (int y = 0; y < kN; ++y)
-            if (y < first && y >= sink) r[y] = __float_as_uint(-INFINITY);
-        }
         float m8[8];
 #pragma unroll
         for (int y = 0; y < 8; ++y) m8[y] = fmaxf(__uint_as_float(r[y]), __uint_as_float(r[y + 8]));
@@ -579,29 +603,16 @@ __global__ void __launch_bounds__(kThreads, Form<D>::kCtas)
           for (int z = 0; z < 8; ++z) m8[z] = max3(m8[z], __uint_as_float(r[y + z]), __uint_as_float(r[y + z + 8]));
         float mx = max3(max3(m8[0], m8[1], m8[2]), max3(m8[3], m8[4], m8[5]), fmaxf(m8[6], m8[7]));
         mx = fmaxf(mx * prm.scale_log2, -1e30f);  // finite where a row sees no key of the block
-        bool waited = false;
-        if (t == 0) {
+        const bool need = !first && mx > m + 8.0f;
+        const bool any = __any_sync(0xffffffffu, need);
+        float alpha = 1.f;
+        if (first) {
           m = mx;
           l = 0.f;
-        } else {
-          const bool need = mx > m + 8.0f;
-          if (__any_sync(0xffffffffu, need)) {
-            if (!(ok = wait(&sm.pv_done, (b & 1) ^ 1))) break;  // O holds P V up to the block before
-            waited = true;
-            tc_fence_after();
-            const float alpha = need ? ex2_approx(m - mx) : 1.0f;
-            if (need) m = mx;
-            l *= alpha;
-#pragma unroll 1
-            for (int g = 0; g < D / 16; ++g) {
-              uint32_t o[16];
-              tmem_ld16(lane_base + F::kO + g * 16, o);
-              tmem_wait_ld();
-#pragma unroll
-              for (int y = 0; y < 16; ++y) o[y] = __float_as_uint(__uint_as_float(o[y]) * alpha);
-              tmem_st16(lane_base + F::kO + g * 16, o);
-            }
-          }
+        } else if (need) {
+          alpha = ex2_approx(m - mx);
+          m = mx;
+          l *= alpha;
         }
         const uint64_t m2 = pack_f32x2(-m, -m);
         uint64_t sum[4] = {0, 0, 0, 0};
@@ -618,29 +629,45 @@ __global__ void __launch_bounds__(kThreads, Form<D>::kCtas)
         float a0, a1;
         unpack_f32x2(add_f32x2(add_f32x2(sum[0], sum[1]), add_f32x2(sum[2], sum[3])), a0, a1);
         l += a0 + a1;
-        // P's columns are free once the product of the block before is done
-        if (!waited && !(ok = wait(&sm.pv_done, (b & 1) ^ 1))) break;
+        // P's columns are free, and O holds P V up to the block before, once its
+        // product is done
+        if (!(ok = wait(&sm.pv_done, (b & 1) ^ 1))) break;
         tc_fence_after();
+        if (any) {
+#pragma unroll 1
+          for (int g = 0; g < D / 16; ++g) {
+            uint32_t o[16];
+            tmem_ld16(lane_base + F::kO + g * 16, o);
+            tmem_wait_ld();
+#pragma unroll
+            for (int y = 0; y < 16; ++y) o[y] = __float_as_uint(__uint_as_float(o[y]) * alpha);
+            tmem_st16(lane_base + F::kO + g * 16, o);
+          }
+        }
         tmem_st32(lane_base + F::kP, *reinterpret_cast<uint32_t(*)[32]>(&pk[0]));
         tmem_st32(lane_base + F::kP + 32, *reinterpret_cast<uint32_t(*)[32]>(&pk[32]));
         tmem_wait_st();
         tc_fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive(&sm.p_full);
-        if (t == 0 && pend) write_rows(true, e_hk, e_tok0, e_ntok, e_split, e_m, e_l);
+        ++b;
+        ++t;
+      } else {
+        if (!(ok = wait(&sm.pv_done, (b & 1) ^ 1))) break;
+        tc_fence_after();
       }
-      if (!ok) break;
-      pend = true;
-      e_hk = it.hk;
-      e_tok0 = it.tok0;
-      e_ntok = it.ntok;
-      e_split = it.split;
-      e_m = m;
-      e_l = l;
-    }
-    if (ok && pend && wait(&sm.pv_done, (b & 1) ^ 1)) {
-      tc_fence_after();
-      write_rows(true, e_hk, e_tok0, e_ntok, e_split, e_m, e_l);
+      if (first && pend) write_rows(e_hk, e_tok0, e_ntok, e_split, e_m, e_l);
+      if (first) pend = false;
+      first = last;
+      if (last) {
+        pend = true;
+        e_hk = it.hk;
+        e_tok0 = it.tok0;
+        e_ntok = it.ntok;
+        e_split = it.split;
+        e_m = m;
+        e_l = l;
+      }
     }
   }
   tc_fence_before();
