@@ -11,26 +11,31 @@
 // tokens takes ceil((left + right + t) / 128) of them.
 //
 // CTAs take item after item (NextItem), the head fastest: CTAs in flight share
-// the windows of neighbouring tiles in L2.  Roles (256 threads):
+// the windows of neighbouring tiles in L2.  Roles:
 //   warp 0      TMA: Q, K and V tiles, a ring each
 //   warp 1      TMEM owner and MMA issuer: S = Q K^T, O += P V.  The products
 //               follow one another across items: the next item's first S is
 //               computed while this one's last blocks are in the softmax.
 //   warp 2      asks for the items and decodes them into a ring
-//   warp 3      which keys of a block count: a bias for S, and the rows of the V
+//   warp 3      which keys of a block count, a bit each, and the rows of the V
 //               tile that do not become zero, so that no value they hold (NaN,
 //               infinities) is multiplied
-//   warps 4-7   softmax: thread = row = TMEM lane.  Read S, apply the keys' bias
-//               and the row's own limits (only in blocks where some row of the
-//               warp has one), keep a running maximum (O is rescaled in TMEM only
-//               where it grew by more than 2^8, so the exponentials stay
-//               bounded), write P as bf16; O / l and LSE (or the split's partial
-//               result) of an item are written after the first block of the next.
-// d = 128: one CTA an SM, two S buffers, Q copied to TMEM by the softmax warps
-// (S = Q K^T then reads only K from shared memory).  TMEM columns S0 [0,128),
-// S1 [128,256), O [256,384), P [384,448), Q [448,512).
+//   softmax     thread = row = TMEM lane; at d = 128 two warps share 32 rows and
+//               take 64 columns each.  Pass 1: the maximum; where keys do not
+//               count or a row of the warp has its limits in the block, S becomes
+//               -inf there.  Pass 2: P as bf16 over S.  O is rescaled in TMEM only where the maximum grew by
+//               more than 2^8, so the exponentials stay bounded.
+//   output      Q from shared memory to TMEM (d = 128), O / l and LSE, or the
+//               split's partial result
+// The passes are unrolled over 64 columns, or 32 (d = 64: then S is read again):
+// four warps unrolled over 128 columns are slower (2048 canvas 1,481 us instead of
+// 1,383, a third of a softmax warp's time without an instruction), eight over 32
+// too (1,532).
+// d = 128: one CTA an SM, two S buffers, Q in TMEM (S = Q K^T then reads only K
+// from shared memory).  TMEM columns S0 [0,128), S1 [128,256), O [256,384), Q
+// [384,448), the rows' maximum and sums [448,451).
 // d = 64: two CTAs an SM, whose softmaxes and products overlap; one S buffer, Q
-// in shared memory.  TMEM columns S [0,128), O [128,192), P [192,256).
+// in shared memory.  TMEM columns S [0,128), O [128,192), [192,194).
 // Rounding: P to bf16 for its product (the sum l is of the unrounded values),
 // O once at the end.
 // Every wait is bounded; on expiry the kernel records UT_ERR_TIMEOUT, drains
@@ -45,7 +50,7 @@ namespace ut {
 
 namespace {
 
-constexpr int kM = 128, kN = 128, kThreads = 256;
+constexpr int kM = 128, kN = 128;
 constexpr uint32_t kChunkBytes = 128 * 128;  // 128 rows x 64 bf16
 constexpr int kItemSlots = 3;                // no more are taken ahead: other CTAs may be idle
 
@@ -54,13 +59,15 @@ struct Form {
   static constexpr int kCtas = D == 128 ? 1 : 2;    // an SM
   static constexpr bool kQt = D == 128;             // Q in TMEM
   static constexpr int kS = D == 128 ? 2 : 1;       // S buffers
+  static constexpr int kHalves = D == 128 ? 2 : 1;  // softmax warps of 32 rows
+  static constexpr int kSoftmax = 4 * kHalves, kThreads = 32 * (8 + kSoftmax);
   static constexpr int kQ = D == 128 ? 1 : 2, kK = D == 128 ? 3 : 2, kV = kK;  // tiles in shared memory
   static constexpr uint32_t kCols = D == 128 ? 512 : 256;
-  static constexpr uint32_t kO = D == 128 ? 256 : 128, kP = D == 128 ? 384 : 192, kQc = 448;
-  // registers of the two-CTA form: per thread, launch and setmaxnreg split
-  static constexpr int kRegLaunch = 128, kRegCtl = 64, kRegSoftmax = 192;
+  static constexpr uint32_t kO = D == 128 ? 256 : 128, kQc = 384, kMl = D == 128 ? 448 : 192;
+  // registers per thread of the two-CTA form: launch and setmaxnreg split
+  static constexpr int kRegLaunch = 80, kRegCtl = 64, kRegSoftmax = 112, kRegOut = 64;
+  static_assert(kRegCtl + kRegSoftmax + kRegOut <= 3 * kRegLaunch, "the split must fit the launch");
 };
-static_assert(Form<64>::kRegCtl + Form<64>::kRegSoftmax <= 2 * Form<64>::kRegLaunch, "the split must fit the launch");
 
 struct Item {
   int32_t hk;          // kv head; -1: no more items
@@ -81,9 +88,10 @@ struct Smem {
   alignas(1024) uint8_t q[F::kQ][kTile];
   alignas(1024) uint8_t k[F::kK][kTile];
   alignas(1024) uint8_t v[F::kV][kTile];
-  alignas(16) float bias[F::kV][kN];  // of the keys of a V tile: 0 < bias = attend
+  uint32_t keys[F::kV][4];         // of a V tile: bit = attend
+  float most[2][F::kHalves][kM];   // of the halves of a row
   uint64_t q_full[F::kQ], q_empty[F::kQ], k_full[F::kK], k_empty[F::kK], v_full[F::kV], v_empty[F::kV], v_ready[F::kV];
-  uint64_t qt_full, qt_empty, s_full[F::kS], s_empty[F::kS], p_full, pv_done, o_empty, mma_done;
+  uint64_t qt_full, qt_empty, s_full[F::kS], p_full[F::kS], pair_full[4], pv_done, ml_full, o_full, o_empty, mma_done;
   uint64_t item_full[kItemSlots], item_empty[kItemSlots];
   Item item[kItemSlots];
   NextItem next;
@@ -120,7 +128,7 @@ UT_DEV void empty_rows(const XattnParams& p, int hk, int tok0, int ntok, int spl
 }
 
 template <int D>
-__global__ void __launch_bounds__(kThreads, Form<D>::kCtas)
+__global__ void __launch_bounds__(Form<D>::kThreads, Form<D>::kCtas)
     wattn_fwd_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k,
                         const __grid_constant__ CUtensorMap tm_v, const __grid_constant__ Params prm) {
   extern __shared__ __align__(1024) uint8_t smem_raw[];
@@ -137,7 +145,7 @@ __global__ void __launch_bounds__(kThreads, Form<D>::kCtas)
   if (threadIdx.x == 0) {
     for (int s = 0; s < F::kQ; ++s) {
       mbar_init(&sm.q_full[s], 1);
-      mbar_init(&sm.q_empty[s], F::kQt ? 4 : 1);  // the softmax warps have copied it / S is done
+      mbar_init(&sm.q_empty[s], F::kQt ? 4 : 1);  // the output warps have copied it / S is done
     }
     for (int s = 0; s < F::kK; ++s) {
       mbar_init(&sm.k_full[s], 1);
@@ -152,15 +160,17 @@ __global__ void __launch_bounds__(kThreads, Form<D>::kCtas)
     mbar_init(&sm.qt_empty, 1);
     for (int s = 0; s < F::kS; ++s) {
       mbar_init(&sm.s_full[s], 1);
-      mbar_init(&sm.s_empty[s], 4);
+      mbar_init(&sm.p_full[s], F::kSoftmax);
     }
-    mbar_init(&sm.p_full, 4);
+    for (int s = 0; s < 4; ++s) mbar_init(&sm.pair_full[s], 2);
     mbar_init(&sm.pv_done, 1);
+    mbar_init(&sm.ml_full, F::kSoftmax);
+    mbar_init(&sm.o_full, 1);
     mbar_init(&sm.o_empty, 4);
     mbar_init(&sm.mma_done, 1);
     for (int s = 0; s < kItemSlots; ++s) {
       mbar_init(&sm.item_full[s], 1);
-      mbar_init(&sm.item_empty[s], 7);  // warps 0, 1, 3 and the softmax warps
+      mbar_init(&sm.item_empty[s], 7 + F::kSoftmax);  // warps 0, 1, 3, 4, ...
     }
     next_item_init(sm.next);
     sm.abort_flag = 0;
@@ -199,6 +209,10 @@ __global__ void __launch_bounds__(kThreads, Form<D>::kCtas)
   // Block t of an item holds the keys x .. x + 127 of the segment, those below e.
   auto block_of = [&](const Item& it, int t, int& x, int& e) { win_block<kN>(it.rg, it.j0 + t, x, e); };
   auto all_keys = [&](int x, int e) { return !p.mask && e - x >= kN; };
+
+  // For the warps that read TMEM: thread = row = TMEM lane
+  const uint32_t quarter = warp & 3, lane_base = tmem + ((quarter * 32) << 16), row = quarter * 32 + lane;
+  auto token_of = [&](uint32_t r) -> int { return (int)((r * prm.inv_g) >> 16); };  // r / G
 
   if (warp < 4) {
     if constexpr (F::kCtas == 2) setmaxnreg_dec<F::kRegCtl>();
@@ -323,7 +337,10 @@ __global__ void __launch_bounds__(kThreads, Form<D>::kCtas)
           if (!(ok = wait(&sm.v_full[st], (at / F::kV) & 1))) break;
           if (!all_keys(x, e)) {
 #pragma unroll
-            for (int g = 0; g < 4; ++g) sm.bias[st][g * 32 + lane] = (keys >> g) & 1u ? INFINITY : -INFINITY;
+            for (int g = 0; g < 4; ++g) {
+              const uint32_t word = __ballot_sync(0xffffffffu, (keys >> g) & 1u);
+              if (lane == 0) sm.keys[st][g] = word;
+            }
             if (!__all_sync(0xffffffffu, keys == 15u)) {
               const uint32_t base = smem_u32(sm.v[st]);
 #pragma unroll
@@ -341,40 +358,41 @@ __global__ void __launch_bounds__(kThreads, Form<D>::kCtas)
     } else {
       // -------------------------------------------------------------- MMA issuer
       // Converged, and uniform to the compiler: every branch depends on votes and
-      // on values made uniform.  Step i issues S of block i and P V of block i -
-      // kS; at an item's first block P V comes first, as Q arrives in TMEM late.
+      // on values made uniform.  Step i issues P V of block i - kS, then S of block
+      // i, over whose columns that P lay: the products run in this order.
       constexpr uint32_t idesc_s = idesc_bf16_f32(kM, kN, false, false);
       constexpr uint32_t idesc_o = idesc_bf16_f32(kM, D, false, true);
-      constexpr uint32_t kStep = S::kTile >> 4, kFirst = 2;
+      constexpr uint32_t kStep = S::kTile >> 4, kFirst = 2, kLast = 4;
       const uint32_t q_lo = desc_lo(smem_u32(sm.q[0]), 16), k_lo = desc_lo(smem_u32(sm.k[0]), 16),
                      v_lo = desc_lo(smem_u32(sm.v[0]), kChunkBytes);
       auto waitq = [&](uint64_t* bar, uint32_t parity) -> bool {
         return quick_wait(bar, parity, abort_flag, p.status, p.timeout_ns);
       };
-      uint32_t n = 0, left = 0, nq = 0;      // items taken, blocks left of S's, Q tiles
-      uint32_t ks = 0, kf = 0, vs = 0, vf = 0, sb = 0, sf = 1, pf = 0, of = 1;  // stages and phases
-      uint32_t f0 = 0, f1 = 0;               // flags of the blocks of P V; 0: none
+      uint32_t n = 0, left = 0, qs = F::kQ - 1, qf = 1;           // items taken, blocks left of S's, Q stage
+      uint32_t ks = 0, kf = 0, vs = 0, vf = 0, sb = 0, pf = 0, of = 1;  // stages and phases
+      uint32_t f0 = 0, f1 = 0;                                    // flags of the blocks of P V; 0: none
       bool ok = true, end = false;
-      auto pv = [&](uint32_t f) -> bool {
-        if (!waitq(&sm.v_ready[vs], vf)) return false;
-        if (f & kFirst) {
-          if (!waitq(&sm.o_empty, of)) return false;
-          of ^= 1;
-        }
-        if (!waitq(&sm.p_full, pf)) return false;
-        tc_fence_after();
-        mma_tn<128>(tmem + F::kO, tmem + F::kP, v_lo + vs * kStep, idesc_o, (f & kFirst) ^ kFirst);
-        mma_commit_w(&sm.pv_done);
-        mma_commit_w(&sm.v_empty[vs]);
-        pf ^= 1;
-        if (++vs == F::kV) {
-          vs = 0;
-          vf ^= 1;
-        }
-        return true;
-      };
 #pragma unroll 1
       do {
+        const uint32_t f = F::kS == 2 ? f0 : f1;
+        if (f) {
+          if (!(ok = waitq(&sm.v_ready[vs], vf))) break;
+          if (f & kFirst) {
+            if (!(ok = waitq(&sm.o_empty, of))) break;
+            of ^= 1;
+          }
+          if (!(ok = waitq(&sm.p_full[sb], pf))) break;
+          tc_fence_after();
+          mma_tnh(tmem + F::kO, tmem + sb * kN, v_lo + vs * kStep, idesc_o, (f & kFirst) ^ kFirst);
+          mma_commit_w(&sm.pv_done);
+          mma_commit_w(&sm.v_empty[vs]);
+          if (f & kLast) mma_commit_w(&sm.o_full);
+          if (++vs == F::kV) {
+            vs = 0;
+            vf ^= 1;
+          }
+          if (sb == F::kS - 1) pf ^= 1;
+        }
         uint32_t fn = 0;
         if (left == 0 && !end) {
           const uint32_t s = n % kItemSlots;
@@ -384,124 +402,196 @@ __global__ void __launch_bounds__(kThreads, Form<D>::kCtas)
           __syncwarp();
           if (lane == 0) mbar_arrive(&sm.item_empty[s]);
           ++n;
-          if (!end) fn = kFirst;
-        }
-        const bool early = F::kQt && (fn & kFirst);  // P V first
-        if (early && f0 && !(ok = pv(f0))) break;
-        if (left > 0) {
-          fn |= 1u;
-          --left;
-          if (fn & kFirst) {
-            if (!(ok = F::kQt ? waitq(&sm.qt_full, nq & 1) : waitq(&sm.q_full[nq % F::kQ], (nq / F::kQ) & 1))) break;
-            ++nq;
+          if (!end) {
+            fn = kFirst;
+            if (++qs == F::kQ) {
+              qs = 0;
+              qf ^= 1;
+            }
+            if (!(ok = waitq(F::kQt ? &sm.qt_full : &sm.q_full[qs], qf))) break;
           }
+        }
+        if (left > 0) {
+          --left;
+          fn |= left == 0 ? 1u | kLast : 1u;
           if (!(ok = waitq(&sm.k_full[ks], kf))) break;
-          if (!(ok = waitq(&sm.s_empty[sb], sf))) break;
           tc_fence_after();
           if constexpr (F::kQt)
             mma_tk128(tmem + sb * kN, tmem + F::kQc, k_lo + ks * kStep, idesc_s);
           else
-            mma_nt<D>(tmem + sb * kN, q_lo + ((nq - 1) % F::kQ) * kStep, k_lo + ks * kStep, idesc_s);
+            mma_nt<D>(tmem + sb * kN, q_lo + qs * kStep, k_lo + ks * kStep, idesc_s);
           mma_commit_w(&sm.s_full[sb]);
           mma_commit_w(&sm.k_empty[ks]);
-          if (left == 0) mma_commit_w(F::kQt ? &sm.qt_empty : &sm.q_empty[(nq - 1) % F::kQ]);
+          if (left == 0) mma_commit_w(F::kQt ? &sm.qt_empty : &sm.q_empty[qs]);
           if (++ks == F::kK) {
             ks = 0;
             kf ^= 1;
           }
-          if (++sb == F::kS) {
-            sb = 0;
-            sf ^= 1;
-          }
         }
-        const uint32_t f = F::kS == 2 ? f0 : f1;
-        if (!early && f && !(ok = pv(f))) break;
+        if (F::kS == 2) sb ^= 1;
         f0 = f1;
         f1 = fn;
       } while (f0 | f1);
       mma_commit_w(&sm.mma_done);  // every MMA has completed before TMEM is freed
       drain(&sm.mma_done, 0);
     }
-  } else {
+  } else if (warp < 4 + F::kSoftmax) {
     // ------------------------------------------------------------------- softmax
     if constexpr (F::kCtas == 2) setmaxnreg_inc<F::kRegSoftmax>();
-    const uint32_t quarter = warp & 3, lane_base = tmem + ((quarter * 32) << 16), row = quarter * 32 + lane;
-    auto token_of = [&](uint32_t r) -> int { return (int)((r * prm.inv_g) >> 16); };  // r / G
-    const int rt = token_of(row), rt_first = token_of(quarter * 32), rt_last = token_of(quarter * 32 + 31);
+    constexpr int kCols = kN / F::kHalves, kC = F::kCtas == 2 ? 32 : 64;  // of a warp, of a step
+    constexpr bool kReload = kC < kCols;
+    const uint32_t half = F::kHalves == 2 ? (warp - 4) >> 2 : 0;
+    const int rt = token_of(row), rt_first = token_of(quarter * 32), span = token_of(quarter * 32 + 31) - rt_first;
     const uint64_t c2 = pack_f32x2(prm.scale_log2, prm.scale_log2);
-    uint32_t n = 0, nq = 0, b = 0, vst = 0, vf = 0;  // items, Q tiles copied, blocks; V stage and phase
-    bool ok = true, pend = false;
-    Item it{}, nx{};
-    float m = -1e30f, l = 0.f;
-    // what the pending item's rows need
-    int e_hk = 0, e_tok0 = 0, e_ntok = 0, e_split = 0;
-    float e_m = 0.f, e_l = 0.f;
-
-    // O / l in bf16 and LSE, or the partial result
-    auto write_rows = [&](int hk, int tok0, int ntok, int split, float em, float el) {
-      const int h = hk * p.G + (int)(row - rt * p.G);
-      const bool row_ok = rt < ntok;
-      if (p.nsplit > 1) {
-        const int64_t prow = ((int64_t)split * p.nq + tok0 + rt) * p.H + h;
+    uint32_t n = 0, b = 0, vst = 0, vf = 0;  // items, blocks; V stage and phase
+    bool ok = true;
+    Item it;
+    while (ok && next_item(n, it, ok)) {
+      const int right = it.p0 + rt + prm.w.right, left = it.p0 + rt - prm.w.left;  // last and first key of this row's
+      const int right0 = right + rt_first - rt, left0 = left + rt_first - rt;      // and of the warp's first
+      float m = -1e30f, l = 0.f;
 #pragma unroll 1
-        for (int g = 0; g < D / 32; ++g) {
-          uint32_t r[32];
-          tmem_ld32(lane_base + F::kO + g * 32, r);
-          tmem_wait_ld();
-          if (!row_ok) continue;
+      for (int t = 0; t < it.blocks; ++t, ++b) {
+        int x, e;
+        block_of(it, t, x, e);
+        x += (int)half * kCols;  // of this warp's first column
+        const uint32_t sb = b % F::kS, ts = lane_base + sb * kN + half * kCols;
+        const bool whole = !p.mask && e - x >= kCols;  // every key of this warp's counts
+        if (!(ok = wait(&sm.s_full[sb], (b / F::kS) & 1))) break;
+        if (!whole && !(ok = wait(&sm.v_ready[vst], vf))) break;
+        tc_fence_after();
+        const bool limits = right0 - x < kCols - 1 || (left0 + span > x && x + kCols > prm.w.sinks);
+        // ---- pass 1
+        float m4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+        uint32_t r[kC];
+        auto load = [&](int g) {
 #pragma unroll
-          for (int x = 0; x < 32; x += 4)
-            *reinterpret_cast<uint4*>(p.part_o + prow * D + g * 32 + x) = make_uint4(r[x], r[x + 1], r[x + 2], r[x + 3]);
+          for (int y = 0; y < kC; y += 32) tmem_ld32(ts + g + y, *reinterpret_cast<uint32_t(*)[32]>(&r[y]));
+        };
+#pragma unroll 1
+        for (int g = 0; g < kCols; g += kC) {
+          load(g);
+          tmem_wait_ld();
+          if (!whole || limits) {
+            // a bit for each column this row sees: lo .. hi and those below sink
+            uint32_t on[kC / 32], some = ~0u;
+#pragma unroll
+            for (int w = 0; w < kC / 32; ++w) {
+              const int first = g + 32 * w, hi = right - x - first, lo = left - x - first, sink = prm.w.sinks - x - first;
+              on[w] = whole ? ~0u : sm.keys[vst][half * (kCols / 32) + first / 32];
+              on[w] &= hi >= 31 ? ~0u : (hi < 0 ? 0u : (2u << hi) - 1);
+              on[w] &= (lo <= 0 ? ~0u : (lo > 31 ? 0u : ~0u << lo)) | (sink >= 32 ? ~0u : (sink <= 0 ? 0u : (1u << sink) - 1));
+              some &= on[w];
+            }
+            if (__any_sync(0xffffffffu, some != ~0u)) {
+#pragma unroll
+              for (int y = 0; y < kC; ++y)
+                if (!((on[y / 32] >> (y & 31)) & 1u)) r[y] = 0xff800000u;
+              if (kReload) {
+#pragma unroll
+                for (int y = 0; y < kC; y += 32) tmem_st32(ts + g + y, *reinterpret_cast<uint32_t(*)[32]>(&r[y]));
+              }
+            }
+          }
+#pragma unroll
+          for (int y = 0; y < kC; y += 8)
+#pragma unroll
+            for (int z = 0; z < 4; ++z) m4[z] = max3(m4[z], __uint_as_float(r[y + z]), __uint_as_float(r[y + z + 4]));
         }
-        if (row_ok) p.part_ml[prow] = make_float2(em, el);
+        if (kReload && (!whole || limits)) tmem_wait_st();
+        if (++vst == F::kV) {
+          vst = 0;
+          vf ^= 1;
+        }
+        float mx = fmaxf(max3(m4[0], m4[1], m4[2]), m4[3]) * prm.scale_log2;
+        if constexpr (F::kHalves == 2) {
+          sm.most[b & 1][half][row] = mx;  // both halves take the same reference
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&sm.pair_full[quarter]);
+          if (!(ok = wait(&sm.pair_full[quarter], b & 1))) break;
+          mx = fmaxf(mx, sm.most[b & 1][half ^ 1][row]);
+        }
+        mx = fmaxf(mx, -1e30f);  // finite where a row sees no key of the block
+        if (t == 0) {
+          m = mx;
+        } else {
+          const bool need = mx > m + 8.0f;
+          if (__any_sync(0xffffffffu, need)) {  // the same rows in both halves
+            const float alpha = need ? ex2_approx(m - mx) : 1.0f;
+            if (need) m = mx;
+            l *= alpha;
+            if (!(ok = wait(&sm.pv_done, (b & 1) ^ 1))) break;  // O holds P V up to the block before
+            tc_fence_after();
+            const uint32_t to = lane_base + F::kO + half * (D / F::kHalves);
+#pragma unroll 1
+            for (int g = 0; g < D / F::kHalves; g += 16) {
+              uint32_t o[16];
+              tmem_ld16(to + g, o);
+              tmem_wait_ld();
+#pragma unroll
+              for (int y = 0; y < 16; ++y) o[y] = __float_as_uint(__uint_as_float(o[y]) * alpha);
+              tmem_st16(to + g, o);
+            }
+          }
+        }
+        // ---- pass 2: loads run beside the exponentials of the columns before
+        const uint64_t m2 = pack_f32x2(-m, -m);
+        uint64_t sum[4] = {0, 0, 0, 0};
+        if (kReload) load(0);
+#pragma unroll 1
+        for (int g = 0; g < kCols; g += kC) {
+          if (kReload) tmem_wait_ld();
+          float a[kC];
+#pragma unroll
+          for (int y = 0; y < kC; y += 2) unpack_f32x2(fma_f32x2(pack_u32x2(r[y], r[y + 1]), c2, m2), a[y], a[y + 1]);
+          if (kReload && g + kC < kCols) load(g + kC);
+          uint32_t pk[kC / 2];
+#pragma unroll
+          for (int y = 0; y < kC; y += 2) {
+            a[y] = ex2_approx(a[y]);
+            a[y + 1] = ex2_approx(a[y + 1]);
+            sum[(y >> 1) & 3] = add_f32x2(sum[(y >> 1) & 3], pack_f32x2(a[y], a[y + 1]));
+            pk[y / 2] = pack_bf16x2(a[y], a[y + 1]);
+          }
+          if constexpr (kC == 64)
+            tmem_st32(ts + g, pk);
+          else
+            tmem_st16(ts + (g >> 6) * 64 + ((g >> 5) & 1) * 16, pk);
+        }
+        float a0, a1;
+        unpack_f32x2(add_f32x2(add_f32x2(sum[0], sum[1]), add_f32x2(sum[2], sum[3])), a0, a1);
+        l += a0 + a1;
+        tmem_wait_st();
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) mbar_arrive(&sm.o_empty);
-        return;
+        if (lane == 0) mbar_arrive(&sm.p_full[sb]);
       }
-      if (row_ok) p.lse[(int64_t)h * p.nq + tok0 + rt] = el == 0.f ? -INFINITY : (em + log2f(el)) * kLn2;
-      // A thread holds a row; the four lanes of a quad exchange 16-byte units so
-      // that lane c holds unit c of each of the quad's rows, and a store covers 64
-      // contiguous bytes of eight rows instead of 16 of 32.
-      const float f = el > 0.f ? 1.f / el : (el == 0.f ? 0.f : el);
-      const uint32_t c = lane & 3;
-      __nv_bfloat16* out[4];
-      __nv_bfloat16* const base = static_cast<__nv_bfloat16*>(p.o) + (int64_t)tok0 * p.os + (int64_t)hk * p.G * D + c * 8;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const uint32_t y = quarter * 32 + (lane & ~3u) + i;
-        const int yt = token_of(y);
-        out[i] = yt < ntok ? base + (int64_t)yt * p.os + (y - yt * p.G) * D : nullptr;
-      }
-#pragma unroll 1
-      for (int g = 0; g < D / 32; ++g) {
-        uint32_t r[32], u[4][4];
-        tmem_ld32(lane_base + F::kO + g * 32, r);
-        tmem_wait_ld();
-        if (g == D / 32 - 1) {
-          tc_fence_before();
-          __syncwarp();
-          if (lane == 0) mbar_arrive(&sm.o_empty);
-        }
-#pragma unroll
-        for (int x = 0; x < 16; ++x)
-          u[x >> 2][x & 3] = pack_bf16x2(__uint_as_float(r[2 * x]) * f, __uint_as_float(r[2 * x + 1]) * f);
-        exchange_units<1>(u, c & 1, 0, 1);
-        exchange_units<1>(u, c & 1, 2, 3);
-        exchange_units<2>(u, c >> 1, 0, 2);
-        exchange_units<2>(u, c >> 1, 1, 3);
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-          if (out[i]) *reinterpret_cast<uint4*>(out[i] + g * 32) = make_uint4(u[i][0], u[i][1], u[i][2], u[i][3]);
-      }
-    };
-    // nx's Q tile: shared memory (128B-swizzled, as TMA wrote it) -> TMEM, this
-    // thread's row, bf16 pairs: the A operand of S = Q K^T
-    auto load_q = [&]() -> bool {
-      if (!wait(&sm.q_full[0], nq & 1)) return false;
-      if (!wait(&sm.qt_empty, (nq & 1) ^ 1)) return false;
+      if (!ok) break;
+      // the rows' maximum and sum for the output warps, which have read the last ones
+      if (!(ok = wait(&sm.o_empty, n & 1))) break;
       tc_fence_after();
-#pragma unroll
+      if (half == 0) tmem_st1(lane_base + F::kMl, __float_as_uint(m));
+      tmem_st1(lane_base + F::kMl + 1 + half, __float_as_uint(l));
+      tmem_wait_st();
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&sm.ml_full);
+    }
+  } else {
+    // ------------------------------------------------------------- Q in, O out
+    if constexpr (F::kCtas == 2) setmaxnreg_dec<F::kRegOut>();
+    const int rt = token_of(row);
+    const uint32_t c = lane & 3;
+    uint32_t n = 0, done = 0;
+    bool ok = true;
+    // Q of item i: shared memory (128B-swizzled, as TMA wrote it) -> TMEM, this
+    // thread's row, bf16 pairs: the A operand of S = Q K^T
+    auto load_q = [&](uint32_t i) -> bool {
+      if constexpr (!F::kQt) return true;
+      if (!wait(&sm.q_full[0], i & 1)) return false;
+      if (!wait(&sm.qt_empty, (i & 1) ^ 1)) return false;
+      tc_fence_after();
+#pragma unroll 1
       for (int cc = 0; cc < S::kChunks; ++cc) {
         uint32_t qv[32];
         const uint32_t base = smem_u32(sm.q[0]) + cc * kChunkBytes + row * 128;
@@ -519,154 +609,86 @@ __global__ void __launch_bounds__(kThreads, Form<D>::kCtas)
         mbar_arrive(&sm.qt_full);
         mbar_arrive(&sm.q_empty[0]);
       }
-      ++nq;
       return true;
     };
-
-    bool more = next_item(n, nx, ok), first = true;
-    if (F::kQt && more) ok = load_q();
-    int t = 0, pos = 0;
-    // A block a round; the last round only writes the last item's rows.
+    Item it, nx;
+    bool more = next_item(n, nx, ok);
+    if (more) ok = load_q(0);
+    while (ok && more) {
+      it = nx;
+      more = next_item(n, nx, ok);
+      if (!ok || (more && !(ok = load_q(n - 1)))) break;  // the next one's, once this one's last S is done
+      if (!(ok = wait(&sm.ml_full, done & 1))) break;
+      if (!(ok = wait(&sm.o_full, done & 1))) break;
+      ++done;
+      tc_fence_after();
+      const int64_t tok0 = it.tok0;
+      const int h = it.hk * p.G + (int)row - rt * p.G;
+      const bool row_ok = rt < it.ntok;
+      float m, l, l1 = 0.f;
+      m = __uint_as_float(tmem_ld1(lane_base + F::kMl));
+      l = __uint_as_float(tmem_ld1(lane_base + F::kMl + 1));
+      if (F::kHalves == 2) l1 = __uint_as_float(tmem_ld1(lane_base + F::kMl + 2));
+      tmem_wait_ld();
+      l += l1;
+      if (p.nsplit > 1) {
+        const int64_t prow = ((int64_t)it.split * p.nq + tok0 + rt) * p.H + h;
 #pragma unroll 1
-    while (ok && (more || pend)) {
-      bool last = false;
-      if (more) {
-        if (first) {
-          it = nx;
-          pos = it.p0 + rt;  // of this row's token
-          t = 0;
-        }
-        int x, e;
-        block_of(it, t, x, e);
-        const uint32_t sb = b % F::kS, ts = lane_base + sb * kN;
-        const bool whole = all_keys(x, e);
-        last = t == it.blocks - 1;
-        if (!(ok = wait(&sm.s_full[sb], (b / F::kS) & 1))) break;
-        if (!whole && !(ok = wait(&sm.v_ready[vst], vf))) break;
-        tc_fence_after();
-        // The rows' own limits, where some row of the warp has one in this block:
-        // S there becomes -inf in TMEM, 32 columns at a time.  (In the code below,
-        // unrolled over 128 columns, they cost every block 1,500 cycles: the code
-        // no longer fits the instruction cache.)
-        const bool lim_r = it.p0 + rt_first + prm.w.right - x < kN - 1,
-                   lim_l = it.p0 + rt_last - prm.w.left > x && x + kN > prm.w.sinks;
-        if (lim_r || lim_l) {
-          const int hi = pos + prm.w.right - x, lo = pos - prm.w.left - x, sink = prm.w.sinks - x;
-#pragma unroll 1
-          for (int g = 0; g < kN; g += 32) {
-            const bool cut = (g + 31 > it.p0 + rt_first + prm.w.right - x) ||
-                             (g < it.p0 + rt_last - prm.w.left - x && g + 31 >= sink);
-            if (!cut) continue;
-            uint32_t r[32];
-            tmem_ld32(ts + g, r);
-            tmem_wait_ld();
+        for (int g = 0; g < D / 32; ++g) {
+          uint32_t r[32];
+          tmem_ld32(lane_base + F::kO + g * 32, r);
+          tmem_wait_ld();
+          if (row_ok) {
 #pragma unroll
-            for (int y = 0; y < 32; ++y)
-              if (y > hi - g || (y < lo - g && y >= sink - g)) r[y] = 0xff800000u;
-            tmem_st32(ts + g, r);
+            for (int x = 0; x < 32; x += 4)
+              *reinterpret_cast<uint4*>(p.part_o + prow * D + g * 32 + x) = make_uint4(r[x], r[x + 1], r[x + 2], r[x + 3]);
           }
-          tmem_wait_st();
+          __syncwarp();
         }
-        uint32_t r[kN];
-#pragma unroll
-        for (int g = 0; g < 4; ++g) tmem_ld32(ts + g * 32, *reinterpret_cast<uint32_t(*)[32]>(&r[g * 32]));
-        tmem_wait_ld();
+        if (row_ok) p.part_ml[prow] = make_float2(m, l);
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) mbar_arrive(&sm.s_empty[sb]);
-        if (last) {  // the next item's Q: its first S is computed while this block is in the softmax
-          more = next_item(n, nx, ok);
-          if (F::kQt && more) ok = load_q();
-          if (!ok) break;
-        }
-        if (!whole) {
-          asm volatile("" ::: "memory");  // a branch, not a choice between 128 values
-#pragma unroll
-          for (int y = 0; y < kN; y += 4) {
-            const float4 v = *reinterpret_cast<const float4*>(sm.bias[vst] + y);
-            r[y] = __float_as_uint(fminf(__uint_as_float(r[y]), v.x));
-            r[y + 1] = __float_as_uint(fminf(__uint_as_float(r[y + 1]), v.y));
-            r[y + 2] = __float_as_uint(fminf(__uint_as_float(r[y + 2]), v.z));
-            r[y + 3] = __float_as_uint(fminf(__uint_as_float(r[y + 3]), v.w));
-          }
-        }
-        if (++vst == F::kV) {
-          vst = 0;
-          vf ^= 1;
-        }
-        float m8[8];
-#pragma unroll
-        for (int y = 0; y < 8; ++y) m8[y] = fmaxf(__uint_as_float(r[y]), __uint_as_float(r[y + 8]));
-#pragma unroll
-        for (int y = 16; y < kN; y += 16)
-#pragma unroll
-          for (int z = 0; z < 8; ++z) m8[z] = max3(m8[z], __uint_as_float(r[y + z]), __uint_as_float(r[y + z + 8]));
-        float mx = max3(max3(m8[0], m8[1], m8[2]), max3(m8[3], m8[4], m8[5]), fmaxf(m8[6], m8[7]));
-        mx = fmaxf(mx * prm.scale_log2, -1e30f);  // finite where a row sees no key of the block
-        const bool need = !first && mx > m + 8.0f;
-        const bool any = __any_sync(0xffffffffu, need);
-        float alpha = 1.f;
-        if (first) {
-          m = mx;
-          l = 0.f;
-        } else if (need) {
-          alpha = ex2_approx(m - mx);
-          m = mx;
-          l *= alpha;
-        }
-        const uint64_t m2 = pack_f32x2(-m, -m);
-        uint64_t sum[4] = {0, 0, 0, 0};
-        uint32_t pk[kN / 2];
-#pragma unroll
-        for (int y = 0; y < kN; y += 2) {
-          float p0, p1;
-          unpack_f32x2(fma_f32x2(pack_u32x2(r[y], r[y + 1]), c2, m2), p0, p1);
-          p0 = ex2_approx(p0);
-          p1 = ex2_approx(p1);
-          sum[(y >> 1) & 3] = add_f32x2(sum[(y >> 1) & 3], pack_f32x2(p0, p1));
-          pk[y / 2] = pack_bf16x2(p0, p1);
-        }
-        float a0, a1;
-        unpack_f32x2(add_f32x2(add_f32x2(sum[0], sum[1]), add_f32x2(sum[2], sum[3])), a0, a1);
-        l += a0 + a1;
-        // P's columns are free, and O holds P V up to the block before, once its
-        // product is done
-        if (!(ok = wait(&sm.pv_done, (b & 1) ^ 1))) break;
-        tc_fence_after();
-        if (any) {
-#pragma unroll 1
-          for (int g = 0; g < D / 16; ++g) {
-            uint32_t o[16];
-            tmem_ld16(lane_base + F::kO + g * 16, o);
-            tmem_wait_ld();
-#pragma unroll
-            for (int y = 0; y < 16; ++y) o[y] = __float_as_uint(__uint_as_float(o[y]) * alpha);
-            tmem_st16(lane_base + F::kO + g * 16, o);
-          }
-        }
-        tmem_st32(lane_base + F::kP, *reinterpret_cast<uint32_t(*)[32]>(&pk[0]));
-        tmem_st32(lane_base + F::kP + 32, *reinterpret_cast<uint32_t(*)[32]>(&pk[32]));
-        tmem_wait_st();
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(&sm.p_full);
-        ++b;
-        ++t;
-      } else {
-        if (!(ok = wait(&sm.pv_done, (b & 1) ^ 1))) break;
-        tc_fence_after();
+        if (lane == 0) mbar_arrive(&sm.o_empty);
+        continue;
       }
-      if (first && pend) write_rows(e_hk, e_tok0, e_ntok, e_split, e_m, e_l);
-      if (first) pend = false;
-      first = last;
-      if (last) {
-        pend = true;
-        e_hk = it.hk;
-        e_tok0 = it.tok0;
-        e_ntok = it.ntok;
-        e_split = it.split;
-        e_m = m;
-        e_l = l;
+      // A thread holds a row; the four lanes of a quad exchange 16-byte units so
+      // that lane c holds unit c of each of the quad's rows, and a store covers 64
+      // contiguous bytes of eight rows instead of 16 of 32.
+      const float f = l > 0.f ? 1.f / l : (l == 0.f ? 0.f : l);
+      uint32_t o[D / 2];
+#pragma unroll
+      for (int g = 0; g < D / 32; ++g) {  // all of O first: the next item's first P V waits for it
+        uint32_t r[32];
+        tmem_ld32(lane_base + F::kO + g * 32, r);
+        tmem_wait_ld();
+#pragma unroll
+        for (int x = 0; x < 16; ++x)
+          o[g * 16 + x] = pack_bf16x2(__uint_as_float(r[2 * x]) * f, __uint_as_float(r[2 * x + 1]) * f);
+      }
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&sm.o_empty);
+      if (row_ok) p.lse[(int64_t)h * p.nq + tok0 + rt] = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
+      __nv_bfloat16* out[4];
+      __nv_bfloat16* const base = static_cast<__nv_bfloat16*>(p.o) + tok0 * p.os + (int64_t)it.hk * p.G * D + c * 8;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const uint32_t y = quarter * 32 + (lane & ~3u) + i;
+        const int yt = token_of(y);
+        out[i] = yt < it.ntok ? base + (int64_t)yt * p.os + (y - yt * p.G) * D : nullptr;
+      }
+#pragma unroll
+      for (int g = 0; g < D / 32; ++g) {
+        uint32_t u[4][4];
+#pragma unroll
+        for (int x = 0; x < 16; ++x) u[x >> 2][x & 3] = o[g * 16 + x];
+        exchange_units<1>(u, c & 1, 0, 1);
+        exchange_units<1>(u, c & 1, 2, 3);
+        exchange_units<2>(u, c >> 1, 0, 2);
+        exchange_units<2>(u, c >> 1, 1, 3);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (out[i]) *reinterpret_cast<uint4*>(out[i] + g * 32) = make_uint4(u[i][0], u[i][1], u[i][2], u[i][3]);
       }
     }
   }
@@ -691,7 +713,7 @@ cudaError_t launch_d(const Params& prm, const CUtensorMap* tm, cudaStream_t s) {
     if (e != cudaSuccess) return e;
     if (fa.numRegs != Form<D>::kRegLaunch) return cudaErrorInvalidConfiguration;
   }
-  wattn_fwd_tc_kernel<D><<<(unsigned)prm.n_items, kThreads, smem, s>>>(tm[0], tm[1], tm[2], prm);
+  wattn_fwd_tc_kernel<D><<<(unsigned)prm.n_items, Form<D>::kThreads, smem, s>>>(tm[0], tm[1], tm[2], prm);
   return cudaGetLastError();
 }
 
