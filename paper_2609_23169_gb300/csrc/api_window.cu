@@ -82,9 +82,10 @@ static ut_status window_problem(const ut_xattn_shape* s, const ut_window* win, b
   w->right = win->right < kWinMost ? win->right : kWinMost;
   w->sinks = win->sinks < kWinMost ? win->sinks : kWinMost;
   if (s->n_q > kWinMost || s->n_k > kWinMost) return UT_ERR_UNSUPPORTED;
-  const bool tc = s->dtype == UT_BF16 && !backward;
-  if ((tc ? wattn_fwd_tc_items(*w) : wattn_simt_items(*w, backward)) > INT32_MAX / 2) return UT_ERR_UNSUPPORTED;
-  w->x.nsplit = tc ? wattn_fwd_tc_splits(*w) : wattn_simt_splits(*w, backward);
+  const bool tc = s->dtype == UT_BF16;
+  const int64_t items = !tc ? wattn_simt_items(*w, backward) : (backward ? wattn_bwd_tc_items(*w) : wattn_fwd_tc_items(*w));
+  if (items > INT32_MAX / 2) return UT_ERR_UNSUPPORTED;
+  w->x.nsplit = !tc ? wattn_simt_splits(*w, backward) : (backward ? 1 : wattn_fwd_tc_splits(*w));
   return UT_OK;
 }
 
@@ -95,8 +96,10 @@ static size_t window_fwd_ws(const XattnParams& p) {
 }
 
 // D, then partial dK and dV
-static size_t window_bwd_ws(const XattnParams& p) {
-  return up256((size_t)p.H * p.nq * sizeof(float)) + 2 * up256((size_t)p.nsplit * p.nk * p.Hk * p.d * sizeof(float));
+static size_t window_bwd_ws(const WinParams& w, bool bf16) {
+  const XattnParams& p = w.x;
+  return up256((size_t)p.H * p.nq * sizeof(float)) +
+         (bf16 ? wattn_bwd_tc_ws(w) : 2 * up256((size_t)p.nsplit * p.nk * p.Hk * p.d * sizeof(float)));
 }
 
 }  // namespace ut
@@ -208,7 +211,7 @@ ut_status ut_window_attn_fwd(const ut_xattn_shape* shape, const ut_window* windo
 
 size_t ut_window_attn_bwd_workspace_size(const ut_xattn_shape* shape, const ut_window* window) {
   WinParams w;
-  return window_problem(shape, window, true, &w) == UT_OK ? window_bwd_ws(w.x) : 0;
+  return window_problem(shape, window, true, &w) == UT_OK ? window_bwd_ws(w, shape->dtype == UT_BF16) : 0;
 }
 
 ut_status ut_window_attn_bwd(const ut_xattn_shape* shape, const ut_window* window, const void* q, const void* k,
@@ -241,14 +244,17 @@ ut_status ut_window_attn_bwd(const ut_xattn_shape* shape, const ut_window* windo
   if ((p.nq > 0 && (!dout || !dq)) || (p.nk > 0 && (!dk || !dv))) return UT_ERR_INVALID_ARG;
   if (!at16(dout) || !at16(dq) || !at16(dk) || !at16(dv) || !at4(k_len)) return UT_ERR_INVALID_ARG;
   if (p.nq == 0 && p.nk == 0) return UT_OK;
-  const size_t need = window_bwd_ws(p);
-  if (!ws || ws_bytes < need || !at16(ws)) return UT_ERR_INVALID_ARG;
+  const bool bf16 = shape->dtype == UT_BF16;
+  const size_t need = window_bwd_ws(w, bf16);
+  if (need > 0 && (!ws || ws_bytes < need || !at16(ws))) return UT_ERR_INVALID_ARG;
   char* at = static_cast<char*>(ws);
   p.dsum = reinterpret_cast<float*>(at);
   at += up256((size_t)p.H * p.nq * sizeof(float));
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  if (bf16) return status_of(launch_wattn_bwd_tc(w, at, s));
   p.part_dk = reinterpret_cast<float*>(at);
   p.part_dv = reinterpret_cast<float*>(at + up256((size_t)p.nsplit * p.nk * p.Hk * p.d * sizeof(float)));
-  return status_of(launch_wattn_bwd_simt(w, shape->dtype == UT_BF16, static_cast<cudaStream_t>(stream)));
+  return status_of(launch_wattn_bwd_simt(w, s));
 }
 
 }  // extern "C"

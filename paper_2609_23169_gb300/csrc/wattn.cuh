@@ -24,12 +24,16 @@ struct WinParams {
 constexpr int kWinMost = (1 << 30) - 512;
 
 // Keys of segment s: their first row and number
-__host__ __device__ __forceinline__ void win_keys(const WinParams& w, int s, int64_t& row, int64_t& n) {
-  segment_rows(w.x.cu_k, s, w.x.nk, row, n);
-  if (w.k_len) {
-    const int64_t len = w.k_len[s];
+__host__ __device__ __forceinline__ void win_keys(const int32_t* cu_k, const int32_t* k_len, int64_t nk, int s,
+                                                  int64_t& row, int64_t& n) {
+  segment_rows(cu_k, s, nk, row, n);
+  if (k_len) {
+    const int64_t len = k_len[s];
     n = len < 0 ? 0 : (len < n ? len : n);
   }
+}
+__host__ __device__ __forceinline__ void win_keys(const WinParams& w, int s, int64_t& row, int64_t& n) {
+  win_keys(w.x.cu_k, w.k_len, w.x.nk, s, row, n);
 }
 
 // The keys that the tokens at positions pa .. pb of a segment of n keys see, as
@@ -70,23 +74,31 @@ __host__ __device__ __forceinline__ void win_tokens(int x, int e, int n_k, int n
 }
 
 // Reports numbers of keys outside their segments.  Called by the threads of one block.
-__device__ __forceinline__ void check_lens_of(const WinParams& w) {
-  if (!w.k_len || !w.x.status) return;
-  for (int s = threadIdx.x; s < w.x.B; s += blockDim.x) {
+__device__ __forceinline__ void check_lens_of(const XattnParams& x, const int32_t* k_len) {
+  if (!k_len || !x.status) return;
+  for (int s = threadIdx.x; s < x.B; s += blockDim.x) {
     int64_t row, n;
-    segment_rows(w.x.cu_k, s, w.x.nk, row, n);
-    if (w.k_len[s] < 0 || w.k_len[s] > n) atomicCAS(w.x.status, 0, (int)UT_ERR_INVALID_ARG);
+    segment_rows(x.cu_k, s, x.nk, row, n);
+    if (k_len[s] < 0 || k_len[s] > n) atomicCAS(x.status, 0, (int)UT_ERR_INVALID_ARG);
   }
 }
 
-// wattn_simt.cu
+// A bit for each of 32 consecutive columns: those up to hi, those from lo on
+__device__ __forceinline__ uint32_t bits_to(int hi) { return hi >= 31 ? ~0u : (hi < 0 ? 0u : (2u << hi) - 1); }
+__device__ __forceinline__ uint32_t bits_from(int lo) { return lo <= 0 ? ~0u : (lo > 31 ? 0u : ~0u << lo); }
+
+// wattn_simt.cu (fp32)
 int64_t wattn_simt_items(const WinParams& w, bool backward);
 int wattn_simt_splits(const WinParams& w, bool backward);
-cudaError_t launch_wattn_fwd_simt(const WinParams& w, cudaStream_t s);  // fp32
-cudaError_t launch_wattn_bwd_simt(const WinParams& w, bool bf16, cudaStream_t s);
+cudaError_t launch_wattn_fwd_simt(const WinParams& w, cudaStream_t s);
+cudaError_t launch_wattn_bwd_simt(const WinParams& w, cudaStream_t s);
 // wattn_fwd_tc.cu (bf16)
 int64_t wattn_fwd_tc_items(const WinParams& w);
 int wattn_fwd_tc_splits(const WinParams& w);
 cudaError_t launch_wattn_fwd_tc(const WinParams& w, cudaStream_t s);
+// xattn_bwd_tc.cu (bf16)
+int64_t wattn_bwd_tc_items(const WinParams& w);
+size_t wattn_bwd_tc_ws(const WinParams& w);
+cudaError_t launch_wattn_bwd_tc(const WinParams& w, void* ws, cudaStream_t s);
 
 }  // namespace ut

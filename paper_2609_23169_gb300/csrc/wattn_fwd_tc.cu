@@ -183,7 +183,7 @@ __global__ void __launch_bounds__(Form<D>::kThreads, Form<D>::kCtas)
   if (blockIdx.x == 0) {
     check_cu(p.cu_q, p.B, p.nq, p.status);
     check_cu(p.cu_k, p.B, p.nk, p.status);
-    check_lens_of(prm.w);
+    check_lens_of(p, prm.w.k_len);
   }
   tc_fence_before();
   __syncthreads();

@@ -40,7 +40,7 @@ struct Limits {
 UT_DEV void check_lens(const WinParams& w) {
   check_cu(w.x.cu_q, w.x.B, w.x.nq, w.x.status);
   check_cu(w.x.cu_k, w.x.B, w.x.nk, w.x.status);
-  check_lens_of(w);
+  check_lens_of(w.x, w.k_len);
 }
 
 // grid (q slots, kv heads, key splits)
@@ -295,7 +295,7 @@ __global__ void __launch_bounds__(kXsThreads) wattn_bwd_simt_kernel(const WinPar
   extern __shared__ float sm[];
   grid_wait();
   const uint32_t x = blockIdx.x;
-  if (x == 0) check_lens_of(w);
+  if (x == 0) check_lens_of(w.x, w.k_len);
   if (x < n_kv) {
     const uint32_t y = x / kslots;
     dkdv_tile<T, D>(w, sm, x - y * kslots, (int)(y % w.x.Hk), (int)(y / w.x.Hk));
@@ -329,7 +329,7 @@ cudaError_t bwd(const WinParams& w, cudaStream_t s) {
   if (e == cudaSuccess)
     e = launch_next(wattn_bwd_simt_kernel<T, D>, dim3((unsigned)(n_kv + n_q)), dim3(kXsThreads), smem, s, w,
                     (uint32_t)n_kv, kslots, qslots);
-  if (e == cudaSuccess && p.nk > 0) e = launch_xattn_dkdv_join(p, sizeof(T) == 2, s);
+  if (e == cudaSuccess && p.nk > 0) e = launch_xattn_dkdv_join(p, s);
   return e;
 }
 
@@ -357,8 +357,7 @@ int wattn_simt_splits(const WinParams& w, bool backward) {
 cudaError_t launch_wattn_fwd_simt(const WinParams& w, cudaStream_t s) {
   return w.x.d == 64 ? fwd<float, 64>(w, s) : fwd<float, 128>(w, s);
 }
-cudaError_t launch_wattn_bwd_simt(const WinParams& w, bool bf16, cudaStream_t s) {
-  if (bf16) return w.x.d == 64 ? bwd<__nv_bfloat16, 64>(w, s) : bwd<__nv_bfloat16, 128>(w, s);
+cudaError_t launch_wattn_bwd_simt(const WinParams& w, cudaStream_t s) {
   return w.x.d == 64 ? bwd<float, 64>(w, s) : bwd<float, 128>(w, s);
 }
 

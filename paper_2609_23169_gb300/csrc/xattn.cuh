@@ -44,7 +44,7 @@ int64_t xattn_fwd_tc_items(const XattnParams& p);
 cudaError_t launch_xattn_fwd_simt(const XattnParams& p, cudaStream_t s);  // fp32
 cudaError_t launch_xattn_fwd_tc(const XattnParams& p, cudaStream_t s);    // bf16
 cudaError_t launch_xattn_join(const XattnParams& p, bool bf16, cudaStream_t s);  // of the forward's key splits
-cudaError_t launch_xattn_dkdv_join(const XattnParams& p, bool bf16, cudaStream_t s);  // of the backward's splits
+cudaError_t launch_xattn_dkdv_join(const XattnParams& p, cudaStream_t s);  // of the fp32 backward's splits
 int64_t xattn_bwd_tc_items(const XattnParams& p);
 size_t xattn_bwd_tc_ws(const XattnParams& p);
 cudaError_t launch_xattn_dsum(const XattnParams& p, bool bf16, cudaStream_t s);  // D, and the check of the prefixes

@@ -38,9 +38,13 @@
 // each, and write their bf16 pairs over the first half of their own columns.
 // Every wait is bounded; on expiry a kernel records UT_ERR_TIMEOUT, drains its
 // own copies and MMAs, frees TMEM and returns.
+#include <algorithm>
+#include <type_traits>
+
 #include "common.cuh"
 #include "kernels.h"
 #include "segments.cuh"
+#include "wattn.cuh"
 #include "xattn_tc.cuh"
 
 namespace ut {
@@ -59,6 +63,13 @@ struct BwdParams {
   int64_t n_items;  // of the launch
   float scale_log2;
   int64_t kslots;   // key blocks of all segments (with idle ones): nk / 128 + n_seg
+  // windowed attention (kWin; see wattn.cuh)
+  const int32_t* k_len;
+  int left, right, sinks;
+  int chunks;       // runs of a key block without first keys
+  int Rs, sb;       // tiles of a run and key blocks of a segment with first keys
+  int64_t n_first, qslots;  // items of those, their runs of all segments
+  bool join, join_first;    // the runs' results are partial sums
 };
 
 UT_DEV void tmem_ld64(uint32_t taddr, uint32_t* r) {
@@ -103,7 +114,7 @@ UT_DEV void zero_tail(uint32_t base, int chunks, int first, uint32_t lane) {
 constexpr int kDqThreads = 512;
 constexpr int kDqLaunch = 128, kDqCtl = 80, kDqEw = 152, kDqOut = 128;
 static_assert(kDqCtl + 2 * kDqEw + kDqOut <= 4 * kDqLaunch, "setmaxnreg split must fit the launch");
-constexpr int kDqSlots = 8, kDqReaders = 15;
+constexpr int kDqReaders = 15;
 
 struct DqItem {
   int32_t blocks;  // key blocks; 0: no more items
@@ -111,9 +122,15 @@ struct DqItem {
   int32_t tok0, ntok;
   int32_t key0, keys;
 };
+struct DqWinItem : DqItem {
+  int32_t p0;      // position of the first token
+  WinRange rg;     // the keys that the tile sees, keys = hi
+};
 
-template <int D>
+template <int D, bool kWin>
 struct DqSmem {
+  using Item = std::conditional_t<kWin, DqWinItem, DqItem>;
+  static constexpr int kSlots = kWin ? 4 : 8;
   static constexpr int kC = D / 64;
   static constexpr uint32_t kTile = kT * D * 2;
   static constexpr int kQ = D == 128 ? 1 : 2, kK = D == 128 ? 3 : 4, kV = D == 128 ? 2 : 4;
@@ -126,19 +143,21 @@ struct DqSmem {
   uint64_t s_full[2], ds_full[2], dq_full, dq_empty, mma_done;
   uint64_t pair_full[4];    // kFew: the two warps of 32 rows have their parts of D
   float pair[2][2][kT];
-  uint64_t item_full[kDqSlots], item_empty[kDqSlots];
-  DqItem item[kDqSlots];
+  uint64_t item_full[kSlots], item_empty[kSlots];
+  Item item[kSlots];
   uint32_t tmem_base;
   int abort_flag;
 };
 
-template <int D, bool kFew>
+template <int D, bool kFew, bool kWin>
 __global__ void __launch_bounds__(kDqThreads, 1)
     xattn_dq_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k,
                     const __grid_constant__ CUtensorMap tm_v, const __grid_constant__ CUtensorMap tm_do,
                     const BwdParams prm) {
   extern __shared__ __align__(1024) uint8_t smem_raw[];
-  using S = DqSmem<D>;
+  using S = DqSmem<D, kWin>;
+  using Item = typename S::Item;
+  constexpr int kDqSlots = S::kSlots;
   S& sm = *reinterpret_cast<S*>(smem_raw);
   const XattnParams& p = prm.x;
   const uint32_t warp = warp_id(), lane = lane_id();
@@ -200,7 +219,7 @@ __global__ void __launch_bounds__(kDqThreads, 1)
     if (!mbar_drain(bar, parity, kDrainTimeoutNs)) set_status(p.status, UT_ERR_TIMEOUT);
   };
   // The next item; false at the end or on an abort (then ok = false).
-  auto next_item = [&](uint32_t& n, DqItem& it, bool& ok) -> bool {
+  auto next_item = [&](uint32_t& n, Item& it, bool& ok) -> bool {
     const uint32_t s = n % kDqSlots;
     ok = wait(&sm.item_full[s], (n / kDqSlots) & 1);
     if (!ok) return false;
@@ -209,6 +228,17 @@ __global__ void __launch_bounds__(kDqThreads, 1)
     if (lane == 0) mbar_arrive(&sm.item_empty[s]);
     ++n;
     return it.blocks > 0;
+  };
+  // Block j of an item: its first key (of the segment's), and the keys from there on
+  auto block_of = [&](const Item& it, int j, int& x, int& left) {
+    if constexpr (kWin) {
+      int e;
+      win_block<kT>(it.rg, j, x, e);
+      left = e - x;
+    } else {
+      x = j * kT;
+      left = it.keys - x;
+    }
   };
 
   if (warp < 4) {
@@ -226,7 +256,7 @@ __global__ void __launch_bounds__(kDqThreads, 1)
       for (;;) {
         const uint32_t slot = n % kDqSlots;
         if (!(ok = wait1(&sm.item_full[slot], (n / kDqSlots) & 1))) break;
-        const DqItem it = sm.item[slot];
+        const Item it = sm.item[slot];
         mbar_arrive(&sm.item_empty[slot]);
         if (it.blocks == 0) break;
         const uint32_t qs = n % S::kQ, qf = (n / S::kQ) & 1;
@@ -237,15 +267,17 @@ __global__ void __launch_bounds__(kDqThreads, 1)
         ++n;
         for (int j = 0; j < it.blocks; ++j) {
           const uint32_t ks = at % S::kK, vs = nv % S::kV;
+          int x, left;
+          block_of(it, j, x, left);
           if (!(ok = wait1(&sm.k_empty[ks], ((at / S::kK) & 1) ^ 1))) break;
           mbar_expect_tx(&sm.k_full[ks], S::kTile);
           for (int c = 0; c < S::kC; ++c)
-            tma_load_3d(sm.k[ks] + c * kChunkB, &tm_k, &sm.k_full[ks], c * 64, it.hk, it.key0 + j * kT, keep);
+            tma_load_3d(sm.k[ks] + c * kChunkB, &tm_k, &sm.k_full[ks], c * 64, it.hk, it.key0 + x, keep);
           ++at;
           if (!(ok = wait1(&sm.dp_full[vs], ((nv / S::kV) & 1) ^ 1))) break;
           mbar_expect_tx(&sm.v_full[vs], S::kTile);
           for (int c = 0; c < S::kC; ++c)
-            tma_load_3d(sm.v[vs] + c * kChunkB, &tm_v, &sm.v_full[vs], c * 64, it.hk, it.key0 + j * kT, keep);
+            tma_load_3d(sm.v[vs] + c * kChunkB, &tm_v, &sm.v_full[vs], c * 64, it.hk, it.key0 + x, keep);
           ++nv;
           if (j > 0) continue;
           if (!(ok = wait1(&sm.do_empty[qs], qf ^ 1))) break;
@@ -269,14 +301,23 @@ __global__ void __launch_bounds__(kDqThreads, 1)
       bool ok = true, end = false;
       for (int64_t u0 = blockIdx.x; ok && !end; u0 += (int64_t)32 * gridDim.x) {
         const int64_t u = u0 + (int64_t)lane * gridDim.x;
-        DqItem it{};
+        Item it{};
         if (u < prm.n_items) {
           const Segment g = segment_of_slot(p.cu_q, p.B, p.nq, prm.tpt, u / p.Hk);
           const int64_t t0 = g.tile * prm.tpt;
           int64_t k0, kn;
-          segment_rows(p.cu_k, g.s, p.nk, k0, kn);
-          if (t0 < g.n)  // else an idle slot
-            it.blocks = (int)((kn + kT - 1) / kT);  // 0: no keys, the output warps have it
+          if constexpr (kWin) win_keys(p.cu_k, prm.k_len, p.nk, g.s, k0, kn);
+          else segment_rows(p.cu_k, g.s, p.nk, k0, kn);
+          if (t0 < g.n) {  // else an idle slot
+            if constexpr (kWin) {
+              it.p0 = (int)(kn - g.n + t0);
+              it.rg = win_range(it.p0, it.p0 + (int)min((int64_t)prm.tpt, g.n - t0) - 1, (int)kn, prm.left, prm.right,
+                                prm.sinks);
+              it.blocks = win_blocks<kT>(it.rg);
+            } else {
+              it.blocks = (int)((kn + kT - 1) / kT);  // 0: no keys, the output warps have it
+            }
+          }
           it.hk = (int)(u % p.Hk);
           it.tok0 = (int)(g.row + t0);
           it.ntok = (int)min((int64_t)prm.tpt, g.n - t0);
@@ -307,11 +348,13 @@ __global__ void __launch_bounds__(kDqThreads, 1)
       // And when Q (of a first block), K and V are there.
       uint32_t n = 0, at = 0;
       bool ok = true;
-      DqItem it;
+      Item it;
       while (ok && next_item(n, it, ok))
         for (int j = 0; j < it.blocks; ++j, ++at) {
           const uint32_t st = at % S::kK;
-          const uint32_t keys = lane_keys(p.mask, (int64_t)it.key0 + j * kT, it.keys - j * kT, lane);
+          int x0, left;
+          block_of(it, j, x0, left);
+          const uint32_t keys = lane_keys(p.mask, (int64_t)it.key0 + x0, left, lane);
           auto zero_keys = [&](uint32_t base) {
             for (int g = 0; g < 4; ++g)
               if (!((keys >> g) & 1u))
@@ -420,9 +463,10 @@ __global__ void __launch_bounds__(kDqThreads, 1)
     const uint64_t c2 = pack_f32x2(prm.scale_log2, prm.scale_log2);
     uint32_t n = 0, at = 0, pairs = 0;
     bool ok = true;
-    DqItem it, nx;
+    Item it, nx;
+    const int rt_first = (int)((quarter * 32 * prm.inv_g) >> 16), rt_last = (int)(((quarter * 32 + 31) * prm.inv_g) >> 16);
     // LSE and D of this row, loaded an item ahead; +inf and 0 where there is none
-    auto row_load = [&](const DqItem& x, float& l, float& d) {
+    auto row_load = [&](const Item& x, float& l, float& d) {
       l = INFINITY;
       d = 0.f;
       if (x.blocks > 0 && rt < x.ntok) {
@@ -444,15 +488,35 @@ __global__ void __launch_bounds__(kDqThreads, 1)
       more = next_item(n, nx, ok);
       if (!ok) break;
       row_load(nx, nl, nd);
-      uint32_t keys = lane_keys(p.mask, it.key0, it.keys, lane);
+      int kx, kleft;
+      block_of(it, 0, kx, kleft);
+      uint32_t keys = lane_keys(p.mask, (int64_t)it.key0 + kx, kleft, lane);
       for (int j = 0; j < it.blocks; ++j, ++at) {
         const uint32_t now = keys;
-        if (j + 1 < it.blocks) keys = lane_keys(p.mask, (int64_t)it.key0 + (j + 1) * kT, it.keys - (j + 1) * kT, lane);
+        const int xw = kx + (int)half * 64;  // key of this warp's first column
+        if (j + 1 < it.blocks) {
+          block_of(it, j + 1, kx, kleft);
+          keys = lane_keys(p.mask, (int64_t)it.key0 + kx, kleft, lane);
+        }
         const uint32_t ts = lane_base + (at & 1) * 256 + half * 64;
         if (!(ok = wait(&sm.s_full[at & 1], (at >> 1) & 1))) break;
         tc_fence_after();
         uint32_t r[64];
         tmem_ld64(ts, r);
+        bool whole = __all_sync(0xffffffffu, now == 15u);
+        if constexpr (kWin) {  // the rows' own limits, where some row of the warp has one in this block
+          if (it.p0 + rt_first + prm.right - xw < 63 || (it.p0 + rt_last - prm.left > xw && xw + 64 > prm.sinks)) {
+            const int hi = it.p0 + rt + prm.right - xw, lo = it.p0 + rt - prm.left - xw, sink = prm.sinks - xw;
+            uint32_t on[2];
+#pragma unroll
+            for (int w = 0; w < 2; ++w) on[w] = bits_to(hi - 32 * w) & (bits_from(lo - 32 * w) | bits_to(sink - 1 - 32 * w));
+            asm volatile("" : "+r"(on[0]), "+r"(on[1]));  // a branch: most blocks pass it by
+#pragma unroll
+            for (int x = 0; x < 64; ++x)
+              if (!((on[x >> 5] >> (x & 31)) & 1u)) r[x] = 0xff800000u;
+            whole = false;
+          }
+        }
 #pragma unroll
         for (int x = 0; x < 64; x += 2) {
           float a, b;
@@ -460,7 +524,6 @@ __global__ void __launch_bounds__(kDqThreads, 1)
           r[x] = __float_as_uint(ex2_approx(a));
           r[x + 1] = __float_as_uint(ex2_approx(b));
         }
-        const bool whole = __all_sync(0xffffffffu, now == 15u);
         if (!whole) {  // P of a masked key (S = 0) may be infinite; the others' is at most 1, or NaN, which stays
 #pragma unroll
           for (int x = 0; x < 64; ++x) r[x] = __float_as_uint(min_nan(__uint_as_float(r[x]), 2.f));
@@ -529,7 +592,7 @@ __global__ void __launch_bounds__(kDqThreads, 1)
                             : nullptr;
     };
     // Tiles of segments without keys: dQ = 0.  32 items are looked at together.
-    if (p.cu_k || p.nk == 0)
+    if (kWin || p.cu_k || p.nk == 0)
       for (int64_t u0 = blockIdx.x; u0 < prm.n_items; u0 += (int64_t)32 * gridDim.x) {
         const int64_t u = u0 + (int64_t)lane * gridDim.x;
         int64_t tok0 = 0, k0, kn;
@@ -537,9 +600,15 @@ __global__ void __launch_bounds__(kDqThreads, 1)
         if (u < prm.n_items) {
           const Segment g = segment_of_slot(p.cu_q, p.B, p.nq, prm.tpt, u / p.Hk);
           const int64_t t0 = g.tile * prm.tpt;
-          segment_rows(p.cu_k, g.s, p.nk, k0, kn);
+          if constexpr (kWin) win_keys(p.cu_k, prm.k_len, p.nk, g.s, k0, kn);
+          else segment_rows(p.cu_k, g.s, p.nk, k0, kn);
           tok0 = g.row + t0;
-          if (t0 < g.n && kn == 0) ntok = (int)min((int64_t)prm.tpt, g.n - t0);
+          bool none = kn == 0;
+          if constexpr (kWin) {
+            const int pa = (int)(kn - g.n + t0), pb = pa + (int)min((int64_t)prm.tpt, g.n - t0) - 1;
+            none = win_blocks<kT>(win_range(pa, pb, (int)kn, prm.left, prm.right, prm.sinks)) == 0;
+          }
+          if (t0 < g.n && none) ntok = (int)min((int64_t)prm.tpt, g.n - t0);
         }
         for (uint32_t found = __ballot_sync(0xffffffffu, ntok > 0); found; found &= found - 1) {
           const int who = __ffs(found) - 1;
@@ -555,7 +624,7 @@ __global__ void __launch_bounds__(kDqThreads, 1)
       }
     uint32_t n = 0;
     bool ok = true;
-    DqItem it;
+    Item it;
     while (ok && next_item(n, it, ok)) {
       __nv_bfloat16* out[4];  // the rows of this lane's quad, its 16-byte unit
 #pragma unroll
@@ -616,6 +685,11 @@ struct Work {  // one item: a run of query tiles, a kv head, every ks-th key blo
   int32_t tok0, key0, ntok, keys;           // tokens of the run, keys of the segment
   int32_t kslot;                            // first key block's place among all segments'
 };
+struct WinWork : Work {
+  int32_t p0;      // position of the first token
+  int32_t direct;  // dK and dV are whole: not a partial sum
+  int32_t rows;    // rows of the segment's dK and dV; its keys may be fewer
+};
 
 // Item u, by a whole warp; blocks 0 where its slot is idle.
 UT_DEV Work decode(const BwdParams& b, int u) {
@@ -640,8 +714,66 @@ UT_DEV Work decode(const BwdParams& b, int u) {
   return w;
 }
 
-template <int D>
+// Windowed attention: item u is one key block and a run of the tiles that see it,
+// which begin at the first token that does.  Blocks with first keys, which all
+// later tokens see, come first (longer items), their runs dealt out by the
+// queries' slots.
+UT_DEV WinWork decode_window(const BwdParams& b, int u) {
+  const XattnParams& p = b.x;
+  WinWork w{};
+  w.blocks = -1;  // an idle slot
+  Segment g;
+  int64_t q0, qn, k0, kn;
+  int run, R, j;
+  const bool first = u < b.n_first;
+  if (first) {
+    const int at = u / p.Hk, slot = at / b.sb;
+    w.hk = u - at * p.Hk;
+    j = at - slot * b.sb;
+    R = b.Rs;
+    g = warp_segment_of_slot(p.cu_q, p.B, p.nq, R * b.tpt, slot);
+    segment_rows(p.cu_q, g.s, p.nq, q0, qn);
+    run = (int)g.tile;
+    w.kslot = (b.join ? b.chunks * (int)b.kslots : 0) + slot * b.sb;
+    w.direct = !b.join_first;
+  } else {
+    const int v = (int)(u - b.n_first), at = v / p.Hk, slot = at / b.chunks;
+    w.hk = v - at * p.Hk;
+    run = at - slot * b.chunks;
+    R = b.R;
+    g = warp_segment_of_slot(p.cu_k, p.B, p.nk, kT, slot);
+    segment_rows(p.cu_q, g.s, p.nq, q0, qn);
+    j = (int)g.tile;
+    w.part = run;
+    w.kslot = slot - j;
+    w.direct = !b.join;
+  }
+  int64_t span;
+  segment_rows(p.cu_k, g.s, p.nk, k0, span);
+  win_keys(p.cu_k, b.k_len, p.nk, g.s, k0, kn);
+  const int64_t x = (int64_t)j * kT;
+  if (x >= span || first != (x < b.sinks)) return w;
+  int t0 = 0, t1 = 0;
+  if (x < kn)
+    win_tokens((int)x, (int)min(x + kT, kn), (int)kn, (int)qn, b.left, b.right, b.sinks, t0, t1);
+  const int from = t0 + run * R * b.tpt;
+  w.block0 = j;
+  w.key0 = (int)k0;
+  w.keys = (int)kn;
+  w.rows = (int)span;
+  w.tok0 = (int)(q0 + from);
+  w.ntok = min(R * b.tpt, t1 - from);
+  w.p0 = (int)(kn - qn) + from;
+  if (run > 0 && w.ntok <= 0) return w;
+  w.tiles = w.ntok > 0 ? (w.ntok + b.tpt - 1) / b.tpt : 0;
+  w.blocks = w.tiles > 0 ? 1 : 0;
+  if (w.blocks == 0) w.ntok = (int)min((int64_t)kT, span - x);  // no query sees it: rows to be cleared
+  return w;
+}
+
+template <int D, bool kWin>
 struct KvSmem {
+  using Item = std::conditional_t<kWin, WinWork, Work>;
   static constexpr int kC = D / 64;
   static constexpr uint32_t kTile = kT * D * 2;
   static constexpr int kQ = D == 128 ? 3 : 4, kDo = D == 128 ? 2 : 4;
@@ -649,7 +781,7 @@ struct KvSmem {
   alignas(1024) uint8_t v[kTile];
   alignas(1024) uint8_t q[kQ][kTile];
   alignas(1024) uint8_t dout[kDo][kTile];
-  Work item[kKvSlots];
+  Item item[kKvSlots];
   NextItem next;
   alignas(16) float lse2[2][kT];  // -LSE log2(e) and -D of the rows of a tile
   alignas(16) float dsum[2][kT];
@@ -660,13 +792,14 @@ struct KvSmem {
   int abort_flag;
 };
 
-template <int D>
+template <int D, bool kWin>
 __global__ void __launch_bounds__(kKvThreads, 1)
     xattn_dkdv_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k,
                       const __grid_constant__ CUtensorMap tm_v, const __grid_constant__ CUtensorMap tm_do,
                       const BwdParams prm) {
   extern __shared__ __align__(1024) uint8_t smem_raw[];
-  using S = KvSmem<D>;
+  using S = KvSmem<D, kWin>;
+  using Item = typename S::Item;
   S& sm = *reinterpret_cast<S*>(smem_raw);
   const XattnParams& p = prm.x;
   const uint32_t warp = warp_id(), lane = lane_id();
@@ -709,6 +842,9 @@ __global__ void __launch_bounds__(kKvThreads, 1)
   __syncthreads();
   tc_fence_after();
   grid_wait();
+  if constexpr (kWin) {
+    if (blockIdx.x == 0) check_lens_of(p, prm.k_len);
+  }
   if (sm.tmem_base != 0 && threadIdx.x == 0) {  // as in the dQ kernel
     set_status(p.status, UT_ERR_CUDA);
     sm.abort_flag = 1;
@@ -721,7 +857,7 @@ __global__ void __launch_bounds__(kKvThreads, 1)
   };
 
   // The next item; false at the end or on an abort (then ok = false).  Whole warp.
-  auto next_item = [&](uint32_t& n, Work& w, bool& ok) -> bool {
+  auto next_item = [&](uint32_t& n, Item& w, bool& ok) -> bool {
     const uint32_t s = n % kKvSlots;
     if (!(ok = wait(&sm.item_full[s], (n / kKvSlots) & 1))) return false;
     w = sm.item[s];
@@ -739,8 +875,20 @@ __global__ void __launch_bounds__(kKvThreads, 1)
       uint32_t nkv = 0, nt = 0, n = 0, asked = 0;
       bool ok = true;
       for (int u = (int)blockIdx.x; ok;) {
-        Work w{};
-        if (u >= 0) w = decode(prm, u);
+        Item w{};
+        if constexpr (kWin) {
+          if (u >= 0) w = decode_window(prm, u);
+          if (u >= 0 && w.blocks == 0 && w.direct)  // a key block that no query sees
+            for (int r = (int)lane / 8; r < w.ntok; r += 4)
+              for (int c = (int)(lane & 7) * 8; c < D; c += 64) {
+                const int64_t key = w.key0 + (int64_t)w.block0 * kT + r;
+                *reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(p.dk) + key * p.dks + w.hk * D + c) = make_uint4(0, 0, 0, 0);
+                *reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(p.dv) + key * p.dvs + w.hk * D + c) = make_uint4(0, 0, 0, 0);
+              }
+          if (u < 0) w.blocks = 0;
+        } else {
+          if (u >= 0) w = decode(prm, u);
+        }
         if (u < 0 || w.blocks > 0) {
           const uint32_t s = n % kKvSlots;
           if (!(ok = wait(&sm.item_empty[s], ((n / kKvSlots) & 1) ^ 1))) break;
@@ -868,7 +1016,7 @@ __global__ void __launch_bounds__(kKvThreads, 1)
       const uint64_t keep = policy_evict_last();
       uint32_t n = 0, nt = 0, sent = 0;  // items, tiles made ready, dO tiles asked for
       bool ok = true;
-      Work w;
+      Item w;
       while (ok && next_item(n, w, ok)) {
         int left = w.blocks * w.tiles, tok = w.tok0;  // dO tiles to ask for, the next one's token
         const int end = w.tok0 + w.tiles * prm.tpt;
@@ -950,13 +1098,26 @@ __global__ void __launch_bounds__(kKvThreads, 1)
     const uint64_t c2 = pack_f32x2(prm.scale_log2, prm.scale_log2);
     uint32_t n = 0, nt = 0, ng = 0;
     bool ok = true;
-    Work w;
+    Item w;
     while (ok && next_item(n, w, ok)) {
       for (int b = 0; b < w.blocks && ok; ++b, ++ng) {
         const int j = w.block0 + b * prm.ks;
         const int key = j * kT + (int)krow;
         // P and dS of a masked key are zero: as a mask of the packed pairs
         const uint32_t on = key < w.keys && (!p.mask || p.mask[w.key0 + key]) ? 0xffffffffu : 0u;
+        int ptok = 0;  // position of the tile's first token
+        uint32_t seen[2] = {~0u, ~0u};
+        bool limits = false;
+        if constexpr (kWin) ptok = w.p0;
+        auto keep_seen = [&](uint32_t* pk) {  // the pairs of columns that `seen` has
+          asm volatile("" : "+r"(seen[0]), "+r"(seen[1]));  // a branch: most tiles pass it by
+#pragma unroll
+          for (int x = 0; x < HC; x += 2) {
+            const uint32_t two = seen[x >> 5] >> (x & 31);
+            if (!(two & 1u)) pk[x / 2] &= 0xffff0000u;
+            if (!(two & 2u)) pk[x / 2] &= 0x0000ffffu;
+          }
+        };
         for (int t = 0; t < w.tiles; ++t, ++nt) {
           const uint32_t par = nt & 1;
           const float* ls = sm.lse2[par] + half * HC;
@@ -987,6 +1148,20 @@ __global__ void __launch_bounds__(kKvThreads, 1)
             pk[x / 2] = pack_bf16x2(a, b) & on;
             pk[x / 2 + 1] = pack_bf16x2(c, d) & on;
           }
+          if constexpr (kWin) {
+            // the tokens that this key's limits leave out, where a tile has some
+            const int x0 = j * kT + (int)quarter * 32;  // key of the warp's first row
+            limits = x0 + 31 - prm.right > ptok || (x0 + prm.left < ptok + prm.tpt - 1 && x0 + 31 >= prm.sinks);
+            if (limits) {
+              // (tokens of the tile, then columns)
+              const int from = min(max(key - prm.right - ptok, 0), kT), to = min(max(key + prm.left - ptok + 1, 0), kT);
+              const int c0 = (int)half * HC, lo = from * p.G - c0, hi = key < prm.sinks ? HC : to * p.G - 1 - c0;
+              seen[0] = bits_from(lo) & bits_to(hi);
+              seen[1] = bits_from(lo - 32) & bits_to(hi - 32);
+              keep_seen(pk);
+            }
+            ptok += prm.tpt;
+          }
           tmem_st32(ts, pk);
           tmem_wait_st();
           tc_fence_before();
@@ -1013,6 +1188,9 @@ __global__ void __launch_bounds__(kKvThreads, 1)
               pk[h * 16 + x / 2 + 1] = pack_bf16x2(c, d) & on;
             }
           }
+          if constexpr (kWin) {
+            if (limits) keep_seen(pk);
+          }
           tmem_st32(ts + 128, pk);
           tmem_wait_st();
           tc_fence_before();
@@ -1023,6 +1201,38 @@ __global__ void __launch_bounds__(kKvThreads, 1)
         // this run's dV, dK of the key block
         if (!(ok = wait(&sm.acc_full, ng & 1))) break;
         tc_fence_after();
+        if constexpr (kWin) {
+          if (w.direct) {
+            const int64_t row = (int64_t)w.key0 + key;
+            const bool exists = key < w.rows;
+#pragma unroll 1
+            for (int which = 0; which < 2; ++which) {
+              __nv_bfloat16* dst = which ? static_cast<__nv_bfloat16*>(p.dk) + row * p.dks : static_cast<__nv_bfloat16*>(p.dv) + row * p.dvs;
+              dst += w.hk * D + half * HD;
+              const float f = which ? p.scale : 1.f;
+#pragma unroll 1
+              for (int g = 0; g < HD / 32; ++g) {
+                uint32_t r[32];
+                tmem_ld32(lane_base + (which ? 384 : 256) + half * HD + g * 32, r);
+                tmem_wait_ld();
+                if (exists) {
+#pragma unroll
+                  for (int x = 0; x < 32; x += 8)  // a masked key's row is zero, whatever met its P and dS of 0
+                    *reinterpret_cast<uint4*>(dst + g * 32 + x) = make_uint4(
+                        pack_bf16x2(__uint_as_float(r[x]) * f, __uint_as_float(r[x + 1]) * f) & on,
+                        pack_bf16x2(__uint_as_float(r[x + 2]) * f, __uint_as_float(r[x + 3]) * f) & on,
+                        pack_bf16x2(__uint_as_float(r[x + 4]) * f, __uint_as_float(r[x + 5]) * f) & on,
+                        pack_bf16x2(__uint_as_float(r[x + 6]) * f, __uint_as_float(r[x + 7]) * f) & on);
+                }
+                __syncwarp();
+              }
+            }
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&sm.acc_empty);
+            continue;
+          }
+        }
         const int64_t at =
             ((((int64_t)w.part * prm.kslots + w.kslot + j) * p.Hk + w.hk) * (D / 4) + half * (HD / 4)) * kT + krow;
 #pragma unroll
@@ -1055,7 +1265,7 @@ __global__ void __launch_bounds__(kKvThreads, 1)
 // slots, kv heads, dK / dV), a block one key block: read 16 bytes a thread
 // along the keys, all of a part in flight, written as rows through shared
 // memory.
-template <int D>
+template <int D, bool kWin>
 __global__ void __launch_bounds__(256) xattn_bwd_join_kernel(const BwdParams prm) {
   constexpr int kPer = D / 4 * kT / 256;
   __shared__ __align__(16) uint8_t rows[kT * (D * 2 + 16)];
@@ -1066,12 +1276,32 @@ __global__ void __launch_bounds__(256) xattn_bwd_join_kernel(const BwdParams prm
   if (keys <= 0) return;
   int64_t row, nq;
   segment_rows(p.cu_q, g.s, p.nq, row, nq);
-  const int64_t tiles = (nq + prm.tpt - 1) / prm.tpt;
-  const int parts = (int)((tiles + prm.R - 1) / prm.R);
-  const int64_t kslot = min(g.row / kT + g.s + g.tile, prm.kslots - 1);
+  int64_t tiles = (nq + prm.tpt - 1) / prm.tpt;
+  int parts = (int)((tiles + prm.R - 1) / prm.R);
+  int64_t kslot = min(g.row / kT + g.s + g.tile, prm.kslots - 1), slots = prm.kslots;  // of a part, to the next
+  int64_t n_keys = g.n;
+  if constexpr (kWin) {
+    const int64_t x = g.tile * kT;
+    const bool first = x < prm.sinks;
+    if (!(first ? prm.join_first : prm.join)) return;
+    int64_t k0;
+    win_keys(p.cu_k, prm.k_len, p.nk, g.s, k0, n_keys);
+    int t0 = 0, t1 = 0;
+    if (x < n_keys)
+      win_tokens((int)x, (int)min(x + kT, n_keys), (int)n_keys, (int)nq, prm.left, prm.right, prm.sinks, t0, t1);
+    const int R = first ? prm.Rs : prm.R;
+    tiles = (t1 - t0 + prm.tpt - 1) / prm.tpt;
+    parts = (int)((tiles + R - 1) / R);
+    if (first) {
+      // the segment's first run among all segments'
+      const int64_t run = min(row / (R * prm.tpt) + g.s, prm.qslots - parts);
+      kslot = (prm.join ? prm.chunks * prm.kslots : 0) + run * prm.sb + g.tile;
+      slots = prm.sb;
+    }
+  }
   const bool is_k = blockIdx.z == 0;
   const float* src = (is_k ? p.part_dk : p.part_dv) + (kslot * p.Hk + blockIdx.y) * (D * kT) + threadIdx.x * 4;
-  const int64_t step = prm.kslots * p.Hk * (D * kT);
+  const int64_t step = slots * p.Hk * (D * kT);
   const float f = is_k ? p.scale : 1.f;
   float4 a[kPer];
 #pragma unroll
@@ -1102,13 +1332,15 @@ __global__ void __launch_bounds__(256) xattn_bwd_join_kernel(const BwdParams prm
     const int r = x / (D / 8), e = x % (D / 8);
     const int64_t key = g.row + g.tile * kT + r;
     // a masked key's row is zero, also where a NaN or an infinity of Q or dO met its P and dS of 0
-    const uint4 v = p.mask && !p.mask[key] ? make_uint4(0, 0, 0, 0)
+    const uint4 v = (p.mask && !p.mask[key]) || (kWin && g.tile * kT + r >= n_keys) ? make_uint4(0, 0, 0, 0)
                                            : *reinterpret_cast<const uint4*>(rows + r * (D * 2 + 16) + e * 16);
     *reinterpret_cast<uint4*>(out + key * stride + e * 8) = v;
   }
 }
 
-static_assert(sizeof(DqSmem<128>) <= 232448 && sizeof(KvSmem<128>) <= 232448 && sizeof(DqSmem<64>) <= 232448,
+static_assert(sizeof(DqSmem<128, false>) <= 232448 && sizeof(KvSmem<128, false>) <= 232448 &&
+                  sizeof(DqSmem<64, false>) <= 232448 && sizeof(DqSmem<128, true>) <= 232448 &&
+                  sizeof(KvSmem<128, true>) <= 232448 && sizeof(DqSmem<64, true>) <= 232448,
               "shared layout exceeds the block limit");
 
 // The setmaxnreg split assumes exactly `regs` registers per thread at launch:
@@ -1205,22 +1437,131 @@ cudaError_t launch_xattn_bwd_tc(const XattnParams& p, void* ws, cudaStream_t s) 
       return cudaErrorInvalidValue;
     prm.n_items = segment_slots(p.nq, p.B, prm.tpt) * p.Hk;
     const int64_t grid = prm.n_items < p.sms ? prm.n_items : p.sms;
-    e = p.d == 64 ? launch(few ? xattn_dq_kernel<64, true> : xattn_dq_kernel<64, false>, grid, kDqThreads,
-                           sizeof(DqSmem<64>), kDqLaunch, prm, tm, s)
-                  : launch(few ? xattn_dq_kernel<128, true> : xattn_dq_kernel<128, false>, grid, kDqThreads,
-                           sizeof(DqSmem<128>), kDqLaunch, prm, tm, s);
+    e = p.d == 64 ? launch(few ? xattn_dq_kernel<64, true, false> : xattn_dq_kernel<64, false, false>, grid, kDqThreads,
+                           sizeof(DqSmem<64, false>), kDqLaunch, prm, tm, s)
+                  : launch(few ? xattn_dq_kernel<128, true, false> : xattn_dq_kernel<128, false, false>, grid, kDqThreads,
+                           sizeof(DqSmem<128, false>), kDqLaunch, prm, tm, s);
     if (e != cudaSuccess) return e;
     if (p.nk > 0) {
       prm.n_items = segment_slots(p.nq, p.B, prm.R * prm.tpt) * p.Hk * prm.ks;
-      e = p.d == 64 ? launch(xattn_dkdv_kernel<64>, prm.n_items, kKvThreads, sizeof(KvSmem<64>), kKvLaunch, prm, tm, s)
-                    : launch(xattn_dkdv_kernel<128>, prm.n_items, kKvThreads, sizeof(KvSmem<128>), kKvLaunch, prm, tm, s);
+      e = p.d == 64 ? launch(xattn_dkdv_kernel<64, false>, prm.n_items, kKvThreads, sizeof(KvSmem<64, false>), kKvLaunch,
+                             prm, tm, s)
+                    : launch(xattn_dkdv_kernel<128, false>, prm.n_items, kKvThreads, sizeof(KvSmem<128, false>), kKvLaunch,
+                             prm, tm, s);
       if (e != cudaSuccess) return e;
     }
   }
   if (p.nk > 0) {
     const dim3 grid((unsigned)prm.kslots, p.Hk, 2);
-    e = p.d == 64 ? launch_next(xattn_bwd_join_kernel<64>, grid, dim3(256), 0, s, prm)
-                  : launch_next(xattn_bwd_join_kernel<128>, grid, dim3(256), 0, s, prm);
+    e = p.d == 64 ? launch_next(xattn_bwd_join_kernel<64, false>, grid, dim3(256), 0, s, prm)
+                  : launch_next(xattn_bwd_join_kernel<128, false>, grid, dim3(256), 0, s, prm);
+  }
+  return e;
+}
+
+// ------------------------------------------------------- windowed attention
+namespace {
+
+// The runs of the dK, dV kernel.  A block without first keys is seen by at most
+// `near` tokens: one run, whose dK and dV are written at once, unless there are
+// fewer items than SMs twice.  Blocks with first keys are seen by all later
+// tokens: runs of at least twice those tiles, three times as many as SMs, whose
+// parts are joined; but one run each where there are many such blocks (first
+// keys without a window), or few tokens.
+void window_runs(const WinParams& w, BwdParams& b) {
+  const XattnParams& p = w.x;
+  const int64_t tpt = kT / p.G, all = (p.nq + tpt - 1) / tpt, seen = (int64_t)w.left + w.right + kT;
+  const int64_t near = std::max<int64_t>(1, ((seen < p.nq ? seen : p.nq) + tpt - 1) / tpt);
+  b.kslots = segment_slots(p.nk, p.B, kT);
+  const int64_t items = b.kslots * p.Hk;
+  int64_t chunks = items < 2 * p.sms ? (2 * p.sms + items - 1) / items : 1;
+  chunks = std::min(chunks, (near + 3) / 4);  // four tiles a run at least
+  b.R = (int)((near + chunks - 1) / chunks);
+  b.chunks = (int)((near + b.R - 1) / b.R);
+  b.join = b.chunks > 1;
+  b.sb = (int)(((w.sinks < p.nk ? w.sinks : p.nk) + kT - 1) / kT);
+  b.Rs = (int)std::max<int64_t>(all, 1);
+  b.qslots = 0;
+  if (b.sb > 0) {
+    const int64_t blocks = (int64_t)b.sb * p.Hk;  // of a segment
+    if (blocks * p.B < 4 * p.sms) {
+      const int64_t runs = std::max<int64_t>(1, 3 * p.sms / blocks);
+      b.Rs = (int)std::min<int64_t>(b.Rs, std::max((all + runs - 1) / runs, std::max<int64_t>(2 * near, 8)));
+    }
+    b.qslots = segment_slots(p.nq, p.B, (int)(b.Rs * tpt));
+  }
+  b.join_first = b.sb > 0 && b.Rs < all;
+  b.n_first = b.qslots * b.sb * p.Hk;
+}
+
+// one of the two partial sums: those of blocks without first keys, then those with
+size_t window_part_bytes(const WinParams& w, const BwdParams& b) {
+  const int64_t blocks = (b.join ? b.chunks * b.kslots : 0) + (b.join_first ? b.qslots * b.sb : 0);
+  return (size_t)blocks * w.x.Hk * w.x.d * kT * sizeof(float);
+}
+
+}  // namespace
+
+int64_t wattn_bwd_tc_items(const WinParams& w) {
+  BwdParams b{};
+  window_runs(w, b);
+  return std::max(segment_slots(w.x.nq, w.x.B, kT / w.x.G) * w.x.Hk,
+                  std::max(b.n_first + b.kslots * b.chunks * w.x.Hk, (b.chunks * b.kslots + b.qslots * b.sb)));
+}
+
+size_t wattn_bwd_tc_ws(const WinParams& w) {
+  BwdParams b{};
+  window_runs(w, b);
+  return 2 * window_part_bytes(w, b);
+}
+
+cudaError_t launch_wattn_bwd_tc(const WinParams& w, void* ws, cudaStream_t s) {
+  const XattnParams& p = w.x;
+  BwdParams prm{};
+  prm.x = p;
+  prm.inv_g = (65536u + p.G - 1) / p.G;
+  prm.tpt = kT / p.G;
+  prm.ks = 1;
+  prm.k_len = w.k_len;
+  prm.left = w.left;
+  prm.right = w.right;
+  prm.sinks = w.sinks;
+  window_runs(w, prm);
+  prm.x.part_dk = static_cast<float*>(ws);
+  prm.x.part_dv = reinterpret_cast<float*>(static_cast<char*>(ws) + window_part_bytes(w, prm));
+  prm.scale_log2 = p.scale * kLog2e;
+  cudaError_t e = launch_xattn_dsum(p, true, s);
+  if (e != cudaSuccess) return e;
+  // an empty side has no tensor to describe: its maps are never used
+  const void* any = p.nq > 0 ? p.q : p.k;
+  const int64_t as = p.nq > 0 ? p.qs : p.ks, an = p.nq > 0 ? p.nq : p.nk, ah = p.nq > 0 ? p.H : p.Hk;
+  const bool hq = p.nq > 0, hk = p.nk > 0;
+  CUtensorMap tm[4];
+  if (!encode_tmap_heads_bf16(&tm[0], hq ? p.q : any, p.d, hq ? p.H : ah, hq ? p.nq : an, (hq ? p.qs : as) * 2, hq ? p.G : 1,
+                              hq ? prm.tpt : 1) ||
+      !encode_tmap_heads_bf16(&tm[1], hk ? p.k : any, p.d, hk ? p.Hk : ah, hk ? p.nk : an, (hk ? p.ks : as) * 2, 1, kT) ||
+      !encode_tmap_heads_bf16(&tm[2], hk ? p.v : any, p.d, hk ? p.Hk : ah, hk ? p.nk : an, (hk ? p.vs : as) * 2, 1, kT) ||
+      !encode_tmap_heads_bf16(&tm[3], hq ? p.dout : any, p.d, hq ? p.H : ah, hq ? p.nq : an, (hq ? p.dos : as) * 2,
+                              hq ? p.G : 1, hq ? prm.tpt : 1))
+    return cudaErrorInvalidValue;
+  if (hq) {
+    prm.n_items = segment_slots(p.nq, p.B, prm.tpt) * p.Hk;
+    const int64_t grid = prm.n_items < p.sms ? prm.n_items : p.sms;
+    e = p.d == 64 ? launch(xattn_dq_kernel<64, true, true>, grid, kDqThreads, sizeof(DqSmem<64, true>), kDqLaunch, prm, tm, s)
+                  : launch(xattn_dq_kernel<128, true, true>, grid, kDqThreads, sizeof(DqSmem<128, true>), kDqLaunch, prm, tm, s);
+    if (e != cudaSuccess) return e;
+  }
+  if (hk) {
+    prm.n_items = prm.n_first + prm.kslots * prm.chunks * p.Hk;
+    e = p.d == 64
+            ? launch(xattn_dkdv_kernel<64, true>, prm.n_items, kKvThreads, sizeof(KvSmem<64, true>), kKvLaunch, prm, tm, s)
+            : launch(xattn_dkdv_kernel<128, true>, prm.n_items, kKvThreads, sizeof(KvSmem<128, true>), kKvLaunch, prm, tm, s);
+    if (e != cudaSuccess) return e;
+  }
+  if (hk && (prm.join || prm.join_first)) {
+    const dim3 grid((unsigned)prm.kslots, p.Hk, 2);
+    e = p.d == 64 ? launch_next(xattn_bwd_join_kernel<64, true>, grid, dim3(256), 0, s, prm)
+                  : launch_next(xattn_bwd_join_kernel<128, true>, grid, dim3(256), 0, s, prm);
   }
   return e;
 }

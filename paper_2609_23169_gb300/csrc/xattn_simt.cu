@@ -324,7 +324,6 @@ __global__ void __launch_bounds__(256) xattn_dsum_kernel(const XattnParams p) {
 // dK (blockIdx.y = 0), dV = the sum of the splits' partials, in split order; 4
 // values a thread, small blocks, 16 loads in flight
 constexpr int kJoinThreads = 64;
-template <typename T>
 __global__ void __launch_bounds__(kJoinThreads) xattn_dkdv_join_kernel(const XattnParams p) {
   const int64_t x = (int64_t)blockIdx.x * kJoinThreads + threadIdx.x;
   const int per_row = p.Hk * p.d / 4;
@@ -347,7 +346,7 @@ __global__ void __launch_bounds__(kJoinThreads) xattn_dkdv_join_kernel(const Xat
   const float f = is_v ? 1.f : p.scale;
   // a masked key's row is zero, also where a NaN or an infinity of Q or dO met its P and dS of 0
   if (p.mask && !p.mask[key]) a = make_float4(0, 0, 0, 0);
-  st4(static_cast<T*>(is_v ? p.dv : p.dk) + key * (is_v ? p.dvs : p.dks) + e,
+  st4(static_cast<float*>(is_v ? p.dv : p.dk) + key * (is_v ? p.dvs : p.dks) + e,
       make_float4(a.x * f, a.y * f, a.z * f, a.w * f));
 }
 
@@ -398,10 +397,9 @@ static cudaError_t launch(F kern, dim3 grid, size_t smem, const XattnParams& p, 
   return cudaGetLastError();
 }
 
-cudaError_t launch_xattn_dkdv_join(const XattnParams& p, bool bf16, cudaStream_t s) {
-  const dim3 grid((unsigned)((p.nk * p.Hk * p.d / 4 + kJoinThreads - 1) / kJoinThreads), 2);
-  return bf16 ? launch_next(xattn_dkdv_join_kernel<__nv_bfloat16>, grid, dim3(kJoinThreads), 0, s, p)
-              : launch_next(xattn_dkdv_join_kernel<float>, grid, dim3(kJoinThreads), 0, s, p);
+cudaError_t launch_xattn_dkdv_join(const XattnParams& p, cudaStream_t s) {
+  return launch_next(xattn_dkdv_join_kernel, dim3((unsigned)((p.nk * p.Hk * p.d / 4 + kJoinThreads - 1) / kJoinThreads), 2),
+                     dim3(kJoinThreads), 0, s, p);
 }
 
 template <typename T, int D>
@@ -425,7 +423,7 @@ static cudaError_t bwd(const XattnParams& p, cudaStream_t s) {
   if (e == cudaSuccess)
     e = launch_next(xattn_bwd_simt_kernel<T, D>, dim3((unsigned)(n_kv + n_q)), dim3(kXsThreads), smem, s, p,
                     (uint32_t)n_kv, kslots, qslots);
-  if (e == cudaSuccess && p.nk > 0) e = launch_xattn_dkdv_join(p, sizeof(T) == 2, s);
+  if (e == cudaSuccess && p.nk > 0) e = launch_xattn_dkdv_join(p, s);
   return e;
 }
 
