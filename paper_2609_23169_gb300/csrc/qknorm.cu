@@ -67,13 +67,13 @@ UT_DEV float head_sum(float x) {  // over the lanes of a head
   return x;
 }
 
-// what a lane keeps: its pairs and its columns of the weights
+// What a lane keeps: its pairs, and their sines at the token's position.
 template <typename T, int D>
 struct Lane {
   static constexpr int kVals = Vec<T>::kVals, kPairs = kVals / 2, kLanes = D / kVals, kHeads = 32 / kLanes;
   uint64_t turn[kPairs];
   uint32_t axis[kPairs];
-  float wq[kVals], wk[kVals], cs[kPairs], sn[kPairs];
+  float cs[kPairs], sn[kPairs];
   int group, col;  // the head of a step, the first of its columns
 
   UT_DEV void init(const QkNormParams& p, int lane) {
@@ -83,11 +83,6 @@ struct Lane {
     for (int e = 0; e < kPairs; ++e) {
       turn[e] = p.turn[col / 2 + e];
       axis[e] = p.axis[col / 2 + e];
-    }
-#pragma unroll
-    for (int e = 0; e < kVals; ++e) {
-      wq[e] = p.wq ? p.wq[col + e] : 1.f;
-      wk[e] = p.wk ? p.wk[col + e] : 1.f;
     }
   }
   UT_DEV void turn_to(const QkNormParams& p, int32_t pos) {
@@ -100,37 +95,87 @@ struct Lane {
       sincospif((float)part * 4.656612873077393e-10f, &sn[e], &cs[e]);
     }
   }
+  UT_DEV void weights(const float* w, float (&out)[kVals]) const {
+#pragma unroll
+    for (int e = 0; e < kVals; ++e) out[e] = w ? w[col + e] : 1.f;
+  }
 };
 
-// The steps of a token: kHeads heads each, of Q, then K, then V.
-template <int kHeads>
-struct Steps {
-  int q, k, all;
-  UT_DEV Steps(const QkNormParams& p, bool with_v) {
-    q = (p.H + kHeads - 1) / kHeads;
-    k = q + (p.Hk + kHeads - 1) / kHeads;
-    all = k + (with_v ? (p.Hk + kHeads - 1) / kHeads : 0);
+// Steps [s, end) of one tensor of a token, kHeads heads each: y = R (x r w), or
+// a copy.  With the weights in the rotation, a w cos and so on, a pair takes four
+// multiplications and a head its r at the end.
+template <typename T, int D, int kVec, bool kNorm>
+UT_DEV void forward_part(const Lane<T, D>& me, const T* src, T* dst, int heads, int s, int end, const float* wt,
+                         const QkNormParams& p) {
+  using L = Lane<T, D>;
+  if (s >= end) return;
+  float wc[L::kVals], ws[L::kVals];  // w cos, w sin
+  bool ready = false;
+  for (; s < end; s += kVec) {
+    uint4 w[kVec];
+#pragma unroll
+    for (int j = 0; j < kVec; ++j) {
+      const int h = (s + j) * L::kHeads + me.group;
+      w[j] = make_uint4(0, 0, 0, 0);
+      if (s + j < end && h < heads) w[j] = *reinterpret_cast<const uint4*>(src + h * D + me.col);
+    }
+    if (kNorm && !ready) {  // while the loads fly
+      float v[L::kVals];
+      me.weights(wt, v);
+#pragma unroll
+      for (int e = 0; e < L::kVals; ++e) {
+        wc[e] = v[e] * me.cs[e / 2];
+        ws[e] = v[e] * me.sn[e / 2];
+      }
+      ready = true;
+    }
+    if constexpr (kNorm) {
+#pragma unroll
+      for (int j = 0; j < kVec; ++j) {
+        float v[L::kVals], sum = 0.f;
+        unpack<T>(w[j], v);
+#pragma unroll
+        for (int e = 0; e < L::kVals; ++e) sum = fmaf(v[e], v[e], sum);
+        const float r = rsqrtf(head_sum<L::kLanes>(sum) * (1.f / D) + p.eps);
+#pragma unroll
+        for (int e = 0; e < L::kVals; e += 2) {
+          const float x = v[e] * r, y = v[e + 1] * r;
+          v[e] = fmaf(x, wc[e], -y * ws[e + 1]);
+          v[e + 1] = fmaf(x, ws[e], y * wc[e + 1]);
+        }
+        w[j] = pack<T>(v);
+      }
+    }
+    if (!dst) continue;
+#pragma unroll
+    for (int j = 0; j < kVec; ++j) {
+      const int h = (s + j) * L::kHeads + me.group;
+      if (s + j < end && h < heads) *reinterpret_cast<uint4*>(dst + h * D + me.col) = w[j];
+    }
   }
-  // head of a lane's group at step s, -1 where there is none
-  UT_DEV int head(const QkNormParams& p, int s, int group) const {
-    const int h = (s < q ? s : (s < k ? s - q : s - k)) * kHeads + group;
-    return h < (s < q ? p.H : p.Hk) ? h : -1;
-  }
-};
+}
 
 // grid: warps take (token, part of its steps)
 template <typename T, int D, int kVec>
-__global__ void __launch_bounds__(kQnThreads) qknorm_fwd_kernel(const __grid_constant__ QkNormParams p, int parts,
-                                                                int per) {
+__global__ void __launch_bounds__(kQnThreads, 3) qknorm_fwd_kernel(const __grid_constant__ QkNormParams p, int parts,
+                                                                   int per) {
   using L = Lane<T, D>;
   const int lane = threadIdx.x & 31;
   L me;
   me.init(p, lane);
-  const Steps<L::kHeads> st(p, p.vo != nullptr);
+  const int nq = (p.H + L::kHeads - 1) / L::kHeads, nk = (p.Hk + L::kHeads - 1) / L::kHeads;  // steps
   const int64_t warps = (int64_t)gridDim.x * kQnWarps, units = p.n * parts;
-  for (int64_t u = (int64_t)blockIdx.x * kQnWarps + (threadIdx.x >> 5); u < units; u += warps) {
+  int64_t u = (int64_t)blockIdx.x * kQnWarps + (threadIdx.x >> 5);
+  auto pos_of = [&](int64_t unit) -> int32_t {
+    const int64_t row = unit / parts;
+    return p.pos ? p.pos[row] : (int32_t)row;
+  };
+  int32_t next = u < units ? pos_of(u) : 0;
+  for (; u < units; u += warps) {
     const int64_t row = u / parts;
-    const int s0 = (int)(u - row * parts) * per, s1 = min(st.all, s0 + per);
+    const int s0 = (int)(u - row * parts) * per, s1 = s0 + per;
+    const int32_t pos = next;
+    if (u + warps < units) next = pos_of(u + warps);  // a token ahead
     int64_t to = row;  // of K and V
     bool keep = true;
     if (p.rows) {
@@ -138,116 +183,91 @@ __global__ void __launch_bounds__(kQnThreads) qknorm_fwd_kernel(const __grid_con
       keep = to >= 0 && to < p.cache_rows;
       if (to >= p.cache_rows && lane == 0) set_status(p.status, UT_ERR_INVALID_ARG);
     }
-    const int32_t pos = p.pos ? p.pos[row] : (int32_t)row;
-    bool turned = false;
-    for (int s = s0; s < s1; s += kVec) {
-      uint4 w[kVec];
+    if (s0 < nq + nk) me.turn_to(p, pos);
+    forward_part<T, D, kVec, true>(me, static_cast<const T*>(p.q) + row * p.qs, static_cast<T*>(p.qo) + row * p.qos, p.H,
+                                   s0, min(s1, nq), p.wq, p);
+    forward_part<T, D, kVec, true>(me, static_cast<const T*>(p.k) + row * p.ks,
+                                   keep ? static_cast<T*>(p.ko) + to * p.kos : nullptr, p.Hk, max(s0 - nq, 0),
+                                   min(s1 - nq, nk), p.wk, p);
+    if (p.vo)
+      forward_part<T, D, kVec, false>(me, static_cast<const T*>(p.v) + row * p.vs,
+                                      keep ? static_cast<T*>(p.vo) + to * p.vos : nullptr, p.Hk, max(s0 - nq - nk, 0),
+                                      min(s1 - nq - nk, nk), nullptr, p);
+  }
+}
+
+// The heads of one tensor of a token, backward; dw += its terms.
+template <typename T, int D, int kVec>
+UT_DEV void backward_part(const Lane<T, D>& me, const T* src, const T* grad, T* dst, int heads, const float* wt,
+                          float (&dw)[Vec<T>::kVals], const QkNormParams& p) {
+  using L = Lane<T, D>;
+  const int end = (heads + L::kHeads - 1) / L::kHeads;
+  float wv[L::kVals];
+  me.weights(wt, wv);
+  for (int s = 0; s < end; s += kVec) {
+    uint4 w[kVec], dy[kVec];
 #pragma unroll
-      for (int j = 0; j < kVec; ++j) {
-        const int x = s + j, h = x < s1 ? st.head(p, x, me.group) : -1;
-        w[j] = make_uint4(0, 0, 0, 0);
-        if (h < 0) continue;
-        const T* src = x < st.q ? static_cast<const T*>(p.q) + row * p.qs
-                                : (x < st.k ? static_cast<const T*>(p.k) + row * p.ks
-                                            : static_cast<const T*>(p.v) + row * p.vs);
-        w[j] = *reinterpret_cast<const uint4*>(src + (int64_t)h * D + me.col);
+    for (int j = 0; j < kVec; ++j) {
+      const int h = (s + j) * L::kHeads + me.group;
+      w[j] = dy[j] = make_uint4(0, 0, 0, 0);
+      if (s + j < end && h < heads) {
+        w[j] = *reinterpret_cast<const uint4*>(src + h * D + me.col);
+        dy[j] = *reinterpret_cast<const uint4*>(grad + h * D + me.col);
       }
-      if (!turned) me.turn_to(p, pos);  // while the loads fly
-      turned = true;
+    }
 #pragma unroll
-      for (int j = 0; j < kVec; ++j) {
-        const int x = s + j;
-        if (x >= s1) break;  // the same in all lanes
-        const int h = st.head(p, x, me.group);
-        const bool is_q = x < st.q;
-        if (x < st.k) {
-          float v[L::kVals], sum = 0.f;
-          unpack<T>(w[j], v);
+    for (int j = 0; j < kVec; ++j) {
+      float v[L::kVals], g[L::kVals], ss = 0.f, sg = 0.f;
+      unpack<T>(w[j], v);
+      unpack<T>(dy[j], g);
 #pragma unroll
-          for (int e = 0; e < L::kVals; ++e) sum = fmaf(v[e], v[e], sum);
-          const float r = rsqrtf(head_sum<L::kLanes>(sum) * (1.f / D) + p.eps);
-#pragma unroll
-          for (int e = 0; e < L::kVals; ++e) v[e] *= r * (is_q ? me.wq[e] : me.wk[e]);
-#pragma unroll
-          for (int e = 0; e < L::kPairs; ++e) {
-            const float a = v[2 * e], b = v[2 * e + 1];
-            v[2 * e] = fmaf(a, me.cs[e], -b * me.sn[e]);
-            v[2 * e + 1] = fmaf(a, me.sn[e], b * me.cs[e]);
-          }
-          w[j] = pack<T>(v);
-        }
-        if (h < 0 || !(is_q || keep)) continue;
-        T* dst = is_q ? static_cast<T*>(p.qo) + row * p.qos
-                      : (x < st.k ? static_cast<T*>(p.ko) + to * p.kos : static_cast<T*>(p.vo) + to * p.vos);
-        *reinterpret_cast<uint4*>(dst + (int64_t)h * D + me.col) = w[j];
+      for (int e = 0; e < L::kPairs; ++e) {
+        const float a = g[2 * e], b = g[2 * e + 1];
+        g[2 * e] = fmaf(a, me.cs[e], b * me.sn[e]);
+        g[2 * e + 1] = fmaf(b, me.cs[e], -a * me.sn[e]);
       }
+      float t[L::kVals];  // g x
+#pragma unroll
+      for (int e = 0; e < L::kVals; ++e) {
+        t[e] = g[e] * v[e];
+        ss = fmaf(v[e], v[e], ss);
+        sg = fmaf(t[e], wv[e], sg);
+      }
+      const float r = rsqrtf(head_sum<L::kLanes>(ss) * (1.f / D) + p.eps);
+      const float c = head_sum<L::kLanes>(sg) * (1.f / D) * r * r;  // mean(g w xh) r
+#pragma unroll
+      for (int e = 0; e < L::kVals; ++e) {
+        dw[e] = fmaf(t[e], r, dw[e]);
+        v[e] = r * fmaf(-v[e], c, g[e] * wv[e]);
+      }
+      const int h = (s + j) * L::kHeads + me.group;
+      if (s + j < end && h < heads) *reinterpret_cast<uint4*>(dst + h * D + me.col) = pack<T>(v);
     }
   }
 }
 
 template <typename T, int D, int kVec>
-__global__ void __launch_bounds__(kQnThreads) qknorm_bwd_kernel(const __grid_constant__ QkNormParams p) {
+__global__ void __launch_bounds__(kQnThreads, kQnBlocksPerSm) qknorm_bwd_kernel(const __grid_constant__ QkNormParams p) {
   using L = Lane<T, D>;
   __shared__ float sums[kQnWarps * L::kHeads][2][D];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   grid_next();
   L me;
   me.init(p, lane);
-  const Steps<L::kHeads> st(p, false);
   float dwq[L::kVals], dwk[L::kVals];
 #pragma unroll
   for (int e = 0; e < L::kVals; ++e) dwq[e] = dwk[e] = 0.f;
   const int64_t warps = (int64_t)gridDim.x * kQnWarps;
-  for (int64_t row = (int64_t)blockIdx.x * kQnWarps + warp; row < p.n; row += warps) {
-    const int32_t pos = p.pos ? p.pos[row] : (int32_t)row;
-    for (int s = 0; s < st.all; s += kVec) {
-      uint4 w[kVec], dy[kVec];
-#pragma unroll
-      for (int j = 0; j < kVec; ++j) {
-        const int x = s + j, h = x < st.all ? st.head(p, x, me.group) : -1;
-        w[j] = dy[j] = make_uint4(0, 0, 0, 0);
-        if (h < 0) continue;
-        const bool is_q = x < st.q;
-        const int64_t at = (int64_t)h * D + me.col;
-        w[j] = *reinterpret_cast<const uint4*>((is_q ? static_cast<const T*>(p.q) + row * p.qs
-                                                     : static_cast<const T*>(p.k) + row * p.ks) + at);
-        dy[j] = *reinterpret_cast<const uint4*>((is_q ? static_cast<const T*>(p.dqo) + row * p.dqos
-                                                      : static_cast<const T*>(p.dko) + row * p.dkos) + at);
-      }
-      if (s == 0) me.turn_to(p, pos);
-#pragma unroll
-      for (int j = 0; j < kVec; ++j) {
-        const int x = s + j;
-        if (x >= st.all) break;
-        const int h = st.head(p, x, me.group);
-        const bool is_q = x < st.q;
-        float v[L::kVals], g[L::kVals], ss = 0.f, sg = 0.f;
-        unpack<T>(w[j], v);
-        unpack<T>(dy[j], g);
-#pragma unroll
-        for (int e = 0; e < L::kPairs; ++e) {
-          const float a = g[2 * e], b = g[2 * e + 1];
-          g[2 * e] = fmaf(a, me.cs[e], b * me.sn[e]);
-          g[2 * e + 1] = fmaf(b, me.cs[e], -a * me.sn[e]);
-        }
-#pragma unroll
-        for (int e = 0; e < L::kVals; ++e) {
-          ss = fmaf(v[e], v[e], ss);
-          sg = fmaf(g[e] * (is_q ? me.wq[e] : me.wk[e]), v[e], sg);
-        }
-        const float r = rsqrtf(head_sum<L::kLanes>(ss) * (1.f / D) + p.eps);
-        const float c = head_sum<L::kLanes>(sg) * (1.f / D) * r * r;  // mean(g w xh) r
-#pragma unroll
-        for (int e = 0; e < L::kVals; ++e) {
-          if (is_q) dwq[e] = fmaf(g[e], v[e] * r, dwq[e]);
-          else dwk[e] = fmaf(g[e], v[e] * r, dwk[e]);
-          v[e] = r * fmaf(-v[e], c, g[e] * (is_q ? me.wq[e] : me.wk[e]));
-        }
-        if (h < 0) continue;
-        T* dst = is_q ? static_cast<T*>(p.qo) + row * p.qos : static_cast<T*>(p.ko) + row * p.kos;
-        *reinterpret_cast<uint4*>(dst + (int64_t)h * D + me.col) = pack<T>(v);
-      }
-    }
+  int64_t row = (int64_t)blockIdx.x * kQnWarps + warp;
+  auto pos_of = [&](int64_t at) -> int32_t { return p.pos ? p.pos[at] : (int32_t)at; };
+  int32_t next = row < p.n ? pos_of(row) : 0;
+  for (; row < p.n; row += warps) {
+    me.turn_to(p, next);
+    if (row + warps < p.n) next = pos_of(row + warps);  // a token ahead
+    backward_part<T, D, kVec>(me, static_cast<const T*>(p.q) + row * p.qs, static_cast<const T*>(p.dqo) + row * p.dqos,
+                              static_cast<T*>(p.qo) + row * p.qos, p.H, p.wq, dwq, p);
+    backward_part<T, D, kVec>(me, static_cast<const T*>(p.k) + row * p.ks, static_cast<const T*>(p.dko) + row * p.dkos,
+                              static_cast<T*>(p.ko) + row * p.kos, p.Hk, p.wk, dwk, p);
   }
 #pragma unroll
   for (int e = 0; e < L::kVals; ++e) {
@@ -279,18 +299,16 @@ __global__ void __launch_bounds__(512) qknorm_dw_kernel(const float* part, int b
   if (out) out[col < d ? col : col - d] = a;
 }
 
-// Steps in flight: 6 forward (of 12 for 24 heads of 128 in bf16), 3 backward,
-// where a step is two vectors.
 template <typename T, int D>
 cudaError_t fwd(const QkNormParams& p, cudaStream_t s) {
-  constexpr int kHeads = 32 / (D / Vec<T>::kVals), kVec = 6;
+  constexpr int kHeads = 32 / (D / Vec<T>::kVals), kVec = 4;
   const int one = (p.Hk + kHeads - 1) / kHeads, all = (p.H + kHeads - 1) / kHeads + one * (p.vo ? 2 : 1);
   // a whole token a warp where that fills 16 warps an SM, else fewer steps each
   int64_t parts = ((int64_t)p.sms * 16 + p.n - 1) / p.n;
   if (parts > all) parts = all;
   const int per = (int)((all + parts - 1) / parts);
   parts = (all + per - 1) / per;
-  const int64_t want = (p.n * parts + kQnWarps - 1) / kQnWarps, most = (int64_t)p.sms * 8;
+  const int64_t want = (p.n * parts + kQnWarps - 1) / kQnWarps, most = (int64_t)p.sms * 6;
   qknorm_fwd_kernel<T, D, kVec><<<(unsigned)(want < most ? want : most), kQnThreads, 0, s>>>(p, (int)parts, per);
   return cudaGetLastError();
 }
@@ -299,7 +317,7 @@ template <typename T, int D>
 cudaError_t bwd(const QkNormParams& p, cudaStream_t s) {
   const int64_t blocks = qknorm_bwd_blocks(p.n, p.sms);
   if (blocks > 0) {
-    qknorm_bwd_kernel<T, D, 3><<<(unsigned)blocks, kQnThreads, 0, s>>>(p);
+    qknorm_bwd_kernel<T, D, 2><<<(unsigned)blocks, kQnThreads, 0, s>>>(p);
     const cudaError_t e = cudaGetLastError();
     if (e != cudaSuccess) return e;
   }

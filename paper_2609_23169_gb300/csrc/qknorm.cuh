@@ -28,7 +28,7 @@ struct QkNormParams {
   int sms;
 };
 
-constexpr int kQnBlocksPerSm = 4;                // of the backward, whose blocks leave partial sums
+constexpr int kQnBlocksPerSm = 3;                // of the backward, whose blocks leave partial sums
 inline int64_t qknorm_bwd_blocks(int64_t n, int sms) {
   const int64_t want = (n + 7) / 8, most = (int64_t)sms * kQnBlocksPerSm;
   return want < most ? want : most;
