@@ -23,6 +23,8 @@
 // memory, then over blocks by a second kernel, always in the same order.
 #include <math.h>
 
+#include <type_traits>
+
 #include "common.cuh"
 #include "kernels.h"
 #include "qknorm.cuh"
@@ -101,79 +103,88 @@ struct Lane {
   }
 };
 
-// Steps [s, end) of one tensor of a token, kHeads heads each: y = R (x r w), or
-// a copy.  With the weights in the rotation, a w cos and so on, a pair takes four
-// multiplications and a head its r at the end.
-template <typename T, int D, int kVec, bool kNorm>
-UT_DEV void forward_part(const Lane<T, D>& me, const T* src, T* dst, int heads, int s, int end, const float* wt,
-                         const QkNormParams& p) {
-  using L = Lane<T, D>;
-  if (s >= end) return;
-  float wc[L::kVals], ws[L::kVals];  // w cos, w sin
-  bool ready = false;
-  for (; s < end; s += kVec) {
-    uint4 w[kVec];
-#pragma unroll
-    for (int j = 0; j < kVec; ++j) {
-      const int h = (s + j) * L::kHeads + me.group;
-      w[j] = make_uint4(0, 0, 0, 0);
-      if (s + j < end && h < heads) w[j] = *reinterpret_cast<const uint4*>(src + h * D + me.col);
-    }
-    if (kNorm && !ready) {  // while the loads fly
-      float v[L::kVals];
-      me.weights(wt, v);
-#pragma unroll
-      for (int e = 0; e < L::kVals; ++e) {
-        wc[e] = v[e] * me.cs[e / 2];
-        ws[e] = v[e] * me.sn[e / 2];
-      }
-      ready = true;
-    }
-    if constexpr (kNorm) {
-#pragma unroll
-      for (int j = 0; j < kVec; ++j) {
-        float v[L::kVals], sum = 0.f;
-        unpack<T>(w[j], v);
-#pragma unroll
-        for (int e = 0; e < L::kVals; ++e) sum = fmaf(v[e], v[e], sum);
-        const float r = rsqrtf(head_sum<L::kLanes>(sum) * (1.f / D) + p.eps);
-#pragma unroll
-        for (int e = 0; e < L::kVals; e += 2) {
-          const float x = v[e] * r, y = v[e + 1] * r;
-          v[e] = fmaf(x, wc[e], -y * ws[e + 1]);
-          v[e + 1] = fmaf(x, ws[e], y * wc[e + 1]);
-        }
-        w[j] = pack<T>(v);
-      }
-    }
-    if (!dst) continue;
-#pragma unroll
-    for (int j = 0; j < kVec; ++j) {
-      const int h = (s + j) * L::kHeads + me.group;
-      if (s + j < end && h < heads) *reinterpret_cast<uint4*>(dst + h * D + me.col) = w[j];
-    }
-  }
+// The steps of a token: kHeads heads each, of Q, then of K, then of V.
+struct Steps {
+  int q, k, all;  // where K's begin, V's begin, the end
+};
+template <int kHeads>
+UT_DEV Steps steps_of(const QkNormParams& p, bool with_v) {
+  const int q = (p.H + kHeads - 1) / kHeads, k = (p.Hk + kHeads - 1) / kHeads;
+  return Steps{q, q + k, q + k + (with_v ? k : 0)};
 }
 
-// grid: warps take (token, part of its steps)
-template <typename T, int D, int kVec>
-__global__ void __launch_bounds__(kQnThreads, 3) qknorm_fwd_kernel(const __grid_constant__ QkNormParams p, int parts,
-                                                                   int per) {
+// What a warp reads is asked for kAhead steps before it is used, through shared
+// memory, where it costs no registers; each lane reads what it asked for itself.
+template <int kSlots>
+struct Ahead {
+  static constexpr int kAhead = kSlots - 1;  // a slot is filled again a step after it was read
+  UT_DEV static void copy(uint4* dst, const void* src, bool there) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem_u32(dst)), "l"(src), "r"(there ? 16 : 0) : "memory");
+  }
+  UT_DEV static void commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+  template <int kPending>
+  UT_DEV static void wait() {
+    asm volatile("cp.async.wait_group %0;" ::"n"(kPending) : "memory");
+  }
+};
+
+constexpr int kFwdSlots = 8, kBwdSlots = 6;
+
+// Warps take units: a token, or `per` of its steps.
+template <typename T, int D>
+__global__ void __launch_bounds__(kQnThreads, kQnFwdBlocksPerSm) qknorm_fwd_kernel(const __grid_constant__ QkNormParams p,
+                                                                                   int parts, int per) {
   using L = Lane<T, D>;
-  const int lane = threadIdx.x & 31;
+  using A = Ahead<kFwdSlots>;
+  constexpr int kTwo = 2;  // steps at a time
+  __shared__ uint4 slots[kQnWarps][kFwdSlots][32];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   L me;
   me.init(p, lane);
-  const int nq = (p.H + L::kHeads - 1) / L::kHeads, nk = (p.Hk + L::kHeads - 1) / L::kHeads;  // steps
+  const Steps st = steps_of<L::kHeads>(p, p.vo != nullptr);
   const int64_t warps = (int64_t)gridDim.x * kQnWarps, units = p.n * parts;
-  int64_t u = (int64_t)blockIdx.x * kQnWarps + (threadIdx.x >> 5);
+  const int64_t first = (int64_t)blockIdx.x * kQnWarps + warp;
+  uint4* const mine = &slots[warp][0][lane];
+  int64_t au = first;  // unit and step to ask for next
+  int as = 0, aend = 0, at = 0;
+  const T *aq = nullptr, *ak = nullptr, *av = nullptr;
+  auto begin = [&]() {
+    if (au >= units) return;
+    const int64_t row = au / parts;
+    as = (int)(au - row * parts) * per;
+    aend = min(st.all, as + per);
+    aq = static_cast<const T*>(p.q) + row * p.qs + me.col;
+    ak = static_cast<const T*>(p.k) + row * p.ks + me.col;
+    av = static_cast<const T*>(p.v) + row * p.vs + me.col;
+  };
+  auto ask = [&]() {
+    if (au < units) {
+      const bool is_q = as < st.q;
+      const int h = (is_q ? as : (as < st.k ? as - st.q : as - st.k)) * L::kHeads + me.group;
+      const T* src = is_q ? aq : (as < st.k ? ak : av);
+      const bool there = h < (is_q ? p.H : p.Hk);
+      A::copy(mine + (at & (kFwdSlots - 1)) * 32, there ? src + h * D : src, there);
+      if (++as == aend) {
+        au += warps;
+        begin();
+      }
+    }
+    ++at;
+    A::commit();
+  };
+  begin();
+#pragma unroll
+  for (int i = 0; i < A::kAhead - 1; ++i) ask();
   auto pos_of = [&](int64_t unit) -> int32_t {
     const int64_t row = unit / parts;
     return p.pos ? p.pos[row] : (int32_t)row;
   };
-  int32_t next = u < units ? pos_of(u) : 0;
-  for (; u < units; u += warps) {
+  int32_t next = first < units ? pos_of(first) : 0;
+  int use = 0;  // steps used
+  for (int64_t u = first; u < units; u += warps) {
     const int64_t row = u / parts;
-    const int s0 = (int)(u - row * parts) * per, s1 = s0 + per;
+    int s = (int)(u - row * parts) * per;
+    const int s1 = min(st.all, s + per);
     const int32_t pos = next;
     if (u + warps < units) next = pos_of(u + warps);  // a token ahead
     int64_t to = row;  // of K and V
@@ -183,92 +194,144 @@ __global__ void __launch_bounds__(kQnThreads, 3) qknorm_fwd_kernel(const __grid_
       keep = to >= 0 && to < p.cache_rows;
       if (to >= p.cache_rows && lane == 0) set_status(p.status, UT_ERR_INVALID_ARG);
     }
-    if (s0 < nq + nk) me.turn_to(p, pos);
-    forward_part<T, D, kVec, true>(me, static_cast<const T*>(p.q) + row * p.qs, static_cast<T*>(p.qo) + row * p.qos, p.H,
-                                   s0, min(s1, nq), p.wq, p);
-    forward_part<T, D, kVec, true>(me, static_cast<const T*>(p.k) + row * p.ks,
-                                   keep ? static_cast<T*>(p.ko) + to * p.kos : nullptr, p.Hk, max(s0 - nq, 0),
-                                   min(s1 - nq, nk), p.wk, p);
-    if (p.vo)
-      forward_part<T, D, kVec, false>(me, static_cast<const T*>(p.v) + row * p.vs,
-                                      keep ? static_cast<T*>(p.vo) + to * p.vos : nullptr, p.Hk, max(s0 - nq - nk, 0),
-                                      min(s1 - nq - nk, nk), nullptr, p);
+    if (s < st.k) me.turn_to(p, pos);
+    // one tensor's steps up to `end`: y = R (x r w), or a copy.  With the weights in
+    // the rotation (w cos and so on), a pair takes four multiplications and its r.
+    auto part = [&](auto norm, T* dst, int heads, int begin, int end, const float* wt) {
+      constexpr bool kNorm = decltype(norm)::value;
+      if (s >= end) return;
+      float wc[L::kVals], ws[L::kVals];
+      if constexpr (kNorm) {
+        me.weights(wt, wc);
+#pragma unroll
+        for (int e = 0; e < L::kVals; ++e) {
+          ws[e] = wc[e] * me.sn[e / 2];
+          wc[e] *= me.cs[e / 2];
+        }
+      }
+      for (; s < end; s += kTwo) {
+        const int some = min(kTwo, end - s);
+        ask();
+        if (some == kTwo) ask();
+        A::template wait<A::kAhead - 1>();  // all but the last kAhead - 1 asked for: those of now are there
+        uint4 w[kTwo];
+#pragma unroll
+        for (int j = 0; j < kTwo; ++j) w[j] = mine[((use + j) & (kFwdSlots - 1)) * 32];
+        use += some;
+#pragma unroll
+        for (int j = 0; j < kTwo; ++j) {
+          if constexpr (kNorm) {
+            float v[L::kVals], sum = 0.f;
+            unpack<T>(w[j], v);
+#pragma unroll
+            for (int e = 0; e < L::kVals; ++e) sum = fmaf(v[e], v[e], sum);
+            const float r = rsqrtf(head_sum<L::kLanes>(sum) * (1.f / D) + p.eps);
+#pragma unroll
+            for (int e = 0; e < L::kVals; e += 2) {
+              const float x = v[e] * r, y = v[e + 1] * r;
+              v[e] = fmaf(x, wc[e], -y * ws[e + 1]);
+              v[e + 1] = fmaf(x, ws[e], y * wc[e + 1]);
+            }
+            w[j] = pack<T>(v);
+          }
+          const int h = (s + j - begin) * L::kHeads + me.group;
+          if (dst && j < some && h < heads) *reinterpret_cast<uint4*>(dst + h * D + me.col) = w[j];
+        }
+      }
+      s = end;
+    };
+    part(std::true_type{}, static_cast<T*>(p.qo) + row * p.qos, p.H, 0, min(s1, st.q), p.wq);
+    part(std::true_type{}, keep ? static_cast<T*>(p.ko) + to * p.kos : nullptr, p.Hk, st.q, min(s1, st.k), p.wk);
+    part(std::false_type{}, keep && p.vo ? static_cast<T*>(p.vo) + to * p.vos : nullptr, p.Hk, st.k, s1, nullptr);
   }
+  A::template wait<0>();
 }
 
-// The heads of one tensor of a token, backward; dw += its terms.
-template <typename T, int D, int kVec>
-UT_DEV void backward_part(const Lane<T, D>& me, const T* src, const T* grad, T* dst, int heads, const float* wt,
-                          float (&dw)[Vec<T>::kVals], const QkNormParams& p) {
-  using L = Lane<T, D>;
-  const int end = (heads + L::kHeads - 1) / L::kHeads;
-  float wv[L::kVals];
-  me.weights(wt, wv);
-  for (int s = 0; s < end; s += kVec) {
-    uint4 w[kVec], dy[kVec];
-#pragma unroll
-    for (int j = 0; j < kVec; ++j) {
-      const int h = (s + j) * L::kHeads + me.group;
-      w[j] = dy[j] = make_uint4(0, 0, 0, 0);
-      if (s + j < end && h < heads) {
-        w[j] = *reinterpret_cast<const uint4*>(src + h * D + me.col);
-        dy[j] = *reinterpret_cast<const uint4*>(grad + h * D + me.col);
-      }
-    }
-#pragma unroll
-    for (int j = 0; j < kVec; ++j) {
-      float v[L::kVals], g[L::kVals], ss = 0.f, sg = 0.f;
-      unpack<T>(w[j], v);
-      unpack<T>(dy[j], g);
-#pragma unroll
-      for (int e = 0; e < L::kPairs; ++e) {
-        const float a = g[2 * e], b = g[2 * e + 1];
-        g[2 * e] = fmaf(a, me.cs[e], b * me.sn[e]);
-        g[2 * e + 1] = fmaf(b, me.cs[e], -a * me.sn[e]);
-      }
-      float t[L::kVals];  // g x
-#pragma unroll
-      for (int e = 0; e < L::kVals; ++e) {
-        t[e] = g[e] * v[e];
-        ss = fmaf(v[e], v[e], ss);
-        sg = fmaf(t[e], wv[e], sg);
-      }
-      const float r = rsqrtf(head_sum<L::kLanes>(ss) * (1.f / D) + p.eps);
-      const float c = head_sum<L::kLanes>(sg) * (1.f / D) * r * r;  // mean(g w xh) r
-#pragma unroll
-      for (int e = 0; e < L::kVals; ++e) {
-        dw[e] = fmaf(t[e], r, dw[e]);
-        v[e] = r * fmaf(-v[e], c, g[e] * wv[e]);
-      }
-      const int h = (s + j) * L::kHeads + me.group;
-      if (s + j < end && h < heads) *reinterpret_cast<uint4*>(dst + h * D + me.col) = pack<T>(v);
-    }
-  }
-}
-
-template <typename T, int D, int kVec>
+template <typename T, int D>
 __global__ void __launch_bounds__(kQnThreads, kQnBlocksPerSm) qknorm_bwd_kernel(const __grid_constant__ QkNormParams p) {
   using L = Lane<T, D>;
-  __shared__ float sums[kQnWarps * L::kHeads][2][D];
+  using A = Ahead<kBwdSlots>;
+  extern __shared__ __align__(16) uint8_t smem[];
+  auto& slots = *reinterpret_cast<uint4(*)[kQnWarps][kBwdSlots][2][32]>(smem);
+  auto& sums = *reinterpret_cast<float(*)[kQnWarps * L::kHeads][2][D]>(smem);
+  static_assert(sizeof(sums) <= sizeof(slots), "the sums take the slots' place");
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   grid_next();
   L me;
   me.init(p, lane);
+  const Steps st = steps_of<L::kHeads>(p, false);
   float dwq[L::kVals], dwk[L::kVals];
 #pragma unroll
   for (int e = 0; e < L::kVals; ++e) dwq[e] = dwk[e] = 0.f;
-  const int64_t warps = (int64_t)gridDim.x * kQnWarps;
-  int64_t row = (int64_t)blockIdx.x * kQnWarps + warp;
-  auto pos_of = [&](int64_t at) -> int32_t { return p.pos ? p.pos[at] : (int32_t)at; };
-  int32_t next = row < p.n ? pos_of(row) : 0;
-  for (; row < p.n; row += warps) {
+  const int64_t warps = (int64_t)gridDim.x * kQnWarps, first = (int64_t)blockIdx.x * kQnWarps + warp;
+  uint4* const mine = &slots[warp][0][0][lane];
+  int64_t arow = first;  // row and step to ask for next
+  int as = 0, at = 0;
+  auto ask = [&]() {
+    if (arow < p.n) {
+      const bool is_q = as < st.q;
+      const int h = (is_q ? as : as - st.q) * L::kHeads + me.group;
+      const bool there = h < (is_q ? p.H : p.Hk);
+      const int off = there ? h * D + me.col : me.col;
+      const T* x = (is_q ? static_cast<const T*>(p.q) + arow * p.qs : static_cast<const T*>(p.k) + arow * p.ks) + off;
+      const T* g = (is_q ? static_cast<const T*>(p.dqo) + arow * p.dqos : static_cast<const T*>(p.dko) + arow * p.dkos) + off;
+      A::copy(mine + at * 64, x, there);
+      A::copy(mine + at * 64 + 32, g, there);
+      if (++as == st.all) {
+        as = 0;
+        arow += warps;
+      }
+    }
+    at = at + 1 == kBwdSlots ? 0 : at + 1;
+    A::commit();
+  };
+#pragma unroll
+  for (int i = 0; i < A::kAhead; ++i) ask();
+  auto pos_of = [&](int64_t row) -> int32_t { return p.pos ? p.pos[row] : (int32_t)row; };
+  int32_t next = first < p.n ? pos_of(first) : 0;
+  int use = 0;
+  for (int64_t row = first; row < p.n; row += warps) {
     me.turn_to(p, next);
     if (row + warps < p.n) next = pos_of(row + warps);  // a token ahead
-    backward_part<T, D, kVec>(me, static_cast<const T*>(p.q) + row * p.qs, static_cast<const T*>(p.dqo) + row * p.dqos,
-                              static_cast<T*>(p.qo) + row * p.qos, p.H, p.wq, dwq, p);
-    backward_part<T, D, kVec>(me, static_cast<const T*>(p.k) + row * p.ks, static_cast<const T*>(p.dko) + row * p.dkos,
-                              static_cast<T*>(p.ko) + row * p.kos, p.Hk, p.wk, dwk, p);
+    auto part = [&](T* dst, int heads, const float* wt, float(&dw)[L::kVals]) {
+      float wv[L::kVals];
+      me.weights(wt, wv);
+      for (int h = me.group; h - me.group < heads; h += L::kHeads) {
+        A::template wait<A::kAhead - 1>();
+        const uint4 w = mine[use * 64], dy = mine[use * 64 + 32];
+        use = use + 1 == kBwdSlots ? 0 : use + 1;
+        float v[L::kVals], g[L::kVals], ss = 0.f, sg = 0.f;
+        unpack<T>(w, v);
+        unpack<T>(dy, g);
+#pragma unroll
+        for (int e = 0; e < L::kPairs; ++e) {
+          const float a = g[2 * e], b = g[2 * e + 1];
+          g[2 * e] = fmaf(a, me.cs[e], b * me.sn[e]);
+          g[2 * e + 1] = fmaf(b, me.cs[e], -a * me.sn[e]);
+        }
+        float t[L::kVals];  // g x
+#pragma unroll
+        for (int e = 0; e < L::kVals; ++e) {
+          t[e] = g[e] * v[e];
+          ss = fmaf(v[e], v[e], ss);
+          sg = fmaf(t[e], wv[e], sg);
+        }
+        ask();
+        const float r = rsqrtf(head_sum<L::kLanes>(ss) * (1.f / D) + p.eps);
+        const float c = head_sum<L::kLanes>(sg) * (1.f / D) * r * r;  // mean(g w xh) r
+#pragma unroll
+        for (int e = 0; e < L::kVals; ++e) {
+          dw[e] = fmaf(t[e], r, dw[e]);
+          v[e] = r * fmaf(-v[e], c, g[e] * wv[e]);
+        }
+        if (h < heads) *reinterpret_cast<uint4*>(dst + h * D + me.col) = pack<T>(v);
+      }
+    };
+    part(static_cast<T*>(p.qo) + row * p.qos, p.H, p.wq, dwq);
+    part(static_cast<T*>(p.ko) + row * p.kos, p.Hk, p.wk, dwk);
   }
+  A::template wait<0>();
+  __syncthreads();
 #pragma unroll
   for (int e = 0; e < L::kVals; ++e) {
     sums[warp * L::kHeads + me.group][0][me.col + e] = dwq[e];
@@ -282,34 +345,34 @@ __global__ void __launch_bounds__(kQnThreads, kQnBlocksPerSm) qknorm_bwd_kernel(
   }
 }
 
-// dw = the sum of the blocks' parts; a block 32 columns, 16 threads a column
-__global__ void __launch_bounds__(512) qknorm_dw_kernel(const float* part, int blocks, int d, float* dwq, float* dwk) {
-  __shared__ float sums[16][32];
+// dw = the sum of the blocks' parts; a block 32 columns, 32 threads a column
+__global__ void __launch_bounds__(1024) qknorm_dw_kernel(const float* part, int blocks, int d, float* dwq, float* dwk) {
+  __shared__ float sums[32][32];
   const int col = blockIdx.x * 32 + (threadIdx.x & 31), i0 = threadIdx.x >> 5;
   grid_wait();
   float a = 0.f;
-#pragma unroll 8
-  for (int i = i0; i < blocks; i += 16) a += part[(int64_t)i * 2 * d + col];
+#pragma unroll 16
+  for (int i = i0; i < blocks; i += 32) a += part[(int64_t)i * 2 * d + col];
   sums[i0][threadIdx.x & 31] = a;
   __syncthreads();
   if (i0 > 0) return;
 #pragma unroll
-  for (int i = 1; i < 16; ++i) a += sums[i][threadIdx.x];
+  for (int i = 1; i < 32; ++i) a += sums[i][threadIdx.x];
   float* out = col < d ? dwq : dwk;
   if (out) out[col < d ? col : col - d] = a;
 }
 
 template <typename T, int D>
 cudaError_t fwd(const QkNormParams& p, cudaStream_t s) {
-  constexpr int kHeads = 32 / (D / Vec<T>::kVals), kVec = 4;
+  constexpr int kHeads = 32 / (D / Vec<T>::kVals);
   const int one = (p.Hk + kHeads - 1) / kHeads, all = (p.H + kHeads - 1) / kHeads + one * (p.vo ? 2 : 1);
-  // a whole token a warp where that fills 16 warps an SM, else fewer steps each
-  int64_t parts = ((int64_t)p.sms * 16 + p.n - 1) / p.n;
+  // a whole token a warp where that makes four of them a warp, else fewer steps each
+  int64_t parts = ((int64_t)p.sms * kQnFwdBlocksPerSm * kQnWarps * 4 + p.n - 1) / p.n;
   if (parts > all) parts = all;
   const int per = (int)((all + parts - 1) / parts);
   parts = (all + per - 1) / per;
-  const int64_t want = (p.n * parts + kQnWarps - 1) / kQnWarps, most = (int64_t)p.sms * 6;
-  qknorm_fwd_kernel<T, D, kVec><<<(unsigned)(want < most ? want : most), kQnThreads, 0, s>>>(p, (int)parts, per);
+  const int64_t want = (p.n * parts + kQnWarps - 1) / kQnWarps, most = (int64_t)p.sms * kQnFwdBlocksPerSm;
+  qknorm_fwd_kernel<T, D><<<(unsigned)(want < most ? want : most), kQnThreads, 0, s>>>(p, (int)parts, per);
   return cudaGetLastError();
 }
 
@@ -317,12 +380,15 @@ template <typename T, int D>
 cudaError_t bwd(const QkNormParams& p, cudaStream_t s) {
   const int64_t blocks = qknorm_bwd_blocks(p.n, p.sms);
   if (blocks > 0) {
-    qknorm_bwd_kernel<T, D, 2><<<(unsigned)blocks, kQnThreads, 0, s>>>(p);
-    const cudaError_t e = cudaGetLastError();
+    const int smem = kQnWarps * kBwdSlots * 2 * 32 * sizeof(uint4);
+    cudaError_t e = cudaFuncSetAttribute(qknorm_bwd_kernel<T, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    if (e != cudaSuccess) return e;
+    qknorm_bwd_kernel<T, D><<<(unsigned)blocks, kQnThreads, smem, s>>>(p);
+    e = cudaGetLastError();
     if (e != cudaSuccess) return e;
   }
   if (!p.dwq && !p.dwk) return cudaSuccess;
-  return launch_next(qknorm_dw_kernel, dim3(2 * D / 32), dim3(512), 0, s, (const float*)p.part, (int)blocks, D, p.dwq,
+  return launch_next(qknorm_dw_kernel, dim3(2 * D / 32), dim3(1024), 0, s, (const float*)p.part, (int)blocks, D, p.dwq,
                      p.dwk);
 }
 

@@ -28,7 +28,10 @@ struct QkNormParams {
   int sms;
 };
 
-constexpr int kQnBlocksPerSm = 3;                // of the backward, whose blocks leave partial sums
+// Blocks an SM (4 and 3, with fewer registers each: 2048 canvas 387 us instead of
+// 335, training step of a 1024 canvas 282 instead of 250); the backward's leave
+// partial sums.
+constexpr int kQnFwdBlocksPerSm = 3, kQnBlocksPerSm = 2;
 inline int64_t qknorm_bwd_blocks(int64_t n, int sms) {
   const int64_t want = (n + 7) / 8, most = (int64_t)sms * kQnBlocksPerSm;
   return want < most ? want : most;
