@@ -85,7 +85,8 @@ static ut_status window_problem(const ut_xattn_shape* s, const ut_window* win, b
   const bool tc = s->dtype == UT_BF16;
   const int64_t items = !tc ? wattn_simt_items(*w, backward) : (backward ? wattn_bwd_tc_items(*w) : wattn_fwd_tc_items(*w));
   if (items > INT32_MAX / 2) return UT_ERR_UNSUPPORTED;
-  w->x.nsplit = !tc ? wattn_simt_splits(*w, backward) : (backward ? 1 : wattn_fwd_tc_splits(*w));
+  w->x.nsplit = backward ? 1 : (tc ? wattn_fwd_tc_splits(*w) : wattn_simt_splits(*w));
+  if (!tc && backward) wattn_simt_parts(*w);
   return UT_OK;
 }
 
@@ -99,7 +100,7 @@ static size_t window_fwd_ws(const XattnParams& p) {
 static size_t window_bwd_ws(const WinParams& w, bool bf16) {
   const XattnParams& p = w.x;
   return up256((size_t)p.H * p.nq * sizeof(float)) +
-         (bf16 ? wattn_bwd_tc_ws(w) : 2 * up256((size_t)p.nsplit * p.nk * p.Hk * p.d * sizeof(float)));
+         (bf16 ? wattn_bwd_tc_ws(w) : 2 * up256(wattn_simt_part_rows(w) * p.Hk * p.d * sizeof(float)));
 }
 
 }  // namespace ut
@@ -253,7 +254,7 @@ ut_status ut_window_attn_bwd(const ut_xattn_shape* shape, const ut_window* windo
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   if (bf16) return status_of(launch_wattn_bwd_tc(w, at, s));
   p.part_dk = reinterpret_cast<float*>(at);
-  p.part_dv = reinterpret_cast<float*>(at + up256((size_t)p.nsplit * p.nk * p.Hk * p.d * sizeof(float)));
+  p.part_dv = reinterpret_cast<float*>(at + up256(wattn_simt_part_rows(w) * p.Hk * p.d * sizeof(float)));
   return status_of(launch_wattn_bwd_simt(w, s));
 }
 

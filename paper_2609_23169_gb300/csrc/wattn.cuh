@@ -18,6 +18,7 @@ struct WinParams {
   XattnParams x;
   const int32_t* k_len;    // [B] or NULL
   int left, right, sinks;  // at most kWinMost
+  int parts, first_parts, sb;  // of the fp32 backward: parts of a key tile, key tiles of a segment with first keys
 };
 // Most rows, and the most that left, right and sinks need to be: positions of a
 // tile's rows (a few behind the last too) plus right or less left fit 32 bits.
@@ -89,7 +90,9 @@ __device__ __forceinline__ uint32_t bits_from(int lo) { return lo <= 0 ? ~0u : (
 
 // wattn_simt.cu (fp32)
 int64_t wattn_simt_items(const WinParams& w, bool backward);
-int wattn_simt_splits(const WinParams& w, bool backward);
+int wattn_simt_splits(const WinParams& w);
+void wattn_simt_parts(WinParams& w);
+size_t wattn_simt_part_rows(const WinParams& w);
 cudaError_t launch_wattn_fwd_simt(const WinParams& w, cudaStream_t s);
 cudaError_t launch_wattn_bwd_simt(const WinParams& w, cudaStream_t s);
 // wattn_fwd_tc.cu (bf16)

@@ -180,6 +180,7 @@ __global__ void __launch_bounds__(Form<D>::kThreads, Form<D>::kCtas)
     tmem_alloc(&sm.tmem_base, F::kCols);
     tmem_relinquish();
   }
+  grid_next();  // the kernel that joins the splits
   if (blockIdx.x == 0) {
     check_cu(p.cu_q, p.B, p.nq, p.status);
     check_cu(p.cu_k, p.B, p.nk, p.status);

@@ -6,14 +6,17 @@
 //   dQ = scale dS K,  dK = scale sum dS^T Q,  dV = sum P^T dO
 //
 // Tiles of 64 rows (the G heads of a kv head of 64 / G tokens) and 64 keys, as
-// cross attention has them (xattn_simt.cuh).  A query tile goes over the blocks
-// of its two key ranges, a key tile over the query tiles that see some of its
-// keys, so work grows with rows times window.  Rows and keys that do not exist,
-// and masked keys, are staged as zeros and never enter a product; inside a
-// block a row's own limits are applied to its scores.
-// Bound by latency of the staged rows and of the shared-memory reads, two
-// blocks an SM.
+// cross attention has them (xattn_simt.cuh).  A query tile goes over the keys of
+// its two ranges one after the other, 64 at a time (a block may hold first keys
+// and window keys), a key tile over the query tiles that see some of its keys,
+// so work grows with rows times window.  Rows and keys that do not exist, and
+// masked keys, are staged as zeros and never enter a product; inside a block a
+// row's own limits are applied to its scores.  A key tile that many tokens see
+// (first keys) is split over them, at least kXsRun tiles a part, and joined.
+// Bound by latency of the staged rows and of the shared-memory reads.
 #include <math.h>
+
+#include <algorithm>
 
 #include "common.cuh"
 #include "kernels.h"
@@ -37,6 +40,39 @@ struct Limits {
   }
 };
 
+constexpr int kXsRun = 6;  // query tiles of a part
+// Parts that the `tiles` query tiles of a key tile are split into
+UT_DEV int parts_of(int tiles, int most) { return max(1, min(most, (tiles + kXsRun - 1) / kXsRun)); }
+
+// Key i of a tile's two ranges (of the segment), and how many there are
+UT_DEV int key_of(const WinRange& r, int i) { return i < r.first ? i : i + (r.lo - r.first); }
+UT_DEV int keys_of(const WinRange& r) { return r.first + r.hi - r.lo; }
+
+// on[64] <- 1 where key i0 + r exists and is not masked; whether any is.  Synchronises the block.
+UT_DEV bool stage_window_mask(float* on, const WinRange& rg, const uint8_t* mask, int64_t k0, int i0) {
+  const int r = threadIdx.x;
+  const bool is = r < kXs && i0 + r < keys_of(rg) && (!mask || mask[k0 + key_of(rg, i0 + r)]);
+  if (r < kXs) on[r] = is ? 1.f : 0.f;
+  return __syncthreads_or(is);
+}
+// ks, vs [64][D + 4] <- keys i0 .. of kv head hk (zeros where `on` is 0)
+template <typename T, int D>
+UT_DEV void stage_window(float* ks, float* vs, const XattnParams& p, const WinRange& rg, int64_t k0, int i0, const float* on,
+                         int hk) {
+#pragma unroll 2
+  for (int e = threadIdx.x; e < kXs * (D / 4); e += kXsThreads) {
+    const int r = e / (D / 4), c = (e % (D / 4)) * 4;
+    float4 k = make_float4(0, 0, 0, 0), v = k;
+    if (on[r] != 0.f) {
+      const int64_t row = k0 + key_of(rg, i0 + r);
+      k = ld4(static_cast<const T*>(p.k) + row * p.ks + (int64_t)hk * D + c);
+      v = ld4(static_cast<const T*>(p.v) + row * p.vs + (int64_t)hk * D + c);
+    }
+    st4(ks + r * (D + 4) + c, k);
+    st4(vs + r * (D + 4) + c, v);
+  }
+}
+
 UT_DEV void check_lens(const WinParams& w) {
   check_cu(w.x.cu_q, w.x.B, w.x.nq, w.x.status);
   check_cu(w.x.cu_k, w.x.B, w.x.nk, w.x.status);
@@ -45,7 +81,7 @@ UT_DEV void check_lens(const WinParams& w) {
 
 // grid (q slots, kv heads, key splits)
 template <typename T, int D>
-__global__ void __launch_bounds__(kXsThreads) wattn_fwd_simt_kernel(const WinParams w) {
+__global__ void __launch_bounds__(kXsThreads, D == 64 ? 3 : 1) wattn_fwd_simt_kernel(const WinParams w) {
   const XattnParams& p = w.x;
   extern __shared__ float sm[];
   float* qs = sm;
@@ -64,7 +100,7 @@ __global__ void __launch_bounds__(kXsThreads) wattn_fwd_simt_kernel(const WinPar
   const int p0 = (int)(kn - g.n) + t0;
   const Limits lim(w, p0, p.G);
   const WinRange rg = win_range(p0, p0 + ntok - 1, (int)kn, w.left, w.right, w.sinks);
-  const int nblk = win_blocks<kXs>(rg), per = (nblk + p.nsplit - 1) / p.nsplit;
+  const int nblk = (keys_of(rg) + kXs - 1) / kXs, per = (nblk + p.nsplit - 1) / p.nsplit;
   const int b0 = min(nblk, per * split), b1 = min(nblk, b0 + per);
   const int ty = threadIdx.x >> 4, tx = threadIdx.x & 15;
   stage_q<T, D>(qs, p.q, t, p.qs);
@@ -78,13 +114,13 @@ __global__ void __launch_bounds__(kXsThreads) wattn_fwd_simt_kernel(const WinPar
     for (int c = 0; c < D / 64; ++c) o[i][c] = make_float4(0, 0, 0, 0);
   }
   for (int b = b0; b < b1; ++b) {
-    int x, e;
-    win_block<kXs>(rg, b, x, e);
     __syncthreads();
-    if (!stage_mask(on, p.mask, k0 + x, e - x)) continue;  // no key of the tile is left
-    stage_k<T, D>(ks, p.k, k0 + x, on, hk, p.ks);
-    stage_k<T, D>(vs, p.v, k0 + x, on, hk, p.vs);
+    if (!stage_window_mask(on, rg, p.mask, k0, b * kXs)) continue;  // no key of the tile is left
+    stage_window<T, D>(ks, vs, p, rg, k0, b * kXs, on, hk);
     __syncthreads();
+    int key[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) key[j] = key_of(rg, b * kXs + tx + 16 * j);
     float s[4][4];
     product_nt<D>(qs, ks, s);
 #pragma unroll
@@ -92,7 +128,7 @@ __global__ void __launch_bounds__(kXsThreads) wattn_fwd_simt_kernel(const WinPar
       float mx = -INFINITY;
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        s[i][j] = on[tx + 16 * j] != 0.f && lim.sees(i, x + tx + 16 * j) ? s[i][j] * p.scale : -INFINITY;
+        s[i][j] = on[tx + 16 * j] != 0.f && lim.sees(i, key[j]) ? s[i][j] * p.scale : -INFINITY;
         mx = fmaxf(mx, s[i][j]);
       }
       mx = fmaxf(m[i], half_warp_max(mx));
@@ -141,7 +177,7 @@ __global__ void __launch_bounds__(kXsThreads) wattn_fwd_simt_kernel(const WinPar
 }
 
 // P and dS of one 64 x 64 pair of tiles; s, dp are its products
-UT_DEV void probabilities(const XattnParams& p, const Limits& lim, int x, const float* on, const float* lse,
+UT_DEV void probabilities(const XattnParams& p, const Limits& lim, const int (&key)[4], const float* on, const float* lse,
                           const float* dsum, float (&s)[4][4], float (&dp)[4][4]) {
   const int ty = threadIdx.x >> 4, tx = threadIdx.x & 15;
 #pragma unroll
@@ -149,7 +185,7 @@ UT_DEV void probabilities(const XattnParams& p, const Limits& lim, int x, const 
     const float le = lse[ty * 4 + i], ds = dsum[ty * 4 + i];
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      const bool is = on[tx + 16 * j] != 0.f && le != -INFINITY && lim.sees(i, x + tx + 16 * j);
+      const bool is = on[tx + 16 * j] != 0.f && le != -INFINITY && lim.sees(i, key[j]);
       s[i][j] = is ? expf(s[i][j] * p.scale - le) : 0.f;
       dp[i][j] = is ? s[i][j] * (dp[i][j] - ds) : 0.f;
     }
@@ -187,18 +223,18 @@ UT_DEV void dq_tile(const WinParams& w, float* sm, int64_t slot, int hk) {
   for (int i = 0; i < 4; ++i)
 #pragma unroll
     for (int c = 0; c < D / 64; ++c) acc[i][c] = make_float4(0, 0, 0, 0);
-  for (int b = 0; b < win_blocks<kXs>(rg); ++b) {
-    int x, e;
-    win_block<kXs>(rg, b, x, e);
+  for (int i0 = 0; i0 < keys_of(rg); i0 += kXs) {
     __syncthreads();
-    if (!stage_mask(on, p.mask, k0 + x, e - x)) continue;  // no key of the tile is left
-    stage_k<T, D>(ks, p.k, k0 + x, on, hk, p.ks);
-    stage_k<T, D>(vs, p.v, k0 + x, on, hk, p.vs);
+    if (!stage_window_mask(on, rg, p.mask, k0, i0)) continue;  // no key of the tile is left
+    stage_window<T, D>(ks, vs, p, rg, k0, i0, on, hk);
     __syncthreads();
+    int key[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) key[j] = key_of(rg, i0 + tx + 16 * j);
     float s[4][4], dp[4][4];
     product_nt<D>(qs, ks, s);
     product_nt<D>(dos, vs, dp);
-    probabilities(p, lim, x, on, lse, dsum, s, dp);
+    probabilities(p, lim, key, on, lse, dsum, s, dp);
 #pragma unroll
     for (int i = 0; i < 4; ++i)
 #pragma unroll
@@ -215,6 +251,31 @@ UT_DEV void dq_tile(const WinParams& w, float* sm, int64_t slot, int hk) {
       st4(static_cast<T*>(p.dq) + t.off(r, p.dqs, D) + tx * 4 + 64 * c,
           make_float4(acc[i][c].x * p.scale, acc[i][c].y * p.scale, acc[i][c].z * p.scale, acc[i][c].w * p.scale));
   }
+}
+
+// The query tiles [a, b) that see keys of key tile x0 of a segment of n_k keys and n_q queries
+UT_DEV void tiles_of(const WinParams& w, int x0, int n_k, int n_q, int& a, int& b) {
+  const int tpt = kXs / w.x.G;
+  a = b = 0;
+  if (x0 < n_k) win_tokens(x0, min(x0 + kXs, n_k), n_k, n_q, w.left, w.right, w.sinks, a, b);
+  b = (b + tpt - 1) / tpt;
+  a = min(a / tpt, b);
+}
+
+// Row r of part i of a key tile: [parts, nk, Hk, d], and behind them those of the
+// tiles with first keys where they have more parts, [B, sb, first_parts, 64, Hk, d]
+struct KeyParts {
+  int parts;       // of this key tile
+  int64_t at, step;  // its row 0 of part 0, rows from part to part
+};
+UT_DEV KeyParts key_parts(const WinParams& w, const Segment& g, int64_t k0, int tiles) {
+  const int64_t x0 = g.tile * kXs;
+  const bool first = x0 < w.sinks && w.first_parts > w.parts;
+  KeyParts k;
+  k.parts = parts_of(tiles, first ? w.first_parts : w.parts);
+  k.step = first ? kXs : w.x.nk;
+  k.at = first ? w.parts * w.x.nk + ((int64_t)g.s * w.sb + g.tile) * w.first_parts * kXs : k0 + x0;
+  return k;
 }
 
 // Partial dK, dV of a key tile over a part of the query tiles that see it
@@ -237,11 +298,11 @@ UT_DEV void dkdv_tile(const WinParams& w, float* sm, int64_t slot, int hk, int s
   win_keys(w, g.s, k0, kn);
   const int x0 = (int)g.tile * kXs, rows = (int)min((int64_t)kXs, g.n - x0);  // rows of dK, dV; keys may be fewer
   const int tpt = kXs / p.G;
-  int a = 0, b = 0;  // tokens, then tiles
-  if (x0 < kn) win_tokens(x0, min(x0 + kXs, (int)kn), (int)kn, (int)qn, w.left, w.right, w.sinks, a, b);
-  b = (b + tpt - 1) / tpt;
-  a = min(a / tpt, b);
-  const int per = (b - a + p.nsplit - 1) / p.nsplit, first = min(b, a + per * split), last = min(b, first + per);
+  int a, b;
+  tiles_of(w, x0, (int)kn, (int)qn, a, b);
+  const KeyParts kp = key_parts(w, g, k0, b - a);
+  if (split >= kp.parts) return;
+  const int per = (b - a + kp.parts - 1) / kp.parts, first = min(b, a + per * split), last = min(b, first + per);
   const int ty = threadIdx.x >> 4, tx = threadIdx.x & 15;
   const bool any = stage_mask(on, p.mask, k0 + x0, kn - x0);
   stage_k<T, D>(ks, p.k, k0 + x0, on, hk, p.ks);
@@ -262,7 +323,8 @@ UT_DEV void dkdv_tile(const WinParams& w, float* sm, int64_t slot, int hk, int s
     float s[4][4], dp[4][4];
     product_nt<D>(qs, ks, s);
     product_nt<D>(dos, vs, dp);
-    probabilities(p, lim, x0, on, lse, dsum, s, dp);
+    const int key[4] = {x0 + tx, x0 + tx + 16, x0 + tx + 32, x0 + tx + 48};
+    probabilities(p, lim, key, on, lse, dsum, s, dp);
 #pragma unroll
     for (int i = 0; i < 4; ++i)
 #pragma unroll
@@ -278,7 +340,7 @@ UT_DEV void dkdv_tile(const WinParams& w, float* sm, int64_t slot, int hk, int s
   for (int i = 0; i < 4; ++i) {
     const int r = ty * 4 + i;
     if (r >= rows) continue;
-    const int64_t row = ((int64_t)split * p.nk + k0 + x0 + r) * p.Hk + hk;
+    const int64_t row = (kp.at + split * kp.step + r) * p.Hk + hk;
 #pragma unroll
     for (int c = 0; c < D / 64; ++c) {
       st4(p.part_dk + row * D + tx * 4 + 64 * c, dk[i][c]);
@@ -287,10 +349,47 @@ UT_DEV void dkdv_tile(const WinParams& w, float* sm, int64_t slot, int hk, int s
   }
 }
 
+// dK (blockIdx.z = 0), dV = the sum of the parts, in their order; a block a key
+// tile and kv head
+template <int D>
+__global__ void __launch_bounds__(kXsThreads) wattn_join_simt_kernel(const WinParams w) {
+  const XattnParams& p = w.x;
+  grid_wait();
+  const Segment g = segment_of_slot(p.cu_k, p.B, p.nk, kXs, blockIdx.x);
+  if (g.tile * kXs >= g.n) return;
+  int64_t q0, qn, k0, kn;
+  segment_rows(p.cu_q, g.s, p.nq, q0, qn);
+  win_keys(w, g.s, k0, kn);
+  const int x0 = (int)g.tile * kXs, rows = (int)min((int64_t)kXs, g.n - x0), hk = blockIdx.y;
+  int a, b;
+  tiles_of(w, x0, (int)kn, (int)qn, a, b);
+  const KeyParts kp = key_parts(w, g, k0, b - a);
+  const bool is_v = blockIdx.z;
+  const float* part = is_v ? p.part_dv : p.part_dk;
+  const float f = is_v ? 1.f : p.scale;
+  for (int e = threadIdx.x; e < rows * (D / 4); e += kXsThreads) {
+    const int r = e / (D / 4), c = (e % (D / 4)) * 4;
+    const int64_t key = k0 + x0 + r;
+    float4 sum = make_float4(0, 0, 0, 0);
+#pragma unroll 4
+    for (int i = 0; i < kp.parts; ++i) {
+      const float4 v = ld4(part + ((kp.at + i * kp.step + r) * p.Hk + hk) * D + c);
+      sum.x += v.x;
+      sum.y += v.y;
+      sum.z += v.z;
+      sum.w += v.w;
+    }
+    // a masked key's row is zero, also where a NaN or an infinity of Q or dO met its P and dS of 0
+    if (p.mask && !p.mask[key]) sum = make_float4(0, 0, 0, 0);
+    st4(static_cast<float*>(is_v ? p.dv : p.dk) + key * (is_v ? p.dvs : p.dks) + (int64_t)hk * D + c,
+        make_float4(sum.x * f, sum.y * f, sum.z * f, sum.w * f));
+  }
+}
+
 // One launch for both: n_kv blocks of dK, dV (k slots fastest, then kv heads,
 // splits), then dQ (q slots, kv heads).
 template <typename T, int D>
-__global__ void __launch_bounds__(kXsThreads) wattn_bwd_simt_kernel(const WinParams w, uint32_t n_kv, uint32_t kslots,
+__global__ void __launch_bounds__(kXsThreads, D == 64 ? 2 : 1) wattn_bwd_simt_kernel(const WinParams w, uint32_t n_kv, uint32_t kslots,
                                                                     uint32_t qslots) {
   extern __shared__ float sm[];
   grid_wait();
@@ -323,13 +422,14 @@ cudaError_t bwd(const WinParams& w, cudaStream_t s) {
   if (e != cudaSuccess) return e;
   const size_t smem = sizeof(float) * (4 * kXs * (D + 4) + 2 * kXs * kXsLdP + 3 * kXs);
   const uint32_t kslots = (uint32_t)segment_slots(p.nk, p.B, kXs), qslots = (uint32_t)segment_slots(p.nq, p.B, kXs / p.G);
-  const int64_t n_kv = p.nk > 0 ? (int64_t)kslots * p.Hk * p.nsplit : 0, n_q = p.nq > 0 ? (int64_t)qslots * p.Hk : 0;
+  const int64_t n_kv = p.nk > 0 ? (int64_t)kslots * p.Hk * max(w.parts, w.first_parts) : 0, n_q = p.nq > 0 ? (int64_t)qslots * p.Hk : 0;
   if (n_kv + n_q > INT32_MAX) return cudaErrorInvalidValue;
   e = cudaFuncSetAttribute(wattn_bwd_simt_kernel<T, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
   if (e == cudaSuccess)
     e = launch_next(wattn_bwd_simt_kernel<T, D>, dim3((unsigned)(n_kv + n_q)), dim3(kXsThreads), smem, s, w,
                     (uint32_t)n_kv, kslots, qslots);
-  if (e == cudaSuccess && p.nk > 0) e = launch_xattn_dkdv_join(p, s);
+  if (e == cudaSuccess && p.nk > 0)
+    e = launch_next(wattn_join_simt_kernel<D>, dim3(kslots, p.Hk, 2), dim3(kXsThreads), 0, s, w);
   return e;
 }
 
@@ -340,18 +440,31 @@ int64_t wattn_simt_items(const WinParams& w, bool backward) {
   return (backward ? segment_slots(p.nk, p.B, kXs) : segment_slots(p.nq, p.B, kXs / p.G)) * p.Hk;
 }
 
-// Enough parts for two blocks an SM (four backward), none shorter than two
-// blocks of a mean segment (one tile backward).  Of the keys a tile sees, and
-// of the tiles that see a key tile: all of a segment's for the first keys.
-int wattn_simt_splits(const WinParams& w, bool backward) {
+// Enough parts of the keys for two blocks an SM, none shorter than two blocks of
+// a mean segment's, as far as a tile sees them.
+int wattn_simt_splits(const WinParams& w) {
   const XattnParams& p = w.x;
-  const int64_t tpt = kXs / p.G, items = wattn_simt_items(w, backward);
-  const int64_t want = ((backward ? 4 : 2) * (int64_t)p.sms + items - 1) / items;
-  const int64_t near = (int64_t)w.left + w.right + (backward ? kXs : w.sinks + tpt), rows = (backward ? p.nq : p.nk) / p.B;
-  const int64_t seen = near < rows && !(backward && w.sinks > 0) ? near : rows;
-  const int64_t most = backward ? (seen + tpt - 1) / tpt : (seen + kXs - 1) / kXs / 2;
-  const int64_t n = want < most ? want : most;
+  const int64_t tpt = kXs / p.G, rows = p.nk / p.B, near = (int64_t)w.left + w.right + w.sinks + tpt;
+  const int64_t want = (2 * (int64_t)p.sms + wattn_simt_items(w, false) - 1) / wattn_simt_items(w, false);
+  const int64_t most = ((near < rows ? near : rows) + kXs - 1) / kXs / 2, n = want < most ? want : most;
   return (int)(n < 1 ? 1 : n > 1024 ? 1024 : n);
+}
+
+// The most parts of a key tile, of kXsRun query tiles at least: of those that a
+// window's tokens see, and of those with first keys, which all later tokens see
+// (unless there are many of these).
+void wattn_simt_parts(WinParams& w) {
+  const XattnParams& p = w.x;
+  const int64_t tpt = kXs / p.G, all = (p.nq + tpt - 1) / tpt, seen = (int64_t)w.left + w.right + kXs;
+  const int64_t near = seen < p.nq ? (seen + 2 * tpt - 2) / tpt : all;
+  auto parts = [&](int64_t tiles) { return (int)std::min<int64_t>(16, std::max<int64_t>(1, (tiles + kXsRun - 1) / kXsRun)); };
+  const bool enough = segment_slots(p.nk, p.B, kXs) * p.Hk >= 8 * (int64_t)p.sms;
+  w.parts = enough ? 1 : parts(near);
+  w.sb = (int)((std::min<int64_t>(w.sinks, p.nk) + kXs - 1) / kXs);
+  w.first_parts = w.sb > 0 && (int64_t)w.sb * p.B * p.Hk < 2 * p.sms ? parts(all) : w.parts;
+}
+size_t wattn_simt_part_rows(const WinParams& w) {  // of Hk * d values, each of dK and dV
+  return (size_t)w.parts * w.x.nk + (w.first_parts > w.parts ? (size_t)w.x.B * w.sb * w.first_parts * kXs : 0);
 }
 
 cudaError_t launch_wattn_fwd_simt(const WinParams& w, cudaStream_t s) {

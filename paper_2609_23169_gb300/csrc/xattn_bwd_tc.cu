@@ -735,7 +735,6 @@ UT_DEV WinWork decode_window(const BwdParams& b, int u) {
     segment_rows(p.cu_q, g.s, p.nq, q0, qn);
     run = (int)g.tile;
     w.kslot = (b.join ? b.chunks * (int)b.kslots : 0) + slot * b.sb;
-    w.direct = !b.join_first;
   } else {
     const int v = (int)(u - b.n_first), at = v / p.Hk, slot = at / b.chunks;
     w.hk = v - at * p.Hk;
@@ -746,7 +745,6 @@ UT_DEV WinWork decode_window(const BwdParams& b, int u) {
     j = (int)g.tile;
     w.part = run;
     w.kslot = slot - j;
-    w.direct = !b.join;
   }
   int64_t span;
   segment_rows(p.cu_k, g.s, p.nk, k0, span);
@@ -757,6 +755,7 @@ UT_DEV WinWork decode_window(const BwdParams& b, int u) {
   if (x < kn)
     win_tokens((int)x, (int)min(x + kT, kn), (int)kn, (int)qn, b.left, b.right, b.sinks, t0, t1);
   const int from = t0 + run * R * b.tpt;
+  w.direct = t1 - t0 <= R * b.tpt;  // one run, or none
   w.block0 = j;
   w.key0 = (int)k0;
   w.keys = (int)kn;
@@ -1271,7 +1270,14 @@ __global__ void __launch_bounds__(256) xattn_bwd_join_kernel(const BwdParams prm
   __shared__ __align__(16) uint8_t rows[kT * (D * 2 + 16)];
   const XattnParams& p = prm.x;
   grid_wait();
-  const Segment g = segment_of_slot(p.cu_k, p.B, p.nk, kT, blockIdx.x);
+  Segment g;
+  if (kWin && !prm.join) {  // blocks with first keys only
+    g.s = blockIdx.x / prm.sb;
+    g.tile = blockIdx.x - g.s * prm.sb;
+    segment_rows(p.cu_k, g.s, p.nk, g.row, g.n);
+  } else {
+    g = segment_of_slot(p.cu_k, p.B, p.nk, kT, blockIdx.x);
+  }
   const int keys = (int)min((int64_t)kT, g.n - g.tile * kT);
   if (keys <= 0) return;
   int64_t row, nq;
@@ -1283,7 +1289,6 @@ __global__ void __launch_bounds__(256) xattn_bwd_join_kernel(const BwdParams prm
   if constexpr (kWin) {
     const int64_t x = g.tile * kT;
     const bool first = x < prm.sinks;
-    if (!(first ? prm.join_first : prm.join)) return;
     int64_t k0;
     win_keys(p.cu_k, prm.k_len, p.nk, g.s, k0, n_keys);
     int t0 = 0, t1 = 0;
@@ -1292,6 +1297,7 @@ __global__ void __launch_bounds__(256) xattn_bwd_join_kernel(const BwdParams prm
     const int R = first ? prm.Rs : prm.R;
     tiles = (t1 - t0 + prm.tpt - 1) / prm.tpt;
     parts = (int)((tiles + R - 1) / R);
+    if (parts <= 1) return;  // written at once
     if (first) {
       // the segment's first run among all segments'
       const int64_t run = min(row / (R * prm.tpt) + g.s, prm.qslots - parts);
@@ -1559,7 +1565,7 @@ cudaError_t launch_wattn_bwd_tc(const WinParams& w, void* ws, cudaStream_t s) {
     if (e != cudaSuccess) return e;
   }
   if (hk && (prm.join || prm.join_first)) {
-    const dim3 grid((unsigned)prm.kslots, p.Hk, 2);
+    const dim3 grid((unsigned)(prm.join ? prm.kslots : p.B * (int64_t)prm.sb), p.Hk, 2);
     e = p.d == 64 ? launch_next(xattn_bwd_join_kernel<64, true>, grid, dim3(256), 0, s, prm)
                   : launch_next(xattn_bwd_join_kernel<128, true>, grid, dim3(256), 0, s, prm);
   }

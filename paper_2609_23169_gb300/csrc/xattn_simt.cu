@@ -356,6 +356,7 @@ __global__ void __launch_bounds__(256) xattn_join_kernel(const XattnParams p) {
   const int64_t x = ((int64_t)blockIdx.x * blockDim.x + threadIdx.x) >> 4;
   const int lane = threadIdx.x & 15;
   const int64_t rows = p.nq * p.H;
+  grid_wait();
   if (x >= rows) return;
   float m = -INFINITY;
   for (int s = 0; s < p.nsplit; ++s) m = fmaxf(m, p.part_ml[s * rows + x].x);
@@ -465,12 +466,12 @@ cudaError_t launch_xattn_fwd_simt(const XattnParams& p, cudaStream_t s) {
 }
 
 cudaError_t launch_xattn_join(const XattnParams& p, bool bf16, cudaStream_t s) {
-  const dim3 grid((unsigned)((p.nq * p.H + 15) / 16));
+  const dim3 grid((unsigned)((p.nq * p.H + 15) / 16)), block(kXsThreads);
   if (bf16)
-    return p.d == 64 ? launch(xattn_join_kernel<__nv_bfloat16, 64>, grid, 0, p, s)
-                     : launch(xattn_join_kernel<__nv_bfloat16, 128>, grid, 0, p, s);
-  return p.d == 64 ? launch(xattn_join_kernel<float, 64>, grid, 0, p, s)
-                   : launch(xattn_join_kernel<float, 128>, grid, 0, p, s);
+    return p.d == 64 ? launch_next(xattn_join_kernel<__nv_bfloat16, 64>, grid, block, 0, s, p)
+                     : launch_next(xattn_join_kernel<__nv_bfloat16, 128>, grid, block, 0, s, p);
+  return p.d == 64 ? launch_next(xattn_join_kernel<float, 64>, grid, block, 0, s, p)
+                   : launch_next(xattn_join_kernel<float, 128>, grid, block, 0, s, p);
 }
 
 template <typename T, int D>
