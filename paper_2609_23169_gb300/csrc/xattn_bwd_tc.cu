@@ -784,7 +784,7 @@ struct KvSmem {
   NextItem next;
   alignas(16) float lse2[2][kT];  // -LSE log2(e) and -D of the rows of a tile
   alignas(16) float dsum[2][kT];
-  uint64_t kv_full, kv_empty, q_full[kQ], q_empty[kQ], do_full[kDo], do_empty[kDo], q_ready[4], do_ready[4];
+  uint64_t k_full, k_empty, v_full, v_empty, q_full[kQ], q_empty[kQ], do_full[kDo], do_empty[kDo], q_ready[4], do_ready[4];
   uint64_t item_full[kKvSlots], item_empty[kKvSlots];
   uint64_t s_full, dp_full, p_full, ds_full, acc_full, acc_empty, mma_done;
   uint32_t tmem_base;
@@ -808,7 +808,7 @@ __global__ void __launch_bounds__(kKvThreads, 1)
     return;
   }
   if (threadIdx.x == 0) {
-    uint64_t* one[] = {&sm.kv_full, &sm.kv_empty, &sm.s_full, &sm.dp_full, &sm.acc_full, &sm.mma_done};
+    uint64_t* one[] = {&sm.k_full, &sm.k_empty, &sm.v_full, &sm.v_empty, &sm.s_full, &sm.dp_full, &sm.acc_full, &sm.mma_done};
     for (uint64_t* x : one) mbar_init(x, 1);
     for (int s = 0; s < S::kQ; ++s) {
       mbar_init(&sm.q_full[s], 1);
@@ -871,7 +871,7 @@ __global__ void __launch_bounds__(kKvThreads, 1)
     if (warp == 0) {
       const uint64_t keep = policy_evict_last();
       const uint32_t bytes = (uint32_t)prm.tpt * p.G * 128 * S::kC;
-      uint32_t nkv = 0, nt = 0, n = 0, asked = 0;
+      uint32_t nk = 0, nkv = 0, nt = 0, n = 0, asked = 0;  // K and V tiles, Q tiles, items
       bool ok = true;
       for (int u = (int)blockIdx.x; ok;) {
         Item w{};
@@ -900,16 +900,20 @@ __global__ void __launch_bounds__(kKvThreads, 1)
           if (u < 0) break;  // no more items
           for (int b = 0; b < w.blocks && ok; ++b) {
             const int j = w.block0 + b * prm.ks;
-            if (!(ok = wait(&sm.kv_empty, (nkv & 1) ^ 1))) break;
-            if (lane == 0) {
-              mbar_expect_tx(&sm.kv_full, 2 * S::kTile);
-              for (int c = 0; c < S::kC; ++c) {
-                tma_load_3d(sm.k + c * kChunkB, &tm_k, &sm.kv_full, c * 64, w.hk, w.key0 + j * kT, keep);
-                tma_load_3d(sm.v + c * kChunkB, &tm_v, &sm.kv_full, c * 64, w.hk, w.key0 + j * kT, keep);
+            auto load_block = [&](uint8_t* dst, const void* tm, uint64_t* full, uint64_t* empty) -> bool {
+              if (!wait(empty, (nkv & 1) ^ 1)) return false;
+              if (lane == 0) {
+                mbar_expect_tx(full, S::kTile);
+                for (int c = 0; c < S::kC; ++c)
+                  tma_load_3d(dst + c * kChunkB, tm, full, c * 64, w.hk, w.key0 + j * kT, keep);
               }
-            }
-            __syncwarp();
-            ++nkv;
+              __syncwarp();
+              return true;
+            };
+            // K, the first Q tile and V in the order of their use: K's place is free
+            // after the block before's last S, V's after its last dP
+            if (!(ok = load_block(sm.k, &tm_k, &sm.k_full, &sm.k_empty))) break;
+            ++nk;
             for (int t = 0; t < w.tiles; ++t, ++nt) {
               const uint32_t st = nt % S::kQ;
               if (!(ok = wait(&sm.q_empty[st], ((nt / S::kQ) & 1) ^ 1))) break;
@@ -920,7 +924,12 @@ __global__ void __launch_bounds__(kKvThreads, 1)
                               w.tok0 + t * prm.tpt, keep);
               }
               __syncwarp();
+              if (t == 0) {
+                if (!(ok = load_block(sm.v, &tm_v, &sm.v_full, &sm.v_empty))) break;
+                ++nkv;
+              }
             }
+            if (!ok) break;
           }
           if (!ok) break;
         }
@@ -936,7 +945,8 @@ __global__ void __launch_bounds__(kKvThreads, 1)
       }
       if (lane == 0) {
         if (asked > 0) drain(&sm.next.full[(asked - 1) & 1], ((asked - 1) >> 1) & 1);
-        if (nkv > 0) drain(&sm.kv_full, (nkv - 1) & 1);
+        if (nk > 0) drain(&sm.k_full, (nk - 1) & 1);
+        if (nkv > 0) drain(&sm.v_full, (nkv - 1) & 1);
         for (uint32_t x = nt > S::kQ ? nt - S::kQ : 0; x < nt; ++x) drain(&sm.q_full[x % S::kQ], (x / S::kQ) & 1);
       }
     } else if (warp == 1) {
@@ -971,12 +981,15 @@ __global__ void __launch_bounds__(kKvThreads, 1)
         if (lane == 0) mbar_arrive(&sm.item_empty[s]);
         if (blocks == 0) break;
         for (; blocks > 0; --blocks) {
-          if (!(ok = waitq(&sm.kv_full, nkv & 1))) break;
+          if (!(ok = waitq(&sm.k_full, nkv & 1))) break;
           if (!(ok = waitq(&sm.q_ready[nt & 3], (nt >> 2) & 1))) break;
           tc_fence_after();
           issue_s();
+          if (tiles == 1) mma_commit_w(&sm.k_empty);
+          if (!(ok = waitq(&sm.v_full, nkv & 1))) break;
           if (!(ok = waitq(&sm.do_ready[nt & 3], (nt >> 2) & 1))) break;
           issue_dp();
+          if (tiles == 1) mma_commit_w(&sm.v_empty);
           if (!(ok = waitq(&sm.acc_empty, (nkv & 1) ^ 1))) break;
 #pragma unroll 1
           for (uint32_t t = 0; t < tiles; ++t, ++nt) {
@@ -987,7 +1000,10 @@ __global__ void __launch_bounds__(kKvThreads, 1)
             mma_tnh(256, 0, do_mn + ds * kStep, idesc_acc, t);
             mma_commit_w(&sm.do_empty[ds]);
             ds = ds + 1 == S::kDo ? 0 : ds + 1;
-            if (more) issue_s();
+            if (more) {
+              issue_s();
+              if (t + 2 == tiles) mma_commit_w(&sm.k_empty);
+            }
             if (!(ok = waitq(&sm.ds_full, nt & 1))) break;
             tc_fence_after();
             mma_tnh(384, 128, q_mn + qs * kStep, idesc_acc, t);
@@ -996,10 +1012,10 @@ __global__ void __launch_bounds__(kKvThreads, 1)
             if (more) {
               if (!(ok = waitq(&sm.do_ready[(nt + 1) & 3], ((nt + 1) >> 2) & 1))) break;
               issue_dp();
+              if (t + 2 == tiles) mma_commit_w(&sm.v_empty);
             }
           }
           if (!ok) break;
-          mma_commit_w(&sm.kv_empty);
           mma_commit_w(&sm.acc_full);
           ++nkv;
         }
