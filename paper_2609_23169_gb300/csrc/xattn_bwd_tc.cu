@@ -1218,29 +1218,34 @@ __global__ void __launch_bounds__(kKvThreads, 1)
         tc_fence_after();
         if constexpr (kWin) {
           if (w.direct) {
-            const int64_t row = (int64_t)w.key0 + key;
-            const bool exists = key < w.rows;
+            // The four lanes of a quad exchange 16-byte units: a store covers 64
+            // bytes of eight rows, not 16 of 32 (those took 6,400 cycles a block).
+            const uint32_t c = lane & 3;
+            const int row0 = key - (int)c;  // of the quad's rows
+            const int64_t at = (int64_t)w.key0 + row0;
+            __nv_bfloat16* const dk = static_cast<__nv_bfloat16*>(p.dk) + at * p.dks + w.hk * D + half * HD + c * 8;
+            __nv_bfloat16* const dv = static_cast<__nv_bfloat16*>(p.dv) + at * p.dvs + w.hk * D + half * HD + c * 8;
 #pragma unroll 1
-            for (int which = 0; which < 2; ++which) {
-              __nv_bfloat16* dst = which ? static_cast<__nv_bfloat16*>(p.dk) + row * p.dks : static_cast<__nv_bfloat16*>(p.dv) + row * p.dvs;
-              dst += w.hk * D + half * HD;
-              const float f = which ? p.scale : 1.f;
-#pragma unroll 1
-              for (int g = 0; g < HD / 32; ++g) {
-                uint32_t r[32];
-                tmem_ld32(lane_base + (which ? 384 : 256) + half * HD + g * 32, r);
-                tmem_wait_ld();
-                if (exists) {
+            for (int g = 0; g < HD / 16; ++g) {
+              const bool is_k = g >= HD / 32;
+              const int col = (is_k ? g - HD / 32 : g) * 32;
+              const float f = is_k ? p.scale : 1.f;
+              __nv_bfloat16* const dst = (is_k ? dk : dv) + col;
+              const int64_t stride = is_k ? p.dks : p.dvs;
+              uint32_t r[32], u[4][4];
+              tmem_ld32(lane_base + (is_k ? 384 : 256) + half * HD + col, r);
+              tmem_wait_ld();
 #pragma unroll
-                  for (int x = 0; x < 32; x += 8)  // a masked key's row is zero, whatever met its P and dS of 0
-                    *reinterpret_cast<uint4*>(dst + g * 32 + x) = make_uint4(
-                        pack_bf16x2(__uint_as_float(r[x]) * f, __uint_as_float(r[x + 1]) * f) & on,
-                        pack_bf16x2(__uint_as_float(r[x + 2]) * f, __uint_as_float(r[x + 3]) * f) & on,
-                        pack_bf16x2(__uint_as_float(r[x + 4]) * f, __uint_as_float(r[x + 5]) * f) & on,
-                        pack_bf16x2(__uint_as_float(r[x + 6]) * f, __uint_as_float(r[x + 7]) * f) & on);
-                }
-                __syncwarp();
-              }
+              for (int x = 0; x < 16; ++x)  // a masked key's row is zero, whatever met its P and dS of 0
+                u[x >> 2][x & 3] = pack_bf16x2(__uint_as_float(r[2 * x]) * f, __uint_as_float(r[2 * x + 1]) * f) & on;
+              exchange_units<1>(u, c & 1, 0, 1);
+              exchange_units<1>(u, c & 1, 2, 3);
+              exchange_units<2>(u, c >> 1, 0, 2);
+              exchange_units<2>(u, c >> 1, 1, 3);
+#pragma unroll
+              for (int i = 0; i < 4; ++i)
+                if (row0 + i < w.rows)
+                  *reinterpret_cast<uint4*>(dst + i * stride) = make_uint4(u[i][0], u[i][1], u[i][2], u[i][3]);
             }
             tc_fence_before();
             __syncwarp();
