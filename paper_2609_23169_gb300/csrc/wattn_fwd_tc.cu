@@ -91,13 +91,17 @@ struct Smem {
   uint32_t keys[F::kV][4];         // of a V tile: bit = attend
   float most[2][F::kHalves][kM];   // of the halves of a row
   uint64_t q_full[F::kQ], q_empty[F::kQ], k_full[F::kK], k_empty[F::kK], v_full[F::kV], v_empty[F::kV], v_ready[F::kV];
-  uint64_t qt_full, qt_empty, s_full[F::kS], p_full[F::kS], pair_full[4], pv_done, ml_full, o_full, o_empty, mma_done;
+  uint64_t qt_full, qt_empty, s_full[F::kS], p_full[F::kS], pv_done, ml_full, o_full, o_empty, mma_done;
   uint64_t item_full[kItemSlots], item_empty[kItemSlots];
   Item item[kItemSlots];
   NextItem next;
   uint32_t tmem_base;
   int abort_flag;
 };
+
+// The two warps of 32 rows (hardware barriers 1 to 4)
+UT_DEV void pair_sync(uint32_t id) { asm volatile("barrier.cta.sync %0, 64;" ::"r"(id) : "memory"); }
+UT_DEV void pair_arrive(uint32_t id) { asm volatile("barrier.cta.arrive %0, 64;" ::"r"(id) : "memory"); }
 
 struct Params {
   WinParams w;
@@ -162,7 +166,6 @@ __global__ void __launch_bounds__(Form<D>::kThreads, Form<D>::kCtas)
       mbar_init(&sm.s_full[s], 1);
       mbar_init(&sm.p_full[s], F::kSoftmax);
     }
-    for (int s = 0; s < 4; ++s) mbar_init(&sm.pair_full[s], 2);
     mbar_init(&sm.pv_done, 1);
     mbar_init(&sm.ml_full, F::kSoftmax);
     mbar_init(&sm.o_full, 1);
@@ -507,9 +510,7 @@ __global__ void __launch_bounds__(Form<D>::kThreads, Form<D>::kCtas)
         float mx = fmaxf(max3(m4[0], m4[1], m4[2]), m4[3]) * prm.scale_log2;
         if constexpr (F::kHalves == 2) {
           sm.most[b & 1][half][row] = mx;  // both halves take the same reference
-          __syncwarp();
-          if (lane == 0) mbar_arrive(&sm.pair_full[quarter]);
-          if (!(ok = wait(&sm.pair_full[quarter], b & 1))) break;
+          pair_sync(1 + quarter);
           mx = fmaxf(mx, sm.most[b & 1][half ^ 1][row]);
         }
         mx = fmaxf(mx, -1e30f);  // finite where a row sees no key of the block
@@ -578,6 +579,8 @@ __global__ void __launch_bounds__(Form<D>::kThreads, Form<D>::kCtas)
       __syncwarp();
       if (lane == 0) mbar_arrive(&sm.ml_full);
     }
+    // a warp that gave up does not keep its partner waiting
+    if (F::kHalves == 2 && !ok) pair_arrive(1 + quarter);
   } else {
     // ------------------------------------------------------------- Q in, O out
     if constexpr (F::kCtas == 2) setmaxnreg_dec<F::kRegOut>();
