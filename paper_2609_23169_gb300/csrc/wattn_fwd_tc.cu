@@ -511,6 +511,7 @@ __global__ void __launch_bounds__(Form<D>::kThreads, Form<D>::kCtas)
         if constexpr (F::kHalves == 2) {
           sm.most[b & 1][half][row] = mx;  // both halves take the same reference
           pair_sync(1 + quarter);
+          if (!(ok = !__any_sync(0xffffffffu, *abort_flag))) break;  // the partner may have given up
           mx = fmaxf(mx, sm.most[b & 1][half ^ 1][row]);
         }
         mx = fmaxf(mx, -1e30f);  // finite where a row sees no key of the block
@@ -579,8 +580,14 @@ __global__ void __launch_bounds__(Form<D>::kThreads, Form<D>::kCtas)
       __syncwarp();
       if (lane == 0) mbar_arrive(&sm.ml_full);
     }
-    // a warp that gave up does not keep its partner waiting
-    if (F::kHalves == 2 && !ok) pair_arrive(1 + quarter);
+    // A warp that gave up does not keep its partner waiting: it comes to their
+    // barrier once more, after the flag, and so the partner, which looks at the
+    // flag behind the barrier, does not come to another.
+    if (F::kHalves == 2 && !ok) {
+      __threadfence_block();
+      __syncwarp();
+      pair_arrive(1 + quarter);
+    }
   } else {
     // ------------------------------------------------------------- Q in, O out
     if constexpr (F::kCtas == 2) setmaxnreg_dec<F::kRegOut>();
