@@ -379,8 +379,9 @@ __global__ void __launch_bounds__(kXsThreads) wattn_join_simt_kernel(const WinPa
       sum.z += v.z;
       sum.w += v.w;
     }
-    // a masked key's row is zero, also where a NaN or an infinity of Q or dO met its P and dS of 0
-    if (p.mask && !p.mask[key]) sum = make_float4(0, 0, 0, 0);
+    // a masked key's row is zero, and one behind the keys, also where a NaN or an
+    // infinity of Q or dO met its P and dS of 0
+    if (x0 + r >= kn || (p.mask && !p.mask[key])) sum = make_float4(0, 0, 0, 0);
     st4(static_cast<float*>(is_v ? p.dv : p.dk) + key * (is_v ? p.dvs : p.dks) + (int64_t)hk * D + c,
         make_float4(sum.x * f, sum.y * f, sum.z * f, sum.w * f));
   }

@@ -67,7 +67,8 @@ struct BwdParams {
   const int32_t* k_len;
   int left, right, sinks;
   int chunks;       // runs of a key block without first keys
-  int Rs, sb;       // tiles of a run and key blocks of a segment with first keys
+  int first;        // blocks that begin below it have runs of their own (0 or sinks)
+  int Rs, sb;       // tiles of those, how many such blocks a segment has at most
   int64_t n_first, qslots;  // items of those, their runs of all segments
   bool join, join_first;    // the runs' results are partial sums
 };
@@ -750,11 +751,13 @@ UT_DEV WinWork decode_window(const BwdParams& b, int u) {
   segment_rows(p.cu_k, g.s, p.nk, k0, span);
   win_keys(p.cu_k, b.k_len, p.nk, g.s, k0, kn);
   const int64_t x = (int64_t)j * kT;
-  if (x >= span || first != (x < b.sinks)) return w;
+  if (x >= span || first != (x < b.first)) return w;
   int t0 = 0, t1 = 0;
   if (x < kn)
     win_tokens((int)x, (int)min(x + kT, kn), (int)kn, (int)qn, b.left, b.right, b.sinks, t0, t1);
-  const int from = t0 + run * R * b.tpt;
+  const int64_t to = t0 + (int64_t)run * R * b.tpt;
+  if (run > 0 && to >= t1) return w;
+  const int from = (int)to;
   w.direct = t1 - t0 <= R * b.tpt;  // one run, or none
   w.block0 = j;
   w.key0 = (int)k0;
@@ -763,7 +766,6 @@ UT_DEV WinWork decode_window(const BwdParams& b, int u) {
   w.tok0 = (int)(q0 + from);
   w.ntok = min(R * b.tpt, t1 - from);
   w.p0 = (int)(kn - qn) + from;
-  if (run > 0 && w.ntok <= 0) return w;
   w.tiles = w.ntok > 0 ? (w.ntok + b.tpt - 1) / b.tpt : 0;
   w.blocks = w.tiles > 0 ? 1 : 0;
   if (w.blocks == 0) w.ntok = (int)min((int64_t)kT, span - x);  // no query sees it: rows to be cleared
@@ -1309,7 +1311,7 @@ __global__ void __launch_bounds__(256) xattn_bwd_join_kernel(const BwdParams prm
   int64_t n_keys = g.n;
   if constexpr (kWin) {
     const int64_t x = g.tile * kT;
-    const bool first = x < prm.sinks;
+    const bool first = x < prm.first;
     int64_t k0;
     win_keys(p.cu_k, prm.k_len, p.nk, g.s, k0, n_keys);
     int t0 = 0, t1 = 0;
@@ -1494,19 +1496,24 @@ namespace {
 // fewer items than SMs twice.  Blocks with first keys are seen by all later
 // tokens: runs of at least twice those tiles, three times as many as SMs, whose
 // parts are joined; but one run each where there are many such blocks (first
-// keys without a window), or few tokens.
+// keys without a window), or few tokens.  Where the first keys are more than a
+// mean segment has, their blocks have no runs of their own: an item of each
+// segment's most blocks would be idle work that grows with segments times keys.
 void window_runs(const WinParams& w, BwdParams& b) {
   const XattnParams& p = w.x;
-  const int64_t tpt = kT / p.G, all = (p.nq + tpt - 1) / tpt, seen = (int64_t)w.left + w.right + kT;
-  const int64_t near = std::max<int64_t>(1, ((seen < p.nq ? seen : p.nq) + tpt - 1) / tpt);
   b.kslots = segment_slots(p.nk, p.B, kT);
+  b.sb = (int)(((w.sinks < p.nk ? w.sinks : p.nk) + kT - 1) / kT);
+  const bool own = (int64_t)b.sb * p.B <= b.kslots;
+  if (!own) b.sb = 0;
+  b.first = own ? w.sinks : 0;
+  const int64_t tpt = kT / p.G, all = (p.nq + tpt - 1) / tpt, seen = own ? (int64_t)w.left + w.right + kT : p.nq;
+  const int64_t near = std::max<int64_t>(1, ((seen < p.nq ? seen : p.nq) + tpt - 1) / tpt);
   const int64_t items = b.kslots * p.Hk;
   int64_t chunks = items < 2 * p.sms ? (2 * p.sms + items - 1) / items : 1;
   chunks = std::min(chunks, (near + 3) / 4);  // four tiles a run at least
   b.R = (int)((near + chunks - 1) / chunks);
   b.chunks = (int)((near + b.R - 1) / b.R);
   b.join = b.chunks > 1;
-  b.sb = (int)(((w.sinks < p.nk ? w.sinks : p.nk) + kT - 1) / kT);
   b.Rs = (int)std::max<int64_t>(all, 1);
   b.qslots = 0;
   if (b.sb > 0) {
