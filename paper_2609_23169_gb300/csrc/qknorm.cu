@@ -16,9 +16,13 @@
 // One warp takes a token; a head's 16-byte vectors lie in neighbouring lanes (8
 // to 32 of them), a lane meets the same pairs in every head, so it takes their
 // sines once a token, and its columns of w and dw stay in registers.  Where
-// there are few tokens their heads are dealt out to several warps.  Up to kVec
-// loads a lane in flight.  Bound by memory: Q and K are read once and written
-// once (backward: x and dy read, dx written).
+// there are few tokens their heads are dealt out to several warps.  What a warp
+// reads is asked for up to six steps ahead into shared memory (cp.async), which
+// keeps the reads of a warp in flight across tokens without registers: with
+// loads into registers, a token's at a time, the 2048 canvas took 359 us.
+// Bound by memory: Q and K are read once and written once (backward: x and dy
+// read, dx written).  Measured, 24 + 24 heads of 128: 85,714 rows 337 us, 6.24
+// TB/s or 0.92 of a copy; 23,959 rows forward 103, backward 145 and dw 9 us.
 // dw: a lane's sums over its tokens, then over the block's warps in shared
 // memory, then over blocks by a second kernel, always in the same order.
 #include <math.h>

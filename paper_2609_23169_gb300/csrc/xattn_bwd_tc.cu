@@ -36,6 +36,15 @@
 // what they hold, NaN or infinities, is never multiplied), warps 4-11 are the
 // elementwise stage: warps w and w + 4 share 32 TMEM lanes and take 64 columns
 // each, and write their bf16 pairs over the first half of their own columns.
+// Windowed attention (kWin; wattn.cuh) has the same formulas over the keys that a
+// row sees, and these kernels with other items: dQ takes a tile's blocks, which
+// begin at its window's first key; dK, dV a key block and the run of tiles that
+// see it, cut from the first token that does.  The elementwise warps clear what a
+// row's own limits leave out, in the few blocks where a limit falls.  A window's
+// run is short, so that dK and dV of most blocks are whole at once and written as
+// bf16; runs of first keys, which all later tokens see, and of few blocks are
+// joined (window_runs).  24,471 rows, 24 heads of 128, 512 keys each side and 512
+// first ones: dQ 477 us and dK, dV 628, tensor pipe active 69% and 68%, join 17.
 // Every wait is bounded; on expiry a kernel records UT_ERR_TIMEOUT, drains its
 // own copies and MMAs, frees TMEM and returns.
 #include <algorithm>
