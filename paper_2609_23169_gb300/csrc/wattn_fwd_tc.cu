@@ -12,14 +12,14 @@
 //
 // CTAs take item after item (NextItem), the head fastest: CTAs in flight share
 // the windows of neighbouring tiles in L2.  Roles:
-//   warp 0      TMA: Q, K and V tiles, a ring each
+//   warp 0      TMA: Q, K and V tiles, a ring each; which keys of a block the mask
+//               leaves, a bit each
 //   warp 1      TMEM owner and MMA issuer: S = Q K^T, O += P V.  The products
 //               follow one another across items: the next item's first S is
 //               computed while this one's last blocks are in the softmax.
 //   warp 2      asks for the items and decodes them into a ring
-//   warp 3      which keys of a block count, a bit each, and the rows of the V
-//               tile that do not become zero, so that no value they hold (NaN,
-//               infinities) is multiplied
+//   warp 3      the rows of a V tile whose keys do not count become zero, so that
+//               no value they hold (NaN, infinities) is multiplied
 //   softmax     thread = row = TMEM lane; at d = 128 two warps share 32 rows and
 //               take 64 columns each.  Pass 1: the maximum; where keys do not
 //               count or a row of the warp has its limits in the block, S becomes
@@ -61,6 +61,10 @@ namespace {
 
 constexpr int kM = 128, kN = 128;
 constexpr uint32_t kChunkBytes = 128 * 128;  // 128 rows x 64 bf16
+// Slots of key bits.  Those of block c are written when S of block c - 3 is done
+// (K's stage is free), and S follows P of the block that had its buffer: of c - 5
+// at the earliest, so that five are in use.
+constexpr int kKeySlots = 8;
 constexpr int kItemSlots = 3;                // no more are taken ahead: other CTAs may be idle
 
 template <int D>
@@ -97,7 +101,7 @@ struct Smem {
   alignas(1024) uint8_t q[F::kQ][kTile];
   alignas(1024) uint8_t k[F::kK][kTile];
   alignas(1024) uint8_t v[F::kV][kTile];
-  uint32_t keys[F::kV][4];         // of a V tile: bit = attend
+  uint32_t keys[kKeySlots][4];     // masked keys: of a K tile, a bit set where it counts
   float most[2][F::kHalves][kM];   // of the halves of a row
   uint64_t q_full[F::kQ], q_empty[F::kQ], k_full[F::kK], k_empty[F::kK], v_full[F::kV], v_empty[F::kV], v_ready[F::kV];
   uint64_t qt_full, qt_empty, s_full[F::kS], p_full[F::kS], pv_done, ml_full, o_full, o_empty, mma_done;
@@ -251,11 +255,28 @@ __global__ void __launch_bounds__(Form<D>::kThreads, Form<D>::kCtas)
         }
         __syncwarp();
         ++nq;
+        uint32_t next[4];  // the mask of the keys lane, lane + 32, ..., a block ahead
+        auto load_mask = [&](int t) {
+          int x, e;
+          block_of(it, t, x, e);
+#pragma unroll
+          for (int w = 0; w < 4; ++w) next[w] = x + w * 32 + (int)lane < e ? p.mask[(int64_t)it.key0 + x + w * 32 + lane] : 0u;
+        };
+        if (p.mask) load_mask(0);
         for (int t = 0; t < it.blocks; ++t) {
           int x, e;
           block_of(it, t, x, e);
           const uint32_t st = at % F::kK, ph = ((at / F::kK) & 1) ^ 1;
           if (!(ok = wait(&sm.k_empty[st], ph))) break;
+          if (p.mask) {  // there before K is, and so before S
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+              asm volatile("" : "+r"(next[w]));  // not looked at before
+              const uint32_t word = __ballot_sync(0xffffffffu, next[w] != 0);
+              if (lane == 0) sm.keys[at % kKeySlots][w] = word;
+            }
+            if (t + 1 < it.blocks) load_mask(t + 1);
+          }
           if (lane == 0) {
             mbar_expect_tx(&sm.k_full[st], S::kTile);
             for (int c = 0; c < S::kChunks; ++c)
@@ -349,11 +370,6 @@ __global__ void __launch_bounds__(Form<D>::kThreads, Form<D>::kCtas)
           if (t + 1 < it.blocks) next = keys_of(t + 1);  // a block ahead
           if (!(ok = wait(&sm.v_full[st], (at / F::kV) & 1))) break;
           if (!all_keys(x, e)) {
-#pragma unroll
-            for (int g = 0; g < 4; ++g) {
-              const uint32_t word = __ballot_sync(0xffffffffu, (keys >> g) & 1u);
-              if (lane == 0) sm.keys[st][g] = word;
-            }
             if (!__all_sync(0xffffffffu, keys == 15u)) {
               const uint32_t base = smem_u32(sm.v[st]);
 #pragma unroll
@@ -456,7 +472,7 @@ __global__ void __launch_bounds__(Form<D>::kThreads, Form<D>::kCtas)
     const uint32_t half = F::kHalves == 2 ? (warp - 4) >> 2 : 0;
     const int rt = token_of(row), rt_first = token_of(quarter * 32), span = token_of(quarter * 32 + 31) - rt_first;
     const uint64_t c2 = pack_f32x2(prm.scale_log2, prm.scale_log2);
-    uint32_t n = 0, b = 0, vst = 0, vf = 0;  // items, blocks; V stage and phase
+    uint32_t n = 0, b = 0;  // items, blocks
     bool ok = true;
     Item it;
     while (ok && next_item(n, it, ok)) {
@@ -469,10 +485,16 @@ __global__ void __launch_bounds__(Form<D>::kThreads, Form<D>::kCtas)
         block_of(it, t, x, e);
         x += (int)half * kCols;  // of this warp's first column
         const uint32_t sb = b % F::kS, ts = lane_base + sb * kN + half * kCols;
-        const bool whole = !p.mask && e - x >= kCols;  // every key of this warp's counts
         if (!(ok = wait(&sm.s_full[sb], (b / F::kS) & 1))) break;
-        if (!whole && !(ok = wait(&sm.v_ready[vst], vf))) break;
         tc_fence_after();
+        bool whole = e - x >= kCols;  // every key of this warp's counts
+        const uint32_t* const keys = &sm.keys[b % kKeySlots][half * (kCols / 32)];
+        if (p.mask) {
+          uint32_t all = keys[0];
+#pragma unroll
+          for (int w = 1; w < kCols / 32; ++w) all &= keys[w];
+          whole = all == ~0u;
+        }
         const bool limits = right0 - x < kCols - 1 || (left0 + span > x && x + kCols > prm.w.sinks);
         // ---- pass 1
         float m4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
@@ -491,9 +513,7 @@ __global__ void __launch_bounds__(Form<D>::kThreads, Form<D>::kCtas)
 #pragma unroll
             for (int w = 0; w < kC / 32; ++w) {
               const int first = g + 32 * w, hi = right - x - first, lo = left - x - first, sink = prm.w.sinks - x - first;
-              on[w] = whole ? ~0u : sm.keys[vst][half * (kCols / 32) + first / 32];
-              on[w] &= hi >= 31 ? ~0u : (hi < 0 ? 0u : (2u << hi) - 1);
-              on[w] &= (lo <= 0 ? ~0u : (lo > 31 ? 0u : ~0u << lo)) | (sink >= 32 ? ~0u : (sink <= 0 ? 0u : (1u << sink) - 1));
+              on[w] = (p.mask ? keys[first / 32] : bits_to(e - 1 - x - first)) & bits_to(hi) & (bits_from(lo) | bits_to(sink - 1));
               some &= on[w];
             }
             if (__any_sync(0xffffffffu, some != ~0u)) {
@@ -512,10 +532,6 @@ __global__ void __launch_bounds__(Form<D>::kThreads, Form<D>::kCtas)
             for (int z = 0; z < 4; ++z) m4[z] = max3(m4[z], __uint_as_float(r[y + z]), __uint_as_float(r[y + z + 4]));
         }
         if (kReload && (!whole || limits)) tmem_wait_st();
-        if (++vst == F::kV) {
-          vst = 0;
-          vf ^= 1;
-        }
         float mx = fmaxf(max3(m4[0], m4[1], m4[2]), m4[3]) * prm.scale_log2;
         if constexpr (F::kHalves == 2) {
           sm.most[b & 1][half][row] = mx;  // both halves take the same reference
