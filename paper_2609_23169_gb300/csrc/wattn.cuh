@@ -52,18 +52,28 @@ __host__ __device__ __forceinline__ WinRange win_range(int pa, int pb, int n, in
   if (r.lo <= r.first) r.first = r.lo = 0;
   return r;
 }
-// Its blocks of N keys: those of [0, first), then those of [lo, hi).  Block j
-// begins at key x and holds keys below e.
+// Its blocks of N keys: those of [0, first), then those of [lo, hi).
 template <int N>
 __host__ __device__ __forceinline__ int win_blocks(const WinRange& r) {
   return (r.first + N - 1) / N + (r.hi - r.lo + N - 1) / N;
 }
+// One after another: a block begins at key x and holds keys below e.
 template <int N>
-__host__ __device__ __forceinline__ void win_block(const WinRange& r, int j, int& x, int& e) {
-  const int a = (r.first + N - 1) / N;
-  x = j < a ? j * N : r.lo + (j - a) * N;
-  e = j < a ? r.first : r.hi;
-}
+struct WinBlock {
+  int x, e;
+  __host__ __device__ __forceinline__ explicit WinBlock(const WinRange& r, int j = 0) {  // block j
+    const int a = (r.first + N - 1) / N;
+    x = j < a ? j * N : r.lo + (j - a) * N;
+    e = j < a ? r.first : r.hi;
+  }
+  __host__ __device__ __forceinline__ void next(const WinRange& r) {
+    x += N;
+    if (x >= e) {
+      x = r.lo;
+      e = r.hi;
+    }
+  }
+};
 // The tokens [t0, t1) of n that see some key of [x, e): those of positions
 // x - right .. e - 1 + left, all behind the first where a key is below sinks.
 __host__ __device__ __forceinline__ void win_tokens(int x, int e, int n_k, int n_q, int left, int right, int sinks,

@@ -223,9 +223,8 @@ __global__ void __launch_bounds__(Form<D>::kThreads, Form<D>::kCtas)
     ++n;
     return it.hk >= 0;
   };
-  // Block t of an item holds the keys x .. x + 127 of the segment, those below e.
-  auto block_of = [&](const Item& it, int t, int& x, int& e) { win_block<kN>(it.rg, it.j0 + t, x, e); };
-  auto all_keys = [&](int x, int e) { return !p.mask && e - x >= kN; };
+  using Block = WinBlock<kN>;
+  auto all_keys = [&](const Block& b) { return !p.mask && b.e - b.x >= kN; };
 
   // For the warps that read TMEM: thread = row = TMEM lane
   const uint32_t quarter = warp & 3, lane_base = tmem + ((quarter * 32) << 16), row = quarter * 32 + lane;
@@ -256,16 +255,16 @@ __global__ void __launch_bounds__(Form<D>::kThreads, Form<D>::kCtas)
         __syncwarp();
         ++nq;
         uint32_t next[4];  // the mask of the keys lane, lane + 32, ..., a block ahead
-        auto load_mask = [&](int t) {
-          int x, e;
-          block_of(it, t, x, e);
+        auto load_mask = [&](const Block& b) {
 #pragma unroll
-          for (int w = 0; w < 4; ++w) next[w] = x + w * 32 + (int)lane < e ? p.mask[(int64_t)it.key0 + x + w * 32 + lane] : 0u;
+          for (int w = 0; w < 4; ++w)
+            next[w] = b.x + w * 32 + (int)lane < b.e ? p.mask[(int64_t)it.key0 + b.x + w * 32 + lane] : 0u;
         };
-        if (p.mask) load_mask(0);
+        Block blk(it.rg, it.j0);
+        if (p.mask) load_mask(blk);
         for (int t = 0; t < it.blocks; ++t) {
-          int x, e;
-          block_of(it, t, x, e);
+          const int x = blk.x;
+          blk.next(it.rg);
           const uint32_t st = at % F::kK, ph = ((at / F::kK) & 1) ^ 1;
           if (!(ok = wait(&sm.k_empty[st], ph))) break;
           if (p.mask) {  // there before K is, and so before S
@@ -275,7 +274,7 @@ __global__ void __launch_bounds__(Form<D>::kThreads, Form<D>::kCtas)
               const uint32_t word = __ballot_sync(0xffffffffu, next[w] != 0);
               if (lane == 0) sm.keys[at % kKeySlots][w] = word;
             }
-            if (t + 1 < it.blocks) load_mask(t + 1);
+            if (t + 1 < it.blocks) load_mask(blk);
           }
           if (lane == 0) {
             mbar_expect_tx(&sm.k_full[st], S::kTile);
@@ -357,19 +356,18 @@ __global__ void __launch_bounds__(Form<D>::kThreads, Form<D>::kCtas)
       bool ok = true;
       Item it;
       while (ok && next_item(n, it, ok)) {
-        auto keys_of = [&](int t) -> uint32_t {
-          int x, e;
-          block_of(it, t, x, e);
-          return all_keys(x, e) ? 15u : lane_keys(p.mask, (int64_t)it.key0 + x, e - x, lane);
+        auto keys_of = [&](const Block& b) -> uint32_t {
+          return all_keys(b) ? 15u : lane_keys(p.mask, (int64_t)it.key0 + b.x, b.e - b.x, lane);
         };
-        uint32_t next = keys_of(0);
+        Block blk(it.rg, it.j0);
+        uint32_t next = keys_of(blk);
         for (int t = 0; t < it.blocks; ++t, ++at) {
           const uint32_t st = at % F::kV, keys = next;
-          int x, e;
-          block_of(it, t, x, e);
-          if (t + 1 < it.blocks) next = keys_of(t + 1);  // a block ahead
+          const bool whole = all_keys(blk);
+          blk.next(it.rg);
+          if (t + 1 < it.blocks) next = keys_of(blk);  // a block ahead
           if (!(ok = wait(&sm.v_full[st], (at / F::kV) & 1))) break;
-          if (!all_keys(x, e)) {
+          if (!whole) {
             if (!__all_sync(0xffffffffu, keys == 15u)) {
               const uint32_t base = smem_u32(sm.v[st]);
 #pragma unroll
@@ -479,11 +477,11 @@ __global__ void __launch_bounds__(Form<D>::kThreads, Form<D>::kCtas)
       const int right = it.p0 + rt + prm.w.right, left = it.p0 + rt - prm.w.left;  // last and first key of this row's
       const int right0 = right + rt_first - rt, left0 = left + rt_first - rt;      // and of the warp's first
       float m = -1e30f, l = 0.f;
+      Block blk(it.rg, it.j0);
 #pragma unroll 1
       for (int t = 0; t < it.blocks; ++t, ++b) {
-        int x, e;
-        block_of(it, t, x, e);
-        x += (int)half * kCols;  // of this warp's first column
+        const int e = blk.e, x = blk.x + (int)half * kCols;  // of this warp's first column
+        blk.next(it.rg);
         const uint32_t sb = b % F::kS, ts = lane_base + sb * kN + half * kCols;
         if (!(ok = wait(&sm.s_full[sb], (b / F::kS) & 1))) break;
         tc_fence_after();

@@ -239,17 +239,17 @@ __global__ void __launch_bounds__(kDqThreads, 1)
     ++n;
     return it.blocks > 0;
   };
-  // Block j of an item: its first key (of the segment's), and the keys from there on
-  auto block_of = [&](const Item& it, int j, int& x, int& left) {
-    if constexpr (kWin) {
-      int e;
-      win_block<kT>(it.rg, j, x, e);
-      left = e - x;
-    } else {
-      x = j * kT;
-      left = it.keys - x;
-    }
+  // The blocks of an item: their keys of the segment.
+  struct Seq {  // 0, 128, ...
+    int x = 0, e;
+    __device__ explicit Seq(const Item& it) : e(it.keys) {}
+    __device__ void next(const Item&) { x += kT; }
   };
+  struct SeqWin : WinBlock<kT> {
+    __device__ explicit SeqWin(const DqWinItem& it) : WinBlock<kT>(it.rg) {}
+    __device__ void next(const DqWinItem& it) { WinBlock<kT>::next(it.rg); }
+  };
+  using Block = std::conditional_t<kWin, SeqWin, Seq>;
 
   if (warp < 4) {
     setmaxnreg_dec<kDqCtl>();
@@ -275,10 +275,10 @@ __global__ void __launch_bounds__(kDqThreads, 1)
         for (int c = 0; c < S::kC; ++c)
           tma_load_3d(sm.q[qs] + c * kChunkB, &tm_q, &sm.q_full[qs], c * 64, it.hk * p.G, it.tok0, keep);
         ++n;
-        for (int j = 0; j < it.blocks; ++j) {
+        Block blk(it);
+        for (int j = 0; j < it.blocks; ++j, blk.next(it)) {
           const uint32_t ks = at % S::kK, vs = nv % S::kV;
-          int x, left;
-          block_of(it, j, x, left);
+          const int x = blk.x;
           if (!(ok = wait1(&sm.k_empty[ks], ((at / S::kK) & 1) ^ 1))) break;
           mbar_expect_tx(&sm.k_full[ks], S::kTile);
           for (int c = 0; c < S::kC; ++c)
@@ -359,12 +359,11 @@ __global__ void __launch_bounds__(kDqThreads, 1)
       uint32_t n = 0, at = 0;
       bool ok = true;
       Item it;
-      while (ok && next_item(n, it, ok))
-        for (int j = 0; j < it.blocks; ++j, ++at) {
+      while (ok && next_item(n, it, ok)) {
+        Block blk(it);
+        for (int j = 0; j < it.blocks; ++j, ++at, blk.next(it)) {
           const uint32_t st = at % S::kK;
-          int x0, left;
-          block_of(it, j, x0, left);
-          const uint32_t keys = lane_keys(p.mask, (int64_t)it.key0 + x0, left, lane);
+          const uint32_t keys = lane_keys(p.mask, (int64_t)it.key0 + blk.x, blk.e - blk.x, lane);
           auto zero_keys = [&](uint32_t base) {
             for (int g = 0; g < 4; ++g)
               if (!((keys >> g) & 1u))
@@ -381,6 +380,7 @@ __global__ void __launch_bounds__(kDqThreads, 1)
           if (some) zero_keys(smem_u32(sm.v[at % S::kV]));
           if (lane == 0) mbar_arrive(&sm.ready[st]);
         }
+      }
     } else if (warp == 1) {
       // ---------------------------------------------------------- products
       constexpr uint32_t idesc_s = idesc_bf16_f32(kT, kT, false, false);
@@ -498,15 +498,14 @@ __global__ void __launch_bounds__(kDqThreads, 1)
       more = next_item(n, nx, ok);
       if (!ok) break;
       row_load(nx, nl, nd);
-      int kx, kleft;
-      block_of(it, 0, kx, kleft);
-      uint32_t keys = lane_keys(p.mask, (int64_t)it.key0 + kx, kleft, lane);
+      Block blk(it);
+      uint32_t keys = lane_keys(p.mask, (int64_t)it.key0 + blk.x, blk.e - blk.x, lane);
       for (int j = 0; j < it.blocks; ++j, ++at) {
         const uint32_t now = keys;
-        const int xw = kx + (int)half * 64;  // key of this warp's first column
+        const int xw = blk.x + (int)half * 64;  // key of this warp's first column
         if (j + 1 < it.blocks) {
-          block_of(it, j + 1, kx, kleft);
-          keys = lane_keys(p.mask, (int64_t)it.key0 + kx, kleft, lane);
+          blk.next(it);
+          keys = lane_keys(p.mask, (int64_t)it.key0 + blk.x, blk.e - blk.x, lane);
         }
         const uint32_t ts = lane_base + (at & 1) * 256 + half * 64;
         if (!(ok = wait(&sm.s_full[at & 1], (at >> 1) & 1))) break;

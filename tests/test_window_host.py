@@ -279,9 +279,11 @@ int check(int n_q, int n_k, int left, int right, int sinks, int tile) {
     const int t1 = t0 + tile < n_q ? t0 + tile : n_q, pa = n_k - n_q + t0, pb = n_k - n_q + t1 - 1;
     const WinRange r = win_range(pa, pb, n_k, left, right, sinks);
     std::vector<int> in(n_k, 0);
-    for (int j = 0; j < win_blocks<N>(r); ++j) {
-      int x, e;
-      win_block<N>(r, j, x, e);
+    WinBlock<N> b(r);
+    for (int j = 0; j < win_blocks<N>(r); ++j, b.next(r)) {
+      const int x = b.x, e = b.e;
+      const WinBlock<N> same(r, j);
+      wrong += same.x != x || same.e != e;
       wrong += x < 0 || e > n_k || x >= e;
       for (int key = x; key < e && key < x + N; ++key) ++in[key];
     }
