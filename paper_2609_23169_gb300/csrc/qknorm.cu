@@ -16,7 +16,7 @@
 // One warp takes a token; a head's 16-byte vectors lie in neighbouring lanes (8
 // to 32 of them), a lane meets the same pairs in every head, so it takes their
 // sines once a token, and its columns of w and dw stay in registers.  Where
-// there are few tokens their heads are dealt out to several warps.  What a warp
+// whole tokens do not fill the warps evenly, the forward deals out their heads.  What a warp
 // reads is asked for up to six steps ahead into shared memory (cp.async), which
 // keeps the reads of a warp in flight across tokens without registers: with
 // loads into registers, a token's at a time, the 2048 canvas took 359 us.
@@ -370,11 +370,23 @@ template <typename T, int D>
 cudaError_t fwd(const QkNormParams& p, cudaStream_t s) {
   constexpr int kHeads = 32 / (D / Vec<T>::kVals);
   const int one = (p.Hk + kHeads - 1) / kHeads, all = (p.H + kHeads - 1) / kHeads + one * (p.vo ? 2 : 1);
-  // a whole token a warp where that makes four of them a warp, else fewer steps each
-  int64_t parts = ((int64_t)p.sms * kQnFwdBlocksPerSm * kQnWarps * 4 + p.n - 1) / p.n;
-  if (parts > all) parts = all;
-  const int per = (int)((all + parts - 1) / parts);
-  parts = (all + per - 1) / per;
+  // The parts of a token with the least work for the warps that get most: a part
+  // takes as long as its steps and about kBegin more (sines, weights).  Instead of
+  // whole tokens wherever they make four a warp: 7,781 rows, 24 / 8 / 8 heads of 64
+  // in bf16 21 -> 16 us, 2,501 rows, 8 / 4 heads in fp32 14 -> 7.  (The backward
+  // gains nothing: 23,959 rows 250 -> 260.)
+  constexpr int kBegin = 4;
+  const int64_t warps = (int64_t)p.sms * kQnFwdBlocksPerSm * kQnWarps;
+  int64_t parts = 1, least = INT64_MAX;
+  int per = all;
+  for (int x = 1; x <= all && x <= 64; ++x) {
+    const int64_t steps = (all + x - 1) / x, some = (all + steps - 1) / steps;
+    const int64_t work = (p.n * some + warps - 1) / warps * (steps + kBegin);
+    if (work >= least) continue;
+    least = work;
+    parts = some;
+    per = (int)steps;
+  }
   const int64_t want = (p.n * parts + kQnWarps - 1) / kQnWarps, most = (int64_t)p.sms * kQnFwdBlocksPerSm;
   qknorm_fwd_kernel<T, D><<<(unsigned)(want < most ? want : most), kQnThreads, 0, s>>>(p, (int)parts, per);
   return cudaGetLastError();
