@@ -49,6 +49,8 @@
 // O once at the end.
 // Every wait is bounded; on expiry the kernel records UT_ERR_TIMEOUT, drains
 // its own copies and MMAs, frees TMEM and returns.
+#include <float.h>
+
 #include "common.cuh"
 #include "kernels.h"
 #include "segments.cuh"
@@ -476,7 +478,7 @@ __global__ void __launch_bounds__(Form<D>::kThreads, Form<D>::kCtas)
     while (ok && next_item(n, it, ok)) {
       const int right = it.p0 + rt + prm.w.right, left = it.p0 + rt - prm.w.left;  // last and first key of this row's
       const int right0 = right + rt_first - rt, left0 = left + rt_first - rt;      // and of the warp's first
-      float m = -1e30f, l = 0.f;
+      float m = -1e30f, l = 0.f, most = 0.f;  // most: what a row's maximum may grow to without a new reference
       Block blk(it.rg, it.j0);
 #pragma unroll 1
       for (int t = 0; t < it.blocks; ++t, ++b) {
@@ -538,17 +540,24 @@ __global__ void __launch_bounds__(Form<D>::kThreads, Form<D>::kCtas)
         if constexpr (F::kHalves == 2) {
           sm.most[b & 1][half][row] = mx;  // both halves take the same reference
           pair_sync(1 + quarter);
-          if (!(ok = !__any_sync(0xffffffffu, *abort_flag))) break;  // the partner may have given up
           mx = fmaxf(mx, sm.most[b & 1][half ^ 1][row]);
         }
         mx = fmaxf(mx, -1e30f);  // finite where a row sees no key of the block
+        // a partner that gave up leaves infinite maxima: both branches look
+        auto given_up = [&]() -> bool { return F::kHalves == 2 && __any_sync(0xffffffffu, *abort_flag); };
         if (t == 0) {
           m = mx;
+          most = fminf(m + 8.0f, FLT_MAX);  // two halves: an infinite maximum always asks for one
+          if (!(ok = !given_up())) break;
         } else {
-          const bool need = mx > m + 8.0f;
+          const bool need = mx > (F::kHalves == 2 ? most : m + 8.0f);
           if (__any_sync(0xffffffffu, need)) {  // the same rows in both halves
+            if (!(ok = !given_up())) break;
             const float alpha = need ? ex2_approx(m - mx) : 1.0f;
-            if (need) m = mx;
+            if (need) {
+              m = mx;
+              most = fminf(m + 8.0f, FLT_MAX);
+            }
             l *= alpha;
             if (!(ok = wait(&sm.pv_done, (b & 1) ^ 1))) break;  // O holds P V up to the block before
             tc_fence_after();
@@ -613,9 +622,10 @@ __global__ void __launch_bounds__(Form<D>::kThreads, Form<D>::kCtas)
       if (lane == 0) mbar_arrive(&sm.ml_full);
     }
     // A warp that gave up does not keep its partner waiting: it comes to their
-    // barrier once more, after the flag, and so the partner, which looks at the
-    // flag behind the barrier, does not come to another.
+    // barrier once more, and its infinite maxima, which are there before, send the
+    // partner behind that barrier to the abort flag, not to another barrier.
     if (F::kHalves == 2 && !ok) {
+      for (int x = 0; x < 2; ++x) sm.most[x][half][row] = INFINITY;
       __threadfence_block();
       __syncwarp();
       pair_arrive(1 + quarter);
