@@ -32,19 +32,21 @@
 // Four warps unrolled over 128 columns (2048 canvas 1,481 us instead of 1,383 at
 // that step, a third of a softmax warp's time without an instruction) and eight
 // over 32 (1,532) were slower.  The two warps of 32 rows exchange their maxima at
-// a hardware barrier: with an mbarrier, polled, 1,393 instead of 1,339.
+// a hardware barrier: with an mbarrier, polled, 1,393 instead of 1,339.  Taking
+// the exponentials with the old reference meanwhile gains nothing (1024 canvas
+// 357 us instead of 347): the two share a scheduler, which has work either way.
 // d = 128: one CTA an SM, two S buffers, Q in TMEM (S = Q K^T then reads only K
 // from shared memory).  TMEM columns S0 [0,128), S1 [128,256), O [256,384), Q
 // [384,448), the rows' maximum and sums [448,451).
 // d = 64: two CTAs an SM, whose softmaxes and products overlap; one S buffer, Q
 // in shared memory.  TMEM columns S [0,128), O [128,192), [192,194).
 // Measured (two products of 128 x 128 x d a pair of tile and block): 85,714 rows,
-// 24 heads of 128, 512 keys each side and 512 first ones 1,339 to 1,389 us, 1.2
-// PFLOP/s, tensor pipe active 61%; 23,959 rows in 13 images, 24 heads of 64, 192
-// each side, masked 157 us.  Both are bound by a softmax warp's chain of waits,
-// TMEM reads and arithmetic between the products, not by any one unit.  13 rows
-// over 40,000 keys of a cache and 512 first ones, 24 heads of 128, split: 78 us,
-// 6.4 TB/s, bound by DRAM.
+// 24 heads of 128, 512 keys each side and 512 first ones 1,320 to 1,380 us (GPUs
+// differ), 1.2 PFLOP/s, tensor pipe active 62%; 23,959 rows in 13 images, 24 heads
+// of 64, 192 each side, masked 153 us.  Both are bound by a softmax warp's chain of
+// waits, TMEM reads and arithmetic between the products, not by any one unit.  13
+// rows over 40,000 keys of a cache and 512 first ones, 24 heads of 128, split: 77
+// us, 6.5 TB/s, bound by DRAM.
 // Rounding: P to bf16 for its product (the sum l is of the unrounded values),
 // O once at the end.
 // Every wait is bounded; on expiry the kernel records UT_ERR_TIMEOUT, drains
