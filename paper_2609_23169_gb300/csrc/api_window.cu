@@ -116,7 +116,7 @@ ut_status ut_qk_norm_rope_fwd(const ut_qknorm_shape* shape, const ut_rope* rope,
   const ut_status st = qknorm_problem(shape, rope, false, &p);
   if (st != UT_OK) return st;
   const int64_t esz = shape->dtype == UT_BF16 ? 2 : 4, kw = (int64_t)p.Hk * p.d;
-  if ((v == nullptr) != (v_out == nullptr)) return UT_ERR_INVALID_ARG;
+  if (p.n > 0 && (v == nullptr) != (v_out == nullptr)) return UT_ERR_INVALID_ARG;  // (no rows have no address)
   if (v && (!row_ok(shape->v_stride, kw, esz) || !row_ok(shape->vo_stride, kw, esz))) return UT_ERR_INVALID_ARG;
   if (rows && (shape->cache_rows < 0 || shape->cache_rows > INT32_MAX / 2)) return UT_ERR_INVALID_ARG;
   if (!at16(q) || !at16(k) || !at16(v) || !at16(q_out) || !at16(k_out) || !at16(v_out)) return UT_ERR_INVALID_ARG;

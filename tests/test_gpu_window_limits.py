@@ -179,3 +179,37 @@ def test_other_devices_and_host_memory_are_refused(u, i, monkeypatch):
             f(ws=torch.empty(1 << 23, dtype=torch.uint8, device="cuda")[::2])
     f()
     torch.cuda.synchronize()
+
+
+@BOTH
+def test_block_without_tokens(u, dtype):
+    """A block over no tokens, and caches that get none: nothing is read or written, and the gradients are zero."""
+    from paper_2609_23169_gb300.window import WindowBlock, WindowCache, WindowWeights
+    H, HK, D, C = 4, 2, 64, 96
+    g = torch.Generator().manual_seed(40)
+
+    def normal(*shape):
+        return (torch.randn(*shape, generator=g) * 0.1).to(dtype).cuda()
+
+    w = WindowWeights(normal((H + 2 * HK) * D, C), torch.ones(D, device="cuda"), torch.ones(D, device="cuda"), normal(C, H * D))
+    block = WindowBlock(H, HK, D, u.rope_config(1, (D, 0, 0)), 10, 0, 2)
+    status = u.status_word()
+    x = normal(0, C)
+    y = block.forward(x, w, cu=i32([0, 0, 0]), status=status)
+    dx, dw = block.backward(x)
+    assert y.shape == dx.shape == (0, C)
+    for t, like in zip((dw.wqkv, dw.norm_q, dw.norm_k, dw.wo), (w.wqkv, w.norm_q, w.norm_k, w.wo)):
+        assert t.shape == like.shape and not to_np(t).any()
+    cache = WindowCache(3, 20, HK, D, dtype=dtype)
+    block.extend(normal(7, C), w, cache, i32([0, 3, 3, 7]), status=status)
+    before = cache.k.clone(), cache.v.clone(), cache.length.clone()
+    assert before[2].tolist() == [3, 0, 4]
+    assert block.extend(x, w, cache, i32([0, 0, 0, 0]), status=status).shape == (0, C)
+    assert all(torch.equal(a, b) for a, b in zip(before, (cache.k, cache.v, cache.length)))
+    block.extend(normal(2, C), w, cache, i32([0, 0, 2, 2]), status=status)  # one segment alone
+    u.check_status(status)
+    assert cache.length.tolist() == [3, 2, 4]
+    rows = torch.ones(60, dtype=torch.bool, device="cuda")
+    rows[20:22] = False
+    assert torch.equal(cache.k[rows], before[0][rows]) and torch.equal(cache.v[rows], before[1][rows])
+    assert to_np(cache.k[20:22]).any()
