@@ -53,6 +53,8 @@
 // its own copies and MMAs, frees TMEM and returns.
 #include <float.h>
 
+#include <algorithm>
+
 #include "common.cuh"
 #include "kernels.h"
 #include "segments.cuh"
@@ -776,26 +778,29 @@ cudaError_t launch_d(const Params& prm, const CUtensorMap* tm, cudaStream_t s) {
 
 int64_t wattn_fwd_tc_items(const WinParams& w) { return segment_slots(w.x.nq, w.x.B, kM / w.x.G) * w.x.Hk; }
 
-// Parts of the keys of a tile: the fewest whole waves of items that fill the SMs
-// (to a tenth of the best of four), none shorter than two blocks of a mean
-// segment's keys, as far as a tile sees them.
+// Parts of the keys of a tile: of one, and of as many as fill one to four waves of
+// CTAs, what takes least by this count: a wave lasts as long as an item's blocks
+// and two more, and joining parts takes as long as six.  (4 queries of 24 heads of
+// 128 over 1,024 keys each: 28 us in three parts, 24 whole; of 24 / 8 heads of 64:
+// 20 in parts, 24 whole.)  The blocks are a mean segment's, as far as a tile sees
+// them.
 int wattn_fwd_tc_splits(const WinParams& w) {
   const XattnParams& p = w.x;
   const int64_t items = wattn_fwd_tc_items(w), ctas = (int64_t)p.sms * (p.d == 64 ? Form<64>::kCtas : Form<128>::kCtas);
-  double best = 0;
-  int64_t want = 1;
-  for (int v = 1; v <= 4; ++v) {
-    const int64_t n = v * ctas / items;
-    const double use = (double)(n * items) / ((double)v * ctas);
-    if (n >= 1 && use > best + 0.1) {
-      best = use;
-      want = n;
-    }
-  }
   const int64_t near = (int64_t)w.left + w.right + w.sinks + kM / p.G, rows = p.nk / p.B;
-  const int64_t most = ((near < rows ? near : rows) + kN - 1) / kN / 2;
-  const int64_t n = want < most ? want : most;
-  return (int)(n < 1 ? 1 : n > 1024 ? 1024 : n);
+  const int64_t blocks = std::max<int64_t>(1, (std::min(near, rows) + kN - 1) / kN);
+  int64_t least = (items + ctas - 1) / ctas * (blocks + 2), want = 1;
+  for (int v = 1; v <= 4; ++v) {
+    int64_t n = std::min<int64_t>(std::min<int64_t>(v * ctas / items, blocks), 1024);
+    if (n < 2) continue;
+    const int64_t each = (blocks + n - 1) / n;
+    n = (blocks + each - 1) / each;  // the fewest parts as short
+    const int64_t time = (n * items + ctas - 1) / ctas * (each + 2) + 6;
+    if (time >= least) continue;
+    least = time;
+    want = n;
+  }
+  return (int)want;
 }
 
 cudaError_t launch_wattn_fwd_tc(const WinParams& w, cudaStream_t s) {
