@@ -285,7 +285,7 @@ UT_DEV KeyParts key_parts(const WinParams& w, const Segment& g, int64_t k0, int 
 
 // Partial dK, dV of a key tile over a part of the query tiles that see it
 template <typename T, int D>
-UT_DEV void dkdv_tile(const WinParams& w, float* sm, int64_t slot, int hk, int split) {
+UT_DEV void dkdv_tile(const WinParams& w, float* sm, const Segment& g, int hk, int split) {
   const XattnParams& p = w.x;
   float* qs = sm;
   float* dos = qs + kXs * (D + 4);
@@ -296,7 +296,6 @@ UT_DEV void dkdv_tile(const WinParams& w, float* sm, int64_t slot, int hk, int s
   float* on = dss + kXs * kXsLdP;
   float* lse = on + kXs;
   float* dsum = lse + kXs;
-  const Segment g = segment_of_slot(p.cu_k, p.B, p.nk, kXs, slot);
   if (g.tile * kXs >= g.n) return;
   int64_t q0, qn, k0, kn;
   segment_rows(p.cu_q, g.s, p.nq, q0, qn);
@@ -393,17 +392,27 @@ __global__ void __launch_bounds__(kXsThreads) wattn_join_simt_kernel(const WinPa
 }
 
 // One launch for both: n_kv blocks of dK, dV (k slots fastest, then kv heads,
-// splits), then dQ (q slots, kv heads).
+// parts; behind n_all those of the tiles with first keys that have more parts:
+// their tiles fastest, then segments, kv heads, parts), then dQ (q slots, kv heads).
 template <typename T, int D>
-__global__ void __launch_bounds__(kXsThreads, D == 64 ? 2 : 1) wattn_bwd_simt_kernel(const WinParams w, uint32_t n_kv, uint32_t kslots,
-                                                                    uint32_t qslots) {
+__global__ void __launch_bounds__(kXsThreads, D == 64 ? 2 : 1) wattn_bwd_simt_kernel(const WinParams w, uint32_t n_all, uint32_t n_kv,
+                                                                    uint32_t kslots, uint32_t qslots) {
   extern __shared__ float sm[];
   grid_wait();
   const uint32_t x = blockIdx.x;
   if (x == 0) check_lens_of(w.x, w.k_len);
   if (x < n_kv) {
-    const uint32_t y = x / kslots;
-    dkdv_tile<T, D>(w, sm, x - y * kslots, (int)(y % w.x.Hk), (int)(y / w.x.Hk));
+    const bool more = x >= n_all;
+    const uint32_t i = more ? x - n_all : x, tiles = more ? (uint32_t)w.sb * w.x.B : kslots, y = i / tiles, z = i - y * tiles;
+    Segment g;
+    if (more) {
+      g.s = (int)(z / w.sb);
+      g.tile = z - g.s * w.sb;
+      segment_rows(w.x.cu_k, g.s, w.x.nk, g.row, g.n);
+    } else {
+      g = segment_of_slot(w.x.cu_k, w.x.B, w.x.nk, kXs, z);
+    }
+    dkdv_tile<T, D>(w, sm, g, (int)(y % w.x.Hk), (int)(y / w.x.Hk) + (more ? w.parts : 0));
   } else {
     const uint32_t y = (x - n_kv) / qslots;
     dq_tile<T, D>(w, sm, x - n_kv - y * qslots, (int)y);
@@ -428,12 +437,14 @@ cudaError_t bwd(const WinParams& w, cudaStream_t s) {
   if (e != cudaSuccess) return e;
   const size_t smem = sizeof(float) * (4 * kXs * (D + 4) + 2 * kXs * kXsLdP + 3 * kXs);
   const uint32_t kslots = (uint32_t)segment_slots(p.nk, p.B, kXs), qslots = (uint32_t)segment_slots(p.nq, p.B, kXs / p.G);
-  const int64_t n_kv = p.nk > 0 ? (int64_t)kslots * p.Hk * max(w.parts, w.first_parts) : 0, n_q = p.nq > 0 ? (int64_t)qslots * p.Hk : 0;
+  const int64_t n_all = p.nk > 0 ? (int64_t)kslots * p.Hk * w.parts : 0;
+  const int64_t n_kv = n_all + (p.nk > 0 && w.first_parts > w.parts ? (int64_t)w.sb * p.B * p.Hk * (w.first_parts - w.parts) : 0);
+  const int64_t n_q = p.nq > 0 ? (int64_t)qslots * p.Hk : 0;
   if (n_kv + n_q > INT32_MAX) return cudaErrorInvalidValue;
   e = cudaFuncSetAttribute(wattn_bwd_simt_kernel<T, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
   if (e == cudaSuccess)
     e = launch_next(wattn_bwd_simt_kernel<T, D>, dim3((unsigned)(n_kv + n_q)), dim3(kXsThreads), smem, s, w,
-                    (uint32_t)n_kv, kslots, qslots);
+                    (uint32_t)n_all, (uint32_t)n_kv, kslots, qslots);
   if (e == cudaSuccess && p.nk > 0)
     e = launch_next(wattn_join_simt_kernel<D>, dim3(kslots, p.Hk, 2), dim3(kXsThreads), 0, s, w);
   return e;
