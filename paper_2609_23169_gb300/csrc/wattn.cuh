@@ -18,7 +18,8 @@ struct WinParams {
   XattnParams x;
   const int32_t* k_len;    // [B] or NULL
   int left, right, sinks;  // at most kWinMost
-  int parts, first_parts, sb;  // of the fp32 backward: parts of a key tile, key tiles of a segment with first keys
+  // of the fp32 backward: parts of a key tile, key tiles of a segment with first keys, query tiles of a part
+  int parts, first_parts, sb, run;
 };
 // Most rows, and the most that left, right and sinks need to be: positions of a
 // tile's rows (a few behind the last too) plus right or less left fit 32 bits.

@@ -12,7 +12,7 @@
 // so work grows with rows times window.  Rows and keys that do not exist, and
 // masked keys, are staged as zeros and never enter a product; inside a block a
 // row's own limits are applied to its scores.  A key tile that many tokens see
-// (first keys) is split over them, at least kXsRun tiles a part, and joined.
+// (first keys) is split over them and joined.
 // Bound by latency of the staged rows and of the shared-memory reads: 2,501 rows
 // in 3 segments, 8 / 4 heads of 64, 100 keys before, 28 behind, 7 first ones,
 // masked: forward 53 us, D 6, gradient 163 (44% of the issue slots), join 15;
@@ -45,9 +45,8 @@ struct Limits {
   }
 };
 
-constexpr int kXsRun = 6;  // query tiles of a part
 // Parts that the `tiles` query tiles of a key tile are split into
-UT_DEV int parts_of(int tiles, int most) { return max(1, min(most, (tiles + kXsRun - 1) / kXsRun)); }
+UT_DEV int parts_of(const WinParams& w, int tiles, int most) { return max(1, min(most, (tiles + w.run - 1) / w.run)); }
 
 // Key i of a tile's two ranges (of the segment), and how many there are
 UT_DEV int key_of(const WinRange& r, int i) { return i < r.first ? i : i + (r.lo - r.first); }
@@ -86,7 +85,7 @@ UT_DEV void check_lens(const WinParams& w) {
 
 // grid (q slots, kv heads, key splits)
 template <typename T, int D>
-__global__ void __launch_bounds__(kXsThreads, D == 64 ? 3 : 1) wattn_fwd_simt_kernel(const WinParams w) {
+__global__ void __launch_bounds__(kXsThreads, D == 64 ? 2 : 1) wattn_fwd_simt_kernel(const WinParams w) {
   const XattnParams& p = w.x;
   extern __shared__ float sm[];
   float* qs = sm;
@@ -277,7 +276,7 @@ UT_DEV KeyParts key_parts(const WinParams& w, const Segment& g, int64_t k0, int 
   const int64_t x0 = g.tile * kXs;
   const bool first = x0 < w.sinks && w.first_parts > w.parts;
   KeyParts k;
-  k.parts = parts_of(tiles, first ? w.first_parts : w.parts);
+  k.parts = parts_of(w, tiles, first ? w.first_parts : w.parts);
   k.step = first ? kXs : w.x.nk;
   k.at = first ? w.parts * w.x.nk + ((int64_t)g.s * w.sb + g.tile) * w.first_parts * kXs : k0 + x0;
   return k;
@@ -467,14 +466,20 @@ int wattn_simt_splits(const WinParams& w) {
   return (int)(n < 1 ? 1 : n > 1024 ? 1024 : n);
 }
 
-// The most parts of a key tile, of kXsRun query tiles at least: of those that a
+// The most parts of a key tile, of `run` query tiles at least: of those that a
 // window's tokens see, and of those with first keys, which all later tokens see
-// (unless there are many of these).
+// (unless there are many of these).  A run has six tiles, or fewer, two at least,
+// where the pairs of tiles do not make two such blocks for each that an SM holds
+// (800 rows of 4 heads of 64: 76 us in runs of six, 50 in runs of two; 8,000 rows of
+// 8: 895 and 977).
 void wattn_simt_parts(WinParams& w) {
   const XattnParams& p = w.x;
   const int64_t tpt = kXs / p.G, all = (p.nq + tpt - 1) / tpt, seen = (int64_t)w.left + w.right + kXs;
   const int64_t near = seen < p.nq ? (seen + 2 * tpt - 2) / tpt : all;
-  auto parts = [&](int64_t tiles) { return (int)std::min<int64_t>(16, std::max<int64_t>(1, (tiles + kXsRun - 1) / kXsRun)); };
+  const int64_t span = (int64_t)w.left + w.right + tpt, blocks = ((span < p.nk ? span : p.nk) + kXs - 1) / kXs;
+  const int64_t pairs = segment_slots(p.nk, p.B, kXs) * p.Hk * near + segment_slots(p.nq, p.B, (int)tpt) * p.Hk * blocks;
+  w.run = (int)std::min<int64_t>(6, std::max<int64_t>(2, pairs / ((p.d == 64 ? 4 : 2) * (int64_t)p.sms)));
+  auto parts = [&](int64_t tiles) { return (int)std::min<int64_t>(16, std::max<int64_t>(1, (tiles + w.run - 1) / w.run)); };
   const bool enough = segment_slots(p.nk, p.B, kXs) * p.Hk >= 8 * (int64_t)p.sms;
   w.parts = enough ? 1 : parts(near);
   w.sb = (int)((std::min<int64_t>(w.sinks, p.nk) + kXs - 1) / kXs);
