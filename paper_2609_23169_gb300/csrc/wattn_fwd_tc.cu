@@ -778,9 +778,9 @@ cudaError_t launch_d(const Params& prm, const CUtensorMap* tm, cudaStream_t s) {
 
 int64_t wattn_fwd_tc_items(const WinParams& w) { return segment_slots(w.x.nq, w.x.B, kM / w.x.G) * w.x.Hk; }
 
-// Parts of the keys of a tile: of one, and of as many as fill one to four waves of
-// CTAs, what takes least by this count: a wave lasts as long as an item's blocks
-// and two more, and joining parts takes as long as six.  (4 queries of 24 heads of
+// Parts of the keys of a tile: of one, of as many as fill one to four waves of CTAs,
+// and of fewer and longer ones, what takes least by this count: a wave lasts as long
+// as an item's blocks and two more, joining n parts as long as 4 + n / 2.  (4 queries of 24 heads of
 // 128 over 1,024 keys each: 28 us in three parts, 24 whole; of 24 / 8 heads of 64:
 // 20 in parts, 24 whole.)  The blocks are a mean segment's, as far as a tile sees
 // them.
@@ -789,16 +789,17 @@ int wattn_fwd_tc_splits(const WinParams& w) {
   const int64_t items = wattn_fwd_tc_items(w), ctas = (int64_t)p.sms * (p.d == 64 ? Form<64>::kCtas : Form<128>::kCtas);
   const int64_t near = (int64_t)w.left + w.right + w.sinks + kM / p.G, rows = p.nk / p.B;
   const int64_t blocks = std::max<int64_t>(1, (std::min(near, rows) + kN - 1) / kN);
-  int64_t least = (items + ctas - 1) / ctas * (blocks + 2), want = 1;
+  int64_t least = 2 * ((items + ctas - 1) / ctas * (blocks + 2)), want = 1;
   for (int v = 1; v <= 4; ++v) {
-    int64_t n = std::min<int64_t>(std::min<int64_t>(v * ctas / items, blocks), 1024);
-    if (n < 2) continue;
-    const int64_t each = (blocks + n - 1) / n;
-    n = (blocks + each - 1) / each;  // the fewest parts as short
-    const int64_t time = (n * items + ctas - 1) / ctas * (each + 2) + 6;
-    if (time >= least) continue;
-    least = time;
-    want = n;
+    const int64_t most = std::min<int64_t>(std::min<int64_t>(v * ctas / items, blocks), 1024);
+    if (most < 2) continue;
+    for (int64_t each = (blocks + most - 1) / most; each < blocks; each += (each + 1) / 2) {
+      const int64_t n = (blocks + each - 1) / each;  // the fewest parts of that length
+      const int64_t time = 2 * ((n * items + ctas - 1) / ctas * (each + 2) + 4) + n;
+      if (time >= least) continue;
+      least = time;
+      want = n;
+    }
   }
   return (int)want;
 }

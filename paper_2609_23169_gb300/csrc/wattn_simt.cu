@@ -15,10 +15,10 @@
 // (first keys) is split over them and joined.
 // Bound by latency of the staged rows and of the shared-memory reads: 2,501 rows
 // in 3 segments, 8 / 4 heads of 64, 100 keys before, 28 behind, 7 first ones,
-// masked: forward 53 us, D 6, gradient 163 (44% of the issue slots), join 15;
-// 8,000 rows, 500 before, 8 heads of 64: 28 TFLOP/s forward, the shared-memory
+// masked: forward 50 us, D 6, gradient 142 (44% of the issue slots), join 15;
+// 8,000 rows, 500 before, 8 heads of 64: 29 TFLOP/s forward, the shared-memory
 // path 70% busy.  (Eight rows a thread read a quarter less from it, but leave half
-// the warps: 291 -> 303 us.)
+// the warps: 291 -> 303 us at that step.)
 #include <math.h>
 
 #include <algorithm>
