@@ -25,7 +25,8 @@ class WindowWeights:
 
 
 class WindowCache:
-    """Keys and values of `segments` sequences, `capacity` rows each; their lengths stay on the device."""
+    """Keys and values of `segments` sequences, `capacity` rows each; their lengths stay on the device.  Calls that are
+    given no status word report in the cache's own, which ``ultratex.check_status(cache.status)`` reads."""
 
     def __init__(self, segments: int, capacity: int, kv_heads: int, head_dim: int, dtype=torch.bfloat16, device="cuda"):
         self.segments, self.capacity = segments, capacity
@@ -33,14 +34,21 @@ class WindowCache:
         self.v = torch.zeros_like(self.k)
         self.cu = torch.arange(segments + 1, dtype=torch.int32, device=device) * capacity
         self.length = torch.zeros(segments, dtype=torch.int32, device=device)
+        self.status = torch.zeros(1, dtype=torch.int32, device=device)
 
     def place(self, cu_q: torch.Tensor, n: int):
-        """Positions [n] and cache rows [n] (int32) of n new tokens in the segments of cu_q.  A token that its cache has
-        no room for gets the row behind the caches, which the operators report in the status word."""
+        """Positions [n] and cache rows [n] (int32) of n new tokens in the segments of cu_q, and the rows [segments] that
+        each segment holds in this call; the lengths grow.  A segment that has no room for all of its new tokens takes
+        none: their rows are behind the caches, which the operators report in the status word, its length stays, and in
+        this call it holds none."""
+        length = self.length + (cu_q[1:] - cu_q[:-1])
+        room = length <= self.capacity
         token = torch.arange(n, dtype=torch.int32, device=cu_q.device)
         s = torch.bucketize(token, cu_q[1:], right=True, out_int32=True).clamp_(max=self.segments - 1)
-        pos = token - cu_q[s] + self.length[s]
-        return pos, torch.where(pos < self.capacity, self.cu[s] + pos, self.k.shape[0])
+        pos = token + (self.length - cu_q[:-1])[s]
+        rows = pos + torch.where(room, self.cu[:-1], self.k.shape[0])[s]
+        torch.where(room, length, self.length, out=self.length)
+        return pos, rows, length * room
 
 
 class WindowBlock:
@@ -82,13 +90,15 @@ class WindowBlock:
                pos: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None) -> torch.Tensor:
         """New tokens x [n, C] of the cache's segments (prefix cu_q [segments + 1], on the device), a prompt or single
         tokens: their keys and values are appended, and they attend to what their caches then hold.  pos: canvas
-        positions of the rotation, by default those in the sequence.  Returns [n, C]."""
+        positions of the rotation, by default those in the sequence.  Of a segment that has no room for all of its new
+        tokens none is appended, which is reported in the status word (default: the cache's); they attend to nothing and
+        their rows of the result are those of x.  Returns [n, C]."""
+        status = cache.status if status is None else status
         q, k, v = self._project(x, w)
-        place, rows = cache.place(cu_q, x.shape[0])
+        place, rows, k_len = cache.place(cu_q, x.shape[0])
         qn, _, _ = u.ut_qk_norm_rope_fwd(q, k, self.rope, v=v, wq=w.norm_q, wk=w.norm_k, eps=self.eps,
                                          pos=place if pos is None else pos, rows=rows, k_out=cache.k, v_out=cache.v,
                                          status=status)
-        cache.length += cu_q[1:] - cu_q[:-1]
-        o, _ = u.ut_window_attn_fwd(qn, cache.k, cache.v, cu_q=cu_q, cu_k=cache.cu, k_len=cache.length, status=status,
+        o, _ = u.ut_window_attn_fwd(qn, cache.k, cache.v, cu_q=cu_q, cu_k=cache.cu, k_len=k_len, status=status,
                                     **self.window)
         return x + o.flatten(1) @ w.wo.t()
