@@ -536,7 +536,8 @@ typedef struct {
 /*   shape, q, k, v, cu_q, cu_k, key_mask, softmax_scale, o, lse   as ut_xattn_fwd
  *   k_len        [n_seg] int32 (n_seg = 1 without prefixes too), or NULL; values
  *                outside 0 .. rows of the segment are clamped and reported in
- *                dev_status
+ *                dev_status (with n_q = 0 the forward looks at none, nor at the
+ *                prefixes: it launches nothing)
  *   ws           ut_window_attn_fwd_workspace_size(shape, window) bytes (may be
  *                0: then NULL is fine), 16-byte aligned
  * The result does not depend on the run. */

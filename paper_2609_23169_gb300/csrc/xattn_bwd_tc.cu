@@ -214,6 +214,9 @@ __global__ void __launch_bounds__(kDqThreads, 1)
   __syncthreads();
   tc_fence_after();
   grid_wait();
+  if constexpr (kWin) {
+    if (blockIdx.x == 0 && p.nk == 0) check_lens_of(p, prm.k_len);  // else the dK, dV kernel does
+  }
   // all 512 columns are this CTA's, so they start at address 0
   if (sm.tmem_base != 0 && threadIdx.x == 0) {
     set_status(p.status, UT_ERR_CUDA);
