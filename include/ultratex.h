@@ -462,8 +462,11 @@ ut_status ut_group_norm_bwd(const ut_gnorm_shape* shape, const void* x, const vo
  *   y = R(pos) (x r w),   r = 1 / sqrt(mean(x^2) + eps)
  * with the rotation of ut_rope at canvas position pos (positions below
  * rope->prefix, negative ones too, are not rotated; side = 1 and axes
- * {head_dim, 0, 0} give the plain rotation by the position itself).  Angles are
- * exact to 2^-32 turns for positions up to 2^17, and to 2^-20 turns for any. */
+ * {head_dim, 0, 0} give the plain rotation by the position itself).  With
+ * theta >= 1 an angle is off by at most 2^-25 turns for positions up to 2^17, and
+ * by 2^-20 turns for any.  With theta < 1, where pairs turn f =
+ * theta^(-2j / axis) / (2 pi) times a token, position * f * 2^-46 turns come on
+ * top. */
 typedef struct {
   int64_t n_rows;         /* tokens, >= 0 */
   int32_t n_heads;        /* heads of q */

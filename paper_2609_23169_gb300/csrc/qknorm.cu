@@ -11,7 +11,9 @@
 // Positions run to 2^31, where the fp32 product coordinate * frequency is off
 // by whole radians.  So a pair's frequency is held in turns as a 64-bit
 // fraction; the product with the integer coordinate wraps at whole turns, which
-// is all that sin and cos want: its upper 32 bits are the turn, exact to 2^-32.
+// is all that sin and cos want: its upper 32 bits are the turn, to 2^-32 and the
+// error of the frequency as a double times the coordinate.  Of the 32 bits fp32
+// keeps 24: up to 2^-26 turns, as much as sin and cos round near 1.
 //
 // One warp takes a token; a head's 16-byte vectors lie in neighbouring lanes (8
 // to 32 of them), a lane meets the same pairs in every head, so it takes their
