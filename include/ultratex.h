@@ -527,9 +527,10 @@ ut_status ut_qk_norm_rope_bwd(const ut_qknorm_shape* shape, const ut_rope* rope,
  * that none of a tile of consecutive queries sees (128 / (H / H_kv) tokens in
  * bf16, half of that in fp32) never enter a product: whatever they hold has no
  * effect.  A value that is not finite in a key or value that some queries of
- * such a tile see may show in the tile's other rows too, and in the gradients
- * of the 128 keys beside it; one in a row of Q or dO in the gradients of all
- * keys that are in a block of 128 (fp32: 64) with a key that its tile sees. */
+ * such a tile see may show in O and dQ of the tile's other rows too; one in a
+ * row of Q, O or dO, and so also in a row of O that a value has shown in, in the
+ * gradients of all keys that are in a block of 128 (fp32: 64; from the segment's
+ * first key on) with a key that its tile sees. */
 typedef struct {
   int32_t left;           /* keys before p that are seen, >= 0 */
   int32_t right;          /* keys behind p that are seen, >= 0 */
