@@ -553,7 +553,12 @@ ut_status ut_window_attn_fwd(const ut_xattn_shape* shape, const ut_window* windo
 
 /* Gradient of ut_window_attn_fwd given dO, with the formulas of ut_xattn_bwd
  * over the keys that each query sees.  dk and dv are fully overwritten: rows
- * behind k_len, masked keys and keys that no query sees get zeros.
+ * behind k_len, masked keys and keys that no query sees get zeros.  In bf16 the
+ * roundings are those of ut_xattn_bwd; D is the sum of P dP where a tile's keys
+ * make one block of 128 (the first keys, or the window of all its queries), else
+ * dO . O of the rounded O.  The latter shows in dQ and dK of rows with few keys:
+ * their error is up to 2.5 times that of rounding them once at two keys a row,
+ * 1.9 at 5 and 1.6 from 17 on, where it is else 1.45.
  *   ws           ut_window_attn_bwd_workspace_size(shape, window) bytes, 16-byte
  *                aligned
  * The result does not depend on the run. */

@@ -116,6 +116,14 @@ UT_DEV void zero_tail(uint32_t base, int chunks, int first, uint32_t lane) {
 // not depend on the others.  A form of its own because its code costs long
 // segments up to 6% of a backward pass (23,959 rows and 13 segments of 257 keys at d =
 // 64: 290 -> 309 us; 85,202 and 13 of 512 at d = 128: 1,836 -> 1,840 us).
+// Windows always have it: any of them has tiles with one block where a segment
+// begins or is short, which the host does not see, and its code costs little there
+// (gradient with and without: 24,471 rows at d = 128, 512 each side and 512 first
+// keys, 1,187 and 1,188 us; 7,780 causal rows in 13 segments 150 and 148; 23,959 rows
+// at d = 64, 2,047 before, 1,182 and 1,206).  A window's tile has more blocks than its
+// rows need, so rows of few keys may keep O's rounding: dQ and dK are then off by 2.3
+// times the error of rounding them once at two keys a row, 1.8 at 5, 1.6 at 17, 1.5
+// from 32 on.
 // The issuing warp's instructions are fetched anew every block (the
 // elementwise code lies between), and it bounded the first form: 700 of them a
 // block, 3,900 cycles.  So it counts stages instead of dividing, follows one
