@@ -43,10 +43,14 @@
 // Measured (two products of 128 x 128 x d a pair of tile and block): 85,714 rows,
 // 24 heads of 128, 512 keys each side and 512 first ones 1,320 to 1,380 us (GPUs
 // differ), 1.2 PFLOP/s, tensor pipe active 62%; 23,959 rows in 13 images, 24 heads
-// of 64, 192 each side, masked 153 us.  Both are bound by a softmax warp's chain of
-// waits, TMEM reads and arithmetic between the products, not by any one unit.  13
-// rows over 40,000 keys of a cache and 512 first ones, 24 heads of 128, split: 77
-// us, 6.5 TB/s, bound by DRAM.
+// of 64, 192 each side, masked 153 us.  Both are bound by the chain of waits, TMEM
+// reads and arithmetic of a block's softmax between its products, and by what an
+// item costs beside its blocks.  In SM cycles, of a line through windows of 8 to 64
+// blocks (85,714 rows, no first keys): d = 128 3,800 an item and 1,350 a block, whose
+// products need 1,024, so that of an item of 13 blocks 18% is its own; the card's
+// power cap holds the clock at 1,720 to 1,770 MHz there.  d = 64 (two CTAs) 3,000 and
+// 1,580, products 512, at 2,070 MHz.  13 rows over 40,000 keys of a cache and 512
+// first ones, 24 heads of 128, split: 77 us, 6.5 TB/s, bound by DRAM.
 // Rounding: P to bf16 for its product (the sum l is of the unrounded values),
 // O once at the end.
 // Every wait is bounded; on expiry the kernel records UT_ERR_TIMEOUT, drains
@@ -782,8 +786,9 @@ int64_t wattn_fwd_tc_items(const WinParams& w) { return segment_slots(w.x.nq, w.
 // and of fewer and longer ones, what takes least by this count: a wave lasts as long
 // as an item's blocks and two more, joining n parts as long as 4 + n / 2.  (4 queries of 24 heads of
 // 128 over 1,024 keys each: 28 us in three parts, 24 whole; of 24 / 8 heads of 64:
-// 20 in parts, 24 whole.)  The blocks are a mean segment's, as far as a tile sees
-// them.
+// 20 in parts, 24 whole.)  The blocks are those of n_k / n_seg rows, as far as a
+// tile sees them: of caches their capacity, for how far they are filled is not
+// known on the host.
 int wattn_fwd_tc_splits(const WinParams& w) {
   const XattnParams& p = w.x;
   const int64_t items = wattn_fwd_tc_items(w), ctas = (int64_t)p.sms * (p.d == 64 ? Form<64>::kCtas : Form<128>::kCtas);

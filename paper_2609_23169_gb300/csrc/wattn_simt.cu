@@ -457,7 +457,7 @@ int64_t wattn_simt_items(const WinParams& w, bool backward) {
 }
 
 // Enough parts of the keys for two blocks an SM, none shorter than two blocks of
-// a mean segment's, as far as a tile sees them.
+// n_k / n_seg rows (of caches their capacity), as far as a tile sees them.
 int wattn_simt_splits(const WinParams& w) {
   const XattnParams& p = w.x;
   const int64_t tpt = kXs / p.G, rows = p.nk / p.B, near = (int64_t)w.left + w.right + w.sinks + tpt;
