@@ -37,18 +37,19 @@ class WindowCache:
         self.status = torch.zeros(1, dtype=torch.int32, device=device)
 
     def place(self, cu_q: torch.Tensor, n: int):
-        """Positions [n] and cache rows [n] (int32) of n new tokens in the segments of cu_q, and the rows [segments] that
-        each segment holds in this call; the lengths grow.  A segment that has no room for all of its new tokens takes
-        none: their rows are behind the caches, which the operators report in the status word, its length stays, and in
-        this call it holds none."""
+        """Positions [n] and cache rows [n] (int32) of n new tokens in the segments of cu_q.  A segment that has no room
+        for all of its new tokens takes none: their rows are behind the caches, which the operators report in the status
+        word."""
+        return self._place(cu_q, n)[:2]
+
+    def _place(self, cu_q: torch.Tensor, n: int):
+        """Positions and rows as place, the lengths [segments] with the new tokens, and which segments have room."""
         length = self.length + (cu_q[1:] - cu_q[:-1])
         room = length <= self.capacity
         token = torch.arange(n, dtype=torch.int32, device=cu_q.device)
         s = torch.bucketize(token, cu_q[1:], right=True, out_int32=True).clamp_(max=self.segments - 1)
         pos = token + (self.length - cu_q[:-1])[s]
-        rows = pos + torch.where(room, self.cu[:-1], self.k.shape[0])[s]
-        torch.where(room, length, self.length, out=self.length)
-        return pos, rows, length * room
+        return pos, pos + torch.where(room, self.cu[:-1], self.k.shape[0])[s], length, room
 
 
 class WindowBlock:
@@ -95,10 +96,11 @@ class WindowBlock:
         their rows of the result are those of x.  Returns [n, C]."""
         status = cache.status if status is None else status
         q, k, v = self._project(x, w)
-        place, rows, k_len = cache.place(cu_q, x.shape[0])
+        place, rows, length, room = cache._place(cu_q, x.shape[0])
         qn, _, _ = u.ut_qk_norm_rope_fwd(q, k, self.rope, v=v, wq=w.norm_q, wk=w.norm_k, eps=self.eps,
                                          pos=place if pos is None else pos, rows=rows, k_out=cache.k, v_out=cache.v,
                                          status=status)
-        o, _ = u.ut_window_attn_fwd(qn, cache.k, cache.v, cu_q=cu_q, cu_k=cache.cu, k_len=k_len, status=status,
+        torch.where(room, length, cache.length, out=cache.length)
+        o, _ = u.ut_window_attn_fwd(qn, cache.k, cache.v, cu_q=cu_q, cu_k=cache.cu, k_len=length * room, status=status,
                                     **self.window)
         return x + o.flatten(1) @ w.wo.t()

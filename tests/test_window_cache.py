@@ -116,3 +116,12 @@ def test_a_status_word_of_the_call_is_used(setup, device):
     assert cache.length.tolist() == [0, 0, 0]
     block.extend(tokens(4), w, cache, prefix([4, 0, 0], device))
     assert not reported(cache) and cache.length.tolist() == [4, 0, 0]
+
+
+@BOTH
+def test_places_do_not_change_the_cache(setup, device):
+    cache = setup[3](8)
+    cache.length.copy_(torch.tensor([3, 7, 0], dtype=torch.int32))
+    pos, rows = cache.place(prefix([2, 2, 1], device), 5)
+    assert pos.tolist() == [3, 4, 7, 8, 0] and cache.length.tolist() == [3, 7, 0]
+    assert rows.tolist()[:2] + rows.tolist()[4:] == [3, 4, 16] and min(rows.tolist()[2:4]) >= 24
